@@ -47,7 +47,8 @@ EXPORTS = ("gsit_im_qkv_proj", "gsit_im_attention_fwd", "gsit_im_layer_fwd", "gs
            "gsit_test_late_write", "gsit_im_layer_fwd_static",
            "gsit_stack_head_fwd", "gsit_im_layer_pair_fwd",
            "gsit_plan_rows", "gsit_pack_rows", "gsit_unpack_rows", "gsit_plan_pack_rows", "gsit_plan_pack_map_rows",
-           "gsit_im_encoder_fwd", "gsit_encoder_runs_chained", "gsit_im_layer_scatter_fwd", "gsit_layer_scatters", "gsit_attention_uses_workspace")
+           "gsit_im_encoder_fwd", "gsit_encoder_runs_chained", "gsit_im_layer_scatter_fwd", "gsit_layer_scatters", "gsit_attention_uses_workspace",
+           "gsit_rotary_fwd", "gsit_rotary_bwd", "gsit_layer_norm_fwd", "gsit_layer_norm_bwd", "gsit_layer_norm_bwd_workspace")
 STATIC_SCRATCH_BYTES = 4 << 20
 KERNEL_ATTENTION, KERNEL_LINEAR, KERNEL_LAYERNORM = 0, 1, 2
 ATTN_DEFAULT, ATTN_UNFUSED, ATTN_LEGACY, ATTN_TMEM = 0, 8, 9, 10   # gsit_kernel_choice of include/gsit_test.h
@@ -299,3 +300,28 @@ def stack_head_fwd(c, w_f, b_f, seg_len, valid_len=None, out=None):
     """c float32 [B, L, dc] (row stride free) -> float32 [B, out_features]: the last real step of each modality segment,
     concatenated, through the linear map w_f [out_features, 3*dc] (float32 or bfloat16) and bias b_f."""
     return native().stack_head_fwd(c, w_f, b_f, seg_len, valid_len, out)
+
+
+def rotary_fwd(q, k, positions, sections, seg_len, valid_len=None, base=10000.0, interleaved=False, out_q=None, out_k=None):
+    """q [B, L, H, hd], k [B, L, Hk, hd] or None (views whose rows are evenly spaced, e.g. qkv[:, :, 0] of the fused buffer), rotated by
+    positions int32 [axes, B, L] (or [axes, L]: all samples alike): the first sections[0] pairs of a head by axis 0 (time), the next by
+    axis 1 (height) and axis 2 (width).  Pair p of n = sum(sections) is features (p, n + p), or (2 p, 2 p + 1) when interleaved, and turns
+    by position * base^(-p / n); features from 2 n on are copied.  Returns (q', k') or q'; out_q may be q (in place)."""
+    return native().rotary(q, k, positions, sections, seg_len, valid_len, base, interleaved, out_q, out_k, False)
+
+
+def rotary_bwd(dq, dk, positions, sections, seg_len, valid_len=None, base=10000.0, interleaved=False, out_q=None, out_k=None):
+    """Gradients of rotary_fwd's inputs from those of its results (the rotation by the opposite angles)."""
+    return native().rotary(dq, dk, positions, sections, seg_len, valid_len, base, interleaved, out_q, out_k, True)
+
+
+def layer_norm_fwd(x, gamma=None, beta=None, seg_len=None, valid_len=None, eps=1e-5, out_dtype=None, want_stats=False, out=None):
+    """x float32 or bfloat16 [B, L, d] (row stride free) -> y [B, L, d] in out_dtype (default: of x); with want_stats (y, mean, rstd), the
+    statistics float32 [B, L] that layer_norm_bwd takes.  seg_len None: rows of one segment."""
+    return native().layer_norm_fwd(x, gamma, beta, seg_len, valid_len, eps, -1 if out_dtype is None else _dtype_code(out_dtype), want_stats, out)
+
+
+def layer_norm_bwd(dy, x, mean, rstd, gamma=None, seg_len=None, valid_len=None, residual=None, want_params=True, out=None, workspace=None):
+    """(dx, dgamma, dbeta) of layer_norm_fwd, or dx alone without want_params.  residual [B, L, d] of x's type: the gradient that reaches x
+    past the norm, added to dx (it may be `out` itself)."""
+    return native().layer_norm_bwd(dy, x, mean, rstd, gamma, seg_len, valid_len, residual, want_params, out, workspace)

@@ -13,7 +13,8 @@ CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 OBJ_DIR = PKG / "_build"
 LIB = PKG / "libgsit.so"
-SOURCES = ["gsit_api.cu", "attn_f32.cu", "attn_bf16.cu", "attn_tc.cu", "attn_tcs.cu", "linear.cu", "linear_f32.cu", "gemm_tc.cu", "fused_layer.cu", "fused_layer_tc.cu", "fused_layer_tc128.cu", "fused_rows.cu", "attn_mlp_rows.cu", "layer_static.cu", "stack_head.cu", "rows.cu"]
+SOURCES = ["gsit_api.cu", "attn_f32.cu", "attn_bf16.cu", "attn_tc.cu", "attn_tcs.cu", "linear.cu", "linear_f32.cu", "gemm_tc.cu", "fused_layer.cu", "fused_layer_tc.cu", "fused_layer_tc128.cu", "fused_rows.cu", "attn_mlp_rows.cu", "layer_static.cu", "stack_head.cu", "rows.cu",
+           "ops_api.cu", "rotary.cu", "layer_norm.cu"]
 EXT_SOURCE = CSRC / "torch_ext.cpp"
 EXT = PKG / "_native.so"
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -60,7 +61,7 @@ def build(force: bool = False, verbose: bool = False) -> Path:
             cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", str(CSRC / src), "-o", str(obj)]
             jobs.append(cmd)
     ext_obj, ext_jobs = OBJ_DIR / "torch_ext.o", []
-    if force or _stale(ext_obj, [EXT_SOURCE, Path(__file__)] + list(INCLUDE.glob("*.h"))):
+    if force or _stale(ext_obj, [EXT_SOURCE, Path(__file__)] + list(CSRC.glob("*.h")) + list(INCLUDE.glob("*.h"))):
         ext_jobs.append(_ext_commands()[0])
 
     def run(cmd):

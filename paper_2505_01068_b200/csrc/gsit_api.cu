@@ -45,8 +45,12 @@ gsit_status allowed_bits(const gsit_shape* s, uint32_t* bits) {
   }
 }
 
-// Validates the shape and fills the kernel-side geometry (without the status pointer).
-gsit_status make_geometry(const gsit_shape* s, Geometry* g) {
+}  // namespace
+
+cudaError_t device_status_word(unsigned int** p) { return status_ptr(p); }
+
+// Validates sizes, type, phase and layout and fills the kernel-side geometry (without the status pointer).
+gsit_status basic_geometry(const gsit_shape* s, Geometry* g) {
   if (s == nullptr) return GSIT_ERR_INVALID_ARG;
   if (s->batch < 1 || s->heads < 1 || s->d_model < 1 || s->d_model % s->heads != 0) return GSIT_ERR_INVALID_ARG;
   if (s->dtype != GSIT_F32 && s->dtype != GSIT_BF16) return GSIT_ERR_INVALID_ARG;
@@ -80,6 +84,15 @@ gsit_status make_geometry(const gsit_shape* s, Geometry* g) {
     if ((int64_t)s->packed_capacity > 0x7fffffffLL / 4) return GSIT_ERR_UNSUPPORTED;
     g->capacity = s->packed_capacity;
   }
+  return GSIT_OK;
+}
+
+namespace {
+
+// ... and holds it against what the layer kernels cover.
+gsit_status make_geometry(const gsit_shape* s, Geometry* g) {
+  const gsit_status st = basic_geometry(s, g);
+  if (st != GSIT_OK) return st;
   if (s->dtype == GSIT_BF16) {
     if (g->d % 16 != 0) return GSIT_ERR_UNSUPPORTED;
     if (g->hd != 8 && g->hd != 16 && g->hd != 32 && g->hd != 64) return GSIT_ERR_UNSUPPORTED;

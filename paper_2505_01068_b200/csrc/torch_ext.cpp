@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "gsit.h"
+#include "gsit_ops.h"
 
 namespace {
 
@@ -579,6 +580,9 @@ PyObject* stack_forward(PyObject* const* a) {
   return PyLong_FromLong(st);
 }
 
+// ---- training operators ----
+#include "torch_ops.h"
+
 // ---- module ----
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -617,6 +621,9 @@ PyMethodDef methods[] = {def<init, 1>("init"),
                          def<im_layer_pair_fwd, 14>("im_layer_pair_fwd"),
                          def<stack_head_fwd, 6>("stack_head_fwd"),
                          def<stack_forward, 11>("stack_forward"),
+                         def<rotary, 11>("rotary"),
+                         def<layer_norm_fwd, 9>("layer_norm_fwd"),
+                         def<layer_norm_bwd, 11>("layer_norm_bwd"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -9,7 +9,7 @@ from .binding import (CALL_ATTENTION, CALL_LAYER, CALL_QKV_PROJ, DEVFLAG_CLAMPED
                       status_string, trace_enable, trace_launches, trace_read, tune_attention, version, workspace_bytes,
                       KERNEL_ATTENTION, KERNEL_LINEAR, KERNEL_LAYERNORM, ATTN_DEFAULT, ATTN_UNFUSED, ATTN_LEGACY, ATTN_TMEM,
                       expire_wait_selftest, late_write, wait_answers,
-                      rotary_fwd, rotary_bwd, layer_norm_fwd, layer_norm_bwd)
+                      rotary_fwd, rotary_bwd, layer_norm_fwd, layer_norm_bwd, im_scored_attention_fwd, im_scored_attention_bwd)
 from .stack import GsitStack
 from .hostio import HostPipeline
 

@@ -48,7 +48,8 @@ EXPORTS = ("gsit_im_qkv_proj", "gsit_im_attention_fwd", "gsit_im_layer_fwd", "gs
            "gsit_stack_head_fwd", "gsit_im_layer_pair_fwd",
            "gsit_plan_rows", "gsit_pack_rows", "gsit_unpack_rows", "gsit_plan_pack_rows", "gsit_plan_pack_map_rows",
            "gsit_im_encoder_fwd", "gsit_encoder_runs_chained", "gsit_im_layer_scatter_fwd", "gsit_layer_scatters", "gsit_attention_uses_workspace",
-           "gsit_rotary_fwd", "gsit_rotary_bwd", "gsit_layer_norm_fwd", "gsit_layer_norm_bwd", "gsit_layer_norm_bwd_workspace")
+           "gsit_rotary_fwd", "gsit_rotary_bwd", "gsit_layer_norm_fwd", "gsit_layer_norm_bwd", "gsit_layer_norm_bwd_workspace",
+           "gsit_im_scored_attention_fwd", "gsit_im_scored_attention_bwd", "gsit_scored_attention_fwd_workspace", "gsit_scored_attention_bwd_workspace")
 STATIC_SCRATCH_BYTES = 4 << 20
 KERNEL_ATTENTION, KERNEL_LINEAR, KERNEL_LAYERNORM = 0, 1, 2
 ATTN_DEFAULT, ATTN_UNFUSED, ATTN_LEGACY, ATTN_TMEM = 0, 8, 9, 10   # gsit_kernel_choice of include/gsit_test.h
@@ -325,3 +326,22 @@ def layer_norm_bwd(dy, x, mean, rstd, gamma=None, seg_len=None, valid_len=None, 
     """(dx, dgamma, dbeta) of layer_norm_fwd, or dx alone without want_params.  residual [B, L, d] of x's type: the gradient that reaches x
     past the norm, added to dx (it may be `out` itself)."""
     return native().layer_norm_bwd(dy, x, mean, rstd, gamma, seg_len, valid_len, residual, want_params, out, workspace)
+
+
+def im_scored_attention_fwd(q, k, v, seg_len, valid_len=None, phase=PHASE_INTER_FWD, custom_mask=0, scale=0.0, softcap=0.0, slopes=None,
+                            times=None, documents=None, causal=False, prefix=None, q_len=None, want_lse=False, out=None, workspace=None):
+    """im_attention_fwd with a rule on the scores x = scale * q.k:  softcap > 0: softcap * tanh(x / softcap);  slopes float32 [H]:
+    less slopes[h] * |time_i - time_j|, times float32 [B, L] (default: the index inside the segment);  documents int32 [B, L]: only
+    keys of the query's document;  causal: only keys with time_j <= time_i, or time_j < prefix[b] (float32 [B]).
+    q [B, L, H, hd], k and v [B, L, Hk, hd] with H a multiple of Hk, row strides free.  Returns out [B, L, d] (and lse [B, H, L]).
+    q_len (three numbers): q holds only that many newest positions of each segment, [B, sum(q_len), H, hd], and so does out."""
+    return native().scored_fwd(q, k, v, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix, q_len,
+                               want_lse, out, workspace)
+
+
+def im_scored_attention_bwd(dout, q, k, v, out, lse, seg_len, valid_len=None, phase=PHASE_INTER_FWD, custom_mask=0, scale=0.0, softcap=0.0,
+                            slopes=None, times=None, documents=None, causal=False, prefix=None, grads=None, workspace=None):
+    """(dq, dk, dv) of im_scored_attention_fwd called with the same rule; out and lse are its results.  grads: three tensors (or views, e.g.
+    of one fused buffer) to write to."""
+    return native().scored_bwd(dout, q, k, v, out, lse, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal,
+                               prefix, grads, workspace)

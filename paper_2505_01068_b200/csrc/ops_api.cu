@@ -1,6 +1,7 @@
 // C ABI of the training operators (gsit_ops.h): argument checks and launches.
 #include "gsit_ops.h"
 #include "ops.cuh"
+#include "scored.cuh"
 
 namespace gsit {
 namespace {
@@ -48,6 +49,51 @@ gsit_status norm_geometry(const gsit_shape* shape, Geometry* g) {
   const gsit_status st = padded_geometry(shape, g);
   if (st != GSIT_OK) return st;
   return g->d <= MAX_NORM_WIDTH ? GSIT_OK : GSIT_ERR_UNSUPPORTED;
+}
+
+
+// Geometry and rule of an attention call, checked; the tensors are filled in by the caller.
+gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geometry* g, ScoredArgs* a) {
+  const gsit_status st = padded_geometry(shape, g);
+  if (st != GSIT_OK) return st;
+  if (r == nullptr) return GSIT_ERR_INVALID_ARG;
+  *a = {};
+  a->kv_heads = r->kv_heads == 0 ? g->heads : r->kv_heads;
+  if (a->kv_heads < 1 || g->heads % a->kv_heads != 0 || r->softcap != r->softcap) return GSIT_ERR_INVALID_ARG;
+  a->group = g->heads / a->kv_heads;
+  if (g->batch > 65535 || g->heads > 65535) return GSIT_ERR_UNSUPPORTED;
+  if (shape->dtype == GSIT_BF16 ? (g->hd != 8 && g->hd != 16 && g->hd != 32 && g->hd != 64) : g->hd > 128) return GSIT_ERR_UNSUPPORTED;
+  if (!aligned(r->slopes, 4) || !aligned(r->times, 4) || !aligned(r->documents, 4) || !aligned(r->prefix, 4)) return GSIT_ERR_INVALID_ARG;
+  a->tail = r->tail != 0;
+  for (int s = 0; s < 3; ++s) {
+    a->q_len[s] = a->tail ? r->q_len[s] : g->seg_len[s];
+    if (a->q_len[s] < 0 || a->q_len[s] > g->seg_len[s]) return GSIT_ERR_INVALID_ARG;
+    a->q_off[s] = a->Lq;
+    a->Lq += a->q_len[s];
+  }
+  if (a->Lq < 1) return GSIT_ERR_INVALID_ARG;
+  a->scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)g->hd);
+  a->softcap = r->softcap > 0.f ? r->softcap : 0.f;
+  a->inner = a->softcap > 0.f ? a->scale / a->softcap : a->scale * LOG2E;
+  a->outer = a->softcap * LOG2E;
+  a->causal = r->causal != 0;
+  a->slopes = r->slopes;
+  a->times = r->times;
+  a->documents = r->documents;
+  a->prefix = a->causal ? r->prefix : nullptr;
+  return GSIT_OK;
+}
+
+// Which kernels serve a call, and the scratch they need.
+size_t scored_fwd_scratch(const Geometry&, int, const ScoredArgs&) { return 0; }
+cudaError_t launch_scored_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) { return launch_scored_rows_fwd(g, dtype, a, st); }
+size_t scored_bwd_scratch(const Geometry& g, int, const ScoredArgs&) { return sizeof(float2) * (size_t)g.batch * g.heads * g.L; }
+cudaError_t launch_scored_bwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) { return launch_scored_rows_bwd(g, dtype, a, st); }
+
+// A matrix of `cols` columns whose rows the kernels may load: 16-byte pieces for bf16, elements for float.
+bool rows_ok(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
+  if (p == nullptr || ld < cols) return false;
+  return dtype == GSIT_BF16 ? aligned(p, 16) && ld % 8 == 0 : aligned(p, 4);
 }
 
 }  // namespace
@@ -126,6 +172,75 @@ gsit_status gsit_layer_norm_bwd(const gsit_shape* shape, int32_t y_dtype, const 
   c.dgamma = dgamma; c.dbeta = dbeta;
   c.partial = dgamma != nullptr ? static_cast<float*>(workspace) : nullptr;
   return status_of(launch_layer_norm_bwd(g, c, static_cast<cudaStream_t>(stream)));
+}
+
+size_t gsit_scored_attention_fwd_workspace(const gsit_shape* shape, const gsit_score_rule* rule) {
+  Geometry g;
+  ScoredArgs a;
+  return scored_args(shape, rule, &g, &a) == GSIT_OK ? scored_fwd_scratch(g, shape->dtype, a) : (size_t)-1;
+}
+
+gsit_status gsit_im_scored_attention_fwd(const gsit_shape* shape, const gsit_score_rule* rule, const void* q, int64_t q_row_stride,
+                                         const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride, void* out, float* lse,
+                                         void* workspace, size_t workspace_bytes, gsit_stream stream) {
+  Geometry g;
+  ScoredArgs a;
+  const gsit_status st = scored_args(shape, rule, &g, &a);
+  if (st != GSIT_OK) return st;
+  const int64_t dk = (int64_t)a.kv_heads * g.hd;
+  const int32_t t = shape->dtype;
+  if (!rows_ok(q, q_row_stride, g.d, t) || !rows_ok(k, k_row_stride, dk, t) || !rows_ok(v, v_row_stride, dk, t) || !rows_ok(out, g.d, g.d, t) ||
+      !aligned(lse, 4))
+    return GSIT_ERR_INVALID_ARG;
+  const size_t need = scored_fwd_scratch(g, t, a);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return GSIT_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return GSIT_ERR_INVALID_ARG;
+  if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
+  a.q = q; a.ldq = q_row_stride;
+  a.k = k; a.ldk = k_row_stride;
+  a.v = v; a.ldv = v_row_stride;
+  a.out = out; a.ldo = g.d;
+  a.lse = lse;
+  a.partial = static_cast<float*>(workspace);
+  return status_of(launch_scored_fwd(g, t, a, static_cast<cudaStream_t>(stream)));
+}
+
+size_t gsit_scored_attention_bwd_workspace(const gsit_shape* shape, const gsit_score_rule* rule) {
+  Geometry g;
+  ScoredArgs a;
+  return scored_args(shape, rule, &g, &a) == GSIT_OK && !a.tail ? scored_bwd_scratch(g, shape->dtype, a) : (size_t)-1;
+}
+
+gsit_status gsit_im_scored_attention_bwd(const gsit_shape* shape, const gsit_score_rule* rule, const void* q, int64_t q_row_stride,
+                                         const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride, const void* out,
+                                         int64_t out_row_stride, const float* lse, const void* dout, int64_t dout_row_stride, void* dq,
+                                         int64_t dq_row_stride, void* dk, int64_t dk_row_stride, void* dv, int64_t dv_row_stride,
+                                         void* workspace, size_t workspace_bytes, gsit_stream stream) {
+  Geometry g;
+  ScoredArgs a;
+  const gsit_status st = scored_args(shape, rule, &g, &a);
+  if (st != GSIT_OK) return st;
+  if (a.tail) return GSIT_ERR_UNSUPPORTED;
+  const int64_t cols = (int64_t)a.kv_heads * g.hd;
+  const int32_t t = shape->dtype;
+  if (!rows_ok(q, q_row_stride, g.d, t) || !rows_ok(k, k_row_stride, cols, t) || !rows_ok(v, v_row_stride, cols, t) ||
+      !rows_ok(out, out_row_stride, g.d, t) || !rows_ok(dout, dout_row_stride, g.d, t) || !rows_ok(dq, dq_row_stride, g.d, t) ||
+      !rows_ok(dk, dk_row_stride, cols, t) || !rows_ok(dv, dv_row_stride, cols, t) || lse == nullptr || !aligned(lse, 4))
+    return GSIT_ERR_INVALID_ARG;
+  if (workspace == nullptr || workspace_bytes < scored_bwd_scratch(g, t, a)) return GSIT_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return GSIT_ERR_INVALID_ARG;
+  if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
+  a.q = q; a.ldq = q_row_stride;
+  a.k = k; a.ldk = k_row_stride;
+  a.v = v; a.ldv = v_row_stride;
+  a.out = const_cast<void*>(out); a.ldo = out_row_stride;
+  a.lse = const_cast<float*>(lse);
+  a.dout = dout; a.lddo = dout_row_stride;
+  a.dq = dq; a.lddq = dq_row_stride;
+  a.dk = dk; a.lddk = dk_row_stride;
+  a.dv = dv; a.lddv = dv_row_stride;
+  a.row_stats = static_cast<float2*>(workspace);
+  return status_of(launch_scored_bwd(g, t, a, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -202,3 +202,113 @@ PyObject* layer_norm_bwd(PyObject* const* a) {
   if (!params) return THPVariable_Wrap(std::move(dx));
   return pack({dx, dgamma, dbeta});
 }
+
+// The rule of an attention call: softcap, slopes, times, documents, causal, prefix at a[0] .. a[5].
+gsit_score_rule score_rule(PyObject* const* a, int64_t B, int64_t L, int64_t H, int64_t HK) {
+  gsit_score_rule r = {};
+  r.softcap = (float)as_float(a[0]);
+  r.slopes = float_vector(opt_tensor(a[1]), H, "slopes: contiguous float32 [heads] on the device");
+  r.times = float_vector(opt_tensor(a[2]), B * L, "times: contiguous float32 [B, L] on the device");
+  const at::Tensor* docs = opt_tensor(a[3]);
+  require(docs == nullptr || (docs->is_cuda() && docs->scalar_type() == at::kInt && docs->is_contiguous() && docs->numel() == B * L),
+          "documents: contiguous int32 [B, L] on the device");
+  r.documents = static_cast<const int32_t*>(ptr(docs));
+  r.causal = as_bool(a[4]);
+  r.prefix = float_vector(opt_tensor(a[5]), B, "prefix: contiguous float32 [B] on the device");
+  r.kv_heads = (int32_t)HK;
+  return r;
+}
+
+const char* const QKV_VIEWS = "q, k, v: [B, L, H, hd] on the device, heads contiguous, rows evenly spaced";
+
+// q, k, v, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix, q_len, want_lse, out, workspace
+PyObject* scored_fwd(PyObject* const* a) {
+  const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
+  const at::Tensor *valid = opt_tensor(a[4]), *out = opt_tensor(a[16]), *ws = opt_tensor(a[17]);
+  const int64_t ldq = head_rows(q, QKV_VIEWS), ldk = head_rows(k, QKV_VIEWS), ldv = head_rows(v, QKV_VIEWS);
+  const int64_t B = q.size(0), Lq = q.size(1), H = q.size(2), hd = q.size(3), L = k.size(1), HK = k.size(2);
+  require(k.sizes() == v.sizes() && k.size(0) == B && k.size(3) == hd && k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type(),
+          "q, k and v share batch, head width and dtype, k and v their shape");
+  const gsit_shape s = make_shape(B, a[3], H * hd, H, valid, dtype_code(q), as_int(a[5]), as_int(a[6]), as_float(a[7]));
+  require_length(s, L);
+  gsit_score_rule r = score_rule(a + 8, B, L, H, HK);
+  if (a[14] != Py_None) {
+    r.tail = 1;
+    read_segments(a[14], r.q_len);
+    require((int64_t)r.q_len[0] + r.q_len[1] + r.q_len[2] == Lq, "q_len adds up to the rows of q");
+  } else {
+    require(Lq == L, "q, k and v share their length (or q_len says how many of the newest positions q holds)");
+  }
+  const bool want_lse = as_bool(a[15]);
+  at::Tensor made, lse, made_ws;
+  if (out == nullptr) made = empty({B, Lq, H * hd}, q.scalar_type(), q.device());
+  else require(out->is_cuda() && out->is_contiguous() && out->scalar_type() == q.scalar_type() && out->numel() == B * Lq * H * hd, "out: contiguous [B, L, d] of q's dtype");
+  if (want_lse) lse = empty({B, H, Lq}, at::kFloat, q.device());
+  const size_t need = gsit_scored_attention_fwd_workspace(&s, &r);
+  if (ws == nullptr && need != (size_t)-1 && need > 0) {
+    made_ws = empty({(int64_t)need}, at::kByte, q.device());
+    ws = &made_ws;
+  }
+  void* dst = out != nullptr ? out->data_ptr() : made.data_ptr();
+  float* lse_p = want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr;
+  gsit_status st;
+  {
+    NoGil n;
+    st = gsit_im_scored_attention_fwd(&s, &r, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, dst, lse_p, ptr(ws),
+                                      ws == nullptr ? 0 : (size_t)ws->nbytes(), stream());
+  }
+  check(st, "gsit_im_scored_attention_fwd");
+  if (!want_lse) return out != nullptr ? Py_NewRef(a[16]) : THPVariable_Wrap(std::move(made));
+  return pack({out != nullptr ? *out : made, lse});
+}
+
+// dout, q, k, v, out, lse, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix, grads, workspace
+PyObject* scored_bwd(PyObject* const* a) {
+  const at::Tensor &dout = tensor(a[0]), &q = tensor(a[1]), &k = tensor(a[2]), &v = tensor(a[3]), &out = tensor(a[4]), &lse = tensor(a[5]);
+  const at::Tensor *valid = opt_tensor(a[7]), *ws = opt_tensor(a[18]);
+  const int64_t ldq = head_rows(q, QKV_VIEWS), ldk = head_rows(k, QKV_VIEWS), ldv = head_rows(v, QKV_VIEWS);
+  const int64_t B = q.size(0), L = q.size(1), H = q.size(2), hd = q.size(3), HK = k.size(2);
+  require(k.sizes() == v.sizes() && k.size(0) == B && k.size(1) == L && k.size(3) == hd && k.scalar_type() == q.scalar_type() &&
+              v.scalar_type() == q.scalar_type(), "q, k and v share batch, length, head width and dtype, k and v their shape");
+  for (const at::Tensor* t : {&out, &dout})
+    require(t->scalar_type() == q.scalar_type() && t->dim() == 3 && t->size(0) == B && t->size(1) == L && t->size(2) == H * hd, "out, dout: [B, L, d] of q's dtype");
+  const int64_t ldo = feature_rows(out, "out: [B, L, d] on the device, features contiguous, rows evenly spaced");
+  const int64_t lddo = feature_rows(dout, "dout: [B, L, d] on the device, features contiguous, rows evenly spaced");
+  const float* lse_p = float_vector(&lse, B * H * L, "lse: contiguous float32 [B, H, L] on the device");
+  const gsit_shape s = make_shape(B, a[6], H * hd, H, valid, dtype_code(q), as_int(a[8]), as_int(a[9]), as_float(a[10]));
+  require_length(s, L);
+  const gsit_score_rule r = score_rule(a + 11, B, L, H, HK);
+  at::Tensor grad[3], made_ws;
+  int64_t ld[3];
+  const at::Tensor* like[3] = {&q, &k, &v};
+  PyObject* given = a[17] == Py_None ? nullptr : PySequence_Fast(a[17], "grads must be a sequence of three tensors");
+  if (a[17] != Py_None && given == nullptr) throw PyFail{};
+  struct Release {
+    PyObject* o;
+    ~Release() { Py_XDECREF(o); }
+  } release{given};
+  require(given == nullptr || PySequence_Fast_GET_SIZE(given) == 3, "grads must be a sequence of three tensors");
+  for (int i = 0; i < 3; ++i) {
+    if (given != nullptr) {
+      grad[i] = tensor(PySequence_Fast_GET_ITEM(given, i));
+      require(grad[i].sizes() == like[i]->sizes() && grad[i].scalar_type() == q.scalar_type(), "grads: shape and dtype of q, k and v");
+    } else {
+      grad[i] = empty(like[i]->sizes(), q.scalar_type(), q.device());
+    }
+    ld[i] = head_rows(grad[i], "grads: [B, L, H, hd] on the device, heads contiguous, rows evenly spaced");
+  }
+  const size_t need = gsit_scored_attention_bwd_workspace(&s, &r);
+  if (ws == nullptr && need != (size_t)-1) {
+    made_ws = empty({(int64_t)need}, at::kByte, q.device());
+    ws = &made_ws;
+  }
+  gsit_status st;
+  {
+    NoGil n;
+    st = gsit_im_scored_attention_bwd(&s, &r, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, out.data_ptr(), ldo, lse_p, dout.data_ptr(), lddo,
+                                      grad[0].data_ptr(), ld[0], grad[1].data_ptr(), ld[1], grad[2].data_ptr(), ld[2], ptr(ws),
+                                      ws == nullptr ? 0 : (size_t)ws->nbytes(), stream());
+  }
+  check(st, "gsit_im_scored_attention_bwd");
+  return pack({grad[0], grad[1], grad[2]});
+}

@@ -86,9 +86,13 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
 
 // Which kernels serve a call, and the scratch they need.
 size_t scored_fwd_scratch(const Geometry&, int, const ScoredArgs&) { return 0; }
-cudaError_t launch_scored_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) { return launch_scored_rows_fwd(g, dtype, a, st); }
+cudaError_t launch_scored_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
+  return dtype == GSIT_BF16 ? launch_scored_fwd_bf16(g, a, st) : launch_scored_rows_fwd(g, dtype, a, st);
+}
 size_t scored_bwd_scratch(const Geometry& g, int, const ScoredArgs&) { return sizeof(float2) * (size_t)g.batch * g.heads * g.L; }
-cudaError_t launch_scored_bwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) { return launch_scored_rows_bwd(g, dtype, a, st); }
+cudaError_t launch_scored_bwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
+  return dtype == GSIT_BF16 ? launch_scored_bwd_bf16(g, a, st) : launch_scored_rows_bwd(g, dtype, a, st);
+}
 
 // A matrix of `cols` columns whose rows the kernels may load: 16-byte pieces for bf16, elements for float.
 bool rows_ok(const void* p, int64_t ld, int64_t cols, int32_t dtype) {

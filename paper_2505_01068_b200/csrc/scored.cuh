@@ -260,5 +260,7 @@ __device__ __noinline__ void dkv_row(const Geometry& g, const ScoredArgs& a, int
 // ---- launch entry points ----
 cudaError_t launch_scored_rows_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st);   // scored_rows.cu
 cudaError_t launch_scored_rows_bwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st);
+cudaError_t launch_scored_fwd_bf16(const Geometry& g, const ScoredArgs& a, cudaStream_t st);              // scored_fwd.cu
+cudaError_t launch_scored_bwd_bf16(const Geometry& g, const ScoredArgs& a, cudaStream_t st);              // scored_bwd.cu
 
 }  // namespace gsit

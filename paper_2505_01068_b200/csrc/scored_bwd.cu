@@ -1,0 +1,502 @@
+// Scored attention, backward, bf16, on mma.sync (see scored_tile.cuh).
+//
+// With P = exp(x - lse), dP = dO V^T and delta = rowsum(dO o O):  dX = P o (dP - delta),  dS = dX o (derivative of the cap),
+// dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.  Two kernels, each of which owns the rows it adds up and recomputes the scores:
+// no atomics, no partial sums in memory, the same bits every time.
+//   dq    a warp owns 16 * MT query rows and walks keys (as the forward kernel does); it also writes each row's (lse in base 2, delta)
+//   dkv   a warp owns 16 * MT key rows and walks the queries of all heads that share them, products transposed: x^T = K Q^T
+// delta enters as the start of the accumulators of dP.
+#include "scored_tile.cuh"
+
+namespace gsit {
+namespace {
+
+struct Tiles {
+  int count[3];
+  int order;
+};
+__device__ __forceinline__ int find_tile(const Tiles& tiles, int tile, int& s) {
+  s = tiles.order & 3;
+  if (tile >= tiles.count[s]) {
+    tile -= tiles.count[s];
+    s = (tiles.order >> 2) & 3;
+    if (tile >= tiles.count[s]) {
+      tile -= tiles.count[s];
+      s = tiles.order >> 4;
+    }
+  }
+  return tile;
+}
+
+template <int HD, int MT, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(TILE_THREADS)
+scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * TILE_WARPS, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
+  constexpr bool TIMES = BIAS || MASK;
+  __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
+  __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
+  __shared__ int s_doc[2][MASK ? KC : 1];
+  const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31;
+  const int h = blockIdx.x % g.heads, b = blockIdx.y, hk = h / a.group;
+  int s;
+  const int tile = find_tile(tiles, blockIdx.x / g.heads, s);
+  ptx::load_params_early(g, a);
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+
+  const int q0 = tile * TQ, n_q = valid_rows(g, b, s), q_end = min(q0 + TQ, g.len(s));
+  int n_keys[3], chunks = 0, first_chunk[3];
+#pragma unroll
+  for (int r = 0; r < 3; ++r) {
+    n_keys[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
+    first_chunk[r] = chunks;
+    chunks += (n_keys[r] + KC - 1) / KC;
+  }
+  if (q0 >= n_q) chunks = 0;
+
+  // ---- the warp's rows: q, dO, statistics ----
+  const int w0 = q0 + warp * 16 * MT;
+  const int64_t row0 = (int64_t)b * g.L + g.off(s), stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s);
+  uint32_t qf[MT][(HD + 15) / 16][4], gf[MT][(HD + 15) / 16][4];
+  float own_time[MT][2], limit[MT][2], lse2[MT][2], delta[MT][2];
+  int own_doc[MT][2];
+  bool real[MT][2];
+  Range mine = NO_ROWS;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const bf16 *pq[2], *pg[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = w0 + 16 * m + 8 * i + (lane >> 2);
+      const float lse = row < min(q_end, n_q) ? a.lse[stat0 + row] : -INFINITY;
+      real[m][i] = lse != -INFINITY;   // a row without an open key has no gradient
+      pq[i] = real[m][i] ? static_cast<const bf16*>(a.q) + (row0 + row) * a.ldq + (int64_t)h * HD : nullptr;
+      pg[i] = real[m][i] ? static_cast<const bf16*>(a.dout) + (row0 + row) * a.lddo + (int64_t)h * HD : nullptr;
+      lse2[m][i] = real[m][i] ? lse * LOG2E : INFINITY;
+      own_time[m][i] = 0.f;
+      limit[m][i] = INFINITY;
+      own_doc[m][i] = 0;
+      if (TIMES && real[m][i]) {
+        own_time[m][i] = time_of(g, a, b, s, row);
+        limit[m][i] = latest_seen(a, b, own_time[m][i]);
+        own_doc[m][i] = document_of(g, a, b, s, row);
+        mine.t_lo = min(mine.t_lo, ordered(limit[m][i]));
+        mine.t_hi = max(mine.t_hi, ordered(limit[m][i]));
+        mine.d_lo = min(mine.d_lo, own_doc[m][i]);
+        mine.d_hi = max(mine.d_hi, own_doc[m][i]);
+      }
+    }
+    own_rows<HD>(pq[0], pq[1], lane, qf[m]);
+    own_rows<HD>(pg[0], pg[1], lane, gf[m]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = w0 + 16 * m + 8 * i + (lane >> 2);
+      float d = 0.f;
+      if (real[m][i]) {   // the same features of O as this lane holds of dO
+        const bf16* po = static_cast<const bf16*>(a.out) + (row0 + row) * a.ldo + (int64_t)h * HD + 2 * (lane & 3);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          float ox, oy, gx, gy;
+          unpack_bf16(*reinterpret_cast<const uint32_t*>(po + 8 * c), ox, oy);
+          unpack_bf16(gf[m][c / 2][2 * (c & 1) + i], gx, gy);
+          d += ox * gx + oy * gy;
+        }
+      }
+      d += __shfl_xor_sync(0xffffffffu, d, 1);
+      d += __shfl_xor_sync(0xffffffffu, d, 2);
+      delta[m][i] = d;
+      if (row < q_end && (lane & 3) == 0) a.row_stats[stat0 + row] = make_float2(lse2[m][i], d);
+    }
+  }
+  if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
+  const bool working = w0 < min(q_end, n_q);
+  const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
+
+  auto segment_of_chunk = [&](int c) { return c >= first_chunk[2] && n_keys[2] > 0 ? 2 : c >= first_chunk[1] && n_keys[1] > 0 ? 1 : 0; };
+  auto stage = [&](int c) {
+    const int r = segment_of_chunk(c), j0 = (c - first_chunk[r]) * KC, buf = c & 1;
+    const int rem = n_keys[r] - j0, need = min(KC, (rem + BLOCK - 1) / BLOCK * BLOCK);
+    const int64_t key0 = (int64_t)b * g.L + g.off(r) + j0;
+    const bf16 *k = static_cast<const bf16*>(a.k) + (int64_t)hk * HD, *v = static_cast<const bf16*>(a.v) + (int64_t)hk * HD;
+    const uint32_t dk = smem_u32(s_k[buf]), dv = smem_u32(s_v[buf]);
+    for (int i = tid; i < need * CH; i += TILE_THREADS) {
+      const int row = i / CH, c16 = i % CH;
+      const bool in = row < rem;
+      const int64_t at = key0 + (in ? row : 0);
+      cp16(dk + piece_at<HD>(row, c16), k + at * a.ldk + 8 * c16, in);
+      cp16(dv + piece_at<HD>(row, c16), v + at * a.ldv + 8 * c16, in);
+    }
+    cp_commit();
+    if (TIMES)
+      for (int i = tid; i < need; i += TILE_THREADS) {
+        s_time[buf][i] = i < rem ? time_of(g, a, b, r, j0 + i) : 0.f;
+        if (MASK) s_doc[buf][i] = i < rem ? document_of(g, a, b, r, j0 + i) : 0;
+      }
+  };
+
+  float dq[MT][CH][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dq[m][c][e] = 0.f;
+
+  if (chunks > 0) stage(0);
+  for (int c = 0; c < chunks; ++c) {
+    cp_wait();
+    __syncthreads();
+    if (c + 1 < chunks) stage(c + 1);
+    if (!working) continue;
+    const int r = segment_of_chunk(c), buf = c & 1, rem = min(KC, n_keys[r] - (c - first_chunk[r]) * KC);
+    const uint32_t bk = smem_u32(s_k[buf]), bv = smem_u32(s_v[buf]);
+    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
+      Openness open = ALL;
+      if (MASK) {
+        Range theirs = NO_ROWS;
+#pragma unroll
+        for (int i = 0; i < BLOCK; i += 32)
+          if (j0 + i + lane < rem) {
+            const int t = ordered(s_time[buf][j0 + i + lane]), d = s_doc[buf][j0 + i + lane];
+            theirs = {min(theirs.t_lo, t), max(theirs.t_hi, t), min(theirs.d_lo, d), max(theirs.d_hi, d)};
+          }
+        open = openness(mine, warp_range(theirs.t_lo, theirs.t_hi, theirs.d_lo, theirs.d_hi));
+        if (open == SHUT) continue;
+      }
+#pragma unroll 1
+      for (int j = j0; j < min(j0 + BLOCK, rem); j += STEP) {
+        float x[MT][NT][4], dp[MT][NT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[m][n][e] = 0.f;
+              dp[m][n][e] = -delta[m][e >> 1];
+            }
+        product_over_features<HD, MT, NT>(x, qf, bk, j, lane);
+        product_over_features<HD, MT, NT>(dp, gf, bv, j, lane);
+        uint32_t w[MT][NT][2];
+        const bool ragged = j + STEP > rem;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          float bend[CAP ? NT : 1][4];
+          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer);
+          if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
+          if (ragged || (MASK && open == SOME)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int col = j + 8 * n + 2 * (lane & 3) + e;
+                const bool in = col < rem;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                  if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
+              }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float2 y = __fadd2_rn(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(-lse2[m][i], -lse2[m][i]));
+              float2 ds = __fmul2_rn(make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]));
+              if constexpr (CAP) ds = __fmul2_rn(ds, make_float2(bend[n][2 * i], bend[n][2 * i + 1]));
+              w[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
+            }
+        }
+        product_over_partners<HD, MT, NT>(dq, w, bk, j, lane);
+      }
+    }
+  }
+
+  bool broken = false;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = w0 + 16 * m + 8 * i + (lane >> 2);
+      if (MASK && real[m][i]) {
+        broken = broken || !finite(delta[m][i]);
+#pragma unroll
+        for (int q = 0; q < CH; ++q) broken = broken || !finite(dq[m][q][2 * i]) || !finite(dq[m][q][2 * i + 1]);
+      }
+      if (row < q_end) {
+        bf16* dst = static_cast<bf16*>(a.dq) + (row0 + row) * a.lddq + (int64_t)h * HD + 2 * (lane & 3);
+#pragma unroll
+        for (int q = 0; q < CH; ++q)
+          *reinterpret_cast<uint32_t*>(dst + 8 * q) = real[m][i] ? ptx::pack_bf16(dq[m][q][2 * i] * a.scale, dq[m][q][2 * i + 1] * a.scale) : 0u;
+      }
+    }
+  if (MASK && __any_sync(0xffffffffu, broken))
+    for (int row = w0; row < min(w0 + 16 * MT, min(q_end, n_q)); ++row) dq_row<bf16, HD>(g, a, b, h, s, row);
+}
+
+template <int HD, int MT, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(TILE_THREADS)
+scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
+  constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * TILE_WARPS, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
+  constexpr bool TIMES = BIAS || MASK;
+  __shared__ __align__(128) uint8_t s_q[2][QC * HD * 2], s_g[2][QC * HD * 2];
+  __shared__ __align__(16) float2 s_stats[2][QC];
+  __shared__ __align__(16) float s_time[2][TIMES ? QC : 4], s_limit[2][MASK ? QC : 4];
+  __shared__ int s_doc[2][MASK ? QC : 1];
+  const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31;
+  const int hk = blockIdx.x % a.kv_heads, b = blockIdx.y;
+  int r;
+  const int tile = find_tile(tiles, blockIdx.x / a.kv_heads, r);
+  ptx::load_params_early(g, a);
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+
+  const int k0 = tile * TK, n_k = valid_rows(g, b, r), k_end = min(k0 + TK, g.len(r));
+  int n_rows[3], per_head = 0, first_chunk[3];
+#pragma unroll
+  for (int s = 0; s < 3; ++s) {
+    n_rows[s] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, s) : 0;
+    first_chunk[s] = per_head;
+    per_head += (n_rows[s] + QC - 1) / QC;
+  }
+  const int chunks = k0 < n_k ? per_head * a.group : 0;
+
+  const int w0 = k0 + warp * 16 * MT;
+  const int64_t key0 = (int64_t)b * g.L + g.off(r);
+  uint32_t kf[MT][(HD + 15) / 16][4], vf[MT][(HD + 15) / 16][4];
+  float own_time[MT][2];
+  int own_doc[MT][2];
+  bool real[MT][2];
+  Range mine = NO_ROWS;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const bf16 *pk[2], *pv[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = w0 + 16 * m + 8 * i + (lane >> 2);
+      real[m][i] = row < min(k_end, n_k);
+      pk[i] = real[m][i] ? static_cast<const bf16*>(a.k) + (key0 + row) * a.ldk + (int64_t)hk * HD : nullptr;
+      pv[i] = real[m][i] ? static_cast<const bf16*>(a.v) + (key0 + row) * a.ldv + (int64_t)hk * HD : nullptr;
+      own_time[m][i] = 0.f;
+      own_doc[m][i] = 0;
+      if (TIMES && real[m][i]) {
+        own_time[m][i] = time_of(g, a, b, r, row);
+        own_doc[m][i] = document_of(g, a, b, r, row);
+        mine.t_lo = min(mine.t_lo, ordered(own_time[m][i]));
+        mine.t_hi = max(mine.t_hi, ordered(own_time[m][i]));
+        mine.d_lo = min(mine.d_lo, own_doc[m][i]);
+        mine.d_hi = max(mine.d_hi, own_doc[m][i]);
+      }
+    }
+    own_rows<HD>(pk[0], pk[1], lane, kf[m]);
+    own_rows<HD>(pv[0], pv[1], lane, vf[m]);
+  }
+  if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
+  const bool working = w0 < min(k_end, n_k);
+
+  auto locate = [&](int c, int& h, int& s, int& i0) {
+    const int in_head = c % per_head;
+    h = hk * a.group + c / per_head;
+    s = in_head >= first_chunk[2] && n_rows[2] > 0 ? 2 : in_head >= first_chunk[1] && n_rows[1] > 0 ? 1 : 0;
+    i0 = (in_head - first_chunk[s]) * QC;
+  };
+  auto stage = [&](int c) {
+    int h, s, i0;
+    locate(c, h, s, i0);
+    const int buf = c & 1, rem = n_rows[s] - i0, need = min(QC, (rem + BLOCK - 1) / BLOCK * BLOCK);
+    const int64_t row0 = (int64_t)b * g.L + g.off(s) + i0, stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s) + i0;
+    const bf16 *q = static_cast<const bf16*>(a.q) + (int64_t)h * HD, *go = static_cast<const bf16*>(a.dout) + (int64_t)h * HD;
+    const uint32_t dq = smem_u32(s_q[buf]), dg = smem_u32(s_g[buf]);
+    for (int i = tid; i < need * CH; i += TILE_THREADS) {
+      const int row = i / CH, c16 = i % CH;
+      const bool in = row < rem;
+      const int64_t at = row0 + (in ? row : 0);
+      cp16(dq + piece_at<HD>(row, c16), q + at * a.ldq + 8 * c16, in);
+      cp16(dg + piece_at<HD>(row, c16), go + at * a.lddo + 8 * c16, in);
+    }
+    cp_commit();
+    for (int i = tid; i < need; i += TILE_THREADS) {
+      s_stats[buf][i] = i < rem ? a.row_stats[stat0 + i] : make_float2(INFINITY, 0.f);
+      if (TIMES) {
+        const float t = i < rem ? time_of(g, a, b, s, i0 + i) : 0.f;
+        s_time[buf][i] = t;
+        if (MASK) {
+          s_limit[buf][i] = latest_seen(a, b, t);
+          s_doc[buf][i] = i < rem ? document_of(g, a, b, s, i0 + i) : 0;
+        }
+      }
+    }
+  };
+
+  float dk[MT][CH][4], dv[MT][CH][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dk[m][c][e] = dv[m][c][e] = 0.f;
+
+  if (chunks > 0) stage(0);
+  for (int c = 0; c < chunks; ++c) {
+    cp_wait();
+    __syncthreads();
+    if (c + 1 < chunks) stage(c + 1);
+    if (!working) continue;
+    int h, s, i0;
+    locate(c, h, s, i0);
+    const int buf = c & 1, rem = min(QC, n_rows[s] - i0);
+    const uint32_t bq = smem_u32(s_q[buf]), bg = smem_u32(s_g[buf]);
+    const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
+    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
+      Openness open = ALL;
+      if (MASK) {
+        Range theirs = NO_ROWS;
+#pragma unroll
+        for (int i = 0; i < BLOCK; i += 32)
+          if (j0 + i + lane < rem) {
+            const int t = ordered(s_limit[buf][j0 + i + lane]), d = s_doc[buf][j0 + i + lane];
+            theirs = {min(theirs.t_lo, t), max(theirs.t_hi, t), min(theirs.d_lo, d), max(theirs.d_hi, d)};
+          }
+        open = openness(warp_range(theirs.t_lo, theirs.t_hi, theirs.d_lo, theirs.d_hi), mine);
+        if (open == SHUT) continue;
+      }
+#pragma unroll 1
+      for (int j = j0; j < min(j0 + BLOCK, rem); j += STEP) {
+        float x[MT][NT][4], dp[MT][NT][4];
+        float2 st[NT][2];   // (lse, delta) of this lane's two columns of every tile
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const float4 t = *reinterpret_cast<const float4*>(&s_stats[buf][j + 8 * n + 2 * (lane & 3)]);
+          st[n][0] = make_float2(t.x, t.y);
+          st[n][1] = make_float2(t.z, t.w);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[m][n][e] = 0.f;
+              dp[m][n][e] = -st[n][e & 1].y;
+            }
+        }
+        product_over_features<HD, MT, NT>(x, kf, bq, j, lane);
+        product_over_features<HD, MT, NT>(dp, vf, bg, j, lane);
+        uint32_t wp[MT][NT][2], ws[MT][NT][2];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          float bend[CAP ? NT : 1][4];
+          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer);
+          if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
+          if (MASK && open == SOME) {   // columns past the last row have an lse of +inf: no weight
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int col = j + 8 * n + 2 * (lane & 3) + e;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                  if (own_time[m][i] > s_limit[buf][col] || s_doc[buf][col] != own_doc[m][i]) x[m][n][2 * i + e] = -INFINITY;
+              }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float2 y = __fadd2_rn(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(-st[n][0].x, -st[n][1].x));
+              const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
+              float2 ds = __fmul2_rn(p, make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]));
+              if constexpr (CAP) ds = __fmul2_rn(ds, make_float2(bend[n][2 * i], bend[n][2 * i + 1]));
+              wp[m][n][i] = ptx::pack_bf16(p.x, p.y);
+              ws[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
+            }
+        }
+        product_over_partners<HD, MT, NT>(dv, wp, bg, j, lane);
+        product_over_partners<HD, MT, NT>(dk, ws, bq, j, lane);
+      }
+    }
+  }
+
+  bool broken = false;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = w0 + 16 * m + 8 * i + (lane >> 2);
+      if (row < k_end) {
+        bf16* pk = static_cast<bf16*>(a.dk) + (key0 + row) * a.lddk + (int64_t)hk * HD + 2 * (lane & 3);
+        bf16* pv = static_cast<bf16*>(a.dv) + (key0 + row) * a.lddv + (int64_t)hk * HD + 2 * (lane & 3);
+#pragma unroll
+        for (int q = 0; q < CH; ++q) {
+          const float2 k2 = make_float2(dk[m][q][2 * i] * a.scale, dk[m][q][2 * i + 1] * a.scale), v2 = make_float2(dv[m][q][2 * i], dv[m][q][2 * i + 1]);
+          if (MASK && real[m][i]) broken = broken || !finite(k2.x) || !finite(k2.y) || !finite(v2.x) || !finite(v2.y);
+          *reinterpret_cast<uint32_t*>(pk + 8 * q) = real[m][i] ? ptx::pack_bf16(k2.x, k2.y) : 0u;
+          *reinterpret_cast<uint32_t*>(pv + 8 * q) = real[m][i] ? ptx::pack_bf16(v2.x, v2.y) : 0u;
+        }
+      }
+    }
+  if (MASK && __any_sync(0xffffffffu, broken))
+    for (int row = w0; row < min(w0 + 16 * MT, min(k_end, n_k)); ++row) dkv_row<bf16, HD>(g, a, b, hk, r, row);
+}
+
+// Which of the two kernels, by a type.
+struct Dq {
+  template <int HD, int MT, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, MT, CAP, BIAS, MASK>;
+};
+struct Dkv {
+  template <int HD, int MT, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dkv_kernel<HD, MT, CAP, BIAS, MASK>;
+};
+
+template <typename K, int HD, int MT, bool CAP, bool BIAS>
+cudaError_t launch_masked(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
+  return rule_masks(a) ? launch_overlapped(K::template kernel<HD, MT, CAP, BIAS, true>, grid, dim3(TILE_THREADS), 0, st, g, a, t)
+                       : launch_overlapped(K::template kernel<HD, MT, CAP, BIAS, false>, grid, dim3(TILE_THREADS), 0, st, g, a, t);
+}
+template <typename K, int HD, int MT>
+cudaError_t launch_rule(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
+  const bool cap = a.softcap > 0.f, bias = a.slopes != nullptr;
+  return cap ? (bias ? launch_masked<K, HD, MT, true, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, true, false>(g, a, t, grid, st))
+             : (bias ? launch_masked<K, HD, MT, false, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, false, false>(g, a, t, grid, st));
+}
+// Blocks the keys of segment r are open to, transposed: bit (3 r + s).
+uint32_t transposed(uint32_t allowed) {
+  uint32_t t = 0;
+  for (int s = 0; s < 3; ++s)
+    for (int r = 0; r < 3; ++r)
+      if ((allowed >> (3 * s + r)) & 1u) t |= 1u << (3 * r + s);
+  return t;
+}
+template <typename K, int HD>
+cudaError_t launch_pass(const Geometry& g, const ScoredArgs& a, int heads, uint32_t walks, int n_sm, cudaStream_t st) {
+  Tiles t = {};
+  t.order = segment_order(g, walks);
+  auto tiles = [&](int rows) {
+    int64_t n = 0;
+    for (int s = 0; s < 3; ++s) n += t.count[s] = (g.len(s) + rows - 1) / rows;
+    return n * heads;
+  };
+  constexpr int MT = HD <= 16 ? 2 : 1;   // wider heads: two row tiles' accumulators do not fit the registers
+  const bool tall = MT == 2 && tiles(128) * g.batch >= 6LL * n_sm;
+  const int64_t n = tiles(tall ? 128 : 64);
+  if (n > 0x7fffffffLL) return cudaErrorNotSupported;
+  const dim3 grid((unsigned)n, g.batch);
+  return tall ? launch_rule<K, HD, MT>(g, a, t, grid, st) : launch_rule<K, HD, 1>(g, a, t, grid, st);
+}
+template <int HD>
+cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
+  int n_sm = 0;
+  cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
+  if (e != cudaSuccess) return e;
+  e = launch_pass<Dq, HD>(g, a, g.heads, g.allowed, n_sm, st);
+  return e != cudaSuccess ? e : launch_pass<Dkv, HD>(g, a, a.kv_heads, transposed(g.allowed), n_sm, st);
+}
+
+}  // namespace
+
+cudaError_t launch_scored_bwd_bf16(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
+  switch (g.hd) {
+    case 8: return launch_width<8>(g, a, st);
+    case 16: return launch_width<16>(g, a, st);
+    case 32: return launch_width<32>(g, a, st);
+    case 64: return launch_width<64>(g, a, st);
+    default: return cudaErrorNotSupported;
+  }
+}
+
+}  // namespace gsit

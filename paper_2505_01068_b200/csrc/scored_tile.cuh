@@ -1,0 +1,221 @@
+// Tiles of the scored attention on mma.sync: staging of partner rows, fragments, the score function on accumulators.
+//
+// A warp owns 16 * MT rows (queries in the forward pass and for dq, keys for dk and dv) and walks the other side, its partners, in
+// chunks that the CTA stages into shared memory (cp.async, two buffers) and in blocks of 64 rows inside a chunk.  A block is skipped
+// when none of its pairs can be open -- its documents or moments lie apart from the warp's -- and takes the element-wise mask only
+// when some are and some are not.
+#pragma once
+#include "scored.cuh"
+
+namespace gsit {
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int TILE_WARPS = 4, TILE_THREADS = 32 * TILE_WARPS;
+constexpr int BLOCK = 64;                                            // partners that are classified together
+template <int HD> constexpr int CHUNK_ROWS = HD == 8 ? 256 : HD == 64 ? 64 : 128;
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0));
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {   // zeros where the row is not real
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
+// Byte offset of 16-byte piece c of row r in a staged tile: pieces are permuted within the 128 bytes that eight rows' worth of
+// ldmatrix addresses must spread over.
+template <int HD> __device__ __forceinline__ uint32_t piece_at(int r, int c) {
+  constexpr int CH = HD / 8;
+  return (uint32_t)(r * HD * 2 + ((CH == 1 ? 0 : c ^ ((r / (8 / CH)) % CH)) << 4));
+}
+
+// Fragments of 16 staged rows (or 32 rows of 8 features) as the B operand.
+//   rows_as_n: the product runs over features; f[ks] = {n 0-7 k lo, n 0-7 k hi, n 8-15 k lo, n 8-15 k hi} of feature step ks
+//   rows_as_k: the product runs over the rows; f[c2] = {c lo: rows 0-7, rows 8-15, c hi: the same} of feature pieces 2 c2, 2 c2 + 1
+template <int HD> __device__ __forceinline__ void frag_rows_as_n(uint32_t base, int row0, int lane, uint32_t (&f)[HD / 16][4]) {
+#pragma unroll
+  for (int ks = 0; ks < HD / 16; ++ks) ldsm4(base + piece_at<HD>(row0 + ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)), f[ks]);
+}
+template <int HD> __device__ __forceinline__ void frag_rows_as_k(uint32_t base, int row0, int lane, uint32_t (&f)[HD / 16][4]) {
+#pragma unroll
+  for (int c = 0; c < HD / 16; ++c) ldsm4_t(base + piece_at<HD>(row0 + (((lane >> 3) & 1) << 3) + (lane & 7), 2 * c + (lane >> 4)), f[c]);
+}
+// 16 rows of 8 features, read through one x4 load of 32 rows: f[i] = rows 8 i .. 8 i + 7, as n (plain) or as k (transposed).
+__device__ __forceinline__ void frag8(uint32_t base, int row0, int lane, uint32_t (&f)[4]) { ldsm4(base + (row0 + lane) * 16, f); }
+__device__ __forceinline__ void frag8_t(uint32_t base, int row0, int lane, uint32_t (&f)[4]) { ldsm4_t(base + (row0 + lane) * 16, f); }
+
+// A operand of a warp's own rows, straight from memory: rows row0 + lane / 4 and + 8, zeros where not real.  Head width 8 uses words 0, 1.
+template <int HD> __device__ __forceinline__ void own_rows(const bf16* p0, const bf16* p1, int lane, uint32_t (&f)[(HD + 15) / 16][4]) {
+#pragma unroll
+  for (int ks = 0; ks < (HD + 15) / 16; ++ks) {
+    const int c = 16 * ks + 2 * (lane & 3);
+    f[ks][0] = p0 != nullptr ? *reinterpret_cast<const uint32_t*>(p0 + c) : 0u;
+    f[ks][1] = p1 != nullptr ? *reinterpret_cast<const uint32_t*>(p1 + c) : 0u;
+    f[ks][2] = HD > 8 && p0 != nullptr ? *reinterpret_cast<const uint32_t*>(p0 + c + 8) : 0u;
+    f[ks][3] = HD > 8 && p1 != nullptr ? *reinterpret_cast<const uint32_t*>(p1 + c + 8) : 0u;
+  }
+}
+
+// c[mt][nt] += own rows x partner rows, over features, for NT tiles of 8 partners from row0 on.
+template <int HD, int MT, int NT>
+__device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], const uint32_t (&own)[MT][(HD + 15) / 16][4], uint32_t base, int row0, int lane) {
+  if constexpr (HD == 8) {
+#pragma unroll
+    for (int q = 0; q < NT / 4; ++q) {
+      uint32_t f[4];
+      frag8(base, row0 + 32 * q, lane, f);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma8(c[m][4 * q + i], own[m][0][0], own[m][0][1], f[i]);
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < NT / 2; ++p) {
+      uint32_t f[HD / 16][4];
+      frag_rows_as_n<HD>(base, row0 + 16 * p, lane, f);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int ks = 0; ks < HD / 16; ++ks) {
+          mma16(c[m][2 * p], own[m][ks], f[ks][0], f[ks][1]);
+          mma16(c[m][2 * p + 1], own[m][ks], f[ks][2], f[ks][3]);
+        }
+    }
+  }
+}
+// o[mt][feature tile] += weights [own rows x partners] x partner rows, over NT tiles of 8 partners from row0 on; weights as packed
+// accumulators w[mt][nt] = {row g, row g + 8}.
+template <int HD, int MT, int NT>
+__device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4], const uint32_t (&w)[MT][NT][2], uint32_t base, int row0, int lane) {
+  if constexpr (HD == 8) {
+#pragma unroll
+    for (int q = 0; q < NT / 4; ++q) {
+      uint32_t f[4];
+      frag8_t(base, row0 + 32 * q, lane, f);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int nt = 4 * q + 2 * i;
+          const uint32_t a[4] = {w[m][nt][0], w[m][nt][1], w[m][nt + 1][0], w[m][nt + 1][1]};
+          mma16(o[m][0], a, f[2 * i], f[2 * i + 1]);
+        }
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < NT / 2; ++p) {
+      uint32_t f[HD / 16][4];
+      frag_rows_as_k<HD>(base, row0 + 16 * p, lane, f);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const uint32_t a[4] = {w[m][2 * p][0], w[m][2 * p][1], w[m][2 * p + 1][0], w[m][2 * p + 1][1]};
+#pragma unroll
+        for (int c = 0; c < HD / 16; ++c) {
+          mma16(o[m][2 * c], a, f[c][0], f[c][1]);
+          mma16(o[m][2 * c + 1], a, f[c][2], f[c][3]);
+        }
+      }
+    }
+  }
+}
+
+// Dots -> scores in base 2 (in place), and where wanted the derivative of the cap.  One range check for the whole warp decides between
+// the polynomial alone and the form for any argument.
+template <bool CAP, bool BEND, int NT>
+__device__ __forceinline__ void bend_scores(float (&x)[NT][4], float (&bend)[BEND ? NT : 1][4], float inner, float outer) {
+  if constexpr (!CAP) {
+    const float2 f = make_float2(inner, inner);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const float2 y = __fmul2_rn(make_float2(x[n][i], x[n][i + 1]), f);
+        x[n][i] = y.x;
+        x[n][i + 1] = y.y;
+      }
+  } else {
+    float top = 0.f;
+    const float2 f = make_float2(inner, inner), o = make_float2(outer, outer);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const float2 y = __fmul2_rn(make_float2(x[n][i], x[n][i + 1]), f);
+        top = ptx::fmax3(top, fabsf(y.x), fabsf(y.y));
+        x[n][i] = y.x;
+        x[n][i + 1] = y.y;
+      }
+    const bool far = __any_sync(0xffffffffu, top > TANH_RANGE);
+    auto all = [&](auto tanh2) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const float2 t = tanh2(make_float2(x[n][i], x[n][i + 1]));
+          if constexpr (BEND) {
+            const float2 b = __ffma2_rn(make_float2(-t.x, -t.y), t, make_float2(1.f, 1.f));
+            bend[n][i] = b.x;
+            bend[n][i + 1] = b.y;
+          }
+          const float2 y = __fmul2_rn(t, o);
+          x[n][i] = y.x;
+          x[n][i + 1] = y.y;
+        }
+    };
+    if (far) all([](float2 y) { return tanh_any2(y); });
+    else all([](float2 y) { return tanh_near2(y); });
+  }
+}
+// x -= slope2 * |own time - partner time|.  own[2]: rows g, g + 8; partner times in shared memory from column 0 on.
+template <int NT> __device__ __forceinline__ void add_bias(float (&x)[NT][4], const float (&own)[2], const float* times, int lane, float slope2) {
+  const float2 f = make_float2(-slope2, -slope2);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const float2 t = *reinterpret_cast<const float2*>(times + 8 * n + 2 * (lane & 3));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 y = __ffma2_rn(make_float2(fabsf(own[i] - t.x), fabsf(own[i] - t.y)), f, make_float2(x[n][2 * i], x[n][2 * i + 1]));
+      x[n][2 * i] = y.x;
+      x[n][2 * i + 1] = y.y;
+    }
+  }
+}
+
+// ---- which pairs of a block are open ----
+__device__ __forceinline__ int ordered(float f) {   // floats as integers of the same order
+  const int i = __float_as_int(f);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+struct Range {   // over real rows: moments (as ordered integers) and documents
+  int t_lo, t_hi, d_lo, d_hi;
+};
+__device__ __forceinline__ Range warp_range(int t_lo, int t_hi, int d_lo, int d_hi) {
+  return {__reduce_min_sync(0xffffffffu, t_lo), __reduce_max_sync(0xffffffffu, t_hi), __reduce_min_sync(0xffffffffu, d_lo), __reduce_max_sync(0xffffffffu, d_hi)};
+}
+constexpr Range NO_ROWS = {0x7fffffff, (int)0x80000000, 0x7fffffff, (int)0x80000000};
+// Queries have their latest moment seen in t, keys their own moment.
+enum Openness { SHUT, SOME, ALL };
+__device__ __forceinline__ Openness openness(const Range& queries, const Range& keys) {
+  if (queries.d_hi < keys.d_lo || keys.d_hi < queries.d_lo || keys.t_lo > queries.t_hi) return SHUT;
+  return queries.d_lo == queries.d_hi && keys.d_lo == keys.d_hi && keys.t_hi <= queries.t_lo ? ALL : SOME;
+}
+
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+
+}  // namespace
+}  // namespace gsit

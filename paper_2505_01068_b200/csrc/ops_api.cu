@@ -76,6 +76,7 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
   a->softcap = r->softcap > 0.f ? r->softcap : 0.f;
   a->inner = a->softcap > 0.f ? a->scale / a->softcap : a->scale * LOG2E;
   a->outer = a->softcap * LOG2E;
+  a->bend_scale = a->softcap > 0.f ? 1.0f / (a->outer * a->outer) : 0.f;
   a->causal = r->causal != 0;
   a->slopes = r->slopes;
   a->times = r->times;
@@ -87,11 +88,13 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
 // Which kernels serve a call, and the scratch they need.
 size_t scored_fwd_scratch(const Geometry&, int, const ScoredArgs&) { return 0; }
 cudaError_t launch_scored_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
-  return dtype == GSIT_BF16 ? launch_scored_fwd_bf16(g, a, st) : launch_scored_rows_fwd(g, dtype, a, st);
+  if (dtype == GSIT_BF16) return launch_scored_fwd_bf16(g, a, st);
+  return g.hd <= 64 ? launch_scored_fwd_f32(g, a, st) : launch_scored_rows_fwd(g, a, st);
 }
 size_t scored_bwd_scratch(const Geometry& g, int, const ScoredArgs&) { return sizeof(float2) * (size_t)g.batch * g.heads * g.L; }
 cudaError_t launch_scored_bwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
-  return dtype == GSIT_BF16 ? launch_scored_bwd_bf16(g, a, st) : launch_scored_rows_bwd(g, dtype, a, st);
+  if (dtype == GSIT_BF16) return launch_scored_bwd_bf16(g, a, st);
+  return g.hd <= 64 ? launch_scored_bwd_f32(g, a, st) : launch_scored_rows_bwd(g, a, st);
 }
 
 // A matrix of `cols` columns whose rows the kernels may load: 16-byte pieces for bf16, elements for float.

@@ -11,27 +11,10 @@
 namespace gsit {
 namespace {
 
-struct Tiles {
-  int count[3];
-  int order;
-};
-__device__ __forceinline__ int find_tile(const Tiles& tiles, int tile, int& s) {
-  s = tiles.order & 3;
-  if (tile >= tiles.count[s]) {
-    tile -= tiles.count[s];
-    s = (tiles.order >> 2) & 3;
-    if (tile >= tiles.count[s]) {
-      tile -= tiles.count[s];
-      s = tiles.order >> 4;
-    }
-  }
-  return tile;
-}
-
-template <int HD, int MT, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(TILE_THREADS)
+template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(32 * W)
 scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * TILE_WARPS, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
@@ -119,7 +102,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
     const int64_t key0 = (int64_t)b * g.L + g.off(r) + j0;
     const bf16 *k = static_cast<const bf16*>(a.k) + (int64_t)hk * HD, *v = static_cast<const bf16*>(a.v) + (int64_t)hk * HD;
     const uint32_t dk = smem_u32(s_k[buf]), dv = smem_u32(s_v[buf]);
-    for (int i = tid; i < need * CH; i += TILE_THREADS) {
+    for (int i = tid; i < need * CH; i += 32 * W) {
       const int row = i / CH, c16 = i % CH;
       const bool in = row < rem;
       const int64_t at = key0 + (in ? row : 0);
@@ -128,7 +111,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
     }
     cp_commit();
     if (TIMES)
-      for (int i = tid; i < need; i += TILE_THREADS) {
+      for (int i = tid; i < need; i += 32 * W) {
         s_time[buf][i] = i < rem ? time_of(g, a, b, r, j0 + i) : 0.f;
         if (MASK) s_doc[buf][i] = i < rem ? document_of(g, a, b, r, j0 + i) : 0;
       }
@@ -182,7 +165,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           float bend[CAP ? NT : 1][4];
-          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer);
+          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer, a.bend_scale);
           if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
           if (ragged || (MASK && open == SOME)) {
 #pragma unroll
@@ -230,13 +213,13 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       }
     }
   if (MASK && __any_sync(0xffffffffu, broken))
-    for (int row = w0; row < min(w0 + 16 * MT, min(q_end, n_q)); ++row) dq_row<bf16, HD>(g, a, b, h, s, row);
+    for (int row = w0; row < min(w0 + 16 * MT, min(q_end, n_q)); ++row) dq_row<bf16>(g, a, b, h, s, row);
 }
 
-template <int HD, int MT, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(TILE_THREADS)
+template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(32 * W)
 scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * TILE_WARPS, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
+  constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * W, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_q[2][QC * HD * 2], s_g[2][QC * HD * 2];
   __shared__ __align__(16) float2 s_stats[2][QC];
@@ -306,7 +289,7 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     const int64_t row0 = (int64_t)b * g.L + g.off(s) + i0, stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s) + i0;
     const bf16 *q = static_cast<const bf16*>(a.q) + (int64_t)h * HD, *go = static_cast<const bf16*>(a.dout) + (int64_t)h * HD;
     const uint32_t dq = smem_u32(s_q[buf]), dg = smem_u32(s_g[buf]);
-    for (int i = tid; i < need * CH; i += TILE_THREADS) {
+    for (int i = tid; i < need * CH; i += 32 * W) {
       const int row = i / CH, c16 = i % CH;
       const bool in = row < rem;
       const int64_t at = row0 + (in ? row : 0);
@@ -314,7 +297,7 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       cp16(dg + piece_at<HD>(row, c16), go + at * a.lddo + 8 * c16, in);
     }
     cp_commit();
-    for (int i = tid; i < need; i += TILE_THREADS) {
+    for (int i = tid; i < need; i += 32 * W) {
       s_stats[buf][i] = i < rem ? a.row_stats[stat0 + i] : make_float2(INFINITY, 0.f);
       if (TIMES) {
         const float t = i < rem ? time_of(g, a, b, s, i0 + i) : 0.f;
@@ -382,7 +365,7 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           float bend[CAP ? NT : 1][4];
-          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer);
+          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer, a.bend_scale);
           if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
           if (MASK && open == SOME) {   // columns past the last row have an lse of +inf: no weight
 #pragma unroll
@@ -432,51 +415,38 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       }
     }
   if (MASK && __any_sync(0xffffffffu, broken))
-    for (int row = w0; row < min(w0 + 16 * MT, min(k_end, n_k)); ++row) dkv_row<bf16, HD>(g, a, b, hk, r, row);
+    for (int row = w0; row < min(w0 + 16 * MT, min(k_end, n_k)); ++row) dkv_row<bf16>(g, a, b, hk, r, row);
 }
 
 // Which of the two kernels, by a type.
 struct Dq {
-  template <int HD, int MT, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, MT, CAP, BIAS, MASK>;
+  template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, MT, W, CAP, BIAS, MASK>;
 };
 struct Dkv {
-  template <int HD, int MT, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dkv_kernel<HD, MT, CAP, BIAS, MASK>;
+  template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dkv_kernel<HD, MT, W, CAP, BIAS, MASK>;
 };
 
-template <typename K, int HD, int MT, bool CAP, bool BIAS>
+template <typename K, int HD, int MT, int W, bool CAP, bool BIAS>
 cudaError_t launch_masked(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
-  return rule_masks(a) ? launch_overlapped(K::template kernel<HD, MT, CAP, BIAS, true>, grid, dim3(TILE_THREADS), 0, st, g, a, t)
-                       : launch_overlapped(K::template kernel<HD, MT, CAP, BIAS, false>, grid, dim3(TILE_THREADS), 0, st, g, a, t);
+  return rule_masks(a) ? launch_overlapped(K::template kernel<HD, MT, W, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
+                       : launch_overlapped(K::template kernel<HD, MT, W, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
 }
-template <typename K, int HD, int MT>
+template <typename K, int HD, int MT, int W>
 cudaError_t launch_rule(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
   const bool cap = a.softcap > 0.f, bias = a.slopes != nullptr;
-  return cap ? (bias ? launch_masked<K, HD, MT, true, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, true, false>(g, a, t, grid, st))
-             : (bias ? launch_masked<K, HD, MT, false, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, false, false>(g, a, t, grid, st));
-}
-// Blocks the keys of segment r are open to, transposed: bit (3 r + s).
-uint32_t transposed(uint32_t allowed) {
-  uint32_t t = 0;
-  for (int s = 0; s < 3; ++s)
-    for (int r = 0; r < 3; ++r)
-      if ((allowed >> (3 * s + r)) & 1u) t |= 1u << (3 * r + s);
-  return t;
+  return cap ? (bias ? launch_masked<K, HD, MT, W, true, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, W, true, false>(g, a, t, grid, st))
+             : (bias ? launch_masked<K, HD, MT, W, false, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, W, false, false>(g, a, t, grid, st));
 }
 template <typename K, int HD>
 cudaError_t launch_pass(const Geometry& g, const ScoredArgs& a, int heads, uint32_t walks, int n_sm, cudaStream_t st) {
   Tiles t = {};
   t.order = segment_order(g, walks);
-  auto tiles = [&](int rows) {
-    int64_t n = 0;
-    for (int s = 0; s < 3; ++s) n += t.count[s] = (g.len(s) + rows - 1) / rows;
-    return n * heads;
-  };
-  constexpr int MT = HD <= 16 ? 2 : 1;   // wider heads: two row tiles' accumulators do not fit the registers
-  const bool tall = MT == 2 && tiles(128) * g.batch >= 6LL * n_sm;
-  const int64_t n = tiles(tall ? 128 : 64);
+  constexpr int MT = 1;
+  const bool tall = make_tiles(&t, g.seg_len, 128) * heads * g.batch >= 6LL * n_sm;
+  const int64_t n = make_tiles(&t, g.seg_len, tall ? 128 : 64) * heads;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n, g.batch);
-  return tall ? launch_rule<K, HD, MT>(g, a, t, grid, st) : launch_rule<K, HD, 1>(g, a, t, grid, st);
+  return tall ? launch_rule<K, HD, MT, 8 / MT>(g, a, t, grid, st) : launch_rule<K, HD, 1, 4>(g, a, t, grid, st);
 }
 template <int HD>
 cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {

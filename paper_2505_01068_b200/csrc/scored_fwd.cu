@@ -4,30 +4,18 @@
 namespace gsit {
 namespace {
 
-struct Tiles {
-  int count[3];      // query tiles per segment
-  int order;         // segments, longest walks first, two bits each
-};
-
-template <int HD, int MT, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(TILE_THREADS)
+template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(32 * W)
 scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * TILE_WARPS, NT = HD <= 16 ? 8 : 4, STEP = 8 * NT;
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 8 : 4, STEP = 8 * NT;
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
   __shared__ int s_doc[2][MASK ? KC : 1];
   const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31;
   const int h = blockIdx.x % g.heads, b = blockIdx.y, hk = h / a.group;
-  int tile = blockIdx.x / g.heads, s = tiles.order & 3;
-  if (tile >= tiles.count[s]) {
-    tile -= tiles.count[s];
-    s = (tiles.order >> 2) & 3;
-    if (tile >= tiles.count[s]) {
-      tile -= tiles.count[s];
-      s = tiles.order >> 4;
-    }
-  }
+  int s;
+  const int tile = find_tile(tiles, blockIdx.x / g.heads, s);
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
@@ -87,7 +75,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     const int64_t row0 = (int64_t)b * g.L + g.off(r) + j0;
     const bf16 *k = static_cast<const bf16*>(a.k) + (int64_t)hk * HD, *v = static_cast<const bf16*>(a.v) + (int64_t)hk * HD;
     const uint32_t dk = smem_u32(s_k[buf]), dv = smem_u32(s_v[buf]);
-    for (int i = tid; i < need * CH; i += TILE_THREADS) {
+    for (int i = tid; i < need * CH; i += 32 * W) {
       const int row = i / CH, c16 = i % CH;
       const bool in = row < rem;
       const int64_t at = row0 + (in ? row : 0);
@@ -96,7 +84,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     }
     cp_commit();
     if (TIMES)
-      for (int i = tid; i < need; i += TILE_THREADS) {
+      for (int i = tid; i < need; i += 32 * W) {
         s_time[buf][i] = i < rem ? time_of(g, a, b, r, j0 + i) : 0.f;
         if (MASK) s_doc[buf][i] = i < rem ? document_of(g, a, b, r, j0 + i) : 0;
       }
@@ -152,7 +140,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
         const bool ragged = j + STEP > rem;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          bend_scores<CAP, false, NT>(x[m], unused, a.inner, a.outer);
+          bend_scores<CAP, false, NT>(x[m], unused, a.inner, a.outer, a.bend_scale);
           if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
           if (ragged || (MASK && open == SOME)) {
 #pragma unroll
@@ -228,19 +216,19 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     }
   // zero times NaN or Inf of a closed key: those rows once more, pair by pair
   if (MASK && __any_sync(0xffffffffu, broken))
-    for (int row = max(w0, rows.lo); row < min(w0 + 16 * MT, min(q_end, rows.hi)); ++row) attend_row<bf16, HD>(g, a, b, h, s, row);
+    for (int row = max(w0, rows.lo); row < min(w0 + 16 * MT, min(q_end, rows.hi)); ++row) attend_row<bf16>(g, a, b, h, s, row);
 }
 
-template <int HD, int MT, bool CAP, bool BIAS>
+template <int HD, int MT, int W, bool CAP, bool BIAS>
 cudaError_t launch_masked(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
-  return rule_masks(a) ? launch_overlapped(scored_fwd_kernel<HD, MT, CAP, BIAS, true>, grid, dim3(TILE_THREADS), 0, st, g, a, t)
-                       : launch_overlapped(scored_fwd_kernel<HD, MT, CAP, BIAS, false>, grid, dim3(TILE_THREADS), 0, st, g, a, t);
+  return rule_masks(a) ? launch_overlapped(scored_fwd_kernel<HD, MT, W, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
+                       : launch_overlapped(scored_fwd_kernel<HD, MT, W, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
 }
-template <int HD, int MT>
+template <int HD, int MT, int W>
 cudaError_t launch_rule(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
   const bool cap = a.softcap > 0.f, bias = a.slopes != nullptr;
-  return cap ? (bias ? launch_masked<HD, MT, true, true>(g, a, t, grid, st) : launch_masked<HD, MT, true, false>(g, a, t, grid, st))
-             : (bias ? launch_masked<HD, MT, false, true>(g, a, t, grid, st) : launch_masked<HD, MT, false, false>(g, a, t, grid, st));
+  return cap ? (bias ? launch_masked<HD, MT, W, true, true>(g, a, t, grid, st) : launch_masked<HD, MT, W, true, false>(g, a, t, grid, st))
+             : (bias ? launch_masked<HD, MT, W, false, true>(g, a, t, grid, st) : launch_masked<HD, MT, W, false, false>(g, a, t, grid, st));
 }
 template <int HD>
 cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
@@ -249,17 +237,13 @@ cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st
   if (e != cudaSuccess) return e;
   Tiles t = {};
   t.order = segment_order(g, g.allowed);
-  auto tiles = [&](int rows) {
-    int64_t n = 0;
-    for (int s = 0; s < 3; ++s) n += t.count[s] = (a.q_len[s] + rows - 1) / rows;
-    return n * g.heads;
-  };
   // 128 rows a CTA where that still makes several CTAs per SM, 64 below
-  const bool tall = tiles(128) * g.batch >= 6LL * n_sm;
-  const int64_t n = tiles(tall ? 128 : 64);
+  const bool tall = make_tiles(&t, a.q_len, 128) * g.heads * g.batch >= 6LL * n_sm;
+  const int64_t n = make_tiles(&t, a.q_len, tall ? 128 : 64) * g.heads;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n, g.batch);
-  return tall ? launch_rule<HD, 2>(g, a, t, grid, st) : launch_rule<HD, 1>(g, a, t, grid, st);
+  constexpr int MT = HD == 64 ? 2 : 1;
+  return tall ? launch_rule<HD, MT, 8 / MT>(g, a, t, grid, st) : launch_rule<HD, 1, 4>(g, a, t, grid, st);
 }
 
 }  // namespace

@@ -12,7 +12,6 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 
-constexpr int TILE_WARPS = 4, TILE_THREADS = 32 * TILE_WARPS;
 constexpr int BLOCK = 64;                                            // partners that are classified together
 template <int HD> constexpr int CHUNK_ROWS = HD == 8 ? 256 : HD == 64 ? 64 : 128;
 
@@ -134,10 +133,10 @@ __device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4],
   }
 }
 
-// Dots -> scores in base 2 (in place), and where wanted the derivative of the cap.  One range check for the whole warp decides between
+// Dots -> scores in base 2 (in place), and where wanted the derivative of the cap (bend_scale = 1 / outer^2).  One range check for the whole warp decides between
 // the polynomial alone and the form for any argument.
 template <bool CAP, bool BEND, int NT>
-__device__ __forceinline__ void bend_scores(float (&x)[NT][4], float (&bend)[BEND ? NT : 1][4], float inner, float outer) {
+__device__ __forceinline__ void bend_scores(float (&x)[NT][4], float (&bend)[BEND ? NT : 1][4], float inner, float outer, float bend_scale) {
   if constexpr (!CAP) {
     const float2 f = make_float2(inner, inner);
 #pragma unroll
@@ -161,24 +160,29 @@ __device__ __forceinline__ void bend_scores(float (&x)[NT][4], float (&bend)[BEN
         x[n][i + 1] = y.y;
       }
     const bool far = __any_sync(0xffffffffu, top > TANH_RANGE);
-    auto all = [&](auto tanh2) {
+    auto each = [&](auto score) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
-          const float2 t = tanh2(make_float2(x[n][i], x[n][i + 1]));
-          if constexpr (BEND) {
-            const float2 b = __ffma2_rn(make_float2(-t.x, -t.y), t, make_float2(1.f, 1.f));
-            bend[n][i] = b.x;
-            bend[n][i + 1] = b.y;
-          }
-          const float2 y = __fmul2_rn(t, o);
+          const float2 y = score(make_float2(x[n][i], x[n][i + 1]));
           x[n][i] = y.x;
           x[n][i + 1] = y.y;
         }
     };
-    if (far) all([](float2 y) { return tanh_any2(y); });
-    else all([](float2 y) { return tanh_near2(y); });
+    if (far) each([&](float2 y) { return __fmul2_rn(tanh_any2(y), o); });
+    else each([&](float2 y) { return tanh_near2(y, outer); });
+    if constexpr (BEND) {   // 1 - tanh^2
+      const float2 f2 = make_float2(-bend_scale, -bend_scale), one = make_float2(1.f, 1.f);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const float2 y = make_float2(x[n][i], x[n][i + 1]), b = __ffma2_rn(__fmul2_rn(y, f2), y, one);
+          bend[n][i] = b.x;
+          bend[n][i + 1] = b.y;
+        }
+    }
   }
 }
 // x -= slope2 * |own time - partner time|.  own[2]: rows g, g + 8; partner times in shared memory from column 0 on.
@@ -189,7 +193,8 @@ template <int NT> __device__ __forceinline__ void add_bias(float (&x)[NT][4], co
     const float2 t = *reinterpret_cast<const float2*>(times + 8 * n + 2 * (lane & 3));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float2 y = __ffma2_rn(make_float2(fabsf(own[i] - t.x), fabsf(own[i] - t.y)), f, make_float2(x[n][2 * i], x[n][2 * i + 1]));
+      const float2 d = __fadd2_rn(t, make_float2(-own[i], -own[i]));
+      const float2 y = __ffma2_rn(make_float2(fabsf(d.x), fabsf(d.y)), f, make_float2(x[n][2 * i], x[n][2 * i + 1]));
       x[n][2 * i] = y.x;
       x[n][2 * i + 1] = y.y;
     }

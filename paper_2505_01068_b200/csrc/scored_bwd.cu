@@ -11,10 +11,30 @@
 namespace gsit {
 namespace {
 
+// Registers: 24 warps an SM for narrow heads, 16 and 12 for wide ones, whose accumulators are larger.
+template <int HD, int W> constexpr int MIN_CTAS = (HD <= 16 ? 24 : HD == 32 ? 16 : 12) / W;
+
+// x, dp (starting at -delta) -> the weights p (where wanted) and ds = p (dP - delta) bend, packed.  lse: in base 2, of the lane's rows or columns.
+template <bool CAP, bool BIAS, bool PACK_P, int N, typename Lse>
+__device__ __forceinline__ void weigh(float (&x)[N][4], float (&dp)[N][4], uint32_t (&wp)[PACK_P ? N : 1][2], uint32_t (&ws)[N][2], float inner, Lse lse) {
+  constexpr bool RAW = !CAP && !BIAS;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 l = lse(n, i), y = make_float2(x[n][2 * i], x[n][2 * i + 1]);
+      const float2 z = RAW ? __ffma2_rn(y, make_float2(inner, inner), make_float2(-l.x, -l.y)) : __fadd2_rn(y, make_float2(-l.x, -l.y));
+      const float2 p = make_float2(ptx::ex2(z.x), ptx::ex2(z.y));
+      const float2 ds = __fmul2_rn(p, make_float2(dp[n][2 * i], dp[n][2 * i + 1]));
+      if constexpr (PACK_P) wp[n][i] = ptx::pack_bf16(p.x, p.y);
+      ws[n][i] = ptx::pack_bf16(ds.x, ds.y);
+    }
+}
+
 template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W)
+__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W>)
 scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
@@ -28,18 +48,29 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   ptx::grid_dep_launch();
 
   const int q0 = tile * TQ, n_q = valid_rows(g, b, s), q_end = min(q0 + TQ, g.len(s));
-  int n_keys[3], chunks = 0, first_chunk[3];
+  Walk next = {};
 #pragma unroll
-  for (int r = 0; r < 3; ++r) {
-    n_keys[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
-    first_chunk[r] = chunks;
-    chunks += (n_keys[r] + KC - 1) / KC;
-  }
-  if (q0 >= n_q) chunks = 0;
+  for (int r = 0; r < 3; ++r) next.n[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
+  if (q0 >= n_q) next.seg = 3;
+  next.settle();
+
+  const int64_t sample0 = (int64_t)b * g.L;
+  const bf16* const k0 = static_cast<const bf16*>(a.k) + sample0 * a.ldk + (int64_t)hk * HD;
+  const bf16* const v0 = static_cast<const bf16*>(a.v) + sample0 * a.ldv + (int64_t)hk * HD;
+  auto stage = [&](const Walk& w, int buf) {
+    const int row0 = g.off(w.seg) + w.pos, rem = w.left();
+    stage_pair<HD, KC, W>(smem_u32(s_k[buf]), smem_u32(s_v[buf]), k0 + (int64_t)row0 * a.ldk, a.ldk, v0 + (int64_t)row0 * a.ldv, a.ldv, rem, tid);
+    if (TIMES)
+      for (int i = tid; i < min(KC, (rem + BLOCK - 1) / BLOCK * BLOCK); i += 32 * W) {
+        s_time[buf][i] = i >= rem ? 0.f : a.times != nullptr ? a.times[sample0 + row0 + i] : (float)(w.pos + i);
+        if (MASK) s_doc[buf][i] = i < rem && a.documents != nullptr ? a.documents[sample0 + row0 + i] : 0;
+      }
+  };
+  if (!next.over()) stage(next, 0);
 
   // ---- the warp's rows: q, dO, statistics ----
   const int w0 = q0 + warp * 16 * MT;
-  const int64_t row0 = (int64_t)b * g.L + g.off(s), stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s);
+  const int64_t row0 = sample0 + g.off(s), stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s);
   uint32_t qf[MT][(HD + 15) / 16][4], gf[MT][(HD + 15) / 16][4];
   float own_time[MT][2], limit[MT][2], lse2[MT][2], delta[MT][2];
   int own_doc[MT][2];
@@ -59,14 +90,11 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       own_time[m][i] = 0.f;
       limit[m][i] = INFINITY;
       own_doc[m][i] = 0;
-      if (TIMES && real[m][i]) {
-        own_time[m][i] = time_of(g, a, b, s, row);
+      if (TIMES && real[m][i]) own_time[m][i] = time_of(g, a, b, s, row);
+      if (MASK && real[m][i]) {
         limit[m][i] = latest_seen(a, b, own_time[m][i]);
         own_doc[m][i] = document_of(g, a, b, s, row);
-        mine.t_lo = min(mine.t_lo, ordered(limit[m][i]));
-        mine.t_hi = max(mine.t_hi, ordered(limit[m][i]));
-        mine.d_lo = min(mine.d_lo, own_doc[m][i]);
-        mine.d_hi = max(mine.d_hi, own_doc[m][i]);
+        mine = {min(mine.t_lo, ordered(limit[m][i])), max(mine.t_hi, ordered(limit[m][i])), min(mine.d_lo, own_doc[m][i]), max(mine.d_hi, own_doc[m][i])};
       }
     }
     own_rows<HD>(pq[0], pq[1], lane, qf[m]);
@@ -95,28 +123,6 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   const bool working = w0 < min(q_end, n_q);
   const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
 
-  auto segment_of_chunk = [&](int c) { return c >= first_chunk[2] && n_keys[2] > 0 ? 2 : c >= first_chunk[1] && n_keys[1] > 0 ? 1 : 0; };
-  auto stage = [&](int c) {
-    const int r = segment_of_chunk(c), j0 = (c - first_chunk[r]) * KC, buf = c & 1;
-    const int rem = n_keys[r] - j0, need = min(KC, (rem + BLOCK - 1) / BLOCK * BLOCK);
-    const int64_t key0 = (int64_t)b * g.L + g.off(r) + j0;
-    const bf16 *k = static_cast<const bf16*>(a.k) + (int64_t)hk * HD, *v = static_cast<const bf16*>(a.v) + (int64_t)hk * HD;
-    const uint32_t dk = smem_u32(s_k[buf]), dv = smem_u32(s_v[buf]);
-    for (int i = tid; i < need * CH; i += 32 * W) {
-      const int row = i / CH, c16 = i % CH;
-      const bool in = row < rem;
-      const int64_t at = key0 + (in ? row : 0);
-      cp16(dk + piece_at<HD>(row, c16), k + at * a.ldk + 8 * c16, in);
-      cp16(dv + piece_at<HD>(row, c16), v + at * a.ldv + 8 * c16, in);
-    }
-    cp_commit();
-    if (TIMES)
-      for (int i = tid; i < need; i += 32 * W) {
-        s_time[buf][i] = i < rem ? time_of(g, a, b, r, j0 + i) : 0.f;
-        if (MASK) s_doc[buf][i] = i < rem ? document_of(g, a, b, r, j0 + i) : 0;
-      }
-  };
-
   float dq[MT][CH][4];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -125,72 +131,66 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
 #pragma unroll
       for (int e = 0; e < 4; ++e) dq[m][c][e] = 0.f;
 
-  if (chunks > 0) stage(0);
-  for (int c = 0; c < chunks; ++c) {
-    cp_wait();
-    __syncthreads();
-    if (c + 1 < chunks) stage(c + 1);
-    if (!working) continue;
-    const int r = segment_of_chunk(c), buf = c & 1, rem = min(KC, n_keys[r] - (c - first_chunk[r]) * KC);
-    const uint32_t bk = smem_u32(s_k[buf]), bv = smem_u32(s_v[buf]);
-    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
-      Openness open = ALL;
-      if (MASK) {
-        Range theirs = NO_ROWS;
+  auto step = [&](auto some_tag, int buf, int j, int rem) {
+    constexpr bool SOME_SHUT = decltype(some_tag)::value;
+    float x[MT][NT][4], dp[MT][NT][4];
 #pragma unroll
-        for (int i = 0; i < BLOCK; i += 32)
-          if (j0 + i + lane < rem) {
-            const int t = ordered(s_time[buf][j0 + i + lane]), d = s_doc[buf][j0 + i + lane];
-            theirs = {min(theirs.t_lo, t), max(theirs.t_hi, t), min(theirs.d_lo, d), max(theirs.d_hi, d)};
-          }
-        open = openness(mine, warp_range(theirs.t_lo, theirs.t_hi, theirs.d_lo, theirs.d_hi));
-        if (open == SHUT) continue;
-      }
-#pragma unroll 1
-      for (int j = j0; j < min(j0 + BLOCK, rem); j += STEP) {
-        float x[MT][NT][4], dp[MT][NT][4];
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              x[m][n][e] = 0.f;
-              dp[m][n][e] = -delta[m][e >> 1];
-            }
-        product_over_features<HD, MT, NT>(x, qf, bk, j, lane);
-        product_over_features<HD, MT, NT>(dp, gf, bv, j, lane);
-        uint32_t w[MT][NT][2];
-        const bool ragged = j + STEP > rem;
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          float bend[CAP ? NT : 1][4];
-          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer, a.bend_scale);
-          if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
-          if (ragged || (MASK && open == SOME)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int col = j + 8 * n + 2 * (lane & 3) + e;
-                const bool in = col < rem;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                  if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
-              }
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float2 y = __fadd2_rn(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(-lse2[m][i], -lse2[m][i]));
-              float2 ds = __fmul2_rn(make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]));
-              if constexpr (CAP) ds = __fmul2_rn(ds, make_float2(bend[n][2 * i], bend[n][2 * i + 1]));
-              w[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
-            }
+        for (int e = 0; e < 4; ++e) {
+          x[m][n][e] = 0.f;
+          dp[m][n][e] = -delta[m][e >> 1];
         }
-        product_over_partners<HD, MT, NT>(dq, w, bk, j, lane);
+    product_over_features<HD, MT, NT>(x, qf, smem_u32(s_k[buf]), j, lane);
+    product_over_features<HD, MT, NT>(dp, gf, smem_u32(s_v[buf]), j, lane);
+    uint32_t w[MT][NT][2], unused[1][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      if constexpr (CAP) {
+        cap_scores<NT>(x[m], a.inner, a.outer);
+        times_bend<NT>(dp[m], x[m], a.bend_scale);
+      } else if constexpr (BIAS) {
+        scale_scores<NT>(x[m], a.inner);
       }
+      if constexpr (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
+      if constexpr (SOME_SHUT) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int col = j + 8 * n + 2 * (lane & 3) + e;
+            const bool in = col < rem;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
+          }
+      }
+      weigh<CAP, BIAS, false, NT>(x[m], dp[m], unused, w[m], a.inner, [&](int, int i) { return make_float2(lse2[m][i], lse2[m][i]); });
+    }
+    product_over_partners<HD, MT, NT>(dq, w, smem_u32(s_k[buf]), j, lane);
+  };
+
+  for (int buf = 0; !next.over(); buf ^= 1) {
+    const int rem = min(KC, next.left());
+    cp_wait();
+    __syncthreads();   // the chunk is there, and nobody reads the other buffer any more
+    next.pos += KC;
+    next.settle();
+    if (!next.over()) stage(next, buf ^ 1);
+    if (!working) continue;
+#pragma unroll 1
+    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
+      const Openness open = MASK ? openness(mine, block_range(s_time[buf], s_doc[buf], j0, rem, lane)) : ALL;
+      if (MASK && open == SHUT) continue;
+      const int end = min(j0 + BLOCK, rem);
+      int j = j0;
+      if (open == ALL)
+#pragma unroll 1
+        for (; j + 8 * NT <= end; j += 8 * NT) step(IntTag<0>{}, buf, j, rem);
+#pragma unroll 1
+      for (; j < end; j += 8 * NT) step(IntTag<1>{}, buf, j, rem);
     }
   }
 
@@ -217,9 +217,9 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
 }
 
 template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W)
+__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W>)
 scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * W, NT = HD <= 16 ? 4 : 2, STEP = 8 * NT;
+  constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_q[2][QC * HD * 2], s_g[2][QC * HD * 2];
   __shared__ __align__(16) float2 s_stats[2][QC];
@@ -234,17 +234,37 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   ptx::grid_dep_launch();
 
   const int k0 = tile * TK, n_k = valid_rows(g, b, r), k_end = min(k0 + TK, g.len(r));
-  int n_rows[3], per_head = 0, first_chunk[3];
+  Walk next = {};
 #pragma unroll
-  for (int s = 0; s < 3; ++s) {
-    n_rows[s] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, s) : 0;
-    first_chunk[s] = per_head;
-    per_head += (n_rows[s] + QC - 1) / QC;
-  }
-  const int chunks = k0 < n_k ? per_head * a.group : 0;
+  for (int s = 0; s < 3; ++s) next.n[s] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, s) : 0;
+  if (k0 >= n_k) next.seg = 3;
+  next.settle();
+  const Walk first = next;
+  int h = hk * a.group;   // the head whose queries come next
+  const int last_head = h + a.group - 1;
+
+  const int64_t sample0 = (int64_t)b * g.L;
+  auto stage = [&](const Walk& w, int head, int buf) {
+    const int row0 = g.off(w.seg) + w.pos, rem = w.left();
+    stage_pair<HD, QC, W>(smem_u32(s_q[buf]), smem_u32(s_g[buf]), static_cast<const bf16*>(a.q) + (sample0 + row0) * a.ldq + (int64_t)head * HD, a.ldq,
+                          static_cast<const bf16*>(a.dout) + (sample0 + row0) * a.lddo + (int64_t)head * HD, a.lddo, rem, tid);
+    const float2* stats = a.row_stats + ((int64_t)b * g.heads + head) * g.L + row0;
+    for (int i = tid; i < min(QC, (rem + BLOCK - 1) / BLOCK * BLOCK); i += 32 * W) {
+      s_stats[buf][i] = i < rem ? stats[i] : make_float2(INFINITY, 0.f);   // no weight for rows past the last
+      if (TIMES) {
+        const float t = i >= rem ? 0.f : a.times != nullptr ? a.times[sample0 + row0 + i] : (float)(w.pos + i);
+        s_time[buf][i] = t;
+        if (MASK) {
+          s_limit[buf][i] = latest_seen(a, b, t);
+          s_doc[buf][i] = i < rem && a.documents != nullptr ? a.documents[sample0 + row0 + i] : 0;
+        }
+      }
+    }
+  };
+  if (!next.over()) stage(next, h, 0);
 
   const int w0 = k0 + warp * 16 * MT;
-  const int64_t key0 = (int64_t)b * g.L + g.off(r);
+  const int64_t key0 = sample0 + g.off(r);
   uint32_t kf[MT][(HD + 15) / 16][4], vf[MT][(HD + 15) / 16][4];
   float own_time[MT][2];
   int own_doc[MT][2];
@@ -261,13 +281,10 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       pv[i] = real[m][i] ? static_cast<const bf16*>(a.v) + (key0 + row) * a.ldv + (int64_t)hk * HD : nullptr;
       own_time[m][i] = 0.f;
       own_doc[m][i] = 0;
-      if (TIMES && real[m][i]) {
-        own_time[m][i] = time_of(g, a, b, r, row);
+      if (TIMES && real[m][i]) own_time[m][i] = time_of(g, a, b, r, row);
+      if (MASK && real[m][i]) {
         own_doc[m][i] = document_of(g, a, b, r, row);
-        mine.t_lo = min(mine.t_lo, ordered(own_time[m][i]));
-        mine.t_hi = max(mine.t_hi, ordered(own_time[m][i]));
-        mine.d_lo = min(mine.d_lo, own_doc[m][i]);
-        mine.d_hi = max(mine.d_hi, own_doc[m][i]);
+        mine = {min(mine.t_lo, ordered(own_time[m][i])), max(mine.t_hi, ordered(own_time[m][i])), min(mine.d_lo, own_doc[m][i]), max(mine.d_hi, own_doc[m][i])};
       }
     }
     own_rows<HD>(pk[0], pk[1], lane, kf[m]);
@@ -275,40 +292,6 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   }
   if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
   const bool working = w0 < min(k_end, n_k);
-
-  auto locate = [&](int c, int& h, int& s, int& i0) {
-    const int in_head = c % per_head;
-    h = hk * a.group + c / per_head;
-    s = in_head >= first_chunk[2] && n_rows[2] > 0 ? 2 : in_head >= first_chunk[1] && n_rows[1] > 0 ? 1 : 0;
-    i0 = (in_head - first_chunk[s]) * QC;
-  };
-  auto stage = [&](int c) {
-    int h, s, i0;
-    locate(c, h, s, i0);
-    const int buf = c & 1, rem = n_rows[s] - i0, need = min(QC, (rem + BLOCK - 1) / BLOCK * BLOCK);
-    const int64_t row0 = (int64_t)b * g.L + g.off(s) + i0, stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s) + i0;
-    const bf16 *q = static_cast<const bf16*>(a.q) + (int64_t)h * HD, *go = static_cast<const bf16*>(a.dout) + (int64_t)h * HD;
-    const uint32_t dq = smem_u32(s_q[buf]), dg = smem_u32(s_g[buf]);
-    for (int i = tid; i < need * CH; i += 32 * W) {
-      const int row = i / CH, c16 = i % CH;
-      const bool in = row < rem;
-      const int64_t at = row0 + (in ? row : 0);
-      cp16(dq + piece_at<HD>(row, c16), q + at * a.ldq + 8 * c16, in);
-      cp16(dg + piece_at<HD>(row, c16), go + at * a.lddo + 8 * c16, in);
-    }
-    cp_commit();
-    for (int i = tid; i < need; i += 32 * W) {
-      s_stats[buf][i] = i < rem ? a.row_stats[stat0 + i] : make_float2(INFINITY, 0.f);
-      if (TIMES) {
-        const float t = i < rem ? time_of(g, a, b, s, i0 + i) : 0.f;
-        s_time[buf][i] = t;
-        if (MASK) {
-          s_limit[buf][i] = latest_seen(a, b, t);
-          s_doc[buf][i] = i < rem ? document_of(g, a, b, s, i0 + i) : 0;
-        }
-      }
-    }
-  };
 
   float dk[MT][CH][4], dv[MT][CH][4];
 #pragma unroll
@@ -318,80 +301,74 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 #pragma unroll
       for (int e = 0; e < 4; ++e) dk[m][c][e] = dv[m][c][e] = 0.f;
 
-  if (chunks > 0) stage(0);
-  for (int c = 0; c < chunks; ++c) {
+  auto step = [&](auto some_tag, int buf, int j, float slope2) {
+    constexpr bool SOME_SHUT = decltype(some_tag)::value;
+    float x[MT][NT][4], dp[MT][NT][4];
+    float2 lse2[NT];   // of this lane's two columns of every tile
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float4 t = *reinterpret_cast<const float4*>(&s_stats[buf][j + 8 * n + 2 * (lane & 3)]);
+      lse2[n] = make_float2(t.x, t.z);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[m][n][e] = 0.f;
+          dp[m][n][e] = (e & 1) ? -t.w : -t.y;
+        }
+    }
+    product_over_features<HD, MT, NT>(x, kf, smem_u32(s_q[buf]), j, lane);
+    product_over_features<HD, MT, NT>(dp, vf, smem_u32(s_g[buf]), j, lane);
+    uint32_t wp[MT][NT][2], ws[MT][NT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      if constexpr (CAP) {
+        cap_scores<NT>(x[m], a.inner, a.outer);
+        times_bend<NT>(dp[m], x[m], a.bend_scale);
+      } else if constexpr (BIAS) {
+        scale_scores<NT>(x[m], a.inner);
+      }
+      if constexpr (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
+      if constexpr (SOME_SHUT) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int col = j + 8 * n + 2 * (lane & 3) + e;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (own_time[m][i] > s_limit[buf][col] || s_doc[buf][col] != own_doc[m][i]) x[m][n][2 * i + e] = -INFINITY;
+          }
+      }
+      weigh<CAP, BIAS, true, NT>(x[m], dp[m], wp[m], ws[m], a.inner, [&](int n, int) { return lse2[n]; });
+    }
+    product_over_partners<HD, MT, NT>(dv, wp, smem_u32(s_g[buf]), j, lane);
+    product_over_partners<HD, MT, NT>(dk, ws, smem_u32(s_q[buf]), j, lane);
+  };
+
+  for (int buf = 0; !next.over(); buf ^= 1) {
+    const int rem = min(QC, next.left()), head = h;
     cp_wait();
     __syncthreads();
-    if (c + 1 < chunks) stage(c + 1);
+    next.pos += QC;
+    next.settle();
+    if (next.over() && h < last_head) {
+      next = first;
+      ++h;
+    }
+    if (!next.over()) stage(next, h, buf ^ 1);
     if (!working) continue;
-    int h, s, i0;
-    locate(c, h, s, i0);
-    const int buf = c & 1, rem = min(QC, n_rows[s] - i0);
-    const uint32_t bq = smem_u32(s_q[buf]), bg = smem_u32(s_g[buf]);
-    const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
-    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
-      Openness open = ALL;
-      if (MASK) {
-        Range theirs = NO_ROWS;
-#pragma unroll
-        for (int i = 0; i < BLOCK; i += 32)
-          if (j0 + i + lane < rem) {
-            const int t = ordered(s_limit[buf][j0 + i + lane]), d = s_doc[buf][j0 + i + lane];
-            theirs = {min(theirs.t_lo, t), max(theirs.t_hi, t), min(theirs.d_lo, d), max(theirs.d_hi, d)};
-          }
-        open = openness(warp_range(theirs.t_lo, theirs.t_hi, theirs.d_lo, theirs.d_hi), mine);
-        if (open == SHUT) continue;
-      }
+    const float slope2 = BIAS ? a.slopes[head] * LOG2E : 0.f;
 #pragma unroll 1
-      for (int j = j0; j < min(j0 + BLOCK, rem); j += STEP) {
-        float x[MT][NT][4], dp[MT][NT][4];
-        float2 st[NT][2];   // (lse, delta) of this lane's two columns of every tile
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const float4 t = *reinterpret_cast<const float4*>(&s_stats[buf][j + 8 * n + 2 * (lane & 3)]);
-          st[n][0] = make_float2(t.x, t.y);
-          st[n][1] = make_float2(t.z, t.w);
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              x[m][n][e] = 0.f;
-              dp[m][n][e] = -st[n][e & 1].y;
-            }
-        }
-        product_over_features<HD, MT, NT>(x, kf, bq, j, lane);
-        product_over_features<HD, MT, NT>(dp, vf, bg, j, lane);
-        uint32_t wp[MT][NT][2], ws[MT][NT][2];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          float bend[CAP ? NT : 1][4];
-          bend_scores<CAP, CAP, NT>(x[m], bend, a.inner, a.outer, a.bend_scale);
-          if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
-          if (MASK && open == SOME) {   // columns past the last row have an lse of +inf: no weight
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int col = j + 8 * n + 2 * (lane & 3) + e;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                  if (own_time[m][i] > s_limit[buf][col] || s_doc[buf][col] != own_doc[m][i]) x[m][n][2 * i + e] = -INFINITY;
-              }
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float2 y = __fadd2_rn(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(-st[n][0].x, -st[n][1].x));
-              const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
-              float2 ds = __fmul2_rn(p, make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]));
-              if constexpr (CAP) ds = __fmul2_rn(ds, make_float2(bend[n][2 * i], bend[n][2 * i + 1]));
-              wp[m][n][i] = ptx::pack_bf16(p.x, p.y);
-              ws[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
-            }
-        }
-        product_over_partners<HD, MT, NT>(dv, wp, bg, j, lane);
-        product_over_partners<HD, MT, NT>(dk, ws, bq, j, lane);
+    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
+      const Openness open = MASK ? openness(block_range(s_limit[buf], s_doc[buf], j0, rem, lane), mine) : ALL;
+      if (MASK && open == SHUT) continue;
+      if (!MASK || open == ALL) {
+#pragma unroll 1
+        for (int j = j0; j < min(j0 + BLOCK, rem); j += 8 * NT) step(IntTag<0>{}, buf, j, slope2);
+      } else if constexpr (MASK) {
+#pragma unroll 1
+        for (int j = j0; j < min(j0 + BLOCK, rem); j += 8 * NT) step(IntTag<1>{}, buf, j, slope2);
       }
     }
   }
@@ -441,12 +418,11 @@ template <typename K, int HD>
 cudaError_t launch_pass(const Geometry& g, const ScoredArgs& a, int heads, uint32_t walks, int n_sm, cudaStream_t st) {
   Tiles t = {};
   t.order = segment_order(g, walks);
-  constexpr int MT = 1;
-  const bool tall = make_tiles(&t, g.seg_len, 128) * heads * g.batch >= 6LL * n_sm;
+  const bool tall = HD <= 32 && make_tiles(&t, g.seg_len, 128) * heads * g.batch >= 6LL * n_sm;
   const int64_t n = make_tiles(&t, g.seg_len, tall ? 128 : 64) * heads;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n, g.batch);
-  return tall ? launch_rule<K, HD, MT, 8 / MT>(g, a, t, grid, st) : launch_rule<K, HD, 1, 4>(g, a, t, grid, st);
+  return tall ? launch_rule<K, HD, 1, HD <= 32 ? 8 : 4>(g, a, t, grid, st) : launch_rule<K, HD, 1, 4>(g, a, t, grid, st);
 }
 template <int HD>
 cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {

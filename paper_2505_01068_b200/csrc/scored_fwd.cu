@@ -4,11 +4,15 @@
 namespace gsit {
 namespace {
 
+// Registers: as many warps as hide the latency of a step's chain of products, exponentials and products (24 an SM for narrow heads, 16
+// and 8 for wide ones, whose accumulators are larger).
+template <int HD, int MT, int W> constexpr int MIN_CTAS = (HD <= 16 ? 24 : HD == 32 ? 16 : MT == 2 ? 8 : 16) / W;
+
 template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W)
+__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, MT, W>)
 scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 8 : 4, STEP = 8 * NT;
-  constexpr bool TIMES = BIAS || MASK;
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 8 : 4;
+  constexpr bool TIMES = BIAS || MASK, RAW = !CAP && !BIAS;   // RAW: the scale is folded into the exponent's multiply-add
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
   __shared__ int s_doc[2][MASK ? KC : 1];
@@ -22,14 +26,25 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 
   const int q0 = tile * TQ, q_end = min(q0 + TQ, a.q_len[s]);
   const QueryRows rows = query_rows(g, a, b, s);
-  int n_keys[3], chunks = 0, first_chunk[3];
+  Walk next = {};
 #pragma unroll
-  for (int r = 0; r < 3; ++r) {
-    n_keys[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
-    first_chunk[r] = chunks;
-    chunks += (n_keys[r] + KC - 1) / KC;
-  }
-  if (max(q0, rows.lo) >= min(q_end, rows.hi)) chunks = 0;
+  for (int r = 0; r < 3; ++r) next.n[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
+  if (max(q0, rows.lo) >= min(q_end, rows.hi)) next.seg = 3;
+  next.settle();
+
+  const int64_t sample0 = (int64_t)b * g.L;
+  const bf16* const k0 = static_cast<const bf16*>(a.k) + sample0 * a.ldk + (int64_t)hk * HD;
+  const bf16* const v0 = static_cast<const bf16*>(a.v) + sample0 * a.ldv + (int64_t)hk * HD;
+  auto stage = [&](const Walk& w, int buf) {
+    const int row0 = g.off(w.seg) + w.pos, rem = w.left();
+    stage_pair<HD, KC, W>(smem_u32(s_k[buf]), smem_u32(s_v[buf]), k0 + (int64_t)row0 * a.ldk, a.ldk, v0 + (int64_t)row0 * a.ldv, a.ldv, rem, tid);
+    if (TIMES)
+      for (int i = tid; i < min(KC, (rem + BLOCK - 1) / BLOCK * BLOCK); i += 32 * W) {
+        s_time[buf][i] = i >= rem ? 0.f : a.times != nullptr ? a.times[sample0 + row0 + i] : (float)(w.pos + i);
+        if (MASK) s_doc[buf][i] = i < rem && a.documents != nullptr ? a.documents[sample0 + row0 + i] : 0;
+      }
+  };
+  if (!next.over()) stage(next, 0);
 
   // ---- the warp's rows ----
   const int w0 = q0 + warp * 16 * MT;
@@ -47,50 +62,23 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       const int row = w0 + 16 * m + 8 * i + (lane >> 2);
       real[m][i] = row >= rows.lo && row < min(q_end, rows.hi);
       p[i] = real[m][i] ? static_cast<const bf16*>(a.q) + (q_row0 + row) * a.ldq + (int64_t)h * HD : nullptr;
-      if (TIMES && real[m][i]) {
-        own_time[m][i] = time_of(g, a, b, s, row + rows.shift);
+      own_time[m][i] = 0.f;
+      limit[m][i] = INFINITY;
+      own_doc[m][i] = 0;
+      if (TIMES && real[m][i]) own_time[m][i] = time_of(g, a, b, s, row + rows.shift);
+      if (MASK && real[m][i]) {
         limit[m][i] = latest_seen(a, b, own_time[m][i]);
         own_doc[m][i] = document_of(g, a, b, s, row + rows.shift);
-        mine.t_lo = min(mine.t_lo, ordered(limit[m][i]));
-        mine.t_hi = max(mine.t_hi, ordered(limit[m][i]));
-        mine.d_lo = min(mine.d_lo, own_doc[m][i]);
-        mine.d_hi = max(mine.d_hi, own_doc[m][i]);
-      } else {
-        own_time[m][i] = 0.f;
-        limit[m][i] = INFINITY;
-        own_doc[m][i] = 0;
+        mine = {min(mine.t_lo, ordered(limit[m][i])), max(mine.t_hi, ordered(limit[m][i])), min(mine.d_lo, own_doc[m][i]), max(mine.d_hi, own_doc[m][i])};
       }
     }
     own_rows<HD>(p[0], p[1], lane, qf[m]);
   }
   if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
   const bool working = w0 < min(q_end, rows.hi) && w0 + 16 * MT > rows.lo;
-  const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
+  const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f, unit = RAW ? a.inner : 1.f;
 
-  // ---- staging ----
-  auto segment_of_chunk = [&](int c) { return c >= first_chunk[2] && n_keys[2] > 0 ? 2 : c >= first_chunk[1] && n_keys[1] > 0 ? 1 : 0; };
-  auto stage = [&](int c) {
-    const int r = segment_of_chunk(c), j0 = (c - first_chunk[r]) * KC, buf = c & 1;
-    const int rem = n_keys[r] - j0, need = min(KC, (rem + BLOCK - 1) / BLOCK * BLOCK);   // rows past the last block are not read
-    const int64_t row0 = (int64_t)b * g.L + g.off(r) + j0;
-    const bf16 *k = static_cast<const bf16*>(a.k) + (int64_t)hk * HD, *v = static_cast<const bf16*>(a.v) + (int64_t)hk * HD;
-    const uint32_t dk = smem_u32(s_k[buf]), dv = smem_u32(s_v[buf]);
-    for (int i = tid; i < need * CH; i += 32 * W) {
-      const int row = i / CH, c16 = i % CH;
-      const bool in = row < rem;
-      const int64_t at = row0 + (in ? row : 0);
-      cp16(dk + piece_at<HD>(row, c16), k + at * a.ldk + 8 * c16, in);
-      cp16(dv + piece_at<HD>(row, c16), v + at * a.ldv + 8 * c16, in);
-    }
-    cp_commit();
-    if (TIMES)
-      for (int i = tid; i < need; i += 32 * W) {
-        s_time[buf][i] = i < rem ? time_of(g, a, b, r, j0 + i) : 0.f;
-        if (MASK) s_doc[buf][i] = i < rem ? document_of(g, a, b, r, j0 + i) : 0;
-      }
-  };
-
-  float o[MT][CH][4], ref[MT][2];
+  float o[MT][CH][4], ref[MT][2];   // ref: in base 2
   float2 sum[MT][2];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
@@ -105,86 +93,97 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     }
   }
 
-  if (chunks > 0) stage(0);
-  for (int c = 0; c < chunks; ++c) {
-    cp_wait();
-    __syncthreads();   // chunk c is there, and nobody reads the other buffer any more
-    if (c + 1 < chunks) stage(c + 1);
-    if (!working) continue;
-    const int r = segment_of_chunk(c), buf = c & 1, rem = min(KC, n_keys[r] - (c - first_chunk[r]) * KC);
-    const uint32_t bk = smem_u32(s_k[buf]), bv = smem_u32(s_v[buf]);
-    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
-      Openness open = ALL;
-      if (MASK) {
-        Range theirs = NO_ROWS;
+  // One step: 8 N keys from column j of the chunk on; `some`: pairs of it may be closed, or it reaches past the last key.
+  auto step = [&](auto n_tag, auto some_tag, int buf, int j, int rem) {
+    constexpr int N = decltype(n_tag)::value;
+    constexpr bool SOME_SHUT = decltype(some_tag)::value;
+    float x[MT][N][4];
 #pragma unroll
-        for (int i = 0; i < BLOCK; i += 32)
-          if (j0 + i + lane < rem) {
-            const int t = ordered(s_time[buf][j0 + i + lane]), d = s_doc[buf][j0 + i + lane];
-            theirs = {min(theirs.t_lo, t), max(theirs.t_hi, t), min(theirs.d_lo, d), max(theirs.d_hi, d)};
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[m][n][e] = 0.f;
+    product_over_features<HD, MT, N>(x, qf, smem_u32(s_k[buf]), j, lane);
+    uint32_t w[MT][N][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      if constexpr (CAP) cap_scores<N>(x[m], a.inner, a.outer);
+      else if constexpr (BIAS) scale_scores<N>(x[m], a.inner);
+      if constexpr (BIAS) add_bias<N>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
+      if constexpr (SOME_SHUT) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int col = j + 8 * n + 2 * (lane & 3) + e;
+            const bool in = col < rem;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
           }
-        open = openness(mine, warp_range(theirs.t_lo, theirs.t_hi, theirs.d_lo, theirs.d_hi));
-        if (open == SHUT) continue;
       }
-#pragma unroll 1
-      for (int j = j0; j < min(j0 + BLOCK, rem); j += STEP) {
-        float x[MT][NT][4], unused[1][4];
+      // the reference follows the maximum only when that has grown by more than 2^8 (weights stay below 256): as long as no lane's
+      // own scores have, the lanes of a row need not be brought together
+      float top[2];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+      for (int i = 0; i < 2; ++i) {
+        top[i] = -INFINITY;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < N; ++n) top[i] = ptx::fmax3(top[i], x[m][n][2 * i], x[m][n][2 * i + 1]);
+        top[i] *= unit;
+      }
+      if (__any_sync(0xffffffffu, top[0] > ref[m][0] + 8.f || top[1] > ref[m][1] + 8.f)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[m][n][e] = 0.f;
-        product_over_features<HD, MT, NT>(x, qf, bk, j, lane);
-        uint32_t w[MT][NT][2];
-        const bool ragged = j + STEP > rem;
+        for (int i = 0; i < 2; ++i) {
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+          if (top[i] > ref[m][i]) {
+            const float f = ptx::ex2(ref[m][i] - top[i]);
+            sum[m][i] = __fmul2_rn(sum[m][i], make_float2(f, f));
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          bend_scores<CAP, false, NT>(x[m], unused, a.inner, a.outer, a.bend_scale);
-          if (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
-          if (ragged || (MASK && open == SOME)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int col = j + 8 * n + 2 * (lane & 3) + e;
-                const bool in = col < rem;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                  if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
-              }
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) top = ptx::fmax3(top, x[m][n][2 * i], x[m][n][2 * i + 1]);
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // the reference follows the maximum only when it has grown by more than 2^8: weights stay below 256
-            const bool grow = top > ref[m][i] + 8.f;
-            if (__any_sync(0xffffffffu, grow)) {
-              const float f = grow ? ptx::ex2(ref[m][i] - top) : 1.f;
-              sum[m][i] = __fmul2_rn(sum[m][i], make_float2(f, f));
-#pragma unroll
-              for (int q = 0; q < CH; ++q) {
-                o[m][q][2 * i] *= f;
-                o[m][q][2 * i + 1] *= f;
-              }
-              if (grow) ref[m][i] = top;
+            for (int q = 0; q < CH; ++q) {
+              o[m][q][2 * i] *= f;
+              o[m][q][2 * i + 1] *= f;
             }
-            // a row that has seen no open key yet keeps weights of zero
-            const float nr = ref[m][i] == -INFINITY ? 0.f : -ref[m][i];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const float2 y = __fadd2_rn(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(nr, nr));
-              const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
-              sum[m][i] = __fadd2_rn(sum[m][i], p);
-              w[m][n][i] = ptx::pack_bf16(p.x, p.y);
-            }
+            ref[m][i] = top[i];
           }
         }
-        product_over_partners<HD, MT, NT>(o, w, bv, j, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float r = ref[m][i] == -INFINITY ? 0.f : -ref[m][i];   // a row that has seen no open key yet keeps weights of zero
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const float2 y = make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), rr = make_float2(r, r);
+          const float2 z = RAW ? __ffma2_rn(y, make_float2(unit, unit), rr) : __fadd2_rn(y, rr);
+          const float2 p = make_float2(ptx::ex2(z.x), ptx::ex2(z.y));
+          sum[m][i] = __fadd2_rn(sum[m][i], p);
+          w[m][n][i] = ptx::pack_bf16(p.x, p.y);
+        }
+      }
+    }
+    product_over_partners<HD, MT, N>(o, w, smem_u32(s_v[buf]), j, lane);
+  };
+
+  for (int buf = 0; !next.over(); buf ^= 1) {
+    const int rem = min(KC, next.left());
+    cp_wait();
+    __syncthreads();   // the chunk is there, and nobody reads the other buffer any more
+    next.pos += KC;
+    next.settle();
+    if (!next.over()) stage(next, buf ^ 1);
+    if (!working) continue;
+#pragma unroll 1
+    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
+      const Openness open = MASK ? openness(mine, block_range(s_time[buf], s_doc[buf], j0, rem, lane)) : ALL;
+      if (MASK && open == SHUT) continue;
+      if (open == ALL && j0 + BLOCK <= rem) {
+#pragma unroll 1
+        for (int j = j0; j < j0 + BLOCK; j += 8 * NT) step(IntTag<NT>{}, IntTag<0>{}, buf, j, rem);
+      } else {
+#pragma unroll 1
+        for (int j = j0; j < min(j0 + BLOCK, rem); j += 4 * NT) step(IntTag<NT / 2>{}, IntTag<1>{}, buf, j, rem);
       }
     }
   }
@@ -242,7 +241,7 @@ cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st
   const int64_t n = make_tiles(&t, a.q_len, tall ? 128 : 64) * g.heads;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n, g.batch);
-  constexpr int MT = HD == 64 ? 2 : 1;
+  constexpr int MT = HD == 64 ? 2 : 1;   // wide heads: a row tile more per fragment of K and V that is read
   return tall ? launch_rule<HD, MT, 8 / MT>(g, a, t, grid, st) : launch_rule<HD, 1, 4>(g, a, t, grid, st);
 }
 

@@ -12,6 +12,7 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 
+template <int V> struct IntTag { static constexpr int value = V; };
 constexpr int BLOCK = 64;                                            // partners that are classified together
 template <int HD> constexpr int CHUNK_ROWS = HD == 8 ? 256 : HD == 64 ? 64 : 128;
 
@@ -133,57 +134,52 @@ __device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4],
   }
 }
 
-// Dots -> scores in base 2 (in place), and where wanted the derivative of the cap (bend_scale = 1 / outer^2).  One range check for the whole warp decides between
-// the polynomial alone and the form for any argument.
-template <bool CAP, bool BEND, int NT>
-__device__ __forceinline__ void bend_scores(float (&x)[NT][4], float (&bend)[BEND ? NT : 1][4], float inner, float outer, float bend_scale) {
-  if constexpr (!CAP) {
-    const float2 f = make_float2(inner, inner);
+// Dots -> capped scores in base 2 (in place).  One range check for the whole warp decides between the polynomial alone and the form
+// for any argument.
+template <int NT> __device__ __forceinline__ void cap_scores(float (&x)[NT][4], float inner, float outer) {
+  float top = 0.f;
+  const float2 f = make_float2(inner, inner), o = make_float2(outer, outer);
+  auto each = [&](auto score) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
-        const float2 y = __fmul2_rn(make_float2(x[n][i], x[n][i + 1]), f);
+        const float2 y = score(make_float2(x[n][i], x[n][i + 1]));
         x[n][i] = y.x;
         x[n][i + 1] = y.y;
       }
-  } else {
-    float top = 0.f;
-    const float2 f = make_float2(inner, inner), o = make_float2(outer, outer);
+  };
+  each([&](float2 y) {
+    y = __fmul2_rn(y, f);
+    top = ptx::fmax3(top, fabsf(y.x), fabsf(y.y));
+    return y;
+  });
+  if (__any_sync(0xffffffffu, top > TANH_RANGE)) each([&](float2 y) { return __fmul2_rn(tanh_any2(y), o); });
+  else each([&](float2 y) { return tanh_near2(y, outer); });
+}
+// d *= 1 - tanh^2, from the capped scores x (bend_scale = 1 / outer^2)
+template <int NT> __device__ __forceinline__ void times_bend(float (&d)[NT][4], const float (&x)[NT][4], float bend_scale) {
+  const float2 f = make_float2(-bend_scale, -bend_scale), one = make_float2(1.f, 1.f);
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        const float2 y = __fmul2_rn(make_float2(x[n][i], x[n][i + 1]), f);
-        top = ptx::fmax3(top, fabsf(y.x), fabsf(y.y));
-        x[n][i] = y.x;
-        x[n][i + 1] = y.y;
-      }
-    const bool far = __any_sync(0xffffffffu, top > TANH_RANGE);
-    auto each = [&](auto score) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          const float2 y = score(make_float2(x[n][i], x[n][i + 1]));
-          x[n][i] = y.x;
-          x[n][i + 1] = y.y;
-        }
-    };
-    if (far) each([&](float2 y) { return __fmul2_rn(tanh_any2(y), o); });
-    else each([&](float2 y) { return tanh_near2(y, outer); });
-    if constexpr (BEND) {   // 1 - tanh^2
-      const float2 f2 = make_float2(-bend_scale, -bend_scale), one = make_float2(1.f, 1.f);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          const float2 y = make_float2(x[n][i], x[n][i + 1]), b = __ffma2_rn(__fmul2_rn(y, f2), y, one);
-          bend[n][i] = b.x;
-          bend[n][i + 1] = b.y;
-        }
+    for (int i = 0; i < 4; i += 2) {
+      const float2 y = make_float2(x[n][i], x[n][i + 1]);
+      const float2 e = __fmul2_rn(make_float2(d[n][i], d[n][i + 1]), __ffma2_rn(__fmul2_rn(y, f), y, one));
+      d[n][i] = e.x;
+      d[n][i + 1] = e.y;
     }
-  }
+}
+template <int NT> __device__ __forceinline__ void scale_scores(float (&x)[NT][4], float inner) {
+  const float2 f = make_float2(inner, inner);
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const float2 y = __fmul2_rn(make_float2(x[n][i], x[n][i + 1]), f);
+      x[n][i] = y.x;
+      x[n][i + 1] = y.y;
+    }
 }
 // x -= slope2 * |own time - partner time|.  own[2]: rows g, g + 8; partner times in shared memory from column 0 on.
 template <int NT> __device__ __forceinline__ void add_bias(float (&x)[NT][4], const float (&own)[2], const float* times, int lane, float slope2) {
@@ -218,6 +214,50 @@ enum Openness { SHUT, SOME, ALL };
 __device__ __forceinline__ Openness openness(const Range& queries, const Range& keys) {
   if (queries.d_hi < keys.d_lo || keys.d_hi < queries.d_lo || keys.t_lo > queries.t_hi) return SHUT;
   return queries.d_lo == queries.d_hi && keys.d_lo == keys.d_hi && keys.t_hi <= queries.t_lo ? ALL : SOME;
+}
+
+// Chunks of C partners through the segments that are walked, in order.
+struct Walk {
+  int n[3];          // rows to walk per segment, 0 where shut
+  int seg, pos;      // where it stands; seg 3: over
+  __device__ __forceinline__ int rows(int s) const { return s == 0 ? n[0] : s == 1 ? n[1] : n[2]; }
+  __device__ __forceinline__ void settle() {   // over segments that hold nothing more
+    if (seg == 0 && pos >= n[0]) { seg = 1; pos = 0; }
+    if (seg == 1 && pos >= n[1]) { seg = 2; pos = 0; }
+    if (seg == 2 && pos >= n[2]) { seg = 3; pos = 0; }
+  }
+  __device__ __forceinline__ bool over() const { return seg == 3; }
+  __device__ __forceinline__ int left() const { return rows(seg) - pos; }
+};
+
+// Moments and documents of a block of 64 partners as a range; `t` holds what openness() compares.
+__device__ __forceinline__ Range block_range(const float* t, const int* d, int j0, int rem, int lane) {
+  Range r = NO_ROWS;
+#pragma unroll
+  for (int i = 0; i < BLOCK; i += 32)
+    if (j0 + i + lane < rem) {
+      const int o = ordered(t[j0 + i + lane]), e = d[j0 + i + lane];
+      r = {min(r.t_lo, o), max(r.t_hi, o), min(r.d_lo, e), max(r.d_hi, e)};
+    }
+  return warp_range(r.t_lo, r.t_hi, r.d_lo, r.d_hi);
+}
+// A chunk of rows of two matrices into shared memory, whole blocks of them, zeros from row `rem` on.
+template <int HD, int C, int W>
+__device__ __forceinline__ void stage_pair(uint32_t d0, uint32_t d1, const bf16* p0, int64_t ld0, const bf16* p1, int64_t ld1, int rem, int tid) {
+  constexpr int CH = HD / 8;
+  const int need = min(C, (rem + BLOCK - 1) / BLOCK * BLOCK), c = tid % CH;
+  int row = tid / CH;
+  p0 += (int64_t)row * ld0 + 8 * c;
+  p1 += (int64_t)row * ld1 + 8 * c;
+#pragma unroll 1
+  for (; row < need; row += 32 * W / CH) {
+    const bool in = row < rem;
+    cp16(d0 + piece_at<HD>(row, c), in ? p0 : p0 - (int64_t)row * ld0, in);
+    cp16(d1 + piece_at<HD>(row, c), in ? p1 : p1 - (int64_t)row * ld1, in);
+    p0 += (32 * W / CH) * ld0;
+    p1 += (32 * W / CH) * ld1;
+  }
+  cp_commit();
 }
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }

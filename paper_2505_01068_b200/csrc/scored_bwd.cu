@@ -123,6 +123,9 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   const bool working = w0 < min(q_end, n_q);
   const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
 
+  const uint32_t at_kn = smem_u32(s_k[0]) + lane_as_n<HD>(lane), at_kk = smem_u32(s_k[0]) + lane_as_k<HD>(lane);
+  const uint32_t at_v = smem_u32(s_v[0]) + lane_as_n<HD>(lane);
+
   float dq[MT][CH][4];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -134,17 +137,12 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   auto step = [&](auto some_tag, int buf, int j, int rem) {
     constexpr bool SOME_SHUT = decltype(some_tag)::value;
     float x[MT][NT][4], dp[MT][NT][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[m][n][e] = 0.f;
-          dp[m][n][e] = -delta[m][e >> 1];
-        }
-    product_over_features<HD, MT, NT>(x, qf, smem_u32(s_k[buf]), j, lane);
-    product_over_features<HD, MT, NT>(dp, gf, smem_u32(s_v[buf]), j, lane);
+    const uint32_t from = (buf * KC + j) * HD * 2;
+    product_over_features<HD, MT, NT>(x, qf, at_kn + from, from_zero);
+    product_over_features<HD, MT, NT>(dp, gf, at_v + from, [&](int m, int, float (&z)[4]) {
+      z[0] = z[1] = -delta[m][0];
+      z[2] = z[3] = -delta[m][1];
+    });
     uint32_t w[MT][NT][2], unused[1][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -169,7 +167,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       }
       weigh<CAP, BIAS, false, NT>(x[m], dp[m], unused, w[m], a.inner, [&](int, int i) { return make_float2(lse2[m][i], lse2[m][i]); });
     }
-    product_over_partners<HD, MT, NT>(dq, w, smem_u32(s_k[buf]), j, lane);
+    product_over_partners<HD, MT, NT>(dq, w, at_kk + from);
   };
 
   for (int buf = 0; !next.over(); buf ^= 1) {
@@ -180,17 +178,24 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
     next.settle();
     if (!next.over()) stage(next, buf ^ 1);
     if (!working) continue;
+    int j = 0;
+    if constexpr (!MASK) {
 #pragma unroll 1
-    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
-      const Openness open = MASK ? openness(mine, block_range(s_time[buf], s_doc[buf], j0, rem, lane)) : ALL;
-      if (MASK && open == SHUT) continue;
-      const int end = min(j0 + BLOCK, rem);
-      int j = j0;
-      if (open == ALL)
+      for (; j + 8 * NT <= rem; j += 8 * NT) step(IntTag<0>{}, buf, j, rem);
+      if (j < rem) step(IntTag<1>{}, buf, j, rem);
+    } else {
 #pragma unroll 1
-        for (; j + 8 * NT <= end; j += 8 * NT) step(IntTag<0>{}, buf, j, rem);
+      while (j < rem) {
+        const Openness open = openness(mine, block_range(s_time[buf], s_doc[buf], j, rem, lane));
+        const int end = min(j + BLOCK, rem);
+        if (open == ALL && end - j == BLOCK)
 #pragma unroll 1
-      for (; j < end; j += 8 * NT) step(IntTag<1>{}, buf, j, rem);
+          for (; j < end; j += 8 * NT) step(IntTag<0>{}, buf, j, rem);
+        else if (open != SHUT)
+#pragma unroll 1
+          for (; j < end; j += 8 * NT) step(IntTag<1>{}, buf, j, rem);
+        j = end;
+      }
     }
   }
 
@@ -293,6 +298,9 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
   const bool working = w0 < min(k_end, n_k);
 
+  const uint32_t at_qn = smem_u32(s_q[0]) + lane_as_n<HD>(lane), at_qk = smem_u32(s_q[0]) + lane_as_k<HD>(lane);
+  const uint32_t at_gn = smem_u32(s_g[0]) + lane_as_n<HD>(lane), at_gk = smem_u32(s_g[0]) + lane_as_k<HD>(lane);
+
   float dk[MT][CH][4], dv[MT][CH][4];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -304,21 +312,19 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   auto step = [&](auto some_tag, int buf, int j, float slope2) {
     constexpr bool SOME_SHUT = decltype(some_tag)::value;
     float x[MT][NT][4], dp[MT][NT][4];
-    float2 lse2[NT];   // of this lane's two columns of every tile
+    float2 lse2[NT], delta[NT];   // of this lane's two columns of every tile
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float4 t = *reinterpret_cast<const float4*>(&s_stats[buf][j + 8 * n + 2 * (lane & 3)]);
       lse2[n] = make_float2(t.x, t.z);
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[m][n][e] = 0.f;
-          dp[m][n][e] = (e & 1) ? -t.w : -t.y;
-        }
+      delta[n] = make_float2(-t.y, -t.w);
     }
-    product_over_features<HD, MT, NT>(x, kf, smem_u32(s_q[buf]), j, lane);
-    product_over_features<HD, MT, NT>(dp, vf, smem_u32(s_g[buf]), j, lane);
+    const uint32_t from = (buf * QC + j) * HD * 2;
+    product_over_features<HD, MT, NT>(x, kf, at_qn + from, from_zero);
+    product_over_features<HD, MT, NT>(dp, vf, at_gn + from, [&](int, int n, float (&z)[4]) {
+      z[0] = z[2] = delta[n].x;
+      z[1] = z[3] = delta[n].y;
+    });
     uint32_t wp[MT][NT][2], ws[MT][NT][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -342,8 +348,8 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       }
       weigh<CAP, BIAS, true, NT>(x[m], dp[m], wp[m], ws[m], a.inner, [&](int n, int) { return lse2[n]; });
     }
-    product_over_partners<HD, MT, NT>(dv, wp, smem_u32(s_g[buf]), j, lane);
-    product_over_partners<HD, MT, NT>(dk, ws, smem_u32(s_q[buf]), j, lane);
+    product_over_partners<HD, MT, NT>(dv, wp, at_gk + from);
+    product_over_partners<HD, MT, NT>(dk, ws, at_qk + from);
   };
 
   for (int buf = 0; !next.over(); buf ^= 1) {
@@ -359,16 +365,22 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     if (!next.over()) stage(next, h, buf ^ 1);
     if (!working) continue;
     const float slope2 = BIAS ? a.slopes[head] * LOG2E : 0.f;
+    int j = 0;
+    if constexpr (!MASK) {
 #pragma unroll 1
-    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
-      const Openness open = MASK ? openness(block_range(s_limit[buf], s_doc[buf], j0, rem, lane), mine) : ALL;
-      if (MASK && open == SHUT) continue;
-      if (!MASK || open == ALL) {
+      for (; j < rem; j += 8 * NT) step(IntTag<0>{}, buf, j, slope2);
+    } else {
 #pragma unroll 1
-        for (int j = j0; j < min(j0 + BLOCK, rem); j += 8 * NT) step(IntTag<0>{}, buf, j, slope2);
-      } else if constexpr (MASK) {
+      while (j < rem) {
+        const Openness open = openness(block_range(s_limit[buf], s_doc[buf], j, rem, lane), mine);
+        const int end = min(j + BLOCK, rem);
+        if (open == ALL)
 #pragma unroll 1
-        for (int j = j0; j < min(j0 + BLOCK, rem); j += 8 * NT) step(IntTag<1>{}, buf, j, slope2);
+          for (; j < end; j += 8 * NT) step(IntTag<0>{}, buf, j, slope2);
+        else if (open != SHUT)
+#pragma unroll 1
+          for (; j < end; j += 8 * NT) step(IntTag<1>{}, buf, j, slope2);
+        j = end;
       }
     }
   }

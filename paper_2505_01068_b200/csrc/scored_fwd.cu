@@ -76,7 +76,8 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   }
   if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
   const bool working = w0 < min(q_end, rows.hi) && w0 + 16 * MT > rows.lo;
-  const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f, unit = RAW ? a.inner : 1.f;
+  const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
+  const uint32_t at_k = smem_u32(s_k[0]) + lane_as_n<HD>(lane), at_v = smem_u32(s_v[0]) + lane_as_k<HD>(lane);
 
   float o[MT][CH][4], ref[MT][2];   // ref: in base 2
   float2 sum[MT][2];
@@ -98,13 +99,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     constexpr int N = decltype(n_tag)::value;
     constexpr bool SOME_SHUT = decltype(some_tag)::value;
     float x[MT][N][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[m][n][e] = 0.f;
-    product_over_features<HD, MT, N>(x, qf, smem_u32(s_k[buf]), j, lane);
+    product_over_features<HD, MT, N>(x, qf, at_k + (buf * KC + j) * HD * 2, from_zero);
     uint32_t w[MT][N][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -131,7 +126,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
         top[i] = -INFINITY;
 #pragma unroll
         for (int n = 0; n < N; ++n) top[i] = ptx::fmax3(top[i], x[m][n][2 * i], x[m][n][2 * i + 1]);
-        top[i] *= unit;
+        if constexpr (RAW) top[i] *= a.inner;
       }
       if (__any_sync(0xffffffffu, top[0] > ref[m][0] + 8.f || top[1] > ref[m][1] + 8.f)) {
 #pragma unroll
@@ -156,14 +151,14 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 #pragma unroll
         for (int n = 0; n < N; ++n) {
           const float2 y = make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), rr = make_float2(r, r);
-          const float2 z = RAW ? __ffma2_rn(y, make_float2(unit, unit), rr) : __fadd2_rn(y, rr);
+          const float2 z = RAW ? __ffma2_rn(y, make_float2(a.inner, a.inner), rr) : __fadd2_rn(y, rr);
           const float2 p = make_float2(ptx::ex2(z.x), ptx::ex2(z.y));
           sum[m][i] = __fadd2_rn(sum[m][i], p);
           w[m][n][i] = ptx::pack_bf16(p.x, p.y);
         }
       }
     }
-    product_over_partners<HD, MT, N>(o, w, smem_u32(s_v[buf]), j, lane);
+    product_over_partners<HD, MT, N>(o, w, at_v + (buf * KC + j) * HD * 2);
   };
 
   for (int buf = 0; !next.over(); buf ^= 1) {
@@ -174,16 +169,24 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     next.settle();
     if (!next.over()) stage(next, buf ^ 1);
     if (!working) continue;
+    int j = 0;
+    if constexpr (!MASK) {
 #pragma unroll 1
-    for (int j0 = 0; j0 < rem; j0 += BLOCK) {
-      const Openness open = MASK ? openness(mine, block_range(s_time[buf], s_doc[buf], j0, rem, lane)) : ALL;
-      if (MASK && open == SHUT) continue;
-      if (open == ALL && j0 + BLOCK <= rem) {
+      for (; j + 8 * NT <= rem; j += 8 * NT) step(IntTag<NT>{}, IntTag<0>{}, buf, j, rem);
 #pragma unroll 1
-        for (int j = j0; j < j0 + BLOCK; j += 8 * NT) step(IntTag<NT>{}, IntTag<0>{}, buf, j, rem);
-      } else {
+      for (; j < rem; j += 4 * NT) step(IntTag<NT / 2>{}, IntTag<1>{}, buf, j, rem);
+    } else {
 #pragma unroll 1
-        for (int j = j0; j < min(j0 + BLOCK, rem); j += 4 * NT) step(IntTag<NT / 2>{}, IntTag<1>{}, buf, j, rem);
+      while (j < rem) {
+        const Openness open = openness(mine, block_range(s_time[buf], s_doc[buf], j, rem, lane));
+        const int end = min(j + BLOCK, rem);
+        if (open == ALL && end - j == BLOCK)
+#pragma unroll 1
+          for (; j < end; j += 8 * NT) step(IntTag<NT>{}, IntTag<0>{}, buf, j, rem);
+        else if (open != SHUT)
+#pragma unroll 1
+          for (; j < end; j += 4 * NT) step(IntTag<NT / 2>{}, IntTag<1>{}, buf, j, rem);
+        j = end;
       }
     }
   }

@@ -22,13 +22,15 @@ __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
 __device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// d = a b + c; c is an operand of its own, so that a constant start costs no instruction
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
-__device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0));
+__device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, const float (&c)[4]) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%8,%9,%10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {   // zeros where the row is not real
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
@@ -43,20 +45,19 @@ template <int HD> __device__ __forceinline__ uint32_t piece_at(int r, int c) {
   return (uint32_t)(r * HD * 2 + ((CH == 1 ? 0 : c ^ ((r / (8 / CH)) % CH)) << 4));
 }
 
-// Fragments of 16 staged rows (or 32 rows of 8 features) as the B operand.
-//   rows_as_n: the product runs over features; f[ks] = {n 0-7 k lo, n 0-7 k hi, n 8-15 k lo, n 8-15 k hi} of feature step ks
-//   rows_as_k: the product runs over the rows; f[c2] = {c lo: rows 0-7, rows 8-15, c hi: the same} of feature pieces 2 c2, 2 c2 + 1
-template <int HD> __device__ __forceinline__ void frag_rows_as_n(uint32_t base, int row0, int lane, uint32_t (&f)[HD / 16][4]) {
-#pragma unroll
-  for (int ks = 0; ks < HD / 16; ++ks) ldsm4(base + piece_at<HD>(row0 + ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)), f[ks]);
+// Where a lane's ldmatrix addresses lie from row 0 of a tile on; those of a later group of 16 rows are a multiple of 16 rows further
+// (the permutation repeats), those of feature step ks have that bit flipped in.
+//   as n: the product runs over features; a load of 16 rows gives {n 0-7 k lo, n 0-7 k hi, n 8-15 k lo, n 8-15 k hi} of a feature step
+//   as k: the product runs over the rows; a load gives {features lo: rows 0-7, rows 8-15, features hi: the same} of 16 features
+// Rows of 8 features: one load takes 32 of them, 8 to a matrix, either way.
+template <int HD> __device__ __forceinline__ uint32_t lane_as_n(int lane) {
+  if constexpr (HD == 8) return lane * 16;
+  return piece_at<HD>(((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1);
 }
-template <int HD> __device__ __forceinline__ void frag_rows_as_k(uint32_t base, int row0, int lane, uint32_t (&f)[HD / 16][4]) {
-#pragma unroll
-  for (int c = 0; c < HD / 16; ++c) ldsm4_t(base + piece_at<HD>(row0 + (((lane >> 3) & 1) << 3) + (lane & 7), 2 * c + (lane >> 4)), f[c]);
+template <int HD> __device__ __forceinline__ uint32_t lane_as_k(int lane) {
+  if constexpr (HD == 8) return lane * 16;
+  return piece_at<HD>((((lane >> 3) & 1) << 3) + (lane & 7), lane >> 4);
 }
-// 16 rows of 8 features, read through one x4 load of 32 rows: f[i] = rows 8 i .. 8 i + 7, as n (plain) or as k (transposed).
-__device__ __forceinline__ void frag8(uint32_t base, int row0, int lane, uint32_t (&f)[4]) { ldsm4(base + (row0 + lane) * 16, f); }
-__device__ __forceinline__ void frag8_t(uint32_t base, int row0, int lane, uint32_t (&f)[4]) { ldsm4_t(base + (row0 + lane) * 16, f); }
 
 // A operand of a warp's own rows, straight from memory: rows row0 + lane / 4 and + 8, zeros where not real.  Head width 8 uses words 0, 1.
 template <int HD> __device__ __forceinline__ void own_rows(const bf16* p0, const bf16* p1, int lane, uint32_t (&f)[(HD + 15) / 16][4]) {
@@ -70,69 +71,76 @@ template <int HD> __device__ __forceinline__ void own_rows(const bf16* p0, const
   }
 }
 
-// c[mt][nt] += own rows x partner rows, over features, for NT tiles of 8 partners from row0 on.
-template <int HD, int MT, int NT>
-__device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], const uint32_t (&own)[MT][(HD + 15) / 16][4], uint32_t base, int row0, int lane) {
+// c[mt][nt] = start(mt, nt) + own rows x partner rows, over features, for NT tiles of 8 partners; `at`: the first one's tile + lane_as_n.
+template <int HD, int MT, int NT, typename Start>
+__device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], const uint32_t (&own)[MT][(HD + 15) / 16][4], uint32_t at, Start start) {
   if constexpr (HD == 8) {
 #pragma unroll
     for (int q = 0; q < NT / 4; ++q) {
       uint32_t f[4];
-      frag8(base, row0 + 32 * q, lane, f);
+      ldsm4(at + q * 512, f);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mma8(c[m][4 * q + i], own[m][0][0], own[m][0][1], f[i]);
+        for (int i = 0; i < 4; ++i) {
+          float z[4];
+          start(m, 4 * q + i, z);
+          mma8(c[m][4 * q + i], own[m][0][0], own[m][0][1], f[i], z);
+        }
     }
   } else {
 #pragma unroll
-    for (int p = 0; p < NT / 2; ++p) {
-      uint32_t f[HD / 16][4];
-      frag_rows_as_n<HD>(base, row0 + 16 * p, lane, f);
+    for (int p = 0; p < NT / 2; ++p)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int ks = 0; ks < HD / 16; ++ks) {
+        uint32_t f[4];
+        ldsm4((at ^ (ks << 5)) + p * 32 * HD, f);
 #pragma unroll
-        for (int ks = 0; ks < HD / 16; ++ks) {
-          mma16(c[m][2 * p], own[m][ks], f[ks][0], f[ks][1]);
-          mma16(c[m][2 * p + 1], own[m][ks], f[ks][2], f[ks][3]);
-        }
-    }
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float z[4];
+            if (ks == 0) start(m, 2 * p + i, z);
+            mma16(c[m][2 * p + i], own[m][ks], f[2 * i], f[2 * i + 1], ks == 0 ? z : c[m][2 * p + i]);
+          }
+      }
   }
 }
-// o[mt][feature tile] += weights [own rows x partners] x partner rows, over NT tiles of 8 partners from row0 on; weights as packed
-// accumulators w[mt][nt] = {row g, row g + 8}.
+// o[mt][feature tile] += weights [own rows x partners] x partner rows, over NT tiles of 8 partners; weights as packed accumulators
+// w[mt][nt] = {row g, row g + 8}; `at`: the first partner's tile + lane_as_k.
 template <int HD, int MT, int NT>
-__device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4], const uint32_t (&w)[MT][NT][2], uint32_t base, int row0, int lane) {
+__device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4], const uint32_t (&w)[MT][NT][2], uint32_t at) {
   if constexpr (HD == 8) {
 #pragma unroll
     for (int q = 0; q < NT / 4; ++q) {
       uint32_t f[4];
-      frag8_t(base, row0 + 32 * q, lane, f);
+      ldsm4_t(at + q * 512, f);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int nt = 4 * q + 2 * i;
           const uint32_t a[4] = {w[m][nt][0], w[m][nt][1], w[m][nt + 1][0], w[m][nt + 1][1]};
-          mma16(o[m][0], a, f[2 * i], f[2 * i + 1]);
+          mma16(o[m][0], a, f[2 * i], f[2 * i + 1], o[m][0]);
         }
     }
   } else {
 #pragma unroll
-    for (int p = 0; p < NT / 2; ++p) {
-      uint32_t f[HD / 16][4];
-      frag_rows_as_k<HD>(base, row0 + 16 * p, lane, f);
+    for (int p = 0; p < NT / 2; ++p)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const uint32_t a[4] = {w[m][2 * p][0], w[m][2 * p][1], w[m][2 * p + 1][0], w[m][2 * p + 1][1]};
+      for (int c = 0; c < HD / 16; ++c) {
+        uint32_t f[4];
+        ldsm4_t((at ^ (c << 5)) + p * 32 * HD, f);
 #pragma unroll
-        for (int c = 0; c < HD / 16; ++c) {
-          mma16(o[m][2 * c], a, f[c][0], f[c][1]);
-          mma16(o[m][2 * c + 1], a, f[c][2], f[c][3]);
+        for (int m = 0; m < MT; ++m) {
+          const uint32_t a[4] = {w[m][2 * p][0], w[m][2 * p][1], w[m][2 * p + 1][0], w[m][2 * p + 1][1]};
+          mma16(o[m][2 * c], a, f[0], f[1], o[m][2 * c]);
+          mma16(o[m][2 * c + 1], a, f[2], f[3], o[m][2 * c + 1]);
         }
       }
-    }
   }
 }
+__device__ __forceinline__ void from_zero(int, int, float (&z)[4]) { z[0] = z[1] = z[2] = z[3] = 0.f; }
 
 // Dots -> capped scores in base 2 (in place).  One range check for the whole warp decides between the polynomial alone and the form
 // for any argument.

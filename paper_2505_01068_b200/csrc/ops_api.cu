@@ -88,6 +88,7 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
 // Which kernels serve a call, and the scratch they need.
 size_t scored_fwd_scratch(const Geometry&, int, const ScoredArgs&) { return 0; }
 cudaError_t launch_scored_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
+  if (scored_tail_supported(g, dtype, a)) return launch_scored_tail(g, dtype, a, st);
   if (dtype == GSIT_BF16) return launch_scored_fwd_bf16(g, a, st);
   return g.hd <= 64 ? launch_scored_fwd_f32(g, a, st) : launch_scored_rows_fwd(g, a, st);
 }

@@ -75,12 +75,14 @@ __device__ __forceinline__ float2 tanh_any2(float2 y) {
   return make_float2(fabsf(y.x) > TANH_RANGE ? tanh_far(y.x) : t.x, fabsf(y.y) > TANH_RANGE ? tanh_far(y.y) : t.y);
 }
 
+__device__ __forceinline__ float tanh_any(float y) { return fabsf(y) > TANH_RANGE ? tanh_far(y) : tanh_near2(make_float2(y, y)).x; }
+
 // Score of one pair in base 2, and the derivative of the cap.
 __device__ __forceinline__ float score_of(const ScoredArgs& a, float dot, float slope2, float distance, float* bend) {
   float x = dot * a.inner;
   *bend = 1.f;
   if (a.softcap > 0.f) {
-    const float t = tanh_any2(make_float2(x, x)).x;
+    const float t = tanh_any(x);
     *bend = 1.f - t * t;
     x = t * a.outer;
   }

@@ -20,7 +20,7 @@ constexpr int STEPS = 4;       // key steps whose loads are in flight together
 constexpr int MAX_SPLIT = 8;   // CTAs of a cluster
 
 struct TailRow {
-  float time, limit;
+  float time, limit, slope2;
   int doc, opens;              // opens: bit r set where key segment r is open to it
 };
 
@@ -53,6 +53,23 @@ template <typename T> struct Raw8 {
   }
 };
 
+// Sums over the LANES lanes of a key, of P values each; lane `part` ends with values part * P / LANES and following.
+template <int LANES, int P> __device__ __forceinline__ void scatter_sums(float (&v)[P], int part) {
+  if constexpr (LANES > 1) {
+    constexpr int H = P / 2;
+    const bool upper = (part & (LANES / 2)) != 0;
+    float keep[H];
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      const float mine = upper ? v[H + i] : v[i], other = upper ? v[i] : v[H + i];
+      keep[i] = mine + __shfl_xor_sync(0xffffffffu, other, LANES / 2);
+    }
+    scatter_sums<LANES / 2, H>(keep, part);
+#pragma unroll
+    for (int i = 0; i < P / LANES; ++i) v[i] = keep[i];
+  }
+}
+
 template <typename T, int HD, int R, bool RULE>
 __global__ void __launch_bounds__(THREADS, R <= 3 ? 2 : 1)
 scored_tail_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const int split) {
@@ -69,13 +86,14 @@ scored_tail_kernel(const __grid_constant__ Geometry g, const __grid_constant__ S
   ptx::grid_dep_launch();
 
   if (tid < R) {
-    TailRow t = {0.f, -INFINITY, 0, 0};
+    TailRow t = {0.f, -INFINITY, 0.f, 0, 0};
     if (tid < n_rows) {
       const int p = tid / a.group, s = (p >= a.q_off[2]) ? 2 : (p >= a.q_off[1]) ? 1 : 0, i = p - a.q_off[s];
       const QueryRows rows = query_rows(g, a, b, s);
       if (i >= rows.lo && i < rows.hi) {
         t.time = time_of(g, a, b, s, i + rows.shift);
         t.limit = latest_seen(a, b, t.time);
+        t.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + tid % a.group] * LOG2E : 0.f;
         t.doc = document_of(g, a, b, s, i + rows.shift);
         t.opens = (int)(g.allowed >> (3 * s)) & 7;
       }
@@ -86,110 +104,133 @@ scored_tail_kernel(const __grid_constant__ Geometry g, const __grid_constant__ S
   int opens = 0;
 #pragma unroll
   for (int i = 0; i < R; ++i) opens |= s_row[i].opens;
-  int n[3];
-#pragma unroll
-  for (int r = 0; r < 3; ++r) n[r] = ((opens >> r) & 1) ? valid_rows(g, b, r) : 0;
-  const int total = n[0] + n[1] + n[2];
-  // this CTA's keys of those, in whole steps of the CTA
-  constexpr int CTA_STEP = WARPS * KEYS * STEPS;
-  const int share = ((total + split - 1) / split + KEYS - 1) / KEYS * KEYS, first = min(total, rank * share), last = min(total, first + share);
 
-  float q[R][8], acc[R][8], m[R], l[R];
+  float2 q[R][4], acc[R][4];
+  float m[R], l[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q[i][e] = acc[i][e] = 0.f;
+    float f[8] = {};
     m[i] = -INFINITY;
     l[i] = 0.f;
-    if (s_row[i].opens != 0) {
-      const int h = hk * a.group + i % a.group;
-      load_n(static_cast<const T*>(a.q) + ((int64_t)b * a.Lq + i / a.group) * a.ldq + (int64_t)h * HD + 8 * part, q[i]);
+    if (s_row[i].opens != 0) load_n(static_cast<const T*>(a.q) + ((int64_t)b * a.Lq + i / a.group) * a.ldq + (int64_t)(hk * a.group + i % a.group) * HD + 8 * part, f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      q[i][e] = make_float2(f[2 * e], f[2 * e + 1]);
+      acc[i][e] = make_float2(0.f, 0.f);
     }
   }
-  float slope2[R];
-#pragma unroll
-  for (int i = 0; i < R; ++i) slope2[i] = RULE && a.slopes != nullptr && i < n_rows ? a.slopes[hk * a.group + i % a.group] * LOG2E : 0.f;
 
-  const T* const k0 = static_cast<const T*>(a.k) + (int64_t)b * g.L * a.ldk + (int64_t)hk * HD + 8 * part;
-  const T* const v0 = static_cast<const T*>(a.v) + (int64_t)b * g.L * a.ldv + (int64_t)hk * HD + 8 * part;
-  for (int t0 = first + warp * KEYS * STEPS; t0 < last; t0 += CTA_STEP) {
-    Raw8<T> k[STEPS], v[STEPS];
-    float time[STEPS], x[R][STEPS];
-    int seg[STEPS], doc[STEPS];
+  // Of the STEPS * R scores of a step's keys, score c = u R + i, each lane of a key turns SHARE dots into scores: which ones never changes.
+  constexpr int C = STEPS * R, SHARE = (C + LANES - 1) / LANES;
+  int key_of[SHARE];
+  TailRow row_of[SHARE];
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) {
-      const int t = t0 + u * KEYS + lane / LANES;
-      seg[u] = t >= last ? 3 : t >= n[0] + n[1] ? 2 : t >= n[0] ? 1 : 0;
-      const int j = seg[u] == 2 ? t - n[0] - n[1] : seg[u] == 1 ? t - n[0] : t;
-      const int pos = (seg[u] == 2 ? g.seg_off[2] : seg[u] == 1 ? g.seg_off[1] : g.seg_off[0]) + j;
-      time[u] = 0.f;
-      doc[u] = 0;
-      k[u].clear();
-      v[u].clear();
-      if (seg[u] < 3) {
-        k[u].load(k0 + (int64_t)pos * a.ldk);
-        v[u].load(v0 + (int64_t)pos * a.ldv);
-        if (RULE) {
-          time[u] = a.times != nullptr ? a.times[(int64_t)b * g.L + pos] : (float)j;
-          doc[u] = a.documents != nullptr ? a.documents[(int64_t)b * g.L + pos] : 0;
+  for (int c = 0; c < SHARE; ++c) {
+    const int at = min(part * SHARE + c, C - 1), u = at / R;
+    key_of[c] = u * KEYS + lane / LANES;
+    row_of[c] = s_row[at - u * R];
+    if (part * SHARE + c >= C) row_of[c].opens = 0;
+  }
+#pragma unroll 1
+  for (int r = 0; r < 3; ++r) {
+    const int n = ((opens >> r) & 1) ? valid_rows(g, b, r) : 0;
+    const int share = ((n + split - 1) / split + KEYS - 1) / KEYS * KEYS, first = min(n, rank * share), last = min(n, first + share);   // this CTA's keys
+    const int64_t row0 = (int64_t)b * g.L + g.off(r);
+    const float* const times = RULE && a.times != nullptr ? a.times + row0 : nullptr;
+    const int32_t* const docs = RULE && a.documents != nullptr ? a.documents + row0 : nullptr;
+    const int t_first = first + warp * KEYS * STEPS;
+    const T* kp = static_cast<const T*>(a.k) + (row0 + t_first + lane / LANES) * a.ldk + (int64_t)hk * HD + 8 * part;
+    const T* vp = static_cast<const T*>(a.v) + (row0 + t_first + lane / LANES) * a.ldv + (int64_t)hk * HD + 8 * part;
+#pragma unroll 1
+    for (int t0 = t_first; t0 < last; t0 += WARPS * KEYS * STEPS, kp += WARPS * KEYS * STEPS * a.ldk, vp += WARPS * KEYS * STEPS * a.ldv) {
+      Raw8<T> k[STEPS], v[STEPS];
+#pragma unroll
+      for (int u = 0; u < STEPS; ++u) {
+        k[u].clear();
+        v[u].clear();
+        if (t0 + u * KEYS + lane / LANES < last) {
+          k[u].load(kp + u * KEYS * a.ldk);
+          v[u].load(vp + u * KEYS * a.ldv);
         }
       }
-    }
+      float time[SHARE];
+      bool open[SHARE];
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) {
-      float f[8];
-      k[u].get(f);
+      for (int c = 0; c < SHARE; ++c) {
+        const int t = t0 + key_of[c];
+        open[c] = t < last && ((row_of[c].opens >> r) & 1);
+        time[c] = (float)t;
+        if (RULE && open[c]) {
+          if (times != nullptr) time[c] = times[t];
+          if (docs != nullptr) open[c] = docs[t] == row_of[c].doc;
+        }
+      }
+      float x[SHARE * LANES];
+#pragma unroll
+      for (int c = C; c < SHARE * LANES; ++c) x[c] = 0.f;
+#pragma unroll
+      for (int u = 0; u < STEPS; ++u) {
+        float f[8];
+        k[u].get(f);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          float2 d = __fmul2_rn(q[i][0], make_float2(f[0], f[1]));
+#pragma unroll
+          for (int e = 1; e < 4; ++e) d = __ffma2_rn(q[i][e], make_float2(f[2 * e], f[2 * e + 1]), d);
+          x[u * R + i] = d.x + d.y;
+        }
+      }
+      scatter_sums<LANES, SHARE * LANES>(x, part);
+#pragma unroll
+      for (int c = 0; c < SHARE; ++c) {
+        float d = x[c] * a.inner;
+        if (a.softcap > 0.f) d = tanh_any(d) * a.outer;
+        if (RULE) d -= row_of[c].slope2 * fabsf(row_of[c].time - time[c]);
+        x[c] = open[c] && (!RULE || time[c] <= row_of[c].limit) ? d : -INFINITY;
+      }
+      // every lane of the key gets all its scores back, to weigh its own features
+      float y[C];
+      bool all = true;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        y[c] = LANES == 1 ? x[c] : __shfl_sync(0xffffffffu, x[c % SHARE], (lane / LANES) * LANES + c / SHARE);
+        all = all && y[c] != -INFINITY;
+      }
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        float d = 0.f;
+        float top = m[i];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d += q[i][e] * f[e];
+        for (int u = 0; u < STEPS; ++u) top = fmaxf(top, y[u * R + i]);
+        if (__any_sync(0xffffffffu, top > m[i])) {
+          const float f = m[i] == -INFINITY ? 0.f : ptx::ex2(m[i] - top);
+          l[i] *= f;
 #pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-        x[i][u] = d * a.inner;
+          for (int e = 0; e < 4; ++e) acc[i][e] = __fmul2_rn(acc[i][e], make_float2(f, f));
+          m[i] = top;
+        }
+        const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) {
+          y[u * R + i] = ptx::ex2(y[u * R + i] - base);
+          l[i] += y[u * R + i];
+        }
       }
-    }
-    bool all = true;
-    uint32_t open = 0;   // bit R u + i
+      auto weigh = [&](bool whole) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const TailRow row = s_row[i];
-      float top = m[i];
+        for (int u = 0; u < STEPS; ++u) {
+          float f[8];
+          v[u].get(f);
 #pragma unroll
-      for (int u = 0; u < STEPS; ++u) {
-        float d = x[i][u];
-        if (a.softcap > 0.f) d = tanh_any2(make_float2(d, d)).x * a.outer;
-        if (RULE) d -= slope2[i] * fabsf(row.time - time[u]);
-        const bool is = ((row.opens >> seg[u]) & 1) && (!RULE || (time[u] <= row.limit && doc[u] == row.doc));   // bit 3 is never set
-        x[i][u] = is ? d : -INFINITY;
-        open |= is ? 1u << (R * u + i) : 0u;
-        all = all && is;
-        top = fmaxf(top, x[i][u]);
-      }
-      if (__any_sync(0xffffffffu, top > m[i])) {
-        const float f = m[i] == -INFINITY ? 0.f : ptx::ex2(m[i] - top);
-        l[i] *= f;
+          for (int i = 0; i < R; ++i) {
+            const float p = y[u * R + i];
+            if (whole || p != 0.f)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[i][e] *= f;
-        m[i] = top;
-      }
-      const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-      for (int u = 0; u < STEPS; ++u) {
-        x[i][u] = ptx::ex2(x[i][u] - base);
-        l[i] += x[i][u];
-      }
-    }
-    const bool whole = __all_sync(0xffffffffu, all);
-#pragma unroll
-    for (int u = 0; u < STEPS; ++u) {
-      float f[8];
-      v[u].get(f);
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-        if (whole || (open >> (R * u + i) & 1u))   // what stands in a closed key's value must not count, not even times zero
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[i][e] += x[i][u] * f[e];
+              for (int e = 0; e < 4; ++e) acc[i][e] = __ffma2_rn(make_float2(p, p), make_float2(f[2 * e], f[2 * e + 1]), acc[i][e]);
+          }
+        }
+      };
+      if (__all_sync(0xffffffffu, all)) weigh(true);
+      else weigh(false);   // what stands in a closed key's value must not count, not even times zero
     }
   }
 
@@ -205,7 +246,7 @@ scored_tail_kernel(const __grid_constant__ Geometry g, const __grid_constant__ S
     for (int o = LANES; o < 32; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float v = m[i] == -INFINITY ? 0.f : acc[i][e] * f;
+      float v = m[i] == -INFINITY ? 0.f : (e & 1 ? acc[i][e / 2].y : acc[i][e / 2].x) * f;
 #pragma unroll
       for (int o = LANES; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
       if (lane < LANES) s_acc[warp][i][8 * part + e] = v;
@@ -292,9 +333,9 @@ cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st
   int n_sm = 0;
   const cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
   if (e != cudaSuccess) return e;
-  // CTAs per (sample, key head): until there are four for every SM, as long as each still gets a turn of its warps
+  // CTAs per (sample, key head): until every SM has one, as long as each still gets two turns of its warps
   int split = 1;
-  while (split < MAX_SPLIT && (int64_t)g.batch * a.kv_heads * split < 4LL * n_sm && g.L > 2 * split * WARPS * STEPS * (256 / HD)) split *= 2;
+  while (split < MAX_SPLIT && (int64_t)g.batch * a.kv_heads * split < n_sm && g.L > 2 * split * WARPS * STEPS * (256 / HD)) split *= 2;
   const int rows = a.Lq * a.group;
   return rows <= 1   ? launch_rows<T, HD, 1>(g, a, split, st)
          : rows <= 3 ? launch_rows<T, HD, 3>(g, a, split, st)

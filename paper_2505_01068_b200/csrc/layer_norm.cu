@@ -13,6 +13,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MAX_PARTIALS = 1024;   // CTAs of the backward kernel at most (workspace)
+constexpr int FWD_CTAS_PER_SM = 16;
 
 template <int G>
 struct GroupSum {
@@ -39,65 +40,82 @@ struct GroupSum {
   }
 };
 
+// Rows that a group has in flight together: four or two where a row is one or two loads of each thread.
+template <int NV, int VEC> constexpr int ROWS_AT_ONCE = NV * VEC <= 4 ? 4 : NV * VEC <= 8 ? 2 : 1;
+
+// Whether row `row` is a real position (32-bit division: a call's rows are fewer than 2^29).
+__device__ __forceinline__ bool real_row(const Geometry& g, int row) {
+  const int b = (uint32_t)row / (uint32_t)g.L, l = row - b * g.L, s = segment_of(g, l);
+  return l - g.off(s) < valid_rows(g, b, s);
+}
+
 template <typename TX, typename TY, int VEC, int G, int NV>
 __global__ void __launch_bounds__(THREADS)
 layer_norm_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ NormCall c) {
   __shared__ float2 sums[THREADS / 32];
-  constexpr int GROUPS = THREADS / G;
-  const int group = threadIdx.x / G, t = threadIdx.x % G;
-  const int64_t rows = (int64_t)g.batch * g.L;
+  constexpr int GROUPS = THREADS / G, U = G > 32 ? 1 : ROWS_AT_ONCE<NV, VEC>;
+  const int group = threadIdx.x / G, t = threadIdx.x % G, rows = g.batch * g.L;
   ptx::load_params_early(g, c);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   const float inv_d = 1.0f / g.d;
-  // whole groups of a warp run together: the row index is clamped, and only real groups store
-  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
-    const int64_t row = first + group;
-    const bool in = row < rows, real = in && row_is_real(g, row);
-    float x[NV][VEC];
-    const TX* src = static_cast<const TX*>(c.x) + (in ? row : 0) * c.ldx;
-    float2 s = make_float2(0.f, 0.f);
+  // whole groups of a warp run together: rows past the last are walked, too, without loads or stores
+  for (int first = blockIdx.x * GROUPS * U; first < rows; first += gridDim.x * GROUPS * U) {
+    float x[U][NV][VEC];
+    bool real[U];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * G + t) * VEC;
+    for (int u = 0; u < U; ++u) {
+      const int row = first + u * GROUPS + group;
+      real[u] = row < rows && real_row(g, row);
+      const TX* src = static_cast<const TX*>(c.x) + (int64_t)row * c.ldx;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[v][e] = 0.f;
-      if (real && col < g.d) load_n(src + col, x[v]);
+      for (int v = 0; v < NV; ++v) {
+        const int col = (v * G + t) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][v][e] = 0.f;
+        if (real[u] && col < g.d) load_n(src + col, x[u][v]);
+      }
     }
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int u = 0; u < U; ++u) {
+      const int row = first + u * GROUPS + group;
+      float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s.x += x[v][e];
-    const float mean = GroupSum<G>::run(s, sums).x * inv_d;
-    s = make_float2(0.f, 0.f);
+      for (int v = 0; v < NV; ++v)
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+        for (int e = 0; e < VEC; ++e) s.x += x[u][v][e];
+      const float mean = GroupSum<G>::run(s, sums).x * inv_d;
+      s = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float z = (v * G + t) * VEC < g.d ? x[v][e] - mean : 0.f;
-        s.x += z * z;
-      }
-    const float rstd = rsqrtf(GroupSum<G>::run(s, sums).x * inv_d + c.eps);
-    if (!in) continue;
-    TY* dst = static_cast<TY*>(c.y) + row * c.ldy;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * G + t) * VEC;
-      if (col < g.d) {
-        float ga[VEC], be[VEC], y[VEC];
-        if (c.gamma != nullptr) load_n(c.gamma + col, ga);
-        if (c.beta != nullptr) load_n(c.beta + col, be);
+      for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          const float h = (x[v][e] - mean) * rstd, scaled = c.gamma != nullptr ? h * ga[e] : h;
-          y[e] = real ? (c.beta != nullptr ? scaled + be[e] : scaled) : 0.f;
+          const float z = (v * G + t) * VEC < g.d ? x[u][v][e] - mean : 0.f;
+          s.x += z * z;
         }
-        store_n(dst + col, y);
+      const float rstd = rsqrtf(GroupSum<G>::run(s, sums).x * inv_d + c.eps);
+      if (row < rows) {
+        TY* dst = static_cast<TY*>(c.y) + (int64_t)row * c.ldy;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int col = (v * G + t) * VEC;
+          if (col < g.d) {
+            float ga[VEC], be[VEC], y[VEC];
+            if (c.gamma != nullptr) load_n(c.gamma + col, ga);
+            if (c.beta != nullptr) load_n(c.beta + col, be);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              const float h = (x[u][v][e] - mean) * rstd, scaled = c.gamma != nullptr ? h * ga[e] : h;
+              y[e] = real[u] ? (c.beta != nullptr ? scaled + be[e] : scaled) : 0.f;
+            }
+            store_n(dst + col, y);
+          }
+        }
+        if (t == 0 && c.mean != nullptr) {
+          c.mean[row] = real[u] ? mean : 0.f;
+          c.rstd[row] = real[u] ? rstd : 0.f;
+        }
       }
-    }
-    if (t == 0 && c.mean != nullptr) {
-      c.mean[row] = real ? mean : 0.f;
-      c.rstd[row] = real ? rstd : 0.f;
     }
   }
 }
@@ -106,61 +124,72 @@ template <typename TX, typename TY, int VEC, int G, int NV>
 __global__ void __launch_bounds__(THREADS)
 layer_norm_bwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ NormCall c) {
   __shared__ float2 sums[THREADS / 32];
-  constexpr int GROUPS = THREADS / G;
-  const int group = threadIdx.x / G, t = threadIdx.x % G;
-  const int64_t rows = (int64_t)g.batch * g.L;
+  constexpr int GROUPS = THREADS / G, U = G > 32 ? 1 : (ROWS_AT_ONCE<NV, VEC> + 1) / 2;
+  const int group = threadIdx.x / G, t = threadIdx.x % G, rows = g.batch * g.L;
   ptx::load_params_early(g, c);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   const float inv_d = 1.0f / g.d;
   float dga[NV][VEC] = {}, dbe[NV][VEC] = {};
-  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
-    const int64_t row = first + group;
-    const bool in = row < rows, real = in && row_is_real(g, row);
-    const int64_t at = in ? row : 0;
-    float x[NV][VEC], dy[NV][VEC], res[NV][VEC];
-    const float mean = c.mean[at], rstd = c.rstd[at];
+  for (int first = blockIdx.x * GROUPS * U; first < rows; first += gridDim.x * GROUPS * U) {
+    float x[U][NV][VEC], dy[U][NV][VEC], res[U][NV][VEC], mean[U], rstd[U];
+    bool real[U];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * G + t) * VEC;
+    for (int u = 0; u < U; ++u) {
+      const int row = first + u * GROUPS + group;
+      real[u] = row < rows && real_row(g, row);
+      mean[u] = rstd[u] = 0.f;
+      if (real[u]) {
+        mean[u] = c.mean[row];
+        rstd[u] = c.rstd[row];
+      }
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[v][e] = dy[v][e] = res[v][e] = 0.f;
-      if (real && col < g.d) {
-        load_n(static_cast<const TX*>(c.x) + at * c.ldx + col, x[v]);
-        load_n(static_cast<const TY*>(c.dy) + at * c.lddy + col, dy[v]);
-        if (c.residual != nullptr) load_n(static_cast<const TX*>(c.residual) + at * c.ldres + col, res[v]);
+      for (int v = 0; v < NV; ++v) {
+        const int col = (v * G + t) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][v][e] = dy[u][v][e] = res[u][v][e] = 0.f;
+        if (real[u] && col < g.d) {
+          load_n(static_cast<const TX*>(c.x) + (int64_t)row * c.ldx + col, x[u][v]);
+          load_n(static_cast<const TY*>(c.dy) + (int64_t)row * c.lddy + col, dy[u][v]);
+          if (c.residual != nullptr) load_n(static_cast<const TX*>(c.residual) + (int64_t)row * c.ldres + col, res[u][v]);
+        }
       }
     }
-    float2 s = make_float2(0.f, 0.f);   // sums of g and of g h
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * G + t) * VEC;
-      float ga[VEC];
-      const bool scaled = c.gamma != nullptr && col < g.d;
-      if (scaled) load_n(c.gamma + col, ga);
+    for (int u = 0; u < U; ++u) {
+      const int row = first + u * GROUPS + group;
+      float2 s = make_float2(0.f, 0.f);   // sums of g and of g h
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float h = real ? (x[v][e] - mean) * rstd : 0.f;
-        dga[v][e] += dy[v][e] * h;
-        dbe[v][e] += dy[v][e];
-        x[v][e] = h;
-        dy[v][e] = scaled ? dy[v][e] * ga[e] : dy[v][e];
-        s.x += dy[v][e];
-        s.y += dy[v][e] * h;
+      for (int v = 0; v < NV; ++v) {
+        const int col = (v * G + t) * VEC;
+        float ga[VEC];
+        const bool scaled = c.gamma != nullptr && col < g.d;
+        if (scaled) load_n(c.gamma + col, ga);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float h = (x[u][v][e] - mean[u]) * rstd[u];   // columns past the last meet a dy of zero
+          dga[v][e] += dy[u][v][e] * h;
+          dbe[v][e] += dy[u][v][e];
+          x[u][v][e] = h;
+          dy[u][v][e] = scaled ? dy[u][v][e] * ga[e] : dy[u][v][e];
+          s.x += dy[u][v][e];
+          s.y += dy[u][v][e] * h;
+        }
       }
-    }
-    s = GroupSum<G>::run(s, sums);
-    if (!in) continue;
-    const float m1 = s.x * inv_d, m2 = s.y * inv_d;
-    TX* dst = static_cast<TX*>(c.dx) + row * c.lddx;
+      s = GroupSum<G>::run(s, sums);
+      if (row < rows) {
+        const float m1 = s.x * inv_d, m2 = s.y * inv_d;
+        TX* dst = static_cast<TX*>(c.dx) + (int64_t)row * c.lddx;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * G + t) * VEC;
-      if (col < g.d) {
-        float dx[VEC];
+        for (int v = 0; v < NV; ++v) {
+          const int col = (v * G + t) * VEC;
+          if (col < g.d) {
+            float dx[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) dx[e] = real ? (dy[v][e] - m1 - x[v][e] * m2) * rstd + res[v][e] : 0.f;
-        store_n(dst + col, dx);
+            for (int e = 0; e < VEC; ++e) dx[e] = real[u] ? (dy[u][v][e] - m1 - x[u][v][e] * m2) * rstd[u] + res[u][v][e] : 0.f;
+            store_n(dst + col, dx);
+          }
+        }
       }
     }
   }
@@ -286,7 +315,10 @@ size_t layer_norm_bwd_scratch(const Geometry& g) { return sizeof(float) * 2 * (s
 cudaError_t launch_layer_norm_fwd(const Geometry& g, const NormCall& c, cudaStream_t st) {
   const bool wide = g.d % 4 == 0 && vectors(c.x, c.ldx, c.x_dtype) && vectors(c.y, c.ldy, c.y_dtype) && vectors(c.gamma, 0, GSIT_F32) &&
                     vectors(c.beta, 0, GSIT_F32);
-  return launch_any<1>(g, c, wide, (unsigned)row_groups(g), st);
+  int n_sm = 0;
+  const cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
+  if (e != cudaSuccess) return e;
+  return launch_any<1>(g, c, wide, (unsigned)min(row_groups(g), (int64_t)FWD_CTAS_PER_SM * n_sm), st);
 }
 
 cudaError_t launch_layer_norm_bwd(const Geometry& g, const NormCall& c, cudaStream_t st) {

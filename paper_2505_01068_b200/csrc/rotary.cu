@@ -46,28 +46,37 @@ rotary_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Rotary
   constexpr int E = 16 / sizeof(T);                         // elements of a piece
   constexpr int BATCH = FORM == SCALAR ? 1 : FORM == SPLIT ? 2 : 4;   // units whose loads are in flight together
   __shared__ float2 table[THREADS];                         // (cos, sin) of row r, pair p at [r * pairs + p]
-  __shared__ int real[THREADS];                             // per row
   const int tid = threadIdx.x;
   const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_cta;
   const int here = (int)min((int64_t)a.rows_per_cta, (int64_t)g.batch * g.L - row0);
+  const int b0 = (int)(row0 / g.L), l0 = (int)(row0 - (int64_t)b0 * g.L);
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
 
-  if (tid < here * a.pairs) {
-    const int r = tid / a.pairs, p = tid - r * a.pairs;
-    const int64_t row = row0 + r;
-    const int b = (int)(row / g.L), l = (int)(row - (int64_t)b * g.L), s = segment_of(g, l);
-    const int axis = (p >= a.axis2) ? 2 : (p >= a.axis1) ? 1 : 0;
-    const double t = (double)a.positions[axis * a.axis_stride + b * a.batch_stride + l] * a.turns[p];
-    float sn, cs;
-    sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
-    table[tid] = make_float2(cs, a.sign * sn);
-    if (p == 0) real[r] = l - g.off(s) < valid_rows(g, b, s);
-  }
-  __syncthreads();
-
-  struct Place { int64_t src, dst; int row, k, unit; };   // element offsets of the head's first feature
+  // sample and position of the CTA's row r
+  auto locate = [&](int r, int& b, int& l) {
+    b = b0;
+    l = l0 + r;
+    if (l >= g.L) {
+      b += l / g.L;
+      l %= g.L;
+    }
+  };
+  auto angles = [&] {
+    if (tid < here * a.pairs) {
+      const int r = tid / a.pairs, p = tid - r * a.pairs;
+      int b, l;
+      locate(r, b, l);
+      const int axis = (p >= a.axis2) ? 2 : (p >= a.axis1) ? 1 : 0;
+      const double t = (double)a.positions[axis * a.axis_stride + b * a.batch_stride + l] * a.turns[p];
+      float sn, cs;
+      sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
+      table[tid] = make_float2(cs, a.sign * sn);
+    }
+    __syncthreads();
+  };
+  struct Place { int64_t src, dst; int row, k, unit; bool real; };   // element offsets of the head's first feature
   auto place = [&](int u) {
     Place p;
     p.row = FORM == SCALAR ? u / a.row_units : div_magic(u, a.row_units, a.row_magic);
@@ -78,49 +87,58 @@ rotary_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Rotary
     if (p.k) head -= a.q_heads;
     p.src = (row0 + p.row) * (p.k ? a.in_stride[1] : a.in_stride[0]) + (int64_t)head * g.hd;
     p.dst = (row0 + p.row) * (p.k ? a.out_stride[1] : a.out_stride[0]) + (int64_t)head * g.hd;
+    int b, l;
+    locate(p.row, b, l);
+    const int s = segment_of(g, l);
+    p.real = l - g.off(s) < valid_rows(g, b, s);
     return p;
   };
   auto src = [&](const Place& p) { return static_cast<const T*>(p.k ? a.in[1] : a.in[0]) + p.src; };
   auto dst = [&](const Place& p) { return static_cast<T*>(p.k ? a.out[1] : a.out[0]) + p.dst; };
   const int n_units = here * a.row_units;
 
-  for (int u0 = tid; u0 < n_units; u0 += THREADS * BATCH) {
-    if constexpr (FORM == SCALAR) {
-      const Place p = place(u0);
-      const bool keep = real[p.row];
+  if constexpr (FORM == SCALAR) {
+    angles();
+    for (int u = tid; u < n_units; u += THREADS) {
+      const Place p = place(u);
       const T* x = src(p);
       T* y = dst(p);
       if (p.unit >= a.pairs) {
         const int f = a.pairs + p.unit;
-        store_as(y + f, keep ? to_float(x[f]) : 0.f);
+        store_as(y + f, p.real ? to_float(x[f]) : 0.f);
       } else {
         const int i = a.adjacent ? 2 * p.unit : p.unit, j = a.adjacent ? i + 1 : a.pairs + i;
         const float2 cs = table[p.row * a.pairs + p.unit];
-        const float lo = keep ? to_float(x[i]) : 0.f, hi = keep ? to_float(x[j]) : 0.f;
-        store_as(y + i, keep ? lo * cs.x - hi * cs.y : 0.f);
-        store_as(y + j, keep ? lo * cs.y + hi * cs.x : 0.f);
+        const float lo = p.real ? to_float(x[i]) : 0.f, hi = p.real ? to_float(x[j]) : 0.f;
+        store_as(y + i, p.real ? lo * cs.x - hi * cs.y : 0.f);
+        store_as(y + j, p.real ? lo * cs.y + hi * cs.x : 0.f);
       }
-    } else {
+    }
+  } else {
+    // the first units' loads are under way while the angles are computed
+    for (int u0 = tid, turn = 0; turn == 0 || u0 < n_units; u0 += THREADS * BATCH, ++turn) {
       Place p[BATCH];
       float v[BATCH][E], w[FORM == SPLIT ? BATCH : 1][E];
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) {
         const int u = u0 + i * THREADS;
-        p[i] = place(u < n_units ? u : u0);
-        if (u < n_units && real[p[i].row]) {
-          load_n(src(p[i]) + p[i].unit * E, v[i]);
-          if constexpr (FORM == SPLIT) load_n(src(p[i]) + a.pairs + p[i].unit * E, w[i]);
+        if (u < n_units) {
+          p[i] = place(u);
+          if (p[i].real) {
+            load_n(src(p[i]) + p[i].unit * E, v[i]);
+            if constexpr (FORM == SPLIT) load_n(src(p[i]) + a.pairs + p[i].unit * E, w[i]);
+          }
         }
       }
+      if (turn == 0) angles();
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) {
         if (u0 + i * THREADS >= n_units) break;
         float y[E], z[E];
-        const bool keep = real[p[i].row];
         const float2* t = table + p[i].row * a.pairs + (FORM == SPLIT ? p[i].unit * E : FORM == ADJACENT ? p[i].unit * (E / 2) : 0);
 #pragma unroll
         for (int e = 0; e < E; ++e) y[e] = z[e] = 0.f;
-        if (keep) {
+        if (p[i].real) {
           if constexpr (FORM == SPLIT) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {

@@ -8,7 +8,7 @@
 // CTAs that share a (sample, key head) through the shared memory of a cluster, in a fixed order.
 #include <cooperative_groups.h>
 
-#include "scored.cuh"
+#include "scored_tile.cuh"
 
 namespace gsit {
 namespace {
@@ -23,6 +23,100 @@ struct TailRow {
   float time, limit, slope2;
   int doc, opens;              // opens: bit r set where key segment r is open to it
 };
+
+// What the parts of a row's softmax are joined through.
+template <int HD, int R> struct JoinRoom {
+  float acc[WARPS][R][HD], joined[R][HD];
+  float2 ml[WARPS][R], joined_ml[R];   // (maximum, sum); a part without a key has a maximum of -inf and takes no part
+  float scale[MAX_SPLIT > WARPS ? MAX_SPLIT : WARPS][R];
+};
+// acc and ml hold the warps' parts: adds them up, and those of the cluster's CTAs, in order; CTA 0 writes the results.  Whole CTAs.
+template <typename T, int HD, int R>
+__device__ __forceinline__ void join_warps_and_ctas(const Geometry& g, const ScoredArgs& a, JoinRoom<HD, R>& room, int b, int hk, int rank, int split, int n_rows) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid < R) {
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, room.ml[w][tid].x);
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float f = room.ml[w][tid].x == -INFINITY ? 0.f : ptx::ex2(room.ml[w][tid].x - top);
+      room.scale[w][tid] = f;
+      sum += f * room.ml[w][tid].y;
+    }
+    room.joined_ml[tid] = make_float2(top, sum);
+  }
+  __syncthreads();
+  for (int c = tid; c < R * HD; c += THREADS) {
+    const int i = c / HD, f = c % HD;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w)
+      if (room.scale[w][i] != 0.f) v += room.scale[w][i] * room.acc[w][i][f];
+    room.joined[i][f] = v;
+  }
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  if (rank == 0) {
+    if (tid < R) {
+      float top = -INFINITY, sum = 0.f;
+      float2 ml[MAX_SPLIT];
+      for (int c = 0; c < split; ++c) {
+        ml[c] = cluster.map_shared_rank(room.joined_ml, c)[tid];
+        top = fmaxf(top, ml[c].x);
+      }
+      for (int c = 0; c < split; ++c) {
+        const float f = ml[c].x == -INFINITY ? 0.f : ptx::ex2(ml[c].x - top);
+        room.scale[c][tid] = f;
+        sum += f * ml[c].y;
+      }
+      room.ml[0][tid] = make_float2(top, sum);
+    }
+    __syncthreads();
+    bool broken = false;
+    for (int c = tid; c < n_rows * HD; c += THREADS) {
+      const int i = c / HD, f = c % HD;
+      float v = 0.f;
+      for (int k = 0; k < split; ++k)
+        if (room.scale[k][i] != 0.f) v += room.scale[k][i] * cluster.map_shared_rank(&room.joined[0][0], k)[c];
+      const float sum = room.ml[0][i].y, o = sum != 0.f ? v / sum : 0.f;
+      broken = broken || (__float_as_uint(o) & 0x7f800000u) == 0x7f800000u;
+      store_as(static_cast<T*>(a.out) + ((int64_t)b * a.Lq + i / a.group) * a.ldo + (int64_t)(hk * a.group + i % a.group) * HD + f, o);
+    }
+    if (a.lse != nullptr && tid < n_rows) {
+      const float2 ml = room.ml[0][tid];
+      a.lse[((int64_t)b * g.heads + hk * a.group + tid % a.group) * a.Lq + tid / a.group] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * LN2 : -INFINITY;
+    }
+    // zero times NaN or Inf of a closed key: the rows once more, pair by pair
+    if (__syncthreads_or(broken))
+      for (int i = tid >> 5; i < n_rows; i += WARPS) {
+        const int p = i / a.group, s = (p >= a.q_off[2]) ? 2 : (p >= a.q_off[1]) ? 1 : 0;
+        attend_row<T>(g, a, b, hk * a.group + i % a.group, s, p - a.q_off[s]);
+      }
+  }
+  cluster.sync();   // nobody's shared memory goes away while it is read
+}
+
+// The sample's query rows that read key head hk: row i is query row i / group, head hk * group + i % group.
+template <int R> __device__ __forceinline__ void find_rows(const Geometry& g, const ScoredArgs& a, int b, int hk, int n_rows, TailRow (&row)[R]) {
+  const int i = threadIdx.x;
+  if (i < R) {
+    TailRow t = {0.f, -INFINITY, 0.f, 0, 0};
+    if (i < n_rows) {
+      const int p = i / a.group, s = (p >= a.q_off[2]) ? 2 : (p >= a.q_off[1]) ? 1 : 0, at = p - a.q_off[s];
+      const QueryRows rows = query_rows(g, a, b, s);
+      if (at >= rows.lo && at < rows.hi) {
+        t.time = time_of(g, a, b, s, at + rows.shift);
+        t.limit = latest_seen(a, b, t.time);
+        t.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + i % a.group] * LOG2E : 0.f;
+        t.doc = document_of(g, a, b, s, at + rows.shift);
+        t.opens = (int)(g.allowed >> (3 * s)) & 7;
+      }
+    }
+    row[i] = t;
+  }
+}
 
 // 8 elements of a row as they lie in memory.
 template <typename T> struct Raw8 {
@@ -71,35 +165,19 @@ template <int LANES, int P> __device__ __forceinline__ void scatter_sums(float (
 }
 
 template <typename T, int HD, int R, bool RULE>
-__global__ void __launch_bounds__(THREADS, R <= 3 ? 2 : 1)
+__global__ void __launch_bounds__(THREADS, R == 1 ? 2 : 1)
 scored_tail_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const int split) {
   constexpr int LANES = HD / 8, KEYS = 32 / LANES;   // lanes of a key, keys of a step
   __shared__ TailRow s_row[R];
-  __shared__ __align__(16) float s_acc[WARPS][R][HD], s_joined[R][HD];
-  __shared__ float2 s_ml[WARPS][R], s_joined_ml[R];
-  __shared__ float s_scale[MAX_SPLIT > WARPS ? MAX_SPLIT : WARPS][R];
+  __shared__ JoinRoom<HD, R> room;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, part = lane % LANES;
   const int rank = blockIdx.x % split, hk = blockIdx.x / split, b = blockIdx.y;
-  const int n_rows = a.Lq * a.group;                 // row i: query row i / group of the sample, head hk * group + i % group
+  const int n_rows = a.Lq * a.group;
   ptx::load_params_early(g, a, split);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
 
-  if (tid < R) {
-    TailRow t = {0.f, -INFINITY, 0.f, 0, 0};
-    if (tid < n_rows) {
-      const int p = tid / a.group, s = (p >= a.q_off[2]) ? 2 : (p >= a.q_off[1]) ? 1 : 0, i = p - a.q_off[s];
-      const QueryRows rows = query_rows(g, a, b, s);
-      if (i >= rows.lo && i < rows.hi) {
-        t.time = time_of(g, a, b, s, i + rows.shift);
-        t.limit = latest_seen(a, b, t.time);
-        t.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + tid % a.group] * LOG2E : 0.f;
-        t.doc = document_of(g, a, b, s, i + rows.shift);
-        t.opens = (int)(g.allowed >> (3 * s)) & 7;
-      }
-    }
-    s_row[tid] = t;
-  }
+  find_rows<R>(g, a, b, hk, n_rows, s_row);
   __syncthreads();
   int opens = 0;
 #pragma unroll
@@ -249,73 +327,185 @@ scored_tail_kernel(const __grid_constant__ Geometry g, const __grid_constant__ S
       float v = m[i] == -INFINITY ? 0.f : (e & 1 ? acc[i][e / 2].y : acc[i][e / 2].x) * f;
 #pragma unroll
       for (int o = LANES; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (lane < LANES) s_acc[warp][i][8 * part + e] = v;
+      if (lane < LANES) room.acc[warp][i][8 * part + e] = v;
     }
-    if (lane == 0) s_ml[warp][i] = make_float2(top, l[i]);
+    if (lane == 0) room.ml[warp][i] = make_float2(top, l[i]);
   }
-  __syncthreads();
-  if (tid < R) {
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, s_ml[w][tid].x);
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      const float f = s_ml[w][tid].x == -INFINITY ? 0.f : ptx::ex2(s_ml[w][tid].x - top);
-      s_scale[w][tid] = f;
-      sum += f * s_ml[w][tid].y;
-    }
-    s_joined_ml[tid] = make_float2(top, sum);
-  }
-  __syncthreads();
-  for (int c = tid; c < R * HD; c += THREADS) {
-    const int i = c / HD, f = c % HD;
-    float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w)
-      if (s_scale[w][i] != 0.f) v += s_scale[w][i] * s_acc[w][i][f];
-    s_joined[i][f] = v;
-  }
-  cg::cluster_group cluster = cg::this_cluster();
-  cluster.sync();
-  if (rank == 0) {
-    if (tid < R) {
-      float top = -INFINITY, sum = 0.f;
-      float2 ml[MAX_SPLIT];
-      for (int c = 0; c < split; ++c) {
-        ml[c] = cluster.map_shared_rank(s_joined_ml, c)[tid];
-        top = fmaxf(top, ml[c].x);
-      }
-      for (int c = 0; c < split; ++c) {
-        const float f = ml[c].x == -INFINITY ? 0.f : ptx::ex2(ml[c].x - top);
-        s_scale[c][tid] = f;
-        sum += f * ml[c].y;
-      }
-      s_ml[0][tid] = make_float2(top, sum);
-    }
-    __syncthreads();
-    for (int c = tid; c < n_rows * HD; c += THREADS) {
-      const int i = c / HD, f = c % HD;
-      float v = 0.f;
-      for (int k = 0; k < split; ++k)
-        if (s_scale[k][i] != 0.f) v += s_scale[k][i] * cluster.map_shared_rank(&s_joined[0][0], k)[c];
-      const float sum = s_ml[0][i].y;
-      store_as(static_cast<T*>(a.out) + ((int64_t)b * a.Lq + i / a.group) * a.ldo + (int64_t)(hk * a.group + i % a.group) * HD + f, sum != 0.f ? v / sum : 0.f);
-    }
-    if (a.lse != nullptr && tid < n_rows) {
-      const float2 ml = s_ml[0][tid];
-      a.lse[((int64_t)b * g.heads + hk * a.group + tid % a.group) * a.Lq + tid / a.group] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * LN2 : -INFINITY;
-    }
-  }
-  cluster.sync();   // nobody's shared memory goes away while it is read
+  join_warps_and_ctas<T, HD, R>(g, a, room, b, hk, rank, split, n_rows);
 }
 
-template <typename T, int HD, int R>
-cudaError_t launch_rows(const Geometry& g, const ScoredArgs& a, int split, cudaStream_t st) {
-  const bool rule = rule_masks(a) || a.slopes != nullptr;
-  const auto kernel = rule ? scored_tail_kernel<T, HD, R, true> : scored_tail_kernel<T, HD, R, false>;
+// bf16 on mma.sync: a warp walks its own keys with all the rows (at most 8, the upper half of a fragment's 16) through a ring of its
+// own, so that nothing but its own copies is waited for.  110 instructions to 4 KB of keys and values, where lanes that hold features
+// took 600: what bounds it is the copies.
+template <int HD> struct TailRing {
+  static constexpr int KEYS = 1024 / HD;                                      // of a stage: 2 KB of keys, 2 KB of values
+  static constexpr int STAGES = 3, STAGE = 4096 + 8 * KEYS, BYTES = STAGES * STAGE;   // behind them the moments and documents
+};
+constexpr int TILE_ROWS = 8;
+
+template <int HD, bool CAP, bool RULE>
+__global__ void __launch_bounds__(THREADS, 2)
+scored_tail_tile_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const int split) {
+  using Ring = TailRing<HD>;
+  constexpr int KS = Ring::KEYS, CH = HD / 8, NT = HD == 8 ? 4 : 2;
+  extern __shared__ __align__(128) uint8_t s_ring[];
+  __shared__ TailRow s_row[TILE_ROWS];
+  const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31;
+  const int rank = blockIdx.x % split, hk = blockIdx.x / split, b = blockIdx.y, n_rows = a.Lq * a.group;
+  ptx::load_params_early(g, a, split);
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+  find_rows<TILE_ROWS>(g, a, b, hk, n_rows, s_row);
+  __syncthreads();
+  int opens = 0;
+#pragma unroll
+  for (int i = 0; i < TILE_ROWS; ++i) opens |= s_row[i].opens;
+  const TailRow own = s_row[lane >> 2];
+  uint32_t qf[1][(HD + 15) / 16][4];
+  own_rows<HD>(own.opens != 0 ? static_cast<const bf16*>(a.q) + ((int64_t)b * a.Lq + (lane >> 2) / a.group) * a.ldq + (int64_t)(hk * a.group + (lane >> 2) % a.group) * HD
+                              : nullptr, nullptr, lane, qf[0]);
+
+  // this warp's stages: every WARPS-th of the CTA's share of every segment
+  Walk ahead = {};
+  int first[3];
+#pragma unroll
+  for (int r = 0; r < 3; ++r) {
+    const int n = ((opens >> r) & 1) ? valid_rows(g, b, r) : 0, share = ((n + split - 1) / split + KS - 1) / KS * KS;
+    first[r] = min(n, rank * share) + warp * KS;
+    ahead.n[r] = min(n, min(n, rank * share) + share);
+  }
+  auto settle = [&](Walk& w) {
+    if (w.seg == 0 && w.pos >= w.n[0]) { w.seg = 1; w.pos = first[1]; }
+    if (w.seg == 1 && w.pos >= w.n[1]) { w.seg = 2; w.pos = first[2]; }
+    if (w.seg == 2 && w.pos >= w.n[2]) w.seg = 3;
+  };
+  ahead.pos = first[0];
+  settle(ahead);
+  Walk now = ahead;
+  const uint32_t ring = smem_u32(s_ring) + warp * Ring::BYTES;
+  // this lane's piece of a sample's row lane / CH
+  const bf16* const k0 = static_cast<const bf16*>(a.k) + ((int64_t)b * g.L + lane / CH) * a.ldk + (int64_t)hk * HD + 8 * (lane % CH);
+  const bf16* const v0 = static_cast<const bf16*>(a.v) + ((int64_t)b * g.L + lane / CH) * a.ldv + (int64_t)hk * HD + 8 * (lane % CH);
+  const int64_t k_step = 32 / CH * a.ldk, v_step = 32 / CH * a.ldv;
+  auto request = [&](Walk& w, int stage) {
+    if (!w.over()) {
+      const int rem = w.left(), row0 = (w.seg == 0 ? g.seg_off[0] : w.seg == 1 ? g.seg_off[1] : g.seg_off[2]) + w.pos;
+      const uint32_t at = ring + stage * Ring::STAGE;
+      const bf16 *kp = k0 + (int64_t)row0 * a.ldk, *vp = v0 + (int64_t)row0 * a.ldv;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {   // 32 lanes take 32 / CH rows at a time
+        const int row = lane / CH + i * (32 / CH);
+        const bool real = row < rem;    // past the last key: zeros, from an address that is one
+        cp16(at + piece_at<HD>(row, lane % CH), real ? kp : static_cast<const bf16*>(a.k), real);
+        cp16(at + 2048 + piece_at<HD>(row, lane % CH), real ? vp : static_cast<const bf16*>(a.v), real);
+        kp += k_step;
+        vp += v_step;
+      }
+      if (RULE)
+        for (int i = lane; i < KS; i += 32)
+          if (i < rem) {
+            const int64_t from = (int64_t)b * g.L + row0 + i;
+            if (a.times != nullptr) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at + 4096 + 4 * i), "l"(a.times + from) : "memory");
+            if (a.documents != nullptr) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at + 4096 + 4 * (KS + i)), "l"(a.documents + from) : "memory");
+          }
+      w.pos += WARPS * KS;
+      settle(w);
+    }
+    cp_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < Ring::STAGES - 1; ++i) request(ahead, i);
+
+  float o[1][CH][4], ref = -INFINITY;
+  float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[0][c][e] = 0.f;
+  const uint32_t as_n = lane_as_n<HD>(lane), as_k = 2048 + lane_as_k<HD>(lane);
+#pragma unroll 1
+  for (int stage = 0; !now.over(); stage = stage + 1 == Ring::STAGES ? 0 : stage + 1) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(Ring::STAGES - 2) : "memory");
+    __syncwarp();   // every lane's copies are there, and every lane is done with the stage that is filled next
+    request(ahead, stage == 0 ? Ring::STAGES - 1 : stage - 1);
+    const int rem = now.left();
+    const uint32_t at = ring + stage * Ring::STAGE;
+    const float* const times = reinterpret_cast<const float*>(s_ring + warp * Ring::BYTES + stage * Ring::STAGE + 4096);
+    const int* const docs = reinterpret_cast<const int*>(times + KS);
+    const bool mine = (own.opens >> now.seg) & 1;
+#pragma unroll 1
+    for (int j = 0; j < min(KS, rem); j += 8 * NT) {
+      float x[1][NT][4];
+      product_over_features<HD, 1, NT>(x, qf, at + as_n + j * HD * 2, from_zero);
+      uint32_t w[1][NT][2];
+      float top = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float2 y = __fmul2_rn(make_float2(x[0][n][0], x[0][n][1]), make_float2(a.inner, a.inner));
+        if constexpr (CAP) y = __fmul2_rn(tanh_any2(y), make_float2(a.outer, a.outer));
+        float z[2] = {y.x, y.y};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int col = j + 8 * n + 2 * (lane & 3) + e;
+          bool open = mine && col < rem;
+          if constexpr (RULE) {
+            const float t = a.times != nullptr ? times[col] : (float)(now.pos + col);
+            z[e] -= own.slope2 * fabsf(own.time - t);
+            open = open && t <= own.limit && (a.documents == nullptr || docs[col] == own.doc);
+          }
+          x[0][n][e] = open ? z[e] : -INFINITY;
+        }
+        top = ptx::fmax3(top, x[0][n][0], x[0][n][1]);
+      }
+      if (__any_sync(0xffffffffu, top > ref + 8.f)) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        if (top > ref) {
+          const float f = ptx::ex2(ref - top);
+          sum = __fmul2_rn(sum, make_float2(f, f));
+#pragma unroll
+          for (int c = 0; c < CH; ++c) {
+            o[0][c][0] *= f;
+            o[0][c][1] *= f;
+          }
+          ref = top;
+        }
+      }
+      const float r = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float2 y = __fadd2_rn(make_float2(x[0][n][0], x[0][n][1]), make_float2(r, r)), p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
+        sum = __fadd2_rn(sum, p);
+        w[0][n][0] = ptx::pack_bf16(p.x, p.y);
+        w[0][n][1] = 0u;
+      }
+      product_over_partners<HD, 1, NT>(o, w, at + as_k + j * HD * 2);
+    }
+    now.pos += WARPS * KS;
+    settle(now);
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();   // the rings are free: the parts are joined there
+  JoinRoom<HD, TILE_ROWS>& room = *reinterpret_cast<JoinRoom<HD, TILE_ROWS>*>(s_ring);
+  float l = sum.x + sum.y;
+  l += __shfl_xor_sync(0xffffffffu, l, 1);
+  l += __shfl_xor_sync(0xffffffffu, l, 2);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) *reinterpret_cast<float2*>(&room.acc[warp][lane >> 2][8 * c + 2 * (lane & 3)]) = make_float2(o[0][c][0], o[0][c][1]);
+  if ((lane & 3) == 0) room.ml[warp][lane >> 2] = make_float2(ref, l);
+  join_warps_and_ctas<bf16, HD, TILE_ROWS>(g, a, room, b, hk, rank, split, n_rows);
+}
+
+template <typename K>
+cudaError_t launch_cluster(K kernel, size_t bytes, const Geometry& g, const ScoredArgs& a, int split, cudaStream_t st) {
+  if (bytes > 0) {
+    const cudaError_t e = sm_count_and_smem_once(reinterpret_cast<const void*>(kernel), (int)bytes, nullptr);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.kv_heads * split), g.batch);
   cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -328,27 +518,34 @@ cudaError_t launch_rows(const Geometry& g, const ScoredArgs& a, int split, cudaS
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, g, a, split);
 }
-template <typename T, int HD>
-cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
+// CTAs per (sample, key head): until every SM has one, as long as each still gets two turns of its warps, of `turn` keys each.
+int split_keys(const Geometry& g, const ScoredArgs& a, int n_sm, int turn) {
+  int split = 1;
+  while (split < MAX_SPLIT && (int64_t)g.batch * a.kv_heads * split < n_sm && g.L > 2 * split * WARPS * turn) split *= 2;
+  return split;
+}
+template <int HD>
+cudaError_t launch_tile(const Geometry& g, const ScoredArgs& a, int n_sm, cudaStream_t st) {
+  const int split = split_keys(g, a, n_sm, TailRing<HD>::KEYS);
+  constexpr size_t bytes = WARPS * TailRing<HD>::BYTES;
+  static_assert(sizeof(JoinRoom<HD, TILE_ROWS>) <= bytes, "the parts are joined in the rings");
+  const bool rule = rule_masks(a) || a.slopes != nullptr;
+  if (a.softcap > 0.f) return launch_cluster(rule ? scored_tail_tile_kernel<HD, true, true> : scored_tail_tile_kernel<HD, true, false>, bytes, g, a, split, st);
+  return launch_cluster(rule ? scored_tail_tile_kernel<HD, false, true> : scored_tail_tile_kernel<HD, false, false>, bytes, g, a, split, st);
+}
+template <int HD, int R>
+cudaError_t launch_rows(const Geometry& g, const ScoredArgs& a, int n_sm, cudaStream_t st) {
+  const bool rule = rule_masks(a) || a.slopes != nullptr;
+  return launch_cluster(rule ? scored_tail_kernel<float, HD, R, true> : scored_tail_kernel<float, HD, R, false>, 0, g, a, split_keys(g, a, n_sm, STEPS * 256 / HD), st);
+}
+template <int HD>
+cudaError_t launch_width(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
   int n_sm = 0;
   const cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
   if (e != cudaSuccess) return e;
-  // CTAs per (sample, key head): until every SM has one, as long as each still gets two turns of its warps
-  int split = 1;
-  while (split < MAX_SPLIT && (int64_t)g.batch * a.kv_heads * split < n_sm && g.L > 2 * split * WARPS * STEPS * (256 / HD)) split *= 2;
+  if (dtype == GSIT_BF16) return launch_tile<HD>(g, a, n_sm, st);
   const int rows = a.Lq * a.group;
-  return rows <= 1   ? launch_rows<T, HD, 1>(g, a, split, st)
-         : rows <= 3 ? launch_rows<T, HD, 3>(g, a, split, st)
-                     : launch_rows<T, HD, 6>(g, a, split, st);
-}
-template <typename T>
-cudaError_t launch(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
-  switch (g.hd) {
-    case 8: return launch_width<T, 8>(g, a, st);
-    case 16: return launch_width<T, 16>(g, a, st);
-    case 32: return launch_width<T, 32>(g, a, st);
-    default: return launch_width<T, 64>(g, a, st);
-  }
+  return rows <= 1 ? launch_rows<HD, 1>(g, a, n_sm, st) : rows <= 3 ? launch_rows<HD, 3>(g, a, n_sm, st) : launch_rows<HD, 6>(g, a, n_sm, st);
 }
 bool loads_of_16_bytes(const void* p, int64_t ld, int dtype) {
   return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % (dtype == GSIT_BF16 ? 8 : 4) == 0;
@@ -356,15 +553,20 @@ bool loads_of_16_bytes(const void* p, int64_t ld, int dtype) {
 
 }  // namespace
 
-// Up to six query rows to a key head (one position in each of three segments, two query heads): beyond, the registers of a lane that
-// holds 8 features of each row's query and sum are used up, and the tiles of 64 rows take over.
+// bf16: up to eight query rows to a key head, half of a fragment's.  float: up to six (one position in each of three segments, two
+// query heads); beyond, the registers of a lane that holds 8 features of each row's query and sum are used up.
 bool scored_tail_supported(const Geometry& g, int dtype, const ScoredArgs& a) {
-  return a.tail && a.Lq * a.group <= 6 && (g.hd == 8 || g.hd == 16 || g.hd == 32 || g.hd == 64) && loads_of_16_bytes(a.q, a.ldq, dtype) &&
-         loads_of_16_bytes(a.k, a.ldk, dtype) && loads_of_16_bytes(a.v, a.ldv, dtype);
+  return a.tail && a.Lq * a.group <= (dtype == GSIT_BF16 ? TILE_ROWS : 6) && (g.hd == 8 || g.hd == 16 || g.hd == 32 || g.hd == 64) &&
+         loads_of_16_bytes(a.q, a.ldq, dtype) && loads_of_16_bytes(a.k, a.ldk, dtype) && loads_of_16_bytes(a.v, a.ldv, dtype);
 }
 
 cudaError_t launch_scored_tail(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
-  return dtype == GSIT_BF16 ? launch<__nv_bfloat16>(g, a, st) : launch<float>(g, a, st);
+  switch (g.hd) {
+    case 8: return launch_width<8>(g, dtype, a, st);
+    case 16: return launch_width<16>(g, dtype, a, st);
+    case 32: return launch_width<32>(g, dtype, a, st);
+    default: return launch_width<64>(g, dtype, a, st);
+  }
 }
 
 }  // namespace gsit

@@ -1,12 +1,15 @@
 // Rotary positions with several axes: every pair of features (u, v) of a head becomes (u c - v s, u s + v c), with c and s of the
 // pair's angle; the backward pass is the same rotation by the opposite angle.
 //
-// One pass over the rows, q and k read once and written once, which is all that bounds it.  A CTA takes as many rows as make 256
-// (row, pair) angles -- 64 rows at 4 pairs, 8 at 32 -- so that every thread computes one angle into shared memory and all heads of q
-// and k of those rows read it there: an angle costs as much as some 40 rotated pairs, and 2 x heads of them share it.
+// One pass over the rows, q and k read once and written once, which is all that bounds it.  A CTA takes blocks of rows in turn; the
+// angles of a block's rows -- one (row, pair) a thread -- are computed into shared memory, where all heads of q and k read them (an
+// angle costs as much as some 40 rotated pairs), while the loads of the block before are under way.  What a thread does in a block
+// (which rows, heads and features) never changes, so its offsets and its pair's frequency stay in registers.
 // Angles: position * frequency in turns as one double product, less its nearest integer: right to 2^-20 turns even at positions near
 // 2^31, where a float product keeps no bit of the phase; then sincospi of the float remainder.
 #include <math.h>
+
+#include <algorithm>
 
 #include "ops.cuh"
 
@@ -15,6 +18,9 @@ namespace {
 
 constexpr int THREADS = 256;
 
+constexpr int MAX_ROWS = 64;                // of a block
+constexpr int BLOCK_UNITS = 4 * THREADS;    // units of work of a block that a thread's registers hold the offsets of
+
 struct RotaryArgs {
   const void* in[2];
   void* out[2];
@@ -22,9 +28,8 @@ struct RotaryArgs {
   const int32_t* positions;
   int64_t axis_stride, batch_stride;
   float sign;
-  int pairs, rows_per_cta, q_heads;
+  int pairs, block_rows, q_heads;
   int row_units, head_units;             // units of work (see Form) of a row and of a head
-  uint32_t row_magic, head_magic;        // ceil(2^32 / units): division by a multiplication, exact while u * units < 2^32
   int axis1, axis2;                      // first pair of axis 1 and of axis 2
   int adjacent;
   double turns[MAX_ROTARY_PAIRS];        // frequency of a pair in turns a position
@@ -38,128 +43,170 @@ struct RotaryArgs {
 //   SCALAR    one pair, or one feature that is copied: part of a head rotated, odd strides or addresses
 enum Form { SPLIT, ADJACENT, HEAD, SCALAR };
 
-__device__ __forceinline__ int div_magic(int u, int d, uint32_t magic) { return d == 1 ? u : (int)__umulhi((uint32_t)u, magic); }
+template <typename T> __device__ __forceinline__ void unpack_piece(const uint4& v, float (&f)[16 / sizeof(T)]) {
+  if constexpr (sizeof(T) == 2) {
+    unpack_bf16(v.x, f[0], f[1]);
+    unpack_bf16(v.y, f[2], f[3]);
+    unpack_bf16(v.z, f[4], f[5]);
+    unpack_bf16(v.w, f[6], f[7]);
+  } else {
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
+  }
+}
+
+// Place of pair p in a row of the table: groups of eight lie 40 floats apart, so that the four pieces of a head of 64 that a warp reads
+// together meet different banks.
+__device__ __forceinline__ int slot(int p) { return p + (p >> 3) * 2; }
 
 template <typename T, int FORM>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, FORM == SPLIT ? 4 : 3)
 rotary_kernel(const __grid_constant__ Geometry g, const __grid_constant__ RotaryArgs a) {
   constexpr int E = 16 / sizeof(T);                         // elements of a piece
-  constexpr int BATCH = FORM == SCALAR ? 1 : FORM == SPLIT ? 2 : 4;   // units whose loads are in flight together
-  __shared__ float2 table[THREADS];                         // (cos, sin) of row r, pair p at [r * pairs + p]
-  const int tid = threadIdx.x;
-  const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_cta;
-  const int here = (int)min((int64_t)a.rows_per_cta, (int64_t)g.batch * g.L - row0);
-  const int b0 = (int)(row0 / g.L), l0 = (int)(row0 - (int64_t)b0 * g.L);
+  constexpr int BATCH = FORM == SCALAR ? 1 : FORM == SPLIT ? 2 : BLOCK_UNITS / THREADS;   // units whose loads are in flight together
+  constexpr int SLOTS = THREADS + THREADS / 4;
+  __shared__ __align__(16) float s_cos[2][SLOTS], s_sin[2][SLOTS];   // of row r, pair p at [r * row_slots + slot(p)]
+  __shared__ int s_real[2][MAX_ROWS];
+  const int tid = threadIdx.x, row_slots = (slot(a.pairs - 1) + 4) & ~3, rows = g.batch * g.L, blocks = (rows + a.block_rows - 1) / a.block_rows;
   ptx::load_params_early(g, a);
-  ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
 
-  // sample and position of the CTA's row r
-  auto locate = [&](int r, int& b, int& l) {
-    b = b0;
-    l = l0 + r;
-    if (l >= g.L) {
-      b += l / g.L;
-      l %= g.L;
-    }
-  };
-  auto angles = [&] {
-    if (tid < here * a.pairs) {
-      const int r = tid / a.pairs, p = tid - r * a.pairs;
-      int b, l;
-      locate(r, b, l);
-      const int axis = (p >= a.axis2) ? 2 : (p >= a.axis1) ? 1 : 0;
-      const double t = (double)a.positions[axis * a.axis_stride + b * a.batch_stride + l] * a.turns[p];
+  // this thread's angle of a block
+  const int my_row = tid / a.pairs, my_pair = tid - my_row * a.pairs;
+  const double turns = a.turns[my_pair];
+  const int axis = (my_pair >= a.axis2) ? 2 : (my_pair >= a.axis1) ? 1 : 0;
+  auto angles = [&](int block, int buf) {
+    const int row = block * a.block_rows + my_row;
+    if (my_row < a.block_rows && block < blocks && row < rows) {
+      const int b = (uint32_t)row / (uint32_t)g.L, l = row - b * g.L;
+      const double t = (double)a.positions[axis * a.axis_stride + b * a.batch_stride + l] * turns;
       float sn, cs;
       sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
-      table[tid] = make_float2(cs, a.sign * sn);
+      s_cos[buf][my_row * row_slots + slot(my_pair)] = cs;
+      s_sin[buf][my_row * row_slots + slot(my_pair)] = a.sign * sn;
+      if (my_pair == 0) {
+        const int s = segment_of(g, l);
+        s_real[buf][my_row] = l - g.off(s) < valid_rows(g, b, s);
+      }
     }
-    __syncthreads();
   };
-  struct Place { int64_t src, dst; int row, k, unit; bool real; };   // element offsets of the head's first feature
-  auto place = [&](int u) {
-    Place p;
-    p.row = FORM == SCALAR ? u / a.row_units : div_magic(u, a.row_units, a.row_magic);
+  struct Unit {
+    int64_t src, dst;   // element offsets from the block's first row
+    int row, k, at;     // row in the block, which tensor, place of its first angle
+  };
+  auto find = [&](int u) {
+    Unit p;
+    p.row = u / a.row_units;
     const int in_row = u - p.row * a.row_units;
-    int head = FORM == SCALAR ? in_row / a.head_units : div_magic(in_row, a.head_units, a.head_magic);
-    p.unit = in_row - head * a.head_units;
+    int head = in_row / a.head_units;
+    const int unit = in_row - head * a.head_units;
     p.k = head >= a.q_heads;
     if (p.k) head -= a.q_heads;
-    p.src = (row0 + p.row) * (p.k ? a.in_stride[1] : a.in_stride[0]) + (int64_t)head * g.hd;
-    p.dst = (row0 + p.row) * (p.k ? a.out_stride[1] : a.out_stride[0]) + (int64_t)head * g.hd;
-    int b, l;
-    locate(p.row, b, l);
-    const int s = segment_of(g, l);
-    p.real = l - g.off(s) < valid_rows(g, b, s);
+    const int64_t in_head = (int64_t)head * g.hd + (FORM == SCALAR ? 0 : unit * E);
+    p.src = p.row * (p.k ? a.in_stride[1] : a.in_stride[0]) + in_head;
+    p.dst = p.row * (p.k ? a.out_stride[1] : a.out_stride[0]) + in_head;
+    p.at = FORM == SCALAR ? unit : p.row * row_slots + slot(FORM == SPLIT ? unit * E : FORM == ADJACENT ? unit * (E / 2) : 0);
     return p;
   };
-  auto src = [&](const Place& p) { return static_cast<const T*>(p.k ? a.in[1] : a.in[0]) + p.src; };
-  auto dst = [&](const Place& p) { return static_cast<T*>(p.k ? a.out[1] : a.out[0]) + p.dst; };
-  const int n_units = here * a.row_units;
+  const int n_units = a.block_rows * a.row_units;
+  Unit mine[BATCH];
+#pragma unroll
+  for (int i = 0; i < BATCH; ++i) mine[i] = find(min(tid + i * THREADS, n_units - 1));
 
-  if constexpr (FORM == SCALAR) {
-    angles();
-    for (int u = tid; u < n_units; u += THREADS) {
-      const Place p = place(u);
-      const T* x = src(p);
-      T* y = dst(p);
-      if (p.unit >= a.pairs) {
-        const int f = a.pairs + p.unit;
-        store_as(y + f, p.real ? to_float(x[f]) : 0.f);
-      } else {
-        const int i = a.adjacent ? 2 * p.unit : p.unit, j = a.adjacent ? i + 1 : a.pairs + i;
-        const float2 cs = table[p.row * a.pairs + p.unit];
-        const float lo = p.real ? to_float(x[i]) : 0.f, hi = p.real ? to_float(x[j]) : 0.f;
-        store_as(y + i, p.real ? lo * cs.x - hi * cs.y : 0.f);
-        store_as(y + j, p.real ? lo * cs.y + hi * cs.x : 0.f);
-      }
-    }
-  } else {
-    // the first units' loads are under way while the angles are computed
-    for (int u0 = tid, turn = 0; turn == 0 || u0 < n_units; u0 += THREADS * BATCH, ++turn) {
-      Place p[BATCH];
-      float v[BATCH][E], w[FORM == SPLIT ? BATCH : 1][E];
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+  angles(blockIdx.x, 0);
+  __syncthreads();
+  for (int block = blockIdx.x, buf = 0; block < blocks; block += gridDim.x, buf ^= 1) {
+    const int row0 = block * a.block_rows, here = min(a.block_rows, rows - row0);
+    const T *q = static_cast<const T*>(a.in[0]) + row0 * a.in_stride[0], *k = static_cast<const T*>(a.in[1]) + row0 * a.in_stride[1];
+    T *qo = static_cast<T*>(a.out[0]) + row0 * a.out_stride[0], *ko = static_cast<T*>(a.out[1]) + row0 * a.out_stride[1];
+    for (int u0 = 0; u0 < n_units; u0 += THREADS * BATCH) {
+      if (u0 > 0)
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int u = u0 + i * THREADS;
-        if (u < n_units) {
-          p[i] = place(u);
-          if (p[i].real) {
-            load_n(src(p[i]) + p[i].unit * E, v[i]);
-            if constexpr (FORM == SPLIT) load_n(src(p[i]) + a.pairs + p[i].unit * E, w[i]);
-          }
-        }
-      }
-      if (turn == 0) angles();
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        if (u0 + i * THREADS >= n_units) break;
-        float y[E], z[E];
-        const float2* t = table + p[i].row * a.pairs + (FORM == SPLIT ? p[i].unit * E : FORM == ADJACENT ? p[i].unit * (E / 2) : 0);
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = z[e] = 0.f;
-        if (p[i].real) {
-          if constexpr (FORM == SPLIT) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float2 cs = t[e];
-              y[e] = v[i][e] * cs.x - w[i][e] * cs.y;
-              z[e] = v[i][e] * cs.y + w[i][e] * cs.x;
-            }
+        for (int i = 0; i < BATCH; ++i) mine[i] = find(min(u0 + tid + i * THREADS, n_units - 1));
+      if constexpr (FORM == SCALAR) {
+        if (u0 == 0) angles(block + gridDim.x, buf ^ 1);
+        const Unit& p = mine[0];
+        if (u0 + tid < n_units && p.row < here) {
+          const bool keep = s_real[buf][p.row];
+          const T* x = (p.k ? k : q) + p.src;
+          T* y = (p.k ? ko : qo) + p.dst;
+          if (p.at >= a.pairs) {
+            const int f = a.pairs + p.at;
+            store_as(y + f, keep ? to_float(x[f]) : 0.f);
           } else {
-#pragma unroll
-            for (int e = 0; e < E / 2; ++e) {
-              const float2 cs = t[e];
-              const int lo = FORM == HEAD ? e : 2 * e, hi = FORM == HEAD ? e + E / 2 : 2 * e + 1;
-              y[lo] = v[i][lo] * cs.x - v[i][hi] * cs.y;
-              y[hi] = v[i][lo] * cs.y + v[i][hi] * cs.x;
-            }
+            const int i = a.adjacent ? 2 * p.at : p.at, j = a.adjacent ? i + 1 : a.pairs + i, t = p.row * row_slots + slot(p.at);
+            const float lo = keep ? to_float(x[i]) : 0.f, hi = keep ? to_float(x[j]) : 0.f, cs = s_cos[buf][t], sn = s_sin[buf][t];
+            store_as(y + i, keep ? lo * cs - hi * sn : 0.f);
+            store_as(y + j, keep ? lo * sn + hi * cs : 0.f);
           }
         }
-        store_n(dst(p[i]) + p[i].unit * E, y);
-        if constexpr (FORM == SPLIT) store_n(dst(p[i]) + a.pairs + p[i].unit * E, z);
+      } else {
+        uint4 v[BATCH], w[FORM == SPLIT ? BATCH : 1];   // as they lie in memory
+        bool in[BATCH], keep[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          in[i] = u0 + tid + i * THREADS < n_units && mine[i].row < here;
+          keep[i] = in[i] && s_real[buf][mine[i].row];
+          if (keep[i]) {
+            const T* x = (mine[i].k ? k : q) + mine[i].src;
+            v[i] = *reinterpret_cast<const uint4*>(x);
+            if constexpr (FORM == SPLIT) w[i] = *reinterpret_cast<const uint4*>(x + a.pairs);
+          }
+        }
+        if (u0 == 0) {   // while these loads are under way: the next block's lines and angles
+          const int64_t ahead = (int64_t)gridDim.x * a.block_rows;
+#pragma unroll
+          for (int i = 0; i < BATCH; ++i)
+            if (row0 + ahead + mine[i].row < rows) {
+              const T* x = (mine[i].k ? k + ahead * a.in_stride[1] : q + ahead * a.in_stride[0]) + mine[i].src;
+              if ((reinterpret_cast<uintptr_t>(x) & 112u) == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(x));
+            }
+          angles(block + gridDim.x, buf ^ 1);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          if (!in[i]) continue;
+          float y[E], z[E];
+#pragma unroll
+          for (int e = 0; e < E; ++e) y[e] = z[e] = 0.f;
+          if (keep[i]) {
+            const float *pc = s_cos[buf] + mine[i].at, *ps = s_sin[buf] + mine[i].at;
+            float x[E];
+            unpack_piece<T>(v[i], x);
+            if constexpr (FORM == SPLIT) {
+              float x_hi[E];
+              unpack_piece<T>(w[i], x_hi);
+#pragma unroll
+              for (int e = 0; e < E; e += 2) {
+                const float2 c = *reinterpret_cast<const float2*>(pc + e), s = *reinterpret_cast<const float2*>(ps + e);
+                const float2 lo = make_float2(x[e], x[e + 1]), hi = make_float2(x_hi[e], x_hi[e + 1]);
+                const float2 a2 = __ffma2_rn(make_float2(-hi.x, -hi.y), s, __fmul2_rn(lo, c)), b2 = __ffma2_rn(lo, s, __fmul2_rn(hi, c));
+                y[e] = a2.x; y[e + 1] = a2.y;
+                z[e] = b2.x; z[e + 1] = b2.y;
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < E / 2; ++e) {
+                const float c = pc[e], s = ps[e];
+                const int lo = FORM == HEAD ? e : 2 * e, hi = FORM == HEAD ? e + E / 2 : 2 * e + 1;
+                y[lo] = x[lo] * c - x[hi] * s;
+                y[hi] = x[lo] * s + x[hi] * c;
+              }
+            }
+          }
+          T* dst = (mine[i].k ? ko : qo) + mine[i].dst;
+          store_n(dst, y);
+          if constexpr (FORM == SPLIT) store_n(dst + a.pairs, z);
+        }
       }
     }
+    if (n_units > THREADS * BATCH)   // back to the first units' offsets
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) mine[i] = find(min(tid + i * THREADS, n_units - 1));
+    __syncthreads();   // the next block's angles are there, and nobody reads this block's any more
   }
 }
 
@@ -198,16 +245,19 @@ cudaError_t launch_rotary(const Geometry& g, int dtype, const RotaryCall& c, cud
   a.adjacent = c.interleaved;
   a.q_heads = c.heads[0];
   for (int p = 0; p < a.pairs; ++p) a.turns[p] = pow(c.base, -(double)p / a.pairs) / (2.0 * M_PI);
-  a.rows_per_cta = THREADS / a.pairs;
   wide = wide && 2 * a.pairs == g.hd && g.hd % piece == 0;
   const Form form = !wide ? SCALAR : c.interleaved ? ADJACENT : a.pairs % piece == 0 ? SPLIT : g.hd == piece ? HEAD : SCALAR;
   a.head_units = form == SPLIT ? a.pairs / piece : form == SCALAR ? g.hd - a.pairs : g.hd / piece;
   a.row_units = a.head_units * (c.heads[0] + c.heads[1]);
-  const auto magic = [](int d) { return d < 2 ? 0u : (uint32_t)((0x100000000ull + d - 1) / d); };
-  a.head_magic = magic(a.head_units);
-  a.row_magic = magic(a.row_units);
-  const int64_t grid = ((int64_t)g.batch * g.L + a.rows_per_cta - 1) / a.rows_per_cta;
-  return dtype == GSIT_BF16 ? launch<__nv_bfloat16>(g, a, form, (unsigned)grid, st) : launch<float>(g, a, form, (unsigned)grid, st);
+  // rows of a block: an angle a thread, and no more units than the registers keep offsets of
+  const int batch = form == SCALAR ? 1 : form == SPLIT ? 2 : BLOCK_UNITS / THREADS;
+  a.block_rows = std::max(1, std::min(std::min(THREADS / a.pairs, MAX_ROWS), batch * THREADS / a.row_units));
+  int n_sm = 0;
+  const cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = ((int64_t)g.batch * g.L + a.block_rows - 1) / a.block_rows;
+  const unsigned grid = (unsigned)std::min(blocks, (int64_t)4 * n_sm);
+  return dtype == GSIT_BF16 ? launch<__nv_bfloat16>(g, a, form, grid, st) : launch<float>(g, a, form, grid, st);
 }
 
 }  // namespace gsit

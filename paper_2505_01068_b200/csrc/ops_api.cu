@@ -1,4 +1,6 @@
 // C ABI of the training operators (gsit_ops.h): argument checks and launches.
+#include <math.h>
+
 #include "gsit_ops.h"
 #include "ops.cuh"
 #include "scored.cuh"
@@ -76,7 +78,17 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
   a->softcap = r->softcap > 0.f ? r->softcap : 0.f;
   a->inner = a->softcap > 0.f ? a->scale / a->softcap : a->scale * LOG2E;
   a->outer = a->softcap * LOG2E;
-  a->bend_scale = a->softcap > 0.f ? 1.0f / (a->outer * a->outer) : 0.f;
+  if (a->softcap > 0.f) {
+    // tanh(y) / y and 1 - tanh(y)^2 as quadratics of y^2: least squares fits of the relative error over |y| <= 1/4, refined towards equal
+    // error (4.2e-7 and 2.8e-6)
+    static const double P[3] = {0.999999604, -0.333219082, 0.128416126}, B[3] = {0.999997213, -0.999202503, 0.632425479};
+    const double in = (double)a->inner, out = (double)a->outer;
+    a->near_dot = (float)(0.25 / in);
+    for (int i = 0; i < 3; ++i) {
+      a->near_p[i] = (float)(P[i] * out * pow(in, 2 * i + 1));
+      a->near_b[i] = (float)(B[i] * pow(in, 2 * i));
+    }
+  }
   a->causal = r->causal != 0;
   a->slopes = r->slopes;
   a->times = r->times;

@@ -20,7 +20,10 @@ struct ScoredArgs {
   const int32_t* documents;
   int tail, q_len[3], q_off[3], Lq;       // queries per segment and their offsets in q
   // what the scores are computed with, in base 2: x = outer * tanh(inner * dot) with a cap, x = inner * dot without
-  float inner, outer, bend_scale;         // bend_scale = 1 / outer^2
+  float inner, outer;
+  // ... and, for dots of at most near_dot (|tanh's argument| <= 1/4), as polynomials of the dot d:  x = d (p0 + p1 d^2 + p2 d^4),
+  // derivative of the cap = b0 + b1 d^2 + b2 d^4
+  float near_dot, near_p[3], near_b[3];
   // backward
   const void* dout; int64_t lddo;
   void *dq, *dk, *dv;

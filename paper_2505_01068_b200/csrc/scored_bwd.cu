@@ -14,18 +14,14 @@ namespace {
 // Registers: 24 warps an SM for narrow heads, 16 and 12 for wide ones, whose accumulators are larger.
 template <int HD, int W> constexpr int MIN_CTAS = (HD <= 16 ? 24 : HD == 32 ? 16 : 12) / W;
 
-// x, dp (starting at -delta) -> the weights p (where wanted) and ds = p (dP - delta) bend, packed.  lse: in base 2, of the lane's rows or columns.
-template <bool CAP, bool BIAS, bool PACK_P, int N, typename Lse>
-__device__ __forceinline__ void weigh(float (&x)[N][4], float (&dp)[N][4], uint32_t (&wp)[PACK_P ? N : 1][2], uint32_t (&ws)[N][2], float inner, Lse lse) {
-  constexpr bool RAW = !CAP && !BIAS;
+// x (scores less the row's log-sum-exp), dp (less delta, times the cap's derivative) -> the weights p (where wanted) and ds = p dp, packed.
+template <bool PACK_P, int N>
+__device__ __forceinline__ void weigh(const float (&x)[N][4], const float (&dp)[N][4], uint32_t (&wp)[PACK_P ? N : 1][2], uint32_t (&ws)[N][2]) {
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float2 l = lse(n, i), y = make_float2(x[n][2 * i], x[n][2 * i + 1]);
-      const float2 z = RAW ? __ffma2_rn(y, make_float2(inner, inner), make_float2(-l.x, -l.y)) : __fadd2_rn(y, make_float2(-l.x, -l.y));
-      const float2 p = make_float2(ptx::ex2(z.x), ptx::ex2(z.y));
-      const float2 ds = __fmul2_rn(p, make_float2(dp[n][2 * i], dp[n][2 * i + 1]));
+      const float2 p = make_float2(ptx::ex2(x[n][2 * i]), ptx::ex2(x[n][2 * i + 1])), ds = __fmul2_rn(p, make_float2(dp[n][2 * i], dp[n][2 * i + 1]));
       if constexpr (PACK_P) wp[n][i] = ptx::pack_bf16(p.x, p.y);
       ws[n][i] = ptx::pack_bf16(ds.x, ds.y);
     }
@@ -123,8 +119,8 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   const bool working = w0 < min(q_end, n_q);
   const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
 
-  const uint32_t at_kn = smem_u32(s_k[0]) + lane_as_n<HD>(lane), at_kk = smem_u32(s_k[0]) + lane_as_k<HD>(lane);
-  const uint32_t at_v = smem_u32(s_v[0]) + lane_as_n<HD>(lane);
+  const LaneAt<HD> at_kn = lane_as_n<HD>(smem_u32(s_k[0]), lane), at_kk = lane_as_k<HD>(smem_u32(s_k[0]), lane);
+  const LaneAt<HD> at_v = lane_as_n<HD>(smem_u32(s_v[0]), lane);
 
   float dq[MT][CH][4];
 #pragma unroll
@@ -138,20 +134,15 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
     constexpr bool SOME_SHUT = decltype(some_tag)::value;
     float x[MT][NT][4], dp[MT][NT][4];
     const uint32_t from = (buf * KC + j) * HD * 2;
-    product_over_features<HD, MT, NT>(x, qf, at_kn + from, from_zero);
-    product_over_features<HD, MT, NT>(dp, gf, at_v + from, [&](int m, int, float (&z)[4]) {
+    product_over_features<HD, MT, NT>(x, qf, at_kn, from, from_zero);
+    product_over_features<HD, MT, NT>(dp, gf, at_v, from, [&](int m, int, float (&z)[4]) {
       z[0] = z[1] = -delta[m][0];
       z[2] = z[3] = -delta[m][1];
     });
     uint32_t w[MT][NT][2], unused[1][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      if constexpr (CAP) {
-        cap_scores<NT>(x[m], a.inner, a.outer);
-        times_bend<NT>(dp[m], x[m], a.bend_scale);
-      } else if constexpr (BIAS) {
-        scale_scores<NT>(x[m], a.inner);
-      }
+      dots_to_scores<CAP, true, NT>(x[m], dp[m], a, [&](int, int i) { return make_float2(lse2[m][i], lse2[m][i]); });
       if constexpr (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
       if constexpr (SOME_SHUT) {
 #pragma unroll
@@ -165,9 +156,9 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
               if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
           }
       }
-      weigh<CAP, BIAS, false, NT>(x[m], dp[m], unused, w[m], a.inner, [&](int, int i) { return make_float2(lse2[m][i], lse2[m][i]); });
+      weigh<false, NT>(x[m], dp[m], unused, w[m]);
     }
-    product_over_partners<HD, MT, NT>(dq, w, at_kk + from);
+    product_over_partners<HD, MT, NT>(dq, w, at_kk, from);
   };
 
   for (int buf = 0; !next.over(); buf ^= 1) {
@@ -298,8 +289,8 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
   const bool working = w0 < min(k_end, n_k);
 
-  const uint32_t at_qn = smem_u32(s_q[0]) + lane_as_n<HD>(lane), at_qk = smem_u32(s_q[0]) + lane_as_k<HD>(lane);
-  const uint32_t at_gn = smem_u32(s_g[0]) + lane_as_n<HD>(lane), at_gk = smem_u32(s_g[0]) + lane_as_k<HD>(lane);
+  const LaneAt<HD> at_qn = lane_as_n<HD>(smem_u32(s_q[0]), lane), at_qk = lane_as_k<HD>(smem_u32(s_q[0]), lane);
+  const LaneAt<HD> at_gn = lane_as_n<HD>(smem_u32(s_g[0]), lane), at_gk = lane_as_k<HD>(smem_u32(s_g[0]), lane);
 
   float dk[MT][CH][4], dv[MT][CH][4];
 #pragma unroll
@@ -320,20 +311,15 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       delta[n] = make_float2(-t.y, -t.w);
     }
     const uint32_t from = (buf * QC + j) * HD * 2;
-    product_over_features<HD, MT, NT>(x, kf, at_qn + from, from_zero);
-    product_over_features<HD, MT, NT>(dp, vf, at_gn + from, [&](int, int n, float (&z)[4]) {
+    product_over_features<HD, MT, NT>(x, kf, at_qn, from, from_zero);
+    product_over_features<HD, MT, NT>(dp, vf, at_gn, from, [&](int, int n, float (&z)[4]) {
       z[0] = z[2] = delta[n].x;
       z[1] = z[3] = delta[n].y;
     });
     uint32_t wp[MT][NT][2], ws[MT][NT][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      if constexpr (CAP) {
-        cap_scores<NT>(x[m], a.inner, a.outer);
-        times_bend<NT>(dp[m], x[m], a.bend_scale);
-      } else if constexpr (BIAS) {
-        scale_scores<NT>(x[m], a.inner);
-      }
+      dots_to_scores<CAP, true, NT>(x[m], dp[m], a, [&](int n, int) { return lse2[n]; });
       if constexpr (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
       if constexpr (SOME_SHUT) {
 #pragma unroll
@@ -346,10 +332,10 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
               if (own_time[m][i] > s_limit[buf][col] || s_doc[buf][col] != own_doc[m][i]) x[m][n][2 * i + e] = -INFINITY;
           }
       }
-      weigh<CAP, BIAS, true, NT>(x[m], dp[m], wp[m], ws[m], a.inner, [&](int n, int) { return lse2[n]; });
+      weigh<true, NT>(x[m], dp[m], wp[m], ws[m]);
     }
-    product_over_partners<HD, MT, NT>(dv, wp, at_gk + from);
-    product_over_partners<HD, MT, NT>(dk, ws, at_qk + from);
+    product_over_partners<HD, MT, NT>(dv, wp, at_gk, from);
+    product_over_partners<HD, MT, NT>(dk, ws, at_qk, from);
   };
 
   for (int buf = 0; !next.over(); buf ^= 1) {

@@ -12,7 +12,7 @@ template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, MT, W>)
 scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 8 : 4;
-  constexpr bool TIMES = BIAS || MASK, RAW = !CAP && !BIAS;   // RAW: the scale is folded into the exponent's multiply-add
+  constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
   __shared__ int s_doc[2][MASK ? KC : 1];
@@ -77,9 +77,11 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
   const bool working = w0 < min(q_end, rows.hi) && w0 + 16 * MT > rows.lo;
   const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
-  const uint32_t at_k = smem_u32(s_k[0]) + lane_as_n<HD>(lane), at_v = smem_u32(s_v[0]) + lane_as_k<HD>(lane);
+  const LaneAt<HD> at_k = lane_as_n<HD>(smem_u32(s_k[0]), lane), at_v = lane_as_k<HD>(smem_u32(s_v[0]), lane);
 
-  float o[MT][CH][4], ref[MT][2];   // ref: in base 2
+  // ref: what a row's weights are relative to (base 2); it follows the row's maximum when a score exceeds it by more than `room` (2^8, so
+  // that weights stay below 256; any score as long as the row has seen no open key)
+  float o[MT][CH][4], ref[MT][2], room[MT][2];
   float2 sum[MT][2];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
@@ -89,7 +91,8 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       for (int e = 0; e < 4; ++e) o[m][c][e] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      ref[m][i] = -INFINITY;
+      ref[m][i] = 0.f;
+      room[m][i] = -INFINITY;
       sum[m][i] = make_float2(0.f, 0.f);
     }
   }
@@ -99,12 +102,13 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     constexpr int N = decltype(n_tag)::value;
     constexpr bool SOME_SHUT = decltype(some_tag)::value;
     float x[MT][N][4];
-    product_over_features<HD, MT, N>(x, qf, at_k + (buf * KC + j) * HD * 2, from_zero);
+    const uint32_t from = (buf * KC + j) * HD * 2;
+    product_over_features<HD, MT, N>(x, qf, at_k, from, from_zero);
     uint32_t w[MT][N][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      if constexpr (CAP) cap_scores<N>(x[m], a.inner, a.outer);
-      else if constexpr (BIAS) scale_scores<N>(x[m], a.inner);
+      float unused[1][4];
+      dots_to_scores<CAP, false, N>(x[m], unused, a, [&](int, int i) { return make_float2(ref[m][i], ref[m][i]); });
       if constexpr (BIAS) add_bias<N>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
       if constexpr (SOME_SHUT) {
 #pragma unroll
@@ -118,47 +122,47 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
               if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
           }
       }
-      // the reference follows the maximum only when that has grown by more than 2^8 (weights stay below 256): as long as no lane's
-      // own scores have, the lanes of a row need not be brought together
+      // as long as no lane's own scores ask for it, the lanes of a row need not be brought together
       float top[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         top[i] = -INFINITY;
 #pragma unroll
         for (int n = 0; n < N; ++n) top[i] = ptx::fmax3(top[i], x[m][n][2 * i], x[m][n][2 * i + 1]);
-        if constexpr (RAW) top[i] *= a.inner;
       }
-      if (__any_sync(0xffffffffu, top[0] > ref[m][0] + 8.f || top[1] > ref[m][1] + 8.f)) {
+      if (__any_sync(0xffffffffu, top[0] > room[m][0] || top[1] > room[m][1])) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
           top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-          if (top[i] > ref[m][i]) {
-            const float f = ptx::ex2(ref[m][i] - top[i]);
+          if (top[i] > room[m][i]) {
+            const float f = room[m][i] == -INFINITY ? 1.f : ptx::ex2(-top[i]);   // nothing to scale down before the first open key
             sum[m][i] = __fmul2_rn(sum[m][i], make_float2(f, f));
 #pragma unroll
             for (int q = 0; q < CH; ++q) {
               o[m][q][2 * i] *= f;
               o[m][q][2 * i + 1] *= f;
             }
-            ref[m][i] = top[i];
+            ref[m][i] += top[i];
+            room[m][i] = 8.f;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+              x[m][n][2 * i] -= top[i];
+              x[m][n][2 * i + 1] -= top[i];
+            }
           }
         }
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float r = ref[m][i] == -INFINITY ? 0.f : -ref[m][i];   // a row that has seen no open key yet keeps weights of zero
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-          const float2 y = make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), rr = make_float2(r, r);
-          const float2 z = RAW ? __ffma2_rn(y, make_float2(a.inner, a.inner), rr) : __fadd2_rn(y, rr);
-          const float2 p = make_float2(ptx::ex2(z.x), ptx::ex2(z.y));
+          const float2 p = make_float2(ptx::ex2(x[m][n][2 * i]), ptx::ex2(x[m][n][2 * i + 1]));
           sum[m][i] = __fadd2_rn(sum[m][i], p);
           w[m][n][i] = ptx::pack_bf16(p.x, p.y);
         }
-      }
     }
-    product_over_partners<HD, MT, N>(o, w, at_v + (buf * KC + j) * HD * 2);
+    product_over_partners<HD, MT, N>(o, w, at_v, from);
   };
 
   for (int buf = 0; !next.over(); buf ^= 1) {

@@ -422,21 +422,20 @@ scored_tail_tile_kernel(const __grid_constant__ Geometry g, const __grid_constan
   for (int c = 0; c < CH; ++c)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[0][c][e] = 0.f;
-  const uint32_t as_n = lane_as_n<HD>(lane), as_k = 2048 + lane_as_k<HD>(lane);
+  const LaneAt<HD> as_n = lane_as_n<HD>(ring, lane), as_k = lane_as_k<HD>(ring + 2048, lane);
 #pragma unroll 1
   for (int stage = 0; !now.over(); stage = stage + 1 == Ring::STAGES ? 0 : stage + 1) {
     asm volatile("cp.async.wait_group %0;" ::"n"(Ring::STAGES - 2) : "memory");
     __syncwarp();   // every lane's copies are there, and every lane is done with the stage that is filled next
     request(ahead, stage == 0 ? Ring::STAGES - 1 : stage - 1);
     const int rem = now.left();
-    const uint32_t at = ring + stage * Ring::STAGE;
     const float* const times = reinterpret_cast<const float*>(s_ring + warp * Ring::BYTES + stage * Ring::STAGE + 4096);
     const int* const docs = reinterpret_cast<const int*>(times + KS);
     const bool mine = (own.opens >> now.seg) & 1;
 #pragma unroll 1
     for (int j = 0; j < min(KS, rem); j += 8 * NT) {
       float x[1][NT][4];
-      product_over_features<HD, 1, NT>(x, qf, at + as_n + j * HD * 2, from_zero);
+      product_over_features<HD, 1, NT>(x, qf, as_n, stage * Ring::STAGE + j * HD * 2, from_zero);
       uint32_t w[1][NT][2];
       float top = -INFINITY;
 #pragma unroll
@@ -479,7 +478,7 @@ scored_tail_tile_kernel(const __grid_constant__ Geometry g, const __grid_constan
         w[0][n][0] = ptx::pack_bf16(p.x, p.y);
         w[0][n][1] = 0u;
       }
-      product_over_partners<HD, 1, NT>(o, w, at + as_k + j * HD * 2);
+      product_over_partners<HD, 1, NT>(o, w, as_k, stage * Ring::STAGE + j * HD * 2);
     }
     now.pos += WARPS * KS;
     settle(now);

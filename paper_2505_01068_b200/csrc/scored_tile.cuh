@@ -50,13 +50,20 @@ template <int HD> __device__ __forceinline__ uint32_t piece_at(int r, int c) {
 //   as n: the product runs over features; a load of 16 rows gives {n 0-7 k lo, n 0-7 k hi, n 8-15 k lo, n 8-15 k hi} of a feature step
 //   as k: the product runs over the rows; a load gives {features lo: rows 0-7, rows 8-15, features hi: the same} of 16 features
 // Rows of 8 features: one load takes 32 of them, 8 to a matrix, either way.
-template <int HD> __device__ __forceinline__ uint32_t lane_as_n(int lane) {
-  if constexpr (HD == 8) return lane * 16;
-  return piece_at<HD>(((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1);
+template <int HD> struct LaneAt {
+  uint32_t of[(HD + 15) / 16];   // from the tile's first byte, per feature step
+};
+template <int HD> __device__ __forceinline__ LaneAt<HD> lane_steps(uint32_t base, uint32_t first) {
+  LaneAt<HD> at;
+#pragma unroll
+  for (int ks = 0; ks < (HD + 15) / 16; ++ks) at.of[ks] = base + (first ^ (ks << 5));
+  return at;
 }
-template <int HD> __device__ __forceinline__ uint32_t lane_as_k(int lane) {
-  if constexpr (HD == 8) return lane * 16;
-  return piece_at<HD>((((lane >> 3) & 1) << 3) + (lane & 7), lane >> 4);
+template <int HD> __device__ __forceinline__ LaneAt<HD> lane_as_n(uint32_t base, int lane) {
+  return lane_steps<HD>(base, HD == 8 ? lane * 16 : piece_at<HD>(((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1));
+}
+template <int HD> __device__ __forceinline__ LaneAt<HD> lane_as_k(uint32_t base, int lane) {
+  return lane_steps<HD>(base, HD == 8 ? lane * 16 : piece_at<HD>((((lane >> 3) & 1) << 3) + (lane & 7), lane >> 4));
 }
 
 // A operand of a warp's own rows, straight from memory: rows row0 + lane / 4 and + 8, zeros where not real.  Head width 8 uses words 0, 1.
@@ -71,14 +78,15 @@ template <int HD> __device__ __forceinline__ void own_rows(const bf16* p0, const
   }
 }
 
-// c[mt][nt] = start(mt, nt) + own rows x partner rows, over features, for NT tiles of 8 partners; `at`: the first one's tile + lane_as_n.
+// c[mt][nt] = start(mt, nt) + own rows x partner rows, over features, for NT tiles of 8 partners; the first one's row lies
+// `from` bytes behind the tile that `at` (lane_as_n) counts from.
 template <int HD, int MT, int NT, typename Start>
-__device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], const uint32_t (&own)[MT][(HD + 15) / 16][4], uint32_t at, Start start) {
+__device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], const uint32_t (&own)[MT][(HD + 15) / 16][4], const LaneAt<HD>& at, uint32_t from, Start start) {
   if constexpr (HD == 8) {
 #pragma unroll
     for (int q = 0; q < NT / 4; ++q) {
       uint32_t f[4];
-      ldsm4(at + q * 512, f);
+      ldsm4(at.of[0] + from + q * 512, f);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -94,7 +102,7 @@ __device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], con
 #pragma unroll
       for (int ks = 0; ks < HD / 16; ++ks) {
         uint32_t f[4];
-        ldsm4((at ^ (ks << 5)) + p * 32 * HD, f);
+        ldsm4(at.of[ks] + from + p * 32 * HD, f);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -107,14 +115,14 @@ __device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], con
   }
 }
 // o[mt][feature tile] += weights [own rows x partners] x partner rows, over NT tiles of 8 partners; weights as packed accumulators
-// w[mt][nt] = {row g, row g + 8}; `at`: the first partner's tile + lane_as_k.
+// w[mt][nt] = {row g, row g + 8}; `at`: lane_as_k.
 template <int HD, int MT, int NT>
-__device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4], const uint32_t (&w)[MT][NT][2], uint32_t at) {
+__device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4], const uint32_t (&w)[MT][NT][2], const LaneAt<HD>& at, uint32_t from) {
   if constexpr (HD == 8) {
 #pragma unroll
     for (int q = 0; q < NT / 4; ++q) {
       uint32_t f[4];
-      ldsm4_t(at + q * 512, f);
+      ldsm4_t(at.of[0] + from + q * 512, f);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -130,7 +138,7 @@ __device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4],
 #pragma unroll
       for (int c = 0; c < HD / 16; ++c) {
         uint32_t f[4];
-        ldsm4_t((at ^ (c << 5)) + p * 32 * HD, f);
+        ldsm4_t(at.of[c] + from + p * 32 * HD, f);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           const uint32_t a[4] = {w[m][2 * p][0], w[m][2 * p][1], w[m][2 * p + 1][0], w[m][2 * p + 1][1]};
@@ -142,52 +150,51 @@ __device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4],
 }
 __device__ __forceinline__ void from_zero(int, int, float (&z)[4]) { z[0] = z[1] = z[2] = z[3] = 0.f; }
 
-// Dots -> capped scores in base 2 (in place).  One range check for the whole warp decides between the polynomial alone and the form
-// for any argument.
-template <int NT> __device__ __forceinline__ void cap_scores(float (&x)[NT][4], float inner, float outer) {
-  float top = 0.f;
-  const float2 f = make_float2(inner, inner), o = make_float2(outer, outer);
+// Dots -> scores in base 2 less minus(tile, row half), a pair for two columns (in place), and where wanted d *= derivative of the cap.
+// With a cap, one range check for the whole warp decides between polynomials of the dot (quadratics of its square: 4 multiply-adds a
+// score with the subtraction, 3 more for the derivative) and the form for any argument.  The FMA pipe is what these kernels fill first.
+template <bool CAP, bool BEND, int NT, typename Minus>
+__device__ __forceinline__ void dots_to_scores(float (&x)[NT][4], float (&d)[BEND ? NT : 1][4], const ScoredArgs& a, Minus minus) {
   auto each = [&](auto score) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        const float2 y = score(make_float2(x[n][i], x[n][i + 1]));
-        x[n][i] = y.x;
-        x[n][i + 1] = y.y;
+      for (int i = 0; i < 2; ++i) {
+        const float2 m = minus(n, i);
+        float2 bend = make_float2(1.f, 1.f);
+        const float2 y = score(make_float2(x[n][2 * i], x[n][2 * i + 1]), make_float2(-m.x, -m.y), bend);
+        x[n][2 * i] = y.x;
+        x[n][2 * i + 1] = y.y;
+        if constexpr (CAP && BEND) {
+          const float2 e = __fmul2_rn(make_float2(d[n][2 * i], d[n][2 * i + 1]), bend);
+          d[n][2 * i] = e.x;
+          d[n][2 * i + 1] = e.y;
+        }
       }
   };
-  each([&](float2 y) {
-    y = __fmul2_rn(y, f);
-    top = ptx::fmax3(top, fabsf(y.x), fabsf(y.y));
-    return y;
-  });
-  if (__any_sync(0xffffffffu, top > TANH_RANGE)) each([&](float2 y) { return __fmul2_rn(tanh_any2(y), o); });
-  else each([&](float2 y) { return tanh_near2(y, outer); });
-}
-// d *= 1 - tanh^2, from the capped scores x (bend_scale = 1 / outer^2)
-template <int NT> __device__ __forceinline__ void times_bend(float (&d)[NT][4], const float (&x)[NT][4], float bend_scale) {
-  const float2 f = make_float2(-bend_scale, -bend_scale), one = make_float2(1.f, 1.f);
+  auto both = [](float v) { return make_float2(v, v); };
+  if constexpr (!CAP) {
+    each([&](float2 y, float2 m, float2&) { return __ffma2_rn(y, both(a.inner), m); });
+  } else {
+    float top = 0.f;
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      const float2 y = make_float2(x[n][i], x[n][i + 1]);
-      const float2 e = __fmul2_rn(make_float2(d[n][i], d[n][i + 1]), __ffma2_rn(__fmul2_rn(y, f), y, one));
-      d[n][i] = e.x;
-      d[n][i + 1] = e.y;
+      for (int i = 0; i < 4; i += 2) top = ptx::fmax3(top, fabsf(x[n][i]), fabsf(x[n][i + 1]));
+    if (__any_sync(0xffffffffu, top > a.near_dot)) {
+      each([&](float2 y, float2 m, float2& bend) {
+        const float2 t = tanh_any2(__fmul2_rn(y, both(a.inner)));
+        if constexpr (BEND) bend = __ffma2_rn(make_float2(-t.x, -t.y), t, bend);
+        return __ffma2_rn(t, both(a.outer), m);
+      });
+    } else {
+      each([&](float2 y, float2 m, float2& bend) {
+        const float2 z = __fmul2_rn(y, y);
+        if constexpr (BEND) bend = __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0]));
+        return __ffma2_rn(__ffma2_rn(__ffma2_rn(z, both(a.near_p[2]), both(a.near_p[1])), z, both(a.near_p[0])), y, m);
+      });
     }
-}
-template <int NT> __device__ __forceinline__ void scale_scores(float (&x)[NT][4], float inner) {
-  const float2 f = make_float2(inner, inner);
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      const float2 y = __fmul2_rn(make_float2(x[n][i], x[n][i + 1]), f);
-      x[n][i] = y.x;
-      x[n][i + 1] = y.y;
-    }
+  }
 }
 // x -= slope2 * |own time - partner time|.  own[2]: rows g, g + 8; partner times in shared memory from column 0 on.
 template <int NT> __device__ __forceinline__ void add_bias(float (&x)[NT][4], const float (&own)[2], const float* times, int lane, float slope2) {

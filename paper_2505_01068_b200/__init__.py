@@ -11,6 +11,7 @@ from .binding import (CALL_ATTENTION, CALL_LAYER, CALL_QKV_PROJ, DEVFLAG_CLAMPED
                       expire_wait_selftest, late_write, wait_answers,
                       rotary_fwd, rotary_bwd, layer_norm_fwd, layer_norm_bwd, im_scored_attention_fwd, im_scored_attention_bwd)
 from .stack import GsitStack
+from .training import ImEncoderLayer
 from .hostio import HostPipeline
 
 __all__ = [n for n in dir() if not n.startswith("_")]

@@ -5,10 +5,16 @@
 //   x  = own0 partner0^T                       (Q K^T, Q K^T, K Q^T)
 //   dp =                own1 partner1^T        (        dO V^T, V dO^T)
 //   a thread per own row (= lane of tensor memory) turns them into weights p = exp2(score - reference or log-sum-exp) and, backward,
-//   ds = p (dp - delta) bend, packed to bf16 and written over the columns of x and dp that the thread has read
+//   ds = p (dp - delta) bend, packed to bf16 back into tensor memory
 //   acc0 += p partner1 (FWD)  or  ds partner0 (DQ, DKV);   acc1 += p partner1 (DKV)
 // with weights from tensor memory as the A operand and the partner tile, as TMA wrote it, as an MN-major B operand: nothing is
-// transposed, no score leaves the SM.  128 x 64 rows of tensor memory a CTA hold x and dp once, so two CTAs of an SM take turns: while one exponentiates, the other's products run.
+// transposed, no score leaves the SM.  A CTA has 256 columns of tensor memory, so two CTAs share an SM.  What one tile after the
+// other would take is mostly latency (products -> barrier -> scores -> barrier -> products: 4600 clocks a tile of the forward kind,
+// against 212 of products and 512 of exponentials), so the next tile's first products are issued as early as the columns allow:
+//   FWD  x twice (the weights take the columns of the x they come from): x of tile t + 1 beside the scores of tile t
+//   DQ   x, dp, ds and the accumulator, 224 columns: x and dp of tile t + 1 as soon as those of tile t are in registers
+//   DKV  x, dp and two accumulators; p and ds take the columns of dp: x of tile t + 1 as soon as that of tile t is in registers, dp once
+//        the products with p and ds are over
 // Warps: 0 fetches (own tiles once, a ring of three partner stages with what the scores need beside them, and which tiles are open at
 // all), 1 issues every product, 2 .. 5 compute.  All waits are bounded.
 #include <cuda.h>
@@ -38,12 +44,12 @@ template <int KIND> struct Map {   // shared memory, relative to a 1024-byte ali
   static constexpr int OWN_TILES = KIND == FWD ? 1 : 2;
   static constexpr int TILES = OWN_TILES * OWN_BYTES, META = TILES + STAGES * 2 * TILE_BYTES, BARS = META + STAGES * (int)sizeof(Meta);
   static constexpr int BYTES = BARS + 128 + 1024;
-  static constexpr int TMEM = KIND == FWD ? 128 : 256;                 // columns: x [0, 64), dp [64, 128), then the accumulators
-  static constexpr int ACC = KIND == FWD ? 64 : 128;
-  static constexpr int CTAS = 2;
+  static constexpr int TMEM = 256, CTAS = 2;
+  // columns of tensor memory: x (FWD: twice), dp, ds (DQ; FWD: in x, DKV: in dp), accumulators
+  static constexpr int X = 0, DP = 64, DS = 128, ACC = KIND == DQ ? 160 : 128;
 };
-constexpr int BAR_OWN = 0, BAR_FULL = 8, BAR_EMPTY = BAR_FULL + 8 * STAGES, BAR_X = BAR_EMPTY + 8 * STAGES, BAR_W = BAR_X + 8, BAR_ACC = BAR_W + 8,
-              SLOT_TMEM = BAR_ACC + 8, SLOT_GAVE_UP = SLOT_TMEM + 4;
+constexpr int BAR_OWN = 0, BAR_FULL = 8, BAR_EMPTY = BAR_FULL + 8 * STAGES, BAR_X = BAR_EMPTY + 8 * STAGES, BAR_W = BAR_X + 16, BAR_DP = BAR_W + 16,
+              BAR_READ = BAR_DP + 8, BAR_ACC = BAR_READ + 8, SLOT_TMEM = BAR_ACC + 8, SLOT_GAVE_UP = SLOT_TMEM + 4;
 
 struct Maps {
   CUtensorMap own0, own1, partner0, partner1;
@@ -112,9 +118,14 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
       mbar_init(bars + BAR_FULL + 8 * i, 1);
       mbar_init(bars + BAR_EMPTY + 8 * i, 5);   // the products' commit, four computing warps
     }
-    mbar_init(bars + BAR_X, 1);
-    mbar_init(bars + BAR_W, 128);
-    mbar_init(bars + BAR_ACC, 1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bars + BAR_X + 8 * i, 1);     // x is there (FWD: buffer i; backward, i = 0: and dp, but for DKV)
+      mbar_init(bars + BAR_W + 8 * i, 128);   // the weights of tile i, i + 2, .. are there
+    }
+    mbar_init(bars + BAR_DP, 1);              // DKV: dp is there
+    mbar_init(bars + BAR_READ, 128);          // x (DQ: and dp) is in registers
+    mbar_init(bars + BAR_ACC, 1);             // a tile's second products are over
     mbar_init_fence();
   }
   if (warp == 1) tmem_alloc(bars + SLOT_TMEM, M::TMEM);
@@ -232,39 +243,77 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
     // ================================ products ================================
     if (any) {
       constexpr uint32_t TO_X = idesc_bf16(PARTNER, false), TO_ACC = idesc_bf16(HD, true);
+      auto tile_of = [&](int t) { return base + M::TILES + (t % STAGES) * 2 * TILE_BYTES; };
+      auto more = [&](int t) {   // is there a tile t?
+        const bool ok = mbar_wait_warp(wc, bars + BAR_FULL + 8 * (t % STAGES), (t / STAGES) & 1);
+        return ok && uniform(metas[t % STAGES].rem) >= 0;
+      };
+      auto to_x = [&](int t) {
+        const uint32_t tile = tile_of(t);
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k)
+          umma_ss(tmem + M::X + (KIND == FWD ? 64 * (t & 1) : 0), smem_desc_sw128(base + 32 * k), smem_desc_sw128(tile + 32 * k), TO_X, k > 0);
+      };
+      auto to_dp = [&](int t) {
+        const uint32_t tile = tile_of(t) + TILE_BYTES;
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k)
+          umma_ss(tmem + M::DP, smem_desc_sw128(base + OWN_BYTES + 32 * k), smem_desc_sw128(tile + 32 * k), TO_X, k > 0);
+      };
       mbar_wait_warp(wc, bars + BAR_OWN, 0);
-#pragma unroll 1
-      for (int t = 0;; ++t) {
-        const int st = t % STAGES;
-        const bool ok = mbar_wait_warp(wc, bars + BAR_FULL + 8 * st, (t / STAGES) & 1);
-        if (!ok || uniform(metas[st].rem) < 0) break;
-        if (t > 0) mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);   // the weights in the columns of x have been read
-        tc_fence_after();
-        const uint32_t tile = base + M::TILES + st * 2 * TILE_BYTES;
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < HD / 16; ++k) umma_ss(tmem, smem_desc_sw128(base + 32 * k), smem_desc_sw128(tile + 32 * k), TO_X, k > 0);
-          if (BWD)
-#pragma unroll
-            for (int k = 0; k < HD / 16; ++k)
-              umma_ss(tmem + 64, smem_desc_sw128(base + OWN_BYTES + 32 * k), smem_desc_sw128(tile + TILE_BYTES + 32 * k), TO_X, k > 0);
-          umma_commit(bars + BAR_X);
+      bool go = more(0);
+      tc_fence_after();
+      if (go && elect_one()) {
+        to_x(0);
+        if (KIND == DQ) to_dp(0);
+        umma_commit(bars + BAR_X);
+        if (KIND == DKV) {
+          to_dp(0);
+          umma_commit(bars + BAR_DP);
         }
-        __syncwarp();
-        mbar_wait_warp(wc, bars + BAR_W, t & 1);
+      }
+      __syncwarp();
+#pragma unroll 1
+      for (int t = 0; go; ++t) {
+        go = more(t + 1);
+        if (go) {
+          if (KIND == FWD && t > 0) mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);   // the weights of tile t - 1 lie where x of t + 1 goes
+          if (KIND != FWD) mbar_wait_warp(wc, bars + BAR_READ, t & 1);
+          tc_fence_after();
+          if (elect_one()) {
+            to_x(t + 1);
+            if (KIND == DQ) to_dp(t + 1);
+            umma_commit(bars + BAR_X + (KIND == FWD ? 8 * ((t + 1) & 1) : 0));
+          }
+          __syncwarp();
+        }
+        mbar_wait_warp(wc, bars + BAR_W + 8 * (t & 1), (t >> 1) & 1);
         tc_fence_after();
+        const uint32_t tile = tile_of(t);
         if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < PARTNER / 16; ++k)   // p in the columns of x (FWD); ds there (DQ, DKV)
-            umma_ts(tmem + M::ACC, tmem + 8 * k, smem_desc_sw128(tile + (KIND == FWD ? TILE_BYTES : 0) + 2048 * k), TO_ACC, (t > 0 || k > 0) ? 1u : 0u);
-          if (KIND == DKV)
-#pragma unroll
-            for (int k = 0; k < PARTNER / 16; ++k)   // p in the columns of dp
-              umma_ts(tmem + M::ACC + 64, tmem + 64 + 8 * k, smem_desc_sw128(tile + TILE_BYTES + 2048 * k), TO_ACC, (t > 0 || k > 0) ? 1u : 0u);
-          umma_commit(bars + BAR_EMPTY + 8 * st);
+          for (int k = 0; k < PARTNER / 16; ++k) {   // 16 partners: 8 columns of weights, 2048 bytes of a tile
+            const uint32_t acc = (t > 0 || k > 0) ? 1u : 0u;
+            if (KIND == FWD) umma_ts(tmem + M::ACC, tmem + M::X + 64 * (t & 1) + 8 * k, smem_desc_sw128(tile + TILE_BYTES + 2048 * k), TO_ACC, acc);
+            if (KIND == DQ) umma_ts(tmem + M::ACC, tmem + M::DS + 8 * k, smem_desc_sw128(tile + 2048 * k), TO_ACC, acc);
+            if (KIND == DKV) {   // each half of dp's columns: p, then ds
+              umma_ts(tmem + M::ACC + 64, tmem + M::DP + 32 * (k / 2) + 8 * (k % 2), smem_desc_sw128(tile + TILE_BYTES + 2048 * k), TO_ACC, acc);
+              umma_ts(tmem + M::ACC, tmem + M::DP + 32 * (k / 2) + 16 + 8 * (k % 2), smem_desc_sw128(tile + 2048 * k), TO_ACC, acc);
+            }
+          }
+          umma_commit(bars + BAR_EMPTY + 8 * (t % STAGES));
           umma_commit(bars + BAR_ACC);
         }
         __syncwarp();
+        if (KIND == DKV && go) {
+          mbar_wait_warp(wc, bars + BAR_ACC, t & 1);
+          tc_fence_after();
+          if (elect_one()) {
+            to_dp(t + 1);
+            umma_commit(bars + BAR_DP);
+          }
+          __syncwarp();
+        }
       }
     }
   } else {
@@ -325,12 +374,14 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
         const float2 y1 = __ffma2_rn(make_float2(fabsf(d1.x), fabsf(d1.y)), f, make_float2(x2, x3));
         x0 = y0.x; x1 = y0.y; x2 = y1.x; x3 = y1.y;
       };
-      mbar_wait_warp(wc, bars + BAR_X, t & 1);
+      const uint32_t x_at = tl + M::X + (KIND == FWD ? 64 * (t & 1) : 0);
+      if (KIND == FWD) mbar_wait_warp(wc, bars + BAR_X + 8 * (t & 1), (t >> 1) & 1);
+      else mbar_wait_warp(wc, bars + BAR_X, t & 1);
       tc_fence_after();
       if constexpr (KIND == FWD) {
         uint32_t xr[2][32];
-        tmem_ld32(tl, xr[0]);
-        tmem_ld32(tl + 32, xr[1]);
+        tmem_ld32(x_at, xr[0]);
+        tmem_ld32(x_at + 32, xr[1]);
         tmem_wait_ld(xr[0], xr[1]);
         float x[PARTNER], unused[1];
 #pragma unroll
@@ -359,7 +410,9 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
         if (__any_sync(0xffffffffu, top > room)) {
           const bool grow = top > room;
           const float f = grow && room != -INFINITY ? ex2(-top) : 1.f;
-          if (t > 0) {   // the accumulator holds all earlier tiles: their products were over before this tile's began
+          if (t > 0) {   // once the accumulator holds all earlier tiles
+            mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);
+            tc_fence_after();
             sum *= f;
 #pragma unroll
             for (int c = 0; c < HD; c += 16) {
@@ -386,17 +439,38 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
           part[c / 2 % 4] = __fadd2_rn(part[c / 2 % 4], p);
           w[c / 2] = pack_bf16(p.x, p.y);
         }
-        tmem_st32(tl, w);
+        tmem_st32(x_at, w);
         const float2 p2 = __fadd2_rn(__fadd2_rn(part[0], part[1]), __fadd2_rn(part[2], part[3]));
         sum += p2.x + p2.y;
       } else {
+        uint32_t xr[2][32];
+        if (KIND == DKV) {   // x leaves its columns at once
+          tmem_ld32(x_at, xr[0]);
+          tmem_ld32(x_at + 32, xr[1]);
+          tmem_wait_ld(xr[0], xr[1]);
+          tc_fence_before();
+          mbar_arrive(bars + BAR_READ);
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           constexpr int N = 32;
-          uint32_t xr[32], dr[32];
-          tmem_ld32(tl + N * half, xr);
-          tmem_ld32(tl + 64 + N * half, dr);
-          tmem_wait_ld(xr, dr);
+          uint32_t dr[32];
+          if (KIND == DKV) {
+            if (half == 0) {
+              mbar_wait_warp(wc, bars + BAR_DP, t & 1);
+              tc_fence_after();
+            }
+            tmem_ld32(tl + M::DP + N * half, dr);
+            tmem_wait_ld(dr);
+          } else {
+            tmem_ld32(x_at + N * half, xr[half]);
+            tmem_ld32(tl + M::DP + N * half, dr);
+            tmem_wait_ld(xr[half], dr);
+            if (half == 1) {
+              tc_fence_before();
+              mbar_arrive(bars + BAR_READ);
+            }
+          }
           float x[N], d[N];
 #pragma unroll
           for (int c = 0; c < N; c += 4) {
@@ -406,7 +480,7 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
             const float2 d1 = __fadd2_rn(make_float2(__uint_as_float(dr[c + 2]), __uint_as_float(dr[c + 3])), make_float2(-dl.z, -dl.w));
             d[c] = d0.x; d[c + 1] = d0.y; d[c + 2] = d1.x; d[c + 3] = d1.y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[c + e] = __uint_as_float(xr[c + e]);
+            for (int e = 0; e < 4; ++e) x[c + e] = __uint_as_float(xr[half][c + e]);
           }
           if (CAP && rem < PARTNER)
 #pragma unroll
@@ -435,8 +509,16 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
             if (KIND == DKV) wp[c / 2] = pack_bf16(p.x, p.y);
             ws[c / 2] = pack_bf16(ds.x, ds.y);
           }
-          tmem_st16(tl + 16 * half, ws);
-          if (KIND == DKV) tmem_st16(tl + 64 + 16 * half, wp);
+          if (KIND == DKV) {
+            tmem_st16(tl + M::DP + 32 * half, wp);
+            tmem_st16(tl + M::DP + 32 * half + 16, ws);
+          } else {
+            if (half == 0 && t > 0) {   // the products with the last tile's ds are over
+              mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);
+              tc_fence_after();
+            }
+            tmem_st16(tl + M::DS + 16 * half, ws);
+          }
         }
       }
       if (rem < PARTNER) {
@@ -452,7 +534,7 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
       }
       tmem_wait_st();
       tc_fence_before();
-      mbar_arrive(bars + BAR_W);
+      mbar_arrive(bars + BAR_W + 8 * (t & 1));
       __syncwarp();
       if (lane == 0) mbar_arrive(bars + BAR_EMPTY + 8 * st);
     }

@@ -158,6 +158,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       }
       weigh<false, NT>(x[m], dp[m], unused, w[m]);
     }
+    __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, NT>(dq, w, at_kk, from);
   };
 
@@ -334,6 +335,7 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       }
       weigh<true, NT>(x[m], dp[m], wp[m], ws[m]);
     }
+    __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, NT>(dv, wp, at_gk, from);
     product_over_partners<HD, MT, NT>(dk, ws, at_qk, from);
   };

@@ -162,6 +162,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
           w[m][n][i] = ptx::pack_bf16(p.x, p.y);
         }
     }
+    __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, N>(o, w, at_v, from);
   };
 

@@ -478,6 +478,7 @@ scored_tail_tile_kernel(const __grid_constant__ Geometry g, const __grid_constan
         w[0][n][0] = ptx::pack_bf16(p.x, p.y);
         w[0][n][1] = 0u;
       }
+      __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
       product_over_partners<HD, 1, NT>(o, w, as_k, stage * Ring::STAGE + j * HD * 2);
     }
     now.pos += WARPS * KS;

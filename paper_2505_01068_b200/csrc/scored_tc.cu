@@ -51,50 +51,34 @@ template <int KIND> struct Map {   // shared memory, relative to a 1024-byte ali
 constexpr int BAR_OWN = 0, BAR_FULL = 8, BAR_EMPTY = BAR_FULL + 8 * STAGES, BAR_X = BAR_EMPTY + 8 * STAGES, BAR_W = BAR_X + 16, BAR_DP = BAR_W + 16,
               BAR_READ = BAR_DP + 8, BAR_ACC = BAR_READ + 8, SLOT_TMEM = BAR_ACC + 8, SLOT_GAVE_UP = SLOT_TMEM + 4;
 
+template <bool V> struct BoolTag { static constexpr bool value = V; };
+
 struct Maps {
   CUtensorMap own0, own1, partner0, partner1;
 };
 
-// Dots of a row -> scores in base 2 less minus(c), a pair of columns from c on; d *= derivative of the cap (as dots_to_scores()).  Only
-// real rows take part in the choice between the two forms: what padding holds must not change the others' bits.
-template <bool CAP, bool BEND, int N, typename Minus>
-__device__ __forceinline__ void row_to_scores(float (&x)[N], float (&d)[BEND ? N : 1], bool real, const ScoredArgs& a, Minus minus) {
+// Two dots -> scores in base 2 less m; d *= derivative of the cap (as dots_to_scores()).  NEAR: tanh's arguments are at most 1/4.
+template <bool CAP, bool BEND, bool NEAR> __device__ __forceinline__ float2 score_pair(float2 y, float2 m, float2& d, const ScoredArgs& a) {
   auto both = [](float v) { return make_float2(v, v); };
-  auto each = [&](auto score) {
-#pragma unroll
-    for (int c = 0; c < N; c += 2) {
-      const float2 m = minus(c);
-      float2 bend = make_float2(1.f, 1.f);
-      const float2 y = score(make_float2(x[c], x[c + 1]), make_float2(-m.x, -m.y), bend);
-      x[c] = y.x;
-      x[c + 1] = y.y;
-      if constexpr (CAP && BEND) {
-        const float2 e = __fmul2_rn(make_float2(d[c], d[c + 1]), bend);
-        d[c] = e.x;
-        d[c + 1] = e.y;
-      }
-    }
-  };
+  m = make_float2(-m.x, -m.y);
   if constexpr (!CAP) {
-    each([&](float2 y, float2 m, float2&) { return __ffma2_rn(y, both(a.inner), m); });
+    return __ffma2_rn(y, both(a.inner), m);
+  } else if constexpr (NEAR) {
+    const float2 z = __fmul2_rn(y, y);
+    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0])));
+    return __ffma2_rn(__ffma2_rn(__ffma2_rn(z, both(a.near_p[2]), both(a.near_p[1])), z, both(a.near_p[0])), y, m);
   } else {
-    float top = 0.f;
-#pragma unroll
-    for (int c = 0; c < N; c += 2) top = fmax3(top, fabsf(x[c]), fabsf(x[c + 1]));
-    if (__any_sync(0xffffffffu, real && top > a.near_dot)) {
-      each([&](float2 y, float2 m, float2& bend) {
-        const float2 t = tanh_any2(__fmul2_rn(y, both(a.inner)));
-        if constexpr (BEND) bend = __ffma2_rn(make_float2(-t.x, -t.y), t, bend);
-        return __ffma2_rn(t, both(a.outer), m);
-      });
-    } else {
-      each([&](float2 y, float2 m, float2& bend) {
-        const float2 z = __fmul2_rn(y, y);
-        if constexpr (BEND) bend = __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0]));
-        return __ffma2_rn(__ffma2_rn(__ffma2_rn(z, both(a.near_p[2]), both(a.near_p[1])), z, both(a.near_p[0])), y, m);
-      });
-    }
+    const float2 t = tanh_any2(__fmul2_rn(y, both(a.inner)));
+    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(make_float2(-t.x, -t.y), t, both(1.f)));
+    return __ffma2_rn(t, both(a.outer), m);
   }
+}
+// The largest argument of a row's dots.
+template <int N> __device__ __forceinline__ float largest(const float (&x)[N]) {
+  float top[4] = {};
+#pragma unroll
+  for (int c = 0; c < N; c += 2) top[c / 2 % 4] = fmax3(top[c / 2 % 4], fabsf(x[c]), fabsf(x[c + 1]));
+  return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
 
 template <int KIND, bool CAP, bool BIAS, bool MASK>
@@ -366,13 +350,21 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
 #pragma unroll
         for (int e = 0; e < 4; ++e) is[e] = c + e >= rem || (MASK && ((KIND == DKV ? limit > lim[e] : lim[e] > limit) || dc[e] != own_doc));
       };
-      auto bias = [&](int c, float& x0, float& x1, float& x2, float& x3) {
+      auto bias = [&](int c, float2& x0, float2& x1) {
         const float4 tm = *reinterpret_cast<const float4*>(m.time + c);
         const float2 f = make_float2(-slope2, -slope2), d0 = __fadd2_rn(make_float2(tm.x, tm.y), make_float2(-own_time, -own_time)),
                      d1 = __fadd2_rn(make_float2(tm.z, tm.w), make_float2(-own_time, -own_time));
-        const float2 y0 = __ffma2_rn(make_float2(fabsf(d0.x), fabsf(d0.y)), f, make_float2(x0, x1));
-        const float2 y1 = __ffma2_rn(make_float2(fabsf(d1.x), fabsf(d1.y)), f, make_float2(x2, x3));
-        x0 = y0.x; x1 = y0.y; x2 = y1.x; x3 = y1.y;
+        x0 = __ffma2_rn(make_float2(fabsf(d0.x), fabsf(d0.y)), f, x0);
+        x1 = __ffma2_rn(make_float2(fabsf(d1.x), fabsf(d1.y)), f, x1);
+      };
+      // Which form the tile's scores take: one decision for the warp, ahead of everything, so that the multiply-adds of some columns and the
+      // exponentials of others are one stream of instructions.  Only real rows and columns take part: what padding holds must not
+      // change the others' bits.
+      auto in_form = [&](bool far, auto body) {
+        if (CAP && __any_sync(0xffffffffu, real && far)) body(BoolTag<false>{}, BoolTag<true>{});
+        else if (some) body(BoolTag<true>{}, BoolTag<true>{});
+        else body(BoolTag<true>{}, BoolTag<false>{});
+        __syncwarp();   // lanes may have taken different ways; accesses of tensor memory need the whole warp
       };
       const uint32_t x_at = tl + M::X + (KIND == FWD ? 64 * (t & 1) : 0);
       if (KIND == FWD) mbar_wait_warp(wc, bars + BAR_X + 8 * (t & 1), (t >> 1) & 1);
@@ -383,31 +375,46 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
         tmem_ld32(x_at, xr[0]);
         tmem_ld32(x_at + 32, xr[1]);
         tmem_wait_ld(xr[0], xr[1]);
-        float x[PARTNER], unused[1];
+        float x[PARTNER];
 #pragma unroll
         for (int c = 0; c < PARTNER; ++c) x[c] = __uint_as_float(xr[c / 32][c % 32]);
         if (CAP && rem < PARTNER)
 #pragma unroll
           for (int c = 0; c < PARTNER; ++c)
             if (c >= rem) x[c] = 0.f;
-        row_to_scores<CAP, false, PARTNER>(x, unused, real, a, [&](int) { return make_float2(ref, ref); });
-        if constexpr (BIAS)
-#pragma unroll
-          for (int c = 0; c < PARTNER; c += 4) bias(c, x[c], x[c + 1], x[c + 2], x[c + 3]);
-        if (some)
+        uint32_t w[32];
+        float top = -INFINITY, added = 0.f;
+        in_form(CAP && largest(x) > a.near_dot, [&](auto near, auto some_shut) {
+          float2 part[4] = {};
+          float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int c = 0; c < PARTNER; c += 4) {
-            bool is[4];
-            shut(c, is);
+            float2 none, y[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (is[e]) x[c + e] = -INFINITY;
+            for (int e = 0; e < 2; ++e)
+              y[e] = score_pair<CAP, false, decltype(near)::value>(make_float2(x[c + 2 * e], x[c + 2 * e + 1]), make_float2(ref, ref), none, a);
+            if constexpr (BIAS) bias(c, y[0], y[1]);
+            if constexpr (decltype(some_shut)::value) {
+              bool is[4];
+              shut(c, is);
+#pragma unroll
+              for (int e = 0; e < 2; ++e) y[e] = make_float2(is[2 * e] ? -INFINITY : y[e].x, is[2 * e + 1] ? -INFINITY : y[e].y);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              top4[(c / 2 + e) % 4] = fmax3(top4[(c / 2 + e) % 4], y[e].x, y[e].y);
+              x[c + 2 * e] = y[e].x;
+              x[c + 2 * e + 1] = y[e].y;
+              const float2 p = make_float2(ex2(y[e].x), ex2(y[e].y));
+              part[(c / 2 + e) % 4] = __fadd2_rn(part[(c / 2 + e) % 4], p);
+              w[c / 2 + e] = pack_bf16(p.x, p.y);
+            }
           }
-        float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int c = 0; c < PARTNER; c += 2) top4[c / 2 % 4] = fmax3(top4[c / 2 % 4], x[c], x[c + 1]);
-        const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
-        if (__any_sync(0xffffffffu, top > room)) {
+          const float2 p2 = __fadd2_rn(__fadd2_rn(part[0], part[1]), __fadd2_rn(part[2], part[3]));
+          added = p2.x + p2.y;
+          top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+        });
+        if (__any_sync(0xffffffffu, top > room)) {   // rare: the weights once more, relative to a new reference
           const bool grow = top > room;
           const float f = grow && room != -INFINITY ? ex2(-top) : 1.f;
           if (t > 0) {   // once the accumulator holds all earlier tiles
@@ -424,24 +431,25 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
               tmem_st16(tl + M::ACC + c, o);
             }
           }
+          const float shift = grow ? top : 0.f;
           if (grow) {
             ref += top;
             room = 8.f;
-#pragma unroll
-            for (int c = 0; c < PARTNER; ++c) x[c] -= top;
           }
-        }
-        float2 part[4] = {};
-        uint32_t w[32];
+          added = 0.f;
 #pragma unroll
-        for (int c = 0; c < PARTNER; c += 2) {
-          const float2 p = make_float2(ex2(x[c]), ex2(x[c + 1]));
-          part[c / 2 % 4] = __fadd2_rn(part[c / 2 % 4], p);
-          w[c / 2] = pack_bf16(p.x, p.y);
+          for (int c = 0; c < PARTNER; c += 2) {
+            const float2 p = make_float2(ex2(x[c] - shift), ex2(x[c + 1] - shift));
+            added += p.x + p.y;
+            w[c / 2] = pack_bf16(p.x, p.y);
+          }
+          __syncwarp();
         }
+        sum += added;
         tmem_st32(x_at, w);
-        const float2 p2 = __fadd2_rn(__fadd2_rn(part[0], part[1]), __fadd2_rn(part[2], part[3]));
-        sum += p2.x + p2.y;
+        // every warp sees every phase of this barrier: x of the next tile is there before this tile's products with weights are, so a warp
+        // that is ahead of the others could else meet, in the end, the parity of two phases before the one it waits for
+        if (t > 0) mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);
       } else {
         uint32_t xr[2][32];
         if (KIND == DKV) {   // x leaves its columns at once
@@ -471,44 +479,44 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
               mbar_arrive(bars + BAR_READ);
             }
           }
-          float x[N], d[N];
+          float x[N];
 #pragma unroll
-          for (int c = 0; c < N; c += 4) {
-            float4 dl = make_float4(delta, delta, delta, delta);
-            if (KIND == DKV) dl = *reinterpret_cast<const float4*>(m.delta + N * half + c);
-            const float2 d0 = __fadd2_rn(make_float2(__uint_as_float(dr[c]), __uint_as_float(dr[c + 1])), make_float2(-dl.x, -dl.y));
-            const float2 d1 = __fadd2_rn(make_float2(__uint_as_float(dr[c + 2]), __uint_as_float(dr[c + 3])), make_float2(-dl.z, -dl.w));
-            d[c] = d0.x; d[c + 1] = d0.y; d[c + 2] = d1.x; d[c + 3] = d1.y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[c + e] = __uint_as_float(xr[half][c + e]);
-          }
+          for (int c = 0; c < N; ++c) x[c] = __uint_as_float(xr[half][c]);
           if (CAP && rem < PARTNER)
 #pragma unroll
             for (int c = 0; c < N; ++c)
               if (N * half + c >= rem) x[c] = 0.f;
-          row_to_scores<CAP, true, N>(x, d, real, a, [&](int c) { return KIND == DKV ? *reinterpret_cast<const float2*>(m.lse + N * half + c) : make_float2(lse2, lse2); });
-          if constexpr (BIAS)
-#pragma unroll
-            for (int c = 0; c < N; c += 4) bias(N * half + c, x[c], x[c + 1], x[c + 2], x[c + 3]);
-          if (some)
+          uint32_t wp[16], ws[16];
+          in_form(CAP && largest(x) > a.near_dot, [&](auto near, auto some_shut) {
 #pragma unroll
             for (int c = 0; c < N; c += 4) {
-              bool is[4];
-              shut(N * half + c, is);
+              float4 dl = make_float4(delta, delta, delta, delta), ls = make_float4(lse2, lse2, lse2, lse2);
+              if (KIND == DKV) {
+                dl = *reinterpret_cast<const float4*>(m.delta + N * half + c);
+                ls = *reinterpret_cast<const float4*>(m.lse + N * half + c);
+              }
+              float2 d[2] = {__fadd2_rn(make_float2(__uint_as_float(dr[c]), __uint_as_float(dr[c + 1])), make_float2(-dl.x, -dl.y)),
+                             __fadd2_rn(make_float2(__uint_as_float(dr[c + 2]), __uint_as_float(dr[c + 3])), make_float2(-dl.z, -dl.w))};
+              float2 y[2] = {score_pair<CAP, true, decltype(near)::value>(make_float2(x[c], x[c + 1]), make_float2(ls.x, ls.y), d[0], a),
+                             score_pair<CAP, true, decltype(near)::value>(make_float2(x[c + 2], x[c + 3]), make_float2(ls.z, ls.w), d[1], a)};
+              if constexpr (BIAS) bias(N * half + c, y[0], y[1]);
+              if constexpr (decltype(some_shut)::value) {   // rows past the last hold whatever follows in memory: neither factor may be NaN
+                bool is[4];
+                shut(N * half + c, is);
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (is[e]) {   // rows past the last hold whatever follows in memory: neither factor may be NaN
-                  x[c + e] = -INFINITY;
-                  d[c + e] = 0.f;
+                for (int e = 0; e < 2; ++e) {
+                  y[e] = make_float2(is[2 * e] ? -INFINITY : y[e].x, is[2 * e + 1] ? -INFINITY : y[e].y);
+                  d[e] = make_float2(is[2 * e] ? 0.f : d[e].x, is[2 * e + 1] ? 0.f : d[e].y);
                 }
-            }
-          uint32_t wp[16], ws[16];
+              }
 #pragma unroll
-          for (int c = 0; c < N; c += 2) {
-            const float2 p = make_float2(ex2(x[c]), ex2(x[c + 1])), ds = __fmul2_rn(p, make_float2(d[c], d[c + 1]));
-            if (KIND == DKV) wp[c / 2] = pack_bf16(p.x, p.y);
-            ws[c / 2] = pack_bf16(ds.x, ds.y);
-          }
+              for (int e = 0; e < 2; ++e) {
+                const float2 p = make_float2(ex2(y[e].x), ex2(y[e].y)), ds = __fmul2_rn(p, d[e]);
+                if (KIND == DKV) wp[c / 2 + e] = pack_bf16(p.x, p.y);
+                ws[c / 2 + e] = pack_bf16(ds.x, ds.y);
+              }
+            }
+          });
           if (KIND == DKV) {
             tmem_st16(tl + M::DP + 32 * half, wp);
             tmem_st16(tl + M::DP + 32 * half + 16, ws);

@@ -259,6 +259,25 @@ def test_what_stands_in_padding_and_in_closed_documents_never_matters(g, dtype, 
     assert g.last_device_status() == (0, 0)
 
 
+@pytest.mark.parametrize("hd", [8, 64])
+def test_warps_of_uneven_speed(g, hd):
+    """Large values in one document send some warps of a tile through the form of the cap for any argument, others not: whoever is ahead
+    must not take a result before it is whole.  The other documents' rows keep their values on every one of many runs."""
+    p = Problem("bf16", 2, (20, 130, 70), 2, 1, hd, "all", docs=-3, causal=True, seed=5, cap=20.0)
+    base = p.forward(g)
+    clean = p.backward(g, *base)
+    other = p.docs == 1
+    for t in (p.q, p.k, p.v, p.dout):
+        t[other] = 1e15
+    keep = ~other & ~p.padding()
+    for _ in range(40):
+        out, lse = p.forward(g)
+        _close(out[keep], base[0][keep].double(), TOL["bf16"]["out"], "out")
+        for x, y in zip(p.backward(g, out, lse), clean):
+            _close(x[keep], y[keep].double(), TOL["bf16"]["grad"], "grad")
+    assert g.last_device_status() == (0, 0)
+
+
 def test_rows_that_see_nothing(g):
     """Documents without a key, and moments before every key: +0, -inf and no gradient."""
     for dtype in ("f32", "bf16"):

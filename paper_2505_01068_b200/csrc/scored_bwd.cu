@@ -14,19 +14,6 @@ namespace {
 // Registers: 24 warps an SM for narrow heads, 16 and 12 for wide ones, whose accumulators are larger.
 template <int HD, int W> constexpr int MIN_CTAS = (HD <= 16 ? 24 : HD == 32 ? 16 : 12) / W;
 
-// x (scores less the row's log-sum-exp), dp (less delta, times the cap's derivative) -> the weights p (where wanted) and ds = p dp, packed.
-template <bool PACK_P, int N>
-__device__ __forceinline__ void weigh(const float (&x)[N][4], const float (&dp)[N][4], uint32_t (&wp)[PACK_P ? N : 1][2], uint32_t (&ws)[N][2]) {
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float2 p = make_float2(ptx::ex2(x[n][2 * i]), ptx::ex2(x[n][2 * i + 1])), ds = __fmul2_rn(p, make_float2(dp[n][2 * i], dp[n][2 * i + 1]));
-      if constexpr (PACK_P) wp[n][i] = ptx::pack_bf16(p.x, p.y);
-      ws[n][i] = ptx::pack_bf16(ds.x, ds.y);
-    }
-}
-
 template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W>)
 scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
@@ -139,25 +126,29 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       z[0] = z[1] = -delta[m][0];
       z[2] = z[3] = -delta[m][1];
     });
-    uint32_t w[MT][NT][2], unused[1][2];
+    uint32_t w[MT][NT][2];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      dots_to_scores<CAP, true, NT>(x[m], dp[m], a, [&](int, int i) { return make_float2(lse2[m][i], lse2[m][i]); });
-      if constexpr (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
-      if constexpr (SOME_SHUT) {
+    for (int m = 0; m < MT; ++m)
+      in_form<CAP, NT>(x[m], a, [&](auto near) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+          float2 times = make_float2(0.f, 0.f);
+          if constexpr (BIAS) times = *reinterpret_cast<const float2*>(&s_time[buf][j + 8 * n + 2 * (lane & 3)]);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int col = j + 8 * n + 2 * (lane & 3) + e;
-            const bool in = col < rem;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
+          for (int i = 0; i < 2; ++i) {
+            float2 d = make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]);
+            float2 y = score_pair<CAP, true, decltype(near)::value != 0>(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(lse2[m][i], lse2[m][i]), d, a);
+            if constexpr (BIAS) y = bias_pair(y, times, own_time[m][i], slope2);
+            if constexpr (SOME_SHUT) {
+              auto shut = [&](int col) { return col >= rem || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i])); };
+              const int col = j + 8 * n + 2 * (lane & 3);
+              y = make_float2(shut(col) ? -INFINITY : y.x, shut(col + 1) ? -INFINITY : y.y);
+            }
+            const float2 ds = __fmul2_rn(make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), d);
+            w[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
           }
-      }
-      weigh<false, NT>(x[m], dp[m], unused, w[m]);
-    }
+        }
+      });
     __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, NT>(dq, w, at_kk, from);
   };
@@ -319,22 +310,28 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     });
     uint32_t wp[MT][NT][2], ws[MT][NT][2];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      dots_to_scores<CAP, true, NT>(x[m], dp[m], a, [&](int n, int) { return lse2[n]; });
-      if constexpr (BIAS) add_bias<NT>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
-      if constexpr (SOME_SHUT) {
+    for (int m = 0; m < MT; ++m)
+      in_form<CAP, NT>(x[m], a, [&](auto near) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+          float2 times = make_float2(0.f, 0.f);
+          if constexpr (BIAS) times = *reinterpret_cast<const float2*>(&s_time[buf][j + 8 * n + 2 * (lane & 3)]);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int col = j + 8 * n + 2 * (lane & 3) + e;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (own_time[m][i] > s_limit[buf][col] || s_doc[buf][col] != own_doc[m][i]) x[m][n][2 * i + e] = -INFINITY;
+          for (int i = 0; i < 2; ++i) {
+            float2 d = make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]);
+            float2 y = score_pair<CAP, true, decltype(near)::value != 0>(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), lse2[n], d, a);
+            if constexpr (BIAS) y = bias_pair(y, times, own_time[m][i], slope2);
+            if constexpr (SOME_SHUT) {   // columns past the last row have an lse of +inf: no weight
+              auto shut = [&](int col) { return own_time[m][i] > s_limit[buf][col] || s_doc[buf][col] != own_doc[m][i]; };
+              const int col = j + 8 * n + 2 * (lane & 3);
+              y = make_float2(shut(col) ? -INFINITY : y.x, shut(col + 1) ? -INFINITY : y.y);
+            }
+            const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), ds = __fmul2_rn(p, d);
+            wp[m][n][i] = ptx::pack_bf16(p.x, p.y);
+            ws[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
           }
-      }
-      weigh<true, NT>(x[m], dp[m], wp[m], ws[m]);
-    }
+        }
+      });
     __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, NT>(dv, wp, at_gk, from);
     product_over_partners<HD, MT, NT>(dk, ws, at_qk, from);

@@ -107,29 +107,33 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     uint32_t w[MT][N][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      float unused[1][4];
-      dots_to_scores<CAP, false, N>(x[m], unused, a, [&](int, int i) { return make_float2(ref[m][i], ref[m][i]); });
-      if constexpr (BIAS) add_bias<N>(x[m], own_time[m], s_time[buf] + j, lane, slope2);
-      if constexpr (SOME_SHUT) {
+      float top[2] = {-INFINITY, -INFINITY};
+      float2 added[2] = {};
+      in_form<CAP, N>(x[m], a, [&](auto near) {
 #pragma unroll
-        for (int n = 0; n < N; ++n)
+        for (int n = 0; n < N; ++n) {
+          float2 times = make_float2(0.f, 0.f), none;
+          if constexpr (BIAS) times = *reinterpret_cast<const float2*>(&s_time[buf][j + 8 * n + 2 * (lane & 3)]);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int col = j + 8 * n + 2 * (lane & 3) + e;
-            const bool in = col < rem;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (!in || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i]))) x[m][n][2 * i + e] = -INFINITY;
+          for (int i = 0; i < 2; ++i) {
+            float2 y = score_pair<CAP, false, decltype(near)::value != 0>(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(ref[m][i], ref[m][i]), none, a);
+            if constexpr (BIAS) y = bias_pair(y, times, own_time[m][i], slope2);
+            if constexpr (SOME_SHUT) {
+              auto shut = [&](int col) { return col >= rem || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i])); };
+              const int col = j + 8 * n + 2 * (lane & 3);
+              y = make_float2(shut(col) ? -INFINITY : y.x, shut(col + 1) ? -INFINITY : y.y);
+            }
+            top[i] = ptx::fmax3(top[i], y.x, y.y);
+            x[m][n][2 * i] = y.x;
+            x[m][n][2 * i + 1] = y.y;
+            const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
+            added[i] = __fadd2_rn(added[i], p);
+            w[m][n][i] = ptx::pack_bf16(p.x, p.y);
           }
-      }
-      // as long as no lane's own scores ask for it, the lanes of a row need not be brought together
-      float top[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        top[i] = -INFINITY;
-#pragma unroll
-        for (int n = 0; n < N; ++n) top[i] = ptx::fmax3(top[i], x[m][n][2 * i], x[m][n][2 * i + 1]);
-      }
+        }
+      });
+      // rare: a score has outgrown its row's reference (as long as no lane's own have, the lanes of a row need not be brought together);
+      // the weights once more, relative to a new one
       if (__any_sync(0xffffffffu, top[0] > room[m][0] || top[1] > room[m][1])) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -145,22 +149,18 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
             }
             ref[m][i] += top[i];
             room[m][i] = 8.f;
+            added[i] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-              x[m][n][2 * i] -= top[i];
-              x[m][n][2 * i + 1] -= top[i];
+              const float2 p = make_float2(ptx::ex2(x[m][n][2 * i] - top[i]), ptx::ex2(x[m][n][2 * i + 1] - top[i]));
+              added[i] = __fadd2_rn(added[i], p);
+              w[m][n][i] = ptx::pack_bf16(p.x, p.y);
             }
           }
         }
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-          const float2 p = make_float2(ptx::ex2(x[m][n][2 * i]), ptx::ex2(x[m][n][2 * i + 1]));
-          sum[m][i] = __fadd2_rn(sum[m][i], p);
-          w[m][n][i] = ptx::pack_bf16(p.x, p.y);
-        }
+      for (int i = 0; i < 2; ++i) sum[m][i] = __fadd2_rn(sum[m][i], added[i]);
     }
     __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, N>(o, w, at_v, from);

@@ -57,22 +57,6 @@ struct Maps {
   CUtensorMap own0, own1, partner0, partner1;
 };
 
-// Two dots -> scores in base 2 less m; d *= derivative of the cap (as dots_to_scores()).  NEAR: tanh's arguments are at most 1/4.
-template <bool CAP, bool BEND, bool NEAR> __device__ __forceinline__ float2 score_pair(float2 y, float2 m, float2& d, const ScoredArgs& a) {
-  auto both = [](float v) { return make_float2(v, v); };
-  m = make_float2(-m.x, -m.y);
-  if constexpr (!CAP) {
-    return __ffma2_rn(y, both(a.inner), m);
-  } else if constexpr (NEAR) {
-    const float2 z = __fmul2_rn(y, y);
-    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0])));
-    return __ffma2_rn(__ffma2_rn(__ffma2_rn(z, both(a.near_p[2]), both(a.near_p[1])), z, both(a.near_p[0])), y, m);
-  } else {
-    const float2 t = tanh_any2(__fmul2_rn(y, both(a.inner)));
-    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(make_float2(-t.x, -t.y), t, both(1.f)));
-    return __ffma2_rn(t, both(a.outer), m);
-  }
-}
 // The largest argument of a row's dots.
 template <int N> __device__ __forceinline__ float largest(const float (&x)[N]) {
   float top[4] = {};
@@ -645,6 +629,20 @@ cudaError_t launch(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
 }
 
 }  // namespace
+
+// Which calls these kernels serve: those with a row that walks more than one tile.  Forward / gradients, us, these and mma.sync tiles, 30 as
+// cap: 32 x (50, 50, 50), 4 heads 9.9 / 22.5 and 6.3 / 15.5; 2 x (8, 12, 10) 5.3 / 11.3 and 4.7 / 6.8; 8 x (39, 55, 400), 2 heads 10.1 / 24.5
+// and 10.3 / 29.1; 1 x (50, 500, 500), 8 heads 10.9 / 27.2 and 12.3 / 35.2; 4 x (128, 1024, 1024) 38 / 98 and 54 / 189.
+bool scored_tc_preferred(const Geometry& g) {
+  int longest = 0;
+  for (int s = 0; s < 3; ++s) {
+    int walk = 0;
+    for (int r = 0; r < 3; ++r)
+      if ((g.allowed >> (3 * s + r)) & 1u) walk += g.seg_len[r];
+    longest = walk > longest ? walk : longest;
+  }
+  return g.hd == HD && longest > PARTNER;
+}
 
 cudaError_t launch_scored_fwd_tc(const Geometry& g, const ScoredArgs& a, cudaStream_t st) { return launch<FWD>(g, a, st); }
 

@@ -150,66 +150,45 @@ __device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4],
 }
 __device__ __forceinline__ void from_zero(int, int, float (&z)[4]) { z[0] = z[1] = z[2] = z[3] = 0.f; }
 
-// Dots -> scores in base 2 less minus(tile, row half), a pair for two columns (in place), and where wanted d *= derivative of the cap.
-// With a cap, one range check for the whole warp decides between polynomials of the dot (quadratics of its square: 4 multiply-adds a
-// score with the subtraction, 3 more for the derivative) and the form for any argument.  The FMA pipe is what these kernels fill first.
-template <bool CAP, bool BEND, int NT, typename Minus>
-__device__ __forceinline__ void dots_to_scores(float (&x)[NT][4], float (&d)[BEND ? NT : 1][4], const ScoredArgs& a, Minus minus) {
-  auto each = [&](auto score) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float2 m = minus(n, i);
-        float2 bend = make_float2(1.f, 1.f);
-        const float2 y = score(make_float2(x[n][2 * i], x[n][2 * i + 1]), make_float2(-m.x, -m.y), bend);
-        x[n][2 * i] = y.x;
-        x[n][2 * i + 1] = y.y;
-        if constexpr (CAP && BEND) {
-          const float2 e = __fmul2_rn(make_float2(d[n][2 * i], d[n][2 * i + 1]), bend);
-          d[n][2 * i] = e.x;
-          d[n][2 * i + 1] = e.y;
-        }
-      }
-  };
+// Two dots -> scores in base 2 less m; d *= derivative of the cap.  NEAR: tanh's arguments
+// are at most 1/4, and both are polynomials of the dot (quadratics of its square: 4 multiply-adds a score with the subtraction, 3 more for
+// the derivative; the FMA pipe is what these kernels fill first).
+template <bool CAP, bool BEND, bool NEAR> __device__ __forceinline__ float2 score_pair(float2 y, float2 m, float2& d, const ScoredArgs& a) {
   auto both = [](float v) { return make_float2(v, v); };
+  m = make_float2(-m.x, -m.y);
   if constexpr (!CAP) {
-    each([&](float2 y, float2 m, float2&) { return __ffma2_rn(y, both(a.inner), m); });
+    return __ffma2_rn(y, both(a.inner), m);
+  } else if constexpr (NEAR) {
+    const float2 z = __fmul2_rn(y, y);
+    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0])));
+    return __ffma2_rn(__ffma2_rn(__ffma2_rn(z, both(a.near_p[2]), both(a.near_p[1])), z, both(a.near_p[0])), y, m);
   } else {
+    const float2 t = tanh_any2(__fmul2_rn(y, both(a.inner)));
+    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(make_float2(-t.x, -t.y), t, both(1.f)));
+    return __ffma2_rn(t, both(a.outer), m);
+  }
+}
+// score -= slope2 * |own time - partner time| for a pair of partners
+__device__ __forceinline__ float2 bias_pair(float2 y, float2 times, float own, float slope2) {
+  const float2 d = __fadd2_rn(times, make_float2(-own, -own));
+  return __ffma2_rn(make_float2(fabsf(d.x), fabsf(d.y)), make_float2(-slope2, -slope2), y);
+}
+// Runs body(NEAR) for a tile of dots.  One decision for the warp, ahead of everything, so that the multiply-adds of some columns and the
+// exponentials of others are one stream of instructions.
+template <bool CAP, int NT, typename Body>
+__device__ __forceinline__ void in_form(const float (&x)[NT][4], const ScoredArgs& a, Body body) {
+  if constexpr (CAP) {
     float top = 0.f;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; i += 2) top = ptx::fmax3(top, fabsf(x[n][i]), fabsf(x[n][i + 1]));
     if (__any_sync(0xffffffffu, top > a.near_dot)) {
-      each([&](float2 y, float2 m, float2& bend) {
-        const float2 t = tanh_any2(__fmul2_rn(y, both(a.inner)));
-        if constexpr (BEND) bend = __ffma2_rn(make_float2(-t.x, -t.y), t, bend);
-        return __ffma2_rn(t, both(a.outer), m);
-      });
-    } else {
-      each([&](float2 y, float2 m, float2& bend) {
-        const float2 z = __fmul2_rn(y, y);
-        if constexpr (BEND) bend = __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0]));
-        return __ffma2_rn(__ffma2_rn(__ffma2_rn(z, both(a.near_p[2]), both(a.near_p[1])), z, both(a.near_p[0])), y, m);
-      });
+      body(IntTag<0>{});
+      return;
     }
   }
-}
-// x -= slope2 * |own time - partner time|.  own[2]: rows g, g + 8; partner times in shared memory from column 0 on.
-template <int NT> __device__ __forceinline__ void add_bias(float (&x)[NT][4], const float (&own)[2], const float* times, int lane, float slope2) {
-  const float2 f = make_float2(-slope2, -slope2);
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const float2 t = *reinterpret_cast<const float2*>(times + 8 * n + 2 * (lane & 3));
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float2 d = __fadd2_rn(t, make_float2(-own[i], -own[i]));
-      const float2 y = __ffma2_rn(make_float2(fabsf(d.x), fabsf(d.y)), f, make_float2(x[n][2 * i], x[n][2 * i + 1]));
-      x[n][2 * i] = y.x;
-      x[n][2 * i + 1] = y.y;
-    }
-  }
+  body(IntTag<1>{});
 }
 
 // ---- which pairs of a block are open ----

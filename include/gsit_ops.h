@@ -88,7 +88,7 @@ typedef struct gsit_score_rule {
 /*   q              [B, Lq, heads, hd], k, v [B, L, kv_heads, hd], each with a row stride of its own (elements); Lq = L without tail
  *   out            [B, Lq, d] contiguous;  lse float [B, heads, Lq] or NULL
  *   bf16: head_dim 8, 16, 32 or 64, pointers 16-byte aligned, row strides multiples of 8;  f32: head_dim <= 128
- *   workspace      gsit_scored_attention_fwd_workspace() bytes, 16-byte aligned; may be NULL where that is 0 */
+ *   workspace      gsit_scored_attention_fwd_workspace() bytes: none, so NULL and 0 will do */
 gsit_status gsit_im_scored_attention_fwd(const gsit_shape* shape, const gsit_score_rule* rule, const void* q, int64_t q_row_stride,
                                          const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride, void* out, float* lse,
                                          void* workspace, size_t workspace_bytes, gsit_stream stream);

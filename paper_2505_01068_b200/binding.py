@@ -329,14 +329,14 @@ def layer_norm_bwd(dy, x, mean, rstd, gamma=None, seg_len=None, valid_len=None, 
 
 
 def im_scored_attention_fwd(q, k, v, seg_len, valid_len=None, phase=PHASE_INTER_FWD, custom_mask=0, scale=0.0, softcap=0.0, slopes=None,
-                            times=None, documents=None, causal=False, prefix=None, q_len=None, want_lse=False, out=None, workspace=None):
+                            times=None, documents=None, causal=False, prefix=None, q_len=None, want_lse=False, out=None):
     """im_attention_fwd with a rule on the scores x = scale * q.k:  softcap > 0: softcap * tanh(x / softcap);  slopes float32 [H]:
     less slopes[h] * |time_i - time_j|, times float32 [B, L] (default: the index inside the segment);  documents int32 [B, L]: only
     keys of the query's document;  causal: only keys with time_j <= time_i, or time_j < prefix[b] (float32 [B]).
     q [B, L, H, hd], k and v [B, L, Hk, hd] with H a multiple of Hk, row strides free.  Returns out [B, L, d] (and lse [B, H, L]).
     q_len (three numbers): q holds only that many newest positions of each segment, [B, sum(q_len), H, hd], and so does out."""
     return native().scored_fwd(q, k, v, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix, q_len,
-                               want_lse, out, workspace)
+                               want_lse, out)
 
 
 def im_scored_attention_bwd(dout, q, k, v, out, lse, seg_len, valid_len=None, phase=PHASE_INTER_FWD, custom_mask=0, scale=0.0, softcap=0.0,

@@ -97,8 +97,7 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
   return GSIT_OK;
 }
 
-// Which kernels serve a call, and the scratch they need.
-size_t scored_fwd_scratch(const Geometry&, int, const ScoredArgs&) { return 0; }
+// Which kernels serve a call, and the scratch they need (forward: none, running sums and joins stay on the SMs).
 cudaError_t launch_scored_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
   if (scored_tail_supported(g, dtype, a)) return launch_scored_tail(g, dtype, a, st);
   if (dtype == GSIT_BF16) return scored_tc_preferred(g) ? launch_scored_fwd_tc(g, a, st) : launch_scored_fwd_bf16(g, a, st);
@@ -197,12 +196,12 @@ gsit_status gsit_layer_norm_bwd(const gsit_shape* shape, int32_t y_dtype, const 
 size_t gsit_scored_attention_fwd_workspace(const gsit_shape* shape, const gsit_score_rule* rule) {
   Geometry g;
   ScoredArgs a;
-  return scored_args(shape, rule, &g, &a) == GSIT_OK ? scored_fwd_scratch(g, shape->dtype, a) : (size_t)-1;
+  return scored_args(shape, rule, &g, &a) == GSIT_OK ? 0 : (size_t)-1;
 }
 
 gsit_status gsit_im_scored_attention_fwd(const gsit_shape* shape, const gsit_score_rule* rule, const void* q, int64_t q_row_stride,
                                          const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride, void* out, float* lse,
-                                         void* workspace, size_t workspace_bytes, gsit_stream stream) {
+                                         void*, size_t, gsit_stream stream) {
   Geometry g;
   ScoredArgs a;
   const gsit_status st = scored_args(shape, rule, &g, &a);
@@ -212,16 +211,12 @@ gsit_status gsit_im_scored_attention_fwd(const gsit_shape* shape, const gsit_sco
   if (!rows_ok(q, q_row_stride, g.d, t) || !rows_ok(k, k_row_stride, dk, t) || !rows_ok(v, v_row_stride, dk, t) || !rows_ok(out, g.d, g.d, t) ||
       !aligned(lse, 4))
     return GSIT_ERR_INVALID_ARG;
-  const size_t need = scored_fwd_scratch(g, t, a);
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return GSIT_ERR_WORKSPACE;
-  if (need > 0 && !aligned(workspace, 16)) return GSIT_ERR_INVALID_ARG;
   if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
   a.q = q; a.ldq = q_row_stride;
   a.k = k; a.ldk = k_row_stride;
   a.v = v; a.ldv = v_row_stride;
   a.out = out; a.ldo = g.d;
   a.lse = lse;
-  a.partial = static_cast<float*>(workspace);
   return status_of(launch_scored_fwd(g, t, a, static_cast<cudaStream_t>(stream)));
 }
 

@@ -11,11 +11,12 @@
 namespace gsit {
 namespace {
 
-// Registers: 24 warps an SM for narrow heads, 16 and 12 for wide ones, whose accumulators are larger.
-template <int HD, int W> constexpr int MIN_CTAS = (HD <= 16 ? 24 : HD == 32 ? 16 : 12) / W;
+// Registers: 24 warps an SM for narrow heads (32 for dq, which holds less; MOSEI step: dq 94 -> 87 us, dk and dv 96 -> 98), 16 and 12 for
+// wide ones, whose accumulators are larger.
+template <int HD, int W, int NARROW> constexpr int MIN_CTAS = (HD <= 16 ? NARROW : HD == 32 ? 16 : 12) / W;
 
 template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W>)
+__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W, 32>)
 scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
   constexpr bool TIMES = BIAS || MASK;
@@ -23,14 +24,13 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
   __shared__ int s_doc[2][MASK ? KC : 1];
   const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31;
-  const int h = blockIdx.x % g.heads, b = blockIdx.y, hk = h / a.group;
-  int s;
-  const int tile = find_tile(tiles, blockIdx.x / g.heads, s);
+  const Place at = find_place(tiles, g.batch, g.heads);
+  const int b = at.sample, s = at.segment, h = at.head, hk = h / a.group;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
 
-  const int q0 = tile * TQ, n_q = valid_rows(g, b, s), q_end = min(q0 + TQ, g.len(s));
+  const int q0 = at.tile * TQ, n_q = valid_rows(g, b, s), q_end = min(q0 + TQ, g.len(s));
   Walk next = {};
 #pragma unroll
   for (int r = 0; r < 3; ++r) next.n[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
@@ -127,9 +127,9 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       z[2] = z[3] = -delta[m][1];
     });
     uint32_t w[MT][NT][2];
+    in_form<CAP, MT, NT>(x, a, [&](auto near) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-      in_form<CAP, NT>(x[m], a, [&](auto near) {
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float2 times = make_float2(0.f, 0.f);
@@ -148,7 +148,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
             w[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
           }
         }
-      });
+    });
     __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, NT>(dq, w, at_kk, from);
   };
@@ -205,7 +205,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
 }
 
 template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W>)
+__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W, 24>)
 scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
   constexpr bool TIMES = BIAS || MASK;
@@ -214,14 +214,13 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   __shared__ __align__(16) float s_time[2][TIMES ? QC : 4], s_limit[2][MASK ? QC : 4];
   __shared__ int s_doc[2][MASK ? QC : 1];
   const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31;
-  const int hk = blockIdx.x % a.kv_heads, b = blockIdx.y;
-  int r;
-  const int tile = find_tile(tiles, blockIdx.x / a.kv_heads, r);
+  const Place at = find_place(tiles, g.batch, a.kv_heads);
+  const int b = at.sample, r = at.segment, hk = at.head;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
 
-  const int k0 = tile * TK, n_k = valid_rows(g, b, r), k_end = min(k0 + TK, g.len(r));
+  const int k0 = at.tile * TK, n_k = valid_rows(g, b, r), k_end = min(k0 + TK, g.len(r));
   Walk next = {};
 #pragma unroll
   for (int s = 0; s < 3; ++s) next.n[s] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, s) : 0;
@@ -309,9 +308,9 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
       z[1] = z[3] = delta[n].y;
     });
     uint32_t wp[MT][NT][2], ws[MT][NT][2];
+    in_form<CAP, MT, NT>(x, a, [&](auto near) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-      in_form<CAP, NT>(x[m], a, [&](auto near) {
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float2 times = make_float2(0.f, 0.f);
@@ -331,7 +330,7 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
             ws[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
           }
         }
-      });
+    });
     __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, NT>(dv, wp, at_gk, from);
     product_over_partners<HD, MT, NT>(dk, ws, at_qk, from);
@@ -416,9 +415,9 @@ cudaError_t launch_pass(const Geometry& g, const ScoredArgs& a, int heads, uint3
   Tiles t = {};
   t.order = segment_order(g, walks);
   const bool tall = HD <= 32 && make_tiles(&t, g.seg_len, 128) * heads * g.batch >= 6LL * n_sm;
-  const int64_t n = make_tiles(&t, g.seg_len, tall ? 128 : 64) * heads;
+  const int64_t n = make_tiles(&t, g.seg_len, tall ? 128 : 64) * heads * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
-  const dim3 grid((unsigned)n, g.batch);
+  const dim3 grid((unsigned)n);
   return tall ? launch_rule<K, HD, 1, HD <= 32 ? 8 : 4>(g, a, t, grid, st) : launch_rule<K, HD, 1, 4>(g, a, t, grid, st);
 }
 template <int HD>

@@ -206,13 +206,12 @@ scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
   __shared__ Times own, partner;
   __shared__ __align__(16) float s_row[TILE];   // what the accumulators are scaled by, per row
   __shared__ int s_any;
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = blockIdx.x % g.heads, b = blockIdx.y, hk = h / a.group;
-  int s;
-  const int tile = find_tile(tiles, blockIdx.x / g.heads, s);
+  const Place at = find_place(tiles, g.batch, g.heads);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = at.head, b = at.sample, hk = h / a.group, s = at.segment;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int q0 = tile * TILE, q_end = min(q0 + TILE, a.q_len[s]);
+  const int q0 = at.tile * TILE, q_end = min(q0 + TILE, a.q_len[s]);
   const QueryRows rows = query_rows(g, a, b, s);
   const bool rule = rule_masks(a) || a.slopes != nullptr, work = max(q0, rows.lo) < min(q_end, rows.hi);
   const int64_t row0 = (int64_t)b * a.Lq + a.q_off[s] + q0;
@@ -299,13 +298,12 @@ scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__
   __shared__ Times own, partner;
   __shared__ float2 s_stats[TILE];
   __shared__ int s_any;
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = blockIdx.x % g.heads, b = blockIdx.y, hk = h / a.group;
-  int s;
-  const int tile = find_tile(tiles, blockIdx.x / g.heads, s);
+  const Place at = find_place(tiles, g.batch, g.heads);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = at.head, b = at.sample, hk = h / a.group, s = at.segment;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int q0 = tile * TILE, q_end = min(q0 + TILE, g.len(s)), n_q = valid_rows(g, b, s);
+  const int q0 = at.tile * TILE, q_end = min(q0 + TILE, g.len(s)), n_q = valid_rows(g, b, s);
   const bool rule = rule_masks(a) || a.slopes != nullptr;
   const int64_t row0 = (int64_t)b * g.L + g.off(s) + q0, stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s) + q0;
   const float slope2 = a.slopes != nullptr ? a.slopes[h] * LOG2E : 0.f;
@@ -386,13 +384,12 @@ scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
   __shared__ Times own, partner;
   __shared__ float2 s_stats[TILE];
   __shared__ int s_any;
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, hk = blockIdx.x % a.kv_heads, b = blockIdx.y;
-  int r;
-  const int tile = find_tile(tiles, blockIdx.x / a.kv_heads, r);
+  const Place at = find_place(tiles, g.batch, a.kv_heads);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, hk = at.head, b = at.sample, r = at.segment;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int k0 = tile * TILE, k_end = min(k0 + TILE, g.len(r)), n_k = valid_rows(g, b, r), n_rows = min(k_end, n_k) - k0;
+  const int k0 = at.tile * TILE, k_end = min(k0 + TILE, g.len(r)), n_k = valid_rows(g, b, r), n_rows = min(k_end, n_k) - k0;
   const bool rule = rule_masks(a) || a.slopes != nullptr;
   const int64_t key0 = (int64_t)b * g.L + g.off(r) + k0;
   const Piece<HD> piece;
@@ -471,13 +468,13 @@ cudaError_t launch(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
   const int heads = PASS == DKV ? a.kv_heads : g.heads;
   Tiles t = {};
   t.order = segment_order(g, PASS == DKV ? transposed(g.allowed) : g.allowed);
-  const int64_t n = make_tiles(&t, PASS == FWD ? a.q_len : g.seg_len, TILE) * heads;
+  const int64_t n = make_tiles(&t, PASS == FWD ? a.q_len : g.seg_len, TILE) * heads * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const auto kernel = PASS == FWD ? scored_fwd_f32_kernel<HD> : PASS == DQ ? scored_dq_f32_kernel<HD> : scored_dkv_f32_kernel<HD>;
   constexpr int bytes = smem_bytes<HD>(PASS);
   const cudaError_t e = sm_count_and_smem_once(reinterpret_cast<const void*>(kernel), bytes, nullptr);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(kernel, dim3((unsigned)n, g.batch), dim3(THREADS), bytes, st, g, a, t);
+  return launch_overlapped(kernel, dim3((unsigned)n), dim3(THREADS), bytes, st, g, a, t);
 }
 template <int PASS>
 cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {

@@ -4,27 +4,26 @@
 namespace gsit {
 namespace {
 
-// Registers: as many warps as hide the latency of a step's chain of products, exponentials and products (24 an SM for narrow heads, 16
+// Registers: as many warps as hide the latency of a step's chain of products, exponentials and products (32 an SM for narrow heads, 16
 // and 8 for wide ones, whose accumulators are larger).
-template <int HD, int MT, int W> constexpr int MIN_CTAS = (HD <= 16 ? 24 : HD == 32 ? 16 : MT == 2 ? 8 : 16) / W;
+template <int HD, int MT, int W> constexpr int MIN_CTAS = (HD <= 16 ? 32 : HD == 32 ? 16 : MT == 2 ? 8 : 16) / W;
 
 template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, MT, W>)
 scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 8 : 4;
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = 4, NS = HD == 8 ? 4 : 2;   // tiles of 8 keys in a step, and where some pairs are shut
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
   __shared__ int s_doc[2][MASK ? KC : 1];
   const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31;
-  const int h = blockIdx.x % g.heads, b = blockIdx.y, hk = h / a.group;
-  int s;
-  const int tile = find_tile(tiles, blockIdx.x / g.heads, s);
+  const Place at = find_place(tiles, g.batch, g.heads);
+  const int b = at.sample, s = at.segment, h = at.head, hk = h / a.group;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
 
-  const int q0 = tile * TQ, q_end = min(q0 + TQ, a.q_len[s]);
+  const int q0 = at.tile * TQ, q_end = min(q0 + TQ, a.q_len[s]);
   const QueryRows rows = query_rows(g, a, b, s);
   Walk next = {};
 #pragma unroll
@@ -105,11 +104,13 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     const uint32_t from = (buf * KC + j) * HD * 2;
     product_over_features<HD, MT, N>(x, qf, at_k, from, from_zero);
     uint32_t w[MT][N][2];
+    float top[MT][2];
+    float2 added[MT][2] = {};
+    bool outgrown = false;
+    in_form<CAP, MT, N>(x, a, [&](auto near) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      float top[2] = {-INFINITY, -INFINITY};
-      float2 added[2] = {};
-      in_form<CAP, N>(x[m], a, [&](auto near) {
+      for (int m = 0; m < MT; ++m) {
+        top[m][0] = top[m][1] = -INFINITY;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
           float2 times = make_float2(0.f, 0.f), none;
@@ -123,45 +124,52 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
               const int col = j + 8 * n + 2 * (lane & 3);
               y = make_float2(shut(col) ? -INFINITY : y.x, shut(col + 1) ? -INFINITY : y.y);
             }
-            top[i] = ptx::fmax3(top[i], y.x, y.y);
+            top[m][i] = ptx::fmax3(top[m][i], y.x, y.y);
             x[m][n][2 * i] = y.x;
             x[m][n][2 * i + 1] = y.y;
             const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y));
-            added[i] = __fadd2_rn(added[i], p);
+            added[m][i] = __fadd2_rn(added[m][i], p);
             w[m][n][i] = ptx::pack_bf16(p.x, p.y);
           }
         }
-      });
-      // rare: a score has outgrown its row's reference (as long as no lane's own have, the lanes of a row need not be brought together);
-      // the weights once more, relative to a new one
-      if (__any_sync(0xffffffffu, top[0] > room[m][0] || top[1] > room[m][1])) {
+        outgrown = outgrown || top[m][0] > room[m][0] || top[m][1] > room[m][1];
+      }
+    });
+    // rare: a score has outgrown its row's reference (as long as no lane's own have, the lanes of a row need not be brought together);
+    // the weights once more, relative to a new one
+    if (__any_sync(0xffffffffu, outgrown)) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-          if (top[i] > room[m][i]) {
-            const float f = room[m][i] == -INFINITY ? 1.f : ptx::ex2(-top[i]);   // nothing to scale down before the first open key
+          float t = fmaxf(top[m][i], __shfl_xor_sync(0xffffffffu, top[m][i], 1));
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+          if (t > room[m][i]) {
+            // nothing to scale down before the first open key.  The first reference is a maximum in any case: a weight of 1 is exact in
+            // bf16, and with it the output of a row that sees one key
+            const float f = room[m][i] == -INFINITY ? 1.f : ptx::ex2(-t);
+            room[m][i] = 8.f;
             sum[m][i] = __fmul2_rn(sum[m][i], make_float2(f, f));
 #pragma unroll
             for (int q = 0; q < CH; ++q) {
               o[m][q][2 * i] *= f;
               o[m][q][2 * i + 1] *= f;
             }
-            ref[m][i] += top[i];
-            room[m][i] = 8.f;
-            added[i] = make_float2(0.f, 0.f);
+            ref[m][i] += t;
+            added[m][i] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-              const float2 p = make_float2(ptx::ex2(x[m][n][2 * i] - top[i]), ptx::ex2(x[m][n][2 * i + 1] - top[i]));
-              added[i] = __fadd2_rn(added[i], p);
+              const float2 p = make_float2(ptx::ex2(x[m][n][2 * i] - t), ptx::ex2(x[m][n][2 * i + 1] - t));
+              added[m][i] = __fadd2_rn(added[m][i], p);
               w[m][n][i] = ptx::pack_bf16(p.x, p.y);
             }
           }
         }
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) sum[m][i] = __fadd2_rn(sum[m][i], added[i]);
     }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sum[m][i] = __fadd2_rn(sum[m][i], added[m][i]);
     __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
     product_over_partners<HD, MT, N>(o, w, at_v, from);
   };
@@ -179,7 +187,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 #pragma unroll 1
       for (; j + 8 * NT <= rem; j += 8 * NT) step(IntTag<NT>{}, IntTag<0>{}, buf, j, rem);
 #pragma unroll 1
-      for (; j < rem; j += 4 * NT) step(IntTag<NT / 2>{}, IntTag<1>{}, buf, j, rem);
+      for (; j < rem; j += 8 * NS) step(IntTag<NS>{}, IntTag<1>{}, buf, j, rem);
     } else {
 #pragma unroll 1
       while (j < rem) {
@@ -190,7 +198,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
           for (; j < end; j += 8 * NT) step(IntTag<NT>{}, IntTag<0>{}, buf, j, rem);
         else if (open != SHUT)
 #pragma unroll 1
-          for (; j < end; j += 4 * NT) step(IntTag<NT / 2>{}, IntTag<1>{}, buf, j, rem);
+          for (; j < end; j += 8 * NS) step(IntTag<NS>{}, IntTag<1>{}, buf, j, rem);
         j = end;
       }
     }
@@ -246,9 +254,9 @@ cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st
   t.order = segment_order(g, g.allowed);
   // 128 rows a CTA where that still makes several CTAs per SM, 64 below
   const bool tall = make_tiles(&t, a.q_len, 128) * g.heads * g.batch >= 6LL * n_sm;
-  const int64_t n = make_tiles(&t, a.q_len, tall ? 128 : 64) * g.heads;
+  const int64_t n = make_tiles(&t, a.q_len, tall ? 128 : 64) * g.heads * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
-  const dim3 grid((unsigned)n, g.batch);
+  const dim3 grid((unsigned)n);
   constexpr int MT = HD == 64 ? 2 : 1;   // wide heads: a row tile more per fragment of K and V that is read
   return tall ? launch_rule<HD, MT, 8 / MT>(g, a, t, grid, st) : launch_rule<HD, 1, 4>(g, a, t, grid, st);
 }

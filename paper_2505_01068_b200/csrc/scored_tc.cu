@@ -107,9 +107,8 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
   grid_dep_launch();
 
   // ---- the CTA's rows: [o0, o_end) of segment s of sample b, of which [lo, hi) are real; position = row + shift ----
-  const int own_heads = KIND == DKV ? a.kv_heads : g.heads, h = blockIdx.x % own_heads, b = blockIdx.y;
-  int s;
-  const int o0 = find_tile(tiles, blockIdx.x / own_heads, s) * OWN;
+  const Place at = find_place(tiles, g.batch, KIND == DKV ? a.kv_heads : g.heads);
+  const int h = at.head, b = at.sample, s = at.segment, o0 = at.tile * OWN;
   const QueryRows rows = KIND == FWD ? query_rows(g, a, b, s) : QueryRows{0, valid_rows(g, b, s), 0};
   const int own_len = KIND == FWD ? a.q_len[s] : g.len(s), o_end = min(o0 + OWN, own_len), lo = max(o0, rows.lo), hi = min(o_end, rows.hi);
   const int64_t own_row0 = KIND == FWD ? (int64_t)b * a.Lq + a.q_off[s] : (int64_t)b * g.L + g.off(s);
@@ -620,9 +619,9 @@ cudaError_t launch(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
   if (!ok) return cudaErrorInvalidValue;
   Tiles t = {};
   t.order = segment_order(g, KIND == DKV ? transposed(g.allowed) : g.allowed);
-  const int64_t n = make_tiles(&t, KIND == FWD ? a.q_len : g.seg_len, OWN) * (KIND == DKV ? a.kv_heads : g.heads);
+  const int64_t n = make_tiles(&t, KIND == FWD ? a.q_len : g.seg_len, OWN) * (KIND == DKV ? a.kv_heads : g.heads) * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
-  const dim3 grid((unsigned)n, g.batch);
+  const dim3 grid((unsigned)n);
   const bool cap = a.softcap > 0.f, bias = a.slopes != nullptr;
   return cap ? (bias ? launch_masked<KIND, true, true>(maps, g, a, t, grid, st) : launch_masked<KIND, true, false>(maps, g, a, t, grid, st))
              : (bias ? launch_masked<KIND, false, true>(maps, g, a, t, grid, st) : launch_masked<KIND, false, false>(maps, g, a, t, grid, st));

@@ -173,16 +173,18 @@ __device__ __forceinline__ float2 bias_pair(float2 y, float2 times, float own, f
   const float2 d = __fadd2_rn(times, make_float2(-own, -own));
   return __ffma2_rn(make_float2(fabsf(d.x), fabsf(d.y)), make_float2(-slope2, -slope2), y);
 }
-// Runs body(NEAR) for a tile of dots.  One decision for the warp, ahead of everything, so that the multiply-adds of some columns and the
-// exponentials of others are one stream of instructions.
-template <bool CAP, int NT, typename Body>
-__device__ __forceinline__ void in_form(const float (&x)[NT][4], const ScoredArgs& a, Body body) {
+// Runs body(NEAR) for the dots of a step.  One decision for the warp, ahead of everything, so that the multiply-adds of some columns and
+// the exponentials of others are one stream of instructions.
+template <bool CAP, int MT, int NT, typename Body>
+__device__ __forceinline__ void in_form(const float (&x)[MT][NT][4], const ScoredArgs& a, Body body) {
   if constexpr (CAP) {
     float top = 0.f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int i = 0; i < 4; i += 2) top = ptx::fmax3(top, fabsf(x[n][i]), fabsf(x[n][i + 1]));
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) top = ptx::fmax3(top, fabsf(x[m][n][i]), fabsf(x[m][n][i + 1]));
     if (__any_sync(0xffffffffu, top > a.near_dot)) {
       body(IntTag<0>{});
       return;

@@ -624,7 +624,7 @@ PyMethodDef methods[] = {def<init, 1>("init"),
                          def<rotary, 11>("rotary"),
                          def<layer_norm_fwd, 9>("layer_norm_fwd"),
                          def<layer_norm_bwd, 11>("layer_norm_bwd"),
-                         def<scored_fwd, 18>("scored_fwd"),
+                         def<scored_fwd, 17>("scored_fwd"),
                          def<scored_bwd, 19>("scored_bwd"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -221,10 +221,10 @@ gsit_score_rule score_rule(PyObject* const* a, int64_t B, int64_t L, int64_t H, 
 
 const char* const QKV_VIEWS = "q, k, v: [B, L, H, hd] on the device, heads contiguous, rows evenly spaced";
 
-// q, k, v, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix, q_len, want_lse, out, workspace
+// q, k, v, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix, q_len, want_lse, out
 PyObject* scored_fwd(PyObject* const* a) {
   const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
-  const at::Tensor *valid = opt_tensor(a[4]), *out = opt_tensor(a[16]), *ws = opt_tensor(a[17]);
+  const at::Tensor *valid = opt_tensor(a[4]), *out = opt_tensor(a[16]);
   const int64_t ldq = head_rows(q, QKV_VIEWS), ldk = head_rows(k, QKV_VIEWS), ldv = head_rows(v, QKV_VIEWS);
   const int64_t B = q.size(0), Lq = q.size(1), H = q.size(2), hd = q.size(3), L = k.size(1), HK = k.size(2);
   require(k.sizes() == v.sizes() && k.size(0) == B && k.size(3) == hd && k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type(),
@@ -240,22 +240,16 @@ PyObject* scored_fwd(PyObject* const* a) {
     require(Lq == L, "q, k and v share their length (or q_len says how many of the newest positions q holds)");
   }
   const bool want_lse = as_bool(a[15]);
-  at::Tensor made, lse, made_ws;
+  at::Tensor made, lse;
   if (out == nullptr) made = empty({B, Lq, H * hd}, q.scalar_type(), q.device());
   else require(out->is_cuda() && out->is_contiguous() && out->scalar_type() == q.scalar_type() && out->numel() == B * Lq * H * hd, "out: contiguous [B, L, d] of q's dtype");
   if (want_lse) lse = empty({B, H, Lq}, at::kFloat, q.device());
-  const size_t need = gsit_scored_attention_fwd_workspace(&s, &r);
-  if (ws == nullptr && need != (size_t)-1 && need > 0) {
-    made_ws = empty({(int64_t)need}, at::kByte, q.device());
-    ws = &made_ws;
-  }
   void* dst = out != nullptr ? out->data_ptr() : made.data_ptr();
   float* lse_p = want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr;
   gsit_status st;
   {
     NoGil n;
-    st = gsit_im_scored_attention_fwd(&s, &r, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, dst, lse_p, ptr(ws),
-                                      ws == nullptr ? 0 : (size_t)ws->nbytes(), stream());
+    st = gsit_im_scored_attention_fwd(&s, &r, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, dst, lse_p, nullptr, 0, stream());
   }
   check(st, "gsit_im_scored_attention_fwd");
   if (!want_lse) return out != nullptr ? Py_NewRef(a[16]) : THPVariable_Wrap(std::move(made));

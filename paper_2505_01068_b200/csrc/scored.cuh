@@ -260,6 +260,20 @@ __device__ __forceinline__ Place find_place(const Tiles& tiles, int batch, int h
   p.tile = tiles.count[p.segment] - 1 - p.tile;   // from the back: under the causal rule the later rows walk further
   return p;
 }
+// The segments that are walked, in order, in chunks: `pos` is moved on by the caller, settle() goes to the next segment that has rows.
+struct Walk {
+  int n[3];          // rows to walk per segment, 0 where shut
+  int seg, pos;      // where it stands; seg 3: over
+  __device__ __forceinline__ int rows(int s) const { return s == 0 ? n[0] : s == 1 ? n[1] : n[2]; }
+  __device__ __forceinline__ void settle() {   // over segments that hold nothing more
+    if (seg == 0 && pos >= n[0]) { seg = 1; pos = 0; }
+    if (seg == 1 && pos >= n[1]) { seg = 2; pos = 0; }
+    if (seg == 2 && pos >= n[2]) { seg = 3; pos = 0; }
+  }
+  __device__ __forceinline__ bool over() const { return seg == 3; }
+  __device__ __forceinline__ int left() const { return rows(seg) - pos; }
+};
+
 // Tiles of `rows` rows of segments of these lengths; returns their number.
 inline int64_t make_tiles(Tiles* t, const int (&len)[3], int rows) {
   int64_t n = 0;

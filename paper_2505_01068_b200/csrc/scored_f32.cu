@@ -1,39 +1,48 @@
 // Scored attention in single precision, forward and backward, on the FMA pipe (head_dim <= 64).
 //
-// A CTA of 256 threads takes 64 rows (queries in the forward pass and for dq, keys for dk and dv) and walks its partners in tiles of
-// 64.  Two kinds of product, both from row-major tiles in shared memory whose rows are HD + 4 floats apart (any eight lanes that load
-// 16 bytes of neighbouring rows then meet eight different bank groups):
-//   over features  a thread owns rows 4 ty .. and partners tx + 16 j of the 64 x 64 tile: per four features 8 loads of 16 bytes feed 32
-//                  packed multiply-adds, whose halves are the even and the odd features
-//   over partners  the 64 x HD result is owned in pieces of 4 x 4; where that takes fewer than 256 threads the partners of a tile are
-//                  split over groups of them, which are added up once at the end
-// Between the two the weights go through shared memory, partner-major.  With 2 HD (forward), 3 HD (dq) and 4 HD (dk, dv) multiply-adds
-// a pair the FMA pipe is the bound: 128 a clock and SM.
+// A CTA of 256 threads takes 64 rows (queries in the forward pass and for dq, keys for dk and dv), a warp eight of them, and walks the
+// partners in tiles of 64, which cp.async brings into two buffers.  Two kinds of product, both from row-major tiles in shared memory
+// whose rows are HD + 4 floats apart (any eight lanes that load 16 bytes of neighbouring rows then meet eight different bank groups):
+//   over features  a lane owns rows 4 ty .. and partners tx + 16 j of the warp's 8 x 64 pairs: per four features 8 loads of 16 bytes feed
+//                  32 packed multiply-adds, whose halves are the even and the odd features
+//   over partners  the warp's 8 x HD result is owned in pieces of 4 x 4; where that takes fewer than 32 lanes the partners of a tile are
+//                  dealt out to groups of lanes, whose sums shuffles bring together at the end
+// Between the two the weights go through shared memory, partner-major; a warp reads only what its own lanes wrote, so that a tile costs
+// one barrier.  With 2 HD (forward), 3 HD (dq) and 4 HD (dk, dv) multiply-adds a pair the FMA pipe is the bound: 128 a clock and SM.
 #include "scored.cuh"
 
 namespace gsit {
 namespace {
 
-constexpr int THREADS = 256, TILE = 64, PITCH_W = TILE + 4;
+constexpr int THREADS = 256, TILE = 64, WARP_ROWS = 8, WARP_WEIGHTS = TILE * WARP_ROWS;
 
 template <int HD> struct Sizes {
-  static constexpr int PITCH = HD + 4, ROWS = TILE * PITCH;      // floats of a staged tile of rows
-  static constexpr int WEIGHTS = TILE * PITCH_W;                 // floats of a tile of weights, partner-major
-  static constexpr int OWNERS = 4 * HD, GROUPS = THREADS / OWNERS, SHARE = TILE / GROUPS;   // of the 64 x HD result
+  static constexpr int PITCH = HD + 4, ROWS = TILE * PITCH;   // floats of a staged tile of rows
+  static constexpr int OWNERS = HD / 2, GROUPS = 32 / OWNERS; // of a warp's 8 x HD result, in pieces of 4 x 4
 };
 
-// Rows [row0, row0 + TILE) of a [.., ld] matrix (this head's features) into shared memory; zeros from row `n` on and from feature hd on.
+__device__ __forceinline__ void cp_row(float* dst, const float* src, bool real) {    // 16 bytes, zeros where the row is not real
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_float(float* dst, const float* src, bool real) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
+// Rows [0, TILE) behind `src`, a [.., ld] matrix (this head's features), into shared memory; zeros from row `n` >= 1 on and from feature hd on.
 template <int HD> __device__ __forceinline__ void stage_rows(float* dst, const float* src, int64_t ld, int n, int hd) {
   constexpr int P = Sizes<HD>::PITCH;
   if (hd == HD && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(src) & 15u) == 0) {
     for (int i = threadIdx.x; i < TILE * HD / 4; i += THREADS) {
       const int r = i / (HD / 4), c = i % (HD / 4) * 4;
-      *reinterpret_cast<float4*>(dst + r * P + c) = r < n ? *reinterpret_cast<const float4*>(src + r * ld + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      cp_row(dst + r * P + c, src + (r < n ? r * ld + c : 0), r < n);
     }
   } else {
     for (int i = threadIdx.x; i < TILE * HD; i += THREADS) {
       const int r = i / HD, c = i % HD;
-      dst[r * P + c] = r < n && c < hd ? src[r * ld + c] : 0.f;
+      const bool in = r < n && c < hd;
+      cp_float(dst + r * P + c, src + (in ? r * ld + c : 0), in);
     }
   }
 }
@@ -67,27 +76,28 @@ template <int HD> __device__ __forceinline__ void product_over_features(float (&
     for (int j = 0; j < 4; ++j) x[i][j] = s[i][j].x + s[i][j].y;
 }
 
-// w[partner][row] = x
+// The warp's weights: w[partner][row of the warp] = x
 __device__ __forceinline__ void put_weights(float* w, const float (&x)[4][4], int tx, int ty) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(w + (tx + 16 * j) * PITCH_W + 4 * ty) = make_float4(x[0][j], x[1][j], x[2][j], x[3][j]);
+  for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(w + (tx + 16 * j) * WARP_ROWS + 4 * (ty & 1)) = make_float4(x[0][j], x[1][j], x[2][j], x[3][j]);
 }
 
-// This thread's piece of a 64 x HD result: rows 4 rt .., features 4 ct .., and its group's share of the partners.
+// This lane's piece of a warp's 8 x HD result: rows 4 rt .., features 4 ct .., over partners group, group + GROUPS, ...
 template <int HD> struct Piece {
   int rt, ct, group;
   __device__ __forceinline__ Piece() {
-    const int t = threadIdx.x % Sizes<HD>::OWNERS;
+    const int lane = threadIdx.x & 31, t = lane % Sizes<HD>::OWNERS;
     ct = t % (HD / 4);
     rt = t / (HD / 4);
-    group = threadIdx.x / Sizes<HD>::OWNERS;
+    group = lane / Sizes<HD>::OWNERS;
   }
 };
 template <int HD> __device__ __forceinline__ void product_over_partners(float2 (&o)[4][2], const float* w, const float* rows, const Piece<HD>& p) {
-  constexpr int SHARE = Sizes<HD>::SHARE;
+  w += p.group * WARP_ROWS + 4 * p.rt;
+  rows += p.group * Sizes<HD>::PITCH + 4 * p.ct;
 #pragma unroll 4
-  for (int k = p.group * SHARE; k < (p.group + 1) * SHARE; ++k) {
-    const float4 a = *reinterpret_cast<const float4*>(w + k * PITCH_W + 4 * p.rt), v = *reinterpret_cast<const float4*>(rows + k * Sizes<HD>::PITCH + 4 * p.ct);
+  for (int k = 0; k < TILE; k += Sizes<HD>::GROUPS) {
+    const float4 a = *reinterpret_cast<const float4*>(w + k * WARP_ROWS), v = *reinterpret_cast<const float4*>(rows + k * Sizes<HD>::PITCH);
     const float f[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -96,28 +106,21 @@ template <int HD> __device__ __forceinline__ void product_over_partners(float2 (
     }
   }
 }
-// Adds the groups' results up in order; the sums end in group 0.  `room`: (GROUPS - 1) * 64 * HD floats, free.
-template <int HD> __device__ __forceinline__ void join_groups(float2 (&o)[4][2], float* room, const Piece<HD>& p) {
-  constexpr int G = Sizes<HD>::GROUPS;
-  if constexpr (G > 1) {
-    __syncthreads();
-    if (p.group > 0)
+// Adds the groups' results up; every group has the sums.
+template <int HD> __device__ __forceinline__ void join_groups(float2 (&o)[4][2]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(room + ((p.group - 1) * TILE + 4 * p.rt + i) * HD + 4 * p.ct) = make_float4(o[i][0].x, o[i][0].y, o[i][1].x, o[i][1].y);
-    __syncthreads();
-    if (p.group == 0)
-      for (int k = 0; k < G - 1; ++k)
+  for (int d = Sizes<HD>::OWNERS; d < 32; d *= 2)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 v = *reinterpret_cast<const float4*>(room + (k * TILE + 4 * p.rt + i) * HD + 4 * p.ct);
-          o[i][0].x += v.x; o[i][0].y += v.y; o[i][1].x += v.z; o[i][1].y += v.w;
-        }
-  }
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        o[i][e].x += __shfl_xor_sync(0xffffffffu, o[i][e].x, d);
+        o[i][e].y += __shfl_xor_sync(0xffffffffu, o[i][e].y, d);
+      }
 }
 // Row `i` of the piece to memory (group 0); returns whether all of it is finite.
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
-template <int HD> __device__ __forceinline__ bool put_row(float* dst, int hd, const float2 (&o)[2], float scale, bool real, int ct) {
+__device__ __forceinline__ bool put_row(float* dst, int hd, const float2 (&o)[2], float scale, bool real, int ct) {
   const float f[4] = {o[0].x * scale, o[0].y * scale, o[1].x * scale, o[1].y * scale};
   bool ok = true;
 #pragma unroll
@@ -136,36 +139,44 @@ struct Times {   // moments, documents and limits of 64 rows
 __device__ __forceinline__ void stage_times(Times& t, const Geometry& g, const ScoredArgs& a, int b, int s, int pos0, int n) {
   const int i = threadIdx.x;
   if (i < TILE) {
-    const bool in = i >= 0 && i < n && pos0 + i >= 0;
+    const bool in = i < n && pos0 + i >= 0;
     t.time[i] = in ? time_of(g, a, b, s, pos0 + i) : 0.f;
     t.limit[i] = in ? latest_seen(a, b, t.time[i]) : -INFINITY;
     t.doc[i] = in ? document_of(g, a, b, s, pos0 + i) : 0;
   }
 }
 
-// Dots of the tile -> scores in base 2, -inf where closed; `bend` times the cap's derivative.  queries_are_rows tells which side is which.
+// Dots -> scores in base 2, -inf where closed; d *= the cap's derivative.  queries_are_rows tells which side is which.
 template <bool BEND>
-__device__ __forceinline__ void scores(float (&x)[4][4], float (&bend)[BEND ? 4 : 1][4], const ScoredArgs& a, float slope2, const Times& own, const Times& partner,
-                                       int partners, bool rule, bool queries_are_rows, int tx, int ty) {
+__device__ __forceinline__ void scores(float (&x)[4][4], float (&d)[4][4], const ScoredArgs& a, float slope2, const Times& own, const Times& partner,
+                                       int partners, bool queries_are_rows, int tx, int ty) {
   const float2 f = make_float2(a.inner, a.inner);
+  const bool cap = a.softcap > 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; j += 2) {
       float2 y = __fmul2_rn(make_float2(x[i][j], x[i][j + 1]), f);
-      if (BEND) bend[i][j] = bend[i][j + 1] = 1.f;
-      if (a.softcap > 0.f) {
+      if (cap) {
         const float2 t = tanh_any2(y);
         y = __fmul2_rn(t, make_float2(a.outer, a.outer));
         if (BEND) {
-          bend[i][j] = 1.f - t.x * t.x;
-          bend[i][j + 1] = 1.f - t.y * t.y;
+          d[i][j] *= 1.f - t.x * t.x;
+          d[i][j + 1] *= 1.f - t.y * t.y;
         }
       }
       x[i][j] = y.x;
       x[i][j + 1] = y.y;
     }
-  if (rule) {
+  if (a.slopes != nullptr) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float t = partner.time[tx + 16 * j];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i][j] -= slope2 * fabsf(own.time[4 * ty + i] - t);
+    }
+  }
+  if (rule_masks(a)) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int c = tx + 16 * j;
@@ -173,116 +184,128 @@ __device__ __forceinline__ void scores(float (&x)[4][4], float (&bend)[BEND ? 4 
       for (int i = 0; i < 4; ++i) {
         const int r = 4 * ty + i;
         const float limit = queries_are_rows ? own.limit[r] : partner.limit[c], key = queries_are_rows ? partner.time[c] : own.time[r];
-        x[i][j] -= slope2 * fabsf(own.time[r] - partner.time[c]);
         if (key > limit || own.doc[r] != partner.doc[c]) x[i][j] = -INFINITY;
       }
     }
   }
+  if (partners < TILE) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (tx + 16 * j >= partners)
+    for (int j = 0; j < 4; ++j)
+      if (tx + 16 * j >= partners)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i][j] = -INFINITY;
+        for (int i = 0; i < 4; ++i) x[i][j] = -INFINITY;
+  }
 }
 
-// Over the 16 threads that share rows 4 ty ..
-__device__ __forceinline__ float row_max(float v) {
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-__device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
+// CTAs an SM that registers are kept for: what a warp waits for (shared memory, exponentials) another one's products hide.
+template <int HD> constexpr int MIN_CTAS = HD <= 32 ? 2 : 1;
 
 template <int HD>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, MIN_CTAS<HD>)
 scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   using S = Sizes<HD>;
   extern __shared__ __align__(16) float smem[];
-  float *s_q = smem, *s_k = s_q + S::ROWS, *s_v = s_k + S::ROWS, *s_w = s_v + S::ROWS;
-  __shared__ Times own, partner;
-  __shared__ __align__(16) float s_row[TILE];   // what the accumulators are scaled by, per row
+  float *s_q = smem, *s_k = s_q + S::ROWS, *s_v = s_k + 2 * S::ROWS;
+  __shared__ Times own, partner[2];
   __shared__ int s_any;
   const Place at = find_place(tiles, g.batch, g.heads);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = at.head, b = at.sample, hk = h / a.group, s = at.segment;
+  float* const s_w = s_v + 2 * S::ROWS + (tid >> 5) * WARP_WEIGHTS;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   const int q0 = at.tile * TILE, q_end = min(q0 + TILE, a.q_len[s]);
   const QueryRows rows = query_rows(g, a, b, s);
-  const bool rule = rule_masks(a) || a.slopes != nullptr, work = max(q0, rows.lo) < min(q_end, rows.hi);
-  const int64_t row0 = (int64_t)b * a.Lq + a.q_off[s] + q0;
+  const bool rule = rule_masks(a) || a.slopes != nullptr;
+  const int64_t row0 = (int64_t)b * a.Lq + a.q_off[s] + q0, sample0 = (int64_t)b * g.L;
   const float slope2 = a.slopes != nullptr ? a.slopes[h] * LOG2E : 0.f;
   const Piece<HD> piece;
   float2 o[4][2] = {};
-  float ref[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, l[4] = {0.f, 0.f, 0.f, 0.f};
-  if (work) {
+  float ref[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, l[4] = {0.f, 0.f, 0.f, 0.f};   // l: this lane's part of the sums
+  Walk next = {};
+#pragma unroll
+  for (int r = 0; r < 3; ++r) next.n[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
+  if (max(q0, rows.lo) >= min(q_end, rows.hi)) next.seg = 3;
+  next.settle();
+  auto stage = [&](const Walk& w, int buf) {
+    const int64_t key0 = sample0 + g.off(w.seg) + w.pos;
+    stage_rows<HD>(s_k + buf * S::ROWS, static_cast<const float*>(a.k) + key0 * a.ldk + (int64_t)hk * g.hd, a.ldk, w.left(), g.hd);
+    stage_rows<HD>(s_v + buf * S::ROWS, static_cast<const float*>(a.v) + key0 * a.ldv + (int64_t)hk * g.hd, a.ldv, w.left(), g.hd);
+    cp_commit();
+    if (rule) stage_times(partner[buf], g, a, b, w.seg, w.pos, w.left());
+  };
+  if (!next.over()) {
     // rows that are padding are staged as zeros where they come last; in front (tail form) they are real memory, and not stored
     stage_rows<HD>(s_q, static_cast<const float*>(a.q) + row0 * a.ldq + (int64_t)h * g.hd, a.ldq, min(q_end, rows.hi) - q0, g.hd);
     if (rule) stage_times(own, g, a, b, s, q0 + rows.shift, min(q_end, rows.hi) - q0);
-    for (int r = 0; r < 3; ++r) {
-      const int n = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
-      for (int j0 = 0; j0 < n; j0 += TILE) {
-        const int64_t key0 = (int64_t)b * g.L + g.off(r) + j0;
-        __syncthreads();   // the tiles before have been read
-        stage_rows<HD>(s_k, static_cast<const float*>(a.k) + key0 * a.ldk + (int64_t)hk * g.hd, a.ldk, n - j0, g.hd);
-        stage_rows<HD>(s_v, static_cast<const float*>(a.v) + key0 * a.ldv + (int64_t)hk * g.hd, a.ldv, n - j0, g.hd);
-        if (rule) stage_times(partner, g, a, b, r, j0, n - j0);
-        __syncthreads();
-        float x[4][4], unused[1][4];
-        product_over_features<HD>(x, s_q, s_k, tx, ty);
-        scores<false>(x, unused, a, slope2, own, partner, n - j0, rule, true, tx, ty);
-        float scale[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float top = fmaxf(ref[i], row_max(fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]))));
-          const float base = top == -INFINITY ? 0.f : top;   // no open key so far: weights of zero
-          scale[i] = ptx::ex2(ref[i] - base);
-          ref[i] = top;
-          float t = 0.f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) t += x[i][j] = ptx::ex2(x[i][j] - base);
-          l[i] = l[i] * scale[i] + row_sum(t);
-        }
-        put_weights(s_w, x, tx, ty);
-        if (tx == 0) *reinterpret_cast<float4*>(s_row + 4 * ty) = make_float4(scale[0], scale[1], scale[2], scale[3]);
-        __syncthreads();
-        const float4 f = *reinterpret_cast<const float4*>(s_row + 4 * piece.rt);
-        const float fs[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          o[i][0] = __fmul2_rn(o[i][0], make_float2(fs[i], fs[i]));
-          o[i][1] = __fmul2_rn(o[i][1], make_float2(fs[i], fs[i]));
-        }
-        product_over_partners<HD>(o, s_w, s_v, piece);
-      }
-    }
-    __syncthreads();
-    join_groups<HD>(o, smem, piece);
+    stage(next, 0);
   }
-  if (tid == 0) s_any = 0;
-  if (tx == 0)
+  for (int buf = 0; !next.over(); buf ^= 1) {
+    const int rem = next.left();
+    cp_wait();
+    __syncthreads();   // the tile is there, and nobody reads the other buffer any more
+    next.pos += TILE;
+    next.settle();
+    if (!next.over()) stage(next, buf ^ 1);
+    float x[4][4], unused[4][4], top[4];
+    product_over_features<HD>(x, s_q, s_k + buf * S::ROWS, tx, ty);
+    scores<false>(x, unused, a, slope2, own, partner[buf], rem, true, tx, ty);
+    // a row's reference follows its maximum when a score exceeds it by more than 8 (weights stay below 256)
+    bool outgrown = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = q0 + 4 * ty + i;
-      const bool real = row >= rows.lo && row < min(q_end, rows.hi) && l[i] != 0.f;
-      s_row[4 * ty + i] = real ? 1.f / l[i] : 0.f;
-      if (row < q_end && a.lse != nullptr) a.lse[((int64_t)b * g.heads + h) * a.Lq + a.q_off[s] + row] = real ? (ref[i] + log2f(l[i])) * LN2 : -INFINITY;
+      top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
+      outgrown = outgrown || top[i] > ref[i] + 8.f;
     }
-  __syncthreads();
+    if (__any_sync(0xffffffffu, outgrown)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float t = top[i], f = 1.f;
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));   // over the 16 lanes that share the row
+        if (t > ref[i] + 8.f) {
+          f = ptx::ex2(ref[i] - t);
+          l[i] *= f;
+          ref[i] = t;
+        }
+        f = __shfl_sync(0xffffffffu, f, 16 * piece.rt);
+        o[i][0] = __fmul2_rn(o[i][0], make_float2(f, f));
+        o[i][1] = __fmul2_rn(o[i][1], make_float2(f, f));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float base = ref[i] == -INFINITY ? 0.f : ref[i];   // no open key so far: weights of zero
+#pragma unroll
+      for (int j = 0; j < 4; ++j) l[i] += x[i][j] = ptx::ex2(x[i][j] - base);
+    }
+    put_weights(s_w, x, tx, ty);
+    __syncwarp();
+    product_over_partners<HD>(o, s_w, s_v + buf * S::ROWS, piece);
+    __syncwarp();
+  }
+  join_groups<HD>(o);
+  if (tid == 0) s_any = 0;
+  float inv[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+    const int row = q0 + 4 * ty + i;
+    const bool real = row >= rows.lo && row < min(q_end, rows.hi) && l[i] != 0.f;
+    if (tx == 0 && row < q_end && a.lse != nullptr) a.lse[((int64_t)b * g.heads + h) * a.Lq + a.q_off[s] + row] = real ? (ref[i] + log2f(l[i])) * LN2 : -INFINITY;
+    inv[i] = __shfl_sync(0xffffffffu, real ? 1.f / l[i] : 0.f, 16 * piece.rt);
+  }
   bool ok = true;
   if (piece.group == 0)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = 4 * piece.rt + i;
-      const float inv = s_row[row];
-      if (q0 + row < q_end) ok = put_row<HD>(static_cast<float*>(a.out) + (row0 + row) * a.ldo + (int64_t)h * g.hd, g.hd, o[i], inv, inv != 0.f, piece.ct) && ok;
+      const int row = (tid >> 5) * WARP_ROWS + 4 * piece.rt + i;
+      if (q0 + row < q_end) ok = put_row(static_cast<float*>(a.out) + (row0 + row) * a.ldo + (int64_t)h * g.hd, g.hd, o[i], inv[i], inv[i] != 0.f, piece.ct) && ok;
     }
   if (!rule_masks(a)) return;
   // zero times NaN or Inf of a closed key: the tile's rows once more, pair by pair
+  __syncthreads();
   if (!ok) s_any = 1;
   __syncthreads();
   if (s_any != 0)
@@ -290,85 +313,102 @@ scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
 }
 
 template <int HD>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, MIN_CTAS<HD>)
 scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   using S = Sizes<HD>;
   extern __shared__ __align__(16) float smem[];
-  float *s_q = smem, *s_g = s_q + S::ROWS, *s_k = s_g + S::ROWS, *s_v = s_k + S::ROWS, *s_w = s_v + S::ROWS;
-  __shared__ Times own, partner;
+  float *s_q = smem, *s_g = s_q + S::ROWS, *s_k = s_g + S::ROWS, *s_v = s_k + 2 * S::ROWS;
+  __shared__ Times own, partner[2];
   __shared__ float2 s_stats[TILE];
   __shared__ int s_any;
   const Place at = find_place(tiles, g.batch, g.heads);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = at.head, b = at.sample, hk = h / a.group, s = at.segment;
+  float* const s_w = s_v + 2 * S::ROWS + (tid >> 5) * WARP_WEIGHTS;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int q0 = at.tile * TILE, q_end = min(q0 + TILE, g.len(s)), n_q = valid_rows(g, b, s);
+  const int q0 = at.tile * TILE, q_end = min(q0 + TILE, g.len(s)), n_rows = min(q_end, valid_rows(g, b, s)) - q0;   // real rows of this tile
   const bool rule = rule_masks(a) || a.slopes != nullptr;
-  const int64_t row0 = (int64_t)b * g.L + g.off(s) + q0, stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s) + q0;
+  const int64_t sample0 = (int64_t)b * g.L, row0 = sample0 + g.off(s) + q0, stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s) + q0;
   const float slope2 = a.slopes != nullptr ? a.slopes[h] * LOG2E : 0.f;
   const Piece<HD> piece;
   float2 dq[4][2] = {};
-  const int n_rows = min(q_end, n_q) - q0;   // of this tile
-  bool ok = true;
-  if (n_rows > 0) {
+  Walk next = {};
+#pragma unroll
+  for (int r = 0; r < 3; ++r) next.n[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
+  if (n_rows <= 0) next.seg = 3;
+  next.settle();
+  auto stage = [&](const Walk& w, int buf) {
+    const int64_t key0 = sample0 + g.off(w.seg) + w.pos;
+    stage_rows<HD>(s_k + buf * S::ROWS, static_cast<const float*>(a.k) + key0 * a.ldk + (int64_t)hk * g.hd, a.ldk, w.left(), g.hd);
+    stage_rows<HD>(s_v + buf * S::ROWS, static_cast<const float*>(a.v) + key0 * a.ldv + (int64_t)hk * g.hd, a.ldv, w.left(), g.hd);
+    cp_commit();
+    if (rule) stage_times(partner[buf], g, a, b, w.seg, w.pos, w.left());
+  };
+  if (!next.over()) {
     stage_rows<HD>(s_q, static_cast<const float*>(a.q) + row0 * a.ldq + (int64_t)h * g.hd, a.ldq, n_rows, g.hd);
     stage_rows<HD>(s_g, static_cast<const float*>(a.dout) + row0 * a.lddo + (int64_t)h * g.hd, a.lddo, n_rows, g.hd);
     if (rule) stage_times(own, g, a, b, s, q0, n_rows);
-    __syncthreads();
-    if (tid < TILE) {   // (lse in base 2, delta); a row without an open key takes no part
-      float2 st = make_float2(INFINITY, 0.f);
-      if (tid < n_rows) {
-        const float lse = a.lse[stat0 + tid];
-        if (lse != -INFINITY) {
-          st.x = lse * LOG2E;
-          const float* out = static_cast<const float*>(a.out) + (row0 + tid) * a.ldo + (int64_t)h * g.hd;
-          for (int f = 0; f < g.hd; ++f) st.y += out[f] * s_g[tid * S::PITCH + f];
-        }
-      }
-      s_stats[tid] = st;
-      ok = finite(st.y);
-    }
-    __syncthreads();
-    float2 st[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) st[i] = s_stats[4 * ty + i];
-    for (int r = 0; r < 3; ++r) {
-      const int n = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
-      for (int j0 = 0; j0 < n; j0 += TILE) {
-        const int64_t key0 = (int64_t)b * g.L + g.off(r) + j0;
-        __syncthreads();
-        stage_rows<HD>(s_k, static_cast<const float*>(a.k) + key0 * a.ldk + (int64_t)hk * g.hd, a.ldk, n - j0, g.hd);
-        stage_rows<HD>(s_v, static_cast<const float*>(a.v) + key0 * a.ldv + (int64_t)hk * g.hd, a.ldv, n - j0, g.hd);
-        if (rule) stage_times(partner, g, a, b, r, j0, n - j0);
-        __syncthreads();
-        float x[4][4], dp[4][4], bend[4][4];
-        product_over_features<HD>(x, s_q, s_k, tx, ty);
-        scores<true>(x, bend, a, slope2, own, partner, n - j0, rule, true, tx, ty);
-        product_over_features<HD>(dp, s_g, s_v, tx, ty);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[i][j] = ptx::ex2(x[i][j] - st[i].x) * (dp[i][j] - st[i].y) * bend[i][j];
-        put_weights(s_w, x, tx, ty);
-        __syncthreads();
-        product_over_partners<HD>(dq, s_w, s_k, piece);
-      }
-    }
-    __syncthreads();
-    join_groups<HD>(dq, smem + 2 * S::ROWS, piece);
+    stage(next, 0);
   }
+  bool ok = true;
+  {   // (lse in base 2, delta) of the warp's rows, four lanes to a row; a row without an open key takes no part
+    const int row = tid >> 2, part = tid & 3;
+    const float lse = row < n_rows ? a.lse[stat0 + row] : -INFINITY;
+    float delta = 0.f;
+    if (lse != -INFINITY) {
+      const float *out = static_cast<const float*>(a.out) + (row0 + row) * a.ldo + (int64_t)h * g.hd, *grad = static_cast<const float*>(a.dout) + (row0 + row) * a.lddo + (int64_t)h * g.hd;
+#pragma unroll 4
+      for (int f = part; f < g.hd; f += 4) delta += out[f] * grad[f];
+    }
+    __syncwarp();
+    delta += __shfl_xor_sync(0xffffffffu, delta, 1);
+    delta += __shfl_xor_sync(0xffffffffu, delta, 2);
+    ok = finite(delta);
+    if (part == 0) {
+      s_stats[row] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, delta);
+      if (q0 + row < q_end) a.row_stats[stat0 + row] = s_stats[row];
+    }
+    __syncwarp();
+  }
+  float2 st[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) st[i] = s_stats[4 * ty + i];
+  for (int buf = 0; !next.over(); buf ^= 1) {
+    const int rem = next.left();
+    cp_wait();
+    __syncthreads();   // the tile is there, and nobody reads the other buffer any more
+    next.pos += TILE;
+    next.settle();
+    if (!next.over()) stage(next, buf ^ 1);
+    float x[4][4], d[4][4];
+    product_over_features<HD>(d, s_g, s_v + buf * S::ROWS, tx, ty);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) d[i][j] -= st[i].y;
+    product_over_features<HD>(x, s_q, s_k + buf * S::ROWS, tx, ty);
+    scores<true>(x, d, a, slope2, own, partner[buf], rem, true, tx, ty);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] = ptx::ex2(x[i][j] - st[i].x) * d[i][j];
+    put_weights(s_w, x, tx, ty);
+    __syncwarp();
+    product_over_partners<HD>(dq, s_w, s_k + buf * S::ROWS, piece);
+    __syncwarp();
+  }
+  join_groups<HD>(dq);
   if (tid == 0) s_any = 0;
-  if (tid < TILE && q0 + tid < q_end) a.row_stats[stat0 + tid] = n_rows > 0 ? s_stats[tid] : make_float2(INFINITY, 0.f);
-  __syncthreads();
   if (piece.group == 0)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = 4 * piece.rt + i;
+      const int row = (tid >> 5) * WARP_ROWS + 4 * piece.rt + i;
       if (q0 + row < q_end)
-        ok = put_row<HD>(static_cast<float*>(a.dq) + (row0 + row) * a.lddq + (int64_t)h * g.hd, g.hd, dq[i], a.scale, n_rows > 0 && s_stats[row].x != INFINITY, piece.ct) && ok;
+        ok = put_row(static_cast<float*>(a.dq) + (row0 + row) * a.lddq + (int64_t)h * g.hd, g.hd, dq[i], a.scale, s_stats[row].x != INFINITY, piece.ct) && ok;
     }
   if (!rule_masks(a)) return;
+  __syncthreads();
   if (!ok) s_any = 1;
   __syncthreads();
   if (s_any != 0)
@@ -376,78 +416,103 @@ scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__
 }
 
 template <int HD>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, MIN_CTAS<HD>)
 scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   using S = Sizes<HD>;
   extern __shared__ __align__(16) float smem[];
-  float *s_k = smem, *s_v = s_k + S::ROWS, *s_q = s_v + S::ROWS, *s_g = s_q + S::ROWS, *s_p = s_g + S::ROWS, *s_w = s_p + S::WEIGHTS;
-  __shared__ Times own, partner;
-  __shared__ float2 s_stats[TILE];
+  float *s_k = smem, *s_v = s_k + S::ROWS, *s_q = s_v + S::ROWS, *s_g = s_q + 2 * S::ROWS;
+  __shared__ Times own, partner[2];
+  __shared__ float2 s_stats[2][TILE];
   __shared__ int s_any;
   const Place at = find_place(tiles, g.batch, a.kv_heads);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, hk = at.head, b = at.sample, r = at.segment;
+  float* const s_w = s_g + 2 * S::ROWS + (tid >> 5) * WARP_WEIGHTS;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int k0 = at.tile * TILE, k_end = min(k0 + TILE, g.len(r)), n_k = valid_rows(g, b, r), n_rows = min(k_end, n_k) - k0;
+  const int k0 = at.tile * TILE, k_end = min(k0 + TILE, g.len(r)), n_rows = min(k_end, valid_rows(g, b, r)) - k0;
   const bool rule = rule_masks(a) || a.slopes != nullptr;
-  const int64_t key0 = (int64_t)b * g.L + g.off(r) + k0;
+  const int64_t sample0 = (int64_t)b * g.L, key0 = sample0 + g.off(r) + k0;
   const Piece<HD> piece;
   float2 dk[4][2] = {}, dv[4][2] = {};
-  if (n_rows > 0) {
+  Walk next = {};
+#pragma unroll
+  for (int s = 0; s < 3; ++s) next.n[s] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, s) : 0;
+  if (n_rows <= 0) next.seg = 3;
+  next.settle();
+  const Walk first = next;
+  int h = hk * a.group;   // the head whose queries come next
+  const int last_head = h + a.group - 1;
+  auto stage = [&](const Walk& w, int head, int buf) {
+    const int64_t at_row = sample0 + g.off(w.seg) + w.pos;
+    stage_rows<HD>(s_q + buf * S::ROWS, static_cast<const float*>(a.q) + at_row * a.ldq + (int64_t)head * g.hd, a.ldq, w.left(), g.hd);
+    stage_rows<HD>(s_g + buf * S::ROWS, static_cast<const float*>(a.dout) + at_row * a.lddo + (int64_t)head * g.hd, a.lddo, w.left(), g.hd);
+    cp_commit();
+    if (rule) stage_times(partner[buf], g, a, b, w.seg, w.pos, w.left());
+    if (tid < TILE)   // no weight for rows past the last
+      s_stats[buf][tid] = tid < w.left() ? a.row_stats[((int64_t)b * g.heads + head) * g.L + g.off(w.seg) + w.pos + tid] : make_float2(INFINITY, 0.f);
+  };
+  if (!next.over()) {
     stage_rows<HD>(s_k, static_cast<const float*>(a.k) + key0 * a.ldk + (int64_t)hk * g.hd, a.ldk, n_rows, g.hd);
     stage_rows<HD>(s_v, static_cast<const float*>(a.v) + key0 * a.ldv + (int64_t)hk * g.hd, a.ldv, n_rows, g.hd);
     if (rule) stage_times(own, g, a, b, r, k0, n_rows);
-    for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
-      const float slope2 = a.slopes != nullptr ? a.slopes[h] * LOG2E : 0.f;
-      for (int s = 0; s < 3; ++s) {
-        const int n = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, s) : 0;
-        for (int i0 = 0; i0 < n; i0 += TILE) {
-          const int64_t row0 = (int64_t)b * g.L + g.off(s) + i0;
-          __syncthreads();
-          stage_rows<HD>(s_q, static_cast<const float*>(a.q) + row0 * a.ldq + (int64_t)h * g.hd, a.ldq, n - i0, g.hd);
-          stage_rows<HD>(s_g, static_cast<const float*>(a.dout) + row0 * a.lddo + (int64_t)h * g.hd, a.lddo, n - i0, g.hd);
-          if (rule) stage_times(partner, g, a, b, s, i0, n - i0);
-          if (tid < TILE) s_stats[tid] = tid < n - i0 ? a.row_stats[((int64_t)b * g.heads + h) * g.L + g.off(s) + i0 + tid] : make_float2(INFINITY, 0.f);
-          __syncthreads();
-          float x[4][4], dp[4][4], bend[4][4];
-          product_over_features<HD>(x, s_k, s_q, tx, ty);
-          scores<true>(x, bend, a, slope2, own, partner, n - i0, rule, false, tx, ty);
-          product_over_features<HD>(dp, s_v, s_g, tx, ty);
+    stage(next, h, 0);
+  }
+  for (int buf = 0; !next.over(); buf ^= 1) {
+    const int rem = next.left();
+    const float slope2 = a.slopes != nullptr ? a.slopes[h] * LOG2E : 0.f;
+    cp_wait();
+    __syncthreads();   // the tile is there, and nobody reads the other buffer any more
+    next.pos += TILE;
+    next.settle();
+    if (next.over() && h < last_head) {
+      next = first;
+      ++h;
+    }
+    if (!next.over()) stage(next, h, buf ^ 1);
+    float x[4][4], d[4][4];
+    product_over_features<HD>(d, s_v, s_g + buf * S::ROWS, tx, ty);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 st = s_stats[tx + 16 * j];
+    for (int j = 0; j < 4; ++j) {
+      const float delta = s_stats[buf][tx + 16 * j].y;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[i][j] = ptx::ex2(x[i][j] - st.x);
-              dp[i][j] = x[i][j] * (dp[i][j] - st.y) * bend[i][j];
-            }
-          }
-          put_weights(s_p, x, tx, ty);
-          put_weights(s_w, dp, tx, ty);
-          __syncthreads();
-          product_over_partners<HD>(dv, s_p, s_g, piece);
-          product_over_partners<HD>(dk, s_w, s_q, piece);
-        }
+      for (int i = 0; i < 4; ++i) d[i][j] -= delta;
+    }
+    product_over_features<HD>(x, s_k, s_q + buf * S::ROWS, tx, ty);
+    scores<true>(x, d, a, slope2, own, partner[buf], rem, false, tx, ty);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float lse2 = s_stats[buf][tx + 16 * j].x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i][j] = ptx::ex2(x[i][j] - lse2);
+        d[i][j] *= x[i][j];
       }
     }
-    __syncthreads();
-    join_groups<HD>(dk, smem, piece);
-    join_groups<HD>(dv, smem, piece);
+    put_weights(s_w, x, tx, ty);
+    __syncwarp();
+    product_over_partners<HD>(dv, s_w, s_g + buf * S::ROWS, piece);
+    __syncwarp();
+    put_weights(s_w, d, tx, ty);
+    __syncwarp();
+    product_over_partners<HD>(dk, s_w, s_q + buf * S::ROWS, piece);
+    __syncwarp();
   }
+  join_groups<HD>(dk);
+  join_groups<HD>(dv);
   if (tid == 0) s_any = 0;
-  __syncthreads();
   bool ok = true;
   if (piece.group == 0)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = 4 * piece.rt + i;
+      const int row = (tid >> 5) * WARP_ROWS + 4 * piece.rt + i;
       if (k0 + row < k_end) {
-        ok = put_row<HD>(static_cast<float*>(a.dk) + (key0 + row) * a.lddk + (int64_t)hk * g.hd, g.hd, dk[i], a.scale, row < n_rows, piece.ct) && ok;
-        ok = put_row<HD>(static_cast<float*>(a.dv) + (key0 + row) * a.lddv + (int64_t)hk * g.hd, g.hd, dv[i], 1.f, row < n_rows, piece.ct) && ok;
+        ok = put_row(static_cast<float*>(a.dk) + (key0 + row) * a.lddk + (int64_t)hk * g.hd, g.hd, dk[i], a.scale, row < n_rows, piece.ct) && ok;
+        ok = put_row(static_cast<float*>(a.dv) + (key0 + row) * a.lddv + (int64_t)hk * g.hd, g.hd, dv[i], 1.f, row < n_rows, piece.ct) && ok;
       }
     }
   if (!rule_masks(a)) return;
+  __syncthreads();
   if (!ok) s_any = 1;
   __syncthreads();
   if (s_any != 0)
@@ -455,13 +520,7 @@ scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
 }
 
 enum Pass { FWD, DQ, DKV };
-template <int HD> constexpr int smem_bytes(int pass) {
-  using S = Sizes<HD>;
-  return 4 * (pass == FWD ? 3 * S::ROWS + S::WEIGHTS : pass == DQ ? 4 * S::ROWS + S::WEIGHTS : 4 * S::ROWS + 2 * S::WEIGHTS);
-}
-// join_groups() puts (GROUPS - 1) * 64 * HD floats over the tiles (behind the first two for dq)
-static_assert(4 * 7 * 64 * 8 <= smem_bytes<8>(FWD) && 4 * (2 * Sizes<8>::ROWS + 7 * 64 * 8) <= smem_bytes<8>(DQ), "room to join the groups");
-static_assert(4 * 3 * 64 * 16 <= smem_bytes<16>(FWD) && 4 * (2 * Sizes<16>::ROWS + 3 * 64 * 16) <= smem_bytes<16>(DQ), "room to join the groups");
+template <int HD> constexpr int smem_bytes(int pass) { return 4 * ((pass == FWD ? 5 : 6) * Sizes<HD>::ROWS + THREADS / 32 * WARP_WEIGHTS); }
 
 template <int PASS, int HD>
 cudaError_t launch(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {

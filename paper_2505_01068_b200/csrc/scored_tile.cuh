@@ -212,20 +212,6 @@ __device__ __forceinline__ Openness openness(const Range& queries, const Range& 
   return queries.d_lo == queries.d_hi && keys.d_lo == keys.d_hi && keys.t_hi <= queries.t_lo ? ALL : SOME;
 }
 
-// Chunks of C partners through the segments that are walked, in order.
-struct Walk {
-  int n[3];          // rows to walk per segment, 0 where shut
-  int seg, pos;      // where it stands; seg 3: over
-  __device__ __forceinline__ int rows(int s) const { return s == 0 ? n[0] : s == 1 ? n[1] : n[2]; }
-  __device__ __forceinline__ void settle() {   // over segments that hold nothing more
-    if (seg == 0 && pos >= n[0]) { seg = 1; pos = 0; }
-    if (seg == 1 && pos >= n[1]) { seg = 2; pos = 0; }
-    if (seg == 2 && pos >= n[2]) { seg = 3; pos = 0; }
-  }
-  __device__ __forceinline__ bool over() const { return seg == 3; }
-  __device__ __forceinline__ int left() const { return rows(seg) - pos; }
-};
-
 // Moments and documents of a block of 64 partners as a range; `t` holds what openness() compares.
 __device__ __forceinline__ Range block_range(const float* t, const int* d, int j0, int rem, int lane) {
   Range r = NO_ROWS;

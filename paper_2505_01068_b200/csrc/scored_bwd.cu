@@ -11,11 +11,12 @@
 namespace gsit {
 namespace {
 
-// Registers: 24 warps an SM for narrow heads (32 for dq, which holds less; MOSEI step: dq 94 -> 87 us, dk and dv 96 -> 98), 16 and 12 for
-// wide ones, whose accumulators are larger.
-template <int HD, int W, int NARROW> constexpr int MIN_CTAS = (HD <= 16 ? NARROW : HD == 32 ? 16 : 12) / W;
+// Registers: CTAs of W warps an SM.  Narrow heads in large grids (W = 8): 24 warps, 32 for dq, which holds less (MOSEI step: dq 94 -> 87 us,
+// dk and dv 96 -> 98).  W = 4: 16 warps, 12 for heads of 64, whose accumulators are larger.
+template <int HD, int W, int NARROW> constexpr int MIN_CTAS = W == 8 ? NARROW / W : HD == 64 ? 3 : 4;
+constexpr int MT = 1;   // row tiles of a warp (two: dq 107 us for 104, dk and dv 119 for 109)
 
-template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
+template <int HD, int W, bool CAP, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W, 32>)
 scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
@@ -204,7 +205,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
     for (int row = w0; row < min(w0 + 16 * MT, min(q_end, n_q)); ++row) dq_row<bf16>(g, a, b, h, s, row);
 }
 
-template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK>
+template <int HD, int W, bool CAP, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W, 24>)
 scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
   constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
@@ -393,32 +394,36 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 
 // Which of the two kernels, by a type.
 struct Dq {
-  template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, MT, W, CAP, BIAS, MASK>;
+  template <int HD, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, W, CAP, BIAS, MASK>;
 };
 struct Dkv {
-  template <int HD, int MT, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dkv_kernel<HD, MT, W, CAP, BIAS, MASK>;
+  template <int HD, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dkv_kernel<HD, W, CAP, BIAS, MASK>;
 };
 
-template <typename K, int HD, int MT, int W, bool CAP, bool BIAS>
+template <typename K, int HD, int W, bool CAP, bool BIAS>
 cudaError_t launch_masked(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
-  return rule_masks(a) ? launch_overlapped(K::template kernel<HD, MT, W, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
-                       : launch_overlapped(K::template kernel<HD, MT, W, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
+  return rule_masks(a) ? launch_overlapped(K::template kernel<HD, W, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
+                       : launch_overlapped(K::template kernel<HD, W, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
 }
-template <typename K, int HD, int MT, int W>
+template <typename K, int HD, int W>
 cudaError_t launch_rule(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
   const bool cap = a.softcap > 0.f, bias = a.slopes != nullptr;
-  return cap ? (bias ? launch_masked<K, HD, MT, W, true, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, W, true, false>(g, a, t, grid, st))
-             : (bias ? launch_masked<K, HD, MT, W, false, true>(g, a, t, grid, st) : launch_masked<K, HD, MT, W, false, false>(g, a, t, grid, st));
+  return cap ? (bias ? launch_masked<K, HD, W, true, true>(g, a, t, grid, st) : launch_masked<K, HD, W, true, false>(g, a, t, grid, st))
+             : (bias ? launch_masked<K, HD, W, false, true>(g, a, t, grid, st) : launch_masked<K, HD, W, false, false>(g, a, t, grid, st));
 }
 template <typename K, int HD>
 cudaError_t launch_pass(const Geometry& g, const ScoredArgs& a, int heads, uint32_t walks, int n_sm, cudaStream_t st) {
   Tiles t = {};
   t.order = segment_order(g, walks);
-  const bool tall = HD <= 32 && make_tiles(&t, g.seg_len, 128) * heads * g.batch >= 6LL * n_sm;
+  // as in the forward pass; both kernels, 128 / 64 rows, us: 2 x (50, 500, 500), 8 heads of 8 20.7 / 18.5, 8 x 43 / 34, 32 x 108 / 115, 128 x
+  // 414 / 451; heads of 32: 128 x (50, 500, 500) 773 / 743, 64 x (39, 55, 400) 127 / 97
+  const bool tall = HD <= 16 && make_tiles(&t, g.seg_len, 128) * heads * g.batch >= 6LL * n_sm;
   const int64_t n = make_tiles(&t, g.seg_len, tall ? 128 : 64) * heads * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n);
-  return tall ? launch_rule<K, HD, 1, HD <= 32 ? 8 : 4>(g, a, t, grid, st) : launch_rule<K, HD, 1, 4>(g, a, t, grid, st);
+  if constexpr (HD <= 16)
+    if (tall) return launch_rule<K, HD, 8>(g, a, t, grid, st);
+  return launch_rule<K, HD, 4>(g, a, t, grid, st);
 }
 template <int HD>
 cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {

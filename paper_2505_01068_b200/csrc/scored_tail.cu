@@ -1,11 +1,14 @@
 // Scored attention for the newest positions of a stream: a handful of query rows against all keys (forward, float and bf16).
 //
-// The keys and values stream through once, which is all that bounds it (at 32 samples of 2176 positions, 8 heads of 64, bf16: 143 MB,
-// 22 us at the measured copy rate), so the work is cut by keys, not by queries.  All query rows that read a key head -- those of its query heads, in
-// every segment -- are held together by every warp; a lane owns 8 features of one key per step (a head of 64 takes 8 lanes, a warp 4
-// keys), so that a load instruction covers whole rows and a score needs log2(head_dim / 8) shuffles.  Each group of lanes keeps its own
-// running maximum, sum and weighted values; they are joined over the lanes by shuffles, over the warps in shared memory, and over the
-// CTAs that share a (sample, key head) through the shared memory of a cluster, in a fixed order.
+// The keys and values stream through once, which is all that bounds it, so the work is cut by keys, not by queries: the CTAs that share
+// a (sample, key head) form a cluster, and every warp walks its own part of the keys with all query rows that read them -- those of the
+// key head's query heads, in every segment.  Each warp keeps its own running reference, sum and weighted values; they are joined over
+// the warps in shared memory and over the cluster through distributed shared memory, in a fixed order.
+//   bf16   mma.sync on a ring of staged keys and values of each warp's own (scored_tail_tile_kernel): 32 samples of (128, 1024, 1024),
+//          8 heads of 64, half of them padding: 107 MB in 28 us, 3.9 TB/s, 0.60 of the measured copy rate; what is left is the launch, the
+//          first loads and the join, some 8 us, which small calls take whole
+//   float  a lane owns 8 features of a key, so that a load instruction covers whole rows and a score needs log2(head_dim / 8) shuffles;
+//          the same call without padding, 285 MB, 61 us, 4.7 TB/s
 #include <cooperative_groups.h>
 
 #include "scored_tile.cuh"
@@ -518,7 +521,8 @@ cudaError_t launch_cluster(K kernel, size_t bytes, const Geometry& g, const Scor
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, g, a, split);
 }
-// CTAs per (sample, key head): until every SM has one, as long as each still gets two turns of its warps, of `turn` keys each.
+// CTAs per (sample, key head): until every SM has one, as long as each still gets two turns of its warps, of `turn` keys each.  One
+// sample of (128, 1024, 1024), 8 heads of 64, split 1 / 4 / 8 ways: 15.5 / 9.2 / 8.5 us (float 20.9 / 10.7 / 9.4).
 int split_keys(const Geometry& g, const ScoredArgs& a, int n_sm, int turn) {
   int split = 1;
   while (split < MAX_SPLIT && (int64_t)g.batch * a.kv_heads * split < n_sm && g.L > 2 * split * WARPS * turn) split *= 2;
@@ -553,10 +557,14 @@ bool loads_of_16_bytes(const void* p, int64_t ld, int dtype) {
 
 }  // namespace
 
-// bf16: up to eight query rows to a key head, half of a fragment's.  float: up to six (one position in each of three segments, two
-// query heads); beyond, the registers of a lane that holds 8 features of each row's query and sum are used up.
+// bf16: up to eight query rows to a key head, half of a fragment's, and keys enough to pay for the cluster's join.  These kernels /
+// the tiles of whole calls, us, three rows to a key head: 1 x 480 keys, 8 heads of 8 8.9 / 6.4; 1 x 1050 9.0 / 11.7; 4 heads of 32 1 x 180
+// 7.2 / 5.0, 1 x 480 7.6 / 8.1; 8 heads of 64 1 x 60 7.0 / 5.0, 1 x 300 7.3 / 10.3, 32 x 2176 28 / 113.
+// float: up to six rows (one position in each of three segments, two query heads); beyond, the registers of a lane that holds 8 features
+// of each row's query and sum are used up.  1 x 30 keys, 4 heads of 8 9.0 / 7.6, 1 x 300, 8 heads of 8 9.8 / 12.2, 32 x 2176, 8 of 64 61 / 1010.
 bool scored_tail_supported(const Geometry& g, int dtype, const ScoredArgs& a) {
-  return a.tail && a.Lq * a.group <= (dtype == GSIT_BF16 ? TILE_ROWS : 6) && (g.hd == 8 || g.hd == 16 || g.hd == 32 || g.hd == 64) &&
+  const bool rows = dtype == GSIT_BF16 ? a.Lq * a.group <= TILE_ROWS && (int64_t)g.L * g.hd >= 6144 : a.Lq * a.group <= 6;
+  return a.tail && rows && (g.hd == 8 || g.hd == 16 || g.hd == 32 || g.hd == 64) &&
          loads_of_16_bytes(a.q, a.ldq, dtype) && loads_of_16_bytes(a.k, a.ldk, dtype) && loads_of_16_bytes(a.v, a.ldv, dtype);
 }
 

@@ -297,6 +297,13 @@ def test_newest_positions_only(g, q_len, dtype, hd, HK, rule):
     _check(g, Problem(dtype, 3, (20, 90, 45), 4, HK, hd, "all", q_len=q_len, **rule), grads=False)
 
 
+@pytest.mark.parametrize("q_len", [(1, 1, 1), (2, 0, 1)])
+@pytest.mark.parametrize("hd,H,HK", [(8, 4, 2), (16, 2, 2), (32, 4, 2), (64, 3, 3)])
+@pytest.mark.parametrize("rule", [dict(), dict(cap=30.0, causal=True, slopes=True), dict(docs=-3, causal=True, prefix=True, times="seconds")], ids=str)
+def test_newest_positions_of_streams_that_have_run_for_long(g, q_len, hd, H, HK, rule):
+    _check(g, Problem("bf16", 2, (301, 450, 270), H, HK, hd, "all", q_len=q_len, **rule), grads=False)
+
+
 @pytest.mark.parametrize("dtype,hd", [("bf16", 8), ("bf16", 64), ("f32", 32)])
 def test_newest_position_over_long_keys(g, dtype, hd):
     p = Problem(dtype, 2, (5, 5000, 3001), 4, 2, hd, "all", q_len=(1, 1, 1), cap=30.0, slopes=True, times="seconds", causal=True)

@@ -6,6 +6,8 @@
 // Backward: a thread owns the same columns in every row, so the gradients of gamma and beta are sums in its registers over all rows
 // of a persistent CTA; the CTA's groups are added up in order, one partial row per CTA goes to the workspace, and a second small
 // kernel adds those in order: no atomics, the same bits every time.
+// Measured, bf16, forward / backward: 32 x 2176 rows of 512 31 us (4.6 TB/s) / 85 us (2.5 TB/s; float accumulation of dgamma and dbeta beside
+// it); 64 x 1050 rows of 64, 8.6 MB a matrix, which fits L2, 8.4 / 13.8 us, of which launches and the reduction are some 10.
 #include "ops.cuh"
 
 namespace gsit {
@@ -13,7 +15,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MAX_PARTIALS = 1024;   // CTAs of the backward kernel at most (workspace)
-constexpr int FWD_CTAS_PER_SM = 16;
+constexpr int FWD_CTAS_PER_SM = 16;   // of the grid; 4: 36.9 us for 31.3 (32 x 2176 rows of 512), 8: 33.4
 
 template <int G>
 struct GroupSum {
@@ -272,7 +274,9 @@ cudaError_t launch_form(const Geometry& g, const NormCall& c, unsigned grid, cud
   else return launch_overlapped(layer_norm_bwd_kernel<TX, TY, VEC, G, NV>, dim3(grid), dim3(THREADS), 0, st, g, c);
 }
 
-// Threads of a row: 8, 16 or 32 with one vector each up to 128 features (more rows of narrow layers in flight than with idle lanes).
+// Threads of a row: 8, 16 or 32 with one vector each up to 128 features (more rows of narrow layers in flight than with idle lanes), a warp
+// with up to four up to 512, a CTA above.  Forward / backward, us: 64 x 1050 rows of 64 with 16 threads 8.3 / 13.8, with 32 14.1 / 21.3; 32 x 2176
+// rows of 512 with a warp 31 / 85, with a CTA 111 / 174.  Without vectors of four: 50 / 217.
 int row_threads(int d) { return d <= 32 ? 8 : d <= 64 ? 16 : d <= 512 ? 32 : THREADS; }
 
 template <int FWD, typename TX, typename TY>
@@ -319,6 +323,7 @@ int64_t row_groups(const Geometry& g) {
   return ((int64_t)g.batch * g.L + per - 1) / per;
 }
 
+// 4 CTAs an SM: 64 x 1050 rows of 64 13.8 us with 4, 17.5 with 2; 32 x 1000 rows of 1024 102 and 140; 32 x 2176 rows of 512 85 and 80.
 int bwd_ctas(const Geometry& g, int n_sm) { return (int)min((int64_t)min(4 * n_sm, MAX_PARTIALS), row_groups(g)); }
 
 }  // namespace

@@ -7,6 +7,8 @@
 // (which rows, heads and features) never changes, so its offsets and its pair's frequency stay in registers.
 // Angles: position * frequency in turns as one double product, less its nearest integer: right to 2^-20 turns even at positions near
 // 2^31, where a float product keeps no bit of the phase; then sincospi of the float remainder.
+// Measured: gradients of 128 samples of (128, 1024, 1024), a quarter of the rows padding, q and k with 8 heads of 64, bf16: 1072 MB in 229 us, 4.7 TB/s, 0.73 of
+// the measured copy rate; 64 x (50, 500, 500), 8 heads of 8: 30 MB in 12 us.
 #include <math.h>
 
 #include <algorithm>
@@ -41,6 +43,8 @@ struct RotaryArgs {
 //   ADJACENT  a 16-byte piece of whole pairs (interleaved, all of the head rotated)
 //   HEAD      a whole bf16 head of 8 features, pairs (p, p + 4)
 //   SCALAR    one pair, or one feature that is copied: part of a head rotated, odd strides or addresses
+// The wide forms wherever they can: 32 x (128, 1024, 1024), 8 heads of 64, bf16 SPLIT 56 us, ADJACENT 80, SCALAR 338; 64 x (50, 500, 500), 8 heads
+// of 8 HEAD 12 us, SCALAR 37.
 enum Form { SPLIT, ADJACENT, HEAD, SCALAR };
 
 template <typename T> __device__ __forceinline__ void unpack_piece(const uint4& v, float (&f)[16 / sizeof(T)]) {

@@ -1,4 +1,12 @@
-// Scored attention, forward, bf16: flash-style tiles on mma.sync (see scored_tile.cuh), scores in registers, running reference and sum.
+// Scored attention, forward, bf16, on mma.sync (see scored_tile.cuh).
+//
+// One pass over the keys: scores x = outer tanh(inner q.k) - slope |time difference| in base 2 stay in registers, weights 2^(x - ref) go into the
+// second product as they lie there, and a running reference and sum make the softmax.  Weights are rounded to bf16 for that product
+// (their sum is not): the result's error against 64 bits is 2^-8.6 of its norm, where its own rounding to bf16 is 2^-9.2.
+// What bounds it: a pair of scores costs 4 packed multiply-adds (2 clocks each), 2 exponentials (16 a clock and SM), a conversion and what
+// mask and bias add, and products of 8 or 16 features none of the time; for MOSEI's step (64 samples of (50, 500, 500), half of the rows
+// padding, 8 heads of 8, cap and bias: 82 million pairs) that is 18 us of exponentials, measured 76 us.  The rest is a warp's prologue
+// (some 400 instructions for 16 rows that walk 250 keys on average), staging, and the latency of a step's chain.
 #include "scored_tile.cuh"
 
 namespace gsit {

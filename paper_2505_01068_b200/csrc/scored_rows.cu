@@ -1,5 +1,6 @@
 // Attention with a rule on its scores, row by row: a warp takes one query row (forward, dq) or one key row (dk, dv).  For float heads
-// wider than the tiles of scored_f32.cu.
+// wider than the tiles of scored_f32.cu, which no configuration of the models has: kept simple.  A pair costs a shuffle tree and a trip
+// to L2 that nothing overlaps; 8 samples of (30, 480, 230), 4 heads of 96, inter pattern: 754 us forward, 1.95 ms gradients.
 #include "scored.cuh"
 
 namespace gsit {

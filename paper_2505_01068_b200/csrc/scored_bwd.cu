@@ -13,15 +13,13 @@
 namespace gsit {
 namespace {
 
-// Registers: CTAs of W warps an SM.  Narrow heads in large grids (W = 8): 24 warps, 32 for dq, which holds less (MOSEI step: dq 94 -> 87 us,
-// dk and dv 96 -> 98).  W = 4: 16 warps, 12 for heads of 64, whose accumulators are larger.
-template <int HD, int W, int NARROW> constexpr int MIN_CTAS = W == 8 ? NARROW / W : HD == 64 ? 3 : 4;
-constexpr int MT = 1;   // row tiles of a warp (two: dq 107 us for 104, dk and dv 119 for 109)
+constexpr int W = 4;                      // warps of a CTA
+constexpr int MT = 1, OWN = 16 * MT * W;  // row tiles of a warp (two: dq 107 us for 104, dk and dv 119 for 109), rows of a CTA
 
-template <int HD, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W, 32>)
+template <int HD, int CTAS, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(32 * W, CTAS)
 scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, NT = HD <= 16 ? 4 : 2;
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
@@ -31,9 +29,8 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   const int b = at.sample, s = at.segment, h = at.head, hk = h / a.group;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
 
-  const int q0 = at.tile * TQ, n_q = valid_rows(g, b, s), q_end = min(q0 + TQ, g.len(s));
+  const int q0 = at.tile * OWN, n_q = valid_rows(g, b, s), q_end = min(q0 + OWN, g.len(s));
   Walk next = {};
 #pragma unroll
   for (int r = 0; r < 3; ++r) next.n[r] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, r) : 0;
@@ -185,6 +182,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
     }
   }
 
+  ptx::grid_dep_launch();   // see scored_tile.cuh
   bool broken = false;
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -207,10 +205,10 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
     for (int row = w0; row < min(w0 + 16 * MT, min(q_end, n_q)); ++row) dq_row<bf16>(g, a, b, h, s, row);
 }
 
-template <int HD, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W, MIN_CTAS<HD, W, 24>)
+template <int HD, int CTAS, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(32 * W, CTAS)
 scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, TK = 16 * MT * W, NT = HD <= 16 ? 4 : 2;
+  constexpr int QC = CHUNK_ROWS<HD>, CH = HD / 8, NT = HD <= 16 ? 4 : 2;
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_q[2][QC * HD * 2], s_g[2][QC * HD * 2];
   __shared__ __align__(16) float2 s_stats[2][QC];
@@ -221,9 +219,8 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   const int b = at.sample, r = at.segment, hk = at.head;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
 
-  const int k0 = at.tile * TK, n_k = valid_rows(g, b, r), k_end = min(k0 + TK, g.len(r));
+  const int k0 = at.tile * OWN, n_k = valid_rows(g, b, r), k_end = min(k0 + OWN, g.len(r));
   Walk next = {};
 #pragma unroll
   for (int s = 0; s < 3; ++s) next.n[s] = ((g.allowed >> (3 * s + r)) & 1u) ? valid_rows(g, b, s) : 0;
@@ -372,6 +369,7 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     }
   }
 
+  ptx::grid_dep_launch();   // see scored_tile.cuh
   bool broken = false;
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -396,36 +394,37 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 
 // Which of the two kernels, by a type.
 struct Dq {
-  template <int HD, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, W, CAP, BIAS, MASK>;
+  static constexpr int MANY = 8;
+  template <int HD, int CTAS, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, CTAS, CAP, BIAS, MASK>;
 };
 struct Dkv {
-  template <int HD, int W, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dkv_kernel<HD, W, CAP, BIAS, MASK>;
+  static constexpr int MANY = 6;
+  template <int HD, int CTAS, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dkv_kernel<HD, CTAS, CAP, BIAS, MASK>;
 };
 
-template <typename K, int HD, int W, bool CAP, bool BIAS>
+template <typename K, int HD, int CTAS, bool CAP, bool BIAS>
 cudaError_t launch_masked(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
-  return rule_masks(a) ? launch_overlapped(K::template kernel<HD, W, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
-                       : launch_overlapped(K::template kernel<HD, W, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
+  return rule_masks(a) ? launch_overlapped(K::template kernel<HD, CTAS, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
+                       : launch_overlapped(K::template kernel<HD, CTAS, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
 }
-template <typename K, int HD, int W>
+template <typename K, int HD, int CTAS>
 cudaError_t launch_rule(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
   const bool cap = a.softcap > 0.f, bias = a.slopes != nullptr;
-  return cap ? (bias ? launch_masked<K, HD, W, true, true>(g, a, t, grid, st) : launch_masked<K, HD, W, true, false>(g, a, t, grid, st))
-             : (bias ? launch_masked<K, HD, W, false, true>(g, a, t, grid, st) : launch_masked<K, HD, W, false, false>(g, a, t, grid, st));
+  return cap ? (bias ? launch_masked<K, HD, CTAS, true, true>(g, a, t, grid, st) : launch_masked<K, HD, CTAS, true, false>(g, a, t, grid, st))
+             : (bias ? launch_masked<K, HD, CTAS, false, true>(g, a, t, grid, st) : launch_masked<K, HD, CTAS, false, false>(g, a, t, grid, st));
 }
 template <typename K, int HD>
 cudaError_t launch_pass(const Geometry& g, const ScoredArgs& a, int heads, uint32_t walks, int n_sm, cudaStream_t st) {
   Tiles t = {};
   t.order = segment_order(g, walks);
-  // as in the forward pass; both kernels, 128 / 64 rows, us: 2 x (50, 500, 500), 8 heads of 8 20.7 / 18.5, 8 x 43 / 34, 32 x 108 / 115, 128 x
-  // 414 / 451; heads of 32: 128 x (50, 500, 500) 773 / 743, 64 x (39, 55, 400) 127 / 97
-  const bool tall = HD <= 16 && make_tiles(&t, g.seg_len, 128) * heads * g.batch >= 6LL * n_sm;
-  const int64_t n = make_tiles(&t, g.seg_len, tall ? 128 : 64) * heads * g.batch;
+  const int64_t n = make_tiles(&t, g.seg_len, OWN) * heads * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n);
+  // as in the forward pass (dk and dv hold more: 6 for 8); both kernels, more / fewer CTAs an SM, us, 8 heads of 16: 2 x (50, 500, 500) 20.6 / 18.0, 8 x
+  // 43 / 38, 64 x (20, 20, 20) 14.1 / 16.3, 64 x (39, 55, 400) 63 / 70, 512 x (50, 50, 50) 134 / 165
   if constexpr (HD <= 16)
-    if (tall) return launch_rule<K, HD, 8>(g, a, t, grid, st);
-  return launch_rule<K, HD, 4>(g, a, t, grid, st);
+    if (n > 8LL * n_sm) return launch_rule<K, HD, K::MANY>(g, a, t, grid, st);
+  return launch_rule<K, HD, HD == 64 ? 3 : 4>(g, a, t, grid, st);
 }
 template <int HD>
 cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {

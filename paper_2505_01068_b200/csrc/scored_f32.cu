@@ -217,7 +217,6 @@ scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
   float* const s_w = s_v + 2 * S::ROWS + (tid >> 5) * WARP_WEIGHTS;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
   const int q0 = at.tile * TILE, q_end = min(q0 + TILE, a.q_len[s]);
   const QueryRows rows = query_rows(g, a, b, s);
   const bool rule = rule_masks(a) || a.slopes != nullptr;
@@ -288,6 +287,7 @@ scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
     product_over_partners<HD>(o, s_w, s_v + buf * S::ROWS, piece);
     __syncwarp();
   }
+  ptx::grid_dep_launch();   // only now: see scored_tile.cuh
   join_groups<HD>(o);
   if (tid == 0) s_any = 0;
   float inv[4];
@@ -330,7 +330,6 @@ scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__
   float* const s_w = s_v + 2 * S::ROWS + (tid >> 5) * WARP_WEIGHTS;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
   const int q0 = at.tile * TILE, q_end = min(q0 + TILE, g.len(s)), n_rows = min(q_end, valid_rows(g, b, s)) - q0;   // real rows of this tile
   const bool rule = rule_masks(a) || a.slopes != nullptr;
   const int64_t sample0 = (int64_t)b * g.L, row0 = sample0 + g.off(s) + q0, stat0 = ((int64_t)b * g.heads + h) * g.L + g.off(s) + q0;
@@ -402,6 +401,7 @@ scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__
     product_over_partners<HD>(dq, s_w, s_k + buf * S::ROWS, piece);
     __syncwarp();
   }
+  ptx::grid_dep_launch();   // only now: see scored_tile.cuh
   join_groups<HD>(dq);
   if (tid == 0) s_any = 0;
   if (piece.group == 0)
@@ -433,7 +433,6 @@ scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
   float* const s_w = s_g + 2 * S::ROWS + (tid >> 5) * WARP_WEIGHTS;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
   const int k0 = at.tile * TILE, k_end = min(k0 + TILE, g.len(r)), n_rows = min(k_end, valid_rows(g, b, r)) - k0;
   const bool rule = rule_masks(a) || a.slopes != nullptr;
   const int64_t sample0 = (int64_t)b * g.L, key0 = sample0 + g.off(r) + k0;
@@ -502,6 +501,7 @@ scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
     product_over_partners<HD>(dk, s_w, s_q + buf * S::ROWS, piece);
     __syncwarp();
   }
+  ptx::grid_dep_launch();   // only now: see scored_tile.cuh
   join_groups<HD>(dk);
   join_groups<HD>(dv);
   if (tid == 0) s_any = 0;

@@ -12,16 +12,17 @@
 namespace gsit {
 namespace {
 
-// Registers: warps an SM.  Where a grid is large (W = 8, narrow heads only), as many as hide the latency of a step's chain of products,
-// exponentials and products: 32, MOSEI step 76 us for 96 with 24 and steps of 64 keys.  A grid of about one wave (W = 4) has its
-// long walks spread better over the SMs where fewer CTAs fit one: 16, see launch_width().
-constexpr int MIN_CTAS = 4;
+constexpr int W = 4;   // warps of a CTA
 
-template <int HD, int W, bool CAP, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(32 * W, MIN_CTAS)
+// Row tiles of a warp (two share the fragments of K and V, but cost the warps that hide latency: MOSEI's step 103 us for 96) and rows of a CTA
+// (128: 512 x (50, 50, 50), 8 heads of 8 72 us for 50, 128 x (50, 500, 500) 165 for 162)
+constexpr int MT = 1, TQ = 16 * MT * W;
+
+// CTAS: CTAs of an SM that registers are kept for
+template <int HD, int CTAS, bool CAP, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(32 * W, CTAS)
 scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  // MT: row tiles of a warp.  Two share the fragments of K and V, but cost the warps that hide latency: MOSEI step 103 us for 96.
-  constexpr int MT = 1, KC = CHUNK_ROWS<HD>, CH = HD / 8, TQ = 16 * MT * W, NT = 4, NS = HD == 8 ? 4 : 2;   // tiles of 8 keys in a step, and where some pairs are shut
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, NT = 4, NS = HD == 8 ? 4 : 2;   // tiles of 8 keys in a step, and where some pairs are shut
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
@@ -31,7 +32,6 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
   const int b = at.sample, s = at.segment, h = at.head, hk = h / a.group;
   ptx::load_params_early(g, a);
   ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
 
   const int q0 = at.tile * TQ, q_end = min(q0 + TQ, a.q_len[s]);
   const QueryRows rows = query_rows(g, a, b, s);
@@ -214,6 +214,7 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     }
   }
 
+  ptx::grid_dep_launch();   // see scored_tile.cuh
   // ---- results ----
   bool broken = false;
 #pragma unroll
@@ -244,16 +245,16 @@ scored_fwd_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
     for (int row = max(w0, rows.lo); row < min(w0 + 16 * MT, min(q_end, rows.hi)); ++row) attend_row<bf16>(g, a, b, h, s, row);
 }
 
-template <int HD, int W, bool CAP, bool BIAS>
+template <int HD, int CTAS, bool CAP, bool BIAS>
 cudaError_t launch_masked(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
-  return rule_masks(a) ? launch_overlapped(scored_fwd_kernel<HD, W, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
-                       : launch_overlapped(scored_fwd_kernel<HD, W, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
+  return rule_masks(a) ? launch_overlapped(scored_fwd_kernel<HD, CTAS, CAP, BIAS, true>, grid, dim3(32 * W), 0, st, g, a, t)
+                       : launch_overlapped(scored_fwd_kernel<HD, CTAS, CAP, BIAS, false>, grid, dim3(32 * W), 0, st, g, a, t);
 }
-template <int HD, int W>
+template <int HD, int CTAS>
 cudaError_t launch_rule(const Geometry& g, const ScoredArgs& a, const Tiles& t, dim3 grid, cudaStream_t st) {
   const bool cap = a.softcap > 0.f, bias = a.slopes != nullptr;
-  return cap ? (bias ? launch_masked<HD, W, true, true>(g, a, t, grid, st) : launch_masked<HD, W, true, false>(g, a, t, grid, st))
-             : (bias ? launch_masked<HD, W, false, true>(g, a, t, grid, st) : launch_masked<HD, W, false, false>(g, a, t, grid, st));
+  return cap ? (bias ? launch_masked<HD, CTAS, true, true>(g, a, t, grid, st) : launch_masked<HD, CTAS, true, false>(g, a, t, grid, st))
+             : (bias ? launch_masked<HD, CTAS, false, true>(g, a, t, grid, st) : launch_masked<HD, CTAS, false, false>(g, a, t, grid, st));
 }
 template <int HD>
 cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
@@ -262,14 +263,14 @@ cudaError_t launch_width(const Geometry& g, const ScoredArgs& a, cudaStream_t st
   if (e != cudaSuccess) return e;
   Tiles t = {};
   t.order = segment_order(g, g.allowed);
-  // Narrow heads: CTAs of 128 rows where that makes six per SM, of 64 below.  128 / 64 rows, us, 8 heads of 8: 2 x (50, 500, 500) 8.6 / 8.5,
-  // 8 x 18.6 / 14.5, 32 x 42.6 / 46.3, 128 x 160 / 174.  Wider ones: 64.  Heads of 32: 128 x (50, 500, 500) 274 / 268, 64 x (39, 55, 400) 46 / 36.
-  const bool tall = HD <= 16 && make_tiles(&t, a.q_len, 128) * g.heads * g.batch >= 6LL * n_sm;
-  const int64_t n = make_tiles(&t, a.q_len, tall ? 128 : 64) * g.heads * g.batch;
+  const int64_t n = make_tiles(&t, a.q_len, TQ) * g.heads * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n);
+  // Narrow heads: in a grid of more than a wave twice the warps with half the registers, which hide a step's latency; in a smaller one, where there
+  // are no more warps, all registers.  8 / 4 CTAs an SM, us, 8 heads of 16: 2 x (50, 500, 500) 9.3 / 8.6, 8 x 17.6 / 15.8, 64 x (20, 20, 20) 6.9 /
+  // 8.0, 64 x (39, 55, 400) 25.9 / 27.8, 512 x (50, 50, 50) 59 / 65.
   if constexpr (HD <= 16)
-    if (tall) return launch_rule<HD, 8>(g, a, t, grid, st);
+    if (n > 8LL * n_sm) return launch_rule<HD, 8>(g, a, t, grid, st);
   return launch_rule<HD, 4>(g, a, t, grid, st);
 }
 

@@ -109,7 +109,6 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(bars + SLOT_TMEM) : "memory");
   load_params_early(g, a, tiles);
   grid_dep_wait();
-  grid_dep_launch();
 
   // ---- the CTA's rows: [o0, o_end) of segment s of sample b, of which [lo, hi) are real; position = row + shift ----
   const Place at = find_place(tiles, g.batch, KIND == DKV ? a.kv_heads : g.heads);
@@ -535,6 +534,7 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
       if (lane == 0) mbar_arrive(bars + BAR_EMPTY + 8 * st);
     }
 
+    grid_dep_launch();   // see scored_tile.cuh
     // ---- results: each thread its own rows of 128 bytes; padded rows +0 ----
     const bool walked = t > 0;
     if (walked) {

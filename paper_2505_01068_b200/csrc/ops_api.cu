@@ -100,12 +100,12 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
 // Which kernels serve a call, and the scratch they need (forward: none, running sums and joins stay on the SMs).
 cudaError_t launch_scored_fwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
   if (scored_tail_supported(g, dtype, a)) return launch_scored_tail(g, dtype, a, st);
-  if (dtype == GSIT_BF16) return scored_tc_preferred(g) ? launch_scored_fwd_tc(g, a, st) : launch_scored_fwd_bf16(g, a, st);
+  if (dtype == GSIT_BF16) return scored_tc_preferred(g, a.q_len) ? launch_scored_fwd_tc(g, a, st) : launch_scored_fwd_bf16(g, a, st);
   return g.hd <= 64 ? launch_scored_fwd_f32(g, a, st) : launch_scored_rows_fwd(g, a, st);
 }
 size_t scored_bwd_scratch(const Geometry& g, int, const ScoredArgs&) { return sizeof(float2) * (size_t)g.batch * g.heads * g.L; }
 cudaError_t launch_scored_bwd(const Geometry& g, int dtype, const ScoredArgs& a, cudaStream_t st) {
-  if (dtype == GSIT_BF16) return scored_tc_preferred(g) ? launch_scored_bwd_tc(g, a, st) : launch_scored_bwd_bf16(g, a, st);
+  if (dtype == GSIT_BF16) return scored_tc_preferred(g, g.seg_len) ? launch_scored_bwd_tc(g, a, st) : launch_scored_bwd_bf16(g, a, st);
   return g.hd <= 64 ? launch_scored_bwd_f32(g, a, st) : launch_scored_rows_bwd(g, a, st);
 }
 

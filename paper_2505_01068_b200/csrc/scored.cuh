@@ -294,7 +294,7 @@ cudaError_t launch_scored_rows_fwd(const Geometry& g, const ScoredArgs& a, cudaS
 cudaError_t launch_scored_rows_bwd(const Geometry& g, const ScoredArgs& a, cudaStream_t st);
 cudaError_t launch_scored_fwd_f32(const Geometry& g, const ScoredArgs& a, cudaStream_t st);               // scored_f32.cu, head_dim <= 64
 cudaError_t launch_scored_bwd_f32(const Geometry& g, const ScoredArgs& a, cudaStream_t st);
-bool scored_tc_preferred(const Geometry& g);                                                             // scored_tc.cu, head_dim 64
+bool scored_tc_preferred(const Geometry& g, const int (&rows)[3]);                                        // scored_tc.cu, head_dim 64
 cudaError_t launch_scored_fwd_tc(const Geometry& g, const ScoredArgs& a, cudaStream_t st);
 cudaError_t launch_scored_bwd_tc(const Geometry& g, const ScoredArgs& a, cudaStream_t st);
 bool scored_tail_supported(const Geometry& g, int dtype, const ScoredArgs& a);                            // scored_tail.cu

@@ -634,18 +634,25 @@ cudaError_t launch(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-// Which calls these kernels serve: those with a row that walks more than one tile.  Forward / gradients, us, these and mma.sync tiles, 30 as
-// cap: 32 x (50, 50, 50), 4 heads 9.9 / 22.5 and 6.3 / 15.5; 2 x (8, 12, 10) 5.3 / 11.3 and 4.7 / 6.8; 8 x (39, 55, 400), 2 heads 10.1 / 24.5
-// and 10.3 / 29.1; 1 x (50, 500, 500), 8 heads 10.9 / 27.2 and 12.3 / 35.2; 4 x (128, 1024, 1024) 38 / 98 and 54 / 189.
-bool scored_tc_preferred(const Geometry& g) {
-  int longest = 0;
+// Whether these kernels serve a call, or the mma.sync tiles.  A tile of 128 x 64 pairs takes about as long here as 64 x 51 there, a CTA's own time
+// 3.5 tiles (tensor memory, barriers, the first and last trips) and 1.5; and here a walk goes in whole tiles.  Fitted to, forward /
+// gradients, us, here and there, 8 heads:  16 x (50, 500, 500) 40 / 106 and 55 / 171;  4 x (128, 1024, 1024) 27 / 71 and 50 / 165;  64 x (100, 100,
+// 100) 39 / 101 and 37 / 120;  64 x (39, 55, 400) 74 / 177 and 51 / 168;  4 heads, 512 x (50, 50, 50) 107 / 252 and 57 / 182;  8 heads, 4 key
+// heads, all pairs, 64 x (17, 15, 173) 77 / 189 and 53 / 149, 4 x (27, 13, 898) 43 / 115 and 45 / 144.
+bool scored_tc_preferred(const Geometry& g, const int (&rows)[3]) {
+  if (g.hd != HD) return false;
+  int64_t here = 0, there = 0;   // in quarters of a tile's time, 64 of them to a key
   for (int s = 0; s < 3; ++s) {
-    int walk = 0;
+    int64_t tiles = 0, keys = 0;
     for (int r = 0; r < 3; ++r)
-      if ((g.allowed >> (3 * s + r)) & 1u) walk += g.seg_len[r];
-    longest = walk > longest ? walk : longest;
+      if ((g.allowed >> (3 * s + r)) & 1u) {
+        tiles += (g.seg_len[r] + PARTNER - 1) / PARTNER;
+        keys += g.seg_len[r];
+      }
+    here += (int64_t)((rows[s] + OWN - 1) / OWN) * 64 * (4 * tiles + 14);
+    there += (int64_t)((rows[s] + 63) / 64) * (5 * keys + 64 * 6);
   }
-  return g.hd == HD && longest > PARTNER;
+  return here <= there;
 }
 
 cudaError_t launch_scored_fwd_tc(const Geometry& g, const ScoredArgs& a, cudaStream_t st) { return launch<FWD>(g, a, st); }

@@ -84,9 +84,11 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
     static const double P[3] = {0.999999604, -0.333219082, 0.128416126}, B[3] = {0.999997213, -0.999202503, 0.632425479};
     const double in = (double)a->inner, out = (double)a->outer;
     a->near_dot = (float)(0.25 / in);
+    double even = 1.0;   // in^(2 i)
     for (int i = 0; i < 3; ++i) {
-      a->near_p[i] = (float)(P[i] * out * pow(in, 2 * i + 1));
-      a->near_b[i] = (float)(B[i] * pow(in, 2 * i));
+      a->near_p[i] = (float)(P[i] * out * even * in);
+      a->near_b[i] = (float)(B[i] * even);
+      even *= in * in;
     }
   }
   a->causal = r->causal != 0;

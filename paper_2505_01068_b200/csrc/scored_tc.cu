@@ -19,7 +19,8 @@
 // Measured: 32 samples of (128, 1024, 1024), a quarter of the rows padding, 8 heads of 64, cap (272 million pairs): 194 (FWD), 218 (DQ) and 268 us
 // (DKV), together 355 TFLOP/s.  The products alone are 143 us at the measured cuBLAS rate, the exponentials 117 us of the special
 // function units, which are 42%, 33% and 27% busy; two computing warps a scheduler cannot hide the trips through tensor memory and barriers
-// of every tile, and tensor memory holds no third CTA.  Two threads a row, so four warps a scheduler: 793 us for 706.
+// of every tile.  Two threads a row, so four warps a scheduler: 793 us for 706.  Three CTAs an SM in the forward kind, with 128 columns of
+// tensor memory and x only once, so that a CTA's products and scores take turns: 193 us for 189, and 23 for 17 where a grid is small.
 // Warps: 0 fetches (own tiles once, a ring of three partner stages with what the scores need beside them, and which tiles are open at
 // all), 1 issues every product, 2 .. 5 compute.  All waits are bounded.
 #include <cuda.h>

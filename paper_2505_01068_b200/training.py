@@ -7,6 +7,7 @@ type of their weights, as the rest of a training program's are."""
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -20,6 +21,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, gamma, mean, rstd, valid_len = ctx.saved_tensors
         got = B.layer_norm_bwd(dy.contiguous(), x, mean, rstd, gamma, ctx.seg_len, valid_len, want_params=gamma is not None)
@@ -35,10 +37,12 @@ class _Rotary(torch.autograd.Function):
         return B.rotary_fwd(q, k, positions, sections, seg_len, valid_len, base, interleaved)
 
     @staticmethod
-    def backward(ctx, dq, dk):
+    @once_differentiable
+    def backward(ctx, dq, dk=None):
         positions, valid_len = ctx.saved_tensors
         sections, seg_len, base, interleaved = ctx.args
-        dq, dk = B.rotary_bwd(dq.contiguous(), dk.contiguous(), positions, sections, seg_len, valid_len, base, interleaved)
+        got = B.rotary_bwd(dq.contiguous(), None if dk is None else dk.contiguous(), positions, sections, seg_len, valid_len, base, interleaved)
+        dq, dk = (got, None) if dk is None else got
         return dq, dk, None, None, None, None, None, None
 
 
@@ -51,6 +55,7 @@ class _ScoredAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse, valid_len = ctx.saved_tensors
         seg_len, rule = ctx.args
@@ -59,18 +64,23 @@ class _ScoredAttention(torch.autograd.Function):
 
 def layer_norm(x, gamma, beta, seg_len=None, valid_len=None, eps=1e-5, out_dtype=None):
     """Differentiable layer_norm_fwd (gamma and beta: both tensors, or both None)."""
-    assert (gamma is None) == (beta is None), "gamma and beta: both or none"
+    if (gamma is None) != (beta is None):
+        raise ValueError("gamma and beta: both or none")
     return _LayerNorm.apply(x, gamma, beta, seg_len, valid_len, eps, out_dtype)
 
 
 def rotary(q, k, positions, sections, seg_len, valid_len=None, base=10000.0, interleaved=False):
-    """Differentiable rotary_fwd."""
+    """Differentiable rotary_fwd (k None: q' alone)."""
     return _Rotary.apply(q, k, positions, sections, seg_len, valid_len, base, interleaved)
 
 
 def im_scored_attention(q, k, v, seg_len, valid_len=None, **rule):
     """Differentiable im_scored_attention_fwd; rule: phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix (slopes,
-    times and softcap are constants: they get no gradient)."""
+    times and prefix are constants: tensors that ask for a gradient are refused, and so is q_len, which has no backward pass)."""
+    wants = [n for n, t in rule.items() if isinstance(t, torch.Tensor) and t.requires_grad]
+    if wants or rule.get("q_len") is not None:
+        raise ValueError(f"no gradient for {', '.join(wants)}" if wants else "q_len: the newest positions alone have no backward pass")
+    rule.pop("q_len", None)
     return _ScoredAttention.apply(q, k, v, seg_len, valid_len, rule)
 
 

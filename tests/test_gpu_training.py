@@ -90,3 +90,25 @@ def test_the_example_learns_and_streams(g, dtype):
     assert last < 0.5 * first
     assert off <= (1e-1 if dtype == "bf16" else 1e-4)
     assert g.last_device_status() == (0, 0)
+
+
+def test_what_has_no_gradient_is_refused_and_what_has_one_gets_it(g):
+    from paper_2505_01068_b200 import training as t
+    q, k, v = (torch.randn((2, 30, 4, 8), device="cuda", requires_grad=True) for _ in range(3))
+    slopes = torch.rand(4, device="cuda", requires_grad=True)
+    for rule in (dict(slopes=slopes), dict(q_len=(1, 1, 1))):
+        with pytest.raises(ValueError):
+            t.im_scored_attention(q, k, v, (8, 12, 10), **rule)
+    with pytest.raises(ValueError):
+        t.layer_norm(q.flatten(2), torch.ones(32, device="cuda"), None)
+    out = t.im_scored_attention(q, k, v, (8, 12, 10), slopes=slopes.detach(), q_len=None)
+    grads = torch.autograd.grad(out.square().sum(), (q, k, v), create_graph=True)
+    with pytest.raises(RuntimeError):   # once differentiable
+        grads[0].sum().backward()
+    pos = torch.arange(30, device="cuda", dtype=torch.int32)[None]
+    w = torch.randn_like(q)
+    alone, = torch.autograd.grad((t.rotary(q, None, pos, (4,), (8, 12, 10)) * w).sum(), q)
+    both = torch.autograd.grad(sum((x * w).sum() for x in t.rotary(q, k, pos, (4,), (8, 12, 10))), (q, k))
+    assert torch.equal(alone, both[0]) and torch.equal(both[0], both[1])
+    plain, = torch.autograd.grad(t.layer_norm(q.flatten(2), None, None).square().sum() + (q * w).sum(), q)
+    assert bool(torch.isfinite(plain).all())

@@ -73,7 +73,7 @@ gsit_status gsit_layer_norm_bwd(const gsit_shape* shape, int32_t y_dtype, const 
  * A pair that is closed contributes nothing, whatever the rows hold: NaN or Inf in a row reaches those rows only that a path of open
  * pairs connects to it. */
 typedef struct gsit_score_rule {
-  float softcap;              /* <= 0: none */
+  float softcap;              /* <= 0: none; finite, and so is scale / softcap */
   int32_t causal;
   int32_t kv_heads;           /* heads of k and v, a divisor of heads; 0 = heads */
   const float* slopes;        /* DEVICE float [heads] or NULL */

@@ -78,12 +78,13 @@ gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geome
   a->softcap = r->softcap > 0.f ? r->softcap : 0.f;
   a->inner = a->softcap > 0.f ? a->scale / a->softcap : a->scale * LOG2E;
   a->outer = a->softcap * LOG2E;
+  if (!isfinite(a->inner) || !isfinite(a->outer)) return GSIT_ERR_INVALID_ARG;
   if (a->softcap > 0.f) {
     // tanh(y) / y and 1 - tanh(y)^2 as quadratics of y^2: least squares fits of the relative error over |y| <= 1/4, refined towards equal
     // error (4.2e-7 and 2.8e-6)
     static const double P[3] = {0.999999604, -0.333219082, 0.128416126}, B[3] = {0.999997213, -0.999202503, 0.632425479};
     const double in = (double)a->inner, out = (double)a->outer;
-    a->near_dot = (float)(0.25 / in);
+    a->near_dot = in < 1e6 ? (float)(0.25 / in) : -1.f;   // beyond, the coefficients leave the range of float: never
     double even = 1.0;   // in^(2 i)
     for (int i = 0; i < 3; ++i) {
       a->near_p[i] = (float)(P[i] * out * even * in);

@@ -110,3 +110,13 @@ def test_views_of_fused_buffers(g):
     wide = torch.full((2, L, 3, 2, 64), 5.0, device="cuda").bfloat16()
     q.backward(g, o2, l2, grads=tuple(wide[:, :, i] for i in range(3)))
     assert all(torch.equal(wide[:, :, i], grads[i]) for i in range(3))
+
+
+@pytest.mark.parametrize("dtype,hd,seg", [("bf16", 8, SHORT), ("bf16", 32, SHORT), ("bf16", 64, SHORT), ("bf16", 64, LONG), ("f32", 16, SHORT)])
+def test_caps_of_almost_nothing(g, dtype, hd, seg):
+    """A cap far below the scores leaves equal weights, for rows whose scores are zero as well."""
+    p = Problem(dtype, 2, seg, 2, 2, hd, "all", cap=1e-12)
+    p.q[:, ::2] = 0
+    out, lse = _check(g, p, grads=False)
+    assert bool(torch.isfinite(out.float()).all())
+    assert all(bool(torch.isfinite(x.float()).all()) for x in p.backward(g, out, lse))

@@ -94,6 +94,8 @@ def test_scored_attention_refuses(g):
                dict(r=rule(tail=1, q_len=(0, 0, 0))), dict(r=rule(tail=1, q_len=(-1, 1, 1))), dict(shape=_shape(g, phase=7)),
                dict(shape=_shape(g, phase=g.PHASE_CUSTOM, mask=0x200)), dict(lse=ctypes.c_void_p(P + 2))):
         assert fwd(**kw) == 1, kw
+    for cap in (float("inf"), 1e-45):   # a cap without an end, and one that no score can be divided by
+        assert fwd(r=rule(softcap=cap)) == 1, cap
     assert fwd(shape=_shape(g, d=96)) == 2 and fwd(shape=_shape(g, "f32", d=516, heads=4), ldq=516) == 2
 
     def bwd(r=None, lse=vp, dout=vp, dq=vp, lddq=64, dk=vp, ws=vp, size=1 << 20, lddo=64):

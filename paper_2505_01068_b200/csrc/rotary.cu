@@ -264,6 +264,7 @@ cudaError_t launch_rotary(const Geometry& g, int dtype, const RotaryCall& c, cud
   int n_sm = 0;
   const cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
   if (e != cudaSuccess) return e;
+  // (blocks of equal numbers a CTA, so of fewer rows, gain nothing: 64 x (50, 500, 500), half padded, 8 heads of 8 13.2 us for 12.4)
   const int64_t blocks = ((int64_t)g.batch * g.L + a.block_rows - 1) / a.block_rows;
   const unsigned grid = (unsigned)std::min(blocks, (int64_t)4 * n_sm);
   return dtype == GSIT_BF16 ? launch<__nv_bfloat16>(g, a, form, grid, st) : launch<float>(g, a, form, grid, st);

@@ -260,6 +260,37 @@ __device__ __forceinline__ Place find_place(const Tiles& tiles, int batch, int h
   p.tile = tiles.count[p.segment] - 1 - p.tile;   // from the back: under the causal rule the later rows walk further
   return p;
 }
+// ---- which pairs of a block are open ----
+constexpr int BLOCK = 64;   // partners that are classified together
+__device__ __forceinline__ int ordered(float f) {   // floats as integers of the same order
+  const int i = __float_as_int(f);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+struct Range {   // over real rows: moments (as ordered integers) and documents
+  int t_lo, t_hi, d_lo, d_hi;
+};
+__device__ __forceinline__ Range warp_range(int t_lo, int t_hi, int d_lo, int d_hi) {
+  return {__reduce_min_sync(0xffffffffu, t_lo), __reduce_max_sync(0xffffffffu, t_hi), __reduce_min_sync(0xffffffffu, d_lo), __reduce_max_sync(0xffffffffu, d_hi)};
+}
+constexpr Range NO_ROWS = {0x7fffffff, (int)0x80000000, 0x7fffffff, (int)0x80000000};
+// Queries have their latest moment seen in t, keys their own moment.
+enum Openness { SHUT, SOME, ALL };
+__device__ __forceinline__ Openness openness(const Range& queries, const Range& keys) {
+  if (queries.d_hi < keys.d_lo || keys.d_hi < queries.d_lo || keys.t_lo > queries.t_hi) return SHUT;
+  return queries.d_lo == queries.d_hi && keys.d_lo == keys.d_hi && keys.t_hi <= queries.t_lo ? ALL : SOME;
+}
+
+// Moments and documents of a block of 64 partners as a range; `t` holds what openness() compares.
+__device__ __forceinline__ Range block_range(const float* t, const int* d, int j0, int rem, int lane) {
+  Range r = NO_ROWS;
+#pragma unroll
+  for (int i = 0; i < BLOCK; i += 32)
+    if (j0 + i + lane < rem) {
+      const int o = ordered(t[j0 + i + lane]), e = d[j0 + i + lane];
+      r = {min(r.t_lo, o), max(r.t_hi, o), min(r.d_lo, e), max(r.d_hi, e)};
+    }
+  return warp_range(r.t_lo, r.t_hi, r.d_lo, r.d_hi);
+}
 // The segments that are walked, in order, in chunks: `pos` is moved on by the caller, settle() goes to the next segment that has rows.
 struct Walk {
   int n[3];          // rows to walk per segment, 0 where shut

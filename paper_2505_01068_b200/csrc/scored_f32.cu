@@ -9,10 +9,11 @@
 //                  dealt out to groups of lanes, whose sums shuffles bring together at the end
 // Between the two the weights go through shared memory, partner-major; a warp reads only what its own lanes wrote, so that a tile costs
 // one barrier.  With 2 HD (forward), 3 HD (dq) and 4 HD (dk, dv) multiply-adds a pair the FMA pipe is the bound: 128 a clock and SM.
-// Measured: MIntRec's unmasked graph (8 samples of (30, 480, 230), half of the rows padding, 8 heads of 16, forward and gradients) 340 us, of which
+// Measured: MIntRec's unmasked graph (8 samples of (30, 480, 230), half of the rows padding, 8 heads of 16, forward and gradients) 323 us, of which
 // the multiply-adds are 54; 30% of the FMA pipe's time, half of the issue slots (sums over halves, bias, addresses), the rest shared
 // memory's latency and the last of two and a fraction waves of CTAs.  One CTA an SM (more registers, nothing spilled) 350 us; weights
-// exchanged by the whole CTA, which takes two more barriers a tile, 555 us.
+// exchanged by the whole CTA, which takes two more barriers a tile, 555 us.  Warps without a real row only fetch, and tiles without an open
+pair are passed over (341 -> 323 us; 86 x (5, 12, 131), causal, 335 -> 288).
 #include "scored.cuh"
 
 namespace gsit {
@@ -96,11 +97,11 @@ template <int HD> struct Piece {
     group = lane / Sizes<HD>::OWNERS;
   }
 };
-template <int HD> __device__ __forceinline__ void product_over_partners(float2 (&o)[4][2], const float* w, const float* rows, const Piece<HD>& p) {
+template <int HD> __device__ __forceinline__ void product_over_partners(float2 (&o)[4][2], const float* w, const float* rows, const Piece<HD>& p, int partners) {
   w += p.group * WARP_ROWS + 4 * p.rt;
   rows += p.group * Sizes<HD>::PITCH + 4 * p.ct;
 #pragma unroll 4
-  for (int k = 0; k < TILE; k += Sizes<HD>::GROUPS) {
+  for (int k = 0; k < min(TILE, partners); k += Sizes<HD>::GROUPS) {   // weights past the last partner are zero, and so are its rows
     const float4 a = *reinterpret_cast<const float4*>(w + k * WARP_ROWS), v = *reinterpret_cast<const float4*>(rows + k * Sizes<HD>::PITCH);
     const float f[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -201,6 +202,19 @@ __device__ __forceinline__ void scores(float (&x)[4][4], float (&d)[4][4], const
   }
 }
 
+// Moments (or limits) and documents of a warp's rows [row, row + 8) of a segment, as far as they lie in [lo, hi).
+__device__ __forceinline__ Range rows_range(const Geometry& g, const ScoredArgs& a, int b, int s, int row, int lo, int hi, int shift, bool limits) {
+  const int i = row + (threadIdx.x & 7);
+  Range r = NO_ROWS;
+  if (i >= lo && i < hi) {
+    const float t = time_of(g, a, b, s, i + shift);
+    r.t_lo = r.t_hi = ordered(limits ? latest_seen(a, b, t) : t);
+    r.d_lo = r.d_hi = document_of(g, a, b, s, i + shift);
+  }
+  __syncwarp();
+  return warp_range(r.t_lo, r.t_hi, r.d_lo, r.d_hi);
+}
+
 // CTAs an SM that registers are kept for: what a warp waits for (shared memory, exponentials) another one's products hide.
 template <int HD> constexpr int MIN_CTAS = HD <= 32 ? 2 : 1;
 
@@ -243,6 +257,9 @@ scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
     if (rule) stage_times(own, g, a, b, s, q0 + rows.shift, min(q_end, rows.hi) - q0);
     stage(next, 0);
   }
+  const int w0 = q0 + (tid >> 5) * WARP_ROWS;   // the warp's rows; one without a real row only fetches, and tiles without an open pair are passed
+  const bool working = w0 < min(q_end, rows.hi) && w0 + WARP_ROWS > rows.lo, masks = rule_masks(a);
+  const Range mine = masks ? rows_range(g, a, b, s, w0, rows.lo, min(q_end, rows.hi), rows.shift, true) : NO_ROWS;
   for (int buf = 0; !next.over(); buf ^= 1) {
     const int rem = next.left();
     cp_wait();
@@ -250,6 +267,7 @@ scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
     next.pos += TILE;
     next.settle();
     if (!next.over()) stage(next, buf ^ 1);
+    if (!working || (masks && openness(mine, block_range(partner[buf].time, partner[buf].doc, 0, rem, tid & 31)) == SHUT)) continue;
     float x[4][4], unused[4][4], top[4];
     product_over_features<HD>(x, s_q, s_k + buf * S::ROWS, tx, ty);
     scores<false>(x, unused, a, slope2, own, partner[buf], rem, true, tx, ty);
@@ -284,7 +302,7 @@ scored_fwd_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
     }
     put_weights(s_w, x, tx, ty);
     __syncwarp();
-    product_over_partners<HD>(o, s_w, s_v + buf * S::ROWS, piece);
+    product_over_partners<HD>(o, s_w, s_v + buf * S::ROWS, piece, rem);
     __syncwarp();
   }
   ptx::grid_dep_launch();   // only now: see scored_tile.cuh
@@ -377,6 +395,9 @@ scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__
   float2 st[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) st[i] = s_stats[4 * ty + i];
+  const int w0 = (tid >> 5) * WARP_ROWS;
+  const bool working = w0 < n_rows, masks = rule_masks(a);
+  const Range mine = masks ? rows_range(g, a, b, s, q0 + w0, 0, q0 + n_rows, 0, true) : NO_ROWS;
   for (int buf = 0; !next.over(); buf ^= 1) {
     const int rem = next.left();
     cp_wait();
@@ -384,6 +405,7 @@ scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__
     next.pos += TILE;
     next.settle();
     if (!next.over()) stage(next, buf ^ 1);
+    if (!working || (masks && openness(mine, block_range(partner[buf].time, partner[buf].doc, 0, rem, tid & 31)) == SHUT)) continue;
     float x[4][4], d[4][4];
     product_over_features<HD>(d, s_g, s_v + buf * S::ROWS, tx, ty);
 #pragma unroll
@@ -398,7 +420,7 @@ scored_dq_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant__
       for (int j = 0; j < 4; ++j) x[i][j] = ptx::ex2(x[i][j] - st[i].x) * d[i][j];
     put_weights(s_w, x, tx, ty);
     __syncwarp();
-    product_over_partners<HD>(dq, s_w, s_k + buf * S::ROWS, piece);
+    product_over_partners<HD>(dq, s_w, s_k + buf * S::ROWS, piece, rem);
     __syncwarp();
   }
   ptx::grid_dep_launch();   // only now: see scored_tile.cuh
@@ -461,6 +483,9 @@ scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
     if (rule) stage_times(own, g, a, b, r, k0, n_rows);
     stage(next, h, 0);
   }
+  const int w0 = (tid >> 5) * WARP_ROWS;
+  const bool working = w0 < n_rows, masks = rule_masks(a);
+  const Range mine = masks ? rows_range(g, a, b, r, k0 + w0, 0, k0 + n_rows, 0, false) : NO_ROWS;
   for (int buf = 0; !next.over(); buf ^= 1) {
     const int rem = next.left();
     const float slope2 = a.slopes != nullptr ? a.slopes[h] * LOG2E : 0.f;
@@ -473,6 +498,7 @@ scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
       ++h;
     }
     if (!next.over()) stage(next, h, buf ^ 1);
+    if (!working || (masks && openness(block_range(partner[buf].limit, partner[buf].doc, 0, rem, tid & 31), mine) == SHUT)) continue;
     float x[4][4], d[4][4];
     product_over_features<HD>(d, s_v, s_g + buf * S::ROWS, tx, ty);
 #pragma unroll
@@ -494,11 +520,11 @@ scored_dkv_f32_kernel(const __grid_constant__ Geometry g, const __grid_constant_
     }
     put_weights(s_w, x, tx, ty);
     __syncwarp();
-    product_over_partners<HD>(dv, s_w, s_g + buf * S::ROWS, piece);
+    product_over_partners<HD>(dv, s_w, s_g + buf * S::ROWS, piece, rem);
     __syncwarp();
     put_weights(s_w, d, tx, ty);
     __syncwarp();
-    product_over_partners<HD>(dk, s_w, s_q + buf * S::ROWS, piece);
+    product_over_partners<HD>(dk, s_w, s_q + buf * S::ROWS, piece, rem);
     __syncwarp();
   }
   ptx::grid_dep_launch();   // only now: see scored_tile.cuh

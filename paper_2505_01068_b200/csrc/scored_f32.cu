@@ -13,7 +13,7 @@
 // the multiply-adds are 54; 30% of the FMA pipe's time, half of the issue slots (sums over halves, bias, addresses), the rest shared
 // memory's latency and the last of two and a fraction waves of CTAs.  One CTA an SM (more registers, nothing spilled) 350 us; weights
 // exchanged by the whole CTA, which takes two more barriers a tile, 555 us.  Warps without a real row only fetch, and tiles without an open
-pair are passed over (341 -> 323 us; 86 x (5, 12, 131), causal, 335 -> 288).
+// pair are passed over (341 -> 323 us; 86 x (5, 12, 131), causal, 335 -> 288).
 #include "scored.cuh"
 
 namespace gsit {

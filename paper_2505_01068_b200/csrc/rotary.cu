@@ -61,19 +61,21 @@ template <typename T> __device__ __forceinline__ void unpack_piece(const uint4& 
   }
 }
 
-// Place of pair p in a row of the table: groups of eight lie 40 floats apart, so that the four pieces of a head of 64 that a warp reads
-// together meet different banks.
-__device__ __forceinline__ int slot(int p) { return p + (p >> 3) * 2; }
+// Place of pair p in a row of the table: groups of eight lie ten floats apart, so that the four pieces of a head of 64 that a warp reads
+// together meet different banks.  A row takes whole groups of four floats, so some numbers of pairs fill more of the table than a float a
+// thread and a quarter (12 pairs: 16 floats, of which 21 rows, one angle a thread, would be 336): TABLE bounds the rows of a block, too.
+constexpr int TABLE = THREADS + THREADS / 4;   // floats
+__host__ __device__ __forceinline__ int slot(int p) { return p + (p >> 3) * 2; }
+__host__ __device__ __forceinline__ int table_row(int pairs) { return (slot(pairs - 1) + 4) & ~3; }
 
 template <typename T, int FORM>
 __global__ void __launch_bounds__(THREADS, FORM == SPLIT ? 4 : 3)
 rotary_kernel(const __grid_constant__ Geometry g, const __grid_constant__ RotaryArgs a) {
   constexpr int E = 16 / sizeof(T);                         // elements of a piece
   constexpr int BATCH = FORM == SCALAR ? 1 : FORM == SPLIT ? 2 : BLOCK_UNITS / THREADS;   // units whose loads are in flight together
-  constexpr int SLOTS = THREADS + THREADS / 4;
-  __shared__ __align__(16) float s_cos[2][SLOTS], s_sin[2][SLOTS];   // of row r, pair p at [r * row_slots + slot(p)]
+  __shared__ __align__(16) float s_cos[2][TABLE], s_sin[2][TABLE];   // of row r, pair p at [r * row_slots + slot(p)]
   __shared__ int s_real[2][MAX_ROWS];
-  const int tid = threadIdx.x, row_slots = (slot(a.pairs - 1) + 4) & ~3, rows = g.batch * g.L, blocks = (rows + a.block_rows - 1) / a.block_rows;
+  const int tid = threadIdx.x, row_slots = table_row(a.pairs), rows = g.batch * g.L, blocks = (rows + a.block_rows - 1) / a.block_rows;
   ptx::load_params_early(g, a);
 
   // this thread's angle of a block
@@ -258,9 +260,9 @@ cudaError_t launch_rotary(const Geometry& g, int dtype, const RotaryCall& c, cud
   const Form form = !wide ? SCALAR : c.interleaved ? ADJACENT : a.pairs % piece == 0 ? SPLIT : g.hd == piece ? HEAD : SCALAR;
   a.head_units = form == SPLIT ? a.pairs / piece : form == SCALAR ? g.hd - a.pairs : g.hd / piece;
   a.row_units = a.head_units * (c.heads[0] + c.heads[1]);
-  // rows of a block: an angle a thread, and no more units than the registers keep offsets of
+  // rows of a block: an angle a thread, all of them in the table, and no more units than the registers keep offsets of
   const int batch = form == SCALAR ? 1 : form == SPLIT ? 2 : BLOCK_UNITS / THREADS;
-  a.block_rows = std::max(1, std::min(std::min(THREADS / a.pairs, MAX_ROWS), batch * THREADS / a.row_units));
+  a.block_rows = std::max(1, std::min({THREADS / a.pairs, TABLE / table_row(a.pairs), MAX_ROWS, batch * THREADS / a.row_units}));
   int n_sm = 0;
   const cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
   if (e != cudaSuccess) return e;

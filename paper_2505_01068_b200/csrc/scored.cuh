@@ -262,8 +262,8 @@ __device__ __forceinline__ Place find_place(const Tiles& tiles, int batch, int h
 }
 // ---- which pairs of a block are open ----
 constexpr int BLOCK = 64;   // partners that are classified together
-__device__ __forceinline__ int ordered(float f) {   // floats as integers of the same order
-  const int i = __float_as_int(f);
+__device__ __forceinline__ int ordered(float f) {   // floats as integers of the same order; both zeros are 0, as comparisons have them
+  const int i = __float_as_int(f + 0.f);
   return i ^ ((i >> 31) & 0x7fffffff);
 }
 struct Range {   // over real rows: moments (as ordered integers) and documents

@@ -1,0 +1,43 @@
+"""Scored attention where single values decide."""
+import pytest
+import torch
+
+from test_gpu_scored_attention import Problem, _check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_2505_01068_b200 as lib
+    lib.load()
+    return lib
+
+
+# ---- moments of -0.0 and +0.0 are one moment ----
+
+def _ages(p, seg):
+    """Segment 0 timed by its age, so that its newest position has -0.0; the others start at +0.0."""
+    t = torch.cat([-1.0 * torch.arange(seg[0] - 1, -1, -1, dtype=torch.float32), torch.arange(seg[1]).float() * 0.25, torch.arange(seg[2]).float() * 0.5])
+    p.times = t.cuda().expand(p.B, -1).contiguous()
+    assert float(p.times[0, seg[0] - 1]) == 0.0 and bool(torch.signbit(p.times[0, seg[0] - 1]))
+
+
+@pytest.mark.parametrize("dtype,hd,seg", [("bf16", 8, (20, 90, 45)), ("bf16", 16, (20, 90, 45)), ("bf16", 32, (70, 64, 300)), ("bf16", 64, (70, 41, 60)),
+                                          ("bf16", 64, (130, 300, 257)), ("f32", 16, (20, 90, 45)), ("f32", 64, (70, 200, 3)), ("f32", 96, (20, 90, 45))])
+@pytest.mark.parametrize("rule", [dict(), dict(cap=20.0, slopes=True), dict(docs=-1)], ids=str)
+def test_moments_of_either_zero_are_equal(g, dtype, hd, seg, rule):
+    """The newest position of segment 0 sees the first key of segment 1 and nothing else: its result is that key's value."""
+    p = Problem(dtype, 2, seg, 2, 1, hd, "fwd", padded=False, causal=True, **rule)
+    _ages(p, seg)
+    out, lse = _check(g, p)
+    row = out[:, seg[0] - 1].view(2, 2, hd)
+    assert torch.equal(row, p.v[:, seg[0]].expand(2, 2, hd)) and bool(torch.isfinite(lse[:, :, seg[0] - 1]).all())
+
+
+@pytest.mark.parametrize("dtype,hd,seg", [("bf16", 16, (20, 900, 45)), ("bf16", 64, (130, 300, 257)), ("f32", 16, (20, 90, 45)), ("f32", 24, (20, 90, 45))])
+def test_moments_of_either_zero_are_equal_to_the_newest_position(g, dtype, hd, seg):
+    p = Problem(dtype, 2, seg, 2, 1, hd, "fwd", padded=False, causal=True, q_len=(1, 1, 1))
+    _ages(p, seg)
+    out, _ = _check(g, p, grads=False)
+    assert torch.equal(out[:, 0].view(2, 2, hd), p.v[:, seg[0]].expand(2, 2, hd))

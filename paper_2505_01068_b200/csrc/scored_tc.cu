@@ -71,6 +71,11 @@ template <int N> __device__ __forceinline__ float largest(const float (&x)[N]) {
   return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
 
+__device__ __forceinline__ float sum_of(const float2 (&part)[4]) {
+  const float2 s = __fadd2_rn(__fadd2_rn(part[0], part[1]), __fadd2_rn(part[2], part[3]));
+  return s.x + s.y;
+}
+
 template <int KIND, bool CAP, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(THREADS, Map<KIND>::CTAS)
 scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
@@ -398,12 +403,11 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
               w[c / 2 + e] = pack_bf16(p.x, p.y);
             }
           }
-          const float2 p2 = __fadd2_rn(__fadd2_rn(part[0], part[1]), __fadd2_rn(part[2], part[3]));
-          added = p2.x + p2.y;
+          added = sum_of(part);
           top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
         });
-        if (__any_sync(0xffffffffu, top > room)) {   // rare: the weights once more, relative to a new reference
-          const bool grow = top > room;
+        const bool grow = real && top > room;
+        if (__any_sync(0xffffffffu, grow)) {   // rare: the weights once more, relative to a new reference, added up in the same order
           const float f = grow && room != -INFINITY ? ex2(-top) : 1.f;
           if (t > 0) {   // once the accumulator holds all earlier tiles
             mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);
@@ -424,13 +428,14 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
             ref += top;
             room = 8.f;
           }
-          added = 0.f;
+          float2 part[4] = {};
 #pragma unroll
           for (int c = 0; c < PARTNER; c += 2) {
             const float2 p = make_float2(ex2(x[c] - shift), ex2(x[c + 1] - shift));
-            added += p.x + p.y;
+            part[c / 2 % 4] = __fadd2_rn(part[c / 2 % 4], p);
             w[c / 2] = pack_bf16(p.x, p.y);
           }
+          added = sum_of(part);
           __syncwarp();
         }
         sum += added;

@@ -41,3 +41,30 @@ def test_moments_of_either_zero_are_equal_to_the_newest_position(g, dtype, hd, s
     _ages(p, seg)
     out, _ = _check(g, p, grads=False)
     assert torch.equal(out[:, 0].view(2, 2, hd), p.v[:, seg[0]].expand(2, 2, hd))
+
+
+# ---- rows beside a tile's real ones ----
+
+@pytest.mark.parametrize("seg", [(130, 300, 257), (100, 200, 192)], ids=str)
+@pytest.mark.parametrize("phase", ["intra", "all"])
+def test_other_rows_of_a_tile_leave_a_rows_bits(g, seg, phase):
+    """head_dim 64, scores without a cap: padded queries, and the queries of the next segment and of the next sample, which a tile's load
+    brings along, may hold large values that outgrow their references late; the bits of the other rows stay."""
+    p = Problem("bf16", 3, seg, 2, 2, 64, phase, seed=11)
+    pad, L = p.padding(), sum(seg)
+    large = (torch.randn(p.q.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)) * 100).bfloat16()
+    q = p.q.clone()
+    p.q = torch.where(pad[:, :, None, None], 0.0, q)
+    out, lse = p.forward(g)
+    p.q = torch.where(pad[:, :, None, None], large, q)
+    got = p.forward(g)
+    assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+    p.q = q.clone()
+    p.q[:, seg[0]:] = large[:, seg[0]:]
+    got = p.forward(g)
+    assert torch.equal(got[0][:, :seg[0]], out[:, :seg[0]]) and torch.equal(got[1][:, :, :seg[0]], lse[:, :, :seg[0]])
+    p.q = q.clone()
+    p.q[1:] = large[1:]
+    got = p.forward(g)
+    assert torch.equal(got[0][0], out[0]) and torch.equal(got[1][0], lse[0])
+    assert g.last_device_status() == (0, 0)

@@ -163,7 +163,7 @@ __device__ __forceinline__ void scores(float (&x)[4][4], float (&d)[4][4], const
     for (int j = 0; j < 4; j += 2) {
       float2 y = __fmul2_rn(make_float2(x[i][j], x[i][j + 1]), f);
       if (cap) {
-        const float2 t = tanh_any2(y);
+        const float2 t = make_float2(tanhf(y.x), tanhf(y.y));
         y = __fmul2_rn(t, make_float2(a.outer, a.outer));
         if (BEND) {
           d[i][j] *= 1.f - t.x * t.x;

@@ -265,7 +265,7 @@ scored_tail_kernel(const __grid_constant__ Geometry g, const __grid_constant__ S
 #pragma unroll
       for (int c = 0; c < SHARE; ++c) {
         float d = x[c] * a.inner;
-        if (a.softcap > 0.f) d = tanh_any(d) * a.outer;
+        if (a.softcap > 0.f) d = tanhf(d) * a.outer;
         if (RULE) d -= row_of[c].slope2 * fabsf(row_of[c].time - time[c]);
         x[c] = open[c] && (!RULE || time[c] <= row_of[c].limit) ? d : -INFINITY;
       }

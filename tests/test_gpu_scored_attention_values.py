@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_scored_attention import Problem, _check
+from test_gpu_scored_attention import TOL, Problem, _check, _close
 
 pytestmark = pytest.mark.gpu
 
@@ -43,6 +43,78 @@ def test_moments_of_either_zero_are_equal_to_the_newest_position(g, dtype, hd, s
     _ages(p, seg)
     out, _ = _check(g, p, grads=False)
     assert torch.equal(out[:, 0].view(2, 2, hd), p.v[:, seg[0]].expand(2, 2, hd))
+
+
+# ---- NaN in a stream's rows ----
+
+STREAMS = [("bf16", 8, 4, 2, (1, 1, 1)), ("bf16", 16, 2, 2, (1, 1, 1)), ("bf16", 32, 4, 1, (1, 0, 1)), ("bf16", 64, 4, 2, (2, 1, 1)), ("f32", 8, 1, 1, (1, 0, 0)),
+           ("f32", 16, 2, 2, (1, 1, 1)), ("f32", 32, 4, 2, (1, 1, 1)), ("f32", 64, 2, 2, (1, 1, 1)), ("f32", 24, 2, 1, (1, 1, 1))]
+SEG = (100, 500, 300)
+
+
+@pytest.mark.parametrize("rule", [dict(), dict(cap=20.0), dict(slopes=True, docs=-3, causal=True)], ids=str)
+@pytest.mark.parametrize("stream", STREAMS, ids=str)
+def test_nan_reaches_the_newest_rows_that_it_is_open_to(g, stream, rule):
+    """NaN in a query, in an open key, in an open value: NaN in what depends on it, other rows to rounding."""
+    dtype, hd, H, HK, q_len = stream
+    make = lambda: Problem(dtype, 2, SEG, H, HK, hd, "intra", padded=False, q_len=q_len, **rule)
+    base, blse = make().forward(g)
+    base = base.view(2, sum(q_len), H, hd)
+    last = q_len[0] - 1                      # the newest row of segment 0, position 99
+    for what in ("q", "k", "v"):
+        p = make()
+        if what == "q":
+            p.q[0, last, 0, 1] = float("nan")
+            hit = [0]
+        else:
+            getattr(p, what)[0, 99, 0, 1] = float("nan")
+            hit = list(range(H // HK))
+        out, lse = p.forward(g)
+        out = out.view(2, sum(q_len), H, hd)
+        broken = torch.zeros_like(out, dtype=torch.bool)
+        rows = [last] if what == "q" or rule.get("causal") else list(range(last + 1))   # without causality every query of segment 0 sees key 99
+        for i in rows:
+            broken[0, i, hit] = True
+        if what == "v":
+            broken[..., :1] = broken[..., 2:] = False
+        assert bool(out[broken].isnan().all()), what
+        _close(torch.where(broken, 0.0, out.float()), torch.where(broken, 0.0, base.double()), TOL[dtype]["out"], what)
+        lse_broken = torch.zeros_like(lse, dtype=torch.bool)
+        if what != "v":
+            for i in rows:
+                lse_broken[0, hit, i] = True
+        assert bool(lse[lse_broken].isnan().all()) and torch.allclose(lse[~lse_broken], blse[~lse_broken], atol=2e-5, rtol=2e-5), what
+    assert g.last_device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("fill", [float("nan"), float("inf"), -3.38e38])
+@pytest.mark.parametrize("stream", STREAMS, ids=str)
+def test_what_stands_in_closed_keys_does_not_reach_the_newest_rows(g, stream, fill):
+    """Keys of another document, and keys past the valid ones."""
+    dtype, hd, H, HK, q_len = stream
+    p = Problem(dtype, 2, SEG, H, HK, hd, "all", q_len=q_len, docs=-3, causal=True, seed=4)
+    base = p.forward(g)
+    for t in (p.k, p.v):
+        t[p.padding()] = fill
+    got = p.forward(g)
+    assert torch.equal(got[0], base[0]) and torch.equal(got[1], base[1])
+    shut = p.docs == 1
+    assert bool((shut & ~p.padding()).any())
+    keep = torch.zeros(2, sum(q_len), dtype=torch.bool, device="cuda")   # rows whose own document is another
+    first = (0, SEG[0], SEG[0] + SEG[1])
+    for b in range(2):
+        i = 0
+        for s in range(3):
+            for r in range(q_len[s]):
+                at = int(p.n[b, s]) - q_len[s] + r
+                keep[b, i] = at >= 0 and int(p.docs[b, first[s] + at]) != 1
+                i += 1
+    assert bool(keep.any())
+    for t in (p.k, p.v):
+        t[shut] = fill
+    out, lse = p.forward(g)
+    _close(out[keep], base[0][keep].double(), TOL[dtype]["out"], "out")
+    assert torch.allclose(lse.transpose(1, 2)[keep], base[1].transpose(1, 2)[keep], atol=2e-5, rtol=2e-5)
 
 
 # ---- rows beside a tile's real ones ----

@@ -50,16 +50,18 @@ class _ScoredAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, seg_len, valid_len, rule):
         out, lse = B.im_scored_attention_fwd(q, k, v, seg_len, valid_len, want_lse=True, **rule)
-        ctx.save_for_backward(q, k, v, out, lse, valid_len)
-        ctx.args = (seg_len, rule)
+        # the rule's tensors are saved as the others are: what is written to them before the backward pass raises there
+        tensors = {n: t for n, t in rule.items() if isinstance(t, torch.Tensor)}
+        ctx.save_for_backward(q, k, v, out, lse, valid_len, *tensors.values())
+        ctx.args = (seg_len, {n: t for n, t in rule.items() if n not in tensors}, tuple(tensors))
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        q, k, v, out, lse, valid_len = ctx.saved_tensors
-        seg_len, rule = ctx.args
-        return B.im_scored_attention_bwd(dout.contiguous(), q, k, v, out, lse, seg_len, valid_len, **rule) + (None, None, None)
+        q, k, v, out, lse, valid_len, *tensors = ctx.saved_tensors
+        seg_len, rule, names = ctx.args
+        return B.im_scored_attention_bwd(dout.contiguous(), q, k, v, out, lse, seg_len, valid_len, **rule, **dict(zip(names, tensors))) + (None, None, None)
 
 
 def layer_norm(x, gamma, beta, seg_len=None, valid_len=None, eps=1e-5, out_dtype=None):

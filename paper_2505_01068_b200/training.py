@@ -107,6 +107,9 @@ class ImEncoderLayer(torch.nn.Module):
         for name in ("ln1", "ln2"):
             setattr(self, name + "_g", torch.nn.Parameter(torch.ones(d_model, device=device)))
             setattr(self, name + "_b", torch.nn.Parameter(torch.zeros(d_model, device=device)))
+        # of every row its place in its segment, and that segment: on the device once, so that a captured step has nothing to copy
+        self.register_buffer("place", torch.cat([torch.arange(n, device=device) for n in self.seg_len]), persistent=False)
+        self.register_buffer("segment", torch.cat([torch.full((n,), s, device=device) for s, n in enumerate(self.seg_len)]), persistent=False)
 
     def project(self, x, valid_len=None, positions=None, seg_len=None):
         """(q, k, v) [B, L, H, hd] of the layer: norm, shared projection, rotation."""
@@ -129,7 +132,5 @@ class ImEncoderLayer(torch.nn.Module):
         y = self.finish(x, im_scored_attention(q, k, v, self.seg_len, valid_len, **rule), valid_len)
         if valid_len is None:
             return y
-        seg = torch.tensor(self.seg_len, device=x.device)
-        place = torch.cat([torch.arange(n, device=x.device) for n in self.seg_len])
-        real = place[None, :] < torch.repeat_interleave(valid_len, seg, dim=1, output_size=int(sum(self.seg_len)))
+        real = self.place < valid_len[:, self.segment]
         return torch.where(real[:, :, None], y, 0.0)

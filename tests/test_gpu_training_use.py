@@ -1,4 +1,4 @@
-"""The differentiable operators as a training program uses them: tensors that are written to between the passes."""
+"""The differentiable operators as a training program uses them: tensors that are written to between the passes, steps that are captured."""
 import pytest
 import torch
 
@@ -47,3 +47,36 @@ def test_saved_tensor_hooks_see_the_rule(g):
         out = t.im_scored_attention(q, k, v, SEG, **rule)
     assert {rule[n].data_ptr() for n in ("slopes", "times", "documents", "prefix")} <= set(seen)
     assert all(torch.equal(a, b) for a, b in zip(want, torch.autograd.grad(out.square().sum(), (q, k, v))))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_layers_step_is_captured(g, dtype):
+    """Forward and backward pass in a CUDA graph, with lengths that change from replay to replay: the bits of plain calls."""
+    from paper_2505_01068_b200.training import ImEncoderLayer
+    torch.manual_seed(2)
+    layer = ImEncoderLayer(32, 4, SEG, sections=(2, 1, 1), dtype=dtype)
+    assert not any("place" in n or "segment" in n for n in layer.state_dict())
+    x, w = (torch.randn((3, 78, 32), device="cuda") for _ in range(2))
+    pos = torch.randint(0, 50, (3, 3, 78), device="cuda", dtype=torch.int32)
+    lengths = [torch.tensor(n, dtype=torch.int32, device="cuda") for n in ([[8, 40, 30], [3, 20, 0], [0, 1, 30]], [[1, 2, 3], [8, 40, 30], [5, 0, 29]])]
+    valid = lengths[0].clone()
+    x.requires_grad_()
+
+    def step():
+        y = layer(x, valid, pos, phase=g.PHASE_INTER_FWD, softcap=10.0)
+        return [y.detach()] + list(torch.autograd.grad((y * w).sum(), [x, *layer.parameters()]))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for n in (1, 0, 1):
+        valid.copy_(lengths[n])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), n
+    assert g.last_device_status() == (0, 0)

@@ -22,10 +22,19 @@ gsit_status padded_geometry(const gsit_shape* shape, Geometry* g) {
   return g->row_start == nullptr ? GSIT_OK : GSIT_ERR_UNSUPPORTED;
 }
 
+// The shape of a call that reads no block pattern: what stands in its fields is not looked at.
+gsit_shape any_phase(gsit_shape s) {
+  s.phase = GSIT_PHASE_INTRA;
+  s.custom_mask = 0;
+  return s;
+}
+
 gsit_status rotary(const gsit_shape* shape, const gsit_rotary* r, const void* q, int64_t ldq, const void* k, int64_t ldk, void* q_out, int64_t ldqo,
                    void* k_out, int64_t ldko, bool backward, gsit_stream stream) {
+  if (shape == nullptr) return GSIT_ERR_INVALID_ARG;
+  const gsit_shape rows = any_phase(*shape);
   Geometry g;
-  const gsit_status st = padded_geometry(shape, &g);
+  const gsit_status st = padded_geometry(&rows, &g);
   if (st != GSIT_OK) return st;
   if (r == nullptr || r->positions == nullptr || q == nullptr || q_out == nullptr || (k == nullptr) != (k_out == nullptr)) return GSIT_ERR_INVALID_ARG;
   int64_t pairs = 0;
@@ -48,11 +57,14 @@ gsit_status rotary(const gsit_shape* shape, const gsit_rotary* r, const void* q,
 
 bool norm_type(int32_t t) { return t == GSIT_F32 || t == GSIT_BF16; }
 gsit_status norm_geometry(const gsit_shape* shape, Geometry* g) {
-  const gsit_status st = padded_geometry(shape, g);
+  if (shape == nullptr) return GSIT_ERR_INVALID_ARG;
+  gsit_shape rows = any_phase(*shape);   // rows of d_model features: neither heads nor the type are read
+  rows.heads = 1;
+  rows.dtype = GSIT_F32;
+  const gsit_status st = padded_geometry(&rows, g);
   if (st != GSIT_OK) return st;
   return g->d <= MAX_NORM_WIDTH ? GSIT_OK : GSIT_ERR_UNSUPPORTED;
 }
-
 
 // Geometry and rule of an attention call, checked; the tensors are filled in by the caller.
 gsit_status scored_args(const gsit_shape* shape, const gsit_score_rule* r, Geometry* g, ScoredArgs* a) {

@@ -48,7 +48,7 @@ gsit_status rotary(const gsit_shape* shape, const gsit_rotary* r, const void* q,
   const int64_t dq = g.d, dk = (int64_t)kv_heads * g.hd;
   if (ldq < dq || ldqo < dq || (k != nullptr && (ldk < dk || ldko < dk))) return GSIT_ERR_INVALID_ARG;
   const size_t es = element_size(shape->dtype);
-  if (!aligned(q, es) || !aligned(k, es) || !aligned(q_out, es) || !aligned(k_out, es)) return GSIT_ERR_INVALID_ARG;
+  if (!aligned(q, es) || !aligned(k, es) || !aligned(q_out, es) || !aligned(k_out, es) || !aligned(r->positions, 4)) return GSIT_ERR_INVALID_ARG;
   if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
   const RotaryCall c = {{q, k}, {q_out, k_out}, {ldq, ldk}, {ldqo, ldko}, {g.heads, k == nullptr ? 0 : kv_heads}, r->positions, r->axis_stride,
                         r->batch_stride, {r->sections[0], r->sections[1], r->sections[2]}, r->interleaved != 0, backward, r->base};

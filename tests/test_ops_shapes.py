@@ -36,3 +36,9 @@ def test_rotary_reads_no_pattern(g, name):
     call = lambda s: _call(lib, name, s, r, vp, 256, vp, 256, vp, 256, vp, 256, None)
     assert call(_shape(g, d=256, heads=1)) == 2
     assert call(_odd(g, d=256, heads=1)) == 2
+
+
+def test_rotary_refuses_positions_between_integers(g):
+    lib, vp = g.load(), ctypes.c_void_p(P)
+    r = Rotary(P + 2, 20, 10, (ctypes.c_int32 * 3)(4, 2, 2), 0, 0, 10000.0)
+    assert _call(lib, "gsit_rotary_fwd", _shape(g), r, vp, 64, vp, 64, vp, 64, vp, 64, None) == 1

@@ -21,6 +21,12 @@ const float* float_vector(const at::Tensor* t, int64_t n, const char* what) {
   require(t == nullptr || (t->is_cuda() && t->scalar_type() == at::kFloat && t->is_contiguous() && t->numel() == n), what);
   return static_cast<const float*>(ptr(t));
 }
+// A workspace that the caller gives.
+const at::Tensor* scratch(PyObject* o) {
+  const at::Tensor* t = opt_tensor(o);
+  require(t == nullptr || (t->is_cuda() && t->is_contiguous()), "workspace: contiguous, on the device");
+  return t;
+}
 PyObject* pack(std::initializer_list<at::Tensor> ts) {
   PyObject* tuple = PyTuple_New((Py_ssize_t)ts.size());
   if (tuple == nullptr) throw PyFail{};
@@ -157,7 +163,7 @@ PyObject* layer_norm_fwd(PyObject* const* a) {
 // dy, x, mean, rstd, gamma, seg_len, valid_len, residual, want_params, out, workspace
 PyObject* layer_norm_bwd(PyObject* const* a) {
   const at::Tensor &dy = tensor(a[0]), &x = tensor(a[1]), &mean = tensor(a[2]), &rstd = tensor(a[3]);
-  const at::Tensor *gamma = opt_tensor(a[4]), *valid = opt_tensor(a[6]), *residual = opt_tensor(a[7]), *out = opt_tensor(a[9]), *ws = opt_tensor(a[10]);
+  const at::Tensor *gamma = opt_tensor(a[4]), *valid = opt_tensor(a[6]), *residual = opt_tensor(a[7]), *out = opt_tensor(a[9]), *ws = scratch(a[10]);
   const int64_t ldx = feature_rows(x, "x: [B, L, d] on the device, features contiguous, rows evenly spaced");
   const int64_t lddy = feature_rows(dy, "dy: [B, L, d] on the device, features contiguous, rows evenly spaced");
   require(dy.sizes() == x.sizes(), "dy and x share their shape");
@@ -259,7 +265,7 @@ PyObject* scored_fwd(PyObject* const* a) {
 // dout, q, k, v, out, lse, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix, grads, workspace
 PyObject* scored_bwd(PyObject* const* a) {
   const at::Tensor &dout = tensor(a[0]), &q = tensor(a[1]), &k = tensor(a[2]), &v = tensor(a[3]), &out = tensor(a[4]), &lse = tensor(a[5]);
-  const at::Tensor *valid = opt_tensor(a[7]), *ws = opt_tensor(a[18]);
+  const at::Tensor *valid = opt_tensor(a[7]), *ws = scratch(a[18]);
   const int64_t ldq = head_rows(q, QKV_VIEWS), ldk = head_rows(k, QKV_VIEWS), ldv = head_rows(v, QKV_VIEWS);
   const int64_t B = q.size(0), L = q.size(1), H = q.size(2), hd = q.size(3), HK = k.size(2);
   require(k.sizes() == v.sizes() && k.size(0) == B && k.size(1) == L && k.size(3) == hd && k.scalar_type() == q.scalar_type() &&

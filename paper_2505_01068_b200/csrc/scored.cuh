@@ -28,7 +28,7 @@ struct ScoredArgs {
   const void* dout; int64_t lddo;
   void *dq, *dk, *dv;
   int64_t lddq, lddk, lddv;
-  float2* row_stats;                      // [B, H, L]: (lse in base 2, +inf for a row without open keys; dO . O)
+  float2* row_stats;                      // [B, H, L]: (lse in base 2, +inf for a row without open keys; sum over P dP)
 };
 
 __host__ __device__ __forceinline__ bool rule_masks(const ScoredArgs& a) { return a.causal != 0 || a.documents != nullptr; }
@@ -171,8 +171,8 @@ __device__ __noinline__ void dq_row(const Geometry& g, const ScoredArgs& a, int 
   const int64_t row = (int64_t)b * g.L + g.off(s) + i, at = ((int64_t)b * g.heads + h) * g.L + g.off(s) + i;
   const int64_t head = (int64_t)h * g.hd, key_head = (int64_t)(h / a.group) * g.hd;
   const float lse = i < valid_rows(g, b, s) ? a.lse[at] : -INFINITY;
-  float lse2 = INFINITY, delta = 0.f;
-  LaneRow acc = {};
+  float lse2 = INFINITY, delta = 0.f, more = 0.f;   // more, along: see scored_bwd.cu
+  LaneRow acc = {}, along = {};
   if (lse != -INFINITY) {
     const LaneRow q = lane_row<T>(a.q, row * a.ldq + head, g.hd), go = lane_row<T>(a.dout, row * a.lddo + head, g.hd);
     delta = lane_dot(lane_row<T>(a.out, row * a.ldo + head, g.hd), go);
@@ -188,13 +188,17 @@ __device__ __noinline__ void dq_row(const Geometry& g, const ScoredArgs& a, int 
         const LaneRow k = lane_row<T>(a.k, key * a.ldk + key_head, g.hd);
         float bend;
         const float p = ptx::ex2(score_of(a, lane_dot(k, q), slope2, fabsf(t - tj), &bend) - lse2);
-        lane_add(acc, p * (lane_dot(lane_row<T>(a.v, key * a.ldv + key_head, g.hd), go) - delta) * bend, k);
+        const float d = lane_dot(lane_row<T>(a.v, key * a.ldv + key_head, g.hd), go) - delta;
+        more += p * d;
+        lane_add(acc, p * d * bend, k);
+        lane_add(along, p * bend, k);
       }
     }
   }
+  lane_add(acc, -more, along);
   __syncwarp();
   store_lane_row<T>(a.dq, row * a.lddq + head, g.hd, acc, a.scale);
-  if ((threadIdx.x & 31) == 0) a.row_stats[at] = make_float2(lse2, delta);
+  if ((threadIdx.x & 31) == 0) a.row_stats[at] = make_float2(lse2, delta + more);
 }
 
 // Gradients of key and value row j of segment r, key head hk: over the query heads that share it and all their open rows.

@@ -3,11 +3,19 @@
 // With P = exp(x - lse), dP = dO V^T and delta = rowsum(dO o O):  dX = P o (dP - delta),  dS = dX o (derivative of the cap),
 // dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.  Two kernels, each of which owns the rows it adds up and recomputes the scores:
 // no atomics, no partial sums in memory, the same bits every time.
-//   dq    a warp owns 16 * MT query rows and walks keys (as the forward kernel does); it also writes each row's (lse in base 2, delta)
+//   dq    a warp owns 16 * MT query rows and walks keys (as the forward kernel does); it also writes each row's (lse in base 2, delta), delta as
+//         the sum over P dP that it makes on its way
 //   dkv   a warp owns 16 * MT key rows and walks the queries of all heads that share them, products transposed: x^T = K Q^T
-// delta enters as the start of the accumulators of dP.  P and dS are rounded to bf16 for the second products (as any product on these
-// units rounds its operands; sums are held in 32 bits): gradients are 2^-8.5 of their norm off 64 bits, where rounding them to bf16 is 2^-9.2.
-// What bounds them is what bounds the forward kernel, with 10 packed multiply-adds for 7: MOSEI's step 87 (dq) and 96 us (dk and dv).
+// delta enters as the start of the accumulators of dP.
+// What is rounded to fewer bits: P and dS, to bf16, as operands of the second products (any product on these units rounds its operands; sums are
+// held in 32 bits), which makes as large an error as rounding the gradients does: together 2^-8.7 of their norm, where the latter alone is 2^-9.2.
+// Two more errors of that size are taken out, in dq:
+//   the O that comes in was rounded, so dO . O is not the sum over P dP, and where rows see a handful of keys dq and dk had 2^-8.1 to 2^-8.6 from
+//   that.  With r = sum over P (dP - dO . O), summed up in 32 bits, dq takes off r times sum over P o bend K (`along`, one product more)
+//   and dk and dv get delta = dO . O + r.
+//   heads of 8: the terms of dq cancel (2^-8.65 of its norm with one rounded operand), so dS goes into the product as two bf16 terms.
+// Gradients of MOSEI's step 187 us, 169 without either (dq 108 for 89 under the profiler); 64 x (39, 55, 400), 8 heads of 16 65 us for 63.
+// What bounds them is what bounds the forward kernel, with more instructions to a pair of scores: 71 M (dq) and 63 M (dk and dv) for 58 M.
 #include "scored_tile.cuh"
 
 namespace gsit {
@@ -19,7 +27,8 @@ constexpr int MT = 1, OWN = 16 * MT * W;  // row tiles of a warp (two: dq 107 us
 template <int HD, int CTAS, bool CAP, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(32 * W, CTAS)
 scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ ScoredArgs a, const __grid_constant__ Tiles tiles) {
-  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, NT = HD <= 16 ? 4 : 2;
+  constexpr int KC = CHUNK_ROWS<HD>, CH = HD / 8, NT = HD == 8 || (HD == 16 && CTAS < 7) ? 4 : 2;
+  constexpr bool REST = HD == 8;   // dS as two terms
   constexpr bool TIMES = BIAS || MASK;
   __shared__ __align__(128) uint8_t s_k[2][KC * HD * 2], s_v[2][KC * HD * 2];
   __shared__ __align__(16) float s_time[2][TIMES ? KC : 4];
@@ -99,7 +108,6 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       d += __shfl_xor_sync(0xffffffffu, d, 1);
       d += __shfl_xor_sync(0xffffffffu, d, 2);
       delta[m][i] = d;
-      if (row < q_end && (lane & 3) == 0) a.row_stats[stat0 + row] = make_float2(lse2[m][i], d);
     }
   }
   if (MASK) mine = warp_range(mine.t_lo, mine.t_hi, mine.d_lo, mine.d_hi);
@@ -109,13 +117,14 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
   const LaneAt<HD> at_kn = lane_as_n<HD>(smem_u32(s_k[0]), lane), at_kk = lane_as_k<HD>(smem_u32(s_k[0]), lane);
   const LaneAt<HD> at_v = lane_as_n<HD>(smem_u32(s_v[0]), lane);
 
-  float dq[MT][CH][4];
+  float dq[MT][CH][4], along[MT][CH][4];
+  float2 missed[MT][2] = {};   // sums over P (dP - dO . O)
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) dq[m][c][e] = 0.f;
+      for (int e = 0; e < 4; ++e) dq[m][c][e] = along[m][c][e] = 0.f;
 
   auto step = [&](auto some_tag, int buf, int j, int rem) {
     constexpr bool SOME_SHUT = decltype(some_tag)::value;
@@ -126,7 +135,7 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
       z[0] = z[1] = -delta[m][0];
       z[2] = z[3] = -delta[m][1];
     });
-    uint32_t w[MT][NT][2];
+    uint32_t w[MT][NT][2], wb[MT][NT][2], rest[MT][REST ? NT : 2][2];
     in_form<CAP, MT, NT>(x, a, [&](auto near) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
@@ -136,21 +145,28 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
           if constexpr (BIAS) times = *reinterpret_cast<const float2*>(&s_time[buf][j + 8 * n + 2 * (lane & 3)]);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float2 d = make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]);
-            float2 y = score_pair<CAP, true, decltype(near)::value != 0>(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(lse2[m][i], lse2[m][i]), d, a);
+            const float2 d = make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]);
+            float2 bend, y = score_pair<CAP, true, decltype(near)::value != 0>(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), make_float2(lse2[m][i], lse2[m][i]), bend, a);
             if constexpr (BIAS) y = bias_pair(y, times, own_time[m][i], slope2);
             if constexpr (SOME_SHUT) {
               auto shut = [&](int col) { return col >= rem || (MASK && (s_time[buf][col] > limit[m][i] || s_doc[buf][col] != own_doc[m][i])); };
               const int col = j + 8 * n + 2 * (lane & 3);
               y = make_float2(shut(col) ? -INFINITY : y.x, shut(col + 1) ? -INFINITY : y.y);
             }
-            const float2 ds = __fmul2_rn(make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), d);
+            const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), pb = times_bend<CAP>(p, bend), ds = __fmul2_rn(pb, d);
+            missed[m][i] = CAP ? __ffma2_rn(p, d, missed[m][i]) : __fadd2_rn(missed[m][i], ds);
             w[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
+            if constexpr (REST) rest[m][n][i] = pack_rest(ds, w[m][n][i]);
+            wb[m][n][i] = ptx::pack_bf16(pb.x, pb.y);
           }
         }
     });
     __syncwarp();   // lanes may have taken different ways; matrix instructions need the whole warp
-    product_over_partners<HD, MT, NT>(dq, w, at_kk, from);
+    for_partner_rows<HD, NT>(at_kk, from, [&](int first, int c, const uint32_t (&f)[4]) {
+      add_product<HD>(dq, w, first, c, f);
+      if constexpr (REST) add_product<HD>(dq, rest, first, c, f);
+      add_product<HD>(along, wb, first, c, f);
+    });
   };
 
   for (int buf = 0; !next.over(); buf ^= 1) {
@@ -189,8 +205,17 @@ scored_dq_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sco
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = w0 + 16 * m + 8 * i + (lane >> 2);
+      float more = missed[m][i].x + missed[m][i].y;
+      more += __shfl_xor_sync(0xffffffffu, more, 1);
+      more += __shfl_xor_sync(0xffffffffu, more, 2);
+      if (!real[m][i]) more = 0.f;
+      if (row < q_end && (lane & 3) == 0) a.row_stats[stat0 + row] = make_float2(lse2[m][i], delta[m][i] + more);
+#pragma unroll
+      for (int q = 0; q < CH; ++q)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) dq[m][q][2 * i + e] -= more * along[m][q][2 * i + e];
       if (MASK && real[m][i]) {
-        broken = broken || !finite(delta[m][i]);
+        broken = broken || !finite(delta[m][i] + more);
 #pragma unroll
         for (int q = 0; q < CH; ++q) broken = broken || !finite(dq[m][q][2 * i]) || !finite(dq[m][q][2 * i + 1]);
       }
@@ -317,15 +342,15 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
           if constexpr (BIAS) times = *reinterpret_cast<const float2*>(&s_time[buf][j + 8 * n + 2 * (lane & 3)]);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float2 d = make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]);
-            float2 y = score_pair<CAP, true, decltype(near)::value != 0>(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), lse2[n], d, a);
+            const float2 d = make_float2(dp[m][n][2 * i], dp[m][n][2 * i + 1]);
+            float2 bend, y = score_pair<CAP, true, decltype(near)::value != 0>(make_float2(x[m][n][2 * i], x[m][n][2 * i + 1]), lse2[n], bend, a);
             if constexpr (BIAS) y = bias_pair(y, times, own_time[m][i], slope2);
             if constexpr (SOME_SHUT) {   // columns past the last row have an lse of +inf: no weight
               auto shut = [&](int col) { return own_time[m][i] > s_limit[buf][col] || s_doc[buf][col] != own_doc[m][i]; };
               const int col = j + 8 * n + 2 * (lane & 3);
               y = make_float2(shut(col) ? -INFINITY : y.x, shut(col + 1) ? -INFINITY : y.y);
             }
-            const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), ds = __fmul2_rn(p, d);
+            const float2 p = make_float2(ptx::ex2(y.x), ptx::ex2(y.y)), ds = __fmul2_rn(p, times_bend<CAP>(d, bend));
             wp[m][n][i] = ptx::pack_bf16(p.x, p.y);
             ws[m][n][i] = ptx::pack_bf16(ds.x, ds.y);
           }
@@ -394,7 +419,7 @@ scored_dkv_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Sc
 
 // Which of the two kernels, by a type.
 struct Dq {
-  static constexpr int MANY = 8;
+  static constexpr int MANY = 7;
   template <int HD, int CTAS, bool CAP, bool BIAS, bool MASK> static constexpr auto kernel = scored_dq_kernel<HD, CTAS, CAP, BIAS, MASK>;
 };
 struct Dkv {
@@ -420,8 +445,9 @@ cudaError_t launch_pass(const Geometry& g, const ScoredArgs& a, int heads, uint3
   const int64_t n = make_tiles(&t, g.seg_len, OWN) * heads * g.batch;
   if (n > 0x7fffffffLL) return cudaErrorNotSupported;
   const dim3 grid((unsigned)n);
-  // as in the forward pass (dk and dv hold more: 6 for 8); both kernels, more / fewer CTAs an SM, us, 8 heads of 16: 2 x (50, 500, 500) 20.6 / 18.0, 8 x
-  // 43 / 38, 64 x (20, 20, 20) 14.1 / 16.3, 64 x (39, 55, 400) 63 / 70, 512 x (50, 50, 50) 134 / 165
+  // as in the forward pass (these hold more: dq 7, dk and dv 6 for 8); both kernels, more / fewer CTAs an SM, us, 8 heads of 16: 2 x (50, 500, 500)
+  // 22.7 / 18.5, 8 x 46 / 40, 64 x (20, 20, 20) 14.4 / 16.7, 64 x (39, 55, 400) 65 / 74, 512 x (50, 50, 50) 141 / 169; dq with 8 CTAs an SM 73 us for
+  // 70 (64 x (39, 55, 400)), with steps of 32 keys in place of 16 70 for 65
   if constexpr (HD <= 16)
     if (n > 8LL * n_sm) return launch_rule<K, HD, K::MANY>(g, a, t, grid, st);
   return launch_rule<K, HD, HD == 64 ? 3 : 4>(g, a, t, grid, st);

@@ -6,20 +6,23 @@
 //   dp =                own1 partner1^T        (        dO V^T, V dO^T)
 //   a thread per own row (= lane of tensor memory) turns them into weights p = exp2(score - reference or log-sum-exp) and, backward,
 //   ds = p (dp - delta) bend, packed to bf16 back into tensor memory
-//   acc0 += p partner1 (FWD)  or  ds partner0 (DQ, DKV);   acc1 += p partner1 (DKV)
+//   acc0 += p partner1 (FWD)  or  ds partner0 (DQ, DKV);   acc1 += p partner1 (DKV)  or  p bend partner0 (DQ, what dq is corrected along: scored_bwd.cu)
 // with weights from tensor memory as the A operand and the partner tile, as TMA wrote it, as an MN-major B operand: nothing is
 // transposed, no score leaves the SM.  A CTA has 256 columns of tensor memory, so two CTAs share an SM.  What one tile after the
 // other would take is mostly latency (products -> barrier -> scores -> barrier -> products: 4600 clocks a tile of the forward kind,
 // against 212 of products and 512 of exponentials), so the next tile's first products are issued as early as the columns allow:
 //   FWD  x twice (the weights take the columns of the x they come from): x of tile t + 1 beside the scores of tile t
-//   DQ   x, dp, ds and the accumulator, 224 columns: x and dp of tile t + 1 as soon as those of tile t are in registers
-//   DKV  x, dp and two accumulators; p and ds take the columns of dp: x of tile t + 1 as soon as that of tile t is in registers, dp once
-//        the products with p and ds are over
+//   DQ, DKV  x, dp and two accumulators; p and ds take the columns of dp: x of tile t + 1 as soon as that of tile t is in registers, dp
+//        once the products with p and ds are over
 // Weights and ds are rounded to bf16 for the second products, as in scored_fwd.cu and scored_bwd.cu.
-// Measured: 32 samples of (128, 1024, 1024), a quarter of the rows padding, 8 heads of 64, cap (272 million pairs): 194 (FWD), 218 (DQ) and 268 us
-// (DKV), together 355 TFLOP/s.  The products alone are 143 us at the measured cuBLAS rate, the exponentials 117 us of the special
-// function units, which are 42%, 33% and 27% busy; two computing warps a scheduler cannot hide the trips through tensor memory and barriers
-// of every tile.  Two threads a row, so four warps a scheduler: 793 us for 706.  Three CTAs an SM in the forward kind, with 128 columns of
+// Measured: 32 samples of (128, 1024, 1024), a quarter of the rows padding, 8 heads of 64, cap (272 million pairs): 184 us (FWD) and 514 (DQ and DKV,
+// half each), 350 TFLOP/s; 463 without what dq is corrected along, where ds had columns of its own and dp of the next tile came early, too.  The
+// products alone are 143 us at the measured cuBLAS rate, the exponentials 117 us of the special function units, which are 38%, 24% and 25% busy:
+// two computing warps a scheduler do not hide the trips through tensor memory and barriers of every tile.  attn_tc.cu, which keeps weights in
+// columns of their own and sets up once for many items, takes 116 us for the forward pass of the same pairs without a cap (162 here).
+// With documents and causality a quarter of the pairs are open, in 45% of the tiles, and nothing is gained: 211 + 568 us; the fetching warp looks
+// at tiles one after the other, closed ones, too, and a partly open one costs two loads and two comparisons for four columns.
+// Two threads a row, so four warps a scheduler: 793 us for 706.  Three CTAs an SM in the forward kind, with 128 columns of
 // tensor memory and x only once, so that a CTA's products and scores take turns: 193 us for 189, and 23 for 17 where a grid is small.
 // Warps: 0 fetches (own tiles once, a ring of three partner stages with what the scores need beside them, and which tiles are open at
 // all), 1 issues every product, 2 .. 5 compute.  All waits are bounded.
@@ -51,8 +54,8 @@ template <int KIND> struct Map {   // shared memory, relative to a 1024-byte ali
   static constexpr int TILES = OWN_TILES * OWN_BYTES, META = TILES + STAGES * 2 * TILE_BYTES, BARS = META + STAGES * (int)sizeof(Meta);
   static constexpr int BYTES = BARS + 128 + 1024;
   static constexpr int TMEM = 256, CTAS = 2;
-  // columns of tensor memory: x (FWD: twice), dp, ds (DQ; FWD: in x, DKV: in dp), accumulators
-  static constexpr int X = 0, DP = 64, DS = 128, ACC = KIND == DQ ? 160 : 128;
+  // columns of tensor memory: x (FWD: twice, and weights there), dp (and weights and ds there), accumulators
+  static constexpr int X = 0, DP = 64, ACC = 128;
 };
 constexpr int BAR_OWN = 0, BAR_FULL = 8, BAR_EMPTY = BAR_FULL + 8 * STAGES, BAR_X = BAR_EMPTY + 8 * STAGES, BAR_W = BAR_X + 16, BAR_DP = BAR_W + 16,
               BAR_READ = BAR_DP + 8, BAR_ACC = BAR_READ + 8, SLOT_TMEM = BAR_ACC + 8, SLOT_GAVE_UP = SLOT_TMEM + 4;
@@ -99,11 +102,11 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bars + BAR_X + 8 * i, 1);     // x is there (FWD: buffer i; backward, i = 0: and dp, but for DKV)
+      mbar_init(bars + BAR_X + 8 * i, 1);     // x is there (FWD: buffer i; backward: i = 0)
       mbar_init(bars + BAR_W + 8 * i, 128);   // the weights of tile i, i + 2, .. are there
     }
-    mbar_init(bars + BAR_DP, 1);              // DKV: dp is there
-    mbar_init(bars + BAR_READ, 128);          // x (DQ: and dp) is in registers
+    mbar_init(bars + BAR_DP, 1);              // backward: dp is there
+    mbar_init(bars + BAR_READ, 128);          // ... and x is in registers
     mbar_init(bars + BAR_ACC, 1);             // a tile's second products are over
     mbar_init_fence();
   }
@@ -242,9 +245,8 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
       tc_fence_after();
       if (go && elect_one()) {
         to_x(0);
-        if (KIND == DQ) to_dp(0);
         umma_commit(bars + BAR_X);
-        if (KIND == DKV) {
+        if (BWD) {
           to_dp(0);
           umma_commit(bars + BAR_DP);
         }
@@ -259,7 +261,6 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
           tc_fence_after();
           if (elect_one()) {
             to_x(t + 1);
-            if (KIND == DQ) to_dp(t + 1);
             umma_commit(bars + BAR_X + (KIND == FWD ? 8 * ((t + 1) & 1) : 0));
           }
           __syncwarp();
@@ -272,9 +273,8 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
           for (int k = 0; k < PARTNER / 16; ++k) {   // 16 partners: 8 columns of weights, 2048 bytes of a tile
             const uint32_t acc = (t > 0 || k > 0) ? 1u : 0u;
             if (KIND == FWD) umma_ts(tmem + M::ACC, tmem + M::X + 64 * (t & 1) + 8 * k, smem_desc_sw128(tile + TILE_BYTES + 2048 * k), TO_ACC, acc);
-            if (KIND == DQ) umma_ts(tmem + M::ACC, tmem + M::DS + 8 * k, smem_desc_sw128(tile + 2048 * k), TO_ACC, acc);
-            if (KIND == DKV) {   // each half of dp's columns: p, then ds
-              umma_ts(tmem + M::ACC + 64, tmem + M::DP + 32 * (k / 2) + 8 * (k % 2), smem_desc_sw128(tile + TILE_BYTES + 2048 * k), TO_ACC, acc);
+            if (BWD) {   // each half of dp's columns: p, then ds
+              umma_ts(tmem + M::ACC + 64, tmem + M::DP + 32 * (k / 2) + 8 * (k % 2), smem_desc_sw128(tile + (KIND == DKV ? TILE_BYTES : 0) + 2048 * k), TO_ACC, acc);
               umma_ts(tmem + M::ACC, tmem + M::DP + 32 * (k / 2) + 16 + 8 * (k % 2), smem_desc_sw128(tile + 2048 * k), TO_ACC, acc);
             }
           }
@@ -282,7 +282,7 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
           umma_commit(bars + BAR_ACC);
         }
         __syncwarp();
-        if (KIND == DKV && go) {
+        if (BWD && go) {
           mbar_wait_warp(wc, bars + BAR_ACC, t & 1);
           tc_fence_after();
           if (elect_one()) {
@@ -321,8 +321,8 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
           for (int e = 0; e < 8; ++e) delta += o8[e] * g8[e];
         }
       }
-      if (row < o_end) a.row_stats[stat] = make_float2(lse2, delta);
     }
+    float2 missed = make_float2(0.f, 0.f);   // DQ: see scored_bwd.cu
     float ref = 0.f, room = -INFINITY, sum = 0.f;   // FWD: see scored_fwd.cu
     int t = 0;
 #pragma unroll 1
@@ -444,34 +444,22 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
         // that is ahead of the others could else meet, in the end, the parity of two phases before the one it waits for
         if (t > 0) mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);
       } else {
-        uint32_t xr[2][32];
-        if (KIND == DKV) {   // x leaves its columns at once
-          tmem_ld32(x_at, xr[0]);
-          tmem_ld32(x_at + 32, xr[1]);
-          tmem_wait_ld(xr[0], xr[1]);
-          tc_fence_before();
-          mbar_arrive(bars + BAR_READ);
-        }
+        uint32_t xr[2][32];   // x leaves its columns at once
+        tmem_ld32(x_at, xr[0]);
+        tmem_ld32(x_at + 32, xr[1]);
+        tmem_wait_ld(xr[0], xr[1]);
+        tc_fence_before();
+        mbar_arrive(bars + BAR_READ);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           constexpr int N = 32;
           uint32_t dr[32];
-          if (KIND == DKV) {
-            if (half == 0) {
-              mbar_wait_warp(wc, bars + BAR_DP, t & 1);
-              tc_fence_after();
-            }
-            tmem_ld32(tl + M::DP + N * half, dr);
-            tmem_wait_ld(dr);
-          } else {
-            tmem_ld32(x_at + N * half, xr[half]);
-            tmem_ld32(tl + M::DP + N * half, dr);
-            tmem_wait_ld(xr[half], dr);
-            if (half == 1) {
-              tc_fence_before();
-              mbar_arrive(bars + BAR_READ);
-            }
+          if (half == 0) {
+            mbar_wait_warp(wc, bars + BAR_DP, t & 1);
+            tc_fence_after();
           }
+          tmem_ld32(tl + M::DP + N * half, dr);
+          tmem_wait_ld(dr);
           float x[N];
 #pragma unroll
           for (int c = 0; c < N; ++c) x[c] = __uint_as_float(xr[half][c]);
@@ -490,8 +478,8 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
               }
               float2 d[2] = {__fadd2_rn(make_float2(__uint_as_float(dr[c]), __uint_as_float(dr[c + 1])), make_float2(-dl.x, -dl.y)),
                              __fadd2_rn(make_float2(__uint_as_float(dr[c + 2]), __uint_as_float(dr[c + 3])), make_float2(-dl.z, -dl.w))};
-              float2 y[2] = {score_pair<CAP, true, decltype(near)::value>(make_float2(x[c], x[c + 1]), make_float2(ls.x, ls.y), d[0], a),
-                             score_pair<CAP, true, decltype(near)::value>(make_float2(x[c + 2], x[c + 3]), make_float2(ls.z, ls.w), d[1], a)};
+              float2 bend[2], y[2] = {score_pair<CAP, true, decltype(near)::value>(make_float2(x[c], x[c + 1]), make_float2(ls.x, ls.y), bend[0], a),
+                                      score_pair<CAP, true, decltype(near)::value>(make_float2(x[c + 2], x[c + 3]), make_float2(ls.z, ls.w), bend[1], a)};
               if constexpr (BIAS) bias(N * half + c, y[0], y[1]);
               if constexpr (decltype(some_shut)::value) {   // rows past the last hold whatever follows in memory: neither factor may be NaN
                 bool is[4];
@@ -504,22 +492,16 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
               }
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const float2 p = make_float2(ex2(y[e].x), ex2(y[e].y)), ds = __fmul2_rn(p, d[e]);
-                if (KIND == DKV) wp[c / 2 + e] = pack_bf16(p.x, p.y);
+                const float2 p = make_float2(ex2(y[e].x), ex2(y[e].y)), pb = KIND == DQ ? times_bend<CAP>(p, bend[e]) : p;
+                const float2 ds = KIND == DQ ? __fmul2_rn(pb, d[e]) : __fmul2_rn(p, times_bend<CAP>(d[e], bend[e]));
+                if (KIND == DQ) missed = CAP ? __ffma2_rn(p, d[e], missed) : __fadd2_rn(missed, ds);
+                wp[c / 2 + e] = pack_bf16(pb.x, pb.y);
                 ws[c / 2 + e] = pack_bf16(ds.x, ds.y);
               }
             }
           });
-          if (KIND == DKV) {
-            tmem_st16(tl + M::DP + 32 * half, wp);
-            tmem_st16(tl + M::DP + 32 * half + 16, ws);
-          } else {
-            if (half == 0 && t > 0) {   // the products with the last tile's ds are over
-              mbar_wait_warp(wc, bars + BAR_ACC, (t - 1) & 1);
-              tc_fence_after();
-            }
-            tmem_st16(tl + M::DS + 16 * half, ws);
-          }
+          tmem_st16(tl + M::DP + 32 * half, wp);
+          tmem_st16(tl + M::DP + 32 * half + 16, ws);
         }
       }
       if (rem < PARTNER) {
@@ -556,6 +538,12 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
       scale[0] = a.scale;
       scale[1] = 1.f;
     }
+    float more = 0.f;
+    if (KIND == DQ) {
+      if (lse2 != INFINITY) more = missed.x + missed.y;
+      delta += more;
+      if (row < o_end) a.row_stats[stat] = make_float2(lse2, delta);
+    }
     const bool store = real && (KIND == FWD ? scale[0] != 0.f : KIND == DQ ? lse2 != INFINITY : true);
     bool broken = MASK && store && KIND == FWD && !finite(sum);
     if (KIND == DQ) broken = broken || (MASK && store && !finite(delta));
@@ -573,6 +561,13 @@ scored_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Geom
         if (walked) {
           tmem_ld32(tl + M::ACC + 64 * k + 32 * c, v);
           tmem_wait_ld(v);
+        }
+        if (KIND == DQ && walked) {
+          uint32_t along[32];
+          tmem_ld32(tl + M::ACC + 64 + 32 * c, along);
+          tmem_wait_ld(along);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) - more * __uint_as_float(along[e]));
         }
         if (row < o_end) {
 #pragma unroll
@@ -641,10 +636,10 @@ cudaError_t launch(const Geometry& g, const ScoredArgs& a, cudaStream_t st) {
 }  // namespace
 
 // Whether these kernels serve a call, or the mma.sync tiles.  A tile of 128 x 64 pairs takes about as long here as 64 x 51 there, a CTA's own time
-// 3.5 tiles (tensor memory, barriers, the first and last trips) and 1.5; and here a walk goes in whole tiles.  Fitted to, forward /
-// gradients, us, here and there, 8 heads:  16 x (50, 500, 500) 40 / 106 and 55 / 171;  4 x (128, 1024, 1024) 27 / 71 and 50 / 165;  64 x (100, 100,
-// 100) 39 / 101 and 37 / 120;  64 x (39, 55, 400) 74 / 177 and 51 / 168;  4 heads, 512 x (50, 50, 50) 107 / 252 and 57 / 182;  8 heads, 4 key
-// heads, all pairs, 64 x (17, 15, 173) 77 / 189 and 53 / 149, 4 x (27, 13, 898) 43 / 115 and 45 / 144.
+// 3.5 tiles (tensor memory, barriers, the first and last trips) and 1.5; and here a walk goes in whole tiles.  Fitted to calls without masks, forward /
+// gradients, us, here and there, 8 heads:  16 x (50, 500, 500) 40 / 113 and 55 / 187;  4 x (128, 1024, 1024) 27 / 75 and 50 / 187;  64 x (100, 100,
+// 100) 39 / 105 and 37 / 129;  64 x (39, 55, 400) 73 / 182 and 51 / 179;  4 heads, 512 x (50, 50, 50) 107 / 254 and 57 / 193;  8 heads, 4 key
+// heads, all pairs, 64 x (17, 15, 173) 76 / 201 and 53 / 162, 4 x (27, 13, 898) 43 / 125 and 45 / 169.
 bool scored_tc_preferred(const Geometry& g, const int (&rows)[3]) {
   if (g.hd != HD) return false;
   int64_t here = 0, there = 0;   // in quarters of a tile's time, 64 of them to a key

@@ -116,59 +116,65 @@ __device__ __forceinline__ void product_over_features(float (&c)[MT][NT][4], con
       }
   }
 }
-// o[mt][feature tile] += weights [own rows x partners] x partner rows, over NT tiles of 8 partners; weights as packed accumulators
-// w[mt][nt] = {row g, row g + 8}; `at`: lane_as_k.
+// Fragments of partner rows for products over NT tiles of 8 partners, as use(first of their weights' tiles, feature step, fragment); `at`: lane_as_k.
+template <int HD, int NT, typename Use>
+__device__ __forceinline__ void for_partner_rows(const LaneAt<HD>& at, uint32_t from, Use use) {
+#pragma unroll
+  for (int p = 0; p < (HD == 8 ? NT / 4 : NT / 2); ++p)
+#pragma unroll
+    for (int c = 0; c < (HD == 8 ? 1 : HD / 16); ++c) {
+      uint32_t f[4];
+      ldsm4_t(at.of[c] + from + (HD == 8 ? p * 512 : p * 32 * HD), f);
+      use(HD == 8 ? 4 * p : 2 * p, c, f);
+    }
+}
+// o[mt][feature tile] += weights [own rows x partners] x one such fragment; weights as packed accumulators w[mt][nt] = {row g, row g + 8}.
+template <int HD, int MT, int NT>
+__device__ __forceinline__ void add_product(float (&o)[MT][HD / 8][4], const uint32_t (&w)[MT][NT][2], int first, int c, const uint32_t (&f)[4]) {
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int nt = HD == 8 ? first + 2 * i : first;
+      const uint32_t a[4] = {w[m][nt][0], w[m][nt][1], w[m][nt + 1][0], w[m][nt + 1][1]};
+      float (&d)[4] = o[m][HD == 8 ? 0 : 2 * c + i];
+      mma16(d, a, f[2 * i], f[2 * i + 1], d);
+    }
+}
 template <int HD, int MT, int NT>
 __device__ __forceinline__ void product_over_partners(float (&o)[MT][HD / 8][4], const uint32_t (&w)[MT][NT][2], const LaneAt<HD>& at, uint32_t from) {
-  if constexpr (HD == 8) {
-#pragma unroll
-    for (int q = 0; q < NT / 4; ++q) {
-      uint32_t f[4];
-      ldsm4_t(at.of[0] + from + q * 512, f);
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int nt = 4 * q + 2 * i;
-          const uint32_t a[4] = {w[m][nt][0], w[m][nt][1], w[m][nt + 1][0], w[m][nt + 1][1]};
-          mma16(o[m][0], a, f[2 * i], f[2 * i + 1], o[m][0]);
-        }
-    }
-  } else {
-#pragma unroll
-    for (int p = 0; p < NT / 2; ++p)
-#pragma unroll
-      for (int c = 0; c < HD / 16; ++c) {
-        uint32_t f[4];
-        ldsm4_t(at.of[c] + from + p * 32 * HD, f);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const uint32_t a[4] = {w[m][2 * p][0], w[m][2 * p][1], w[m][2 * p + 1][0], w[m][2 * p + 1][1]};
-          mma16(o[m][2 * c], a, f[0], f[1], o[m][2 * c]);
-          mma16(o[m][2 * c + 1], a, f[2], f[3], o[m][2 * c + 1]);
-        }
-      }
-  }
+  for_partner_rows<HD, NT>(at, from, [&](int first, int c, const uint32_t (&f)[4]) { add_product<HD>(o, w, first, c, f); });
 }
 __device__ __forceinline__ void from_zero(int, int, float (&z)[4]) { z[0] = z[1] = z[2] = z[3] = 0.f; }
 
-// Two dots -> scores in base 2 less m; d *= derivative of the cap.  NEAR: tanh's arguments
+// Two dots -> scores in base 2 less m; bend = derivative of the cap, where there is one.  NEAR: tanh's arguments
 // are at most 1/4, and both are polynomials of the dot (quadratics of its square: 4 multiply-adds a score with the subtraction, 3 more for
 // the derivative; the FMA pipe is what these kernels fill first).
-template <bool CAP, bool BEND, bool NEAR> __device__ __forceinline__ float2 score_pair(float2 y, float2 m, float2& d, const ScoredArgs& a) {
+template <bool CAP, bool BEND, bool NEAR> __device__ __forceinline__ float2 score_pair(float2 y, float2 m, float2& bend, const ScoredArgs& a) {
   auto both = [](float v) { return make_float2(v, v); };
   m = make_float2(-m.x, -m.y);
   if constexpr (!CAP) {
     return __ffma2_rn(y, both(a.inner), m);
   } else if constexpr (NEAR) {
     const float2 z = __fmul2_rn(y, y);
-    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0])));
+    if constexpr (BEND) bend = __ffma2_rn(__ffma2_rn(z, both(a.near_b[2]), both(a.near_b[1])), z, both(a.near_b[0]));
     return __ffma2_rn(__ffma2_rn(__ffma2_rn(z, both(a.near_p[2]), both(a.near_p[1])), z, both(a.near_p[0])), y, m);
   } else {
     const float2 t = tanh_any2(__fmul2_rn(y, both(a.inner)));
-    if constexpr (BEND) d = __fmul2_rn(d, __ffma2_rn(make_float2(-t.x, -t.y), t, both(1.f)));
+    if constexpr (BEND) bend = __ffma2_rn(make_float2(-t.x, -t.y), t, both(1.f));
     return __ffma2_rn(t, both(a.outer), m);
   }
+}
+// What rounding a pair to bf16 leaves, in bf16: the two terms together hold 16 bits.
+__device__ __forceinline__ uint32_t pack_rest(float2 v, uint32_t rounded) {
+  float2 r;
+  unpack_bf16(rounded, r.x, r.y);
+  const float2 rest = __fadd2_rn(v, make_float2(-r.x, -r.y));
+  return ptx::pack_bf16(rest.x, rest.y);
+}
+template <bool CAP> __device__ __forceinline__ float2 times_bend(float2 v, float2 bend) {
+  if constexpr (CAP) return __fmul2_rn(v, bend);
+  return v;
 }
 // score -= slope2 * |own time - partner time| for a pair of partners
 __device__ __forceinline__ float2 bias_pair(float2 y, float2 times, float own, float slope2) {

@@ -7,8 +7,8 @@
 // (which rows, heads and features) never changes, so its offsets and its pair's frequency stay in registers.
 // Angles: position * frequency in turns as one double product, less its nearest integer: right to 2^-20 turns even at positions near
 // 2^31, where a float product keeps no bit of the phase; then sincospi of the float remainder.
-// Measured: gradients of 128 samples of (128, 1024, 1024), a quarter of the rows padding, q and k with 8 heads of 64, bf16: 1072 MB in 229 us, 4.7 TB/s, 0.73 of
-// the measured copy rate; 64 x (50, 500, 500), 8 heads of 8: 30 MB in 12 us.
+// Measured: gradients of 128 samples of (128, 1024, 1024), a quarter of the rows padding, q and k with 8 heads of 64, bf16: 1072 MB in 223 - 229 us, 4.8 TB/s, 0.74 of
+// the measured copy rate (lines that are asked for ahead are so for padded rows, too: an eighth of what is read there); 64 x (50, 500, 500), 8 heads of 8: 30 MB in 12 us.
 #include <math.h>
 
 #include <algorithm>

@@ -9,8 +9,8 @@
 //                  dealt out to groups of lanes, whose sums shuffles bring together at the end
 // Between the two the weights go through shared memory, partner-major; a warp reads only what its own lanes wrote, so that a tile costs
 // one barrier.  With 2 HD (forward), 3 HD (dq) and 4 HD (dk, dv) multiply-adds a pair the FMA pipe is the bound: 128 a clock and SM.
-// Measured: MIntRec's unmasked graph (8 samples of (30, 480, 230), half of the rows padding, 8 heads of 16, forward and gradients) 323 us, of which
-// the multiply-adds are 54; 30% of the FMA pipe's time, half of the issue slots (sums over halves, bias, addresses), the rest shared
+// Measured: MIntRec's unmasked graph (8 samples of (30, 480, 230), half of the rows padding, 8 heads of 16, forward and gradients) 305 - 349 us by
+// the lengths drawn, of which the multiply-adds are 54; 30% of the FMA pipe's time, half of the issue slots (sums over halves, bias, addresses), the rest shared
 // memory's latency and the last of two and a fraction waves of CTAs.  One CTA an SM (more registers, nothing spilled) 350 us; weights
 // exchanged by the whole CTA, which takes two more barriers a tile, 555 us.  Warps without a real row only fetch, and tiles without an open
 // pair are passed over (341 -> 323 us; 86 x (5, 12, 131), causal, 335 -> 288).

@@ -44,6 +44,25 @@ gsit_status gsit_rotary_bwd(const gsit_shape* shape, const gsit_rotary* rotary, 
                             int64_t dk_row_stride, void* dq_out, int64_t dq_out_row_stride, void* dk_out, int64_t dk_out_row_stride,
                             gsit_stream stream);
 
+/* Norms of the heads of q and k with the rotation above in the same pass:  y = R (x * r * gamma),  r = 1 / sqrt(mean(x^2) + eps)  over the
+ * head_dim features of each head; sections all 0: no rotation, and positions and base are not read.
+ *   q, k         as above (k may be NULL: only q), head_dim <= 256;  q_out, k_out may be q and k themselves
+ *   q_gamma, k_gamma  float [head_dim], one for all heads, or NULL (1);  eps <= 0 selects 1e-6
+ * Backward, from the gradients dq and dk of the results, with u = R^-1 dy, g = u * gamma and h = x * r:  dx = r * (g - h * mean(g h)),
+ * dgamma = sum over real rows and heads of u * h.  q and k are the inputs of the forward call: nothing else is kept for it.
+ *   dq_out, dk_out  like q and k, row strides of their own; may be dq and dk themselves
+ *   dq_gamma, dk_gamma  float [head_dim] or NULL (both or none)
+ *   workspace    gsit_head_norm_rotary_bwd_workspace(shape) bytes, 16-byte aligned; may be NULL when dq_gamma is */
+gsit_status gsit_head_norm_rotary_fwd(const gsit_shape* shape, const gsit_rotary* rotary, float eps, const void* q, int64_t q_row_stride,
+                                      const float* q_gamma, const void* k, int64_t k_row_stride, const float* k_gamma, void* q_out,
+                                      int64_t q_out_row_stride, void* k_out, int64_t k_out_row_stride, gsit_stream stream);
+size_t gsit_head_norm_rotary_bwd_workspace(const gsit_shape* shape);   /* (size_t)-1 for an invalid shape */
+gsit_status gsit_head_norm_rotary_bwd(const gsit_shape* shape, const gsit_rotary* rotary, float eps, const void* q, int64_t q_row_stride,
+                                      const float* q_gamma, const void* k, int64_t k_row_stride, const float* k_gamma, const void* dq,
+                                      int64_t dq_row_stride, const void* dk, int64_t dk_row_stride, void* dq_out, int64_t dq_out_row_stride,
+                                      void* dk_out, int64_t dk_out_row_stride, float* dq_gamma, float* dk_gamma, void* workspace,
+                                      size_t workspace_bytes, gsit_stream stream);
+
 /* LayerNorm over rows of d_model <= 8192 features:  y = (x - mean) * rstd * gamma + beta,  rstd = 1 / sqrt(var + eps).
  *   shape        batch, seg_len, valid_len, d_model are read (heads, dtype and the rest are not)
  *   x            [B, L, d] of x_dtype, row stride in elements;  y [B, L, d] of y_dtype

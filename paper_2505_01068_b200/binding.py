@@ -48,7 +48,7 @@ EXPORTS = ("gsit_im_qkv_proj", "gsit_im_attention_fwd", "gsit_im_layer_fwd", "gs
            "gsit_stack_head_fwd", "gsit_im_layer_pair_fwd",
            "gsit_plan_rows", "gsit_pack_rows", "gsit_unpack_rows", "gsit_plan_pack_rows", "gsit_plan_pack_map_rows",
            "gsit_im_encoder_fwd", "gsit_encoder_runs_chained", "gsit_im_layer_scatter_fwd", "gsit_layer_scatters", "gsit_attention_uses_workspace",
-           "gsit_rotary_fwd", "gsit_rotary_bwd", "gsit_layer_norm_fwd", "gsit_layer_norm_bwd", "gsit_layer_norm_bwd_workspace",
+           "gsit_rotary_fwd", "gsit_rotary_bwd", "gsit_head_norm_rotary_fwd", "gsit_head_norm_rotary_bwd", "gsit_head_norm_rotary_bwd_workspace", "gsit_layer_norm_fwd", "gsit_layer_norm_bwd", "gsit_layer_norm_bwd_workspace",
            "gsit_im_scored_attention_fwd", "gsit_im_scored_attention_bwd", "gsit_scored_attention_fwd_workspace", "gsit_scored_attention_bwd_workspace")
 STATIC_SCRATCH_BYTES = 4 << 20
 KERNEL_ATTENTION, KERNEL_LINEAR, KERNEL_LAYERNORM = 0, 1, 2
@@ -314,6 +314,21 @@ def rotary_fwd(q, k, positions, sections, seg_len, valid_len=None, base=10000.0,
 def rotary_bwd(dq, dk, positions, sections, seg_len, valid_len=None, base=10000.0, interleaved=False, out_q=None, out_k=None):
     """Gradients of rotary_fwd's inputs from those of its results (the rotation by the opposite angles)."""
     return native().rotary(dq, dk, positions, sections, seg_len, valid_len, base, interleaved, out_q, out_k, True)
+
+
+def head_norm_rotary_fwd(q, k, q_gamma=None, k_gamma=None, positions=None, sections=None, seg_len=None, valid_len=None, base=10000.0, interleaved=False,
+                         eps=1e-6, out_q=None, out_k=None):
+    """Every head x of q [B, L, H, hd] and k [B, L, Hk, hd] (or None) as x * gamma / sqrt(mean(x^2) + eps), q_gamma and k_gamma float32 [hd] or None (1), then
+    rotated as rotary_fwd does (sections None: not at all).  hd <= 256.  Returns (q', k') or q'; out_q may be q (in place)."""
+    return native().head_norm_fwd(q, k, q_gamma, k_gamma, positions, sections, seg_len, valid_len, base, interleaved, eps, out_q, out_k)
+
+
+def head_norm_rotary_bwd(dq, dk, q, k, q_gamma=None, k_gamma=None, positions=None, sections=None, seg_len=None, valid_len=None, base=10000.0, interleaved=False,
+                         eps=1e-6, want_params=True, out_q=None, out_k=None, workspace=None):
+    """(dq', dk', dq_gamma, dk_gamma) of head_norm_rotary_fwd called with the same q and k, from the gradients dq and dk of its results; without k (dq',
+    dq_gamma), and without want_params the gradients of q and k alone.  out_q may be dq (in place)."""
+    return native().head_norm_bwd(dq, dk, q, k, q_gamma, k_gamma, positions, sections, seg_len, valid_len, base, interleaved, eps, out_q, out_k, want_params,
+                                  workspace)
 
 
 def layer_norm_fwd(x, gamma=None, beta=None, seg_len=None, valid_len=None, eps=1e-5, out_dtype=None, want_stats=False, out=None):

@@ -1,5 +1,7 @@
 // What the operators of gsit_ops.h share: row vectors of either type, geometry checks, launch entry points.
 #pragma once
+#include <math.h>
+
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -71,6 +73,34 @@ struct RotaryCall {
   double base;
 };
 cudaError_t launch_rotary(const Geometry& g, int dtype, const RotaryCall& c, cudaStream_t st);
+// Frequencies of the pairs, base^(-p / pairs), in turns a position.  They are products of those of p's powers of two (six doubles at most):
+// 32 calls of pow are a fifth of a small call.
+inline void rotary_turns(double base, int pairs, double (&turns)[MAX_ROTARY_PAIRS]) {
+  double power[MAX_ROTARY_PAIRS];
+  for (int p = 0; p < pairs; ++p) {
+    power[p] = (p & (p - 1)) != 0 ? power[p & (p - 1)] * power[p & -p] : pow(base, -(double)p / pairs);
+    turns[p] = power[p] / (2.0 * M_PI);
+  }
+}
+
+// head_norm.cu
+constexpr int MAX_NORM_HEAD = 256;
+struct HeadNormCall {
+  const void *x[2], *dy[2];              // q and k; backward: gradients of the results
+  void* out[2];
+  int64_t ldx[2], lddy[2], ldo[2];       // elements between rows
+  const float* gamma[2];
+  int heads[2];                          // (0: no k)
+  const int32_t* positions;
+  int64_t axis_stride, batch_stride;
+  int sections[3];                       // all 0: no rotation
+  bool interleaved, backward;
+  double base;
+  float eps;
+  float *dgamma[2], *partial;            // partial null: gradients of the rows alone
+};
+cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c, cudaStream_t st);
+size_t head_norm_scratch(const Geometry& g);
 
 // layer_norm.cu
 constexpr int MAX_NORM_WIDTH = 8192;

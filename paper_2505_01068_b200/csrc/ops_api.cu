@@ -55,6 +55,60 @@ gsit_status rotary(const gsit_shape* shape, const gsit_rotary* r, const void* q,
   return status_of(launch_rotary(g, shape->dtype, c, static_cast<cudaStream_t>(stream)));
 }
 
+// Norms of heads with the rotation, or (dq != nullptr) their gradients: the checks of both.
+struct HeadRows {
+  const void* p;
+  int64_t ld;
+};
+gsit_status head_norm(const gsit_shape* shape, const gsit_rotary* r, float eps, const HeadRows (&x)[2], const float* const (&gamma)[2], const HeadRows* dy,
+                      const HeadRows (&out)[2], float* const (&dgamma)[2], void* workspace, size_t workspace_bytes, gsit_stream stream) {
+  if (shape == nullptr) return GSIT_ERR_INVALID_ARG;
+  const gsit_shape rows = any_phase(*shape);
+  Geometry g;
+  const gsit_status st = padded_geometry(&rows, &g);
+  if (st != GSIT_OK) return st;
+  if (r == nullptr || x[0].p == nullptr || (eps > 0.f && !isfinite(eps)) || eps != eps) return GSIT_ERR_INVALID_ARG;
+  const bool has_k = x[1].p != nullptr;
+  HeadNormCall c = {};
+  int64_t pairs = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (r->sections[i] < 0) return GSIT_ERR_INVALID_ARG;
+    pairs += c.sections[i] = r->sections[i];
+  }
+  const int kv_heads = r->kv_heads == 0 ? g.heads : r->kv_heads;
+  if (2 * pairs > g.hd || kv_heads < 1) return GSIT_ERR_INVALID_ARG;
+  if (pairs > 0 && (r->positions == nullptr || !aligned(r->positions, 4) || !(r->base > 0.0) || r->axis_stride < 0 || r->batch_stride < 0)) return GSIT_ERR_INVALID_ARG;
+  if (pairs > MAX_ROTARY_PAIRS || g.hd > MAX_NORM_HEAD || (int64_t)(g.heads + kv_heads) * g.hd > 65536) return GSIT_ERR_UNSUPPORTED;
+  const size_t es = element_size(shape->dtype);
+  for (int i = 0; i < 2; ++i) {
+    const bool here = i == 0 || has_k;
+    for (const HeadRows* m : {&x[i], dy == nullptr ? &x[i] : &dy[i], &out[i]})
+      if (here ? m->p == nullptr || m->ld < (int64_t)(i == 0 ? g.heads : kv_heads) * g.hd || !aligned(m->p, es) : m->p != nullptr) return GSIT_ERR_INVALID_ARG;
+    if (!aligned(gamma[i], 4) || !aligned(dgamma[i], 4) || (!here && dgamma[i] != nullptr)) return GSIT_ERR_INVALID_ARG;
+    c.heads[i] = !here ? 0 : i == 0 ? g.heads : kv_heads;
+    c.x[i] = x[i].p; c.ldx[i] = x[i].ld;
+    if (dy != nullptr) { c.dy[i] = dy[i].p; c.lddy[i] = dy[i].ld; }
+    c.out[i] = const_cast<void*>(out[i].p); c.ldo[i] = out[i].ld;
+    c.gamma[i] = gamma[i];
+    c.dgamma[i] = dgamma[i];
+  }
+  if (has_k && (dgamma[0] == nullptr) != (dgamma[1] == nullptr)) return GSIT_ERR_INVALID_ARG;
+  if (dgamma[0] != nullptr) {
+    if (workspace == nullptr || workspace_bytes < head_norm_scratch(g)) return GSIT_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return GSIT_ERR_INVALID_ARG;
+    c.partial = static_cast<float*>(workspace);
+  }
+  if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
+  c.positions = r->positions;
+  c.axis_stride = r->axis_stride;
+  c.batch_stride = r->batch_stride;
+  c.interleaved = r->interleaved != 0;
+  c.backward = dy != nullptr;
+  c.base = r->base;
+  c.eps = eps > 0.f ? eps : 1e-6f;
+  return status_of(launch_head_norm(g, shape->dtype, c, static_cast<cudaStream_t>(stream)));
+}
+
 bool norm_type(int32_t t) { return t == GSIT_F32 || t == GSIT_BF16; }
 gsit_status norm_geometry(const gsit_shape* shape, Geometry* g) {
   if (shape == nullptr) return GSIT_ERR_INVALID_ARG;
@@ -147,6 +201,30 @@ gsit_status gsit_rotary_bwd(const gsit_shape* shape, const gsit_rotary* rotary_,
                             int64_t dk_row_stride, void* dq_out, int64_t dq_out_row_stride, void* dk_out, int64_t dk_out_row_stride,
                             gsit_stream stream) {
   return rotary(shape, rotary_, dq, dq_row_stride, dk, dk_row_stride, dq_out, dq_out_row_stride, dk_out, dk_out_row_stride, true, stream);
+}
+
+gsit_status gsit_head_norm_rotary_fwd(const gsit_shape* shape, const gsit_rotary* rotary_, float eps, const void* q, int64_t q_row_stride,
+                                      const float* q_gamma, const void* k, int64_t k_row_stride, const float* k_gamma, void* q_out,
+                                      int64_t q_out_row_stride, void* k_out, int64_t k_out_row_stride, gsit_stream stream) {
+  return head_norm(shape, rotary_, eps, {{q, q_row_stride}, {k, k_row_stride}}, {q_gamma, k_gamma}, nullptr, {{q_out, q_out_row_stride}, {k_out, k_out_row_stride}},
+                   {nullptr, nullptr}, nullptr, 0, stream);
+}
+
+size_t gsit_head_norm_rotary_bwd_workspace(const gsit_shape* shape) {
+  if (shape == nullptr) return (size_t)-1;
+  const gsit_shape rows = any_phase(*shape);
+  Geometry g;
+  return padded_geometry(&rows, &g) == GSIT_OK && g.hd <= MAX_NORM_HEAD ? head_norm_scratch(g) : (size_t)-1;
+}
+
+gsit_status gsit_head_norm_rotary_bwd(const gsit_shape* shape, const gsit_rotary* rotary_, float eps, const void* q, int64_t q_row_stride,
+                                      const float* q_gamma, const void* k, int64_t k_row_stride, const float* k_gamma, const void* dq,
+                                      int64_t dq_row_stride, const void* dk, int64_t dk_row_stride, void* dq_out, int64_t dq_out_row_stride,
+                                      void* dk_out, int64_t dk_out_row_stride, float* dq_gamma, float* dk_gamma, void* workspace,
+                                      size_t workspace_bytes, gsit_stream stream) {
+  const HeadRows dy[2] = {{dq, dq_row_stride}, {dk, dk_row_stride}};
+  return head_norm(shape, rotary_, eps, {{q, q_row_stride}, {k, k_row_stride}}, {q_gamma, k_gamma}, dy, {{dq_out, dq_out_row_stride}, {dk_out, dk_out_row_stride}},
+                   {dq_gamma, dk_gamma}, workspace, workspace_bytes, stream);
 }
 
 gsit_status gsit_layer_norm_fwd(const gsit_shape* shape, int32_t x_dtype, const void* x, int64_t x_row_stride, const float* gamma,

@@ -9,8 +9,6 @@
 // 2^31, where a float product keeps no bit of the phase; then sincospi of the float remainder.
 // Measured: gradients of 128 samples of (128, 1024, 1024), a quarter of the rows padding, q and k with 8 heads of 64, bf16: 1072 MB in 223 - 229 us, 4.8 TB/s, 0.74 of
 // the measured copy rate (lines that are asked for ahead are so for padded rows, too: an eighth of what is read there); 64 x (50, 500, 500), 8 heads of 8: 30 MB in 12 us.
-#include <math.h>
-
 #include <algorithm>
 
 #include "ops.cuh"
@@ -250,12 +248,7 @@ cudaError_t launch_rotary(const Geometry& g, int dtype, const RotaryCall& c, cud
   a.axis2 = c.sections[0] + c.sections[1];
   a.adjacent = c.interleaved;
   a.q_heads = c.heads[0];
-  // base^(-p/n) as the product of those of p's powers of two (a product of six doubles at most): 32 calls of pow are a fifth of a small call
-  double power[MAX_ROTARY_PAIRS];
-  for (int p = 0; p < a.pairs; ++p) {
-    power[p] = (p & (p - 1)) != 0 ? power[p & (p - 1)] * power[p & -p] : pow(c.base, -(double)p / a.pairs);
-    a.turns[p] = power[p] / (2.0 * M_PI);
-  }
+  rotary_turns(c.base, a.pairs, a.turns);
   wide = wide && 2 * a.pairs == g.hd && g.hd % piece == 0;
   const Form form = !wide ? SCALAR : c.interleaved ? ADJACENT : a.pairs % piece == 0 ? SPLIT : g.hd == piece ? HEAD : SCALAR;
   a.head_units = form == SPLIT ? a.pairs / piece : form == SCALAR ? g.hd - a.pairs : g.hd / piece;

@@ -622,6 +622,8 @@ PyMethodDef methods[] = {def<init, 1>("init"),
                          def<stack_head_fwd, 6>("stack_head_fwd"),
                          def<stack_forward, 11>("stack_forward"),
                          def<rotary, 11>("rotary"),
+                         def<head_norm<false>, 13>("head_norm_fwd"),
+                         def<head_norm<true>, 17>("head_norm_bwd"),
                          def<layer_norm_fwd, 9>("layer_norm_fwd"),
                          def<layer_norm_bwd, 11>("layer_norm_bwd"),
                          def<scored_fwd, 17>("scored_fwd"),

@@ -45,22 +45,10 @@ void require_length(const gsit_shape& s, int64_t L) {
   require((int64_t)s.seg_len[0] + s.seg_len[1] + s.seg_len[2] == L, "seg_len adds up to the length of the rows");
 }
 
-// q, k (or None), positions, sections, seg_len, valid_len, base, interleaved, out_q, out_k, backward
-PyObject* rotary(PyObject* const* a) {
-  const at::Tensor &q = tensor(a[0]), &pos = tensor(a[2]);
-  const at::Tensor *k = opt_tensor(a[1]), *valid = opt_tensor(a[5]), *out_q = opt_tensor(a[8]), *out_k = opt_tensor(a[9]);
-  const int64_t ldq = head_rows(q, "q: [B, L, H, hd] on the device, heads contiguous, rows evenly spaced");
-  const int64_t B = q.size(0), L = q.size(1), H = q.size(2), hd = q.size(3);
-  int64_t ldk = 0, HK = 0;
-  if (k != nullptr) {
-    ldk = head_rows(*k, "k: [B, L, H, hd] on the device, heads contiguous, rows evenly spaced");
-    HK = k->size(2);
-    require(k->size(0) == B && k->size(1) == L && k->size(3) == hd && k->scalar_type() == q.scalar_type(), "q and k share batch, length, head width and dtype");
-  }
-  const gsit_shape s = make_shape(B, a[4], H * hd, H, valid, dtype_code(q), GSIT_PHASE_INTRA, 0, 0.0);
-  require_length(s, L);
+// Positions (may be null where none are read) and how many pairs belong to each axis.
+gsit_rotary read_rotary(const at::Tensor* pos, PyObject* of_axis, int64_t B, int64_t L, int64_t hd, int64_t HK) {
   gsit_rotary r = {};
-  PyObject* sections = PySequence_Fast(a[3], "sections must be a sequence of one to three numbers of pairs");
+  PyObject* sections = PySequence_Fast(of_axis, "sections must be a sequence of one to three numbers of pairs");
   if (sections == nullptr) throw PyFail{};
   const Py_ssize_t axes = PySequence_Fast_GET_SIZE(sections);
   bool read = axes >= 1 && axes <= 3;
@@ -75,15 +63,34 @@ PyObject* rotary(PyObject* const* a) {
   }
   Py_DECREF(sections);
   require(read, "sections: one to three numbers of pairs, none negative or above head_dim");
-  require(pos.is_cuda() && pos.scalar_type() == at::kInt && (pos.dim() == 2 || pos.dim() == 3) && pos.size(0) == axes && pos.size(-1) == L &&
-              (L == 1 || pos.stride(-1) == 1), "positions: int32 [axes, B, L] or [axes, L] on the device");
-  require(pos.dim() == 2 || pos.size(1) == B || pos.size(1) == 1, "positions: one row per sample, or one for all");
-  r.positions = static_cast<const int32_t*>(pos.data_ptr());
-  r.axis_stride = axes > 1 ? pos.stride(0) : 0;
-  r.batch_stride = pos.dim() == 3 && pos.size(1) > 1 ? pos.stride(1) : 0;
+  r.kv_heads = (int32_t)HK;
+  if (pos == nullptr) return r;
+  require(pos->is_cuda() && pos->scalar_type() == at::kInt && (pos->dim() == 2 || pos->dim() == 3) && pos->size(0) == axes && pos->size(-1) == L &&
+              (L == 1 || pos->stride(-1) == 1), "positions: int32 [axes, B, L] or [axes, L] on the device");
+  require(pos->dim() == 2 || pos->size(1) == B || pos->size(1) == 1, "positions: one row per sample, or one for all");
+  r.positions = static_cast<const int32_t*>(pos->data_ptr());
+  r.axis_stride = axes > 1 ? pos->stride(0) : 0;
+  r.batch_stride = pos->dim() == 3 && pos->size(1) > 1 ? pos->stride(1) : 0;
+  return r;
+}
+
+// q, k (or None), positions, sections, seg_len, valid_len, base, interleaved, out_q, out_k, backward
+PyObject* rotary(PyObject* const* a) {
+  const at::Tensor &q = tensor(a[0]), &pos = tensor(a[2]);
+  const at::Tensor *k = opt_tensor(a[1]), *valid = opt_tensor(a[5]), *out_q = opt_tensor(a[8]), *out_k = opt_tensor(a[9]);
+  const int64_t ldq = head_rows(q, "q: [B, L, H, hd] on the device, heads contiguous, rows evenly spaced");
+  const int64_t B = q.size(0), L = q.size(1), H = q.size(2), hd = q.size(3);
+  int64_t ldk = 0, HK = 0;
+  if (k != nullptr) {
+    ldk = head_rows(*k, "k: [B, L, H, hd] on the device, heads contiguous, rows evenly spaced");
+    HK = k->size(2);
+    require(k->size(0) == B && k->size(1) == L && k->size(3) == hd && k->scalar_type() == q.scalar_type(), "q and k share batch, length, head width and dtype");
+  }
+  const gsit_shape s = make_shape(B, a[4], H * hd, H, valid, dtype_code(q), GSIT_PHASE_INTRA, 0, 0.0);
+  require_length(s, L);
+  gsit_rotary r = read_rotary(&pos, a[3], B, L, hd, HK);
   r.base = as_float(a[6]);
   r.interleaved = as_bool(a[7]);
-  r.kv_heads = (int32_t)HK;
   at::Tensor mq, mk;
   auto result = [&](const at::Tensor* given, const at::Tensor& like, at::Tensor& made) {
     if (given == nullptr) made = empty(like.sizes(), like.scalar_type(), like.device());
@@ -101,6 +108,89 @@ PyObject* rotary(PyObject* const* a) {
     st = call(&s, &r, q.data_ptr(), ldq, ptr(k), ldk, mq.data_ptr(), ldqo, k == nullptr ? nullptr : mk.data_ptr(), ldko, stream());
   }
   check(st, "gsit_rotary");
+  if (k == nullptr) return THPVariable_Wrap(std::move(mq));
+  return pack({mq, mk});
+}
+
+// Everything lies on the current device: kernels run there, and their pointers are not looked at.
+void here(std::initializer_list<const at::Tensor*> ts) {
+  const int dev = c10::cuda::current_device();
+  for (const at::Tensor* t : ts) require(t == nullptr || (t->is_cuda() && t->device().index() == dev), "tensors on the current device");
+}
+const float* gamma_of(const at::Tensor* t, int64_t hd) { return float_vector(t, hd, "gamma: contiguous float32 [head_dim] on the device"); }
+
+const char* const HEAD_ROWS = "[B, L, H, hd] on the device, heads contiguous, rows evenly spaced";
+
+// q, k (or None), q_gamma, k_gamma, positions, sections, seg_len, valid_len, base, interleaved, eps, out_q, out_k
+// and backward: dq, dk in front, want_params, workspace behind
+template <bool BWD> PyObject* head_norm(PyObject* const* args) {
+  PyObject* const* a = args + (BWD ? 2 : 0);
+  const at::Tensor& q = tensor(a[0]);
+  const at::Tensor *k = opt_tensor(a[1]), *q_gamma = opt_tensor(a[2]), *k_gamma = opt_tensor(a[3]), *pos = opt_tensor(a[4]), *valid = opt_tensor(a[7]);
+  const at::Tensor *out_q = opt_tensor(a[11]), *out_k = opt_tensor(a[12]);
+  const at::Tensor *dq = BWD ? &tensor(args[0]) : nullptr, *dk = BWD ? opt_tensor(args[1]) : nullptr, *ws = BWD ? scratch(a[14]) : nullptr;
+  here({&q, k, q_gamma, k_gamma, pos, valid, out_q, out_k, dq, dk, ws});
+  const int64_t ldq = head_rows(q, HEAD_ROWS), ldk = k == nullptr ? 0 : head_rows(*k, HEAD_ROWS);
+  const int64_t B = q.size(0), L = q.size(1), H = q.size(2), hd = q.size(3), HK = k == nullptr ? 0 : k->size(2);
+  require(k == nullptr || (k->size(0) == B && k->size(1) == L && k->size(3) == hd && k->scalar_type() == q.scalar_type()),
+          "q and k share batch, length, head width and dtype");
+  require(k != nullptr || (out_k == nullptr && k_gamma == nullptr && dk == nullptr), "without k there is nothing for it");
+  const gsit_shape s = make_shape(B, a[6], H * hd, H, valid, dtype_code(q), GSIT_PHASE_INTRA, 0, 0.0);
+  require_length(s, L);
+  gsit_rotary r = {};
+  r.kv_heads = (int32_t)HK;
+  if (a[5] != Py_None) {
+    r = read_rotary(pos, a[5], B, L, hd, HK);
+    require(pos != nullptr || r.sections[0] + r.sections[1] + r.sections[2] == 0, "positions: int32 [axes, B, L] or [axes, L] on the device");
+  } else {
+    require(pos == nullptr, "positions are read with sections only");
+  }
+  r.base = as_float(a[8]);
+  r.interleaved = as_bool(a[9]);
+  const float eps = (float)as_float(a[10]);
+  const float *gq = gamma_of(q_gamma, hd), *gk = gamma_of(k_gamma, hd);
+  int64_t lddq = 0, lddk = 0;
+  if constexpr (BWD) {
+    require(dq->sizes() == q.sizes() && dq->scalar_type() == q.scalar_type() && (dk == nullptr) == (k == nullptr) &&
+                (k == nullptr || (dk->sizes() == k->sizes() && dk->scalar_type() == q.scalar_type())), "gradients: shape and dtype of q and k");
+    lddq = head_rows(*dq, HEAD_ROWS);
+    lddk = dk == nullptr ? 0 : head_rows(*dk, HEAD_ROWS);
+  }
+  at::Tensor mq, mk, gam_q, gam_k, made_ws;
+  auto result = [&](const at::Tensor* given, const at::Tensor& like, at::Tensor& made) {
+    if (given == nullptr) made = empty(like.sizes(), like.scalar_type(), like.device());
+    else {
+      require(given->sizes() == like.sizes() && given->scalar_type() == like.scalar_type(), "results: shape and dtype of the inputs");
+      made = *given;
+    }
+    return head_rows(made, HEAD_ROWS);
+  };
+  const int64_t ldqo = result(out_q, q, mq), ldko = k == nullptr ? 0 : result(out_k, *k, mk);
+  void* ko = k == nullptr ? nullptr : mk.data_ptr();
+  const bool params = BWD && as_bool(a[13]);
+  if (params) {
+    gam_q = empty({hd}, at::kFloat, q.device());
+    if (k != nullptr) gam_k = empty({hd}, at::kFloat, q.device());
+    if (ws == nullptr) {
+      const size_t need = gsit_head_norm_rotary_bwd_workspace(&s);
+      if (need == (size_t)-1) check(GSIT_ERR_UNSUPPORTED, "gsit_head_norm_rotary_bwd_workspace");
+      made_ws = empty({(int64_t)need}, at::kByte, q.device());
+      ws = &made_ws;
+    }
+  }
+  gsit_status st;
+  {
+    NoGil n;
+    if constexpr (!BWD)
+      st = gsit_head_norm_rotary_fwd(&s, &r, eps, q.data_ptr(), ldq, gq, ptr(k), ldk, gk, mq.data_ptr(), ldqo, ko, ldko, stream());
+    else
+      st = gsit_head_norm_rotary_bwd(&s, &r, eps, q.data_ptr(), ldq, gq, ptr(k), ldk, gk, dq->data_ptr(), lddq, ptr(dk), lddk, mq.data_ptr(), ldqo, ko, ldko,
+                                     params ? static_cast<float*>(gam_q.data_ptr()) : nullptr, params && k != nullptr ? static_cast<float*>(gam_k.data_ptr()) : nullptr,
+                                     ptr(ws), ws == nullptr ? 0 : (size_t)ws->nbytes(), stream());
+  }
+  check(st, BWD ? "gsit_head_norm_rotary_bwd" : "gsit_head_norm_rotary_fwd");
+  if (params && k == nullptr) return pack({mq, gam_q});
+  if (params) return pack({mq, mk, gam_q, gam_k});
   if (k == nullptr) return THPVariable_Wrap(std::move(mq));
   return pack({mq, mk});
 }

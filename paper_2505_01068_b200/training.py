@@ -46,6 +46,24 @@ class _Rotary(torch.autograd.Function):
         return dq, dk, None, None, None, None, None, None
 
 
+class _HeadNormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_gamma, k_gamma, positions, sections, seg_len, valid_len, base, interleaved, eps):
+        ctx.save_for_backward(q, k, q_gamma, k_gamma, positions, valid_len)
+        ctx.args = (sections, seg_len, base, interleaved, eps)
+        return B.head_norm_rotary_fwd(q, k, q_gamma, k_gamma, positions, sections, seg_len, valid_len, base, interleaved, eps)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk=None):
+        q, k, q_gamma, k_gamma, positions, valid_len = ctx.saved_tensors
+        sections, seg_len, base, interleaved, eps = ctx.args
+        got = B.head_norm_rotary_bwd(dq.contiguous(), None if dk is None else dk.contiguous(), q, k, q_gamma, k_gamma, positions, sections, seg_len, valid_len, base,
+                                     interleaved, eps)
+        dq, dk, dq_gamma, dk_gamma = (got[0], None, got[1], None) if k is None else got
+        return dq, dk, None if q_gamma is None else dq_gamma, None if k_gamma is None else dk_gamma, None, None, None, None, None, None, None
+
+
 class _ScoredAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, seg_len, valid_len, rule):
@@ -76,6 +94,11 @@ def rotary(q, k, positions, sections, seg_len, valid_len=None, base=10000.0, int
     return _Rotary.apply(q, k, positions, sections, seg_len, valid_len, base, interleaved)
 
 
+def head_norm_rotary(q, k, q_gamma=None, k_gamma=None, positions=None, sections=None, seg_len=None, valid_len=None, base=10000.0, interleaved=False, eps=1e-6):
+    """Differentiable head_norm_rotary_fwd (k None: q' alone): gradients of q, k and both weights."""
+    return _HeadNormRotary.apply(q, k, q_gamma, k_gamma, positions, sections, seg_len, valid_len, base, interleaved, eps)
+
+
 def im_scored_attention(q, k, v, seg_len, valid_len=None, **rule):
     """Differentiable im_scored_attention_fwd; rule: phase, custom_mask, scale, softcap, slopes, times, documents, causal, prefix (slopes,
     times and prefix are constants: tensors that ask for a gradient are refused, and so is q_len, which has no backward pass)."""
@@ -91,10 +114,11 @@ class ImEncoderLayer(torch.nn.Module):
     of `dtype`:
         h = LN1(x);  q, k, v = h W_qkv^T;  q, k rotated by `positions`;  y1 = x + attention(q, k, v) W_o^T;
         y = y1 + relu(LN2(y1) W_1^T) W_2^T
-    sections: pairs of a head that each axis of positions rotates (None: no positions).  Padded rows of the result are +0, and nothing
+    sections: pairs of a head that each axis of positions rotates (None: no positions).  qk_norm: heads of q and k are normalised, with weights of
+    their own, before they are rotated.  Padded rows of the result are +0, and nothing
     that stands in padded rows of the input reaches the result or a gradient."""
 
-    def __init__(self, d_model, heads, seg_len, d_ff=None, kv_heads=None, sections=None, base=10000.0, dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, d_model, heads, seg_len, d_ff=None, kv_heads=None, sections=None, base=10000.0, dtype=torch.bfloat16, device="cuda", qk_norm=False):
         super().__init__()
         kv_heads = heads if kv_heads is None else kv_heads
         self.heads, self.kv_heads, self.hd, self.seg_len, self.sections, self.base, self.dtype = heads, kv_heads, d_model // heads, tuple(seg_len), sections, base, dtype
@@ -107,17 +131,23 @@ class ImEncoderLayer(torch.nn.Module):
         for name in ("ln1", "ln2"):
             setattr(self, name + "_g", torch.nn.Parameter(torch.ones(d_model, device=device)))
             setattr(self, name + "_b", torch.nn.Parameter(torch.zeros(d_model, device=device)))
+        self.qk_norm = qk_norm
+        if qk_norm:
+            self.q_g = torch.nn.Parameter(torch.ones(self.hd, device=device))
+            self.k_g = torch.nn.Parameter(torch.ones(self.hd, device=device))
         # of every row its place in its segment, and that segment: on the device once, so that a captured step has nothing to copy
         self.register_buffer("place", torch.cat([torch.arange(n, device=device) for n in self.seg_len]), persistent=False)
         self.register_buffer("segment", torch.cat([torch.full((n,), s, device=device) for s, n in enumerate(self.seg_len)]), persistent=False)
 
     def project(self, x, valid_len=None, positions=None, seg_len=None):
-        """(q, k, v) [B, L, H, hd] of the layer: norm, shared projection, rotation."""
+        """(q, k, v) [B, L, H, hd] of the layer: norm, shared projection, norms of the heads where there are any, rotation."""
         seg_len = self.seg_len if seg_len is None else seg_len
         h = layer_norm(x, self.ln1_g, self.ln1_b, seg_len, valid_len, out_dtype=self.dtype)
         qkv = (h @ self.w_qkv.to(self.dtype).t()).unflatten(-1, (self.heads + 2 * self.kv_heads, self.hd))
         q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), dim=2)
-        if self.sections is not None:
+        if self.qk_norm:
+            q, k = head_norm_rotary(q, k, self.q_g, self.k_g, positions if self.sections is not None else None, self.sections, seg_len, valid_len, self.base)
+        elif self.sections is not None:
             q, k = rotary(q, k, positions, self.sections, seg_len, valid_len, self.base)
         return q, k, v
 

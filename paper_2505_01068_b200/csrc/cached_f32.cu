@@ -1,0 +1,6 @@
+// Attention over a stream's cache, float rows (see cached_attn.cuh).
+#include "cached_attn.cuh"
+
+namespace gsit {
+cudaError_t launch_cached_f32(const Geometry& g, CachedArgs& a, cudaStream_t st) { return launch_kind<float>(g, a, st); }
+}  // namespace gsit

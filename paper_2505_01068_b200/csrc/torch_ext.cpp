@@ -18,6 +18,7 @@
 
 #include "gsit.h"
 #include "gsit_ops.h"
+#include "gsit_stream.h"
 
 namespace {
 
@@ -582,6 +583,8 @@ PyObject* stack_forward(PyObject* const* a) {
 
 // ---- training operators ----
 #include "torch_ops.h"
+// ---- a stream's cache ----
+#include "torch_stream.h"
 
 // ---- module ----
 template <PyObject* (*F)(PyObject* const*), int N>
@@ -628,6 +631,10 @@ PyMethodDef methods[] = {def<init, 1>("init"),
                          def<layer_norm_bwd, 11>("layer_norm_bwd"),
                          def<scored_fwd, 17>("scored_fwd"),
                          def<scored_bwd, 19>("scored_bwd"),
+                         def<cache_plan, 9>("cache_plan"),
+                         def<cache_append, 16>("cache_append"),
+                         def<cache_read, 14>("cache_read"),
+                         def<cached_attention, 24>("cached_attention"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -43,7 +43,7 @@ typedef struct gsit_cache {
   int32_t blocks;                  /* entries of a segment's row in tables: it can grow to 32 * blocks positions */
   void *keys, *values;             /* DEVICE int8 or e4m3 [pages][kv_heads][32 * head_dim], 16-byte aligned */
   float *key_scale, *value_scale;  /* DEVICE float [pages][kv_heads] */
-  float* times;                    /* DEVICE float [pages][32] or NULL: the moment of each position */
+  float* times;                    /* DEVICE float [pages][32], 16-byte aligned, or NULL: the moment of each position */
   void *open_keys, *open_values;   /* DEVICE dtype [batch][3][2][kv_heads][32][head_dim], 16-byte aligned */
   int32_t* tables;                 /* DEVICE int32 [batch][3][blocks]: page of each block, -1 where there is none */
   int32_t* lengths;                /* DEVICE int32 [batch][3]: positions held */

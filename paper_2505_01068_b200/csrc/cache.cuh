@@ -54,11 +54,11 @@ struct CachedArgs {
   RowTimes times;                      // null: the index inside the segment
   int group, rows, causal;             // rows: query rows of a key head, L * group
   float softcap, inner, outer;         // score = outer * tanh(inner * dot) or inner * dot, base 2
-  int split;                           // CTAs that share a (stream, key head, tile of rows)
-  float* parts;                        // null: they are a cluster; else their parts, [tile][stream][key head][split]
+  int split;                           // CTAs of the cluster that shares a (stream, key head, tile of rows)
+  float* parts;                        // workspace; null: the CTAs of a cluster share the work and need none
 };
-cudaError_t launch_cached_bf16(const Geometry& g, CachedArgs& a, cudaStream_t st);
-cudaError_t launch_cached_f32(const Geometry& g, CachedArgs& a, cudaStream_t st);
-size_t cached_scratch(const Geometry& g, int dtype, const CachedArgs& a);
+// scratch not null: nothing is launched, only the workspace's size is said (0: none).
+cudaError_t launch_cached_bf16(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch);
+cudaError_t launch_cached_f32(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch);
 
 }  // namespace gsit

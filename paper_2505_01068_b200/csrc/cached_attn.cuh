@@ -1,21 +1,23 @@
 // Attention of a step's rows over a stream's cache (gsit_im_cached_attention_fwd); the kernel, for the files that instantiate it.
 //
-// Everything streams through once: a warp takes blocks of 32 positions of one key head, loads a block's bytes straight into the registers that its
-// matrix instructions take them from -- the pages are laid out for that: 16 bytes a lane, whole lines a warp, nothing staged -- and works on one
-// block while the next ones' bytes are under way.  8 query rows of the key head (its query heads, in every segment) are the narrow side of
-// m16n8k16 products:
+// Everything streams through once.  A warp takes blocks of 32 positions of one key head, which one lane has copied into a ring of the warp's own (bulk
+// copies, three stages, nobody else is waited for); the pages are laid out so that a lane finds what its matrix instructions take in 16 bytes, without
+// bank conflicts.  8 query rows of the key head (its query heads, in every segment) are the narrow side of m16n8k16 products:
 //   S^T = K Q^T      keys x rows: 8-bit integers (or e4m3) are exact in f16; q is brought to f16 by a power of two for each row, which loses nothing
 //                    of bf16 worth having (what is 2^-28 of a row's largest feature); float q as two f16 terms, 22 bits
 //   O^T += vs V^T P  features x rows: P turned round by movmatrix, in f16 (2^-11 of each weight, relative), as two terms for float; the block's scale
 //                    is applied to the product in float, so it never meets the range of f16
 // The open block's rows are brought to f16 by a power of two for the block (float: two terms) and go the same way, in the warp whose turn it is.
 // The softmax runs over a reference that is raised only where a score passes it by 2^8, so that most blocks need no exchange between lanes.
-// Warps' parts are joined in shared memory, CTAs' through the cluster's or, where more CTAs than a cluster holds share a (stream, key head), through
-// a workspace and a second small kernel; always in order.
+// Who takes what: where the step is small, the CTAs of a cluster share a (stream, key head, tile of rows) and join their parts through distributed shared
+// memory; where there is much to read, two CTAs an SM share out all blocks of all streams and key heads evenly, whatever their lengths are, and
+// a second small kernel joins the parts of those that more than one of them had.  Always in order.
 // A closed pair's weight is 0 and the bytes it meets are numbers, so nothing of it counts; blocks whose scale is NaN take a way of their own.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "cache.cuh"
 #include "scored.cuh"
@@ -48,23 +50,33 @@ __device__ __forceinline__ uint32_t turned_round(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// d = a b + c, c = (c0, c1) in both halves of the rows: constants, or a column's start, cost no instruction
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
-__device__ __forceinline__ void mma_k8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-  asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(b0));
+__device__ __forceinline__ void mma_k8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, const float (&c)[4]) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%8,%9,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
-// Four bytes as two pairs of f16, exactly.
-template <int KIND> __device__ __forceinline__ void unpack8(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  if constexpr (KIND == GSIT_CACHE_INT8) {   // the byte plus 128 as the last bits of 1024 + ..., less 1152
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Four bytes as two pairs of f16, exactly; integers with BIASED as 1152 + themselves (the byte plus 128 as the last bits of 1024 + ...).
+constexpr float BIAS = 1152.f;
+template <int KIND, bool BIASED> __device__ __forceinline__ void unpack8(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if constexpr (KIND == GSIT_CACHE_INT8) {
     const uint32_t u = w ^ 0x80808080u;
-    const __half2 minus = __halves2half2(__ushort_as_half(0xe480), __ushort_as_half(0xe480));
-    uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-    const __half2 x = __hadd2(*reinterpret_cast<__half2*>(&a), minus), y = __hadd2(*reinterpret_cast<__half2*>(&b), minus);
-    lo = *reinterpret_cast<const uint32_t*>(&x);
-    hi = *reinterpret_cast<const uint32_t*>(&y);
+    lo = __byte_perm(u, 0x64646464u, 0x4140);
+    hi = __byte_perm(u, 0x64646464u, 0x4342);
+    if constexpr (!BIASED) {
+      const __half2 minus = __float2half2_rn(-BIAS), x = __hadd2(*reinterpret_cast<__half2*>(&lo), minus), y = __hadd2(*reinterpret_cast<__half2*>(&hi), minus);
+      lo = *reinterpret_cast<const uint32_t*>(&x);
+      hi = *reinterpret_cast<const uint32_t*>(&y);
+    }
   } else {
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
   }
@@ -80,104 +92,200 @@ __device__ __forceinline__ Power power_for(float top, int to) {
   return {__int_as_float((127 + e) << 23), __int_as_float((127 - e) << 23)};
 }
 
-// What a lane holds of a block of bytes.
-template <int HD> struct Bytes {
-  static constexpr int WORDS = HD == 8 ? 2 : HD / 4;   // of keys, and of values
-  uint32_t k[WORDS], v[WORDS];
-  float ks, vs, time[4];
-  int rows;                // positions: 32, or those of an open block (whose rows are not loaded here)
-  int seg, at, buffer;     // segment, its first position; buffer of an open block, -1: full
-  __device__ __forceinline__ void load(const uint8_t* key, const uint8_t* value) {
-    if constexpr (HD == 8) {
-      const uint2 x = *reinterpret_cast<const uint2*>(key), y = *reinterpret_cast<const uint2*>(value);
-      k[0] = x.x; k[1] = x.y;
-      v[0] = y.x; v[1] = y.y;
-    } else {
-#pragma unroll
-      for (int i = 0; i < HD / 16; ++i) {
-        const uint4 x = *reinterpret_cast<const uint4*>(key + 512 * i);
-        k[4 * i] = x.x; k[4 * i + 1] = x.y; k[4 * i + 2] = x.z; k[4 * i + 3] = x.w;
-      }
-#pragma unroll
-      for (int i = 0; i < HD / 16; ++i) {
-        const uint4 y = *reinterpret_cast<const uint4*>(value + 512 * i);
-        v[4 * i] = y.x; v[4 * i + 1] = y.y; v[4 * i + 2] = y.z; v[4 * i + 3] = y.w;
-      }
-    }
-  }
+// A warp's ring: stages of B blocks -- keys, values and moments of each -- and what is known of them.
+template <int HD> struct Ring {
+  static constexpr int B = HD == 64 ? 1 : HD == 32 ? 2 : 4;            // blocks of a stage: 4 KB, heads of 8 2 KB
+  static constexpr int MATRIX = CACHE_BLOCK * HD, MOMENTS = 4 * CACHE_BLOCK, BLOCK = 2 * MATRIX + MOMENTS;
+  static constexpr int STAGES = 3, BYTES = STAGES * B * BLOCK;
+};
+struct BlockInfo {
+  float ks, vs;
+  int seg, first;          // segment (3: there is no such block), first position
 };
 
-// The parts that are joined: of each warp, then of the CTA.
-template <int HD, int R> struct PartRoom {
-  float acc[WARPS][R][HD], joined[R][HD];
-  float2 ml[WARPS][R], joined_ml[R];      // (reference, sum); a part without a key has a reference of -inf and takes no part
-  float scale[WARPS][R];
-};
-// Factors that bring (at most 8) parts to their common reference, and that reference with the sum.  A part without a number among its scores
-// has no reference: its sum is 0, or NaN where a score was, and then so is everything.
-template <typename Get, typename Put> __device__ __forceinline__ float2 join_sums(int n, Get get, Put put) {
-  float2 p[8];
-  float top = -INFINITY, sum = 0.f;
+// F features of a result, times `by` (out may lie at any element).
+template <int F> __device__ __forceinline__ void store_features(float* out, const float (&v)[F], float by) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    p[i] = i < n ? get(i) : make_float2(-INFINITY, 0.f);
-    top = fmaxf(top, p[i].x);
-  }
+  for (int e = 0; e < F; ++e) out[e] = v[e] * by;
+}
+template <int F> __device__ __forceinline__ void store_features(__nv_bfloat16* out, const float (&v)[F], float by) {
+  if (F == 2 && (reinterpret_cast<uintptr_t>(out) & 3u) == 0) *reinterpret_cast<uint32_t*>(out) = ptx::pack_bf16(v[0] * by, v[F - 1] * by);
+  else
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float f = p[i].x == -INFINITY ? 1.f : ptx::ex2(p[i].x - top);
-    if (i < n) put(i, f);
-    sum += f * p[i].y;
-  }
-  return make_float2(top, sum);
+    for (int e = 0; e < F; ++e) store_as(out + e, v[e] * by);
 }
 
-// How many blocks' bytes a lane asks for at once: 16 to 32 registers of them.
-template <int HD> constexpr int GROUP = HD == 64 ? 1 : HD == 32 ? 2 : 4;
+// The parts that are joined: of each warp, then of the CTA (in the first warp's place).
+template <int HD, int R> struct PartRoom {
+  float acc[WARPS][R][HD + 4];            // (rows four banks apart: a fragment's columns meet other banks)
+  float2 ml[WARPS][R];                    // (reference, sum)
+};
+// Lanes 0 .. 7 of a warp have (reference, sum) of eight parts of a row, or (-inf, 0): to the factors that bring them to one reference, and that
+// reference with the sum, in all lanes.  A part without a number among its scores has no reference: its sum is 0, or NaN where a score was,
+// and then so is everything.
+__device__ __forceinline__ float2 join_sums(float2 part, float& factor) {
+  float top = part.x;
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  factor = part.x == -INFINITY ? 1.f : ptx::ex2(part.x - top);
+  float sum = factor * part.y;
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return make_float2(__shfl_sync(0xffffffffu, top, 0), __shfl_sync(0xffffffffu, sum, 0));
+}
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, int bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+// A stream's list of blocks for one tile of rows: the full blocks of the segments that a real row is open to, then their open ones.
+struct BlockList {
+  int len[3], upto[3];     // positions of the segments that are walked; full blocks up to the end of each
+  int full, all;
+  __device__ __forceinline__ int segment(int i) const { return i >= upto[1] ? 2 : i >= upto[0] ? 1 : 0; }
+};
+__device__ __forceinline__ BlockList list_blocks(const Geometry& g, const CachedArgs& a, int b, int row0, int n_rows) {
+  BlockList l;
+  int real[3], opens = 0;
+#pragma unroll
+  for (int s = 0; s < 3; ++s) {
+    l.len[s] = held_rows(a.c, g.status, b, s);
+    real[s] = valid_rows(g, b, s);
+  }
+#pragma unroll
+  for (int s = 0; s < 3; ++s)
+    if (max(row0, g.off(s) * a.group) < min(row0 + n_rows, (g.off(s) + real[s]) * a.group)) opens |= (int)(g.allowed >> (3 * s)) & 7;
+  l.full = 0;
+  int open = 0;
+#pragma unroll
+  for (int s = 0; s < 3; ++s) {
+    if (!((opens >> s) & 1)) l.len[s] = 0;
+    l.full += l.len[s] / CACHE_BLOCK;
+    l.upto[s] = l.full;
+    open += l.len[s] % CACHE_BLOCK != 0;
+  }
+  l.all = l.full + open;
+  return l;
+}
+
+// Parts in the workspace: of every CTA its first and its last piece.
+template <int HD, int R> struct Part {
+  float acc[R][HD];
+  float2 ml[R];
+};
+
+// CTAs of an SM: two where their registers allow it.
+template <typename T, int NT> constexpr int RESIDENT = NT == 1 || (NT == 2 && sizeof(T) == 2) ? 2 : 1;
 
 template <typename T, int HD, int KIND, int NT>
-__global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1)
+__global__ void __launch_bounds__(THREADS, RESIDENT<T, NT>)
 cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CachedArgs a) {
-  constexpr int R = 8 * NT, TERMS = sizeof(T) == 4 ? 2 : 1, KS = HD == 8 ? 1 : HD / 16, MD = KS, B = GROUP<HD>;
+  constexpr int R = 8 * NT, TERMS = sizeof(T) == 4 ? 2 : 1, KS = HD == 8 ? 1 : HD / 16, MD = KS;
+  // bf16 rows leave the 1152 of the integers' f16 form in the products of values and take it out of what they start from: it costs 2^-20 of the block's
+  // largest value or so (in scores it would be seen: 1152 times the sum of a query's features, at 2^-24)
+  constexpr bool BIASED = KIND == GSIT_CACHE_INT8 && TERMS == 1;
+  using RingOf = Ring<HD>;
+  constexpr int B = RingOf::B, STAGES = RingOf::STAGES;
   using Room = PartRoom<HD, R>;
-  extern __shared__ __align__(16) uint8_t smem[];
-  Room& room = *reinterpret_cast<Room*>(smem);
+  extern __shared__ __align__(128) uint8_t smem[];
+  Room& room = *reinterpret_cast<Room*>(smem);             // where the rings were, when they are done with
   __shared__ QueryRow s_row[R];
+  __shared__ BlockInfo s_info[WARPS][STAGES][B];
+  __shared__ __align__(8) uint64_t s_bar[WARPS][STAGES];
+  __shared__ uint32_t s_gave_up;
+  __shared__ int s_sum[WARPS];
+  __shared__ int2 s_first;                   // stream that the share begins in, blocks before it
   const Cache& c = a.c;
   const int tid = threadIdx.x, warp = ptx::uniform(tid >> 5), lane = tid & 31, gr = lane >> 2, t = lane & 3;
-  const int rank = blockIdx.x % a.split, hk = blockIdx.x / a.split, b = blockIdx.y, row0 = blockIdx.z * R;
   ptx::load_params_early(g, a);
+  const uint32_t bars = smem_u32(s_bar[warp]), ring = smem_u32(smem) + warp * RingOf::BYTES;
+  if (lane == 0) {
+    for (int i = 0; i < STAGES; ++i) ptx::mbar_init(bars + 8 * i, B);
+    ptx::mbar_init_fence();
+  }
+  if (tid == 0) s_gave_up = 0;
+  __syncthreads();
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
+  const ptx::WaitCtx wait = {g.status, smem_u32(&s_gave_up)};
+  uint32_t stage = 0, phase = 0;             // of the warp's ring: they go on from piece to piece
+  const bool timed = a.causal != 0 || a.slopes != nullptr;
+
+  // One piece: blocks [lo, hi) of the list of stream b for key head hk, rows from row0 on, into the room (the warps' parts).
+  auto walk = [&](int b, int hk, int row0, int n_rows, const BlockList& list, int lo, int hi) {
+  const int first = lo + warp * B, last = min(hi, list.full);
+  constexpr int turn = WARPS * B;
+  // lanes know where the blocks of the warp's next 32 / B turns lie, and each sees to its own: copies into the stage, and what is known of it
+  int ahead = first, known = 0;
+  int64_t head = -1;
+  const float* moments = nullptr;
+  BlockInfo info = {0.f, 0.f, 3, 0};
+  uint32_t to = stage;
+  auto request = [&]() {
+    if (known == 0) {
+      const int i = ahead + lane / B * turn + lane % B, s = list.segment(i), j = i - (s == 0 ? 0 : s == 1 ? list.upto[0] : list.upto[1]);
+      head = -1;
+      info.seg = 3;
+      if (i < last) {
+        const int page = real_page(c, c.tables[((int64_t)b * 3 + s) * c.blocks + j]);
+        if (page < 0) raise_flag(g, GSIT_DEVFLAG_CLAMPED);
+        else {
+          head = (int64_t)page * c.kv_heads + hk;
+          info = {c.key_scale[head], c.value_scale[head], s, j * CACHE_BLOCK};
+          if (timed && c.times != nullptr) moments = c.times + (int64_t)page * CACHE_BLOCK;
+        }
+      }
+      known = 32 / B;
+    }
+    const int from = (32 / B - known) * B;
+    if (lane >= from && lane < from + B) {
+      const uint32_t bar = bars + 8 * to, at = ring + (to * B + lane - from) * RingOf::BLOCK;
+      s_info[warp][to][lane - from] = info;
+      ptx::mbar_expect_tx(bar, head < 0 ? 0 : 2 * RingOf::MATRIX + (moments != nullptr ? RingOf::MOMENTS : 0));
+      if (head >= 0) {
+        bulk_copy(at, c.keys + head * RingOf::MATRIX, RingOf::MATRIX, bar);
+        bulk_copy(at + RingOf::MATRIX, c.values + head * RingOf::MATRIX, RingOf::MATRIX, bar);
+        if (moments != nullptr) bulk_copy(at + 2 * RingOf::MATRIX, moments, RingOf::MOMENTS, bar);
+      }
+    }
+    ahead += turn;
+    --known;
+    to = to + 1 == STAGES ? 0 : to + 1;
+  };
+#pragma unroll 1
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (ahead < last) request();   // under way while the rows are looked at
 
   // ---- the rows: row r of a key head is row r / group of the step, head hk * group + r % group ----
-  for (int i = tid; i < R; i += THREADS) {
+  if (tid < R) {
     QueryRow x = {0.f, -INFINITY, 0.f, 0};
-    if (row0 + i < a.rows) {
-      const int l = (row0 + i) / a.group, s = segment_of(g, l), at = l - g.off(s), n = valid_rows(g, b, s);
+    if (tid < n_rows) {
+      const int l = (row0 + tid) / a.group, s = segment_of(g, l), at = l - g.off(s), n = valid_rows(g, b, s);
       if (at < n) {
         x.time = a.times.p != nullptr ? a.times.at(b, l) : (float)(held_rows(c, g.status, b, s) - n + at);
         x.limit = a.causal ? x.time : INFINITY;
-        x.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + (row0 + i) % a.group] * LOG2E : 0.f;
+        x.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + (row0 + tid) % a.group] * LOG2E : 0.f;
         x.opens = (int)(g.allowed >> (3 * s)) & 7;
       }
     }
-    s_row[i] = x;
+    s_row[tid] = x;
   }
   __syncthreads();
-  int opens = 0;
-#pragma unroll
-  for (int i = 0; i < R; ++i) opens |= s_row[i].opens;
 
   // ---- queries as B operands, and what brings a dot back to a score ----
   uint32_t qf[NT][TERMS][KS][2];
-  float back[NT][2];                     // of the columns 2 t and 2 t + 1 of each tile
-  int col_opens[NT][2];
+  float2 back[NT];                       // of the columns 2 t and 2 t + 1 of each tile
+  uint32_t col_opens = 0, every = 7;     // four bits for each column; segments that all of them are open to
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int r = row0 + 8 * n + gr;
-    const bool real = s_row[8 * n + gr].opens != 0;
-    const T* q = static_cast<const T*>(a.q) + ((int64_t)b * g.L + (real ? r / a.group : 0)) * a.ldq + (int64_t)(hk * a.group + (real ? r % a.group : 0)) * HD;
+    const bool there = s_row[8 * n + gr].opens != 0;
+    const T* q = static_cast<const T*>(a.q) + ((int64_t)b * g.L + (there ? r / a.group : 0)) * a.ldq + (int64_t)(hk * a.group + (there ? r % a.group : 0)) * HD;
     float2 f[KS][2];
     float top = 0.f;
 #pragma unroll
@@ -185,7 +293,7 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         f[k][h] = make_float2(0.f, 0.f);
-        if (real && (HD > 8 || h == 0)) {
+        if (there && (HD > 8 || h == 0)) {
           if constexpr (sizeof(T) == 2) unpack_bf16(*reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * h + 2 * t), f[k][h].x, f[k][h].y);
           else f[k][h] = *reinterpret_cast<const float2*>(q + 16 * k + 8 * h + 2 * t);
         }
@@ -202,93 +310,33 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
         qf[n][0][k][h] = f16x2(x, y);
         if constexpr (TERMS == 2) qf[n][1][k][h] = f16x2_rest(x, y, qf[n][0][k][h]);
       }
+    back[n] = make_float2(__shfl_sync(0xffffffffu, p.down, 8 * t) * a.inner, __shfl_sync(0xffffffffu, p.down, 8 * t + 4) * a.inner);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      back[n][e] = __shfl_sync(0xffffffffu, p.down, 4 * (2 * t + e)) * a.inner;
-      col_opens[n][e] = s_row[8 * n + 2 * t + e].opens;
+      const int opens = s_row[8 * n + 2 * t + e].opens;
+      col_opens |= (uint32_t)opens << (4 * (2 * n + e));
+      if (8 * n + 2 * t + e < n_rows) every &= opens;   // (columns behind the last row write nothing: whatever they see)
     }
   }
-
-  // ---- this warp's blocks: every (split * WARPS)-th group of those of the open segments, one after the other ----
-  int len[3], upto[3], blocks = 0;       // upto: blocks of the segments before and of this one
-#pragma unroll
-  for (int r = 0; r < 3; ++r) {
-    len[r] = ((opens >> r) & 1) ? held_rows(c, g.status, b, r) : 0;
-    blocks += (len[r] + CACHE_BLOCK - 1) / CACHE_BLOCK;
-    upto[r] = blocks;
-  }
-  const int turn = a.split * WARPS * B;
-  const bool timed = a.causal != 0 || a.slopes != nullptr;
-  // where block i lies: page, or -1 (an open block; none)
-  auto page_of = [&](int i) {
-    if (i >= blocks) return -1;
-    const int r = i >= upto[1] ? 2 : i >= upto[0] ? 1 : 0, j = i - (r == 0 ? 0 : upto[r - 1]);
-    const int page = real_page(c, c.tables[((int64_t)b * 3 + r) * c.blocks + j]);
-    if (page < 0) raise_flag(g, GSIT_DEVFLAG_CLAMPED);
-    return page;
-  };
-  // lanes know the pages of the warp's next 32 / B turns
-  int ahead = (rank * WARPS + warp) * B, known = 0, pages = -1;
-  Bytes<HD> next[B];
-  auto request = [&]() {
-    if (known == 0) {
-      pages = page_of(ahead + lane / B * turn + lane % B);
-      known = 32 / B;
-    }
-#pragma unroll
-    for (int u = 0; u < B; ++u) {
-      Bytes<HD>& x = next[u];
-      const int i = ahead + u, page = __shfl_sync(0xffffffffu, pages, (32 / B - known) * B + u);
-      x.rows = 0;
-      if (i < blocks) {
-        const int r = i >= upto[1] ? 2 : i >= upto[0] ? 1 : 0, j = i - (r == 0 ? 0 : r == 1 ? upto[0] : upto[1]);
-        x.seg = r;
-        x.at = j * CACHE_BLOCK;
-        x.rows = min(CACHE_BLOCK, (r == 0 ? len[0] : r == 1 ? len[1] : len[2]) - x.at);
-        x.buffer = x.rows < CACHE_BLOCK ? j & 1 : -1;
-        if (timed)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x.time[e] = c.times == nullptr ? (float)(x.at + 8 * e + gr) : page >= 0 ? c.times[(int64_t)page * CACHE_BLOCK + 8 * e + gr] : 0.f;
-        if (x.buffer < 0) {
-          if (page < 0) x.rows = 0;
-          else {
-            const int64_t head = (int64_t)page * c.kv_heads + hk;
-            x.load(c.keys + head * (CACHE_BLOCK * HD) + (HD == 8 ? 8 : 16) * lane, c.values + head * (CACHE_BLOCK * HD) + (HD == 8 ? 8 : 16) * lane);
-            x.ks = c.key_scale[head];
-            x.vs = c.value_scale[head];
-          }
-        }
-      }
-    }
-    ahead += turn;
-    --known;
-  };
-
-  float o[MD][NT][4], ref[NT][2], sum[NT][2];
+  every = __reduce_and_sync(0xffffffffu, every);
+  float2 o[MD][NT][2], ref[NT], sum[NT];   // pairs: columns 2 t, 2 t + 1
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
+    ref[n] = make_float2(-INFINITY, -INFINITY);
+    sum[n] = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      ref[n][e] = -INFINITY;
-      sum[n][e] = 0.f;
-    }
-#pragma unroll
-    for (int m = 0; m < MD; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[m][n][e] = 0.f;
+    for (int m = 0; m < MD; ++m) o[m][n][0] = o[m][n][1] = make_float2(0.f, 0.f);
   }
 
-  // One block: keys(m, k, term, fragment) and values(m, k, term, fragment) give A operands, of TERMS_IN terms.
-  auto attend = [&](const Bytes<HD>& x, auto terms_in, float ks, float vs, auto keys, auto values) {
+  // One block of segment `seg`: keys(m, k, term, fragment) and values(m, k, term, fragment) give A operands, of IN terms; FULL: all 32 positions,
+  // biased where bytes are taken that way.
+  auto attend = [&](auto terms_in, auto whole, int seg, int rows, float ks, float vs, const float (&times)[4], auto keys, auto values) {
     constexpr int IN = decltype(terms_in)::value;
+    constexpr bool FULL = decltype(whole)::value != 0, FROM_BIAS = FULL && BIASED;
+    float zero[4] = {0.f, 0.f, 0.f, 0.f};
     float s[2][NT][4];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[m][n][e] = 0.f;
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -299,89 +347,125 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int y = 0; y < TERMS - w; ++y) {   // the product of the two smaller terms is left out: 2^-22 of the score's terms
-              if constexpr (HD == 8) mma_k8(s[m][n], f[0], f[1], qf[n][y][k][0]);
-              else mma(s[m][n], f, qf[n][y][k][0], qf[n][y][k][1]);
+              float (&from)[4] = k + w + y > 0 ? s[m][n] : zero;
+              if constexpr (HD == 8) mma_k8(s[m][n], f[0], f[1], qf[n][y][k][0], from);
+              else mma(s[m][n], f, qf[n][y][k][0], qf[n][y][k][1], from);
             }
         }
+    // scores in base 2, pairs of columns; positions 16 m + 8 h + gr
+    float2 x[NT][2][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float2 f = __fmul2_rn(back[n], make_float2(ks, ks));
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[n][m][h] = __fmul2_rn(make_float2(s[m][n][2 * h], s[m][n][2 * h + 1]), f);
     }
-    // scores in base 2; closed pairs -inf
-    bool raise = false;
+    if (a.softcap > 0.f) {
+      // bf16: 1 - 2 / (e^2y + 1), which is 2^-23 off, next to a cap of 50 in the score 2^-17; `inner` has the factor 2 log2 e
+      auto bend = [&](float y) { return sizeof(T) == 4 ? tanhf(y) * a.outer : fmaf(-2.f * a.outer, reciprocal(ptx::ex2(y) + 1.f), a.outer); };
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const bool mine = (col_opens[n][e] >> x.seg) & 1;
-        const float f = back[n][e] * ks;
-        float time = 0.f, limit = 0.f, slope2 = 0.f;
-        if (timed) {
-          const QueryRow& row = s_row[8 * n + 2 * t + e];
-          time = row.time;
-          limit = row.limit;
-          slope2 = row.slope2;
-        }
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float& v = s[m][n][2 * h + e];
-            v *= f;
-            if (a.softcap > 0.f) v = (sizeof(T) == 4 ? tanhf(v) : tanh_any2(make_float2(v, v)).x) * a.outer;
-            bool open = mine && 16 * m + 8 * h + gr < x.rows;
-            if (timed) {
-              v -= slope2 * fabsf(time - x.time[2 * m + h]);
-              open = open && x.time[2 * m + h] <= limit;
-            }
-            v = open ? v : -INFINITY;
-            raise = raise || !(v <= ref[n][e] + 8.f);   // NaN, too
+          for (int h = 0; h < 2; ++h) x[n][m][h] = make_float2(bend(x[n][m][h].x), bend(x[n][m][h].y));
+    }
+    if (!FULL || timed || !((every >> seg) & 1u)) {   // closed pairs -inf
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const bool m0 = (col_opens >> (8 * n + seg)) & 1u, m1 = (col_opens >> (8 * n + 4 + seg)) & 1u;
+        float2 time = make_float2(0.f, 0.f), limit = time, slope2 = time;
+        if (timed) {
+          const QueryRow &r0 = s_row[8 * n + 2 * t], &r1 = s_row[8 * n + 2 * t + 1];
+          time = make_float2(r0.time, r1.time);
+          limit = make_float2(r0.limit, r1.limit);
+          slope2 = make_float2(-r0.slope2, -r1.slope2);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float2& v = x[n][i / 2][i % 2];
+          const bool there = FULL || 8 * i + gr < rows;
+          bool o0 = m0 && there, o1 = m1 && there;
+          if (timed) {
+            const float2 d = __fadd2_rn(time, make_float2(-times[i], -times[i]));
+            v = __ffma2_rn(slope2, make_float2(fabsf(d.x), fabsf(d.y)), v);
+            o0 = o0 && times[i] <= limit.x;
+            o1 = o1 && times[i] <= limit.y;
           }
+          v = make_float2(o0 ? v.x : -INFINITY, o1 ? v.y : -INFINITY);
+        }
       }
+    }
+    bool raise = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float2 over = __fadd2_rn(ref[n], make_float2(8.f, 8.f));
+      raise = raise || fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x) > over.x ||
+              fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y) > over.y;
+    }
     if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float2 top = make_float2(fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x),
+                                 fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y));
+#pragma unroll
+        for (int l = 4; l < 32; l <<= 1) top = make_float2(fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, l)), fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, l)));
+        top = make_float2(fmaxf(top.x, ref[n].x), fmaxf(top.y, ref[n].y));
+        const float2 f = make_float2(top.x > ref[n].x ? ptx::ex2(ref[n].x - top.x) : 1.f, top.y > ref[n].y ? ptx::ex2(ref[n].y - top.y) : 1.f);
+        sum[n] = __fmul2_rn(sum[n], f);
+#pragma unroll
+        for (int m = 0; m < MD; ++m) {
+          o[m][n][0] = __fmul2_rn(o[m][n][0], f);
+          o[m][n][1] = __fmul2_rn(o[m][n][1], f);
+        }
+        ref[n] = top;
+      }
+    }
+    const bool broken = !(fabsf(vs) < INFINITY);
+    uint32_t seen = 0;                   // where the block's values are broken: columns that any position is open to
+    if (broken)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float top = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e]));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-          if (top > ref[n][e]) {
-            const float f = ptx::ex2(ref[n][e] - top);
-            sum[n][e] *= f;
+          bool any = false;
 #pragma unroll
-            for (int m = 0; m < MD; ++m) {
-              o[m][n][e] *= f;
-              o[m][n][2 + e] *= f;
-            }
-            ref[n][e] = top;
-          }
+          for (int i = 0; i < 4; ++i) any = any || (e ? x[n][i / 2][i % 2].y : x[n][i / 2][i % 2].x) != -INFINITY;
+          const uint32_t who = __ballot_sync(0xffffffffu, any) & (0x11111111u << t);
+          seen |= (who != 0 ? 1u : 0u) << (2 * n + e);
         }
-      __syncwarp();
-    }
-    // weights, turned round into B operands: keys 2 t, 2 t + 1 (and + 8) of row gr
+    // weights, turned round into B operands: keys 2 t, 2 t + 1 (and + 8) of row gr.  What biased values start from is a product with ones: the
+    // sum of the weights as they are rounded, in every lane
     uint32_t pf[NT][TERMS][2][2];
+    float begin[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float r0 = ref[n][0] == -INFINITY ? 0.f : ref[n][0], r1 = ref[n][1] == -INFINITY ? 0.f : ref[n][1];
+      const float2 r = make_float2(ref[n].x == -INFINITY ? 0.f : -ref[n].x, ref[n].y == -INFINITY ? 0.f : -ref[n].y);
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float p0 = ptx::ex2(s[m][n][2 * h] - r0), p1 = ptx::ex2(s[m][n][2 * h + 1] - r1);
-          sum[n][0] += p0;
-          sum[n][1] += p1;
-          const uint32_t p = f16x2(p0, p1);
-          pf[n][0][m][h] = turned_round(p);
-          if constexpr (TERMS == 2) pf[n][1][m][h] = turned_round(f16x2_rest(p0, p1, p));
+          const float2 v = __fadd2_rn(x[n][m][h], r), p = make_float2(ptx::ex2(v.x), ptx::ex2(v.y));
+          sum[n] = __fadd2_rn(sum[n], p);
+          const uint32_t w = f16x2(p.x, p.y);
+          pf[n][0][m][h] = turned_round(w);
+          if constexpr (TERMS == 2) pf[n][1][m][h] = turned_round(f16x2_rest(p.x, p.y, w));
         }
+      if constexpr (FROM_BIAS) {
+        constexpr uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+        float add[4];
+        mma(add, ones, pf[n][0][0][0], pf[n][0][0][1], zero);
+        mma(add, ones, pf[n][0][1][0], pf[n][0][1][1], add);
+        const float2 from = __fmul2_rn(make_float2(add[0], add[1]), make_float2(-BIAS, -BIAS));
+        begin[n][0] = begin[n][2] = from.x;
+        begin[n][1] = begin[n][3] = from.y;
+      }
     }
-    const bool broken = !(fabsf(vs) < INFINITY);
 #pragma unroll
     for (int m = 0; m < MD; ++m) {
       float add[NT][4];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) add[n][e] = 0.f;
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -391,44 +475,97 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int y = 0; y < TERMS - w; ++y) mma(add[n], f, pf[n][y][k][0], pf[n][y][k][1]);
+            for (int y = 0; y < TERMS - w; ++y) mma(add[n], f, pf[n][y][k][0], pf[n][y][k][1], k + w + y > 0 ? add[n] : FROM_BIAS ? begin[n] : zero);
         }
       if (!broken) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[m][n][e] = fmaf(vs, add[n][e], o[m][n][e]);
+        for (int n = 0; n < NT; ++n) {
+          o[m][n][0] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][0], add[n][1]), o[m][n][0]);
+          if constexpr (HD > 8) o[m][n][1] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][2], add[n][3]), o[m][n][1]);
+        }
       }
     }
-    if (broken)   // NaN for the rows to which any position of the block is open
+    if (broken)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          bool any = false;
-#pragma unroll
-          for (int m = 0; m < 2; ++m) any = any || s[m][n][e] != -INFINITY || s[m][n][2 + e] != -INFINITY;
-          uint32_t which = __ballot_sync(0xffffffffu, any);
-          which |= which >> 16;
-          which |= which >> 8;
-          which |= which >> 4;
-          if ((which >> t) & 1u)
-#pragma unroll
-            for (int m = 0; m < MD; ++m) o[m][n][e] = o[m][n][2 + e] = vs;
+        for (int m = 0; m < MD; ++m) {
+          if ((seen >> (2 * n)) & 1u) o[m][n][0].x = o[m][n][1].x = vs;
+          if ((seen >> (2 * n + 1)) & 1u) o[m][n][0].y = o[m][n][1].y = vs;
         }
   };
-  // The open block: rows in memory, brought to f16 by a power of two for all of them.
-  auto open_block = [&](const Bytes<HD>& x) {
-    const int64_t at = ((((int64_t)b * 3 + x.seg) * 2 + x.buffer) * c.kv_heads + hk) * (CACHE_BLOCK * HD);
-    const T* const key = static_cast<const T*>(c.open_keys) + at;
-    const T* const value = static_cast<const T*>(c.open_values) + at;
+
+#pragma unroll 1
+  for (int now = first; now < last; now += turn) {
+    if (ahead < last) request();   // into the stage that was read before this one
+    ptx::mbar_wait_warp(wait, bars + 8 * stage, phase);
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const BlockInfo x = s_info[warp][stage][u];
+      if (x.seg == 3) continue;
+      const uint32_t at = ring + (stage * B + u) * RingOf::BLOCK, key = at + (HD == 8 ? 8 : 16) * lane, value = key + RingOf::MATRIX;
+      float times[4] = {0.f, 0.f, 0.f, 0.f};
+      if (timed)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          times[i] = c.times != nullptr ? *reinterpret_cast<const float*>(smem + (at - smem_u32(smem)) + 2 * RingOf::MATRIX + 4 * (8 * i + gr)) : (float)(x.first + 8 * i + gr);
+      // fragments of keys come by (feature group, position half), of values by (feature group, position half), both halves in 16 bytes
+      uint4 kw[KS], vw[MD];
+      auto take = [&](uint4 (&w)[KS], uint32_t from) {
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          if constexpr (HD == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[i].x), "=r"(w[i].y) : "r"(from) : "memory");
+          else w[i] = lds16(from + 512 * i);
+        }
+      };
+      take(kw, key);
+      attend(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, x.seg, CACHE_BLOCK, x.ks, x.vs, times,
+             [&](int m, int k, int, uint32_t (&f)[4]) {
+               if constexpr (HD == 8) unpack8<KIND, false>(m ? kw[0].y : kw[0].x, f[0], f[1]);
+               else {
+                 unpack8<KIND, false>(m ? kw[k].z : kw[k].x, f[0], f[1]);
+                 unpack8<KIND, false>(m ? kw[k].w : kw[k].y, f[2], f[3]);
+               }
+             },
+             [&](int m, int k, int, uint32_t (&f)[4]) {
+               if (m + k == 0) take(vw, value);
+               if constexpr (HD == 8) {
+                 unpack8<KIND, BIASED>(k ? vw[0].y : vw[0].x, f[0], f[2]);
+                 f[1] = f[3] = 0u;
+               } else {
+                 unpack8<KIND, BIASED>(k ? vw[m].z : vw[m].x, f[0], f[1]);
+                 unpack8<KIND, BIASED>(k ? vw[m].w : vw[m].y, f[2], f[3]);
+               }
+             });
+    }
+    __syncwarp();   // every lane has used what it read of the stage
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    phase ^= stage == 0;
+  }
+  // The open blocks, each the next warp's in turn: rows in memory, brought to f16 by a power of two for all of a block's.
+#pragma unroll 1
+  for (int r = 0, at = list.full; r < 3; ++r) {
+    const int n = r == 0 ? list.len[0] : r == 1 ? list.len[1] : list.len[2], rows = n % CACHE_BLOCK, j = n / CACHE_BLOCK;
+    if (rows == 0) continue;
+    const int i = at++;
+    if (i < lo || i >= hi || ((max(0, last - lo) + B - 1) / B + i - max(lo, list.full)) % WARPS != warp) continue;
+    const int64_t from = open_at(c, b, r, j, hk);
+    const T* const key = static_cast<const T*>(c.open_keys) + from;
+    const T* const value = static_cast<const T*>(c.open_values) + from;
+    float times[4] = {0.f, 0.f, 0.f, 0.f};
+    if (timed) {
+      const int page = c.times == nullptr ? 0 : real_page(c, c.tables[((int64_t)b * 3 + r) * c.blocks + j]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        times[i] = c.times == nullptr ? (float)(j * CACHE_BLOCK + 8 * i + gr) : page >= 0 ? c.times[(int64_t)page * CACHE_BLOCK + 8 * i + gr] : 0.f;
+    }
     Power up[2];
     bool broken[2];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      constexpr int E = 16 / (int)sizeof(T) >= 8 ? 8 : 4;
+      constexpr int E = sizeof(T) == 2 ? 8 : 4;
       uint32_t top = 0;
-      for (int i = lane * E; i < x.rows * HD; i += 32 * E) {
+      for (int i = lane * E; i < rows * HD; i += 32 * E) {
         float f[E];
         load_n(w ? value + i : key + i, f);
 #pragma unroll
@@ -438,151 +575,284 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
       broken[w] = top >= 0x7f800000u;
       up[w] = top > 0 && !broken[w] ? power_for(__uint_as_float(top), 14) : Power{1.f, 1.f};
     }
-    auto terms = [&](float2 v, int w) {
-      const uint32_t r = f16x2(v.x, v.y);
-      return w == 0 ? r : f16x2_rest(v.x, v.y, r);
+    auto pair = [&](const T* p, int row, bool bad, float by) {
+      float2 v = make_float2(0.f, 0.f);
+      if (row < rows && !bad) {
+        if constexpr (sizeof(T) == 2) unpack_bf16(*reinterpret_cast<const uint32_t*>(p), v.x, v.y);
+        else v = *reinterpret_cast<const float2*>(p);
+      }
+      return make_float2(v.x * by, v.y * by);
     };
-    attend(x, std::integral_constant<int, TERMS>{}, broken[0] ? __int_as_float(0x7fffffff) : up[0].down, broken[1] ? __int_as_float(0x7fffffff) : up[1].down,
+    auto term = [&](float2 v, int w) {
+      const uint32_t x = f16x2(v.x, v.y);
+      return w == 0 ? x : f16x2_rest(v.x, v.y, x);
+    };
+    attend(std::integral_constant<int, TERMS>{}, std::integral_constant<int, 0>{}, r, rows, broken[0] ? __int_as_float(0x7fffffff) : up[0].down,
+           broken[1] ? __int_as_float(0x7fffffff) : up[1].down, times,
            [&](int m, int k, int w, uint32_t (&f)[4]) {
 #pragma unroll
              for (int i = 0; i < 4; ++i) {   // position halves i % 2, feature halves i / 2
                const int row = 16 * m + 8 * (i % 2) + gr;
-               float2 v = make_float2(0.f, 0.f);
-               if (row < x.rows && !broken[0] && (HD > 8 || i < 2)) {
-                 const T* p = key + row * HD + 16 * k + 8 * (i / 2) + 2 * t;
-                 if constexpr (sizeof(T) == 2) unpack_bf16(*reinterpret_cast<const uint32_t*>(p), v.x, v.y);
-                 else v = *reinterpret_cast<const float2*>(p);
-               }
-               f[i] = terms(make_float2(v.x * up[0].up, v.y * up[0].up), w);
+               f[i] = HD > 8 || i < 2 ? term(pair(key + row * HD + 16 * k + 8 * (i / 2) + 2 * t, row, broken[0], up[0].up), w) : 0u;
              }
            },
            [&](int m, int k, int w, uint32_t (&f)[4]) {
 #pragma unroll
              for (int i = 0; i < 4; ++i) {   // feature halves i % 2, position halves i / 2; rows of features come in, turned round
                const int row = 16 * k + 8 * (i / 2) + gr;
-               float2 v = make_float2(0.f, 0.f);
-               if (row < x.rows && !broken[1] && (HD > 8 || i % 2 == 0)) {
-                 const T* p = value + row * HD + 16 * m + 8 * (i % 2) + 2 * t;
-                 if constexpr (sizeof(T) == 2) unpack_bf16(*reinterpret_cast<const uint32_t*>(p), v.x, v.y);
-                 else v = *reinterpret_cast<const float2*>(p);
-               }
-               f[i] = turned_round(terms(make_float2(v.x * up[1].up, v.y * up[1].up), w));
+               f[i] = HD > 8 || i % 2 == 0 ? turned_round(term(pair(value + row * HD + 16 * m + 8 * (i % 2) + 2 * t, row, broken[1], up[1].up), w)) : 0u;
              }
            });
+  }
+
+  // ---- the warps' parts ----
+  __syncthreads();   // nobody's ring is in use any more
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = 8 * n + 2 * t;
+#pragma unroll
+    for (int l = 4; l < 32; l <<= 1) sum[n] = make_float2(sum[n].x + __shfl_xor_sync(0xffffffffu, sum[n].x, l), sum[n].y + __shfl_xor_sync(0xffffffffu, sum[n].y, l));
+    if (gr == 0) {
+      room.ml[warp][row] = make_float2(ref[n].x, sum[n].x);
+      room.ml[warp][row + 1] = make_float2(ref[n].y, sum[n].y);
+    }
+#pragma unroll
+    for (int m = 0; m < MD; ++m)
+#pragma unroll
+      for (int h = 0; h < (HD > 8 ? 2 : 1); ++h) {
+        room.acc[warp][row][16 * m + 8 * h + gr] = o[m][n][h].x;
+        room.acc[warp][row + 1][16 * m + 8 * h + gr] = o[m][n][h].y;
+      }
+  }
+  __syncthreads();
   };
 
-  int now = ahead;
-  request();
+  // a warp takes every eighth row of a piece, its lanes the features
+  constexpr int F = HD < 32 ? 1 : HD / 32;
+  const bool mine = lane * F < HD;
+  auto finish = [&](int b, int hk, int row, const float (&v)[F], float2 ml) {
+    const int l = row / a.group, head = hk * a.group + row % a.group;
+    T* const out = static_cast<T*>(a.out) + ((int64_t)b * g.L + l) * g.d + (int64_t)head * HD + lane * F;
+    const float inv = ml.y != 0.f ? 1.f / ml.y : 0.f;
+    if (mine) store_features<F>(out, v, inv);
+    if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * g.heads + head) * g.L + l] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * LN2 : -INFINITY;
+  };
+  // row r of the room, its warps' parts joined
+  auto join_warps = [&](int r, float (&v)[F]) {
+    float factor;
+    const float2 ml = join_sums(lane < WARPS ? room.ml[lane][r] : make_float2(-INFINITY, 0.f), factor);
+#pragma unroll
+    for (int e = 0; e < F; ++e) v[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float f = __shfl_sync(0xffffffffu, factor, w);
+      if (mine)
+#pragma unroll
+        for (int e = 0; e < F; ++e) v[e] = fmaf(f, room.acc[w][r][lane * F + e], v[e]);
+    }
+    return ml;
+  };
+
+  // ---- this CTA's share: one piece, or an even share of all streams' blocks, in pieces of one stream and key head ----
+  const bool even = a.parts != nullptr;
+  const int rank = even ? 0 : (int)blockIdx.x % a.split, row0 = even ? 0 : (int)blockIdx.z * R, n_rows = min(R, a.rows - row0);
+  int b = even ? 0 : (int)blockIdx.y, hk = even ? 0 : (int)blockIdx.x / a.split, pieces = 0;
+  int64_t at = 0, end = 1, base = 0;         // in blocks of all streams and key heads: where the share goes on and ends, where stream b begins
+  if (even) {
+    // Streams' blocks added up, 256 at a time: the total, then the stream that the share begins in.  CTA 0 leaves the sums for the joining kernel.
+    int* const before = reinterpret_cast<int*>(a.parts + (size_t)gridDim.x * 2 * (sizeof(Part<HD, R>) / sizeof(float)));
+    int total = 0;
 #pragma unroll 1
-  for (; now < blocks; now += turn) {
-    Bytes<HD> x[B];
+    for (int pass = 0; pass < 2; ++pass) {
+      at = (int64_t)total * c.kv_heads * blockIdx.x / gridDim.x;
+      int run = 0;
+#pragma unroll 1
+      for (int b0 = 0; b0 < g.batch; b0 += THREADS) {
+        const int i = b0 + tid, n = i < g.batch ? list_blocks(g, a, i, 0, a.rows).all : 0;
+        int upto = n;
 #pragma unroll
-    for (int u = 0; u < B; ++u) x[u] = next[u];
-    request();
+        for (int l = 1; l < 32; l <<= 1) {
+          const int x = __shfl_up_sync(0xffffffffu, upto, l);
+          if (lane >= l) upto += x;
+        }
+        __syncthreads();
+        if (lane == 31) s_sum[warp] = upto;
+        __syncthreads();
+        int here = 0, mine_before = 0;
 #pragma unroll
-    for (int u = 0; u < B; ++u) {
-      if (x[u].rows == 0) continue;
-      if (x[u].buffer >= 0) {
-        open_block(x[u]);
-        continue;
+        for (int w = 0; w < WARPS; ++w) {
+          if (w < warp) mine_before += s_sum[w];
+          here += s_sum[w];
+        }
+        const int from = run + mine_before + upto - n;
+        if (pass == 1) {
+          if ((int64_t)from * c.kv_heads <= at && at < (int64_t)(from + n) * c.kv_heads) s_first = make_int2(i, from);
+          if (blockIdx.x == 0 && i < g.batch) before[i] = from;
+        }
+        run += here;
+        if (g.batch <= THREADS && pass == 0) {   // the one round that there is answers both
+          at = (int64_t)run * c.kv_heads * blockIdx.x / gridDim.x;
+          if ((int64_t)from * c.kv_heads <= at && at < (int64_t)(from + n) * c.kv_heads) s_first = make_int2(i, from);
+          if (blockIdx.x == 0 && i < g.batch) before[i] = from;
+        }
       }
-      attend(x[u], std::integral_constant<int, 1>{}, x[u].ks, x[u].vs,
-             [&](int m, int k, int, uint32_t (&f)[4]) {
-               if constexpr (HD == 8) unpack8<KIND>(x[u].k[m], f[0], f[1]);
-               else {
-                 unpack8<KIND>(x[u].k[4 * k + 2 * m], f[0], f[1]);
-                 unpack8<KIND>(x[u].k[4 * k + 2 * m + 1], f[2], f[3]);
-               }
-             },
-             [&](int m, int k, int, uint32_t (&f)[4]) {
-               if constexpr (HD == 8) {
-                 unpack8<KIND>(x[u].v[k], f[0], f[2]);
-                 f[1] = f[3] = 0u;
-               } else {
-                 unpack8<KIND>(x[u].v[4 * m + 2 * k], f[0], f[1]);
-                 unpack8<KIND>(x[u].v[4 * m + 2 * k + 1], f[2], f[3]);
-               }
-             });
+      total = run;
+      if (g.batch <= THREADS) break;
     }
+    if (blockIdx.x == 0 && tid == 0) before[g.batch] = total;
+    __syncthreads();
+    const int64_t units = (int64_t)total * c.kv_heads;
+    at = units * blockIdx.x / gridDim.x;
+    end = units * (blockIdx.x + 1) / gridDim.x;
+    if (at >= end) return;
+    b = s_first.x;
+    base = (int64_t)s_first.y * c.kv_heads;
   }
-
-  // ---- join: lanes, warps, CTAs ----
+  BlockList list = list_blocks(g, a, b, row0, n_rows);
+#pragma unroll 1
+  while (true) {
+    int lo, hi;
+    if (even) {
+      while (at >= base + (int64_t)list.all * c.kv_heads) {   // the next stream that has any
+        base += (int64_t)list.all * c.kv_heads;
+        list = list_blocks(g, a, ++b, row0, n_rows);
+      }
+      hk = (int)((at - base) / list.all);
+      lo = (int)((at - base) - (int64_t)hk * list.all);
+      hi = (int)min((int64_t)list.all, lo + (end - at));
+      at += hi - lo;
+    } else {
+      lo = (int)((int64_t)list.all * rank / a.split);
+      hi = (int)((int64_t)list.all * (rank + 1) / a.split);
+      at = end;
+    }
+    walk(b, hk, row0, n_rows, list, lo, hi);
+    const bool whole = lo == 0 && hi == list.all;
+    Part<HD, R>& part = reinterpret_cast<Part<HD, R>*>(a.parts)[2 * blockIdx.x + (pieces > 0)];
+    for (int r = warp; r < n_rows; r += WARPS) {
+      float v[F];
+      const float2 ml = join_warps(r, v);
+      if (a.split == 1 && (!even || whole)) finish(b, hk, row0 + r, v, ml);
+      else {
+        __syncwarp();
+        float* const to = even ? part.acc[r] : room.acc[0][r];
+        if (mine)
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float l = sum[n][e];
-      l += __shfl_xor_sync(0xffffffffu, l, 4);
-      l += __shfl_xor_sync(0xffffffffu, l, 8);
-      l += __shfl_xor_sync(0xffffffffu, l, 16);
-      const int row = 8 * n + 2 * t + e;
-      if (gr == 0) room.ml[warp][row] = make_float2(ref[n][e], l);
-#pragma unroll
-      for (int m = 0; m < MD; ++m) {
-        room.acc[warp][row][16 * m + gr] = o[m][n][e];
-        if constexpr (HD > 8) room.acc[warp][row][16 * m + 8 + gr] = o[m][n][2 + e];
+          for (int e = 0; e < F; ++e) to[lane * F + e] = v[e];
+        if (lane == 0) (even ? part.ml[r] : room.ml[0][r]) = ml;
       }
     }
-  __syncthreads();
-  if (tid < R) room.joined_ml[tid] = join_sums(WARPS, [&](int w) { return room.ml[w][tid]; }, [&](int w, float f) { room.scale[w][tid] = f; });
-  __syncthreads();
-  const int n_rows = min(R, a.rows - row0);
-  for (int i = tid; i < n_rows * HD; i += THREADS) {
-    const int r = i / HD, f = i % HD;
-    float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) v += room.scale[w][r] * room.acc[w][r][f];
-    room.joined[r][f] = v;
+    if (at >= end) break;
+    ++pieces;
+    ptx::fence_async_smem();   // what was joined here lies where the next piece's copies go
+    __syncthreads();
   }
-  auto write = [&](int r, int f, float v, float l) {
-    store_as(static_cast<T*>(a.out) + ((int64_t)b * g.L + (row0 + r) / a.group) * g.d + (int64_t)(hk * a.group + (row0 + r) % a.group) * HD + f, l != 0.f ? v / l : 0.f);
-  };
-  auto write_lse = [&](int r, float2 ml) {
-    a.lse[((int64_t)b * g.heads + hk * a.group + (row0 + r) % a.group) * g.L + (row0 + r) / a.group] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * LN2 : -INFINITY;
-  };
+  if (a.split == 1) return;
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
-  if (a.split == 1) {
-    for (int i = tid; i < n_rows * HD; i += THREADS) write(i / HD, i % HD, room.joined[i / HD][i % HD], room.joined_ml[i / HD].y);
-    if (a.lse != nullptr && tid < n_rows) write_lse(tid, room.joined_ml[tid]);
-  } else {
-    // every CTA joins the rows' values of its own share
-    if (tid < R) {
-      const float2 ml = join_sums(a.split, [&](int k) { return cluster.map_shared_rank(room.joined_ml, k)[tid]; },
-                                               [&](int k, float f) { room.scale[k][tid] = f; });
-      room.ml[0][tid] = ml;
-      if (rank == 0 && a.lse != nullptr && tid < n_rows) write_lse(tid, ml);
-    }
-    __syncthreads();
-    const int share = (n_rows * HD + a.split - 1) / a.split, last = min(n_rows * HD, (rank + 1) * share);
-    for (int i = rank * share + tid; i < last; i += THREADS) {
-      const int r = i / HD, f = i % HD;
-      float v = 0.f;
-      for (int k = 0; k < a.split; ++k) v += room.scale[k][r] * cluster.map_shared_rank(&room.joined[0][0], k)[i];
-      write(r, f, v, room.ml[0][r].y);
-    }
-    cluster.sync();   // nobody's shared memory goes away while it is read
+  for (int r = rank * WARPS + warp; r < n_rows; r += a.split * WARPS) {
+    float factor, v[F] = {};
+    const float2 ml = join_sums(lane < a.split ? cluster.map_shared_rank(&room, lane)->ml[0][r] : make_float2(-INFINITY, 0.f), factor);
+#pragma unroll
+    for (int k = 0; k < MAX_CLUSTER; ++k)
+      if (k < a.split) {
+        const float f = __shfl_sync(0xffffffffu, factor, k);
+        if (mine)
+#pragma unroll
+          for (int e = 0; e < F; ++e) v[e] = fmaf(f, cluster.map_shared_rank(&room, k)->acc[0][r][lane * F + e], v[e]);
+      }
+    finish(b, hk, row0 + r, v, ml);
   }
+  cluster.sync();   // nobody's shared memory goes away while it is read
 }
 
-// CTAs per (stream, key head): until every SM has one, as long as each still gets a turn of its warps where the tables are full.
+// Joins the parts of the (stream, key head)s that more than one CTA had, and writes the rows of those that none had.  A warp takes one row.
+template <typename T, int HD, int R>
+__global__ void __launch_bounds__(THREADS) cached_join_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CachedArgs a, const int ctas) {
+  const Part<HD, R>* const parts = reinterpret_cast<const Part<HD, R>*>(a.parts);
+  const int* const before = reinterpret_cast<const int*>(parts + 2 * ctas);
+  const int lane = threadIdx.x & 31, item = (int)(blockIdx.x * WARPS + (threadIdx.x >> 5));
+  constexpr int F = HD < 32 ? 1 : HD / 32;
+  const bool mine = lane * F < HD;
+  ptx::load_params_early(g, a);
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+  const int r = item % a.rows, pair = item / a.rows, hk = pair % a.c.kv_heads, b = pair / a.c.kv_heads;
+  if (b >= g.batch) return;
+  const int start = before[b], n = before[b + 1] - start;
+  const int64_t units = (int64_t)before[g.batch] * a.c.kv_heads, from = (int64_t)start * a.c.kv_heads + (int64_t)hk * n, to = from + n;
+  auto cta_of = [&](int64_t unit) {   // the last one whose share begins at or before it
+    int k = (int)(unit * ctas / units);
+    while (k + 1 < ctas && units * (k + 1) / ctas <= unit) ++k;
+    while (k > 0 && units * k / ctas > unit) --k;
+    return k;
+  };
+  float v[F] = {};
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (n > 0) {
+    const int k0 = cta_of(from), k1 = cta_of(to - 1);
+    if (k0 == k1) return;   // that CTA has written the row
+    auto part_of = [&](int k) -> const Part<HD, R>& { return parts[2 * k + (k == k0 && units * k / ctas < from)]; };
+    float top = -INFINITY, sum = 0.f;
+    auto empty = [&](int k) { return units * k / ctas == units * (k + 1) / ctas; };   // more CTAs than blocks
+    for (int k = k0 + lane; k <= k1; k += 32)
+      if (!empty(k)) top = fmaxf(top, part_of(k).ml[r].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int k = k0; k <= k1; ++k) {
+      if (empty(k)) continue;
+      const float2 p = part_of(k).ml[r];
+      const float f = p.x == -INFINITY ? 1.f : ptx::ex2(p.x - top);
+      sum += f * p.y;
+      if (mine)
+#pragma unroll
+        for (int e = 0; e < F; ++e) v[e] = fmaf(f, part_of(k).acc[r][lane * F + e], v[e]);
+    }
+    ml = make_float2(top, sum);
+  }
+  const int l = r / a.group, head = hk * a.group + r % a.group;
+  if (mine) store_features<F>(static_cast<T*>(a.out) + ((int64_t)b * g.L + l) * g.d + (int64_t)head * HD + lane * F, v, ml.y != 0.f ? 1.f / ml.y : 0.f);
+  if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * g.heads + head) * g.L + l] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * LN2 : -INFINITY;
+}
+
+// Small steps: CTAs per (stream, key head, tile) until every SM has one, as long as each still gets a turn of its warps where the tables are full.
 inline int split_keys(const Geometry& g, const CachedArgs& a, int n_sm, int tiles, int blocks_a_turn) {
   int split = 1;
   while (split < MAX_CLUSTER && (int64_t)g.batch * a.c.kv_heads * tiles * split < n_sm && 3 * a.c.blocks > split * WARPS * blocks_a_turn) split *= 2;
   return split;
 }
+// Even shares for all CTAs that fit the SMs: one tile of rows, and four turns of every warp or more where the tables are full.
+template <int HD> bool even_shares(const Geometry& g, const CachedArgs& a, int tiles, int n_sm) {
+  return tiles == 1 && (int64_t)g.batch * a.c.kv_heads * 3 * a.c.blocks >= (int64_t)2 * n_sm * WARPS * Ring<HD>::B * 4;
+}
 
 template <typename T, int HD, int KIND, int NT>
-cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st) {
+cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch) {
+  constexpr int R = 8 * NT;
   const auto kernel = cached_attention_kernel<T, HD, KIND, NT>;
-  constexpr int bytes = (int)sizeof(PartRoom<HD, 8 * NT>);
+  constexpr int bytes = std::max((int)sizeof(PartRoom<HD, R>), WARPS * Ring<HD>::BYTES);
   static_assert(WARPS == 8 && MAX_CLUSTER == 8, "join_sums takes either");
   int n_sm = 0;
-  const cudaError_t e = sm_count_and_smem_once(reinterpret_cast<const void*>(kernel), bytes, &n_sm);
+  cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
   if (e != cudaSuccess) return e;
-  const int tiles = (a.rows + 8 * NT - 1) / (8 * NT);
+  const int tiles = (a.rows + R - 1) / R, ctas = RESIDENT<T, NT> * n_sm;
   if (tiles > 65535) return cudaErrorNotSupported;
-  a.split = split_keys(g, a, n_sm, tiles, GROUP<HD>);
+  const bool even = even_shares<HD>(g, a, tiles, n_sm);
+  const size_t need = even ? 2 * ctas * sizeof(Part<HD, R>) + sizeof(int) * ((size_t)g.batch + 1) : 0;
+  if (scratch != nullptr) {
+    *scratch = need;
+    return cudaSuccess;
+  }
+  e = sm_count_and_smem_once(reinterpret_cast<const void*>(kernel), bytes, nullptr);
+  if (e != cudaSuccess) return e;
+  if (even) {
+    a.split = 1;
+    e = launch_overlapped(kernel, dim3((unsigned)ctas), dim3(THREADS), bytes, st, g, a);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(cached_join_kernel<T, HD, R>, dim3((unsigned)(((int64_t)g.batch * a.c.kv_heads * a.rows + WARPS - 1) / WARPS)), dim3(THREADS), 0, st, g, a, ctas);
+  }
+  a.parts = nullptr;
+  a.split = split_keys(g, a, n_sm, tiles, Ring<HD>::B);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.c.kv_heads * a.split), (unsigned)g.batch, (unsigned)tiles);
   cfg.blockDim = dim3(THREADS);
@@ -600,21 +870,22 @@ cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, kernel, g, a);
 }
 
-template <typename T, int HD, int KIND> cudaError_t launch_rows(const Geometry& g, CachedArgs& a, cudaStream_t st) {
-  if (a.rows <= 8) return launch_tiles<T, HD, KIND, 1>(g, a, st);
-  if (a.rows <= 16 || sizeof(T) == 4) return launch_tiles<T, HD, KIND, 2>(g, a, st);
-  if constexpr (sizeof(T) == 2) return launch_tiles<T, HD, KIND, 4>(g, a, st);
+template <typename T, int HD, int KIND> cudaError_t launch_rows(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch) {
+  if (a.rows <= 8) return launch_tiles<T, HD, KIND, 1>(g, a, st, scratch);
+  if constexpr (sizeof(T) == 2)
+    if (a.rows > 16) return launch_tiles<T, HD, KIND, 4>(g, a, st, scratch);
+  return launch_tiles<T, HD, KIND, 2>(g, a, st, scratch);
 }
-template <typename T, int KIND> cudaError_t launch_width(const Geometry& g, CachedArgs& a, cudaStream_t st) {
+template <typename T, int KIND> cudaError_t launch_width(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch) {
   switch (a.c.hd) {
-    case 8: return launch_rows<T, 8, KIND>(g, a, st);
-    case 16: return launch_rows<T, 16, KIND>(g, a, st);
-    case 32: return launch_rows<T, 32, KIND>(g, a, st);
-    default: return launch_rows<T, 64, KIND>(g, a, st);
+    case 8: return launch_rows<T, 8, KIND>(g, a, st, scratch);
+    case 16: return launch_rows<T, 16, KIND>(g, a, st, scratch);
+    case 32: return launch_rows<T, 32, KIND>(g, a, st, scratch);
+    default: return launch_rows<T, 64, KIND>(g, a, st, scratch);
   }
 }
-template <typename T> cudaError_t launch_kind(const Geometry& g, CachedArgs& a, cudaStream_t st) {
-  return a.c.kind == GSIT_CACHE_INT8 ? launch_width<T, GSIT_CACHE_INT8>(g, a, st) : launch_width<T, GSIT_CACHE_E4M3>(g, a, st);
+template <typename T> cudaError_t launch_kind(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch) {
+  return a.c.kind == GSIT_CACHE_INT8 ? launch_width<T, GSIT_CACHE_INT8>(g, a, st, scratch) : launch_width<T, GSIT_CACHE_E4M3>(g, a, st, scratch);
 }
 
 }  // namespace

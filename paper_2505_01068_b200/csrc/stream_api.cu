@@ -41,7 +41,7 @@ gsit_status cache_of(const gsit_cache* c, const Geometry& g, Cache* out) {
   if ((c->head_dim != 8 && c->head_dim != 16 && c->head_dim != 32 && c->head_dim != 64) || c->kv_heads > 65535) return GSIT_ERR_UNSUPPORTED;
   for (const void* p : {(const void*)c->keys, (const void*)c->values, (const void*)c->open_keys, (const void*)c->open_values})
     if (p == nullptr || !aligned(p, 16)) return GSIT_ERR_INVALID_ARG;
-  if (c->key_scale == nullptr || c->value_scale == nullptr || !aligned(c->key_scale, 4) || !aligned(c->value_scale, 4) || !aligned(c->times, 4))
+  if (c->key_scale == nullptr || c->value_scale == nullptr || !aligned(c->key_scale, 4) || !aligned(c->value_scale, 4) || !aligned(c->times, 16))
     return GSIT_ERR_INVALID_ARG;
   return GSIT_OK;
 }
@@ -70,9 +70,14 @@ gsit_status attention_args(const gsit_shape* shape, const gsit_score_rule* r, co
   const float scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)g->hd);
   constexpr float LOG2E = 1.4426950408889634f;
   a->softcap = r->softcap > 0.f ? r->softcap : 0.f;
-  a->inner = a->softcap > 0.f ? scale / a->softcap : scale * LOG2E;
+  // tanh(y) is taken as it is for float and by e^2y in base 2 for bf16
+  a->inner = a->softcap > 0.f ? scale / a->softcap * (shape->dtype == GSIT_BF16 ? 2.f * LOG2E : 1.f) : scale * LOG2E;
   a->outer = a->softcap * LOG2E;
   return isfinite(a->inner) && isfinite(a->outer) ? GSIT_OK : GSIT_ERR_INVALID_ARG;
+}
+
+cudaError_t launch_attention(const Geometry& g, int32_t dtype, CachedArgs& a, cudaStream_t st, size_t* scratch) {
+  return dtype == GSIT_BF16 ? launch_cached_bf16(g, a, st, scratch) : launch_cached_f32(g, a, st, scratch);
 }
 
 }  // namespace
@@ -125,24 +130,31 @@ gsit_status gsit_cache_read(const gsit_shape* shape, const gsit_cache* cache, vo
 size_t gsit_cached_attention_workspace(const gsit_shape* shape, const gsit_score_rule* rule, const gsit_cache* cache) {
   Geometry g;
   CachedArgs a;
-  return cache != nullptr && attention_args(shape, rule, cache, {cache->times, 0, 0}, &g, &a) == GSIT_OK ? 0 : (size_t)-1;
+  if (cache == nullptr || attention_args(shape, rule, cache, {cache->times, 0, 0}, &g, &a) != GSIT_OK) return (size_t)-1;
+  size_t need = 0;
+  return launch_attention(g, cache->dtype, a, nullptr, &need) == cudaSuccess ? need : (size_t)-1;
 }
 
 gsit_status gsit_im_cached_attention_fwd(const gsit_shape* shape, const gsit_score_rule* rule, const gsit_cache* cache, const void* q, int64_t q_row_stride,
-                                         const float* times, int64_t times_batch_stride, int64_t times_row_stride, void* out, float* lse, void*, size_t,
-                                         gsit_stream stream) {
+                                         const float* times, int64_t times_batch_stride, int64_t times_row_stride, void* out, float* lse, void* workspace,
+                                         size_t workspace_bytes, gsit_stream stream) {
   Geometry g;
   CachedArgs a;
   const gsit_status st = attention_args(shape, rule, cache, {times, times_batch_stride, times_row_stride}, &g, &a);
   if (st != GSIT_OK) return st;
   if (!rows_ok(q, q_row_stride, g.d, cache->dtype) || out == nullptr || !aligned(out, cache->dtype == GSIT_BF16 ? 2 : 4) || !aligned(lse, 4)) return GSIT_ERR_INVALID_ARG;
+  size_t need = 0;
+  const cudaError_t e = launch_attention(g, cache->dtype, a, nullptr, &need);
+  if (e != cudaSuccess) return status_of(e);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return GSIT_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return GSIT_ERR_INVALID_ARG;
   if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
   a.q = q;
   a.ldq = q_row_stride;
   a.out = out;
   a.lse = lse;
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return status_of(cache->dtype == GSIT_BF16 ? launch_cached_bf16(g, a, s) : launch_cached_f32(g, a, s));
+  a.parts = static_cast<float*>(workspace);
+  return status_of(launch_attention(g, cache->dtype, a, static_cast<cudaStream_t>(stream), nullptr));
 }
 
 }  // extern "C"

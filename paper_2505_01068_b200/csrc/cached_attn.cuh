@@ -194,7 +194,7 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
   using Room = PartRoom<HD, R>;
   extern __shared__ __align__(128) uint8_t smem[];
   Room& room = *reinterpret_cast<Room*>(smem);             // where the rings were, when they are done with
-  __shared__ QueryRow s_row[R];
+  __shared__ QueryRow s_row[WARPS][R];
   __shared__ BlockInfo s_info[WARPS][STAGES][B];
   __shared__ __align__(8) uint64_t s_bar[WARPS][STAGES];
   __shared__ uint32_t s_gave_up;
@@ -220,13 +220,31 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
   auto walk = [&](int b, int hk, int row0, int n_rows, const BlockList& list, int lo, int hi) {
   const int first = lo + warp * B, last = min(hi, list.full);
   constexpr int turn = WARPS * B;
+  // Everything that is waited for is asked for as early as it can be: the queries, pages, the first blocks, what the rows are.
+  uint32_t raw[NT][KS][2][TERMS];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = min(8 * n + gr, n_rows - 1) + row0;
+    const T* q = static_cast<const T*>(a.q) + ((int64_t)b * g.L + r / a.group) * a.ldq + (int64_t)(hk * a.group + r % a.group) * HD + 2 * t;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int h = 0; h < (HD > 8 ? 2 : 1); ++h) {
+        if constexpr (sizeof(T) == 2) raw[n][k][h][0] = *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * h);
+        else {
+          const uint2 v = *reinterpret_cast<const uint2*>(q + 16 * k + 8 * h);
+          raw[n][k][h][0] = v.x;
+          raw[n][k][h][TERMS - 1] = v.y;
+        }
+      }
+  }
   // lanes know where the blocks of the warp's next 32 / B turns lie, and each sees to its own: copies into the stage, and what is known of it
   int ahead = first, known = 0;
   int64_t head = -1;
   const float* moments = nullptr;
   BlockInfo info = {0.f, 0.f, 3, 0};
   uint32_t to = stage;
-  auto request = [&]() {
+  auto copy = [&]() {
     if (known == 0) {
       const int i = ahead + lane / B * turn + lane % B, s = list.segment(i), j = i - (s == 0 ? 0 : s == 1 ? list.upto[0] : list.upto[1]);
       head = -1;
@@ -243,39 +261,48 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
       known = 32 / B;
     }
     const int from = (32 / B - known) * B;
-    if (lane >= from && lane < from + B) {
+    if (lane >= from && lane < from + B && head >= 0) {
       const uint32_t bar = bars + 8 * to, at = ring + (to * B + lane - from) * RingOf::BLOCK;
-      s_info[warp][to][lane - from] = info;
-      ptx::mbar_expect_tx(bar, head < 0 ? 0 : 2 * RingOf::MATRIX + (moments != nullptr ? RingOf::MOMENTS : 0));
-      if (head >= 0) {
-        bulk_copy(at, c.keys + head * RingOf::MATRIX, RingOf::MATRIX, bar);
-        bulk_copy(at + RingOf::MATRIX, c.values + head * RingOf::MATRIX, RingOf::MATRIX, bar);
-        if (moments != nullptr) bulk_copy(at + 2 * RingOf::MATRIX, moments, RingOf::MOMENTS, bar);
-      }
+      bulk_copy(at, c.keys + head * RingOf::MATRIX, RingOf::MATRIX, bar);
+      bulk_copy(at + RingOf::MATRIX, c.values + head * RingOf::MATRIX, RingOf::MATRIX, bar);
+      if (moments != nullptr) bulk_copy(at + 2 * RingOf::MATRIX, moments, RingOf::MOMENTS, bar);
     }
     ahead += turn;
     --known;
     to = to + 1 == STAGES ? 0 : to + 1;
   };
-#pragma unroll 1
-  for (int i = 0; i < STAGES - 1; ++i)
-    if (ahead < last) request();   // under way while the rows are looked at
+  // ... behind the copies, which need not wait for the scales: what is known, and the arrival that lets the stage's phase end
+  auto tell = [&](uint32_t stage_of, int from) {
+    if (lane >= from && lane < from + B) {
+      s_info[warp][stage_of][lane - from] = info;
+      ptx::mbar_expect_tx(bars + 8 * stage_of, head < 0 ? 0 : 2 * RingOf::MATRIX + (moments != nullptr ? RingOf::MOMENTS : 0));
+    }
+  };
+  static_assert(STAGES == 3 && 32 / B >= 2, "two stages of one batch of pages are asked for ahead");
+  const bool one = first < last, two = first + turn < last;
+  if (one) copy();
+  if (two) copy();
 
   // ---- the rows: row r of a key head is row r / group of the step, head hk * group + r % group ----
-  if (tid < R) {
+  QueryRow* const rows_of = s_row[warp];
+  if (lane < R) {
     QueryRow x = {0.f, -INFINITY, 0.f, 0};
-    if (tid < n_rows) {
-      const int l = (row0 + tid) / a.group, s = segment_of(g, l), at = l - g.off(s), n = valid_rows(g, b, s);
+    if (lane < n_rows) {
+      const int l = (row0 + lane) / a.group, s = segment_of(g, l), at = l - g.off(s), n = valid_rows(g, b, s);
       if (at < n) {
-        x.time = a.times.p != nullptr ? a.times.at(b, l) : (float)(held_rows(c, g.status, b, s) - n + at);
+        if (timed) {
+          x.time = a.times.p != nullptr ? a.times.at(b, l) : (float)(held_rows(c, g.status, b, s) - n + at);
+          x.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + (row0 + lane) % a.group] * LOG2E : 0.f;
+        }
         x.limit = a.causal ? x.time : INFINITY;
-        x.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + (row0 + tid) % a.group] * LOG2E : 0.f;
         x.opens = (int)(g.allowed >> (3 * s)) & 7;
       }
     }
-    s_row[tid] = x;
+    rows_of[lane] = x;
   }
-  __syncthreads();
+  __syncwarp();
+  if (one) tell(stage, 0);
+  if (two) tell(stage + 1 == STAGES ? 0 : stage + 1, B);
 
   // ---- queries as B operands, and what brings a dot back to a score ----
   uint32_t qf[NT][TERMS][KS][2];
@@ -283,9 +310,7 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
   uint32_t col_opens = 0, every = 7;     // four bits for each column; segments that all of them are open to
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = row0 + 8 * n + gr;
-    const bool there = s_row[8 * n + gr].opens != 0;
-    const T* q = static_cast<const T*>(a.q) + ((int64_t)b * g.L + (there ? r / a.group : 0)) * a.ldq + (int64_t)(hk * a.group + (there ? r % a.group : 0)) * HD;
+    const bool there = rows_of[8 * n + gr].opens != 0;
     float2 f[KS][2];
     float top = 0.f;
 #pragma unroll
@@ -294,8 +319,8 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
       for (int h = 0; h < 2; ++h) {
         f[k][h] = make_float2(0.f, 0.f);
         if (there && (HD > 8 || h == 0)) {
-          if constexpr (sizeof(T) == 2) unpack_bf16(*reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * h + 2 * t), f[k][h].x, f[k][h].y);
-          else f[k][h] = *reinterpret_cast<const float2*>(q + 16 * k + 8 * h + 2 * t);
+          if constexpr (sizeof(T) == 2) unpack_bf16(raw[n][k][h][0], f[k][h].x, f[k][h].y);
+          else f[k][h] = make_float2(__uint_as_float(raw[n][k][h][0]), __uint_as_float(raw[n][k][h][TERMS - 1]));
         }
         top = ptx::fmax3(top, fabsf(f[k][h].x), fabsf(f[k][h].y));
       }
@@ -313,7 +338,7 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
     back[n] = make_float2(__shfl_sync(0xffffffffu, p.down, 8 * t) * a.inner, __shfl_sync(0xffffffffu, p.down, 8 * t + 4) * a.inner);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int opens = s_row[8 * n + 2 * t + e].opens;
+      const int opens = rows_of[8 * n + 2 * t + e].opens;
       col_opens |= (uint32_t)opens << (4 * (2 * n + e));
       if (8 * n + 2 * t + e < n_rows) every &= opens;   // (columns behind the last row write nothing: whatever they see)
     }
@@ -378,7 +403,7 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
         const bool m0 = (col_opens >> (8 * n + seg)) & 1u, m1 = (col_opens >> (8 * n + 4 + seg)) & 1u;
         float2 time = make_float2(0.f, 0.f), limit = time, slope2 = time;
         if (timed) {
-          const QueryRow &r0 = s_row[8 * n + 2 * t], &r1 = s_row[8 * n + 2 * t + 1];
+          const QueryRow &r0 = rows_of[8 * n + 2 * t], &r1 = rows_of[8 * n + 2 * t + 1];
           time = make_float2(r0.time, r1.time);
           limit = make_float2(r0.limit, r1.limit);
           slope2 = make_float2(-r0.slope2, -r1.slope2);
@@ -495,9 +520,95 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
         }
   };
 
+  // The open blocks, each the next warp's in turn, while the first copies are under way: rows in memory, brought to f16 by a power of two for all of a block's.
+#pragma unroll 1
+  for (int r = 0, at = list.full; r < 3; ++r) {
+    const int n = r == 0 ? list.len[0] : r == 1 ? list.len[1] : list.len[2], rows = n % CACHE_BLOCK, j = n / CACHE_BLOCK;
+    if (rows == 0) continue;
+    const int i = at++;
+    if (i < lo || i >= hi || ((max(0, last - lo) + B - 1) / B + i - max(lo, list.full)) % WARPS != warp) continue;
+    const int64_t from = open_at(c, b, r, j, hk);
+    const T* const key = static_cast<const T*>(c.open_keys) + from;
+    const T* const value = static_cast<const T*>(c.open_values) + from;
+    float times[4] = {0.f, 0.f, 0.f, 0.f};
+    if (timed) {
+      const int page = c.times == nullptr ? 0 : real_page(c, c.tables[((int64_t)b * 3 + r) * c.blocks + j]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        times[i] = c.times == nullptr ? (float)(j * CACHE_BLOCK + 8 * i + gr) : page >= 0 ? c.times[(int64_t)page * CACHE_BLOCK + 8 * i + gr] : 0.f;
+    }
+    // all of it at once into registers, as the fragments want it: pairs of features of positions 8 i + gr
+    uint32_t words[2][4][HD / 8][TERMS];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < HD / 8; ++k) {
+          const T* p = (w ? value : key) + (8 * i + gr) * HD + 8 * k + 2 * t;
+          uint2 v = make_uint2(0u, 0u);
+          if (8 * i + gr < rows) {
+            if constexpr (sizeof(T) == 2) v.x = *reinterpret_cast<const uint32_t*>(p);
+            else v = *reinterpret_cast<const uint2*>(p);
+          }
+          words[w][i][k][0] = v.x;
+          if constexpr (TERMS == 2) words[w][i][k][1] = v.y;
+        }
+    auto pair = [&](int w, int i, int k) {
+      float2 v;
+      if constexpr (sizeof(T) == 2) unpack_bf16(words[w][i][k][0], v.x, v.y);
+      else v = make_float2(__uint_as_float(words[w][i][k][0]), __uint_as_float(words[w][i][k][TERMS - 1]));
+      return v;
+    };
+    Power up[2];
+    float by[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < HD / 8; ++k) {
+          const float2 v = pair(w, i, k);
+          top = max(top, max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu));
+        }
+      top = __reduce_max_sync(0xffffffffu, top);
+      const bool broken = top >= 0x7f800000u;
+      up[w] = top > 0 && !broken ? power_for(__uint_as_float(top), 14) : Power{1.f, 1.f};
+      by[w] = broken ? __int_as_float(0x7fffffff) : up[w].down;
+      if (broken)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int k = 0; k < HD / 8; ++k)
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) words[w][i][k][e] = 0u;
+    }
+    auto term = [&](float2 v, float f, int w) {
+      v = __fmul2_rn(v, make_float2(f, f));
+      const uint32_t x = f16x2(v.x, v.y);
+      return w == 0 ? x : f16x2_rest(v.x, v.y, x);
+    };
+    attend(std::integral_constant<int, TERMS>{}, std::integral_constant<int, 0>{}, r, rows, by[0], by[1], times,
+           [&](int m, int k, int w, uint32_t (&f)[4]) {
+#pragma unroll
+             for (int i = 0; i < 4; ++i)   // position halves i % 2, feature halves i / 2
+               f[i] = HD > 8 || i < 2 ? term(pair(0, 2 * m + i % 2, HD > 8 ? 2 * k + i / 2 : 0), up[0].up, w) : 0u;
+           },
+           [&](int m, int k, int w, uint32_t (&f)[4]) {
+#pragma unroll
+             for (int i = 0; i < 4; ++i)   // feature halves i % 2, position halves i / 2; rows of features come in, turned round
+               f[i] = HD > 8 || i % 2 == 0 ? turned_round(term(pair(1, 2 * k + i / 2, HD > 8 ? 2 * m + i % 2 : 0), up[1].up, w)) : 0u;
+           });
+  }
+
 #pragma unroll 1
   for (int now = first; now < last; now += turn) {
-    if (ahead < last) request();   // into the stage that was read before this one
+    if (ahead < last) {   // into the stage that was read before this one
+      const uint32_t into = to;
+      copy();
+      tell(into, (32 / B - known - 1) * B);
+    }
     ptx::mbar_wait_warp(wait, bars + 8 * stage, phase);
 #pragma unroll
     for (int u = 0; u < B; ++u) {
@@ -542,69 +653,6 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     phase ^= stage == 0;
   }
-  // The open blocks, each the next warp's in turn: rows in memory, brought to f16 by a power of two for all of a block's.
-#pragma unroll 1
-  for (int r = 0, at = list.full; r < 3; ++r) {
-    const int n = r == 0 ? list.len[0] : r == 1 ? list.len[1] : list.len[2], rows = n % CACHE_BLOCK, j = n / CACHE_BLOCK;
-    if (rows == 0) continue;
-    const int i = at++;
-    if (i < lo || i >= hi || ((max(0, last - lo) + B - 1) / B + i - max(lo, list.full)) % WARPS != warp) continue;
-    const int64_t from = open_at(c, b, r, j, hk);
-    const T* const key = static_cast<const T*>(c.open_keys) + from;
-    const T* const value = static_cast<const T*>(c.open_values) + from;
-    float times[4] = {0.f, 0.f, 0.f, 0.f};
-    if (timed) {
-      const int page = c.times == nullptr ? 0 : real_page(c, c.tables[((int64_t)b * 3 + r) * c.blocks + j]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        times[i] = c.times == nullptr ? (float)(j * CACHE_BLOCK + 8 * i + gr) : page >= 0 ? c.times[(int64_t)page * CACHE_BLOCK + 8 * i + gr] : 0.f;
-    }
-    Power up[2];
-    bool broken[2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      constexpr int E = sizeof(T) == 2 ? 8 : 4;
-      uint32_t top = 0;
-      for (int i = lane * E; i < rows * HD; i += 32 * E) {
-        float f[E];
-        load_n(w ? value + i : key + i, f);
-#pragma unroll
-        for (int e = 0; e < E; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
-      }
-      top = __reduce_max_sync(0xffffffffu, top);
-      broken[w] = top >= 0x7f800000u;
-      up[w] = top > 0 && !broken[w] ? power_for(__uint_as_float(top), 14) : Power{1.f, 1.f};
-    }
-    auto pair = [&](const T* p, int row, bool bad, float by) {
-      float2 v = make_float2(0.f, 0.f);
-      if (row < rows && !bad) {
-        if constexpr (sizeof(T) == 2) unpack_bf16(*reinterpret_cast<const uint32_t*>(p), v.x, v.y);
-        else v = *reinterpret_cast<const float2*>(p);
-      }
-      return make_float2(v.x * by, v.y * by);
-    };
-    auto term = [&](float2 v, int w) {
-      const uint32_t x = f16x2(v.x, v.y);
-      return w == 0 ? x : f16x2_rest(v.x, v.y, x);
-    };
-    attend(std::integral_constant<int, TERMS>{}, std::integral_constant<int, 0>{}, r, rows, broken[0] ? __int_as_float(0x7fffffff) : up[0].down,
-           broken[1] ? __int_as_float(0x7fffffff) : up[1].down, times,
-           [&](int m, int k, int w, uint32_t (&f)[4]) {
-#pragma unroll
-             for (int i = 0; i < 4; ++i) {   // position halves i % 2, feature halves i / 2
-               const int row = 16 * m + 8 * (i % 2) + gr;
-               f[i] = HD > 8 || i < 2 ? term(pair(key + row * HD + 16 * k + 8 * (i / 2) + 2 * t, row, broken[0], up[0].up), w) : 0u;
-             }
-           },
-           [&](int m, int k, int w, uint32_t (&f)[4]) {
-#pragma unroll
-             for (int i = 0; i < 4; ++i) {   // feature halves i % 2, position halves i / 2; rows of features come in, turned round
-               const int row = 16 * k + 8 * (i / 2) + gr;
-               f[i] = HD > 8 || i % 2 == 0 ? turned_round(term(pair(value + row * HD + 16 * m + 8 * (i % 2) + 2 * t, row, broken[1], up[1].up), w)) : 0u;
-             }
-           });
-  }
-
   // ---- the warps' parts ----
   __syncthreads();   // nobody's ring is in use any more
 #pragma unroll
@@ -821,9 +869,12 @@ inline int split_keys(const Geometry& g, const CachedArgs& a, int n_sm, int tile
   while (split < MAX_CLUSTER && (int64_t)g.batch * a.c.kv_heads * tiles * split < n_sm && 3 * a.c.blocks > split * WARPS * blocks_a_turn) split *= 2;
   return split;
 }
-// Even shares for all CTAs that fit the SMs: one tile of rows, and four turns of every warp or more where the tables are full.
-template <int HD> bool even_shares(const Geometry& g, const CachedArgs& a, int tiles, int n_sm) {
-  return tiles == 1 && (int64_t)g.batch * a.c.kv_heads * 3 * a.c.blocks >= (int64_t)2 * n_sm * WARPS * Ring<HD>::B * 4;
+// Even shares for all CTAs that fit the SMs, or a cluster for each (stream, key head): by what a warp has to walk where the tables are full, in
+// blocks.  Streams are of unlike lengths, so that clusters wait for the longest (a third more, where they lie between half and full); the second piece of
+// a share and the joining kernel cost as much as some 12 stages.
+template <int HD> bool even_shares(const Geometry& g, const CachedArgs& a, int tiles, int ctas, int split) {
+  const int64_t pairs = (int64_t)g.batch * a.c.kv_heads, turns = pairs * 3 * a.c.blocks / (WARPS * Ring<HD>::B);
+  return tiles == 1 && turns * 4 / (3 * std::min<int64_t>(pairs * split, ctas)) > turns / ctas + 12;
 }
 
 template <typename T, int HD, int KIND, int NT>
@@ -837,7 +888,8 @@ cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st, size
   if (e != cudaSuccess) return e;
   const int tiles = (a.rows + R - 1) / R, ctas = RESIDENT<T, NT> * n_sm;
   if (tiles > 65535) return cudaErrorNotSupported;
-  const bool even = even_shares<HD>(g, a, tiles, n_sm);
+  a.split = split_keys(g, a, n_sm, tiles, Ring<HD>::B);
+  const bool even = even_shares<HD>(g, a, tiles, ctas, a.split);
   const size_t need = even ? 2 * ctas * sizeof(Part<HD, R>) + sizeof(int) * ((size_t)g.batch + 1) : 0;
   if (scratch != nullptr) {
     *scratch = need;
@@ -852,7 +904,6 @@ cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st, size
     return launch_overlapped(cached_join_kernel<T, HD, R>, dim3((unsigned)(((int64_t)g.batch * a.c.kv_heads * a.rows + WARPS - 1) / WARPS)), dim3(THREADS), 0, st, g, a, ctas);
   }
   a.parts = nullptr;
-  a.split = split_keys(g, a, n_sm, tiles, Ring<HD>::B);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.c.kv_heads * a.split), (unsigned)g.batch, (unsigned)tiles);
   cfg.blockDim = dim3(THREADS);

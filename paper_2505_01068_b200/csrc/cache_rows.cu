@@ -8,7 +8,9 @@
 //
 // x / scale is rounded once: the quotient in float is brought to the odd one of its two neighbours wherever a remainder is left (its sign
 // says on which side), so that the rounding to 8 bits that follows meets a tie only where there is one.
-#include <cuda_fp8.h>
+#include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -25,65 +27,61 @@ __device__ __forceinline__ void copies_done() {
   asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
   __syncwarp();
 }
-__device__ __forceinline__ uint32_t transposed8(uint32_t v) {   // of the 8 x 8 matrix of 16-bit elements that the warp holds
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
+// Four 8 x 8 matrices of 16-bit elements between registers and shared memory, as they lie or turned round; lane l gives the address of row l % 8 of matrix l / 8.
+template <bool TURN> __device__ __forceinline__ void load_matrices(uint32_t at, uint32_t (&r)[4]) {
+  if constexpr (TURN)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+  else
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+template <bool TURN> __device__ __forceinline__ void store_matrices(uint32_t at, const uint32_t (&r)[4]) {
+  if constexpr (TURN)
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+  else
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 
-// Eight values of a lane, bytes 8 u .. 8 u + 7 of its piece(s) of the page: [c][h][e], or heads of 8: all of them.  `at`: the staged matrix.
-template <typename T, int HD, bool VALUES> __device__ __forceinline__ void staged(const uint8_t* at, int lane, int u, float (&f)[8]) {
-  const int g = lane >> 2, t = lane & 3;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {   // pairs: c = i / 2, h = i % 2;  heads of 8: keys m = i / 2, h = i % 2, values half = i / 2, c = i % 2
-    int row, col;                 // of the 16-bit pair's operand row (g) and first column (2 t)
-    if constexpr (HD == 8) {
-      row = VALUES ? g : 16 * (i / 2) + 8 * (i % 2) + g;
-      col = VALUES ? 16 * (i / 2) + 8 * (i % 2) + 2 * t : 2 * t;
-    } else {
-      row = (VALUES ? 16 * (u / 2) : 16 * (u % 2)) + 8 * (i % 2) + g;
-      col = (VALUES ? 16 * (u % 2) : 16 * (u / 2)) + 8 * (i / 2) + 2 * t;
-    }
-    if constexpr (!VALUES) {
-      const T* p = reinterpret_cast<const T*>(at + row * PITCH<T, HD>) + col;
-      if constexpr (sizeof(T) == 2) unpack_bf16(*reinterpret_cast<const uint32_t*>(p), f[2 * i], f[2 * i + 1]);
-      else {
-        const float2 v = *reinterpret_cast<const float2*>(p);
-        f[2 * i] = v.x;
-        f[2 * i + 1] = v.y;
-      }
-    } else if constexpr (sizeof(T) == 2) {   // positions 8 (col / 8) + g, features 8 (row / 8) + 2 t, turned round
-      const int position = col / 8 * 8 + g, feature = row / 8 * 8 + 2 * t;
-      unpack_bf16(transposed8(*reinterpret_cast<const uint32_t*>(reinterpret_cast<const T*>(at + position * PITCH<T, HD>) + feature)), f[2 * i], f[2 * i + 1]);
-    } else {
-      f[2 * i] = reinterpret_cast<const T*>(at + col * PITCH<T, HD>)[row];
-      f[2 * i + 1] = reinterpret_cast<const T*>(at + (col + 1) * PITCH<T, HD>)[row];
-    }
-  }
+// Unit u of a lane, bytes 8 u .. 8 u + 7 of its pieces of the page, is eight values, four pairs i = 2 c + h (heads of 8: all there is; keys i = 2 m + h, values
+// i = 2 half + c): pair i is row g of an 8 x 8 matrix of positions x features (values: features x positions), columns 2 t and 2 t + 1.  Where
+// matrix i of the unit begins in the staged rows:
+template <int HD, bool VALUES> __device__ __forceinline__ int2 matrix_at(int u, int i) {   // (position, feature)
+  if constexpr (HD == 8) return make_int2(8 * i, 0);
+  const int c = i / 2, h = i % 2;
+  return VALUES ? make_int2(16 * (u % 2) + 8 * c, 16 * (u / 2) + 8 * h) : make_int2(16 * (u % 2) + 8 * h, 16 * (u / 2) + 8 * c);
 }
-// The other way: eight values to the staged matrix.
-template <typename T, int HD, bool VALUES> __device__ __forceinline__ void stage(uint8_t* at, int lane, int u, const float (&f)[8]) {
+// One unit of a staged matrix as pairs: 16 bits each as they are, or floats.
+template <int HD, bool VALUES> __device__ __forceinline__ void staged(const uint8_t* at, int lane, int u, uint32_t (&w)[4]) {
+  const int2 m = matrix_at<HD, VALUES>(u, lane / 8);
+  load_matrices<VALUES>(smem_u32(at) + (m.x + lane % 8) * PITCH<__nv_bfloat16, HD> + 2 * m.y, w);
+}
+template <int HD, bool VALUES> __device__ __forceinline__ void staged(const uint8_t* at, int lane, int u, float2 (&f)[4]) {
   const int g = lane >> 2, t = lane & 3;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    int row, col;
-    if constexpr (HD == 8) {
-      row = VALUES ? g : 16 * (i / 2) + 8 * (i % 2) + g;
-      col = VALUES ? 16 * (i / 2) + 8 * (i % 2) + 2 * t : 2 * t;
-    } else {
-      row = (VALUES ? 16 * (u / 2) : 16 * (u % 2)) + 8 * (i % 2) + g;
-      col = (VALUES ? 16 * (u % 2) : 16 * (u / 2)) + 8 * (i / 2) + 2 * t;
-    }
-    if constexpr (!VALUES) {
-      T* p = reinterpret_cast<T*>(at + row * PITCH<T, HD>) + col;
-      if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(p) = ptx::pack_bf16(f[2 * i], f[2 * i + 1]);
-      else *reinterpret_cast<float2*>(p) = make_float2(f[2 * i], f[2 * i + 1]);
-    } else if constexpr (sizeof(T) == 2) {
-      const int position = col / 8 * 8 + g, feature = row / 8 * 8 + 2 * t;
-      *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(at + position * PITCH<T, HD>) + feature) = transposed8(ptx::pack_bf16(f[2 * i], f[2 * i + 1]));
-    } else {
-      reinterpret_cast<T*>(at + col * PITCH<T, HD>)[row] = f[2 * i];
-      reinterpret_cast<T*>(at + (col + 1) * PITCH<T, HD>)[row] = f[2 * i + 1];
+    const int2 m = matrix_at<HD, VALUES>(u, i);
+    if constexpr (VALUES)
+      f[i] = make_float2(reinterpret_cast<const float*>(at + (m.x + 2 * t) * PITCH<float, HD>)[m.y + g], reinterpret_cast<const float*>(at + (m.x + 2 * t + 1) * PITCH<float, HD>)[m.y + g]);
+    else
+      f[i] = *reinterpret_cast<const float2*>(at + (m.x + g) * PITCH<float, HD> + 4 * (m.y + 2 * t));
+  }
+}
+// ... and the other way.
+template <typename T, int HD, bool VALUES> __device__ __forceinline__ void stage(uint8_t* at, int lane, int u, const float2 (&f)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    const int2 m = matrix_at<HD, VALUES>(u, lane / 8);
+    const uint32_t w[4] = {ptx::pack_bf16(f[0].x, f[0].y), ptx::pack_bf16(f[1].x, f[1].y), ptx::pack_bf16(f[2].x, f[2].y), ptx::pack_bf16(f[3].x, f[3].y)};
+    store_matrices<VALUES>(smem_u32(at) + (m.x + lane % 8) * PITCH<T, HD> + 2 * m.y, w);
+  } else {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int2 m = matrix_at<HD, VALUES>(u, i);
+      if constexpr (VALUES) {
+        reinterpret_cast<T*>(at + (m.x + 2 * t) * PITCH<T, HD>)[m.y + g] = f[i].x;
+        reinterpret_cast<T*>(at + (m.x + 2 * t + 1) * PITCH<T, HD>)[m.y + g] = f[i].y;
+      } else {
+        *reinterpret_cast<float2*>(at + (m.x + g) * PITCH<T, HD> + 4 * (m.y + 2 * t)) = f[i];
+      }
     }
   }
 }
@@ -91,65 +89,73 @@ template <typename T, int HD, bool VALUES> __device__ __forceinline__ void stage
 template <int HD> constexpr int UNITS = HD == 8 ? 1 : HD / 8;   // of eight bytes of a lane
 template <int HD> __device__ __forceinline__ int unit_at(int lane, int u) { return HD == 8 ? 8 * lane : 512 * (u / 2) + 16 * lane + 8 * (u % 2); }
 
-// x / s to one of its two neighbours in float, the odd one unless it is exact
-__device__ __forceinline__ float odd_quotient(float x, float s, float inv) {
-  float t = x * inv;
-  t = fmaf(fmaf(-t, s, x), inv, t);
-  const float rest = fmaf(-t, s, x);
-  int bits = __float_as_int(t);
-  if (rest != 0.f && (bits & 1) == 0) bits += ((__float_as_int(rest) ^ bits) < 0 && t != 0.f) ? -1 : 1;
-  return __int_as_float(bits);
+// x / s for pairs, to one of its two neighbours in float, the odd one unless it is exact.  The first quotient's remainder brings it to the nearest float (the
+// quotient itself, where that is one); the second remainder, which is exact, brings that to the float next to zero, where nothing is left but to set the
+// last bit if there was any remainder.
+__device__ __forceinline__ float2 odd_quotients(float2 x, float s, float inv) {
+  const float2 less = make_float2(-s, -s), by = make_float2(inv, inv);
+  float2 t = __fmul2_rn(x, by);
+  t = __ffma2_rn(__ffma2_rn(t, less, x), by, t);
+  const float2 rest = __ffma2_rn(t, less, x);
+  t = __ffma2_rz(rest, by, t);
+  return make_float2(__int_as_float(__float_as_int(t.x) | (rest.x != 0.f)), __int_as_float(__float_as_int(t.y) | (rest.y != 0.f)));
 }
-__device__ __forceinline__ uint32_t bytes4(int kind, float a, float b, float c, float d) {
-  if (kind == GSIT_CACHE_INT8) {
-    const int i = __float2int_rn(fminf(fmaxf(a, -127.f), 127.f)), j = __float2int_rn(fminf(fmaxf(b, -127.f), 127.f));
-    const int k = __float2int_rn(fminf(fmaxf(c, -127.f), 127.f)), l = __float2int_rn(fminf(fmaxf(d, -127.f), 127.f));
-    return (uint32_t)(i & 255) | (uint32_t)(j & 255) << 8 | (uint32_t)(k & 255) << 16 | (uint32_t)l << 24;
+// Four quotients (at most 127 or 448 and a little) rounded to bytes.  Integers: the last byte of 3 * 2^22 + the quotient.
+template <int KIND> __device__ __forceinline__ uint32_t bytes4(float2 a, float2 b) {
+  if constexpr (KIND == GSIT_CACHE_INT8) {
+    const float2 big = make_float2(12582912.f, 12582912.f), x = __fadd2_rn(a, big), y = __fadd2_rn(b, big);
+    return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040), __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
+  } else {
+    uint32_t w;
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}" : "=r"(w) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return w;
   }
-  uint16_t lo, hi;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-  return (uint32_t)lo | (uint32_t)hi << 16;
 }
-__device__ __forceinline__ void values4(int kind, uint32_t w, float (&f)[4]) {
-  if (kind == GSIT_CACHE_INT8) {
+template <int KIND> __device__ __forceinline__ void values4(uint32_t w, float2 (&f)[2]) {
+  if constexpr (KIND == GSIT_CACHE_INT8) {
+    f[0] = make_float2((float)(int8_t)w, (float)(int8_t)(w >> 8));
+    f[1] = make_float2((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24));
+  } else {
+    uint32_t h[2];
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(h[0]), "=r"(h[1]) : "r"(w));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = (float)(int8_t)(w >> (8 * i));
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(w >> (16 * i))));
-    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    f[2 * i] = v.x;
-    f[2 * i + 1] = v.y;
+    for (int i = 0; i < 2; ++i) f[i] = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
   }
 }
+// Largest magnitude of a pair, in order as integers, NaN above them all.
+__device__ __forceinline__ uint32_t magnitude(uint32_t w) { return max(w << 16 & 0x7fff0000u, w & 0x7fff0000u); }
+__device__ __forceinline__ uint32_t magnitude(float2 v) { return max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu); }
+__device__ __forceinline__ float2 as_floats(uint32_t w) {
+  float2 v;
+  unpack_bf16(w, v.x, v.y);
+  return v;
+}
+__device__ __forceinline__ float2 as_floats(float2 v) { return v; }
 
 // One staged matrix into a page's head.
-template <typename T, int HD, bool VALUES>
-__device__ __forceinline__ void quantise(int kind, const uint8_t* at, int lane, uint8_t* bytes, float* scale) {
+template <typename T, int HD, int KIND, bool VALUES>
+__device__ __forceinline__ void quantise(const uint8_t* at, int lane, uint8_t* bytes, float* scale) {
   constexpr int U = UNITS<HD>;
-  float f[U][8];
-  uint32_t top = 0;   // magnitudes in order as integers, NaN above them all
+  using Pair = std::conditional_t<sizeof(T) == 2, uint32_t, float2>;
+  Pair x[U][4];
+  uint32_t top = 0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    staged<T, HD, VALUES>(at, lane, u, f[u]);
+    staged<HD, VALUES>(at, lane, u, x[u]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[u][i]) & 0x7fffffffu);
+    for (int i = 0; i < 4; ++i) top = max(top, magnitude(x[u][i]));
   }
   top = __reduce_max_sync(0xffffffffu, top);
   const bool broken = top >= 0x7f800000u;
-  const float s = broken ? 1.f : fmaxf(__fdiv_rn(__uint_as_float(top), kind == GSIT_CACHE_INT8 ? 127.f : 448.f), LEAST_SCALE), inv = __frcp_rn(s);
+  const float s = broken ? 1.f : fmaxf(__fdiv_rn(__uint_as_float(top), KIND == GSIT_CACHE_INT8 ? 127.f : 448.f), LEAST_SCALE), inv = __frcp_rn(s);
+  if (lane == 0) *scale = broken ? __int_as_float(0x7fffffff) : s;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    float t[8];
+    uint32_t w[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = broken ? 0.f : odd_quotient(f[u][i], s, inv);
-    *reinterpret_cast<uint2*>(bytes + unit_at<HD>(lane, u)) = make_uint2(bytes4(kind, t[0], t[1], t[2], t[3]), bytes4(kind, t[4], t[5], t[6], t[7]));
+    for (int e = 0; e < 2; ++e) w[e] = bytes4<KIND>(odd_quotients(as_floats(x[u][2 * e]), s, inv), odd_quotients(as_floats(x[u][2 * e + 1]), s, inv));
+    *reinterpret_cast<uint2*>(bytes + unit_at<HD>(lane, u)) = broken ? make_uint2(0u, 0u) : make_uint2(w[0], w[1]);
   }
-  if (lane == 0) *scale = broken ? __int_as_float(0x7fffffff) : s;
 }
 
 // What a warp works on: block `chunk` of those that a step's rows of segment s of stream b lie in, one key head.
@@ -195,7 +201,7 @@ struct RowArgs {
   int chunks[3];
 };
 
-template <typename T, int HD>
+template <typename T, int HD, int KIND>
 __global__ void __launch_bounds__(THREADS) cache_append_kernel(const __grid_constant__ Geometry g, const __grid_constant__ RowArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   constexpr int VECS = HD * (int)sizeof(T) / 16;   // of a row
@@ -208,17 +214,18 @@ __global__ void __launch_bounds__(THREADS) cache_append_kernel(const __grid_cons
   if (!find_piece(blockIdx.x * WARPS + warp, a.chunks, g.batch, c.kv_heads, &p)) return;
   const int64_t row0 = (int64_t)p.b * g.L + g.off(p.s);
   const int32_t* const slots = a.slots + row0;
+  const int slot0 = slots[0], held = held_rows(c, g.status, p.b, p.s);   // asked for together
   const int n = leading_rows(slots, g.len(p.s), lane);
   if (n == 0) return;
   // the rows [i0, i1) of the segment lie in this block, from place `o` on
-  const int place0 = slots[0] % CACHE_BLOCK, i0 = max(0, p.chunk * CACHE_BLOCK - place0), i1 = min(n, (p.chunk + 1) * CACHE_BLOCK - place0);
+  const int place0 = slot0 % CACHE_BLOCK, i0 = max(0, p.chunk * CACHE_BLOCK - place0), i1 = min(n, (p.chunk + 1) * CACHE_BLOCK - place0);
   if (i0 >= i1) return;
   const int o = p.chunk == 0 ? place0 : 0, slot = slots[i0], page = slot < 0 ? -1 : real_page(c, slot / CACHE_BLOCK);
   if (page < 0) {
     raise_flag(g, GSIT_DEVFLAG_CLAMPED);
     return;
   }
-  const int block = (held_rows(c, g.status, p.b, p.s) - n + i0) / CACHE_BLOCK;
+  const int block = (held - n + i0) / CACHE_BLOCK;
   if (c.times != nullptr && p.head == 0 && i0 + lane < i1) c.times[(int64_t)page * CACHE_BLOCK + o + lane] = a.times.at(p.b, g.off(p.s) + i0 + lane);
   const T* const k = static_cast<const T*>(a.k) + (row0 + i0) * a.ldk + (int64_t)p.head * HD;
   const T* const v = static_cast<const T*>(a.v) + (row0 + i0) * a.ldv + (int64_t)p.head * HD;
@@ -251,11 +258,11 @@ __global__ void __launch_bounds__(THREADS) cache_append_kernel(const __grid_cons
   copies_done();
   if (shared && p.chunk == 0) keep_open(0, tail, k + (n - tail) * a.ldk, v + (n - tail) * a.ldv);   // (i0 is 0 here)
   const int64_t to = (int64_t)page * c.kv_heads + p.head;
-  quantise<T, HD, false>(c.kind, stage_k, lane, c.keys + to * (CACHE_BLOCK * HD), c.key_scale + to);
-  quantise<T, HD, true>(c.kind, stage_v, lane, c.values + to * (CACHE_BLOCK * HD), c.value_scale + to);
+  quantise<T, HD, KIND, false>(stage_k, lane, c.keys + to * (CACHE_BLOCK * HD), c.key_scale + to);
+  quantise<T, HD, KIND, true>(stage_v, lane, c.values + to * (CACHE_BLOCK * HD), c.value_scale + to);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int KIND>
 __global__ void __launch_bounds__(THREADS) cache_read_kernel(const __grid_constant__ Geometry g, const __grid_constant__ RowArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   constexpr int VECS = HD * (int)sizeof(T) / 16, U = UNITS<HD>;
@@ -294,51 +301,63 @@ __global__ void __launch_bounds__(THREADS) cache_read_kernel(const __grid_consta
     y[u] = page < 0 ? make_uint2(0, 0) : *reinterpret_cast<const uint2*>(c.values + from * (CACHE_BLOCK * HD) + unit_at<HD>(lane, u));
   }
   const float ks = page < 0 ? 0.f : c.key_scale[from], vs = page < 0 ? 0.f : c.value_scale[from];
-  uint8_t* const stage_k = smem + warp * 2 * STAGE<T, HD>;
-  uint8_t* const stage_v = stage_k + STAGE<T, HD>;
-  auto spread = [&](const uint2& w, float s, float (&f)[8]) {
-    float lo[4], hi[4];
-    values4(c.kind, w.x, lo);
-    values4(c.kind, w.y, hi);
+  // keys, then values, through one staged matrix: a warp that takes little shared memory has many beside it
+  uint8_t* const staging = smem + warp * STAGE<T, HD>;
+  auto spread = [&](const uint2& w, float s, float2 (&f)[4]) {
+    float2 lo[2], hi[2];
+    values4<KIND>(w.x, lo);
+    values4<KIND>(w.y, hi);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[i] = lo[i] * s;
-      f[4 + i] = hi[i] * s;
+    for (int i = 0; i < 2; ++i) {
+      f[i] = __fmul2_rn(lo[i], make_float2(s, s));
+      f[2 + i] = __fmul2_rn(hi[i], make_float2(s, s));
     }
+  };
+  auto write = [&](T* to, int64_t ld) {
+    __syncwarp();
+    for (int i = lane; i < rows * VECS; i += 32) {
+      const int row = i / VECS, at = i % VECS * (16 / (int)sizeof(T));
+      *reinterpret_cast<uint4*>(to + row * ld + at) = *reinterpret_cast<const uint4*>(staging + row * PITCH<T, HD> + i % VECS * 16);
+    }
+    __syncwarp();
   };
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    float f[8];
+    float2 f[4];
     spread(x[u], ks, f);
-    stage<T, HD, false>(stage_k, lane, u, f);
+    stage<T, HD, false>(staging, lane, u, f);
+  }
+  write(k, a.ldk);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float2 f[4];
     spread(y[u], vs, f);
-    stage<T, HD, true>(stage_v, lane, u, f);
+    stage<T, HD, true>(staging, lane, u, f);
   }
-  __syncwarp();
-  for (int i = lane; i < rows * VECS; i += 32) {
-    const int row = i / VECS, at = i % VECS * (16 / (int)sizeof(T)), in = row * PITCH<T, HD> + i % VECS * 16;
-    *reinterpret_cast<uint4*>(k + row * a.ldk + at) = *reinterpret_cast<const uint4*>(stage_k + in);
-    *reinterpret_cast<uint4*>(v + row * a.ldv + at) = *reinterpret_cast<const uint4*>(stage_v + in);
-  }
+  write(v, a.ldv);
 }
 
-template <typename T, int HD, bool APPEND> cudaError_t launch(const Geometry& g, const RowArgs& a, cudaStream_t st) {
-  const auto kernel = APPEND ? cache_append_kernel<T, HD> : cache_read_kernel<T, HD>;
-  constexpr int bytes = WARPS * 2 * STAGE<T, HD>;
+template <typename T, int HD, int KIND, bool APPEND> cudaError_t launch(const Geometry& g, const RowArgs& a, cudaStream_t st) {
+  const auto kernel = APPEND ? cache_append_kernel<T, HD, KIND> : cache_read_kernel<T, HD, KIND>;
+  constexpr int bytes = WARPS * (APPEND ? 2 : 1) * STAGE<T, HD>;
   const cudaError_t e = sm_count_and_smem_once(reinterpret_cast<const void*>(kernel), bytes, nullptr);
   if (e != cudaSuccess) return e;
   const int64_t items = (int64_t)g.batch * (a.chunks[0] + a.chunks[1] + a.chunks[2]) * a.c.kv_heads, grid = (items + WARPS - 1) / WARPS;
   if (grid > 0x7fffffff / WARPS) return cudaErrorNotSupported;
   return launch_overlapped(kernel, dim3((unsigned)grid), dim3(THREADS), bytes, st, g, a);
 }
-template <bool APPEND> cudaError_t launch_any(const Geometry& g, int dtype, const RowArgs& a, cudaStream_t st) {
-  const bool half = dtype == GSIT_BF16;
+template <typename T, int KIND, bool APPEND> cudaError_t launch_width(const Geometry& g, const RowArgs& a, cudaStream_t st) {
   switch (a.c.hd) {
-    case 8: return half ? launch<__nv_bfloat16, 8, APPEND>(g, a, st) : launch<float, 8, APPEND>(g, a, st);
-    case 16: return half ? launch<__nv_bfloat16, 16, APPEND>(g, a, st) : launch<float, 16, APPEND>(g, a, st);
-    case 32: return half ? launch<__nv_bfloat16, 32, APPEND>(g, a, st) : launch<float, 32, APPEND>(g, a, st);
-    default: return half ? launch<__nv_bfloat16, 64, APPEND>(g, a, st) : launch<float, 64, APPEND>(g, a, st);
+    case 8: return launch<T, 8, KIND, APPEND>(g, a, st);
+    case 16: return launch<T, 16, KIND, APPEND>(g, a, st);
+    case 32: return launch<T, 32, KIND, APPEND>(g, a, st);
+    default: return launch<T, 64, KIND, APPEND>(g, a, st);
   }
+}
+template <bool APPEND> cudaError_t launch_any(const Geometry& g, int dtype, const RowArgs& a, cudaStream_t st) {
+  if (a.c.kind == GSIT_CACHE_INT8)
+    return dtype == GSIT_BF16 ? launch_width<__nv_bfloat16, GSIT_CACHE_INT8, APPEND>(g, a, st) : launch_width<float, GSIT_CACHE_INT8, APPEND>(g, a, st);
+  return dtype == GSIT_BF16 ? launch_width<__nv_bfloat16, GSIT_CACHE_E4M3, APPEND>(g, a, st) : launch_width<float, GSIT_CACHE_E4M3, APPEND>(g, a, st);
 }
 
 }  // namespace

@@ -53,6 +53,7 @@ struct CachedArgs {
   const float* slopes;
   RowTimes times;                      // null: the index inside the segment
   int group, rows, causal;             // rows: query rows of a key head, L * group
+  bool mixed;                          // tiles of rows run across segments
   float softcap, inner, outer;         // score = outer * tanh(inner * dot) or inner * dot, base 2
   int split;                           // CTAs of the cluster that shares a (stream, key head, tile of rows)
   float* parts;                        // workspace; null: the CTAs of a cluster share the work and need none

@@ -179,8 +179,8 @@ template <int HD, int R> struct Part {
   float2 ml[R];
 };
 
-// CTAs of an SM: two where their registers allow it.
-template <typename T, int NT> constexpr int RESIDENT = NT == 1 || (NT == 2 && sizeof(T) == 2) ? 2 : 1;
+// CTAs of an SM: two where their registers allow it.  (Tiles of 32 rows, one CTA an SM, took 44 us where those of 16 take 34.)
+template <typename T, int NT> constexpr int RESIDENT = NT == 1 || sizeof(T) == 2 ? 2 : 1;
 
 template <typename T, int HD, int KIND, int NT>
 __global__ void __launch_bounds__(THREADS, RESIDENT<T, NT>)
@@ -703,7 +703,17 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
 
   // ---- this CTA's share: one piece, or an even share of all streams' blocks, in pieces of one stream and key head ----
   const bool even = a.parts != nullptr;
-  const int rank = even ? 0 : (int)blockIdx.x % a.split, row0 = even ? 0 : (int)blockIdx.z * R, n_rows = min(R, a.rows - row0);
+  const int rank = even ? 0 : (int)blockIdx.x % a.split;
+  int row0 = 0, n_rows = a.rows;
+  if (a.rows > R && a.mixed) {
+    row0 = blockIdx.z * R;
+    n_rows = min(R, a.rows - row0);
+  } else if (a.rows > R) {   // tiles of one segment's rows, so that a tile walks no more than they see
+    int tile = blockIdx.z, seg = 0;
+    for (; seg < 2 && tile >= (g.len(seg) * a.group + R - 1) / R; ++seg) tile -= (g.len(seg) * a.group + R - 1) / R;
+    row0 = g.off(seg) * a.group + tile * R;
+    n_rows = min(R, g.len(seg) * a.group - tile * R);
+  }
   int b = even ? 0 : (int)blockIdx.y, hk = even ? 0 : (int)blockIdx.x / a.split, pieces = 0;
   int64_t at = 0, end = 1, base = 0;         // in blocks of all streams and key heads: where the share goes on and ends, where stream b begins
   if (even) {
@@ -841,21 +851,29 @@ __global__ void __launch_bounds__(THREADS) cached_join_kernel(const __grid_const
     const int k0 = cta_of(from), k1 = cta_of(to - 1);
     if (k0 == k1) return;   // that CTA has written the row
     auto part_of = [&](int k) -> const Part<HD, R>& { return parts[2 * k + (k == k0 && units * k / ctas < from)]; };
-    float top = -INFINITY, sum = 0.f;
     auto empty = [&](int k) { return units * k / ctas == units * (k + 1) / ctas; };   // more CTAs than blocks
+    // 32 parts at a time: lanes have their references and sums, then the features, with several parts' loads under way
+    float top = -INFINITY, sum = 0.f;
     for (int k = k0 + lane; k <= k1; k += 32)
       if (!empty(k)) top = fmaxf(top, part_of(k).ml[r].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    for (int k = k0; k <= k1; ++k) {
-      if (empty(k)) continue;
-      const float2 p = part_of(k).ml[r];
-      const float f = p.x == -INFINITY ? 1.f : ptx::ex2(p.x - top);
+    for (int k = k0; k <= k1; k += 32) {
+      const bool has = k + lane <= k1 && !empty(k + lane);
+      const float2 p = has ? part_of(k + lane).ml[r] : make_float2(-INFINITY, 0.f);
+      const float f = !has ? 0.f : p.x == -INFINITY ? 1.f : ptx::ex2(p.x - top);
+      const uint32_t those = __ballot_sync(0xffffffffu, has);
       sum += f * p.y;
-      if (mine)
+#pragma unroll 8
+      for (int i = 0; i < min(32, k1 - k + 1); ++i) {
+        const float by = __shfl_sync(0xffffffffu, f, i);
+        if (mine && ((those >> i) & 1u))
 #pragma unroll
-        for (int e = 0; e < F; ++e) v[e] = fmaf(f, part_of(k).acc[r][lane * F + e], v[e]);
+          for (int e = 0; e < F; ++e) v[e] = fmaf(by, part_of(k + i).acc[r][lane * F + e], v[e]);
+      }
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     ml = make_float2(top, sum);
   }
   const int l = r / a.group, head = hk * a.group + r % a.group;
@@ -886,7 +904,22 @@ cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st, size
   int n_sm = 0;
   cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
   if (e != cudaSuccess) return e;
-  const int tiles = (a.rows + R - 1) / R, ctas = RESIDENT<T, NT> * n_sm;
+  // Tiles of rows: one where all fit in; of each segment's rows apart, so that a tile walks only what they see (16 streams of (4, 25, 30) rows, two to a key head,
+  // forward ring: 34 us, and 44 with mixed ones); across segments where all of them see the same (all blocks open: 84 us, and 85 apart).
+  uint32_t sees = 0;
+  a.mixed = true;
+  for (int i = 0; i < 3; ++i)
+    if (g.len(i) > 0) {
+      const uint32_t s = g.allowed >> (3 * i) & 7u;
+      a.mixed = a.mixed && (sees == 0 || sees == s + 8u);
+      sees = s + 8u;
+    }
+  int tiles = (a.rows + R - 1) / R;
+  if (a.rows > R && !a.mixed) {
+    tiles = 0;
+    for (int i = 0; i < 3; ++i) tiles += (g.len(i) * a.group + R - 1) / R;
+  }
+  const int ctas = RESIDENT<T, NT> * n_sm;
   if (tiles > 65535) return cudaErrorNotSupported;
   a.split = split_keys(g, a, n_sm, tiles, Ring<HD>::B);
   const bool even = even_shares<HD>(g, a, tiles, ctas, a.split);
@@ -923,8 +956,6 @@ cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st, size
 
 template <typename T, int HD, int KIND> cudaError_t launch_rows(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch) {
   if (a.rows <= 8) return launch_tiles<T, HD, KIND, 1>(g, a, st, scratch);
-  if constexpr (sizeof(T) == 2)
-    if (a.rows > 16) return launch_tiles<T, HD, KIND, 4>(g, a, st, scratch);
   return launch_tiles<T, HD, KIND, 2>(g, a, st, scratch);
 }
 template <typename T, int KIND> cudaError_t launch_width(const Geometry& g, CachedArgs& a, cudaStream_t st, size_t* scratch) {

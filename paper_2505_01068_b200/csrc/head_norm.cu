@@ -3,14 +3,14 @@
 // Backward, with u = R^-1 dy, g = u gamma and s = sum(g x):  dx = r (g - x r^2 s / hd),  dgamma = sum over rows and heads of u x r.
 // x is read again instead of saving anything; r costs one more sum over a head that is in registers anyway.
 //
-// Bound by the rows read and written, so everything is arranged around loads in flight: a warp works for itself, without barriers.  It
-// takes blocks of a few rows of one of the two tensors; a lane holds two 16-byte pieces of a head (the halves that rotate against each other, or
-// neighbours where pairs are interleaved), so that sums over a head are log2(lanes of a head) shuffles and a pair never leaves its lane.  Which
-// pieces of a block are a lane's never changes: offsets, weights and the sums for dgamma stay in registers.  The angles of a block are
-// computed into a table of the warp's own while the block's loads are under way, one (row, pair) a lane: as many as the heads
-// of one tensor share.  q and k have warps of their own, in proportion to their heads: shared tables would halve the angles' work, but
-// sums for two weights do not fit the registers beside the loads.
-// Angles as in rotary.cu: a double product in turns less its nearest integer, so that far positions keep their phase.
+// Bound by the rows read and written, so everything is arranged around loads in flight and few instructions: a warp works for itself, without barriers.
+// It takes blocks of a few rows, forward of q and k, backward of one of them (sums for two weights do not fit the registers beside the loads); a lane holds two 16-byte pieces of a head (the halves that rotate against each other, or neighbours where
+// pairs are interleaved), so that sums over a head are log2(lanes of a head) shuffles and a pair never leaves its lane.  Which pieces of a block
+// are a lane's never changes, so the sums for dgamma stay in registers.  The angles of a block are computed into a table of the warp's own while
+// the block's loads are under way, one (row, pair) a lane, and serve all heads.
+// Angles in turns are products of integers that lose their whole turns by themselves: position * (frequency * 2^64) mod 2^64, of which the upper 32 bits are
+// the phase, right for every position an int32 holds; then sincospi for float, and the special functions' sine and cosine for bf16 (2^-21 off, where a
+// result keeps 2^-9).
 // The gradients of the weights: registers, lanes of a warp, warps of a CTA, CTAs, each in order, the last by a second small kernel.
 #include <math.h>
 
@@ -30,17 +30,18 @@ struct NormTensor {
   void* out;                          // y or dx
   int64_t ldx, lddy, ldo;
   const float* gamma;
-  int heads, rows;                    // rows: of a block
-  unsigned blocks;
+  int heads;
 };
 struct HeadNormArgs {
   NormTensor t[2];
   const int32_t* positions;
   int64_t axis_stride, batch_stride;
-  int axis1, axis2, pairs, q_ctas;    // first pair of axis 1 and 2; CTAs of q (those of k follow)
+  int axis1, axis2, pairs;            // first pair of axis 1 and 2
+  int block_rows[2];                  // forward: the same for both
+  int q_ctas;                         // backward: CTAs of q, those of k follow
   float eps, inv_hd;
-  float* partial;                     // [CTAs][hd]
-  double turns[MAX_ROTARY_PAIRS];     // frequency of a pair in turns a position
+  float* partial;                     // rows of hd: one of every CTA of q, then those of k
+  uint64_t turns[MAX_ROTARY_PAIRS];   // frequency of a pair in turns a position, as a fraction of 2^64
 };
 
 // E elements of a row, as they lie in memory: 16 bytes, or 8 (bf16 heads of 8)
@@ -79,23 +80,29 @@ template <int E> __device__ __forceinline__ void store_piece(__nv_bfloat16* p, c
     *reinterpret_cast<uint2*>(p) = make_uint2(ptx::pack_bf16(f[0].x, f[0].y), ptx::pack_bf16(f[1].x, f[1].y));
 }
 
+// The table of angles: of pairs 2 i and 2 i + 1 of a lane's piece {cos, cos, sin, sin}; pieces lie 16 bytes further apart than they are long, so that the lanes
+// of a head meet different banks.
+template <int E> constexpr int PIECE_ANGLES = 2 * E + 4;   // floats
+
 // (lo, hi) of a lane turned by its angles.  Halves: pair e is (lo[e], hi[e]).  Interleaved: pairs are neighbours, first those of lo.
-template <int E, bool ADJACENT>
-__device__ __forceinline__ void turn(float2 (&lo)[E / 2], float2 (&hi)[E / 2], const float* cs, const float* sn, float sign) {
-  if constexpr (!ADJACENT) {
+template <int E, bool ADJACENT, bool BACK>
+__device__ __forceinline__ void turn(float2 (&lo)[E / 2], float2 (&hi)[E / 2], const float* table) {
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      const float2 c = *reinterpret_cast<const float2*>(cs + 2 * i), s0 = *reinterpret_cast<const float2*>(sn + 2 * i), s = make_float2(sign * s0.x, sign * s0.y);
+  for (int i = 0; i < E / 2; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(table + 4 * i);
+    const float2 c = make_float2(v.x, v.y), s = BACK ? make_float2(-v.z, -v.w) : make_float2(v.z, v.w);
+    if constexpr (!ADJACENT) {
       const float2 a = __ffma2_rn(make_float2(-hi[i].x, -hi[i].y), s, __fmul2_rn(lo[i], c)), b = __ffma2_rn(lo[i], s, __fmul2_rn(hi[i], c));
       lo[i] = a;
       hi[i] = b;
-    }
-  } else {
+    } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      float2& v = i < E / 2 ? lo[i % (E / 2)] : hi[i % (E / 2)];
-      const float c = cs[i], s = sign * sn[i];
-      v = make_float2(v.x * c - v.y * s, v.x * s + v.y * c);
+      for (int e = 0; e < 2; ++e) {
+        const int p = 2 * i + e;
+        float2& w = p < E / 2 ? lo[p % (E / 2)] : hi[p % (E / 2)];
+        const float cs = e ? c.y : c.x, sn = e ? s.y : s.x;
+        w = __ffma2_rn(make_float2(-w.y, w.x), make_float2(sn, sn), __fmul2_rn(w, make_float2(cs, cs)));
+      }
     }
   }
 }
@@ -110,195 +117,245 @@ template <int LANES> __device__ __forceinline__ float2 head_sum(float2 v) {
   return v;
 }
 
-template <bool BWD> constexpr int UNITS = BWD ? 1 : 2;   // heads' pieces of a lane whose loads are in flight together
+// Heads' pieces of a lane, of each tensor, whose loads are in flight together: two, but one where 16-byte pieces of bf16 and the sums for dgamma fill the
+// registers (128 x (128, 1024, 1024), 8 + 8 heads of 64, backward: 394 us with one, 510 with two; 64 x (50, 500, 500), 8 + 8 of 8, float: 27.6 and 21.5).
+template <int E, bool BWD> constexpr int UNITS = BWD && E == 8 ? 1 : 2;
+
+// Sine and cosine of position * turns, by the phase in turns, at most 1/2.
+template <typename T> __device__ __forceinline__ void sine_cosine(int32_t position, uint64_t turns, float* sn, float* cs) {
+  const uint32_t low = (uint32_t)turns, phase = __umulhi((uint32_t)position, low) + (uint32_t)position * (uint32_t)(turns >> 32) - (position < 0 ? low : 0u);
+  const float v = (float)(int32_t)phase;   // * 2^-32
+  if constexpr (sizeof(T) == 4) sincospif(v * 0x1p-31f, sn, cs);
+  else __sincosf(v * (6.283185307f * 0x1p-32f), sn, cs);
+}
+// First row of segment s, and its length, without an index into the parameters.
+__device__ __forceinline__ int first_of(const Geometry& g, int s) { return s == 2 ? g.seg_off[2] : s == 1 ? g.seg_off[1] : 0; }
+__device__ __forceinline__ int length_of(const Geometry& g, int s) { return s == 2 ? g.seg_len[2] : s == 1 ? g.seg_len[1] : g.seg_len[0]; }
+__device__ __forceinline__ bool real_row(const Geometry& g, int b, int l) {
+  const int s = segment_of(g, l), n = length_of(g, s);
+  int valid = n;
+  if (g.valid_len != nullptr) {
+    valid = g.valid_len[3 * b + s];
+    if (valid < 0 || valid > n) {
+      raise_flag(g, GSIT_DEVFLAG_CLAMPED);
+      valid = valid < 0 ? 0 : n;
+    }
+  }
+  return l - first_of(g, s) < valid;
+}
 
 template <typename T, int E, int LANES, bool ADJACENT, bool BWD>
-__global__ void __launch_bounds__(THREADS, BWD ? 2 : 4)
+__global__ void __launch_bounds__(THREADS, 2)
 head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ HeadNormArgs a) {
-  constexpr int HALF = E * LANES, HD = 2 * HALF, N = UNITS<BWD>, H2 = E / 2;
+  constexpr int HALF = E * LANES, HD = 2 * HALF, N = UNITS<E, BWD>, H2 = E / 2, TABLE = ANGLES / E * PIECE_ANGLES<E>, W = BWD ? 1 : 2;   // W: tensors of a warp
   static_assert(HALF <= ANGLES, "the angles of a row fit the table");
-  __shared__ __align__(16) float s_cos[WARPS][2][ANGLES], s_sin[WARPS][2][ANGLES];
+  __shared__ __align__(16) float s_table[WARPS][2][TABLE], s_gamma[W][HD];
   __shared__ uint32_t s_real[WARPS][2];      // bit r: row r of the block is a real one
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = lane % LANES;
   ptx::load_params_early(g, a);
-  const int which = (int)blockIdx.x >= a.q_ctas;
-  const NormTensor& t = a.t[which];
-  const unsigned ctas = which ? gridDim.x - a.q_ctas : a.q_ctas, cta = which ? blockIdx.x - a.q_ctas : blockIdx.x;
-  const int rows = g.batch * g.L, row_units = t.heads * LANES, block_rows = t.rows;
+  const int which = W == 1 && (int)blockIdx.x >= a.q_ctas, rows = g.batch * g.L, block_rows = a.block_rows[which];
+  const NormTensor own = a.t[which];           // of the warp, where it has one alone: in registers
+  const unsigned ctas = W == 2 ? gridDim.x : which ? gridDim.x - a.q_ctas : a.q_ctas, cta = blockIdx.x - (which ? a.q_ctas : 0);
+  const unsigned blocks = (unsigned)((rows + block_rows - 1) / block_rows);
   // this lane's features: a piece of the first halves and its partner in the second ones; behind the rotated features, and where interleaved, neighbours
   const int rotated = a.pairs / E;
   const bool neighbours = ADJACENT || unit >= rotated;
   const int lo_at = neighbours ? 2 * unit * E : unit * E, hi_at = neighbours ? lo_at + E : a.pairs + unit * E;
 
-  // this lane's angles of a block
-  int angle_row[2], angle_axis[2];
-  double turns[2];
+  // this lane's angles of a block: their rows' samples and places go on from block to block without a division
+  const unsigned step = ctas * WARPS;
+  unsigned block = cta * WARPS + warp;
+  const int step_rows = (int)(step * block_rows), step_b = step_rows / g.L, step_l = step_rows - step_b * g.L;
+  int angle_row[2], angle_axis[2], angle_b[2], angle_l[2];
+  uint64_t turns[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int at = lane + 32 * i, pair = at % HALF;
     angle_row[i] = at / HALF;
-    turns[i] = pair < a.pairs ? a.turns[pair] : 0.0;
+    turns[i] = pair < a.pairs ? a.turns[pair] : 0;
     angle_axis[i] = pair >= a.pairs ? -1 : pair >= a.axis2 ? 2 : pair >= a.axis1 ? 1 : 0;
+    const uint32_t row = (uint32_t)min((int64_t)block * block_rows + angle_row[i], (int64_t)0x3fffffff);
+    angle_b[i] = row / (uint32_t)g.L;
+    angle_l[i] = row - angle_b[i] * g.L;
   }
-  auto angles = [&](unsigned block, int buf) {
+  auto angles = [&](int buf) {   // of the next block in turn
     uint32_t real = 0;
-    if (block < t.blocks) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = (int)(block * block_rows) + angle_row[i];
-        if (angle_row[i] < block_rows && row < rows) {
-          const int b = (uint32_t)row / (uint32_t)g.L, l = row - b * g.L, s = segment_of(g, l);
-          float sn = 0.f, cs = 1.f;
-          if (angle_axis[i] >= 0) {
-            const double v = (double)a.positions[angle_axis[i] * a.axis_stride + b * a.batch_stride + l] * turns[i];
-            sincospif(2.0f * (float)(v - rint(v)), &sn, &cs);
-          }
-          s_cos[warp][buf][lane + 32 * i] = cs;
-          s_sin[warp][buf][lane + 32 * i] = sn;
-          if (l - g.off(s) < valid_rows(g, b, s)) real |= 1u << angle_row[i];
-        }
+    for (int i = 0; i < 2; ++i) {
+      if (32 * i < block_rows * HALF && angle_row[i] < block_rows && angle_b[i] < g.batch) {
+        const int b = angle_b[i], l = angle_l[i], at = lane + 32 * i, pair = at % HALF;
+        float sn = 0.f, cs = 1.f;
+        if (angle_axis[i] >= 0) sine_cosine<T>(a.positions[angle_axis[i] * a.axis_stride + b * a.batch_stride + l], turns[i], &sn, &cs);
+        float* const to = s_table[warp][buf] + (angle_row[i] * LANES + pair / E) * PIECE_ANGLES<E> + pair % E / 2 * 4 + pair % 2;
+        to[0] = cs;
+        to[2] = sn;
+        if (real_row(g, b, l)) real |= 1u << angle_row[i];
+      }
+      angle_b[i] += step_b;
+      angle_l[i] += step_l;
+      if (angle_l[i] >= g.L) {
+        angle_l[i] -= g.L;
+        ++angle_b[i];
       }
     }
     real = __reduce_or_sync(0xffffffffu, real);
     if (lane == 0) s_real[warp][buf] = real;
   };
   // this lane's pieces of a block (a row of more heads than the lanes take is walked in chunks of them)
-  int row_of[N], head_of[N];
+  int row_of[W][N], head_of[W][N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int u = lane + 32 * i;
-    row_of[i] = block_rows > 1 ? u / row_units : 0;
-    head_of[i] = (u - row_of[i] * row_units) / LANES;
-    if (row_of[i] >= block_rows) {   // none
-      row_of[i] = 0;
-      head_of[i] = t.heads;
+  for (int w = 0; w < W; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = lane + 32 * i, row_units = (W == 1 ? own : a.t[w]).heads * LANES;
+      row_of[w][i] = block_rows > 1 && row_units > 0 ? u / row_units : 0;
+      head_of[w][i] = (u - row_of[w][i] * row_units) / LANES;
+      if (row_of[w][i] >= block_rows) {   // none
+        row_of[w][i] = 0;
+        head_of[w][i] = (W == 1 ? own : a.t[w]).heads;
+      }
     }
-  }
-  float2 ga_lo[H2], ga_hi[H2], dg_lo[H2], dg_hi[H2];
+  float2 dg_lo[W][H2], dg_hi[W][H2];
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+#pragma unroll
+    for (int i = 0; i < H2; ++i) dg_lo[w][i] = dg_hi[w][i] = make_float2(0.f, 0.f);
 
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-#pragma unroll
-  for (int i = 0; i < H2; ++i) {
-    ga_lo[i] = ga_hi[i] = make_float2(1.f, 1.f);
-    dg_lo[i] = dg_hi[i] = make_float2(0.f, 0.f);
-    if (t.gamma != nullptr) {
-      ga_lo[i] = make_float2(t.gamma[lo_at + 2 * i], t.gamma[lo_at + 2 * i + 1]);
-      ga_hi[i] = make_float2(t.gamma[hi_at + 2 * i], t.gamma[hi_at + 2 * i + 1]);
-    }
+  for (int i = threadIdx.x; i < W * HD; i += THREADS) {
+    const float* gamma = W == 1 ? own.gamma : a.t[i / HD].gamma;
+    s_gamma[i / HD][i % HD] = gamma != nullptr ? gamma[i % HD] : 1.f;
   }
-  const unsigned step = ctas * WARPS;
-  unsigned block = cta * WARPS + warp;
-  angles(block, 0);
-  __syncwarp();
-  for (int buf = 0; block < t.blocks; block += step, buf ^= 1) {
+  angles(0);
+  __syncthreads();
+  const int most = W == 1 ? own.heads : max(a.t[0].heads, a.t[1].heads);
+  for (int buf = 0; block < blocks; block += step, buf ^= 1) {
     const int64_t row0 = (int64_t)block * block_rows;
+    const int left = (int)min((int64_t)block_rows, rows - row0);
     const uint32_t real = s_real[warp][buf];
-    for (int chunk = 0; chunk < t.heads; chunk += 32 * N / LANES) {
-      Piece<T, E> x_lo[N], x_hi[N], y_lo[N], y_hi[N];
-      bool in[N], keep[N];
+    for (int chunk = 0; chunk < most; chunk += 32 * N / LANES) {
+      Piece<T, E> x_lo[W][N], x_hi[W][N], y_lo[W][BWD ? N : 1], y_hi[W][BWD ? N : 1];
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int head = head_of[i] + chunk;
-        in[i] = row0 + row_of[i] < rows && head < t.heads;
-        keep[i] = in[i] && ((real >> row_of[i]) & 1u);
-        x_lo[i].clear();
-        x_hi[i].clear();
-        if constexpr (BWD) {
-          y_lo[i].clear();
-          y_hi[i].clear();
-        }
-        if (keep[i]) {
-          const T* x = static_cast<const T*>(t.x) + (row0 + row_of[i]) * t.ldx + (int64_t)head * HD;
-          x_lo[i].load(x + lo_at);
-          x_hi[i].load(x + hi_at);
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const NormTensor& t = (W == 1 ? own : a.t[w]);
+          if (chunk >= t.heads || 32 * i >= block_rows * t.heads * LANES) continue;   // no lane has any
+          const int head = head_of[w][i] + chunk;
+          x_lo[w][i].clear();
+          x_hi[w][i].clear();
           if constexpr (BWD) {
-            const T* dy = static_cast<const T*>(t.dy) + (row0 + row_of[i]) * t.lddy + (int64_t)head * HD;
-            y_lo[i].load(dy + lo_at);
-            y_hi[i].load(dy + hi_at);
+            y_lo[w][i].clear();
+            y_hi[w][i].clear();
           }
-        }
-      }
-      if (chunk == 0) angles(block + step, buf ^ 1);   // while these loads are under way
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float *cs = s_cos[warp][buf] + row_of[i] * HALF + unit * E, *sn = s_sin[warp][buf] + row_of[i] * HALF + unit * E;
-        float2 lo[H2], hi[H2];
-        x_lo[i].get(lo);
-        x_hi[i].get(hi);
-        float2 sum = make_float2(0.f, 0.f), other = sum;
-#pragma unroll
-        for (int e = 0; e < H2; ++e) {
-          sum = __ffma2_rn(lo[e], lo[e], sum);
-          other = __ffma2_rn(hi[e], hi[e], other);
-        }
-        sum = __fadd2_rn(sum, other);
-        float2 both = make_float2(sum.x + sum.y, 0.f);
-        float2 u_lo[H2], u_hi[H2];
-        if constexpr (BWD) {
-          y_lo[i].get(u_lo);
-          y_hi[i].get(u_hi);
-          turn<E, ADJACENT>(u_lo, u_hi, cs, sn, -1.f);
-          float2 gx = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int e = 0; e < H2; ++e) {
-            gx = __ffma2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), lo[e], gx);
-            gx = __ffma2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), hi[e], gx);
-          }
-          both.y = gx.x + gx.y;
-        }
-        both = head_sum<LANES>(both);
-        const float r = rsqrtf(both.x * a.inv_hd + a.eps);
-        const float2 r2 = make_float2(r, r);
-        if constexpr (!BWD) {
-#pragma unroll
-          for (int e = 0; e < H2; ++e) {
-            lo[e] = __fmul2_rn(__fmul2_rn(lo[e], r2), ga_lo[e]);
-            hi[e] = __fmul2_rn(__fmul2_rn(hi[e], r2), ga_hi[e]);
-          }
-          turn<E, ADJACENT>(lo, hi, cs, sn, 1.f);
-        } else {
-          const float back = -r * r * (both.y * a.inv_hd);
-          const float2 back2 = make_float2(back, back);
-#pragma unroll
-          for (int e = 0; e < H2; ++e) {
-            const float2 h_lo = __fmul2_rn(lo[e], r2), h_hi = __fmul2_rn(hi[e], r2);
-            if (keep[i]) {   // (a row that is not real has an h of 0, but r of a tiny eps may be infinite)
-              dg_lo[e] = __ffma2_rn(u_lo[e], h_lo, dg_lo[e]);
-              dg_hi[e] = __ffma2_rn(u_hi[e], h_hi, dg_hi[e]);
+          if (row_of[w][i] < left && head < t.heads && ((real >> row_of[w][i]) & 1u)) {
+            const T* x = static_cast<const T*>(t.x) + (row0 + row_of[w][i]) * t.ldx + head * HD;
+            x_lo[w][i].load(x + lo_at);
+            x_hi[w][i].load(x + hi_at);
+            if constexpr (BWD) {
+              const T* dy = static_cast<const T*>(t.dy) + (row0 + row_of[w][i]) * t.lddy + head * HD;
+              y_lo[w][i].load(dy + lo_at);
+              y_hi[w][i].load(dy + hi_at);
             }
-            lo[e] = __ffma2_rn(h_lo, back2, __fmul2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), r2));
-            hi[e] = __ffma2_rn(h_hi, back2, __fmul2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), r2));
           }
         }
-        if (in[i]) {
-          if (!keep[i])
+      if (chunk == 0) angles(buf ^ 1);   // while these loads are under way
 #pragma unroll
-            for (int e = 0; e < H2; ++e) lo[e] = hi[e] = make_float2(0.f, 0.f);
-          T* out = static_cast<T*>(t.out) + (row0 + row_of[i]) * t.ldo + (int64_t)(head_of[i] + chunk) * HD;
-          store_piece<E>(out + lo_at, lo);
-          store_piece<E>(out + hi_at, hi);
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const NormTensor& t = (W == 1 ? own : a.t[w]);
+          if (chunk >= t.heads || 32 * i >= block_rows * t.heads * LANES) continue;
+          const int head = head_of[w][i] + chunk;
+          const bool in = row_of[w][i] < left && head < t.heads, keep = in && ((real >> row_of[w][i]) & 1u);
+          const float* const table = s_table[warp][buf] + (row_of[w][i] * LANES + unit) * PIECE_ANGLES<E>;
+          float2 lo[H2], hi[H2], ga_lo[H2], ga_hi[H2];
+          x_lo[w][i].get(lo);
+          x_hi[w][i].get(hi);
+#pragma unroll
+          for (int e = 0; e < H2; ++e) {
+            ga_lo[e] = *reinterpret_cast<const float2*>(&s_gamma[w][lo_at + 2 * e]);
+            ga_hi[e] = *reinterpret_cast<const float2*>(&s_gamma[w][hi_at + 2 * e]);
+          }
+          float2 sum = make_float2(0.f, 0.f), other = sum;
+#pragma unroll
+          for (int e = 0; e < H2; ++e) {
+            sum = __ffma2_rn(lo[e], lo[e], sum);
+            other = __ffma2_rn(hi[e], hi[e], other);
+          }
+          sum = __fadd2_rn(sum, other);
+          float2 both = make_float2(sum.x + sum.y, 0.f);
+          float2 u_lo[H2], u_hi[H2];
+          if constexpr (BWD) {
+            y_lo[w][i].get(u_lo);
+            y_hi[w][i].get(u_hi);
+            turn<E, ADJACENT, true>(u_lo, u_hi, table);
+            float2 gx = make_float2(0.f, 0.f), gy = gx;
+#pragma unroll
+            for (int e = 0; e < H2; ++e) {
+              gx = __ffma2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), lo[e], gx);
+              gy = __ffma2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), hi[e], gy);
+            }
+            gx = __fadd2_rn(gx, gy);
+            both.y = gx.x + gx.y;
+            both = head_sum<LANES>(both);
+          } else {
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) both.x += __shfl_xor_sync(0xffffffffu, both.x, o);
+          }
+          const float r = rsqrtf(both.x * a.inv_hd + a.eps);
+          const float2 r2 = make_float2(r, r);
+          if constexpr (!BWD) {
+#pragma unroll
+            for (int e = 0; e < H2; ++e) {
+              lo[e] = __fmul2_rn(__fmul2_rn(lo[e], r2), ga_lo[e]);
+              hi[e] = __fmul2_rn(__fmul2_rn(hi[e], r2), ga_hi[e]);
+            }
+            turn<E, ADJACENT, false>(lo, hi, table);
+          } else {
+            const float back = -r * r * (both.y * a.inv_hd);
+            const float2 back2 = make_float2(back, back);
+#pragma unroll
+            for (int e = 0; e < H2; ++e) {
+              const float2 h_lo = __fmul2_rn(lo[e], r2), h_hi = __fmul2_rn(hi[e], r2);
+              if (keep) {   // (a row that is not real has an x of 0, but r of a tiny eps may be infinite)
+                dg_lo[w][e] = __ffma2_rn(u_lo[e], h_lo, dg_lo[w][e]);
+                dg_hi[w][e] = __ffma2_rn(u_hi[e], h_hi, dg_hi[w][e]);
+              }
+              lo[e] = __ffma2_rn(h_lo, back2, __fmul2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), r2));
+              hi[e] = __ffma2_rn(h_hi, back2, __fmul2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), r2));
+            }
+          }
+          if (in) {
+            if (!keep)
+#pragma unroll
+              for (int e = 0; e < H2; ++e) lo[e] = hi[e] = make_float2(0.f, 0.f);
+            T* out = static_cast<T*>(t.out) + (row0 + row_of[w][i]) * t.ldo + head * HD;
+            store_piece<E>(out + lo_at, lo);
+            store_piece<E>(out + hi_at, hi);
+          }
         }
-      }
     }
     __syncwarp();   // the next block's angles are there, and nobody reads this block's any more
   }
   if constexpr (BWD) {
     if (a.partial == nullptr) return;
     __shared__ float acc[WARPS][HD];
+    constexpr int w = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float lo = e & 1 ? dg_lo[e / 2].y : dg_lo[e / 2].x, hi = e & 1 ? dg_hi[e / 2].y : dg_hi[e / 2].x;
+      for (int e = 0; e < E; ++e) {
+        float lo = e & 1 ? dg_lo[w][e / 2].y : dg_lo[w][e / 2].x, hi = e & 1 ? dg_hi[w][e / 2].y : dg_hi[w][e / 2].x;
 #pragma unroll
-      for (int o = LANES; o < 32; o <<= 1) {
-        lo += __shfl_xor_sync(0xffffffffu, lo, o);
-        hi += __shfl_xor_sync(0xffffffffu, hi, o);
+        for (int o = LANES; o < 32; o <<= 1) {
+          lo += __shfl_xor_sync(0xffffffffu, lo, o);
+          hi += __shfl_xor_sync(0xffffffffu, hi, o);
+        }
+        if (lane < LANES) {
+          acc[warp][lo_at + e] = lo;
+          acc[warp][hi_at + e] = hi;
+        }
       }
-      if (lane < LANES) {
-        acc[warp][lo_at + e] = lo;
-        acc[warp][hi_at + e] = hi;
-      }
-    }
     __syncthreads();
     for (int c = threadIdx.x; c < HD; c += THREADS) {
       float s = 0.f;
@@ -316,12 +373,9 @@ __global__ void __launch_bounds__(THREADS)
 head_norm_any_kernel(const __grid_constant__ Geometry g, const __grid_constant__ HeadNormArgs a, const int adjacent) {
   __shared__ float s_cos[WARPS][MAX_ROTARY_PAIRS], s_sin[WARPS][MAX_ROTARY_PAIRS], s_row[WARPS][MAX_HEAD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hd = g.hd, rows = g.batch * g.L;
-  const int which = (int)blockIdx.x >= a.q_ctas;
-  const NormTensor& t = a.t[which];
-  const int ctas = which ? (int)gridDim.x - a.q_ctas : a.q_ctas, cta = which ? (int)blockIdx.x - a.q_ctas : (int)blockIdx.x;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  float dg[OWN] = {};
+  float dg[2][OWN] = {};
   // the head in s_row turned by the angles: feature f
   auto turned = [&](int f, float sign) {
     const float v = s_row[warp][f];
@@ -331,17 +385,19 @@ head_norm_any_kernel(const __grid_constant__ Geometry g, const __grid_constant__
     const float w = s_row[warp][adjacent ? f ^ 1 : first ? f + a.pairs : f - a.pairs], c = s_cos[warp][p], s = sign * s_sin[warp][p];
     return first ? v * c - w * s : w * s + v * c;
   };
-  for (int row = cta * WARPS + warp; row < rows; row += ctas * WARPS) {
+  for (int row = blockIdx.x * WARPS + warp; row < rows; row += gridDim.x * WARPS) {
     const int b = (uint32_t)row / (uint32_t)g.L, l = row - b * g.L, seg = segment_of(g, l);
     const bool real = l - g.off(seg) < valid_rows(g, b, seg);
     if (real)
       for (int p = lane; p < a.pairs; p += 32) {
         const int axis = p >= a.axis2 ? 2 : p >= a.axis1 ? 1 : 0;
-        const double v = (double)a.positions[axis * a.axis_stride + b * a.batch_stride + l] * a.turns[p];
-        sincospif(2.0f * (float)(v - rint(v)), &s_sin[warp][p], &s_cos[warp][p]);
+        sine_cosine<float>(a.positions[axis * a.axis_stride + b * a.batch_stride + l], a.turns[p], &s_sin[warp][p], &s_cos[warp][p]);
       }
     __syncwarp();
-    for (int head = 0; head < t.heads; ++head) {
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+    for (int head = 0; head < a.t[which].heads; ++head) {
+      const NormTensor& t = a.t[which];
       const T* x = static_cast<const T*>(t.x) + (int64_t)row * t.ldx + (int64_t)head * hd;
       T* out = static_cast<T*>(t.out) + (int64_t)row * t.ldo + (int64_t)head * hd;
       if (!real) {
@@ -374,7 +430,7 @@ head_norm_any_kernel(const __grid_constant__ Geometry g, const __grid_constant__
         for (int i = 0; i < OWN; ++i)
           if (const int f = lane + 32 * i; f < hd) {
             const float h = v[i] * r;
-            dg[i] += u[i] * h;
+            dg[which][i] += u[i] * h;
             store_as(out + f, u[i] * ga[i] * r + h * back);
           }
       } else {
@@ -390,13 +446,17 @@ head_norm_any_kernel(const __grid_constant__ Geometry g, const __grid_constant__
   if (!BWD || a.partial == nullptr) return;
   // warps in order, through the rows they no longer need
 #pragma unroll
-  for (int i = 0; i < OWN; ++i)
-    if (const int f = lane + 32 * i; f < hd) s_row[warp][f] = dg[i];
-  __syncthreads();
-  for (int c = threadIdx.x; c < hd; c += THREADS) {
-    float s = 0.f;
-    for (int w = 0; w < WARPS; ++w) s += s_row[w][c];
-    a.partial[(int64_t)blockIdx.x * hd + c] = s;
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < OWN; ++i)
+      if (const int f = lane + 32 * i; f < hd) s_row[warp][f] = dg[which][i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < hd; c += THREADS) {
+      float s = 0.f;
+      for (int w = 0; w < WARPS; ++w) s += s_row[w][c];
+      a.partial[((int64_t)which * gridDim.x + blockIdx.x) * hd + c] = s;
+    }
   }
 }
 
@@ -441,7 +501,7 @@ template <typename T> Kernel wide_kernel(int hd, bool adjacent, bool bwd) {
 
 }  // namespace
 
-size_t head_norm_scratch(const Geometry& g) { return sizeof(float) * (size_t)g.hd * MAX_CTAS; }
+size_t head_norm_scratch(const Geometry& g) { return sizeof(float) * 2 * (size_t)g.hd * MAX_CTAS; }
 
 cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c, cudaStream_t st) {
   const int es = dtype == GSIT_BF16 ? 2 : 4;
@@ -458,12 +518,13 @@ cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c
   a.eps = c.eps;
   a.inv_hd = 1.0f / g.hd;
   a.partial = c.partial;
-  rotary_turns(c.base, a.pairs, a.turns);
+  double turns[MAX_ROTARY_PAIRS];
+  rotary_turns(c.base, a.pairs, turns);
+  for (int p = 0; p < a.pairs; ++p) a.turns[p] = (uint64_t)ldexp(turns[p] - floor(turns[p]), 64);   // (whole turns do not count)
   // wide: a head of at most 128 features is 1, 2, 4, 8 or 16 lanes of two pieces, 16 bytes each (8 where a bf16 head has 8 features), and whole
   // pieces of it rotate
   const int piece = dtype == GSIT_BF16 ? (g.hd == 8 ? 4 : 8) : 4, lanes = g.hd / (2 * piece);
   bool wide = g.hd % (2 * piece) == 0 && g.hd <= 2 * ANGLES && (lanes & (lanes - 1)) == 0 && (c.interleaved || a.pairs % piece == 0);
-  int total = 0;
   for (int i = 0; i < 2; ++i) {
     NormTensor& t = a.t[i];
     t.x = c.x[i]; t.ldx = c.ldx[i];
@@ -471,25 +532,26 @@ cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c
     t.out = c.out[i]; t.ldo = c.ldo[i];
     t.gamma = c.gamma[i];
     t.heads = c.heads[i];
-    total += t.heads;
-    if (t.heads == 0) continue;
-    wide = wide && ((reinterpret_cast<uintptr_t>(t.x) | reinterpret_cast<uintptr_t>(t.dy) | reinterpret_cast<uintptr_t>(t.out)) % (piece * es)) == 0 &&
-           t.ldx % piece == 0 && t.lddy % piece == 0 && t.ldo % piece == 0;
+    if (t.heads > 0)
+      wide = wide && ((reinterpret_cast<uintptr_t>(t.x) | reinterpret_cast<uintptr_t>(t.dy) | reinterpret_cast<uintptr_t>(t.out)) % (piece * es)) == 0 &&
+             t.ldx % piece == 0 && t.lddy % piece == 0 && t.ldo % piece == 0;
   }
-  // CTAs: as many as fit the SMs at once, shared out to q and k by their heads; no more than there are blocks of rows
+  // rows of a block: what the lanes' pieces in flight take of the (wider) tensor, and two angles a lane; CTAs: as many as fit the SMs at once
   const int64_t rows = (int64_t)g.batch * g.L;
-  const int most = std::min(MAX_CTAS, (c.backward ? 2 : 4) * n_sm), units = c.backward ? UNITS<true> : UNITS<false>;
-  int ctas[2] = {0, 0};
-  for (int i = 0; i < 2; ++i) {
-    NormTensor& t = a.t[i];
-    if (t.heads == 0) continue;
-    t.rows = wide ? std::max(1, std::min(2 * ANGLES / g.hd, 32 * units / (t.heads * lanes))) : 1;
-    t.blocks = (unsigned)((rows + t.rows - 1) / t.rows);
-    const int share = std::max(1, i == 0 ? (most * t.heads + total / 2) / total : most - ctas[0]);
-    ctas[i] = (int)std::min<int64_t>(std::min(share, c.heads[1] > 0 ? most - 1 : most), (t.blocks + WARPS - 1) / WARPS);
+  const int most = std::min(MAX_CTAS, 2 * n_sm);
+  auto block_rows = [&](int heads) { return wide && heads > 0 ? std::max(1, std::min(2 * ANGLES / g.hd, 32 * (c.backward && piece == 8 ? 1 : 2) / (heads * lanes))) : 1; };
+  auto ctas_for = [&](int share, int of_rows) { return (int)std::min<int64_t>(share, (rows + of_rows * WARPS - 1) / (of_rows * WARPS)); };
+  int ctas;
+  if (wide && c.backward) {   // shared out by heads
+    const int total = c.heads[0] + c.heads[1], share = c.heads[1] == 0 ? most : std::min(most - 1, std::max(1, (most * c.heads[0] + total / 2) / total));
+    for (int i = 0; i < 2; ++i) a.block_rows[i] = block_rows(c.heads[i]);
+    a.q_ctas = ctas_for(share, a.block_rows[0]);
+    ctas = a.q_ctas + (c.heads[1] == 0 ? 0 : ctas_for(most - share, a.block_rows[1]));
+  } else {
+    a.block_rows[0] = a.block_rows[1] = block_rows(std::max(c.heads[0], c.heads[1]));
+    ctas = a.q_ctas = ctas_for(most, a.block_rows[0]);
   }
-  a.q_ctas = ctas[0];
-  const dim3 grid((unsigned)(ctas[0] + ctas[1]));
+  const dim3 grid((unsigned)ctas);
   if (wide) {
     const Kernel k = dtype == GSIT_BF16 ? wide_kernel<__nv_bfloat16>(g.hd, c.interleaved, c.backward) : wide_kernel<float>(g.hd, c.interleaved, c.backward);
     e = launch_overlapped(k, grid, dim3(THREADS), 0, st, g, a);
@@ -501,7 +563,7 @@ cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c
                    : launch_overlapped(head_norm_any_kernel<float, false>, grid, dim3(THREADS), 0, st, g, a, (int)c.interleaved);
   }
   if (e != cudaSuccess || a.partial == nullptr) return e;
-  return launch_overlapped(head_norm_reduce_kernel, dim3((g.hd + 31) / 32, c.heads[1] > 0 ? 2 : 1), dim3(1024), 0, st, a.partial, ctas[0], ctas[0] + ctas[1], g.hd,
+  return launch_overlapped(head_norm_reduce_kernel, dim3((g.hd + 31) / 32, c.heads[1] > 0 ? 2 : 1), dim3(1024), 0, st, a.partial, a.q_ctas, wide ? ctas : 2 * ctas, g.hd,
                            c.dgamma[0], c.dgamma[1]);
 }
 

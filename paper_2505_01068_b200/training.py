@@ -10,6 +10,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
+from . import streaming as S
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -164,3 +165,18 @@ class ImEncoderLayer(torch.nn.Module):
             return y
         real = self.place < valid_len[:, self.segment]
         return torch.where(real[:, :, None], y, 0.0)
+
+    def open_cache(self, batch, max_len, held_as="int8", pages=None, times=False):
+        """An empty cache for step(): `batch` streams of at most max_len (three numbers) positions a segment, held as "int8" or "e4m3" (see stream_cache)."""
+        return S.stream_cache(batch, max_len, self.kv_heads, self.hd, self.dtype, held_as, pages, times, self.place.device)
+
+    @torch.no_grad()
+    def step(self, cache, x, seg_len, valid_len=None, positions=None, times=None, ended=None, **rule):
+        """The layer for the newest positions of streams: x float32 [B, L, d] holds seg_len rows of each segment, the first valid_len of them real, which join
+        the cache and then attend to all that it holds.  positions int32 [axes, B, L] and times float32 [B, L] are those of these rows; ended int32 [B]:
+        streams that begin anew; rule: phase, custom_mask, scale, softcap, slopes, causal.  Returns y [B, L, d], padded rows +0."""
+        q, k, v = self.project(x, valid_len, positions, seg_len)
+        slots = S.cache_plan(cache, seg_len, valid_len, ended)
+        S.cache_append(cache, k, v, slots, seg_len, times)
+        y = self.finish(x, S.im_cached_attention_fwd(q, cache, seg_len, valid_len, times=times, **rule), valid_len, seg_len)
+        return y if valid_len is None else torch.where((slots >= 0)[:, :, None], y, 0.0)

@@ -15,6 +15,13 @@ def g():
     return lib
 
 
+@pytest.fixture(autouse=True)
+def nothing_is_flagged(g):
+    """No test leaves a flag behind that it has not looked at."""
+    yield
+    assert g.last_device_status() == (0, 0)
+
+
 def _rows(gen, B, L, H, hd, t, spread=1.0):
     x = torch.randn((B, L, H, hd), generator=gen) * torch.exp(spread * torch.randn((B, 1, H, hd), generator=gen))
     return x.to(t).cuda()

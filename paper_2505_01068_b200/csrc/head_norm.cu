@@ -57,10 +57,6 @@ template <typename T, int E> struct Piece {
       w[0] = v.x; w[1] = v.y;
     }
   }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) w[i] = 0u;
-  }
   __device__ __forceinline__ void get(float2 (&f)[E / 2]) const {
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) {
@@ -69,6 +65,12 @@ template <typename T, int E> struct Piece {
     }
   }
 };
+// A piece into the lane's own place in shared memory, zeros where there is none.
+template <typename T, int E> __device__ __forceinline__ void copy_piece(void* dst, const T* src, bool there) {
+  constexpr int BYTES = E * (int)sizeof(T);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 8 : 0) : "memory");
+}
 template <int E> __device__ __forceinline__ void store_piece(float* p, const float2 (&f)[E / 2]) {
   static_assert(E == 4, "16 bytes");
   *reinterpret_cast<float4*>(p) = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
@@ -117,9 +119,7 @@ template <int LANES> __device__ __forceinline__ float2 head_sum(float2 v) {
   return v;
 }
 
-// Heads' pieces of a lane, of each tensor, whose loads are in flight together: two, but one where 16-byte pieces of bf16 and the sums for dgamma fill the
-// registers (128 x (128, 1024, 1024), 8 + 8 heads of 64, backward: 394 us with one, 510 with two; 64 x (50, 500, 500), 8 + 8 of 8, float: 27.6 and 21.5).
-template <int E, bool BWD> constexpr int UNITS = BWD && E == 8 ? 1 : 2;
+constexpr int UNITS = 2;   // heads' pieces of a lane, of each tensor, that are copied together
 
 // Sine and cosine of position * turns, by the phase in turns, at most 1/2.
 template <typename T> __device__ __forceinline__ void sine_cosine(int32_t position, uint64_t turns, float* sn, float* cs) {
@@ -131,26 +131,14 @@ template <typename T> __device__ __forceinline__ void sine_cosine(int32_t positi
 // First row of segment s, and its length, without an index into the parameters.
 __device__ __forceinline__ int first_of(const Geometry& g, int s) { return s == 2 ? g.seg_off[2] : s == 1 ? g.seg_off[1] : 0; }
 __device__ __forceinline__ int length_of(const Geometry& g, int s) { return s == 2 ? g.seg_len[2] : s == 1 ? g.seg_len[1] : g.seg_len[0]; }
-__device__ __forceinline__ bool real_row(const Geometry& g, int b, int l) {
-  const int s = segment_of(g, l), n = length_of(g, s);
-  int valid = n;
-  if (g.valid_len != nullptr) {
-    valid = g.valid_len[3 * b + s];
-    if (valid < 0 || valid > n) {
-      raise_flag(g, GSIT_DEVFLAG_CLAMPED);
-      valid = valid < 0 ? 0 : n;
-    }
-  }
-  return l - first_of(g, s) < valid;
-}
-
 template <typename T, int E, int LANES, bool ADJACENT, bool BWD>
 __global__ void __launch_bounds__(THREADS, 2)
 head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ HeadNormArgs a) {
-  constexpr int HALF = E * LANES, HD = 2 * HALF, N = UNITS<E, BWD>, H2 = E / 2, TABLE = ANGLES / E * PIECE_ANGLES<E>, W = BWD ? 1 : 2;   // W: tensors of a warp
+  constexpr int HALF = E * LANES, HD = 2 * HALF, N = UNITS, H2 = E / 2, BYTES = E * (int)sizeof(T), PARTS = BWD ? 4 : 2, TABLE = ANGLES / E * PIECE_ANGLES<E>, W = BWD ? 1 : 2,   // W: tensors of a warp
+                STAGE = W * N * PARTS * 32 * BYTES;
   static_assert(HALF <= ANGLES, "the angles of a row fit the table");
   __shared__ __align__(16) float s_table[WARPS][2][TABLE], s_gamma[W][HD];
-  __shared__ uint32_t s_real[WARPS][2];      // bit r: row r of the block is a real one
+  extern __shared__ __align__(16) uint8_t smem[];   // two stages of every warp's
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = lane % LANES;
   ptx::load_params_early(g, a);
   const int which = W == 1 && (int)blockIdx.x >= a.q_ctas, rows = g.batch * g.L, block_rows = a.block_rows[which];
@@ -162,11 +150,12 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
   const bool neighbours = ADJACENT || unit >= rotated;
   const int lo_at = neighbours ? 2 * unit * E : unit * E, hi_at = neighbours ? lo_at + E : a.pairs + unit * E;
 
-  // this lane's angles of a block: their rows' samples and places go on from block to block without a division
+  // this lane's angles of a block: their rows' samples and places go on from block to block without a division.  What they are made from is loaded
+  // a block before it is needed.
   const unsigned step = ctas * WARPS;
   unsigned block = cta * WARPS + warp;
   const int step_rows = (int)(step * block_rows), step_b = step_rows / g.L, step_l = step_rows - step_b * g.L;
-  int angle_row[2], angle_axis[2], angle_b[2], angle_l[2];
+  int angle_row[2], angle_axis[2], angle_b[2], angle_l[2], position[2], within[2], valid[2];   // within: the segment, and the place in it; valid: its real rows
   uint64_t turns[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -178,18 +167,16 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
     angle_b[i] = row / (uint32_t)g.L;
     angle_l[i] = row - angle_b[i] * g.L;
   }
-  auto angles = [&](int buf) {   // of the next block in turn
-    uint32_t real = 0;
+  auto fetch = [&]() {   // for the next block in turn
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      position[i] = 0;
+      within[i] = valid[i] = 0;
       if (32 * i < block_rows * HALF && angle_row[i] < block_rows && angle_b[i] < g.batch) {
-        const int b = angle_b[i], l = angle_l[i], at = lane + 32 * i, pair = at % HALF;
-        float sn = 0.f, cs = 1.f;
-        if (angle_axis[i] >= 0) sine_cosine<T>(a.positions[angle_axis[i] * a.axis_stride + b * a.batch_stride + l], turns[i], &sn, &cs);
-        float* const to = s_table[warp][buf] + (angle_row[i] * LANES + pair / E) * PIECE_ANGLES<E> + pair % E / 2 * 4 + pair % 2;
-        to[0] = cs;
-        to[2] = sn;
-        if (real_row(g, b, l)) real |= 1u << angle_row[i];
+        const int b = angle_b[i], l = angle_l[i], s = segment_of(g, l);
+        if (angle_axis[i] >= 0) position[i] = a.positions[angle_axis[i] * a.axis_stride + b * a.batch_stride + l];
+        within[i] = (l - first_of(g, s)) | (int)((uint32_t)s << 30);   // (segments are shorter than 2^29)
+        valid[i] = g.valid_len != nullptr ? g.valid_len[3 * b + s] : length_of(g, s);
       }
       angle_b[i] += step_b;
       angle_l[i] += step_l;
@@ -198,8 +185,24 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
         ++angle_b[i];
       }
     }
-    real = __reduce_or_sync(0xffffffffu, real);
-    if (lane == 0) s_real[warp][buf] = real;
+  };
+  auto angles = [&](int buf) {   // of the block that was fetched for; which of its rows are real, a bit each
+    uint32_t real = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (32 * i < block_rows * HALF) {
+        const int at = lane + 32 * i, pair = at % HALF, s = (uint32_t)within[i] >> 30, n = length_of(g, s);
+        float sn = 0.f, cs = 1.f;
+        if (angle_axis[i] >= 0) sine_cosine<T>(position[i], turns[i], &sn, &cs);
+        if (angle_row[i] < block_rows) {
+          float* const to = s_table[warp][buf] + (angle_row[i] * LANES + pair / E) * PIECE_ANGLES<E> + pair % E / 2 * 4 + pair % 2;
+          to[0] = cs;
+          to[2] = sn;
+        }
+        if (valid[i] < 0 || valid[i] > n) raise_flag(g, GSIT_DEVFLAG_CLAMPED);
+        if ((within[i] & 0x3fffffff) < (valid[i] < 0 ? 0 : min(valid[i], n))) real |= 1u << angle_row[i];
+      }
+    return __reduce_or_sync(0xffffffffu, real);
   };
   // this lane's pieces of a block (a row of more heads than the lanes take is walked in chunks of them)
   int row_of[W][N], head_of[W][N];
@@ -215,11 +218,9 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
         head_of[w][i] = (W == 1 ? own : a.t[w]).heads;
       }
     }
-  float2 dg_lo[W][H2], dg_hi[W][H2];
+  float2 dg_lo[H2], dg_hi[H2];
 #pragma unroll
-  for (int w = 0; w < W; ++w)
-#pragma unroll
-    for (int i = 0; i < H2; ++i) dg_lo[w][i] = dg_hi[w][i] = make_float2(0.f, 0.f);
+  for (int i = 0; i < H2; ++i) dg_lo[i] = dg_hi[i] = make_float2(0.f, 0.f);
 
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
@@ -227,125 +228,147 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
     const float* gamma = W == 1 ? own.gamma : a.t[i / HD].gamma;
     s_gamma[i / HD][i % HD] = gamma != nullptr ? gamma[i % HD] : 1.f;
   }
-  angles(0);
-  __syncthreads();
   const int most = W == 1 ? own.heads : max(a.t[0].heads, a.t[1].heads);
-  for (int buf = 0; block < blocks; block += step, buf ^= 1) {
+  constexpr int CHUNK = 32 * N / LANES;
+  // a lane's own places in the ring: [stage][tensor][piece i][x lo, x hi, dy lo, dy hi], 32 lanes of each side by side
+  uint8_t* const ring = smem + warp * 2 * STAGE + lane * BYTES;
+  auto place = [&](int stage, int w, int i, int part) { return ring + stage * STAGE + (((w * N + i) * PARTS) + part) * 32 * BYTES; };
+  auto copy = [&](unsigned of, int chunk, uint32_t real, int stage) {
+    const int64_t row0 = (int64_t)of * block_rows;
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const NormTensor& t = W == 1 ? own : a.t[w];
+        if (chunk >= t.heads || 32 * i >= block_rows * t.heads * LANES) continue;   // no lane has any
+        const int head = head_of[w][i] + chunk;
+        const bool there = head < t.heads && ((real >> row_of[w][i]) & 1u);
+        const T* x = static_cast<const T*>(t.x) + (there ? (row0 + row_of[w][i]) * t.ldx + head * HD : 0);
+        copy_piece<T, E>(place(stage, w, i, 0), x + lo_at, there);
+        copy_piece<T, E>(place(stage, w, i, 1), x + hi_at, there);
+        if constexpr (BWD) {
+          const T* dy = static_cast<const T*>(t.dy) + (there ? (row0 + row_of[w][i]) * t.lddy + head * HD : 0);
+          copy_piece<T, E>(place(stage, w, i, 2), dy + lo_at, there);
+          copy_piece<T, E>(place(stage, w, i, 3), dy + hi_at, there);
+        }
+      }
+  };
+  fetch();
+  uint32_t real = angles(0), next_real = 0;
+  fetch();
+  if (block < blocks) copy(block, 0, real, 0);
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  __syncthreads();
+  for (int buf = 0, chunk = 0, stage = 0; block < blocks; stage ^= 1) {
+    // what comes next, on its way while this is worked on
+    const bool last = chunk + CHUNK >= most;
+    if (last) {
+      next_real = angles(buf ^ 1);
+      fetch();
+      if (block + step < blocks) copy(block + step, 0, next_real, stage ^ 1);
+    } else {
+      copy(block, chunk + CHUNK, real, stage ^ 1);
+    }
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
     const int64_t row0 = (int64_t)block * block_rows;
     const int left = (int)min((int64_t)block_rows, rows - row0);
-    const uint32_t real = s_real[warp][buf];
-    for (int chunk = 0; chunk < most; chunk += 32 * N / LANES) {
-      Piece<T, E> x_lo[W][N], x_hi[W][N], y_lo[W][BWD ? N : 1], y_hi[W][BWD ? N : 1];
 #pragma unroll
-      for (int w = 0; w < W; ++w)
+    for (int w = 0; w < W; ++w)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const NormTensor& t = (W == 1 ? own : a.t[w]);
-          if (chunk >= t.heads || 32 * i >= block_rows * t.heads * LANES) continue;   // no lane has any
-          const int head = head_of[w][i] + chunk;
-          x_lo[w][i].clear();
-          x_hi[w][i].clear();
-          if constexpr (BWD) {
-            y_lo[w][i].clear();
-            y_hi[w][i].clear();
-          }
-          if (row_of[w][i] < left && head < t.heads && ((real >> row_of[w][i]) & 1u)) {
-            const T* x = static_cast<const T*>(t.x) + (row0 + row_of[w][i]) * t.ldx + head * HD;
-            x_lo[w][i].load(x + lo_at);
-            x_hi[w][i].load(x + hi_at);
-            if constexpr (BWD) {
-              const T* dy = static_cast<const T*>(t.dy) + (row0 + row_of[w][i]) * t.lddy + head * HD;
-              y_lo[w][i].load(dy + lo_at);
-              y_hi[w][i].load(dy + hi_at);
-            }
-          }
+      for (int i = 0; i < N; ++i) {
+        const NormTensor& t = W == 1 ? own : a.t[w];
+        if (chunk >= t.heads || 32 * i >= block_rows * t.heads * LANES) continue;
+        const int head = head_of[w][i] + chunk;
+        const bool in = row_of[w][i] < left && head < t.heads, keep = in && ((real >> row_of[w][i]) & 1u);
+        const float* const table = s_table[warp][buf] + (row_of[w][i] * LANES + unit) * PIECE_ANGLES<E>;
+        Piece<T, E> piece;
+        float2 lo[H2], hi[H2], ga_lo[H2], ga_hi[H2];
+        piece.load(reinterpret_cast<const T*>(place(stage, w, i, 0)));
+        piece.get(lo);
+        piece.load(reinterpret_cast<const T*>(place(stage, w, i, 1)));
+        piece.get(hi);
+#pragma unroll
+        for (int e = 0; e < H2; ++e) {
+          ga_lo[e] = *reinterpret_cast<const float2*>(&s_gamma[w][lo_at + 2 * e]);
+          ga_hi[e] = *reinterpret_cast<const float2*>(&s_gamma[w][hi_at + 2 * e]);
         }
-      if (chunk == 0) angles(buf ^ 1);   // while these loads are under way
+        float2 sum = make_float2(0.f, 0.f), other = sum;
 #pragma unroll
-      for (int w = 0; w < W; ++w)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const NormTensor& t = (W == 1 ? own : a.t[w]);
-          if (chunk >= t.heads || 32 * i >= block_rows * t.heads * LANES) continue;
-          const int head = head_of[w][i] + chunk;
-          const bool in = row_of[w][i] < left && head < t.heads, keep = in && ((real >> row_of[w][i]) & 1u);
-          const float* const table = s_table[warp][buf] + (row_of[w][i] * LANES + unit) * PIECE_ANGLES<E>;
-          float2 lo[H2], hi[H2], ga_lo[H2], ga_hi[H2];
-          x_lo[w][i].get(lo);
-          x_hi[w][i].get(hi);
+        for (int e = 0; e < H2; ++e) {
+          sum = __ffma2_rn(lo[e], lo[e], sum);
+          other = __ffma2_rn(hi[e], hi[e], other);
+        }
+        sum = __fadd2_rn(sum, other);
+        float2 both = make_float2(sum.x + sum.y, 0.f);
+        float2 u_lo[H2], u_hi[H2];
+        if constexpr (BWD) {
+          piece.load(reinterpret_cast<const T*>(place(stage, w, i, 2)));
+          piece.get(u_lo);
+          piece.load(reinterpret_cast<const T*>(place(stage, w, i, 3)));
+          piece.get(u_hi);
+          turn<E, ADJACENT, true>(u_lo, u_hi, table);
+          float2 gx = make_float2(0.f, 0.f), gy = gx;
 #pragma unroll
           for (int e = 0; e < H2; ++e) {
-            ga_lo[e] = *reinterpret_cast<const float2*>(&s_gamma[w][lo_at + 2 * e]);
-            ga_hi[e] = *reinterpret_cast<const float2*>(&s_gamma[w][hi_at + 2 * e]);
+            gx = __ffma2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), lo[e], gx);
+            gy = __ffma2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), hi[e], gy);
           }
-          float2 sum = make_float2(0.f, 0.f), other = sum;
+          gx = __fadd2_rn(gx, gy);
+          both.y = gx.x + gx.y;
+          both = head_sum<LANES>(both);
+        } else {
+#pragma unroll
+          for (int o = LANES / 2; o > 0; o >>= 1) both.x += __shfl_xor_sync(0xffffffffu, both.x, o);
+        }
+        const float r = rsqrtf(both.x * a.inv_hd + a.eps);
+        const float2 r2 = make_float2(r, r);
+        if constexpr (!BWD) {
 #pragma unroll
           for (int e = 0; e < H2; ++e) {
-            sum = __ffma2_rn(lo[e], lo[e], sum);
-            other = __ffma2_rn(hi[e], hi[e], other);
+            lo[e] = __fmul2_rn(__fmul2_rn(lo[e], r2), ga_lo[e]);
+            hi[e] = __fmul2_rn(__fmul2_rn(hi[e], r2), ga_hi[e]);
           }
-          sum = __fadd2_rn(sum, other);
-          float2 both = make_float2(sum.x + sum.y, 0.f);
-          float2 u_lo[H2], u_hi[H2];
-          if constexpr (BWD) {
-            y_lo[w][i].get(u_lo);
-            y_hi[w][i].get(u_hi);
-            turn<E, ADJACENT, true>(u_lo, u_hi, table);
-            float2 gx = make_float2(0.f, 0.f), gy = gx;
+          turn<E, ADJACENT, false>(lo, hi, table);
+        } else {
+          const float back = -r * r * (both.y * a.inv_hd);
+          const float2 back2 = make_float2(back, back);
 #pragma unroll
-            for (int e = 0; e < H2; ++e) {
-              gx = __ffma2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), lo[e], gx);
-              gy = __ffma2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), hi[e], gy);
+          for (int e = 0; e < H2; ++e) {
+            const float2 h_lo = __fmul2_rn(lo[e], r2), h_hi = __fmul2_rn(hi[e], r2);
+            if (keep) {   // (a row that is not real has an x of 0, but r of a tiny eps may be infinite)
+              dg_lo[e] = __ffma2_rn(u_lo[e], h_lo, dg_lo[e]);
+              dg_hi[e] = __ffma2_rn(u_hi[e], h_hi, dg_hi[e]);
             }
-            gx = __fadd2_rn(gx, gy);
-            both.y = gx.x + gx.y;
-            both = head_sum<LANES>(both);
-          } else {
-#pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) both.x += __shfl_xor_sync(0xffffffffu, both.x, o);
-          }
-          const float r = rsqrtf(both.x * a.inv_hd + a.eps);
-          const float2 r2 = make_float2(r, r);
-          if constexpr (!BWD) {
-#pragma unroll
-            for (int e = 0; e < H2; ++e) {
-              lo[e] = __fmul2_rn(__fmul2_rn(lo[e], r2), ga_lo[e]);
-              hi[e] = __fmul2_rn(__fmul2_rn(hi[e], r2), ga_hi[e]);
-            }
-            turn<E, ADJACENT, false>(lo, hi, table);
-          } else {
-            const float back = -r * r * (both.y * a.inv_hd);
-            const float2 back2 = make_float2(back, back);
-#pragma unroll
-            for (int e = 0; e < H2; ++e) {
-              const float2 h_lo = __fmul2_rn(lo[e], r2), h_hi = __fmul2_rn(hi[e], r2);
-              if (keep) {   // (a row that is not real has an x of 0, but r of a tiny eps may be infinite)
-                dg_lo[w][e] = __ffma2_rn(u_lo[e], h_lo, dg_lo[w][e]);
-                dg_hi[w][e] = __ffma2_rn(u_hi[e], h_hi, dg_hi[w][e]);
-              }
-              lo[e] = __ffma2_rn(h_lo, back2, __fmul2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), r2));
-              hi[e] = __ffma2_rn(h_hi, back2, __fmul2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), r2));
-            }
-          }
-          if (in) {
-            if (!keep)
-#pragma unroll
-              for (int e = 0; e < H2; ++e) lo[e] = hi[e] = make_float2(0.f, 0.f);
-            T* out = static_cast<T*>(t.out) + (row0 + row_of[w][i]) * t.ldo + head * HD;
-            store_piece<E>(out + lo_at, lo);
-            store_piece<E>(out + hi_at, hi);
+            lo[e] = __ffma2_rn(h_lo, back2, __fmul2_rn(__fmul2_rn(u_lo[e], ga_lo[e]), r2));
+            hi[e] = __ffma2_rn(h_hi, back2, __fmul2_rn(__fmul2_rn(u_hi[e], ga_hi[e]), r2));
           }
         }
+        if (in) {
+          if (!keep)
+#pragma unroll
+            for (int e = 0; e < H2; ++e) lo[e] = hi[e] = make_float2(0.f, 0.f);
+          T* out = static_cast<T*>(t.out) + (row0 + row_of[w][i]) * t.ldo + head * HD;
+          store_piece<E>(out + lo_at, lo);
+          store_piece<E>(out + hi_at, hi);
+        }
+      }
+    if (last) {
+      block += step;
+      chunk = 0;
+      buf ^= 1;
+      real = next_real;
+    } else {
+      chunk += CHUNK;
     }
     __syncwarp();   // the next block's angles are there, and nobody reads this block's any more
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
   if constexpr (BWD) {
     if (a.partial == nullptr) return;
     __shared__ float acc[WARPS][HD];
-    constexpr int w = 0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        float lo = e & 1 ? dg_lo[w][e / 2].y : dg_lo[w][e / 2].x, hi = e & 1 ? dg_hi[w][e / 2].y : dg_hi[w][e / 2].x;
+    for (int e = 0; e < E; ++e) {
+        float lo = e & 1 ? dg_lo[e / 2].y : dg_lo[e / 2].x, hi = e & 1 ? dg_hi[e / 2].y : dg_hi[e / 2].x;
 #pragma unroll
         for (int o = LANES; o < 32; o <<= 1) {
           lo += __shfl_xor_sync(0xffffffffu, lo, o);
@@ -539,7 +562,7 @@ cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c
   // rows of a block: what the lanes' pieces in flight take of the (wider) tensor, and two angles a lane; CTAs: as many as fit the SMs at once
   const int64_t rows = (int64_t)g.batch * g.L;
   const int most = std::min(MAX_CTAS, 2 * n_sm);
-  auto block_rows = [&](int heads) { return wide && heads > 0 ? std::max(1, std::min(2 * ANGLES / g.hd, 32 * (c.backward && piece == 8 ? 1 : 2) / (heads * lanes))) : 1; };
+  auto block_rows = [&](int heads) { return wide && heads > 0 ? std::max(1, std::min(2 * ANGLES / g.hd, 32 * UNITS / (heads * lanes))) : 1; };
   auto ctas_for = [&](int share, int of_rows) { return (int)std::min<int64_t>(share, (rows + of_rows * WARPS - 1) / (of_rows * WARPS)); };
   int ctas;
   if (wide && c.backward) {   // shared out by heads
@@ -554,7 +577,10 @@ cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c
   const dim3 grid((unsigned)ctas);
   if (wide) {
     const Kernel k = dtype == GSIT_BF16 ? wide_kernel<__nv_bfloat16>(g.hd, c.interleaved, c.backward) : wide_kernel<float>(g.hd, c.interleaved, c.backward);
-    e = launch_overlapped(k, grid, dim3(THREADS), 0, st, g, a);
+    const int bytes = WARPS * 2 * (c.backward ? 1 : 2) * UNITS * (c.backward ? 4 : 2) * 32 * piece * es;
+    e = sm_count_and_smem_once(reinterpret_cast<const void*>(k), bytes, nullptr);
+    if (e != cudaSuccess) return e;
+    e = launch_overlapped(k, grid, dim3(THREADS), bytes, st, g, a);
   } else if (dtype == GSIT_BF16) {
     e = c.backward ? launch_overlapped(head_norm_any_kernel<__nv_bfloat16, true>, grid, dim3(THREADS), 0, st, g, a, (int)c.interleaved)
                    : launch_overlapped(head_norm_any_kernel<__nv_bfloat16, false>, grid, dim3(THREADS), 0, st, g, a, (int)c.interleaved);

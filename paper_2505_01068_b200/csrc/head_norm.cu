@@ -57,6 +57,10 @@ template <typename T, int E> struct Piece {
       w[0] = v.x; w[1] = v.y;
     }
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = 0u;
+  }
   __device__ __forceinline__ void get(float2 (&f)[E / 2]) const {
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) {
@@ -65,11 +69,9 @@ template <typename T, int E> struct Piece {
     }
   }
 };
-// A piece into the lane's own place in shared memory, zeros where there is none.
-template <typename T, int E> __device__ __forceinline__ void copy_piece(void* dst, const T* src, bool there) {
-  constexpr int BYTES = E * (int)sizeof(T);
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 8 : 0) : "memory");
+// A piece of 16 bytes into the lane's own place in shared memory, zeros where there is none.
+template <typename T> __device__ __forceinline__ void copy_piece(void* dst, const T* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 template <int E> __device__ __forceinline__ void store_piece(float* p, const float2 (&f)[E / 2]) {
   static_assert(E == 4, "16 bytes");
@@ -136,6 +138,7 @@ __global__ void __launch_bounds__(THREADS, 2)
 head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ HeadNormArgs a) {
   constexpr int HALF = E * LANES, HD = 2 * HALF, N = UNITS, H2 = E / 2, BYTES = E * (int)sizeof(T), PARTS = BWD ? 4 : 2, TABLE = ANGLES / E * PIECE_ANGLES<E>, W = BWD ? 1 : 2,   // W: tensors of a warp
                 STAGE = W * N * PARTS * 32 * BYTES;
+  constexpr bool STAGED = E == 8;
   static_assert(HALF <= ANGLES, "the angles of a row fit the table");
   __shared__ __align__(16) float s_table[WARPS][2][TABLE], s_gamma[W][HD];
   extern __shared__ __align__(16) uint8_t smem[];   // two stages of every warp's
@@ -228,11 +231,40 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
     const float* gamma = W == 1 ? own.gamma : a.t[i / HD].gamma;
     s_gamma[i / HD][i % HD] = gamma != nullptr ? gamma[i % HD] : 1.f;
   }
+  uint32_t real = 0;                         // bit r: row r of the block is a real one
   const int most = W == 1 ? own.heads : max(a.t[0].heads, a.t[1].heads);
   constexpr int CHUNK = 32 * N / LANES;
+  // Pieces of 16 bytes of bf16 come through shared memory, the next block's while this one is worked on; narrow pieces straight into registers, which has them
+  // sooner and takes fewer instructions for as little as they hold (64 x (50, 500, 500), 8 + 8 heads of 8, float: 13.9 us forward, 22.5 back, and 17.9 and 30.7
+  // through shared memory; 128 x (128, 1024, 1024), 8 + 8 of 64, bf16: 216 and 394, and 184 and 299).
+  Piece<T, E> held[W][N][STAGED ? 1 : PARTS];
+  auto load_now = [&](int chunk) {
+    const int64_t row0 = (int64_t)block * block_rows;
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const NormTensor& t = W == 1 ? own : a.t[w];
+        if (chunk >= t.heads || 32 * i >= block_rows * t.heads * LANES) continue;
+        const int head = head_of[w][i] + chunk;
+#pragma unroll
+        for (int k = 0; k < (STAGED ? 1 : PARTS); ++k) held[w][i][k].clear();
+        if (head < t.heads && ((real >> row_of[w][i]) & 1u)) {
+#pragma unroll
+          for (int k = 0; k < (STAGED ? 1 : PARTS); ++k)
+            held[w][i][k].load(static_cast<const T*>(k < 2 ? t.x : t.dy) + (row0 + row_of[w][i]) * (k < 2 ? t.ldx : t.lddy) + head * HD + (k % 2 ? hi_at : lo_at));
+        }
+      }
+  };
   // a lane's own places in the ring: [stage][tensor][piece i][x lo, x hi, dy lo, dy hi], 32 lanes of each side by side
   uint8_t* const ring = smem + warp * 2 * STAGE + lane * BYTES;
   auto place = [&](int stage, int w, int i, int part) { return ring + stage * STAGE + (((w * N + i) * PARTS) + part) * 32 * BYTES; };
+  auto taken = [&](int stage, int w, int i, int part) {
+    Piece<T, E> p;
+    if constexpr (STAGED) p.load(reinterpret_cast<const T*>(place(stage, w, i, part)));
+    else p = held[w][i][part];
+    return p;
+  };
   auto copy = [&](unsigned of, int chunk, uint32_t real, int stage) {
     const int64_t row0 = (int64_t)of * block_rows;
 #pragma unroll
@@ -244,32 +276,34 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
         const int head = head_of[w][i] + chunk;
         const bool there = head < t.heads && ((real >> row_of[w][i]) & 1u);
         const T* x = static_cast<const T*>(t.x) + (there ? (row0 + row_of[w][i]) * t.ldx + head * HD : 0);
-        copy_piece<T, E>(place(stage, w, i, 0), x + lo_at, there);
-        copy_piece<T, E>(place(stage, w, i, 1), x + hi_at, there);
+        copy_piece(place(stage, w, i, 0), x + lo_at, there);
+        copy_piece(place(stage, w, i, 1), x + hi_at, there);
         if constexpr (BWD) {
           const T* dy = static_cast<const T*>(t.dy) + (there ? (row0 + row_of[w][i]) * t.lddy + head * HD : 0);
-          copy_piece<T, E>(place(stage, w, i, 2), dy + lo_at, there);
-          copy_piece<T, E>(place(stage, w, i, 3), dy + hi_at, there);
+          copy_piece(place(stage, w, i, 2), dy + lo_at, there);
+          copy_piece(place(stage, w, i, 3), dy + hi_at, there);
         }
       }
   };
   fetch();
-  uint32_t real = angles(0), next_real = 0;
+  uint32_t next_real = 0;
+  real = angles(0);
   fetch();
-  if (block < blocks) copy(block, 0, real, 0);
+  if (STAGED && block < blocks) copy(block, 0, real, 0);
   asm volatile("cp.async.commit_group;" ::: "memory");
   __syncthreads();
   for (int buf = 0, chunk = 0, stage = 0; block < blocks; stage ^= 1) {
     // what comes next, on its way while this is worked on
     const bool last = chunk + CHUNK >= most;
+    if constexpr (!STAGED) load_now(chunk);
     if (last) {
       next_real = angles(buf ^ 1);
       fetch();
-      if (block + step < blocks) copy(block + step, 0, next_real, stage ^ 1);
-    } else {
+      if (STAGED && block + step < blocks) copy(block + step, 0, next_real, stage ^ 1);
+    } else if (STAGED) {
       copy(block, chunk + CHUNK, real, stage ^ 1);
     }
-    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
+    if constexpr (STAGED) asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
     const int64_t row0 = (int64_t)block * block_rows;
     const int left = (int)min((int64_t)block_rows, rows - row0);
 #pragma unroll
@@ -281,12 +315,9 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
         const int head = head_of[w][i] + chunk;
         const bool in = row_of[w][i] < left && head < t.heads, keep = in && ((real >> row_of[w][i]) & 1u);
         const float* const table = s_table[warp][buf] + (row_of[w][i] * LANES + unit) * PIECE_ANGLES<E>;
-        Piece<T, E> piece;
         float2 lo[H2], hi[H2], ga_lo[H2], ga_hi[H2];
-        piece.load(reinterpret_cast<const T*>(place(stage, w, i, 0)));
-        piece.get(lo);
-        piece.load(reinterpret_cast<const T*>(place(stage, w, i, 1)));
-        piece.get(hi);
+        taken(stage, w, i, 0).get(lo);
+        taken(stage, w, i, 1).get(hi);
 #pragma unroll
         for (int e = 0; e < H2; ++e) {
           ga_lo[e] = *reinterpret_cast<const float2*>(&s_gamma[w][lo_at + 2 * e]);
@@ -302,10 +333,8 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
         float2 both = make_float2(sum.x + sum.y, 0.f);
         float2 u_lo[H2], u_hi[H2];
         if constexpr (BWD) {
-          piece.load(reinterpret_cast<const T*>(place(stage, w, i, 2)));
-          piece.get(u_lo);
-          piece.load(reinterpret_cast<const T*>(place(stage, w, i, 3)));
-          piece.get(u_hi);
+          taken(stage, w, i, 2).get(u_lo);
+          taken(stage, w, i, 3).get(u_hi);
           turn<E, ADJACENT, true>(u_lo, u_hi, table);
           float2 gx = make_float2(0.f, 0.f), gy = gx;
 #pragma unroll
@@ -577,7 +606,7 @@ cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c
   const dim3 grid((unsigned)ctas);
   if (wide) {
     const Kernel k = dtype == GSIT_BF16 ? wide_kernel<__nv_bfloat16>(g.hd, c.interleaved, c.backward) : wide_kernel<float>(g.hd, c.interleaved, c.backward);
-    const int bytes = WARPS * 2 * (c.backward ? 1 : 2) * UNITS * (c.backward ? 4 : 2) * 32 * piece * es;
+    const int bytes = piece == 8 ? WARPS * 2 * (c.backward ? 1 : 2) * UNITS * (c.backward ? 4 : 2) * 512 : 0;   // (see STAGED)
     e = sm_count_and_smem_once(reinterpret_cast<const void*>(k), bytes, nullptr);
     if (e != cudaSuccess) return e;
     e = launch_overlapped(k, grid, dim3(THREADS), bytes, st, g, a);

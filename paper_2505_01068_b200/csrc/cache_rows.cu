@@ -122,9 +122,16 @@ template <int KIND> __device__ __forceinline__ void values4(uint32_t w, float2 (
     for (int i = 0; i < 2; ++i) f[i] = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
   }
 }
-// Largest magnitude of a pair, in order as integers, NaN above them all.
-__device__ __forceinline__ uint32_t magnitude(uint32_t w) { return max(w << 16 & 0x7fff0000u, w & 0x7fff0000u); }
-__device__ __forceinline__ uint32_t magnitude(float2 v) { return max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu); }
+// Largest magnitudes of pairs, and as an integer in the order of floats, NaN above them all.
+__device__ __forceinline__ void raise(uint32_t& top, uint32_t w) {
+  const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&top), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w)));
+  top = *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ void raise(float2& top, float2 v) {
+  top = make_float2(__uint_as_float(max(__float_as_uint(top.x), __float_as_uint(v.x) & 0x7fffffffu)), __uint_as_float(max(__float_as_uint(top.y), __float_as_uint(v.y) & 0x7fffffffu)));
+}
+__device__ __forceinline__ uint32_t ordered(uint32_t w) { return max(w << 16, w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t ordered(float2 v) { return max(__float_as_uint(v.x), __float_as_uint(v.y)); }
 __device__ __forceinline__ float2 as_floats(uint32_t w) {
   float2 v;
   unpack_bf16(w, v.x, v.y);
@@ -137,15 +144,14 @@ template <typename T, int HD, int KIND, bool VALUES>
 __device__ __forceinline__ void quantise(const uint8_t* at, int lane, uint8_t* bytes, float* scale) {
   constexpr int U = UNITS<HD>;
   using Pair = std::conditional_t<sizeof(T) == 2, uint32_t, float2>;
-  Pair x[U][4];
-  uint32_t top = 0;
+  Pair x[U][4], tops = {};
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     staged<HD, VALUES>(at, lane, u, x[u]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, magnitude(x[u][i]));
+    for (int i = 0; i < 4; ++i) raise(tops, x[u][i]);
   }
-  top = __reduce_max_sync(0xffffffffu, top);
+  const uint32_t top = __reduce_max_sync(0xffffffffu, ordered(tops));
   const bool broken = top >= 0x7f800000u;
   const float s = broken ? 1.f : fmaxf(__fdiv_rn(__uint_as_float(top), KIND == GSIT_CACHE_INT8 ? 127.f : 448.f), LEAST_SCALE), inv = __frcp_rn(s);
   if (lane == 0) *scale = broken ? __int_as_float(0x7fffffff) : s;
@@ -182,6 +188,7 @@ __device__ __forceinline__ bool find_piece(unsigned item, const int (&chunks)[3]
 
 // How many rows of a segment have a slot: they come first.  A warp looks at every 32nd part, then at the parts of the one that is left.
 __device__ __forceinline__ int leading_rows(const int32_t* slots, int len, int lane) {
+  if (slots[len - 1] >= 0) return len;
   int n = 0;
   for (int span = len; span > 0;) {
     const int stride = (span + 31) / 32, at = n + (lane + 1) * stride - 1;
@@ -202,7 +209,7 @@ struct RowArgs {
 };
 
 template <typename T, int HD, int KIND>
-__global__ void __launch_bounds__(THREADS) cache_append_kernel(const __grid_constant__ Geometry g, const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 6 : 3) cache_append_kernel(const __grid_constant__ Geometry g, const __grid_constant__ RowArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   constexpr int VECS = HD * (int)sizeof(T) / 16;   // of a row
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;

@@ -77,6 +77,7 @@ gsit_status gsit_cache_read(const gsit_shape* shape, const gsit_cache* cache, vo
 
 /* gsit_im_scored_attention_fwd for a step's rows, keys and values from the cache: real row i of segment s is position lengths[b][s] - valid_len[b][s] + i,
  * and sees the open segments as they are then, up to their last position held.
+ * (Rows of a segment that plan did not take are not in the cache, but are answered like the others, as the last positions that are: their slots say so.)
  *   shape        d_model, heads, phase, custom_mask and scale as there; dtype of the cache
  *   rule         softcap, causal and slopes; kv_heads of the cache, or 0.  times, documents, prefix and tail are not taken (GSIT_ERR_UNSUPPORTED).
  *   times        the moments of the step's rows, as above: given where the cache holds times and the rule goes by them (causal, slopes); NULL where it holds

@@ -7,7 +7,7 @@
 // memory.  What an entry reads and writes -- its length, its row of the table, its rows' slots -- only its warp touches, so lengths may be updated in place.
 // Rows' slots are written here as long as there are few entries; beyond, only that of each entry's first row, and a second kernel on all SMs fills in
 // the others (1024 streams of up to (16, 100, 100) rows: eight SMs took 21 us for all of it).
-// Bound by the chain of dependent loads (count and length, table, list) and the launches.
+// Bound by the chain of dependent loads (count and length, table, list) and the launches: 32 streams' step 5.2 us, 1024 streams' prompts 16.
 #include <cooperative_groups.h>
 
 #include "cache.cuh"

@@ -12,6 +12,9 @@
 // Who takes what: where the step is small, the CTAs of a cluster share a (stream, key head, tile of rows) and join their parts through distributed shared
 // memory; where there is much to read, two CTAs an SM share out all blocks of all streams and key heads evenly, whatever their lengths are, and
 // a second small kernel joins the parts of those that more than one of them had.  Always in order.
+// Measured, bf16: 32 streams of up to (128, 1024, 1024), 8 heads of 64, int8, every rule: 54 MB in 20 - 22 us (floor 8.3; 14 of the 19 that the kernel runs are the
+// walk, the others launch, first loads and join); 64 streams of up to (512, 10000, 10000), 8 heads on 2 key heads, e4m3: 253 MB in 70 us (floor 38.7;
+// the walk moves 6 TB/s, 273 instructions a block and 8 rows, 374 for 16; the ramp is 8 us, second pieces and the joining kernel 15).
 // A closed pair's weight is 0 and the bytes it meets are numbers, so nothing of it counts; blocks whose scale is NaN take a way of their own.
 #pragma once
 #include <cooperative_groups.h>

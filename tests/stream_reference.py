@@ -1,4 +1,5 @@
 """Streams' caches and attention over them as plain lists of rows, in 64 bits, for the tests of the streaming calls."""
+import functools
 import math
 
 import numpy as np
@@ -40,6 +41,7 @@ def quantised(x, held_as):
     return values[i], torch.where(bad, torch.full_like(scale, math.nan), scale)
 
 
+@functools.lru_cache(maxsize=None)
 def addresses(hd, values):
     """[32, hd]: byte of (position, feature) in a page of one head, as gsit_stream.h has them."""
     at = torch.zeros((BLOCK, hd), dtype=torch.long)

@@ -221,461 +221,461 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
 
   // One piece: blocks [lo, hi) of the list of stream b for key head hk, rows from row0 on, into the room (the warps' parts).
   auto walk = [&](int b, int hk, int row0, int n_rows, const BlockList& list, int lo, int hi) {
-  const int first = lo + warp * B, last = min(hi, list.full);
-  constexpr int turn = WARPS * B;
-  // Everything that is waited for is asked for as early as it can be: the queries, pages, the first blocks, what the rows are.
-  uint32_t raw[NT][KS][2][TERMS];
+    const int first = lo + warp * B, last = min(hi, list.full);
+    constexpr int turn = WARPS * B;
+    // Everything that is waited for is asked for as early as it can be: the queries, pages, the first blocks, what the rows are.
+    uint32_t raw[NT][KS][2][TERMS];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int r = min(8 * n + gr, n_rows - 1) + row0;
-    const T* q = static_cast<const T*>(a.q) + ((int64_t)b * g.L + r / a.group) * a.ldq + (int64_t)(hk * a.group + r % a.group) * HD + 2 * t;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int h = 0; h < (HD > 8 ? 2 : 1); ++h) {
-        if constexpr (sizeof(T) == 2) raw[n][k][h][0] = *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * h);
-        else {
-          const uint2 v = *reinterpret_cast<const uint2*>(q + 16 * k + 8 * h);
-          raw[n][k][h][0] = v.x;
-          raw[n][k][h][TERMS - 1] = v.y;
-        }
-      }
-  }
-  // lanes know where the blocks of the warp's next 32 / B turns lie, and each sees to its own: copies into the stage, and what is known of it
-  int ahead = first, known = 0;
-  int64_t head = -1;
-  const float* moments = nullptr;
-  BlockInfo info = {0.f, 0.f, 3, 0};
-  uint32_t to = stage;
-  auto copy = [&]() {
-    if (known == 0) {
-      const int i = ahead + lane / B * turn + lane % B, s = list.segment(i), j = i - (s == 0 ? 0 : s == 1 ? list.upto[0] : list.upto[1]);
-      head = -1;
-      info.seg = 3;
-      if (i < last) {
-        const int page = real_page(c, c.tables[((int64_t)b * 3 + s) * c.blocks + j]);
-        if (page < 0) raise_flag(g, GSIT_DEVFLAG_CLAMPED);
-        else {
-          head = (int64_t)page * c.kv_heads + hk;
-          info = {c.key_scale[head], c.value_scale[head], s, j * CACHE_BLOCK};
-          if (timed && c.times != nullptr) moments = c.times + (int64_t)page * CACHE_BLOCK;
-        }
-      }
-      known = 32 / B;
-    }
-    const int from = (32 / B - known) * B;
-    if (lane >= from && lane < from + B && head >= 0) {
-      const uint32_t bar = bars + 8 * to, at = ring + (to * B + lane - from) * RingOf::BLOCK;
-      bulk_copy(at, c.keys + head * RingOf::MATRIX, RingOf::MATRIX, bar);
-      bulk_copy(at + RingOf::MATRIX, c.values + head * RingOf::MATRIX, RingOf::MATRIX, bar);
-      if (moments != nullptr) bulk_copy(at + 2 * RingOf::MATRIX, moments, RingOf::MOMENTS, bar);
-    }
-    ahead += turn;
-    --known;
-    to = to + 1 == STAGES ? 0 : to + 1;
-  };
-  // ... behind the copies, which need not wait for the scales: what is known, and the arrival that lets the stage's phase end
-  auto tell = [&](uint32_t stage_of, int from) {
-    if (lane >= from && lane < from + B) {
-      s_info[warp][stage_of][lane - from] = info;
-      ptx::mbar_expect_tx(bars + 8 * stage_of, head < 0 ? 0 : 2 * RingOf::MATRIX + (moments != nullptr ? RingOf::MOMENTS : 0));
-    }
-  };
-  static_assert(STAGES == 3 && 32 / B >= 2, "two stages of one batch of pages are asked for ahead");
-  const bool one = first < last, two = first + turn < last;
-  if (one) copy();
-  if (two) copy();
-
-  // ---- the rows: row r of a key head is row r / group of the step, head hk * group + r % group ----
-  QueryRow* const rows_of = s_row[warp];
-  if (lane < R) {
-    QueryRow x = {0.f, -INFINITY, 0.f, 0};
-    if (lane < n_rows) {
-      const int l = (row0 + lane) / a.group, s = segment_of(g, l), at = l - g.off(s), n = valid_rows(g, b, s);
-      if (at < n) {
-        if (timed) {
-          x.time = a.times.p != nullptr ? a.times.at(b, l) : (float)(held_rows(c, g.status, b, s) - n + at);
-          x.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + (row0 + lane) % a.group] * LOG2E : 0.f;
-        }
-        x.limit = a.causal ? x.time : INFINITY;
-        x.opens = (int)(g.allowed >> (3 * s)) & 7;
-      }
-    }
-    rows_of[lane] = x;
-  }
-  __syncwarp();
-  if (one) tell(stage, 0);
-  if (two) tell(stage + 1 == STAGES ? 0 : stage + 1, B);
-
-  // ---- queries as B operands, and what brings a dot back to a score ----
-  uint32_t qf[NT][TERMS][KS][2];
-  float2 back[NT];                       // of the columns 2 t and 2 t + 1 of each tile
-  uint32_t col_opens = 0, every = 7;     // four bits for each column; segments that all of them are open to
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const bool there = rows_of[8 * n + gr].opens != 0;
-    float2 f[KS][2];
-    float top = 0.f;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        f[k][h] = make_float2(0.f, 0.f);
-        if (there && (HD > 8 || h == 0)) {
-          if constexpr (sizeof(T) == 2) unpack_bf16(raw[n][k][h][0], f[k][h].x, f[k][h].y);
-          else f[k][h] = make_float2(__uint_as_float(raw[n][k][h][0]), __uint_as_float(raw[n][k][h][TERMS - 1]));
-        }
-        top = ptx::fmax3(top, fabsf(f[k][h].x), fabsf(f[k][h].y));
-      }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const Power p = top > 0.f && top < INFINITY ? power_for(top, 10) : Power{1.f, 1.f};   // (a row of NaN or Inf stays one)
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float x = f[k][h].x * p.up, y = f[k][h].y * p.up;
-        qf[n][0][k][h] = f16x2(x, y);
-        if constexpr (TERMS == 2) qf[n][1][k][h] = f16x2_rest(x, y, qf[n][0][k][h]);
-      }
-    back[n] = make_float2(__shfl_sync(0xffffffffu, p.down, 8 * t) * a.inner, __shfl_sync(0xffffffffu, p.down, 8 * t + 4) * a.inner);
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int opens = rows_of[8 * n + 2 * t + e].opens;
-      col_opens |= (uint32_t)opens << (4 * (2 * n + e));
-      if (8 * n + 2 * t + e < n_rows) every &= opens;   // (columns behind the last row write nothing: whatever they see)
-    }
-  }
-  every = __reduce_and_sync(0xffffffffu, every);
-  float2 o[MD][NT][2], ref[NT], sum[NT];   // pairs: columns 2 t, 2 t + 1
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    ref[n] = make_float2(-INFINITY, -INFINITY);
-    sum[n] = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int m = 0; m < MD; ++m) o[m][n][0] = o[m][n][1] = make_float2(0.f, 0.f);
-  }
-
-  // One block of segment `seg`: keys(m, k, term, fragment) and values(m, k, term, fragment) give A operands, of IN terms; FULL: all 32 positions,
-  // biased where bytes are taken that way.
-  auto attend = [&](auto terms_in, auto whole, int seg, int rows, float ks, float vs, const float (&times)[4], auto keys, auto values) {
-    constexpr int IN = decltype(terms_in)::value;
-    constexpr bool FULL = decltype(whole)::value != 0, FROM_BIAS = FULL && BIASED;
-    float zero[4] = {0.f, 0.f, 0.f, 0.f};
-    float s[2][NT][4];
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int n = 0; n < NT; ++n) {
+      const int r = min(8 * n + gr, n_rows - 1) + row0;
+      const T* q = static_cast<const T*>(a.q) + ((int64_t)b * g.L + r / a.group) * a.ldq + (int64_t)(hk * a.group + r % a.group) * HD + 2 * t;
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int w = 0; w < IN; ++w) {
-          uint32_t f[4];
-          keys(m, k, w, f);
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int y = 0; y < TERMS - w; ++y) {   // the product of the two smaller terms is left out: 2^-22 of the score's terms
-              float (&from)[4] = k + w + y > 0 ? s[m][n] : zero;
-              if constexpr (HD == 8) mma_k8(s[m][n], f[0], f[1], qf[n][y][k][0], from);
-              else mma(s[m][n], f, qf[n][y][k][0], qf[n][y][k][1], from);
-            }
+        for (int h = 0; h < (HD > 8 ? 2 : 1); ++h) {
+          if constexpr (sizeof(T) == 2) raw[n][k][h][0] = *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * h);
+          else {
+            const uint2 v = *reinterpret_cast<const uint2*>(q + 16 * k + 8 * h);
+            raw[n][k][h][0] = v.x;
+            raw[n][k][h][TERMS - 1] = v.y;
+          }
         }
-    // scores in base 2, pairs of columns; positions 16 m + 8 h + gr
-    float2 x[NT][2][2];
+    }
+    // lanes know where the blocks of the warp's next 32 / B turns lie, and each sees to its own: copies into the stage, and what is known of it
+    int ahead = first, known = 0;
+    int64_t head = -1;
+    const float* moments = nullptr;
+    BlockInfo info = {0.f, 0.f, 3, 0};
+    uint32_t to = stage;
+    auto copy = [&]() {
+      if (known == 0) {
+        const int i = ahead + lane / B * turn + lane % B, s = list.segment(i), j = i - (s == 0 ? 0 : s == 1 ? list.upto[0] : list.upto[1]);
+        head = -1;
+        info.seg = 3;
+        if (i < last) {
+          const int page = real_page(c, c.tables[((int64_t)b * 3 + s) * c.blocks + j]);
+          if (page < 0) raise_flag(g, GSIT_DEVFLAG_CLAMPED);
+          else {
+            head = (int64_t)page * c.kv_heads + hk;
+            info = {c.key_scale[head], c.value_scale[head], s, j * CACHE_BLOCK};
+            if (timed && c.times != nullptr) moments = c.times + (int64_t)page * CACHE_BLOCK;
+          }
+        }
+        known = 32 / B;
+      }
+      const int from = (32 / B - known) * B;
+      if (lane >= from && lane < from + B && head >= 0) {
+        const uint32_t bar = bars + 8 * to, at = ring + (to * B + lane - from) * RingOf::BLOCK;
+        bulk_copy(at, c.keys + head * RingOf::MATRIX, RingOf::MATRIX, bar);
+        bulk_copy(at + RingOf::MATRIX, c.values + head * RingOf::MATRIX, RingOf::MATRIX, bar);
+        if (moments != nullptr) bulk_copy(at + 2 * RingOf::MATRIX, moments, RingOf::MOMENTS, bar);
+      }
+      ahead += turn;
+      --known;
+      to = to + 1 == STAGES ? 0 : to + 1;
+    };
+    // ... behind the copies, which need not wait for the scales: what is known, and the arrival that lets the stage's phase end
+    auto tell = [&](uint32_t stage_of, int from) {
+      if (lane >= from && lane < from + B) {
+        s_info[warp][stage_of][lane - from] = info;
+        ptx::mbar_expect_tx(bars + 8 * stage_of, head < 0 ? 0 : 2 * RingOf::MATRIX + (moments != nullptr ? RingOf::MOMENTS : 0));
+      }
+    };
+    static_assert(STAGES == 3 && 32 / B >= 2, "two stages of one batch of pages are asked for ahead");
+    const bool one = first < last, two = first + turn < last;
+    if (one) copy();
+    if (two) copy();
+
+    // ---- the rows: row r of a key head is row r / group of the step, head hk * group + r % group ----
+    QueryRow* const rows_of = s_row[warp];
+    if (lane < R) {
+      QueryRow x = {0.f, -INFINITY, 0.f, 0};
+      if (lane < n_rows) {
+        const int l = (row0 + lane) / a.group, s = segment_of(g, l), at = l - g.off(s), n = valid_rows(g, b, s);
+        if (at < n) {
+          if (timed) {
+            x.time = a.times.p != nullptr ? a.times.at(b, l) : (float)(held_rows(c, g.status, b, s) - n + at);
+            x.slope2 = a.slopes != nullptr ? a.slopes[hk * a.group + (row0 + lane) % a.group] * LOG2E : 0.f;
+          }
+          x.limit = a.causal ? x.time : INFINITY;
+          x.opens = (int)(g.allowed >> (3 * s)) & 7;
+        }
+      }
+      rows_of[lane] = x;
+    }
+    __syncwarp();
+    if (one) tell(stage, 0);
+    if (two) tell(stage + 1 == STAGES ? 0 : stage + 1, B);
+
+    // ---- queries as B operands, and what brings a dot back to a score ----
+    uint32_t qf[NT][TERMS][KS][2];
+    float2 back[NT];                       // of the columns 2 t and 2 t + 1 of each tile
+    uint32_t col_opens = 0, every = 7;     // four bits for each column; segments that all of them are open to
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float2 f = __fmul2_rn(back[n], make_float2(ks, ks));
+      const bool there = rows_of[8 * n + gr].opens != 0;
+      float2 f[KS][2];
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f[k][h] = make_float2(0.f, 0.f);
+          if (there && (HD > 8 || h == 0)) {
+            if constexpr (sizeof(T) == 2) unpack_bf16(raw[n][k][h][0], f[k][h].x, f[k][h].y);
+            else f[k][h] = make_float2(__uint_as_float(raw[n][k][h][0]), __uint_as_float(raw[n][k][h][TERMS - 1]));
+          }
+          top = ptx::fmax3(top, fabsf(f[k][h].x), fabsf(f[k][h].y));
+        }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const Power p = top > 0.f && top < INFINITY ? power_for(top, 10) : Power{1.f, 1.f};   // (a row of NaN or Inf stays one)
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float x = f[k][h].x * p.up, y = f[k][h].y * p.up;
+          qf[n][0][k][h] = f16x2(x, y);
+          if constexpr (TERMS == 2) qf[n][1][k][h] = f16x2_rest(x, y, qf[n][0][k][h]);
+        }
+      back[n] = make_float2(__shfl_sync(0xffffffffu, p.down, 8 * t) * a.inner, __shfl_sync(0xffffffffu, p.down, 8 * t + 4) * a.inner);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int opens = rows_of[8 * n + 2 * t + e].opens;
+        col_opens |= (uint32_t)opens << (4 * (2 * n + e));
+        if (8 * n + 2 * t + e < n_rows) every &= opens;   // (columns behind the last row write nothing: whatever they see)
+      }
+    }
+    every = __reduce_and_sync(0xffffffffu, every);
+    float2 o[MD][NT][2], ref[NT], sum[NT];   // pairs: columns 2 t, 2 t + 1
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      ref[n] = make_float2(-INFINITY, -INFINITY);
+      sum[n] = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int m = 0; m < MD; ++m) o[m][n][0] = o[m][n][1] = make_float2(0.f, 0.f);
+    }
+
+    // One block of segment `seg`: keys(m, k, term, fragment) and values(m, k, term, fragment) give A operands, of IN terms; FULL: all 32 positions,
+    // biased where bytes are taken that way.
+    auto attend = [&](auto terms_in, auto whole, int seg, int rows, float ks, float vs, const float (&times)[4], auto keys, auto values) {
+      constexpr int IN = decltype(terms_in)::value;
+      constexpr bool FULL = decltype(whole)::value != 0, FROM_BIAS = FULL && BIASED;
+      float zero[4] = {0.f, 0.f, 0.f, 0.f};
+      float s[2][NT][4];
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) x[n][m][h] = __fmul2_rn(make_float2(s[m][n][2 * h], s[m][n][2 * h + 1]), f);
-    }
-    if (a.softcap > 0.f) {
-      // bf16: 1 - 2 / (e^2y + 1), which is 2^-23 off, next to a cap of 50 in the score 2^-17; `inner` has the factor 2 log2 e
-      auto bend = [&](float y) { return sizeof(T) == 4 ? tanhf(y) * a.outer : fmaf(-2.f * a.outer, reciprocal(ptx::ex2(y) + 1.f), a.outer); };
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+          for (int w = 0; w < IN; ++w) {
+            uint32_t f[4];
+            keys(m, k, w, f);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int y = 0; y < TERMS - w; ++y) {   // the product of the two smaller terms is left out: 2^-22 of the score's terms
+                float (&from)[4] = k + w + y > 0 ? s[m][n] : zero;
+                if constexpr (HD == 8) mma_k8(s[m][n], f[0], f[1], qf[n][y][k][0], from);
+                else mma(s[m][n], f, qf[n][y][k][0], qf[n][y][k][1], from);
+              }
+          }
+      // scores in base 2, pairs of columns; positions 16 m + 8 h + gr
+      float2 x[NT][2][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float2 f = __fmul2_rn(back[n], make_float2(ks, ks));
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) x[n][m][h] = make_float2(bend(x[n][m][h].x), bend(x[n][m][h].y));
-    }
-    if (!FULL || timed || !((every >> seg) & 1u)) {   // closed pairs -inf
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const bool m0 = (col_opens >> (8 * n + seg)) & 1u, m1 = (col_opens >> (8 * n + 4 + seg)) & 1u;
-        float2 time = make_float2(0.f, 0.f), limit = time, slope2 = time;
-        if (timed) {
-          const QueryRow &r0 = rows_of[8 * n + 2 * t], &r1 = rows_of[8 * n + 2 * t + 1];
-          time = make_float2(r0.time, r1.time);
-          limit = make_float2(r0.limit, r1.limit);
-          slope2 = make_float2(-r0.slope2, -r1.slope2);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float2& v = x[n][i / 2][i % 2];
-          const bool there = FULL || 8 * i + gr < rows;
-          bool o0 = m0 && there, o1 = m1 && there;
-          if (timed) {
-            const float2 d = __fadd2_rn(time, make_float2(-times[i], -times[i]));
-            v = __ffma2_rn(slope2, make_float2(fabsf(d.x), fabsf(d.y)), v);
-            o0 = o0 && times[i] <= limit.x;
-            o1 = o1 && times[i] <= limit.y;
-          }
-          v = make_float2(o0 ? v.x : -INFINITY, o1 ? v.y : -INFINITY);
-        }
+          for (int h = 0; h < 2; ++h) x[n][m][h] = __fmul2_rn(make_float2(s[m][n][2 * h], s[m][n][2 * h + 1]), f);
       }
-    }
-    bool raise = false;
+      if (a.softcap > 0.f) {
+        // bf16: 1 - 2 / (e^2y + 1), which is 2^-23 off, next to a cap of 50 in the score 2^-17; `inner` has the factor 2 log2 e
+        auto bend = [&](float y) { return sizeof(T) == 4 ? tanhf(y) * a.outer : fmaf(-2.f * a.outer, reciprocal(ptx::ex2(y) + 1.f), a.outer); };
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float2 over = __fadd2_rn(ref[n], make_float2(8.f, 8.f));
-      raise = raise || fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x) > over.x ||
-              fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y) > over.y;
-    }
-    if (__any_sync(0xffffffffu, raise)) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float2 top = make_float2(fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x),
-                                 fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y));
+          for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int l = 4; l < 32; l <<= 1) top = make_float2(fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, l)), fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, l)));
-        top = make_float2(fmaxf(top.x, ref[n].x), fmaxf(top.y, ref[n].y));
-        const float2 f = make_float2(top.x > ref[n].x ? ptx::ex2(ref[n].x - top.x) : 1.f, top.y > ref[n].y ? ptx::ex2(ref[n].y - top.y) : 1.f);
-        sum[n] = __fmul2_rn(sum[n], f);
-#pragma unroll
-        for (int m = 0; m < MD; ++m) {
-          o[m][n][0] = __fmul2_rn(o[m][n][0], f);
-          o[m][n][1] = __fmul2_rn(o[m][n][1], f);
-        }
-        ref[n] = top;
+            for (int h = 0; h < 2; ++h) x[n][m][h] = make_float2(bend(x[n][m][h].x), bend(x[n][m][h].y));
       }
-    }
-    const bool broken = !(fabsf(vs) < INFINITY);
-    uint32_t seen = 0;                   // where the block's values are broken: columns that any position is open to
-    if (broken)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          bool any = false;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) any = any || (e ? x[n][i / 2][i % 2].y : x[n][i / 2][i % 2].x) != -INFINITY;
-          const uint32_t who = __ballot_sync(0xffffffffu, any) & (0x11111111u << t);
-          seen |= (who != 0 ? 1u : 0u) << (2 * n + e);
-        }
-    // weights, turned round into B operands: keys 2 t, 2 t + 1 (and + 8) of row gr.  What biased values start from is a product with ones: the
-    // sum of the weights as they are rounded, in every lane
-    uint32_t pf[NT][TERMS][2][2];
-    float begin[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float2 r = make_float2(ref[n].x == -INFINITY ? 0.f : -ref[n].x, ref[n].y == -INFINITY ? 0.f : -ref[n].y);
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float2 v = __fadd2_rn(x[n][m][h], r), p = make_float2(ptx::ex2(v.x), ptx::ex2(v.y));
-          sum[n] = __fadd2_rn(sum[n], p);
-          const uint32_t w = f16x2(p.x, p.y);
-          pf[n][0][m][h] = turned_round(w);
-          if constexpr (TERMS == 2) pf[n][1][m][h] = turned_round(f16x2_rest(p.x, p.y, w));
-        }
-      if constexpr (FROM_BIAS) {
-        constexpr uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
-        float add[4];
-        mma(add, ones, pf[n][0][0][0], pf[n][0][0][1], zero);
-        mma(add, ones, pf[n][0][1][0], pf[n][0][1][1], add);
-        const float2 from = __fmul2_rn(make_float2(add[0], add[1]), make_float2(-BIAS, -BIAS));
-        begin[n][0] = begin[n][2] = from.x;
-        begin[n][1] = begin[n][3] = from.y;
-      }
-    }
-#pragma unroll
-    for (int m = 0; m < MD; ++m) {
-      float add[NT][4];
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int w = 0; w < IN; ++w) {
-          uint32_t f[4];
-          values(m, k, w, f);
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int y = 0; y < TERMS - w; ++y) mma(add[n], f, pf[n][y][k][0], pf[n][y][k][1], k + w + y > 0 ? add[n] : FROM_BIAS ? begin[n] : zero);
-        }
-      if (!broken) {
+      if (!FULL || timed || !((every >> seg) & 1u)) {   // closed pairs -inf
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          o[m][n][0] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][0], add[n][1]), o[m][n][0]);
-          if constexpr (HD > 8) o[m][n][1] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][2], add[n][3]), o[m][n][1]);
+          const bool m0 = (col_opens >> (8 * n + seg)) & 1u, m1 = (col_opens >> (8 * n + 4 + seg)) & 1u;
+          float2 time = make_float2(0.f, 0.f), limit = time, slope2 = time;
+          if (timed) {
+            const QueryRow &r0 = rows_of[8 * n + 2 * t], &r1 = rows_of[8 * n + 2 * t + 1];
+            time = make_float2(r0.time, r1.time);
+            limit = make_float2(r0.limit, r1.limit);
+            slope2 = make_float2(-r0.slope2, -r1.slope2);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float2& v = x[n][i / 2][i % 2];
+            const bool there = FULL || 8 * i + gr < rows;
+            bool o0 = m0 && there, o1 = m1 && there;
+            if (timed) {
+              const float2 d = __fadd2_rn(time, make_float2(-times[i], -times[i]));
+              v = __ffma2_rn(slope2, make_float2(fabsf(d.x), fabsf(d.y)), v);
+              o0 = o0 && times[i] <= limit.x;
+              o1 = o1 && times[i] <= limit.y;
+            }
+            v = make_float2(o0 ? v.x : -INFINITY, o1 ? v.y : -INFINITY);
+          }
         }
       }
-    }
-    if (broken)
+      bool raise = false;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
+        const float2 over = __fadd2_rn(ref[n], make_float2(8.f, 8.f));
+        raise = raise || fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x) > over.x ||
+                fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y) > over.y;
+      }
+      if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-        for (int m = 0; m < MD; ++m) {
-          if ((seen >> (2 * n)) & 1u) o[m][n][0].x = o[m][n][1].x = vs;
-          if ((seen >> (2 * n + 1)) & 1u) o[m][n][0].y = o[m][n][1].y = vs;
-        }
-  };
-
-  // The open blocks, each the next warp's in turn, while the first copies are under way: rows in memory, brought to f16 by a power of two for all of a block's.
-#pragma unroll 1
-  for (int r = 0, at = list.full; r < 3; ++r) {
-    const int n = r == 0 ? list.len[0] : r == 1 ? list.len[1] : list.len[2], rows = n % CACHE_BLOCK, j = n / CACHE_BLOCK;
-    if (rows == 0) continue;
-    const int i = at++;
-    if (i < lo || i >= hi || ((max(0, last - lo) + B - 1) / B + i - max(lo, list.full)) % WARPS != warp) continue;
-    const int64_t from = open_at(c, b, r, j, hk);
-    const T* const key = static_cast<const T*>(c.open_keys) + from;
-    const T* const value = static_cast<const T*>(c.open_values) + from;
-    float times[4] = {0.f, 0.f, 0.f, 0.f};
-    if (timed) {
-      const int page = c.times == nullptr ? 0 : real_page(c, c.tables[((int64_t)b * 3 + r) * c.blocks + j]);
+        for (int n = 0; n < NT; ++n) {
+          float2 top = make_float2(fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x),
+                                   fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y));
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        times[i] = c.times == nullptr ? (float)(j * CACHE_BLOCK + 8 * i + gr) : page >= 0 ? c.times[(int64_t)page * CACHE_BLOCK + 8 * i + gr] : 0.f;
-    }
-    // all of it at once into registers, as the fragments want it: pairs of features of positions 8 i + gr
-    uint32_t words[2][4][HD / 8][TERMS];
+          for (int l = 4; l < 32; l <<= 1) top = make_float2(fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, l)), fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, l)));
+          top = make_float2(fmaxf(top.x, ref[n].x), fmaxf(top.y, ref[n].y));
+          const float2 f = make_float2(top.x > ref[n].x ? ptx::ex2(ref[n].x - top.x) : 1.f, top.y > ref[n].y ? ptx::ex2(ref[n].y - top.y) : 1.f);
+          sum[n] = __fmul2_rn(sum[n], f);
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int k = 0; k < HD / 8; ++k) {
-          const T* p = (w ? value : key) + (8 * i + gr) * HD + 8 * k + 2 * t;
-          uint2 v = make_uint2(0u, 0u);
-          if (8 * i + gr < rows) {
-            if constexpr (sizeof(T) == 2) v.x = *reinterpret_cast<const uint32_t*>(p);
-            else v = *reinterpret_cast<const uint2*>(p);
+          for (int m = 0; m < MD; ++m) {
+            o[m][n][0] = __fmul2_rn(o[m][n][0], f);
+            o[m][n][1] = __fmul2_rn(o[m][n][1], f);
           }
-          words[w][i][k][0] = v.x;
-          if constexpr (TERMS == 2) words[w][i][k][1] = v.y;
+          ref[n] = top;
         }
-    auto pair = [&](int w, int i, int k) {
-      float2 v;
-      if constexpr (sizeof(T) == 2) unpack_bf16(words[w][i][k][0], v.x, v.y);
-      else v = make_float2(__uint_as_float(words[w][i][k][0]), __uint_as_float(words[w][i][k][TERMS - 1]));
-      return v;
-    };
-    Power up[2];
-    float by[2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int k = 0; k < HD / 8; ++k) {
-          const float2 v = pair(w, i, k);
-          top = max(top, max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu));
-        }
-      top = __reduce_max_sync(0xffffffffu, top);
-      const bool broken = top >= 0x7f800000u;
-      up[w] = top > 0 && !broken ? power_for(__uint_as_float(top), 14) : Power{1.f, 1.f};
-      by[w] = broken ? __int_as_float(0x7fffffff) : up[w].down;
+      }
+      const bool broken = !(fabsf(vs) < INFINITY);
+      uint32_t seen = 0;                   // where the block's values are broken: columns that any position is open to
       if (broken)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int k = 0; k < HD / 8; ++k)
+          for (int e = 0; e < 2; ++e) {
+            bool any = false;
 #pragma unroll
-            for (int e = 0; e < TERMS; ++e) words[w][i][k][e] = 0u;
-    }
-    auto term = [&](float2 v, float f, int w) {
-      v = __fmul2_rn(v, make_float2(f, f));
-      const uint32_t x = f16x2(v.x, v.y);
-      return w == 0 ? x : f16x2_rest(v.x, v.y, x);
-    };
-    attend(std::integral_constant<int, TERMS>{}, std::integral_constant<int, 0>{}, r, rows, by[0], by[1], times,
-           [&](int m, int k, int w, uint32_t (&f)[4]) {
+            for (int i = 0; i < 4; ++i) any = any || (e ? x[n][i / 2][i % 2].y : x[n][i / 2][i % 2].x) != -INFINITY;
+            const uint32_t who = __ballot_sync(0xffffffffu, any) & (0x11111111u << t);
+            seen |= (who != 0 ? 1u : 0u) << (2 * n + e);
+          }
+      // weights, turned round into B operands: keys 2 t, 2 t + 1 (and + 8) of row gr.  What biased values start from is a product with ones: the
+      // sum of the weights as they are rounded, in every lane
+      uint32_t pf[NT][TERMS][2][2];
+      float begin[NT][4];
 #pragma unroll
-             for (int i = 0; i < 4; ++i)   // position halves i % 2, feature halves i / 2
-               f[i] = HD > 8 || i < 2 ? term(pair(0, 2 * m + i % 2, HD > 8 ? 2 * k + i / 2 : 0), up[0].up, w) : 0u;
-           },
-           [&](int m, int k, int w, uint32_t (&f)[4]) {
+      for (int n = 0; n < NT; ++n) {
+        const float2 r = make_float2(ref[n].x == -INFINITY ? 0.f : -ref[n].x, ref[n].y == -INFINITY ? 0.f : -ref[n].y);
 #pragma unroll
-             for (int i = 0; i < 4; ++i)   // feature halves i % 2, position halves i / 2; rows of features come in, turned round
-               f[i] = HD > 8 || i % 2 == 0 ? turned_round(term(pair(1, 2 * k + i / 2, HD > 8 ? 2 * m + i % 2 : 0), up[1].up, w)) : 0u;
-           });
-  }
-
-#pragma unroll 1
-  for (int now = first; now < last; now += turn) {
-    if (ahead < last) {   // into the stage that was read before this one
-      const uint32_t into = to;
-      copy();
-      tell(into, (32 / B - known - 1) * B);
-    }
-    ptx::mbar_wait_warp(wait, bars + 8 * stage, phase);
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const BlockInfo x = s_info[warp][stage][u];
-      if (x.seg == 3) continue;
-      const uint32_t at = ring + (stage * B + u) * RingOf::BLOCK, key = at + (HD == 8 ? 8 : 16) * lane, value = key + RingOf::MATRIX;
-      float times[4] = {0.f, 0.f, 0.f, 0.f};
-      if (timed)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          times[i] = c.times != nullptr ? *reinterpret_cast<const float*>(smem + (at - smem_u32(smem)) + 2 * RingOf::MATRIX + 4 * (8 * i + gr)) : (float)(x.first + 8 * i + gr);
-      // fragments of keys come by (feature group, position half), of values by (feature group, position half), both halves in 16 bytes
-      uint4 kw[KS], vw[MD];
-      auto take = [&](uint4 (&w)[KS], uint32_t from) {
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          if constexpr (HD == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[i].x), "=r"(w[i].y) : "r"(from) : "memory");
-          else w[i] = lds16(from + 512 * i);
+          for (int h = 0; h < 2; ++h) {
+            const float2 v = __fadd2_rn(x[n][m][h], r), p = make_float2(ptx::ex2(v.x), ptx::ex2(v.y));
+            sum[n] = __fadd2_rn(sum[n], p);
+            const uint32_t w = f16x2(p.x, p.y);
+            pf[n][0][m][h] = turned_round(w);
+            if constexpr (TERMS == 2) pf[n][1][m][h] = turned_round(f16x2_rest(p.x, p.y, w));
+          }
+        if constexpr (FROM_BIAS) {
+          constexpr uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+          float add[4];
+          mma(add, ones, pf[n][0][0][0], pf[n][0][0][1], zero);
+          mma(add, ones, pf[n][0][1][0], pf[n][0][1][1], add);
+          const float2 from = __fmul2_rn(make_float2(add[0], add[1]), make_float2(-BIAS, -BIAS));
+          begin[n][0] = begin[n][2] = from.x;
+          begin[n][1] = begin[n][3] = from.y;
         }
+      }
+#pragma unroll
+      for (int m = 0; m < MD; ++m) {
+        float add[NT][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int w = 0; w < IN; ++w) {
+            uint32_t f[4];
+            values(m, k, w, f);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int y = 0; y < TERMS - w; ++y) mma(add[n], f, pf[n][y][k][0], pf[n][y][k][1], k + w + y > 0 ? add[n] : FROM_BIAS ? begin[n] : zero);
+          }
+        if (!broken) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            o[m][n][0] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][0], add[n][1]), o[m][n][0]);
+            if constexpr (HD > 8) o[m][n][1] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][2], add[n][3]), o[m][n][1]);
+          }
+        }
+      }
+      if (broken)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int m = 0; m < MD; ++m) {
+            if ((seen >> (2 * n)) & 1u) o[m][n][0].x = o[m][n][1].x = vs;
+            if ((seen >> (2 * n + 1)) & 1u) o[m][n][0].y = o[m][n][1].y = vs;
+          }
+    };
+
+    // The open blocks, each the next warp's in turn, while the first copies are under way: rows in memory, brought to f16 by a power of two for all of a block's.
+#pragma unroll 1
+    for (int r = 0, at = list.full; r < 3; ++r) {
+      const int n = r == 0 ? list.len[0] : r == 1 ? list.len[1] : list.len[2], rows = n % CACHE_BLOCK, j = n / CACHE_BLOCK;
+      if (rows == 0) continue;
+      const int i = at++;
+      if (i < lo || i >= hi || ((max(0, last - lo) + B - 1) / B + i - max(lo, list.full)) % WARPS != warp) continue;
+      const int64_t from = open_at(c, b, r, j, hk);
+      const T* const key = static_cast<const T*>(c.open_keys) + from;
+      const T* const value = static_cast<const T*>(c.open_values) + from;
+      float times[4] = {0.f, 0.f, 0.f, 0.f};
+      if (timed) {
+        const int page = c.times == nullptr ? 0 : real_page(c, c.tables[((int64_t)b * 3 + r) * c.blocks + j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          times[i] = c.times == nullptr ? (float)(j * CACHE_BLOCK + 8 * i + gr) : page >= 0 ? c.times[(int64_t)page * CACHE_BLOCK + 8 * i + gr] : 0.f;
+      }
+      // all of it at once into registers, as the fragments want it: pairs of features of positions 8 i + gr
+      uint32_t words[2][4][HD / 8][TERMS];
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int k = 0; k < HD / 8; ++k) {
+            const T* p = (w ? value : key) + (8 * i + gr) * HD + 8 * k + 2 * t;
+            uint2 v = make_uint2(0u, 0u);
+            if (8 * i + gr < rows) {
+              if constexpr (sizeof(T) == 2) v.x = *reinterpret_cast<const uint32_t*>(p);
+              else v = *reinterpret_cast<const uint2*>(p);
+            }
+            words[w][i][k][0] = v.x;
+            if constexpr (TERMS == 2) words[w][i][k][1] = v.y;
+          }
+      auto pair = [&](int w, int i, int k) {
+        float2 v;
+        if constexpr (sizeof(T) == 2) unpack_bf16(words[w][i][k][0], v.x, v.y);
+        else v = make_float2(__uint_as_float(words[w][i][k][0]), __uint_as_float(words[w][i][k][TERMS - 1]));
+        return v;
       };
-      take(kw, key);
-      attend(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, x.seg, CACHE_BLOCK, x.ks, x.vs, times,
-             [&](int m, int k, int, uint32_t (&f)[4]) {
-               if constexpr (HD == 8) unpack8<KIND, false>(m ? kw[0].y : kw[0].x, f[0], f[1]);
-               else {
-                 unpack8<KIND, false>(m ? kw[k].z : kw[k].x, f[0], f[1]);
-                 unpack8<KIND, false>(m ? kw[k].w : kw[k].y, f[2], f[3]);
-               }
+      Power up[2];
+      float by[2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int k = 0; k < HD / 8; ++k) {
+            const float2 v = pair(w, i, k);
+            top = max(top, max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu));
+          }
+        top = __reduce_max_sync(0xffffffffu, top);
+        const bool broken = top >= 0x7f800000u;
+        up[w] = top > 0 && !broken ? power_for(__uint_as_float(top), 14) : Power{1.f, 1.f};
+        by[w] = broken ? __int_as_float(0x7fffffff) : up[w].down;
+        if (broken)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < HD / 8; ++k)
+#pragma unroll
+              for (int e = 0; e < TERMS; ++e) words[w][i][k][e] = 0u;
+      }
+      auto term = [&](float2 v, float f, int w) {
+        v = __fmul2_rn(v, make_float2(f, f));
+        const uint32_t x = f16x2(v.x, v.y);
+        return w == 0 ? x : f16x2_rest(v.x, v.y, x);
+      };
+      attend(std::integral_constant<int, TERMS>{}, std::integral_constant<int, 0>{}, r, rows, by[0], by[1], times,
+             [&](int m, int k, int w, uint32_t (&f)[4]) {
+#pragma unroll
+               for (int i = 0; i < 4; ++i)   // position halves i % 2, feature halves i / 2
+                 f[i] = HD > 8 || i < 2 ? term(pair(0, 2 * m + i % 2, HD > 8 ? 2 * k + i / 2 : 0), up[0].up, w) : 0u;
              },
-             [&](int m, int k, int, uint32_t (&f)[4]) {
-               if (m + k == 0) take(vw, value);
-               if constexpr (HD == 8) {
-                 unpack8<KIND, BIASED>(k ? vw[0].y : vw[0].x, f[0], f[2]);
-                 f[1] = f[3] = 0u;
-               } else {
-                 unpack8<KIND, BIASED>(k ? vw[m].z : vw[m].x, f[0], f[1]);
-                 unpack8<KIND, BIASED>(k ? vw[m].w : vw[m].y, f[2], f[3]);
-               }
+             [&](int m, int k, int w, uint32_t (&f)[4]) {
+#pragma unroll
+               for (int i = 0; i < 4; ++i)   // feature halves i % 2, position halves i / 2; rows of features come in, turned round
+                 f[i] = HD > 8 || i % 2 == 0 ? turned_round(term(pair(1, 2 * k + i / 2, HD > 8 ? 2 * m + i % 2 : 0), up[1].up, w)) : 0u;
              });
     }
-    __syncwarp();   // every lane has used what it read of the stage
-    stage = stage + 1 == STAGES ? 0 : stage + 1;
-    phase ^= stage == 0;
-  }
-  // ---- the warps' parts ----
-  __syncthreads();   // nobody's ring is in use any more
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int row = 8 * n + 2 * t;
-#pragma unroll
-    for (int l = 4; l < 32; l <<= 1) sum[n] = make_float2(sum[n].x + __shfl_xor_sync(0xffffffffu, sum[n].x, l), sum[n].y + __shfl_xor_sync(0xffffffffu, sum[n].y, l));
-    if (gr == 0) {
-      room.ml[warp][row] = make_float2(ref[n].x, sum[n].x);
-      room.ml[warp][row + 1] = make_float2(ref[n].y, sum[n].y);
-    }
-#pragma unroll
-    for (int m = 0; m < MD; ++m)
-#pragma unroll
-      for (int h = 0; h < (HD > 8 ? 2 : 1); ++h) {
-        room.acc[warp][row][16 * m + 8 * h + gr] = o[m][n][h].x;
-        room.acc[warp][row + 1][16 * m + 8 * h + gr] = o[m][n][h].y;
+
+#pragma unroll 1
+    for (int now = first; now < last; now += turn) {
+      if (ahead < last) {   // into the stage that was read before this one
+        const uint32_t into = to;
+        copy();
+        tell(into, (32 / B - known - 1) * B);
       }
-  }
-  __syncthreads();
+      ptx::mbar_wait_warp(wait, bars + 8 * stage, phase);
+#pragma unroll
+      for (int u = 0; u < B; ++u) {
+        const BlockInfo x = s_info[warp][stage][u];
+        if (x.seg == 3) continue;
+        const uint32_t at = ring + (stage * B + u) * RingOf::BLOCK, key = at + (HD == 8 ? 8 : 16) * lane, value = key + RingOf::MATRIX;
+        float times[4] = {0.f, 0.f, 0.f, 0.f};
+        if (timed)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            times[i] = c.times != nullptr ? *reinterpret_cast<const float*>(smem + (at - smem_u32(smem)) + 2 * RingOf::MATRIX + 4 * (8 * i + gr)) : (float)(x.first + 8 * i + gr);
+        // fragments of keys come by (feature group, position half), of values by (feature group, position half), both halves in 16 bytes
+        uint4 kw[KS], vw[MD];
+        auto take = [&](uint4 (&w)[KS], uint32_t from) {
+#pragma unroll
+          for (int i = 0; i < KS; ++i) {
+            if constexpr (HD == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[i].x), "=r"(w[i].y) : "r"(from) : "memory");
+            else w[i] = lds16(from + 512 * i);
+          }
+        };
+        take(kw, key);
+        attend(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, x.seg, CACHE_BLOCK, x.ks, x.vs, times,
+               [&](int m, int k, int, uint32_t (&f)[4]) {
+                 if constexpr (HD == 8) unpack8<KIND, false>(m ? kw[0].y : kw[0].x, f[0], f[1]);
+                 else {
+                   unpack8<KIND, false>(m ? kw[k].z : kw[k].x, f[0], f[1]);
+                   unpack8<KIND, false>(m ? kw[k].w : kw[k].y, f[2], f[3]);
+                 }
+               },
+               [&](int m, int k, int, uint32_t (&f)[4]) {
+                 if (m + k == 0) take(vw, value);
+                 if constexpr (HD == 8) {
+                   unpack8<KIND, BIASED>(k ? vw[0].y : vw[0].x, f[0], f[2]);
+                   f[1] = f[3] = 0u;
+                 } else {
+                   unpack8<KIND, BIASED>(k ? vw[m].z : vw[m].x, f[0], f[1]);
+                   unpack8<KIND, BIASED>(k ? vw[m].w : vw[m].y, f[2], f[3]);
+                 }
+               });
+      }
+      __syncwarp();   // every lane has used what it read of the stage
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      phase ^= stage == 0;
+    }
+    // ---- the warps' parts ----
+    __syncthreads();   // nobody's ring is in use any more
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int row = 8 * n + 2 * t;
+#pragma unroll
+      for (int l = 4; l < 32; l <<= 1) sum[n] = make_float2(sum[n].x + __shfl_xor_sync(0xffffffffu, sum[n].x, l), sum[n].y + __shfl_xor_sync(0xffffffffu, sum[n].y, l));
+      if (gr == 0) {
+        room.ml[warp][row] = make_float2(ref[n].x, sum[n].x);
+        room.ml[warp][row + 1] = make_float2(ref[n].y, sum[n].y);
+      }
+#pragma unroll
+      for (int m = 0; m < MD; ++m)
+#pragma unroll
+        for (int h = 0; h < (HD > 8 ? 2 : 1); ++h) {
+          room.acc[warp][row][16 * m + 8 * h + gr] = o[m][n][h].x;
+          room.acc[warp][row + 1][16 * m + 8 * h + gr] = o[m][n][h].y;
+        }
+    }
+    __syncthreads();
   };
 
   // a warp takes every eighth row of a piece, its lanes the features

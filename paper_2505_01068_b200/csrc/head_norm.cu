@@ -4,10 +4,11 @@
 // x is read again instead of saving anything; r costs one more sum over a head that is in registers anyway.
 //
 // Bound by the rows read and written, so everything is arranged around loads in flight and few instructions: a warp works for itself, without barriers.
-// It takes blocks of a few rows, forward of q and k, backward of one of them (sums for two weights do not fit the registers beside the loads); a lane holds two 16-byte pieces of a head (the halves that rotate against each other, or neighbours where
-// pairs are interleaved), so that sums over a head are log2(lanes of a head) shuffles and a pair never leaves its lane.  Which pieces of a block
-// are a lane's never changes, so the sums for dgamma stay in registers.  The angles of a block are computed into a table of the warp's own while
-// the block's loads are under way, one (row, pair) a lane, and serve all heads.
+// It takes blocks of a few rows, forward of q and k, backward of one of them (sums for two weights do not fit the registers beside the rest); a lane holds two
+// 16-byte pieces of a head (the halves that rotate against each other, or neighbours where pairs are interleaved), so that sums over a head are
+// log2(lanes of a head) shuffles and a pair never leaves its lane.  Which pieces of a block are a lane's never changes, so the sums for dgamma stay in
+// registers.  The angles of a block are computed into a table of the warp's own, one (row, pair) a lane, and serve all heads; the rows of the block
+// after it are on their way into shared memory meanwhile.
 // Angles in turns are products of integers that lose their whole turns by themselves: position * (frequency * 2^64) mod 2^64, of which the upper 32 bits are
 // the phase, right for every position an int32 holds; then sincospi for float, and the special functions' sine and cosine for bf16 (2^-21 off, where a
 // result keeps 2^-9).
@@ -450,52 +451,52 @@ head_norm_any_kernel(const __grid_constant__ Geometry g, const __grid_constant__
     __syncwarp();
 #pragma unroll
     for (int which = 0; which < 2; ++which)
-    for (int head = 0; head < a.t[which].heads; ++head) {
-      const NormTensor& t = a.t[which];
-      const T* x = static_cast<const T*>(t.x) + (int64_t)row * t.ldx + (int64_t)head * hd;
-      T* out = static_cast<T*>(t.out) + (int64_t)row * t.ldo + (int64_t)head * hd;
-      if (!real) {
-        for (int f = lane; f < hd; f += 32) store_as(out + f, 0.f);
-        continue;
-      }
-      float v[OWN], ga[OWN], u[OWN], sum = 0.f, gx = 0.f;
+      for (int head = 0; head < a.t[which].heads; ++head) {
+        const NormTensor& t = a.t[which];
+        const T* x = static_cast<const T*>(t.x) + (int64_t)row * t.ldx + (int64_t)head * hd;
+        T* out = static_cast<T*>(t.out) + (int64_t)row * t.ldo + (int64_t)head * hd;
+        if (!real) {
+          for (int f = lane; f < hd; f += 32) store_as(out + f, 0.f);
+          continue;
+        }
+        float v[OWN], ga[OWN], u[OWN], sum = 0.f, gx = 0.f;
 #pragma unroll
-      for (int i = 0; i < OWN; ++i) {
-        const int f = lane + 32 * i;
-        v[i] = f < hd ? to_float(x[f]) : 0.f;
-        ga[i] = f < hd && t.gamma != nullptr ? t.gamma[f] : 1.f;
-        sum += v[i] * v[i];
-        u[i] = 0.f;
-        if (BWD && f < hd) s_row[warp][f] = to_float(static_cast<const T*>(t.dy)[(int64_t)row * t.lddy + (int64_t)head * hd + f]);
-      }
-      if (BWD) {
-        __syncwarp();
+        for (int i = 0; i < OWN; ++i) {
+          const int f = lane + 32 * i;
+          v[i] = f < hd ? to_float(x[f]) : 0.f;
+          ga[i] = f < hd && t.gamma != nullptr ? t.gamma[f] : 1.f;
+          sum += v[i] * v[i];
+          u[i] = 0.f;
+          if (BWD && f < hd) s_row[warp][f] = to_float(static_cast<const T*>(t.dy)[(int64_t)row * t.lddy + (int64_t)head * hd + f]);
+        }
+        if (BWD) {
+          __syncwarp();
 #pragma unroll
-        for (int i = 0; i < OWN; ++i)
-          if (const int f = lane + 32 * i; f < hd) {
-            u[i] = turned(f, -1.f);
-            gx += u[i] * ga[i] * v[i];
-          }
-      }
-      const float2 s = head_sum<32>(make_float2(sum, gx));
-      const float r = rsqrtf(s.x * a.inv_hd + a.eps), back = -r * r * (s.y * a.inv_hd);
-      if (BWD) {
+          for (int i = 0; i < OWN; ++i)
+            if (const int f = lane + 32 * i; f < hd) {
+              u[i] = turned(f, -1.f);
+              gx += u[i] * ga[i] * v[i];
+            }
+        }
+        const float2 s = head_sum<32>(make_float2(sum, gx));
+        const float r = rsqrtf(s.x * a.inv_hd + a.eps), back = -r * r * (s.y * a.inv_hd);
+        if (BWD) {
 #pragma unroll
-        for (int i = 0; i < OWN; ++i)
-          if (const int f = lane + 32 * i; f < hd) {
-            const float h = v[i] * r;
-            dg[which][i] += u[i] * h;
-            store_as(out + f, u[i] * ga[i] * r + h * back);
-          }
-      } else {
+          for (int i = 0; i < OWN; ++i)
+            if (const int f = lane + 32 * i; f < hd) {
+              const float h = v[i] * r;
+              dg[which][i] += u[i] * h;
+              store_as(out + f, u[i] * ga[i] * r + h * back);
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < OWN; ++i)
-          if (const int f = lane + 32 * i; f < hd) s_row[warp][f] = v[i] * r * ga[i];
-        __syncwarp();
-        for (int f = lane; f < hd; f += 32) store_as(out + f, turned(f, 1.f));
+          for (int i = 0; i < OWN; ++i)
+            if (const int f = lane + 32 * i; f < hd) s_row[warp][f] = v[i] * r * ga[i];
+          __syncwarp();
+          for (int f = lane; f < hd; f += 32) store_as(out + f, turned(f, 1.f));
+        }
+        __syncwarp();   // s_row is written by the next head
       }
-      __syncwarp();   // s_row is written by the next head
-    }
   }
   if (!BWD || a.partial == nullptr) return;
   // warps in order, through the rows they no longer need

@@ -226,6 +226,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 6 : 3) cache_append_
   const int slot0 = slots[0], held = held_rows(c, g.status, p.b, p.s);   // asked for together
   const int n = leading_rows(slots, g.len(p.s), lane);
   if (n == 0) return;
+  if (slot0 < 0) {   // rows that have a slot come first: behind one that has none, no place can be told from the first one's
+    raise_flag(g, GSIT_DEVFLAG_CLAMPED);
+    return;
+  }
   // the rows [i0, i1) of the segment lie in this block, from place `o` on
   const int place0 = slot0 % CACHE_BLOCK, i0 = max(0, p.chunk * CACHE_BLOCK - place0), i1 = min(n, (p.chunk + 1) * CACHE_BLOCK - place0);
   if (i0 >= i1) return;

@@ -5,10 +5,13 @@
 // bank conflicts.  8 query rows of the key head (its query heads, in every segment) are the narrow side of m16n8k16 products:
 //   S^T = K Q^T      keys x rows: 8-bit integers (or e4m3) are exact in f16; q is brought to f16 by a power of two for each row, which loses nothing
 //                    of bf16 worth having (what is 2^-28 of a row's largest feature); float q as two f16 terms, 22 bits
-//   O^T += vs V^T P  features x rows: P turned round by movmatrix, in f16 (2^-11 of each weight, relative), as two terms for float; the block's scale
-//                    is applied to the product in float, so it never meets the range of f16
+//   O^T += vs V^T P  features x rows: P turned round by movmatrix, in f16, as two terms for float; the block's scale is applied to the product in float,
+//                    so it never meets the range of f16
 // The open block's rows are brought to f16 by a power of two for the block (float: two terms) and go the same way, in the warp whose turn it is.
-// The softmax runs over a reference that is raised only where a score passes it by 2^8, so that most blocks need no exchange between lanes.
+// The softmax runs over a reference that is raised only where a weight would pass 2^15, the last power of two in f16, so that most blocks need no exchange
+// between lanes.  It is set so that the largest weight is 2^14 for float, 2^7 for bf16 then: f16 ends at 2^-24, and what stands out (a first position, silence) must not
+// take the bits of a long even tail behind it, whose sum is not rounded.  A weight is off by 2^-11 of itself, or 2^-32 of the largest where that is more; by 2^-22, or
+// 2^-39 of the largest, where it has two terms.  (With the largest at 1, 512 positions 17.4 nats below it in a warp lost all of their 1.4e-5.)
 // Who takes what: where the step is small, the CTAs of a cluster share a (stream, key head, tile of rows) and join their parts through distributed shared
 // memory; where there is much to read, two CTAs an SM share out all blocks of all streams and key heads evenly, whatever their lengths are, and
 // a second small kernel joins the parts of those that more than one of them had.  Always in order.
@@ -185,10 +188,16 @@ template <int HD, int R> struct Part {
 // CTAs of an SM: two where their registers allow it.  (Tiles of 32 rows, one CTA an SM, took 44 us where those of 16 take 34.)
 template <typename T, int NT> constexpr int RESIDENT = NT == 1 || sizeof(T) == 2 ? 2 : 1;
 
+// Weights, in base 2: the largest that f16 takes, and where the reference puts a new largest one.  Sums of rows take them in this unit, so that they stay in
+// the range of what they add up.
+constexpr float MOST_WEIGHT = 15.f, WEIGHT_UNIT = 32768.f;
+template <typename T> constexpr float FIRST_WEIGHT = sizeof(T) == 4 ? 14.f : 7.f;
+
 template <typename T, int HD, int KIND, int NT>
 __global__ void __launch_bounds__(THREADS, RESIDENT<T, NT>)
 cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CachedArgs a) {
   constexpr int R = 8 * NT, TERMS = sizeof(T) == 4 ? 2 : 1, KS = HD == 8 ? 1 : HD / 16, MD = KS;
+  constexpr float LIFT = FIRST_WEIGHT<T>;
   // bf16 rows leave the 1152 of the integers' f16 form in the products of values and take it out of what they start from: it costs 2^-20 of the block's
   // largest value or so (in scores it would be seen: 1152 times the sum of a query's features, at 2^-24)
   constexpr bool BIASED = KIND == GSIT_CACHE_INT8 && TERMS == 1;
@@ -428,10 +437,11 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
       }
       bool raise = false;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const float2 over = __fadd2_rn(ref[n], make_float2(8.f, 8.f));
-        raise = raise || fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x) > over.x ||
-                fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y) > over.y;
+      for (int n = 0; n < NT; ++n) {   // (differences, which are exact where it matters: nothing passes 2^15 by a rounding)
+        const float2 top = make_float2(fmaxf(ptx::fmax3(x[n][0][0].x, x[n][0][1].x, x[n][1][0].x), x[n][1][1].x),
+                                       fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y));
+        const float2 over = __fadd2_rn(top, make_float2(-ref[n].x, -ref[n].y));
+        raise = raise || over.x > MOST_WEIGHT || over.y > MOST_WEIGHT;
       }
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
@@ -440,7 +450,11 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
                                    fmaxf(ptx::fmax3(x[n][0][0].y, x[n][0][1].y, x[n][1][0].y), x[n][1][1].y));
 #pragma unroll
           for (int l = 4; l < 32; l <<= 1) top = make_float2(fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, l)), fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, l)));
-          top = make_float2(fmaxf(top.x, ref[n].x), fmaxf(top.y, ref[n].y));
+          auto below = [](float x) {   // (scores of 2^24 and more have no place for the distance)
+            const float r = x - LIFT;
+            return x - r > MOST_WEIGHT ? x : r;
+          };
+          top = make_float2(fmaxf(below(top.x), ref[n].x), fmaxf(below(top.y), ref[n].y));
           const float2 f = make_float2(top.x > ref[n].x ? ptx::ex2(ref[n].x - top.x) : 1.f, top.y > ref[n].y ? ptx::ex2(ref[n].y - top.y) : 1.f);
           sum[n] = __fmul2_rn(sum[n], f);
 #pragma unroll
@@ -506,10 +520,11 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
               for (int y = 0; y < TERMS - w; ++y) mma(add[n], f, pf[n][y][k][0], pf[n][y][k][1], k + w + y > 0 ? add[n] : FROM_BIAS ? begin[n] : zero);
           }
         if (!broken) {
+          const float by = vs * (1.f / WEIGHT_UNIT);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            o[m][n][0] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][0], add[n][1]), o[m][n][0]);
-            if constexpr (HD > 8) o[m][n][1] = __ffma2_rn(make_float2(vs, vs), make_float2(add[n][2], add[n][3]), o[m][n][1]);
+            o[m][n][0] = __ffma2_rn(make_float2(by, by), make_float2(add[n][0], add[n][1]), o[m][n][0]);
+            if constexpr (HD > 8) o[m][n][1] = __ffma2_rn(make_float2(by, by), make_float2(add[n][2], add[n][3]), o[m][n][1]);
           }
         }
       }
@@ -684,7 +699,7 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
   auto finish = [&](int b, int hk, int row, const float (&v)[F], float2 ml) {
     const int l = row / a.group, head = hk * a.group + row % a.group;
     T* const out = static_cast<T*>(a.out) + ((int64_t)b * g.L + l) * g.d + (int64_t)head * HD + lane * F;
-    const float inv = ml.y != 0.f ? 1.f / ml.y : 0.f;
+    const float inv = ml.y != 0.f ? WEIGHT_UNIT / ml.y : 0.f;
     if (mine) store_features<F>(out, v, inv);
     if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * g.heads + head) * g.L + l] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * LN2 : -INFINITY;
   };
@@ -880,7 +895,7 @@ __global__ void __launch_bounds__(THREADS) cached_join_kernel(const __grid_const
     ml = make_float2(top, sum);
   }
   const int l = r / a.group, head = hk * a.group + r % a.group;
-  if (mine) store_features<F>(static_cast<T*>(a.out) + ((int64_t)b * g.L + l) * g.d + (int64_t)head * HD + lane * F, v, ml.y != 0.f ? 1.f / ml.y : 0.f);
+  if (mine) store_features<F>(static_cast<T*>(a.out) + ((int64_t)b * g.L + l) * g.d + (int64_t)head * HD + lane * F, v, ml.y != 0.f ? WEIGHT_UNIT / ml.y : 0.f);
   if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * g.heads + head) * g.L + l] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * LN2 : -INFINITY;
 }
 

@@ -1,7 +1,8 @@
-"""Calls on a stream's cache that its own steps do not make: slots that no plan writes."""
+"""Calls on a stream's cache that its own steps do not make: slots that no plan writes; and pasts in which few positions stand out."""
 import pytest
 import torch
 
+from stream_reference import bytes_of
 from test_gpu_stream import g, nothing_is_flagged   # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -29,3 +30,38 @@ def test_a_first_row_without_a_slot(g, t):
         assert flag == (g.DEVFLAG_CLAMPED if at is slots[0] else 0)
     for a, b in zip(*caches):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def _even_tail(g, t, held_as, below):
+    """Positions that stand out by `below` nats, one in each warp's walk, with values of 0, and 4 100 others with values of 1: what comes out is the tail's weight.
+    Streams that a CTA walks alone, and one that is split over many."""
+    hd, n = 16, 4100
+    for B, HK in ((75, 2), (1, 1)):
+        cache = g.stream_cache(B, (0, n, 1), HK, hd, t, held_as)
+        k, v = torch.zeros((B, n, HK, hd), device="cuda"), torch.ones((B, n, HK, hd), device="cuda")
+        for block in range(0, 128, 4):          # stages of a warp hold four blocks
+            if block < 32 or B == 1:
+                k[:, 32 * block + 5], v[:, 32 * block + 5] = 1.0, 0.0
+        k, v = k.to(t), v.to(t)
+        g.cache_append(cache, k, v, g.cache_plan(cache, (0, n, 0)), (0, n, 0))
+        q = torch.full((B, 1, HK, hd), 4 * below / hd, device="cuda").to(t)
+        out, lse = g.im_cached_attention_fwd(q, cache, (0, 1, 0), phase=g.PHASE_INTRA, want_lse=True)
+        K, V = bytes_of(cache, 0, 1, "k"), bytes_of(cache, 0, 1, "v")
+        assert K.shape[0] == n
+        x = torch.einsum("hc,jhc->hj", q[0, 0].double(), K) * hd ** -0.5
+        p = torch.softmax(x, dim=1)
+        want, total = torch.einsum("hj,jhc->hc", p, V), torch.logsumexp(x, dim=1)
+        # A weight is rounded to 2^-11 of itself or 2^-32 of the largest (float: 2^-22 and 2^-39); a score to 2^-21 of itself and of 8, twice; the result once.
+        score = 2.0 ** -21 * (below + 8)
+        weight, least = (2.0 ** -11, 2.0 ** -32) if t is torch.bfloat16 else (2.0 ** -22, 2.0 ** -39)
+        room = (torch.finfo(t).eps / 2 * 1.01 + weight + 2 * score) * want + n * least
+        off = (out[0].double().reshape(HK, hd) - want).abs()
+        assert bool((off <= room).all()), (B, float(off.max()), float(room.min()), float(want.max()))
+        assert torch.equal(out, out[:1].expand_as(out))
+        assert float((lse[0, :, 0].double() - total).abs().max()) <= 2.0 ** -20 * (below + 8)
+
+
+@pytest.mark.parametrize("below", [10.0, 14.0, 17.4, 21.0])
+@pytest.mark.parametrize("held_as, t", [("e4m3", torch.bfloat16), ("int8", torch.float32), ("e4m3", torch.float32)])
+def test_a_long_even_tail(g, held_as, t, below):
+    _even_tail(g, t, held_as, below)

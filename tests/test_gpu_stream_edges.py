@@ -65,3 +65,9 @@ def _even_tail(g, t, held_as, below):
 @pytest.mark.parametrize("held_as, t", [("e4m3", torch.bfloat16), ("int8", torch.float32), ("e4m3", torch.float32)])
 def test_a_long_even_tail(g, held_as, t, below):
     _even_tail(g, t, held_as, below)
+
+
+@pytest.mark.parametrize("below", [10.0, 14.0, 17.4, 21.0])
+def test_a_long_even_tail_of_integers(g, below):
+    """What stands out has values of 0, so nothing of its weight may be left in the sums."""
+    _even_tail(g, torch.bfloat16, "int8", below)

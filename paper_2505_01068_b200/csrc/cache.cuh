@@ -55,6 +55,7 @@ struct CachedArgs {
   int group, rows, causal;             // rows: query rows of a key head, L * group
   bool mixed;                          // tiles of rows run across segments
   float softcap, inner, outer;         // score = outer * tanh(inner * dot) or inner * dot, base 2
+  bool fast_cap;                       // inner holds 2 log2 e, too: tanh(y) = 1 - 2 / (e^2y + 1) by an exponential in base 2
   int split;                           // CTAs of the cluster that shares a (stream, key head, tile of rows)
   float* parts;                        // workspace; null: the CTAs of a cluster share the work and need none
 };

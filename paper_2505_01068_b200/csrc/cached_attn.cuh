@@ -392,14 +392,19 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
           for (int h = 0; h < 2; ++h) x[n][m][h] = __fmul2_rn(make_float2(s[m][n][2 * h], s[m][n][2 * h + 1]), f);
       }
       if (a.softcap > 0.f) {
-        // bf16: 1 - 2 / (e^2y + 1), which is 2^-23 off, next to a cap of 50 in the score 2^-17; `inner` has the factor 2 log2 e
-        auto bend = [&](float y) { return sizeof(T) == 4 ? tanhf(y) * a.outer : fmaf(-2.f * a.outer, reciprocal(ptx::ex2(y) + 1.f), a.outer); };
+        // bf16: under caps of 64 by an exponential and a reciprocal (see fast_cap), under wider ones to 2^-20 of the score itself
+        auto bend = [&](float2 y) {
+          if (sizeof(T) == 4) return make_float2(tanhf(y.x) * a.outer, tanhf(y.y) * a.outer);
+          if (!a.fast_cap) return __fmul2_rn(tanh_any2(y), make_float2(a.outer, a.outer));
+          auto fast = [&](float v) { return fmaf(-2.f * a.outer, reciprocal(ptx::ex2(v) + 1.f), a.outer); };
+          return make_float2(fast(y.x), fast(y.y));
+        };
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) x[n][m][h] = make_float2(bend(x[n][m][h].x), bend(x[n][m][h].y));
+            for (int h = 0; h < 2; ++h) x[n][m][h] = bend(x[n][m][h]);
       }
       if (!FULL || timed || !((every >> seg) & 1u)) {   // closed pairs -inf
 #pragma unroll

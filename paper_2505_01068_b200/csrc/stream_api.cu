@@ -70,8 +70,10 @@ gsit_status attention_args(const gsit_shape* shape, const gsit_score_rule* r, co
   const float scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)g->hd);
   constexpr float LOG2E = 1.4426950408889634f;
   a->softcap = r->softcap > 0.f ? r->softcap : 0.f;
-  // tanh(y) is taken as it is for float and by e^2y in base 2 for bf16
-  a->inner = a->softcap > 0.f ? scale / a->softcap * (shape->dtype == GSIT_BF16 ? 2.f * LOG2E : 1.f) : scale * LOG2E;
+  // bf16 rows' tanh by 1 - 2 / (e^2y + 1) is off by 2^-22 of 1, however small it is: by 2^-22 of the cap in the score, 2^-16 at FAST_CAP
+  constexpr float FAST_CAP = 64.f;
+  a->fast_cap = shape->dtype == GSIT_BF16 && a->softcap <= FAST_CAP;
+  a->inner = a->softcap > 0.f ? scale / a->softcap * (a->fast_cap ? 2.f * LOG2E : 1.f) : scale * LOG2E;
   a->outer = a->softcap * LOG2E;
   return isfinite(a->inner) && isfinite(a->outer) ? GSIT_OK : GSIT_ERR_INVALID_ARG;
 }

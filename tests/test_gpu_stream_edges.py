@@ -2,8 +2,8 @@
 import pytest
 import torch
 
-from stream_reference import bytes_of
-from test_gpu_stream import g, nothing_is_flagged   # noqa: F401
+from stream_reference import Streams, bytes_of, open_blocks
+from test_gpu_stream import _attention_close, _rows, g, nothing_is_flagged   # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +71,17 @@ def test_a_long_even_tail(g, held_as, t, below):
 def test_a_long_even_tail_of_integers(g, below):
     """What stands out has values of 0, so nothing of its weight may be left in the sums."""
     _even_tail(g, torch.bfloat16, "int8", below)
+
+
+@pytest.mark.parametrize("cap", [1e-3, 1.0, 50.0, 65.0, 1e3, 1e5, 1e9])
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float32])
+def test_caps_of_any_size(g, t, cap):
+    """A cap far above the scores changes nothing of them; one far below leaves their signs."""
+    B, H, HK, hd, seg, gen = 1, 4, 2, 32, (40, 3, 33), torch.Generator().manual_seed(5)
+    cache, ref = g.stream_cache(B, seg, HK, hd, t), Streams(B, "int8")
+    q, k, v = _rows(gen, B, sum(seg), H, hd, t), _rows(gen, B, sum(seg), HK, hd, t), _rows(gen, B, sum(seg), HK, hd, t)
+    g.cache_append(cache, k, v, g.cache_plan(cache, seg), seg)
+    ref.step(seg, [seg], k, v)
+    got = g.im_cached_attention_fwd(q, cache, seg, phase=g.PHASE_CUSTOM, custom_mask=0x1FF, softcap=cap, want_lse=True)
+    want = ref.attention(q, seg, [seg], open_blocks(None, 0x1FF), hd ** -0.5, softcap=cap)
+    _attention_close(got, want, t, cap)

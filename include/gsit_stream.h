@@ -81,7 +81,7 @@ gsit_status gsit_cache_read(const gsit_shape* shape, const gsit_cache* cache, vo
  *   shape        d_model, heads, phase, custom_mask and scale as there; dtype of the cache
  *   rule         softcap, causal and slopes; kv_heads of the cache, or 0.  times, documents, prefix and tail are not taken (GSIT_ERR_UNSUPPORTED).
  *   times        the moments of the step's rows, as above: given where the cache holds times and the rule goes by them (causal, slopes); NULL where it holds
- *                none (the index inside the segment counts)
+ *                none (the index inside the segment counts, in tables of up to 2^19 blocks a segment: GSIT_ERR_UNSUPPORTED beyond)
  *   q            [batch][L][heads][head_dim], as above;  out [batch][L][d] contiguous;  lse float [batch][heads][L] or NULL
  *   workspace    gsit_cached_attention_workspace() bytes, 16-byte aligned (NULL and 0 where that is 0); what stands in it does not matter */
 gsit_status gsit_im_cached_attention_fwd(const gsit_shape* shape, const gsit_score_rule* rule, const gsit_cache* cache, const void* q,

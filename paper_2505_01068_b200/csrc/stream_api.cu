@@ -67,6 +67,8 @@ gsit_status attention_args(const gsit_shape* shape, const gsit_score_rule* r, co
   a->slopes = r->slopes;
   a->times = times;
   if ((a->causal || a->slopes != nullptr) && (times.p != nullptr) != (cache->times != nullptr)) return GSIT_ERR_INVALID_ARG;
+  // indices are compared and subtracted as floats, which are whole numbers up to 2^24
+  if ((a->causal || a->slopes != nullptr) && cache->times == nullptr && cache->blocks > (1 << 24) / CACHE_BLOCK) return GSIT_ERR_UNSUPPORTED;
   const float scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)g->hd);
   constexpr float LOG2E = 1.4426950408889634f;
   a->softcap = r->softcap > 0.f ? r->softcap : 0.f;

@@ -80,5 +80,6 @@ def cache_read(cache, seg_len, out_k=None, out_v=None):
 def im_cached_attention_fwd(q, cache, seg_len, valid_len=None, phase=B.PHASE_INTER_FWD, custom_mask=0, scale=0.0, softcap=0.0, slopes=None, times=None, causal=False,
                             want_lse=False, out=None, workspace=None):
     """im_scored_attention_fwd for a step's rows q [B, L, H, hd] against the cache: real row i of segment s is position lengths - valid_len + i of it.
-    times float32 [B, L]: moments of these rows, where the cache holds moments (None where it does not: the index inside the segment).  Returns out [B, L, d] (and lse [B, H, L])."""
+    times float32 [B, L]: moments of these rows, where the cache holds moments (None where it does not: the index inside the segment, in tables of
+    at most 2^19 blocks).  Returns out [B, L, d] (and lse [B, H, L])."""
     return B.native().cached_attention(*cache, q, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, causal, want_lse, out, workspace)

@@ -8,7 +8,7 @@
  *   gsit_cache_plan             lengths, pages for what the step adds, and the slot of each of its rows
  *   gsit_cache_append           the step's keys and values
  *   gsit_im_cached_attention_fwd   the step's queries against everything the cache holds then
- * Every call reads lengths, tables and counts on the device, so a step can be captured into a graph and replayed while streams grow, end and
+ * or all three by gsit_cache_step.  Every call reads lengths, tables and counts on the device, so a step can be captured into a graph and replayed while streams grow, end and
  * begin.  A step can also be taken again -- after a guess that was wrong, say -- from the lengths before it (plan's `held`), as long as it brought
  * no segment more than 32 rows, or started from nothing: the blocks it filled are filled anew.
  */
@@ -88,6 +88,13 @@ gsit_status gsit_im_cached_attention_fwd(const gsit_shape* shape, const gsit_sco
                                          int64_t q_row_stride, const float* times, int64_t times_batch_stride, int64_t times_row_stride,
                                          void* out, float* lse, void* workspace, size_t workspace_bytes, gsit_stream stream);
 size_t gsit_cached_attention_workspace(const gsit_shape* shape, const gsit_score_rule* rule, const gsit_cache* cache);   /* (size_t)-1: invalid */
+
+/* A step: the three calls above with one shape (that of attention) and the arguments that each of them takes.  What any of them would refuse is refused
+ * before the cache is touched, where one call after the other would leave its lengths counting rows that are not there. */
+gsit_status gsit_cache_step(const gsit_shape* shape, const gsit_score_rule* rule, const gsit_cache* cache, const int32_t* held, const int32_t* ended,
+                            int32_t* slots, const void* q, int64_t q_row_stride, const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride,
+                            const float* times, int64_t times_batch_stride, int64_t times_row_stride, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, gsit_stream stream);
 
 #ifdef __cplusplus
 }

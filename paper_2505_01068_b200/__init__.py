@@ -10,7 +10,7 @@ from .binding import (CALL_ATTENTION, CALL_LAYER, CALL_QKV_PROJ, DEVFLAG_CLAMPED
                       KERNEL_ATTENTION, KERNEL_LINEAR, KERNEL_LAYERNORM, ATTN_DEFAULT, ATTN_UNFUSED, ATTN_LEGACY, ATTN_TMEM,
                       expire_wait_selftest, late_write, wait_answers,
                       rotary_fwd, rotary_bwd, head_norm_rotary_fwd, head_norm_rotary_bwd, layer_norm_fwd, layer_norm_bwd, im_scored_attention_fwd, im_scored_attention_bwd)
-from .streaming import CACHE_BLOCK, StreamCache, StreamTables, cache_append, cache_plan, cache_read, im_cached_attention_fwd, stream_cache, stream_tables
+from .streaming import CACHE_BLOCK, StreamCache, StreamTables, cache_append, cache_plan, cache_read, cache_step, im_cached_attention_fwd, stream_cache, stream_tables
 from .stack import GsitStack
 from .training import ImEncoderLayer
 from .hostio import HostPipeline

@@ -50,7 +50,7 @@ EXPORTS = ("gsit_im_qkv_proj", "gsit_im_attention_fwd", "gsit_im_layer_fwd", "gs
            "gsit_im_encoder_fwd", "gsit_encoder_runs_chained", "gsit_im_layer_scatter_fwd", "gsit_layer_scatters", "gsit_attention_uses_workspace",
            "gsit_rotary_fwd", "gsit_rotary_bwd", "gsit_head_norm_rotary_fwd", "gsit_head_norm_rotary_bwd", "gsit_head_norm_rotary_bwd_workspace", "gsit_layer_norm_fwd", "gsit_layer_norm_bwd", "gsit_layer_norm_bwd_workspace",
            "gsit_im_scored_attention_fwd", "gsit_im_scored_attention_bwd", "gsit_scored_attention_fwd_workspace", "gsit_scored_attention_bwd_workspace",
-           "gsit_cache_plan", "gsit_cache_append", "gsit_cache_read", "gsit_im_cached_attention_fwd", "gsit_cached_attention_workspace")
+           "gsit_cache_plan", "gsit_cache_append", "gsit_cache_read", "gsit_im_cached_attention_fwd", "gsit_cached_attention_workspace", "gsit_cache_step")
 STATIC_SCRATCH_BYTES = 4 << 20
 KERNEL_ATTENTION, KERNEL_LINEAR, KERNEL_LAYERNORM = 0, 1, 2
 ATTN_DEFAULT, ATTN_UNFUSED, ATTN_LEGACY, ATTN_TMEM = 0, 8, 9, 10   # gsit_kernel_choice of include/gsit_test.h

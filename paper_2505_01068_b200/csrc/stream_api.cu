@@ -84,6 +84,49 @@ cudaError_t launch_attention(const Geometry& g, int32_t dtype, CachedArgs& a, cu
   return dtype == GSIT_BF16 ? launch_cached_bf16(g, a, st, scratch) : launch_cached_f32(g, a, st, scratch);
 }
 
+// The calls' checks; what is left behind them is ready() and to launch.
+gsit_status ready(Geometry* g) { return status_of(device_status_word(&g->status)) == GSIT_OK ? GSIT_OK : GSIT_ERR_CUDA; }
+struct Rows {
+  const void* p;
+  int64_t ld;
+};
+gsit_status plan_call(const gsit_shape* shape, const gsit_cache* cache, const int32_t* held, const int32_t* ended, const int32_t* slots, Geometry* g, Cache* c) {
+  gsit_status st = step_geometry(shape, g);
+  if (st == GSIT_OK) st = tables_of(cache, *g, c);
+  if (st != GSIT_OK) return st;
+  for (const void* p : {(const void*)c->free_list, (const void*)c->n_free, (const void*)slots})
+    if (p == nullptr || !aligned(p, 4)) return GSIT_ERR_INVALID_ARG;
+  if (!aligned(held, 4) || !aligned(ended, 4)) return GSIT_ERR_INVALID_ARG;
+  return GSIT_OK;
+}
+gsit_status append_call(const gsit_shape* shape, const gsit_cache* cache, const Rows& k, const Rows& v, const int32_t* slots, const float* times, Geometry* g, Cache* c) {
+  gsit_status st = step_geometry(shape, g);
+  if (st == GSIT_OK) st = cache_of(cache, *g, c);
+  if (st != GSIT_OK) return st;
+  const int64_t cols = (int64_t)c->kv_heads * c->hd;
+  if (!rows_ok(k.p, k.ld, cols, cache->dtype) || !rows_ok(v.p, v.ld, cols, cache->dtype) || slots == nullptr || !aligned(slots, 4) || !aligned(times, 4) ||
+      (c->times != nullptr && times == nullptr))
+    return GSIT_ERR_INVALID_ARG;
+  return GSIT_OK;
+}
+gsit_status attention_call(const gsit_shape* shape, const gsit_score_rule* rule, const gsit_cache* cache, const Rows& q, const RowTimes& times, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, Geometry* g, CachedArgs* a) {
+  const gsit_status st = attention_args(shape, rule, cache, times, g, a);
+  if (st != GSIT_OK) return st;
+  if (!rows_ok(q.p, q.ld, g->d, cache->dtype) || out == nullptr || !aligned(out, cache->dtype == GSIT_BF16 ? 2 : 4) || !aligned(lse, 4)) return GSIT_ERR_INVALID_ARG;
+  size_t need = 0;
+  const cudaError_t e = launch_attention(*g, cache->dtype, *a, nullptr, &need);
+  if (e != cudaSuccess) return status_of(e);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return GSIT_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return GSIT_ERR_INVALID_ARG;
+  a->q = q.p;
+  a->ldq = q.ld;
+  a->out = out;
+  a->lse = lse;
+  a->parts = static_cast<float*>(workspace);
+  return GSIT_OK;
+}
+
 }  // namespace
 }  // namespace gsit
 
@@ -94,28 +137,18 @@ extern "C" {
 gsit_status gsit_cache_plan(const gsit_shape* shape, const gsit_cache* cache, const int32_t* held, const int32_t* ended, int32_t* slots, gsit_stream stream) {
   Geometry g;
   Cache c;
-  gsit_status st = step_geometry(shape, &g);
-  if (st == GSIT_OK) st = tables_of(cache, g, &c);
-  if (st != GSIT_OK) return st;
-  for (const void* p : {(const void*)c.free_list, (const void*)c.n_free, (const void*)slots})
-    if (p == nullptr || !aligned(p, 4)) return GSIT_ERR_INVALID_ARG;
-  if (!aligned(held, 4) || !aligned(ended, 4)) return GSIT_ERR_INVALID_ARG;
-  if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
-  return status_of(launch_cache_plan(g, c, held, ended, slots, static_cast<cudaStream_t>(stream)));
+  gsit_status st = plan_call(shape, cache, held, ended, slots, &g, &c);
+  if (st == GSIT_OK) st = ready(&g);
+  return st != GSIT_OK ? st : status_of(launch_cache_plan(g, c, held, ended, slots, static_cast<cudaStream_t>(stream)));
 }
 
 gsit_status gsit_cache_append(const gsit_shape* shape, const gsit_cache* cache, const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride,
                               const int32_t* slots, const float* times, int64_t times_batch_stride, int64_t times_row_stride, gsit_stream stream) {
   Geometry g;
   Cache c;
-  gsit_status st = step_geometry(shape, &g);
-  if (st == GSIT_OK) st = cache_of(cache, g, &c);
+  gsit_status st = append_call(shape, cache, {k, k_row_stride}, {v, v_row_stride}, slots, times, &g, &c);
+  if (st == GSIT_OK) st = ready(&g);
   if (st != GSIT_OK) return st;
-  const int64_t cols = (int64_t)c.kv_heads * c.hd;
-  if (!rows_ok(k, k_row_stride, cols, cache->dtype) || !rows_ok(v, v_row_stride, cols, cache->dtype) || slots == nullptr || !aligned(slots, 4) ||
-      !aligned(times, 4) || (c.times != nullptr && times == nullptr))
-    return GSIT_ERR_INVALID_ARG;
-  if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
   return status_of(launch_cache_append(g, cache->dtype, c, k, k_row_stride, v, v_row_stride, slots, {times, times_batch_stride, times_row_stride}, static_cast<cudaStream_t>(stream)));
 }
 
@@ -144,21 +177,30 @@ gsit_status gsit_im_cached_attention_fwd(const gsit_shape* shape, const gsit_sco
                                          size_t workspace_bytes, gsit_stream stream) {
   Geometry g;
   CachedArgs a;
-  const gsit_status st = attention_args(shape, rule, cache, {times, times_batch_stride, times_row_stride}, &g, &a);
-  if (st != GSIT_OK) return st;
-  if (!rows_ok(q, q_row_stride, g.d, cache->dtype) || out == nullptr || !aligned(out, cache->dtype == GSIT_BF16 ? 2 : 4) || !aligned(lse, 4)) return GSIT_ERR_INVALID_ARG;
-  size_t need = 0;
-  const cudaError_t e = launch_attention(g, cache->dtype, a, nullptr, &need);
-  if (e != cudaSuccess) return status_of(e);
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return GSIT_ERR_WORKSPACE;
-  if (need > 0 && !aligned(workspace, 16)) return GSIT_ERR_INVALID_ARG;
-  if (status_of(device_status_word(&g.status)) != GSIT_OK) return GSIT_ERR_CUDA;
-  a.q = q;
-  a.ldq = q_row_stride;
-  a.out = out;
-  a.lse = lse;
-  a.parts = static_cast<float*>(workspace);
-  return status_of(launch_attention(g, cache->dtype, a, static_cast<cudaStream_t>(stream), nullptr));
+  gsit_status st = attention_call(shape, rule, cache, {q, q_row_stride}, {times, times_batch_stride, times_row_stride}, out, lse, workspace, workspace_bytes, &g, &a);
+  if (st == GSIT_OK) st = ready(&g);
+  return st != GSIT_OK ? st : status_of(launch_attention(g, cache->dtype, a, static_cast<cudaStream_t>(stream), nullptr));
+}
+
+gsit_status gsit_cache_step(const gsit_shape* shape, const gsit_score_rule* rule, const gsit_cache* cache, const int32_t* held, const int32_t* ended,
+                            int32_t* slots, const void* q, int64_t q_row_stride, const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride,
+                            const float* times, int64_t times_batch_stride, int64_t times_row_stride, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, gsit_stream stream) {
+  const RowTimes moments = {times, times_batch_stride, times_row_stride};
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  Geometry gp = {}, ga = {}, gq = {};
+  Cache tables, c;
+  CachedArgs a;
+  // all checks, then all launches
+  gsit_status st = plan_call(shape, cache, held, ended, slots, &gp, &tables);
+  if (st == GSIT_OK) st = append_call(shape, cache, {k, k_row_stride}, {v, v_row_stride}, slots, times, &ga, &c);
+  if (st == GSIT_OK) st = attention_call(shape, rule, cache, {q, q_row_stride}, moments, out, lse, workspace, workspace_bytes, &gq, &a);
+  if (st == GSIT_OK) st = ready(&gp);
+  ga.status = gq.status = gp.status;
+  if (st == GSIT_OK) st = status_of(launch_cache_plan(gp, tables, held, ended, slots, s));
+  if (st == GSIT_OK) st = status_of(launch_cache_append(ga, cache->dtype, c, k, k_row_stride, v, v_row_stride, slots, moments, s));
+  if (st == GSIT_OK) st = status_of(launch_attention(gq, cache->dtype, a, s, nullptr));
+  return st;
 }
 
 }  // extern "C"

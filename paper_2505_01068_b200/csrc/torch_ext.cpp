@@ -635,6 +635,7 @@ PyMethodDef methods[] = {def<init, 1>("init"),
                          def<cache_append, 16>("cache_append"),
                          def<cache_read, 14>("cache_read"),
                          def<cached_attention, 24>("cached_attention"),
+                         def<cache_step, 28>("cache_step"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -75,6 +75,14 @@ gsit_shape step_shape(const gsit_cache& c, PyObject* seg, const at::Tensor* vali
 }
 int64_t rows_of(const gsit_shape& s) { return (int64_t)s.seg_len[0] + s.seg_len[1] + s.seg_len[2]; }
 
+at::Tensor slots_for(const at::Tensor* given, const gsit_cache& c, int64_t L, const at::Device& dev) {
+  if (given == nullptr) return empty({c.batch, L}, at::kInt, dev);
+  require(given->scalar_type() == at::kInt && given->is_contiguous() && given->dim() == 2 && given->size(0) == c.batch && given->size(1) == L, "slots: contiguous int32 [B, L]");
+  return *given;
+}
+const int32_t* ended_of(const at::Tensor* t, const gsit_cache& c) { return int_vector(t, c.batch, "ended: contiguous int32 [B]"); }
+const int32_t* held_of(const at::Tensor* t, const gsit_cache& c) { return int_vector(t, 3 * (int64_t)c.batch, "held: contiguous int32 [B, 3]"); }
+
 // tables, lengths, free, n_free, seg_len, valid_len, ended, held, slots
 PyObject* cache_plan(PyObject* const* a) {
   const gsit_cache c = tables_of(a);
@@ -82,13 +90,8 @@ PyObject* cache_plan(PyObject* const* a) {
   here({valid, ended, held, slots});
   const gsit_shape s = step_shape(c, a[4], valid);
   for (int n : s.seg_len) require(n >= 0, "seg_len: no length is negative");
-  const int64_t L = rows_of(s);
-  const int32_t* e = int_vector(ended, c.batch, "ended: contiguous int32 [B]");
-  const int32_t* h = int_vector(held, 3 * (int64_t)c.batch, "held: contiguous int32 [B, 3]");
-  at::Tensor made;
-  if (slots == nullptr) made = empty({c.batch, L}, at::kInt, tensor(a[0]).device());
-  else made = *slots;
-  require(made.scalar_type() == at::kInt && made.is_contiguous() && made.dim() == 2 && made.size(0) == c.batch && made.size(1) == L, "slots: contiguous int32 [B, L]");
+  const int32_t *e = ended_of(ended, c), *h = held_of(held, c);
+  at::Tensor made = slots_for(slots, c, rows_of(s), tensor(a[0]).device());
   gsit_status st;
   {
     NoGil n;
@@ -96,6 +99,16 @@ PyObject* cache_plan(PyObject* const* a) {
   }
   check(st, "gsit_cache_plan");
   return THPVariable_Wrap(std::move(made));
+}
+
+// Row strides of a step's keys and values.
+struct NewRows {
+  int64_t ldk, ldv;
+};
+NewRows new_rows(const at::Tensor& k, const at::Tensor& v, const gsit_cache& c, int64_t L) {
+  require(k.dim() == 4 && k.sizes() == v.sizes() && k.size(0) == c.batch && k.size(1) == L && k.size(2) == c.kv_heads && k.size(3) == c.head_dim &&
+              dtype_code(k) == c.dtype && v.scalar_type() == k.scalar_type(), "k, v: [B, L, kv_heads, hd] of the cache's type");
+  return {head_rows(k, HEAD_ROWS), head_rows(v, HEAD_ROWS)};
 }
 
 // the cache (11), k, v, slots, seg_len, times
@@ -106,15 +119,13 @@ PyObject* cache_append(PyObject* const* a) {
   here({&k, &v, &slots, times});
   const gsit_shape s = step_shape(c, a[14], nullptr);
   const int64_t L = rows_of(s);
-  require(k.dim() == 4 && k.sizes() == v.sizes() && k.size(0) == c.batch && k.size(1) == L && k.size(2) == c.kv_heads && k.size(3) == c.head_dim &&
-              dtype_code(k) == c.dtype && v.scalar_type() == k.scalar_type(), "k, v: [B, L, kv_heads, hd] of the cache's type");
-  const int64_t ldk = head_rows(k, HEAD_ROWS), ldv = head_rows(v, HEAD_ROWS);
+  const NewRows ld = new_rows(k, v, c, L);
   const int32_t* sl = int_vector(&slots, c.batch * L, "slots: contiguous int32 [B, L]");
   const RowMoments tm = moments(times, c.batch, L);
   gsit_status st;
   {
     NoGil n;
-    st = gsit_cache_append(&s, &c, k.data_ptr(), ldk, v.data_ptr(), ldv, sl, tm.p, tm.batch, tm.row, stream());
+    st = gsit_cache_append(&s, &c, k.data_ptr(), ld.ldk, v.data_ptr(), ld.ldv, sl, tm.p, tm.batch, tm.row, stream());
   }
   check(st, "gsit_cache_append");
   Py_RETURN_NONE;
@@ -147,41 +158,81 @@ PyObject* cache_read(PyObject* const* a) {
   return pack({mk, mv});
 }
 
+// Queries, rule, result and workspace of an attention call.
+struct AttentionCall {
+  gsit_shape s;
+  gsit_score_rule r;
+  RowMoments times;
+  int64_t ldq;
+  at::Tensor out, made_ws;
+  void* ws;
+  size_t ws_bytes;
+};
+AttentionCall attention_call(const gsit_cache& c, const at::Tensor& q, PyObject* seg, const at::Tensor* valid, PyObject* phase, PyObject* mask, PyObject* scale, PyObject* softcap,
+                             const at::Tensor* slopes, const at::Tensor* times, PyObject* causal, const at::Tensor* out, const at::Tensor* ws) {
+  AttentionCall x = {};
+  x.ldq = head_rows(q, HEAD_ROWS);
+  const int64_t B = q.size(0), L = q.size(1), H = q.size(2), hd = q.size(3);
+  require(B == c.batch && hd == c.head_dim && dtype_code(q) == c.dtype, "q: [B, L, H, hd] of the cache's batch, head width and type");
+  x.s = make_shape(B, seg, H * hd, H, valid, c.dtype, as_int(phase), as_int(mask), as_float(scale));
+  require_length(x.s, L);
+  x.r.softcap = (float)as_float(softcap);
+  x.r.slopes = float_vector(slopes, H, "slopes: contiguous float32 [heads] on the device");
+  x.times = moments(times, B, L);
+  x.r.causal = as_bool(causal);
+  if (out == nullptr) x.out = empty({B, L, H * hd}, q.scalar_type(), q.device());
+  else x.out = *out;
+  require(x.out.is_contiguous() && x.out.scalar_type() == q.scalar_type() && x.out.numel() == B * L * H * hd, "out: contiguous [B, L, d] of q's dtype");
+  if (ws == nullptr) {
+    const size_t need = gsit_cached_attention_workspace(&x.s, &x.r, &c);
+    if (need != (size_t)-1 && need > 0) {
+      x.made_ws = empty({(int64_t)need}, at::kByte, q.device());
+      ws = &x.made_ws;
+    }
+  }
+  x.ws = ptr(ws);
+  x.ws_bytes = ws == nullptr ? 0 : (size_t)ws->nbytes();
+  return x;
+}
+
 // the cache (11), q, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, causal, want_lse, out, workspace
 PyObject* cached_attention(PyObject* const* a) {
   const gsit_cache c = cache_of(a);
   const at::Tensor& q = tensor(a[11]);
   const at::Tensor *valid = opt_tensor(a[13]), *slopes = opt_tensor(a[18]), *times = opt_tensor(a[19]), *out = opt_tensor(a[22]), *ws = scratch(a[23]);
   here({&q, valid, slopes, times, out, ws});
-  const int64_t ldq = head_rows(q, HEAD_ROWS), B = q.size(0), L = q.size(1), H = q.size(2), hd = q.size(3);
-  require(B == c.batch && hd == c.head_dim && dtype_code(q) == c.dtype, "q: [B, L, H, hd] of the cache's batch, head width and type");
-  const gsit_shape s = make_shape(B, a[12], H * hd, H, valid, c.dtype, as_int(a[14]), as_int(a[15]), as_float(a[16]));
-  require_length(s, L);
-  gsit_score_rule r = {};
-  r.softcap = (float)as_float(a[17]);
-  r.slopes = float_vector(slopes, H, "slopes: contiguous float32 [heads] on the device");
-  const RowMoments tm = moments(times, B, L);
-  r.causal = as_bool(a[20]);
+  AttentionCall x = attention_call(c, q, a[12], valid, a[14], a[15], a[16], a[17], slopes, times, a[20], out, ws);
   const bool want_lse = as_bool(a[21]);
-  at::Tensor made, lse, made_ws;
-  if (out == nullptr) made = empty({B, L, H * hd}, q.scalar_type(), q.device());
-  else made = *out;
-  require(made.is_contiguous() && made.scalar_type() == q.scalar_type() && made.numel() == B * L * H * hd, "out: contiguous [B, L, d] of q's dtype");
-  if (want_lse) lse = empty({B, H, L}, at::kFloat, q.device());
-  if (ws == nullptr) {
-    const size_t need = gsit_cached_attention_workspace(&s, &r, &c);
-    if (need != (size_t)-1 && need > 0) {
-      made_ws = empty({(int64_t)need}, at::kByte, q.device());
-      ws = &made_ws;
-    }
-  }
+  at::Tensor lse;
+  if (want_lse) lse = empty({q.size(0), q.size(2), q.size(1)}, at::kFloat, q.device());
   gsit_status st;
   {
     NoGil n;
-    st = gsit_im_cached_attention_fwd(&s, &r, &c, q.data_ptr(), ldq, tm.p, tm.batch, tm.row, made.data_ptr(), want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, ptr(ws),
-                                      ws == nullptr ? 0 : (size_t)ws->nbytes(), stream());
+    st = gsit_im_cached_attention_fwd(&x.s, &x.r, &c, q.data_ptr(), x.ldq, x.times.p, x.times.batch, x.times.row, x.out.data_ptr(),
+                                      want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, x.ws, x.ws_bytes, stream());
   }
   check(st, "gsit_im_cached_attention_fwd");
-  if (!want_lse) return THPVariable_Wrap(std::move(made));
-  return pack({made, lse});
+  if (!want_lse) return THPVariable_Wrap(std::move(x.out));
+  return pack({x.out, lse});
+}
+
+// the cache (11), q, k, v, seg_len, valid_len, ended, held, phase, custom_mask, scale, softcap, slopes, times, causal, slots, out, workspace
+PyObject* cache_step(PyObject* const* a) {
+  const gsit_cache c = cache_of(a);
+  const at::Tensor &q = tensor(a[11]), &k = tensor(a[12]), &v = tensor(a[13]);
+  const at::Tensor *valid = opt_tensor(a[15]), *ended = opt_tensor(a[16]), *held = opt_tensor(a[17]), *slopes = opt_tensor(a[22]), *times = opt_tensor(a[23]),
+                   *slots = opt_tensor(a[25]), *out = opt_tensor(a[26]), *ws = scratch(a[27]);
+  here({&q, &k, &v, valid, ended, held, slopes, times, slots, out, ws});
+  AttentionCall x = attention_call(c, q, a[14], valid, a[18], a[19], a[20], a[21], slopes, times, a[24], out, ws);
+  const NewRows ld = new_rows(k, v, c, q.size(1));
+  const int32_t *e = ended_of(ended, c), *h = held_of(held, c);
+  at::Tensor made = slots_for(slots, c, q.size(1), q.device());
+  gsit_status st;
+  {
+    NoGil n;
+    st = gsit_cache_step(&x.s, &x.r, &c, h, e, static_cast<int32_t*>(made.data_ptr()), q.data_ptr(), x.ldq, k.data_ptr(), ld.ldk, v.data_ptr(), ld.ldv, x.times.p, x.times.batch,
+                         x.times.row, x.out.data_ptr(), nullptr, x.ws, x.ws_bytes, stream());
+  }
+  check(st, "gsit_cache_step");
+  return pack({x.out, made});
 }

@@ -1,7 +1,7 @@
 """A stream's past in 8 bits: caches of keys and values, and the calls of gsit_stream.h on them.
 
 A step of a batch of streams is cache_plan (where do its rows go?), cache_append (its keys and values) and im_cached_attention_fwd (its queries against
-all that is held then).  Lengths, tables and counts stay on the device, so a step can be captured into a graph and replayed."""
+all that is held then), or cache_step, which is all three.  Lengths, tables and counts stay on the device, so a step can be captured into a graph and replayed."""
 from __future__ import annotations
 
 from typing import NamedTuple, Optional
@@ -83,3 +83,10 @@ def im_cached_attention_fwd(q, cache, seg_len, valid_len=None, phase=B.PHASE_INT
     times float32 [B, L]: moments of these rows, where the cache holds moments (None where it does not: the index inside the segment, in tables of
     at most 2^19 blocks).  Returns out [B, L, d] (and lse [B, H, L])."""
     return B.native().cached_attention(*cache, q, seg_len, valid_len, phase, custom_mask, scale, softcap, slopes, times, causal, want_lse, out, workspace)
+
+
+def cache_step(cache, q, k, v, seg_len, valid_len=None, ended=None, held=None, phase=B.PHASE_INTER_FWD, custom_mask=0, scale=0.0, softcap=0.0, slopes=None, times=None,
+               causal=False, slots=None, out=None, workspace=None):
+    """cache_plan, cache_append and im_cached_attention_fwd for a step's rows q [B, L, H, hd], k and v [B, L, Hk, hd], in one call that changes nothing of the
+    cache where any of the three refuses its arguments.  Returns (out [B, L, d], slots [B, L])."""
+    return B.native().cache_step(*cache, q, k, v, seg_len, valid_len, ended, held, phase, custom_mask, scale, softcap, slopes, times, causal, slots, out, workspace)

@@ -46,9 +46,11 @@ def stream_tables(batch, blocks, pages, device="cuda"):
 
 def stream_cache(batch, max_len, kv_heads, head_dim, dtype=torch.bfloat16, held_as="int8", pages=None, times=False, device="cuda"):
     """An empty cache for `batch` streams of at most max_len (three numbers) positions a segment, held as "int8" or "e4m3"; pages: of the pool (default: enough
-    for all streams at their longest).  times: every position has a moment (causality and slopes go by it)."""
+    for all streams at their longest).  times: every position has a moment (causality and slopes go by it).  head_dim 8, 16, 32 or 64; dtype float32 or bfloat16."""
     if held_as not in ("int8", "e4m3"):
         raise ValueError('held_as: "int8" or "e4m3"')
+    if head_dim not in (8, 16, 32, 64) or dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("a cache holds heads of 8, 16, 32 or 64 features, float32 or bfloat16")
     need = [(int(n) + CACHE_BLOCK - 1) // CACHE_BLOCK for n in max_len]
     pages = max(1, batch * sum(need)) if pages is None else int(pages)
     zeros = lambda shape, t: torch.zeros(shape, dtype=t, device=device)

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from test_ops_refusals import P, Rule, _call, _shape, g   # noqa: F401
 from test_stream_refusals import NONE, ODD, VP, _cache
@@ -39,3 +40,12 @@ def test_a_step_refuses_what_its_calls_refuse(g, kw, code):
     a.update(kw)
     assert _call(g.load(), "gsit_cache_step", _shape(g), r, c, a["held"], a["ended"], a["slots"], a["q"], a["ldq"], a["k"], a["ldk"], a["v"], a["ldv"], a["times"], 10, 1, a["out"],
                  a["lse"], NONE, ctypes.c_size_t(0), None) == code
+
+
+def test_a_cache_that_no_call_takes(g):
+    """Refused when it is opened, before a plan has given pages to rows that nothing can hold."""
+    for kw in (dict(head_dim=24), dict(head_dim=128), dict(head_dim=4), dict(dtype=torch.float16), dict(dtype=torch.float64), dict(held_as="fp8")):
+        with pytest.raises(ValueError):
+            g.stream_cache(**{**dict(batch=1, max_len=(3, 3, 3), kv_heads=1, head_dim=16, device="cpu"), **kw})
+    cache = g.stream_cache(2, (40, 0, 64), 3, 8, torch.float32, "e4m3", device="cpu")
+    assert cache.tables.shape == (2, 3, 2) and cache.keys.shape == (8, 3, 256) and cache.open_keys.dtype is torch.float32

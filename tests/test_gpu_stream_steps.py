@@ -62,3 +62,25 @@ def test_a_refused_step_changes_nothing(g, timed):
         assert _same(_parts(caches[0]), before), kw
     assert torch.equal(layer.step(caches[0], x[1], seg, **good), layer.step(caches[1], x[1], seg, **good))
     assert _same(_parts(caches[0]), _parts(caches[1]))
+
+
+@pytest.mark.parametrize("padded", [False, True])
+def test_streams_that_find_no_pages(g, padded):
+    """Rows that did not join the cache are +0, whether or not lengths are given, and the others are what they are with pages for all."""
+    torch.manual_seed(5)
+    B, D, most, seg = 3, 32, (64, 64, 64), (33, 2, 40)
+    layer = g.ImEncoderLayer(D, 4, most)
+    few, many = layer.open_cache(B, most, pages=9), layer.open_cache(B, most)
+    x = torch.randn((B, sum(seg), D), device="cuda")
+    valid = torch.tensor([list(seg)] * B, dtype=torch.int32, device="cuda") if padded else None
+    rule = dict(phase=g.PHASE_INTRA)
+    want = layer.step(many, x, seg, valid, **rule)
+    assert g.last_device_status() == (0, 0)
+    got = layer.step(few, x, seg, valid, **rule)
+    torch.cuda.synchronize()
+    assert g.last_device_status()[1] == g.DEVFLAG_FULL
+    # five blocks a stream: the first stream's, the second's first two segments; its third finds one page, and nothing behind it is taken
+    real = torch.zeros((B, sum(seg), 1), dtype=torch.bool, device="cuda")
+    real[0], real[1, :35] = True, True
+    assert few.lengths.cpu().tolist() == [[33, 2, 40], [33, 2, 0], [0, 0, 0]]
+    assert torch.equal(got, torch.where(real, want, 0.0)) and not torch.signbit(got[~real.expand_as(got)]).any() and bool(want[~real.expand_as(got)].any())

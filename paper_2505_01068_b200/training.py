@@ -171,12 +171,13 @@ class ImEncoderLayer(torch.nn.Module):
         return S.stream_cache(batch, max_len, self.kv_heads, self.hd, self.dtype, held_as, pages, times, self.place.device)
 
     @torch.no_grad()
-    def step(self, cache, x, seg_len, valid_len=None, positions=None, times=None, ended=None, **rule):
+    def step(self, cache, x, seg_len, valid_len=None, positions=None, times=None, ended=None, held=None, **rule):
         """The layer for the newest positions of streams: x float32 [B, L, d] holds seg_len rows of each segment, the first valid_len of them real, which join
         the cache and then attend to all that it holds.  positions int32 [axes, B, L] and times float32 [B, L] are those of these rows; ended int32 [B]:
-        streams that begin anew; rule: phase, custom_mask, scale, softcap, slopes, causal.  Returns y [B, L, d], padded rows +0, and so are
+        streams that begin anew; held int32 [B, 3]: the cache's lengths before a step that is taken again (of 32 rows a segment at most, or one that started from
+        nothing); rule: phase, custom_mask, scale, softcap, slopes, causal.  Returns y [B, L, d], padded rows +0, and so are
         those of segments that found no pages or no room in their tables (DEVFLAG_FULL in last_device_status).  Arguments that are refused leave the cache as it was."""
         q, k, v = self.project(x, valid_len, positions, seg_len)
-        att, slots = S.cache_step(cache, q, k, v, seg_len, valid_len, ended, times=times, **rule)
+        att, slots = S.cache_step(cache, q, k, v, seg_len, valid_len, ended, held, times=times, **rule)
         y = self.finish(x, att, valid_len, seg_len)
         return torch.where((slots >= 0)[:, :, None], y, 0.0)

@@ -84,3 +84,20 @@ def test_streams_that_find_no_pages(g, padded):
     real[0], real[1, :35] = True, True
     assert few.lengths.cpu().tolist() == [[33, 2, 40], [33, 2, 0], [0, 0, 0]]
     assert torch.equal(got, torch.where(real, want, 0.0)) and not torch.signbit(got[~real.expand_as(got)]).any() and bool(want[~real.expand_as(got)].any())
+
+
+def test_a_layers_step_taken_again(g):
+    """A step with other rows from the lengths before it: as if the first one had never been."""
+    torch.manual_seed(6)
+    B, D, most, seg = 2, 32, (80, 80, 80), (3, 32, 1)
+    layer = g.ImEncoderLayer(D, 4, most)
+    x = torch.randn((4, B, sum(seg), D), device="cuda")
+    caches = [layer.open_cache(B, most) for _ in range(2)]
+    for cache in caches:
+        layer.step(cache, x[0], seg)
+    held = caches[0].lengths.clone()
+    layer.step(caches[0], x[1], seg)
+    for i, kw in ((2, dict(held=held)), (3, {})):
+        assert torch.equal(layer.step(caches[0], x[i], seg, **kw), layer.step(caches[1], x[i], seg))
+    assert torch.equal(caches[0].lengths, caches[1].lengths)
+    assert all(torch.equal(a, b) for a, b in zip(g.cache_read(caches[0], most), g.cache_read(caches[1], most)))

@@ -59,10 +59,13 @@ class _HeadNormRotary(torch.autograd.Function):
     def backward(ctx, dq, dk=None):
         q, k, q_gamma, k_gamma, positions, valid_len = ctx.saved_tensors
         sections, seg_len, base, interleaved, eps = ctx.args
+        wants = ctx.needs_input_grad[2:4]
         got = B.head_norm_rotary_bwd(dq.contiguous(), None if dk is None else dk.contiguous(), q, k, q_gamma, k_gamma, positions, sections, seg_len, valid_len, base,
-                                     interleaved, eps)
-        dq, dk, dq_gamma, dk_gamma = (got[0], None, got[1], None) if k is None else got
-        return dq, dk, None if q_gamma is None else dq_gamma, None if k_gamma is None else dk_gamma, None, None, None, None, None, None, None
+                                     interleaved, eps, want_params=any(wants))
+        got = got if isinstance(got, tuple) else (got,)
+        rows = 1 if k is None else 2
+        of = got[:rows] + (None,) * (2 - rows) + got[rows:] + (None,) * 2   # gradients of q, k and the weights that there are
+        return *of[:2], *(d if want else None for d, want in zip(of[2:4], wants)), None, None, None, None, None, None, None
 
 
 class _ScoredAttention(torch.autograd.Function):

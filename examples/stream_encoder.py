@@ -20,6 +20,11 @@ from paper_2505_01068_b200.training import ImEncoderLayer             # noqa: E4
 STEP, D, HEADS, KV_HEADS, SECTIONS, MOST = (1, 5, 3), 128, 4, 2, (8, 4, 4), (80, 400, 240)
 
 
+def further(worst, y, z):
+    """The larger of `worst` and the largest difference of two results; NaN once there was one."""
+    return torch.cat([worst.reshape(1), (y - z).abs().flatten()]).max()
+
+
 @torch.no_grad()
 def run(batch, steps, held_as):
     """(largest difference of a step's rows from attention over 16-bit rows of the same past, positions held, bytes of the cache, of 16-bit rows)."""
@@ -39,7 +44,7 @@ def run(batch, steps, held_as):
     with torch.cuda.graph(graph):
         y = layer.step(cache, x, STEP, valid, positions, times, ended, **rule)
     held = torch.zeros((batch, 3), dtype=torch.int32, device="cuda")
-    worst = 0.0
+    worst = torch.zeros((), device="cuda")
     for i in range(steps):
         x.normal_()
         ended.copy_((torch.rand(batch, device="cuda") < 0.02).int())
@@ -64,10 +69,10 @@ def run(batch, steps, held_as):
             newest[b[real], to[real]] = q[real]
             att = g.im_scored_attention_fwd(newest, k, v, MOST, held, q_len=STEP, times=when, **rule)
             z = layer.finish(x[real][None], att[b[real], to[real]][None], None, (int(real.sum()), 0, 0))
-            worst = max(worst, float((y[real] - z[0]).abs().max()))
+            worst = further(worst, y[real], z[0])
     used = int((cache.tables >= 0).sum())
     per = KV_HEADS * (g.CACHE_BLOCK * (D // HEADS) + 4) * 2
-    return worst, int(held.sum()), used * per, int(held.sum()) * 2 * KV_HEADS * (D // HEADS) * 2
+    return float(worst), int(held.sum()), used * per, int(held.sum()) * 2 * KV_HEADS * (D // HEADS) * 2
 
 
 def main(argv=None):

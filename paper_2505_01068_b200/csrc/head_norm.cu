@@ -10,10 +10,12 @@
 // registers.  The angles of a block are computed into a table of the warp's own, one (row, pair) a lane, and serve all heads; the rows of the block
 // after it are on their way into shared memory meanwhile.
 // Angles in turns are products of integers that lose their whole turns by themselves: position * (frequency * 2^64) mod 2^64, of which the upper 32 bits are
-// the phase, right for every position an int32 holds; then sincospi for float, and the special functions' sine and cosine for bf16 (2^-21 off, where a
-// result keeps 2^-9).
+// the phase, right for every position an int32 holds.  It is at most half a turn and rounded to float, 2^-26 of a turn or 2^-23.3 of the result next to the
+// rounding of float itself (with rsqrtf and sums in float a float result is 1.5e-7 off in all); then sincospi for float, and the special functions' sine and cosine
+// for bf16 (2^-21 off, where a result keeps 2^-9).
 // Measured, bf16, 8 + 8 heads of 64, 128 samples of (128, 1024, 1024), a quarter of them half padding: forward 1071 MB in 184 us, 5.8 TB/s, 0.89 of the measured
-// copy rate; backward 1573 MB in 299 us, 5.3 TB/s, 0.80; 8 + 4 heads, 64 samples, 403 MB in 78 us.  What bounds it then are issue slots (65 %).
+// copy rate; backward 1573 MB in 299 us, 5.3 TB/s, 0.80; one after the other as a training step calls them 485 to 547 by the box; 8 + 4 heads, 64 samples, 403 MB in 77 us.  What bounds it
+// then are issue slots (65 %).
 // The gradients of the weights: registers, lanes of a warp, warps of a CTA, CTAs, each in order, the last by a second small kernel.
 #include <math.h>
 
@@ -136,12 +138,25 @@ template <typename T> __device__ __forceinline__ void sine_cosine(int32_t positi
 // First row of segment s, and its length, without an index into the parameters.
 __device__ __forceinline__ int first_of(const Geometry& g, int s) { return s == 2 ? g.seg_off[2] : s == 1 ? g.seg_off[1] : 0; }
 __device__ __forceinline__ int length_of(const Geometry& g, int s) { return s == 2 ? g.seg_len[2] : s == 1 ? g.seg_len[1] : g.seg_len[0]; }
+// Whether pieces come through shared memory, the next block's while this one is worked on, or straight into registers when they are needed, which has them sooner
+// and takes fewer instructions for what narrow heads hold.  Measured, us forward and back, 8 + 8 heads, rows in samples of (128, 1024, 1024) a quarter of them padding:
+//   float   heads of 8, 64 x (50, 500, 500)    17.6 and 28.2 through shared memory    12.9 and 18.7 straight
+//           16, 64 x (128, 512, 512)           27.2     41.2                          25.8     41.8
+//           32, 64 samples                     92       111                           118      132
+//           64, 64 samples                     181      244                           201      253
+//           128, 32 samples                    180      239                           206      248
+//   bf16    64, 128 samples                    184      299                           216      394
+// (Pieces of 8 bytes, bf16 heads of 8, are narrower than a copy.)
+template <typename T> __host__ __device__ constexpr bool staged_pieces(int elements, int lanes) {
+  return elements * (int)sizeof(T) == 16 && (sizeof(T) == 2 || lanes >= 4);
+}
+
 template <typename T, int E, int LANES, bool ADJACENT, bool BWD>
 __global__ void __launch_bounds__(THREADS, 2)
 head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ HeadNormArgs a) {
   constexpr int HALF = E * LANES, HD = 2 * HALF, N = UNITS, H2 = E / 2, BYTES = E * (int)sizeof(T), PARTS = BWD ? 4 : 2, TABLE = ANGLES / E * PIECE_ANGLES<E>, W = BWD ? 1 : 2,   // W: tensors of a warp
                 STAGE = W * N * PARTS * 32 * BYTES;
-  constexpr bool STAGED = E == 8;
+  constexpr bool STAGED = staged_pieces<T>(E, LANES);
   static_assert(HALF <= ANGLES, "the angles of a row fit the table");
   __shared__ __align__(16) float s_table[WARPS][2][TABLE], s_gamma[W][HD];
   extern __shared__ __align__(16) uint8_t smem[];   // two stages of every warp's
@@ -237,9 +252,6 @@ head_norm_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Hea
   uint32_t real = 0;                         // bit r: row r of the block is a real one
   const int most = W == 1 ? own.heads : max(a.t[0].heads, a.t[1].heads);
   constexpr int CHUNK = 32 * N / LANES;
-  // Pieces of 16 bytes of bf16 come through shared memory, the next block's while this one is worked on; narrow pieces straight into registers, which has them
-  // sooner and takes fewer instructions for as little as they hold (64 x (50, 500, 500), 8 + 8 heads of 8, float: 13.9 us forward, 22.5 back, and 17.9 and 30.7
-  // through shared memory; 128 x (128, 1024, 1024), 8 + 8 of 64, bf16: 216 and 394, and 184 and 299).
   Piece<T, E> held[W][N][STAGED ? 1 : PARTS];
   auto load_now = [&](int chunk) {
     const int64_t row0 = (int64_t)block * block_rows;
@@ -609,7 +621,8 @@ cudaError_t launch_head_norm(const Geometry& g, int dtype, const HeadNormCall& c
   const dim3 grid((unsigned)ctas);
   if (wide) {
     const Kernel k = dtype == GSIT_BF16 ? wide_kernel<__nv_bfloat16>(g.hd, c.interleaved, c.backward) : wide_kernel<float>(g.hd, c.interleaved, c.backward);
-    const int bytes = piece == 8 ? WARPS * 2 * (c.backward ? 1 : 2) * UNITS * (c.backward ? 4 : 2) * 512 : 0;   // (see STAGED)
+    const bool staged = dtype == GSIT_BF16 ? staged_pieces<__nv_bfloat16>(piece, lanes) : staged_pieces<float>(piece, lanes);
+    const int bytes = staged ? WARPS * 2 * (c.backward ? 1 : 2) * UNITS * (c.backward ? 4 : 2) * 512 : 0;
     e = sm_count_and_smem_once(reinterpret_cast<const void*>(k), bytes, nullptr);
     if (e != cudaSuccess) return e;
     e = launch_overlapped(k, grid, dim3(THREADS), bytes, st, g, a);

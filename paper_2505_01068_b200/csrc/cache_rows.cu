@@ -4,7 +4,7 @@
 // the open block's buffer, the others from the call) are staged in shared memory, read from there in the order of the page -- pairs of features of
 // a position for keys, pairs of positions of a feature for values -- and stay in registers while the largest magnitude, the scale and the bytes are found,
 // so that everything is read once and a page's head is written as whole lines.  A block that stays open takes copies of the new rows.  Reading goes
-// the other way.  Bound by the bytes moved.
+// the other way, bound by the bytes moved; an append waits for its rows before it computes, and for issue slots then.
 //
 // x / scale is rounded once: the quotient in float is brought to the odd one of its two neighbours wherever a remainder is left (its sign
 // says on which side), so that the rounding to 8 bits that follows meets a tie only where there is one.

@@ -15,9 +15,9 @@
 // Who takes what: where the step is small, the CTAs of a cluster share a (stream, key head, tile of rows) and join their parts through distributed shared
 // memory; where there is much to read, two CTAs an SM share out all blocks of all streams and key heads evenly, whatever their lengths are, and
 // a second small kernel joins the parts of those that more than one of them had.  Always in order.
-// Measured, bf16: 32 streams of up to (128, 1024, 1024), 8 heads of 64, int8, every rule: 54 MB in 20 - 22 us (floor 8.3; 14 of the 19 that the kernel runs are the
-// walk, the others launch, first loads and join); 64 streams of up to (512, 10000, 10000), 8 heads on 2 key heads, e4m3: 253 MB in 70 us (floor 38.7;
-// the walk moves 6 TB/s, 273 instructions a block and 8 rows, 374 for 16; the ramp is 8 us, second pieces and the joining kernel 15).
+// Measured, bf16: 32 streams of up to (128, 1024, 1024), 8 heads of 64, int8, every rule: 54 MB in 20 - 23 us (floor 8.3; 14 of the 19 that the kernel runs
+// are the walk, the others launch, first loads and join); 64 streams of up to (512, 10000, 10000), 8 heads on 2 key heads, e4m3: 253 MB in 69 us (floor 38.7; the
+// walk moves 6 TB/s; the ramp is 8 us, second pieces and the joining kernel 15).  Instructions a block: 322 for 8 rows and 399 for 16 (e4m3), 416 and 494 (int8).
 // A closed pair's weight is 0 and the bytes it meets are numbers, so nothing of it counts; blocks whose scale is NaN take a way of their own.
 #pragma once
 #include <cooperative_groups.h>
@@ -181,7 +181,7 @@ template <int HD, int R> struct Part {
   float2 ml[R];
 };
 
-// CTAs of an SM: two where their registers allow it.  (Tiles of 32 rows, one CTA an SM, took 44 us where those of 16 take 34.)
+// CTAs of an SM: two where their registers allow it.  (Tiles of 32 rows, one CTA an SM, took 44 us where those of 16 took 34.)
 template <typename T, int NT> constexpr int RESIDENT = NT == 1 || sizeof(T) == 2 ? 2 : 1;
 
 // Weights, in base 2: the largest that f16 takes, and where the reference puts a new largest one.  Sums of rows take them in this unit, so that they stay in
@@ -893,7 +893,12 @@ inline int split_keys(const Geometry& g, const CachedArgs& a, int n_sm, int tile
 }
 // Even shares for all CTAs that fit the SMs, or a cluster for each (stream, key head): by what a warp has to walk where the tables are full, in
 // blocks.  Streams are of unlike lengths, so that clusters wait for the longest (a third more, where they lie between half and full); the second piece of
-// a share and the joining kernel cost as much as some 12 stages.
+// a share and the joining kernel cost as much as some 12 stages.  Both sides, us, heads of 64, full tables:          even    clusters
+//   64 streams, 8 heads on 2 key heads, (512, 10000, 10000) and (2000, 16000, 16000)                                  69, 93    71, 104
+//   one stream, 8 key heads, (8000, 64000, 64000), (4000, 32000, 32000), (1000, 8000, 8000)                           36, 32, 27    43, 31, 13
+//   8 and 32 streams, 8 key heads, (2000, 16000, 16000) and (500, 4000, 4000)                                         51, 49    42, 43
+// and of short streams in tables that are sixteen times as long: 32 of (128, 1024, 1024), 8 key heads, 29 and 16; one of them 26 and 8.  So the 12 is too few where there are
+// few rows, and tables say too much of streams that have just begun: the host knows no lengths, and a share of a few blocks costs what a long one does.
 template <int HD> bool even_shares(const Geometry& g, const CachedArgs& a, int tiles, int ctas, int split) {
   const int64_t pairs = (int64_t)g.batch * a.c.kv_heads, turns = pairs * 3 * a.c.blocks / (WARPS * Ring<HD>::B);
   return tiles == 1 && turns * 4 / (3 * std::min<int64_t>(pairs * split, ctas)) > turns / ctas + 12;
@@ -909,7 +914,7 @@ cudaError_t launch_tiles(const Geometry& g, CachedArgs& a, cudaStream_t st, size
   cudaError_t e = sm_count_and_smem_once(nullptr, 0, &n_sm);
   if (e != cudaSuccess) return e;
   // Tiles of rows: one where all fit in; of each segment's rows apart, so that a tile walks only what they see (16 streams of (4, 25, 30) rows, two to a key head,
-  // forward ring: 34 us, and 44 with mixed ones); across segments where all of them see the same (all blocks open: 84 us, and 85 apart).
+  // forward ring: 33 us, and 41 with mixed ones); across segments where all of them see the same (all blocks open: 76.5 us, and 78 apart).
   uint32_t sees = 0;
   a.mixed = true;
   for (int i = 0; i < 3; ++i)

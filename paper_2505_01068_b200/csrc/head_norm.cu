@@ -14,7 +14,7 @@
 // rounding of float itself (with rsqrtf and sums in float a float result is 1.5e-7 off in all); then sincospi for float, and the special functions' sine and cosine
 // for bf16 (2^-21 off, where a result keeps 2^-9).
 // Measured, bf16, 8 + 8 heads of 64, 128 samples of (128, 1024, 1024), a quarter of them half padding: forward 1071 MB in 184 us, 5.8 TB/s, 0.89 of the measured
-// copy rate; backward 1573 MB in 299 us, 5.3 TB/s, 0.80; one after the other as a training step calls them 485 to 547 by the box; 8 + 4 heads, 64 samples, 403 MB in 77 us.  What bounds it
+// copy rate; backward 1573 MB in 299 us, 5.3 TB/s, 0.80; one after the other as a training step calls them 485 to 547 from machine to machine; 8 + 4 heads, 64 samples, 403 MB in 77 us.  What bounds it
 // then are issue slots (65 %).
 // The gradients of the weights: registers, lanes of a warp, warps of a CTA, CTAs, each in order, the last by a second small kernel.
 #include <math.h>

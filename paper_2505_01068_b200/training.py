@@ -179,7 +179,8 @@ class ImEncoderLayer(torch.nn.Module):
         the cache and then attend to all that it holds.  positions int32 [axes, B, L] and times float32 [B, L] are those of these rows; ended int32 [B]:
         streams that begin anew; held int32 [B, 3]: the cache's lengths before a step that is taken again (of 32 rows a segment at most, or one that started from
         nothing); rule: phase, custom_mask, scale, softcap, slopes, causal.  Returns y [B, L, d], padded rows +0, and so are
-        those of segments that found no pages or no room in their tables (DEVFLAG_FULL in last_device_status).  Arguments that are refused leave the cache as it was."""
+        those of segments that found no pages or no room in their tables (DEVFLAG_FULL in last_device_status).  Arguments that are refused leave the cache as it was.
+        Made for a few rows a segment: a prompt of many is faster by project(), cache_plan, cache_append, im_scored_attention_fwd on its rows, and finish()."""
         q, k, v = self.project(x, valid_len, positions, seg_len)
         att, slots = S.cache_step(cache, q, k, v, seg_len, valid_len, ended, held, times=times, **rule)
         y = self.finish(x, att, valid_len, seg_len)

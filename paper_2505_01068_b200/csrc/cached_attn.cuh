@@ -66,6 +66,14 @@ __device__ __forceinline__ void mma_k8(float (&d)[4], uint32_t a0, uint32_t a1, 
   asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%8,%9,%10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
+__device__ __forceinline__ void add_to(float (&d)[4], const float (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    const float2 s = __fadd2_rn(make_float2(d[i], d[i + 1]), make_float2(v[i], v[i + 1]));
+    d[i] = s.x;
+    d[i + 1] = s.y;
+  }
+}
 __device__ __forceinline__ float reciprocal(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -365,7 +373,8 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
       float zero[4] = {0.f, 0.f, 0.f, 0.f};
       float s[2][NT][4];
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+      for (int m = 0; m < 2; ++m) {
+        float small[NT][4];                // float: the products with a smaller term
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -376,11 +385,24 @@ cached_attention_kernel(const __grid_constant__ Geometry g, const __grid_constan
             for (int n = 0; n < NT; ++n)
 #pragma unroll
               for (int y = 0; y < TERMS - w; ++y) {   // the product of the two smaller terms is left out: 2^-22 of the score's terms
-                float (&from)[4] = k + w + y > 0 ? s[m][n] : zero;
-                if constexpr (HD == 8) mma_k8(s[m][n], f[0], f[1], qf[n][y][k][0], from);
-                else mma(s[m][n], f, qf[n][y][k][0], qf[n][y][k][1], from);
+                auto product = [&](float (&to)[4], const float (&from)[4]) {
+                  if constexpr (HD == 8) mma_k8(to, f[0], f[1], qf[n][y][k][0], from);
+                  else mma(to, f, qf[n][y][k][0], qf[n][y][k][1], from);
+                };
+                if (TERMS == 1 || (k == 0 && w + y == 0)) product(s[m][n], k > 0 ? s[m][n] : zero);
+                else if (w + y > 0) product(small[n], k > 0 || w > 0 ? small[n] : zero);
+                else {   // the matrix instructions cut their sums off, always the same way: float adds them itself, rounded (0 - 3 % of a call's time)
+                  float add[4];
+                  product(add, zero);
+                  add_to(s[m][n], add);
+                }
               }
           }
+        if (TERMS == 2) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) add_to(s[m][n], small[n]);
+        }
+      }
       // scores in base 2, pairs of columns; positions 16 m + 8 h + gr
       float2 x[NT][2][2];
 #pragma unroll

@@ -85,3 +85,25 @@ def test_caps_of_any_size(g, t, cap):
     got = g.im_cached_attention_fwd(q, cache, seg, phase=g.PHASE_CUSTOM, custom_mask=0x1FF, softcap=cap, want_lse=True)
     want = ref.attention(q, seg, [seg], open_blocks(None, 0x1FF), hd ** -0.5, softcap=cap)
     _attention_close(got, want, t, cap)
+
+
+@pytest.mark.parametrize("held_as", ["int8", "e4m3"])
+@pytest.mark.parametrize("hd", [16, 32, 64])
+def test_large_scores_of_float_rows(g, held_as, hd):
+    """Queries and keys of one sign, so that nothing cancels and every sum is cut off the same way; log-sum-exps show the scores' errors."""
+    t, B, HK, H, seg = torch.float32, 16, 8, 24, (40, 64, 33)
+    for seed in range(2):
+        gen = torch.Generator().manual_seed(seed)
+        q, k, v = (_rows(gen, B, sum(seg), h, hd, t) for h in (H, HK, HK))
+        q, k = q.abs(), k.abs()
+        cache = g.stream_cache(B, seg, HK, hd, t, held_as)
+        g.cache_step(cache, q, k, v, seg)
+        _, lse = g.im_cached_attention_fwd(q, cache, seg, phase=g.PHASE_CUSTOM, custom_mask=0x1FF, want_lse=True)
+        for b in range(B):
+            K = torch.cat([bytes_of(cache, b, s, "k") for s in range(3)]).repeat_interleave(H // HK, dim=1)
+            x = torch.einsum("ihc,jhc->hij", q[b].double(), K) * hd ** -0.5
+            # A score, relative to itself: 2^-22 by the two terms of a query, 2^-22 by those of open keys, 2^-22 for products that are cut at 2^-23 twice (the
+            # terms inside and the sum), 2^-22 for four roundings to float of 2^-24.  Exponentials, sums and logarithm: 2^-20 in all.
+            room = 2.0 ** -20 * x.amax(dim=2) + 2.0 ** -20
+            off = (lse[b].double() - torch.logsumexp(x, dim=2)).abs()
+            assert bool((off <= room).all()), (seed, b, float((off / room).max()), float(x.max()))
